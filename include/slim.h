@@ -415,6 +415,44 @@ int slim_decode_layer(const slim_layer_shape* s, const slim_layer_weights* w, co
                       int n_slots, int n_prompt_tokens, void* k_response, void* v_response, int n_response,
                       void* x_out, void* q_out, void* workspace, size_t workspace_bytes, void* stream);
 
+/* ------------------------------------------------------------------------------------------------
+ * A Key-Value cache in 4 bits -- the pools of Section 4.3 with 17/64 of the bytes of bfloat16 to hold and to swap.  A prompt's Key (post-RoPE) and
+ * Value states are written block by block into slots, moved by slim_kv_swap as any payload, read by the decoded tokens' attention where they lie, and
+ * read back as rows, e.g. for a follow-up prompt.
+ *   A row of head_dim channels is cut into groups of 32.  A group holds an exponent e, the smallest for which its largest magnitude is below 7 * 2^e,
+ *   kept in [-125, 125], and per channel a code: bit 3 the sign, bits 0..2 the nearest of 0, 0.5, 1, 1.5, 2, 3, 4, 6 to |x| / 2^e (ties to the even code, 6 for
+ *   what is above).  What it stands for is exact in bfloat16 and float32.  A group that holds an infinity or a NaN reads back as NaN throughout.
+ *   A slot at byte slot * slot_bytes of its pool, at layer_offset, for blocks of `block` tokens (B) and Hkv heads of d:
+ *     the Keys' codes [Hkv, B, d/2] (byte i: channel 2 i in the low half, 2 i + 1 in the high), the Values' codes, the Keys' e + 127 [Hkv, B, d/32]
+ *     (255: NaN), the Values'.  slim_kv4_block_bytes gives its size, a multiple of 16 (0: sizes that are not covered).
+ *   slim_kv4_write:  rows k + t * ldk, v + t * ldv ([Hkv, d] of dtype, ld in elements) are tokens first_token + t of the prompt, t < n_tokens: a whole
+ *                    prompt, a chunk of it, or one token more.  Block b = token / block goes to slot slot_of_block[b] (int32 [n_blocks], device; NULL: slot b);
+ *                    a block whose slot is outside [0, n_slots) is left out.  Two blocks must not name the same slot.  The slots' other rows stay as they were.
+ *                    pool: device memory, or pinned device-mapped host memory (the CPU pool of slim_kv_swap, with NULL).
+ *   slim_kv4_read:   rows of the blocks listed in blocks[n_list] (int32, device, ascending; NULL: every block of the n_tokens prompt tokens) -> k_out, v_out: row
+ *                    i * block + r is token blocks[i] * block + r, so that the kept rows lie densely, as slim_compact_tokens leaves them (only the prompt's
+ *                    last block can be short).  k_out and v_out have room for n_rows rows; those behind are not written.  Rows of a block outside the prompt, or whose slot is outside [0, n_slots), stay as they were.
+ *   slim_decode_attn_kv4, slim_decode_layer_kv4:  slim_decode_attn and slim_decode_layer on such slots; arguments, response rows (of dtype) and workspaces are
+ *                    theirs, up to 16 query heads per kv head, softmax_scale not negative.  A token that sees no key gets zeros.
+ * head_dim 32, 64 or 128 (attention: 128); pools, layer_offset and slot_bytes multiples of 16, rows 16-byte aligned (ld a multiple of 8 bf16 or 4 f32 elements),
+ * block <= 2^24.  Errors: INVALID_ARG (null, sizes, ld < Hkv * head_dim, tokens behind n_blocks blocks, a slot too small), UNSUPPORTED, WORKSPACE_TOO_SMALL.
+ */
+size_t slim_kv4_block_bytes(int block, int n_kv_heads, int head_dim);
+int slim_kv4_write(const void* k, const void* v, int ldk, int ldv, int first_token, int n_tokens, int n_kv_heads, int head_dim, int block,
+                   int dtype, const int* slot_of_block, int n_blocks, void* pool, int n_slots, size_t slot_bytes, size_t layer_offset,
+                   void* stream);
+int slim_kv4_read(const void* pool, int n_slots, size_t slot_bytes, size_t layer_offset, const int* slot_of_block, const int* blocks,
+                  int n_list, int block, int n_tokens, int n_kv_heads, int head_dim, int dtype, void* k_out, void* v_out, int n_rows,
+                  int ldk, int ldv, void* stream);
+int slim_decode_attn_kv4(const void* q, const void* gpu_pool, size_t slot_bytes, size_t layer_offset, const int* block_of_slot, int n_slots,
+                         int block, int n_prompt_tokens, const void* k_response, const void* v_response, int n_response, int n_q_heads,
+                         int n_kv_heads, int head_dim, float softmax_scale, int dtype, void* out, void* workspace, size_t workspace_bytes,
+                         void* stream);
+int slim_decode_layer_kv4(const slim_layer_shape* s, const slim_layer_weights* w, const void* x_new, int position, const void* gpu_pool,
+                          size_t slot_bytes, size_t layer_offset, const int* block_of_slot, int n_slots, int n_prompt_tokens,
+                          void* k_response, void* v_response, int n_response, void* x_out, void* q_out, void* workspace,
+                          size_t workspace_bytes, void* stream);
+
 #ifdef __cplusplus
 }
 #endif

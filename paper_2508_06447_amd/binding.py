@@ -26,7 +26,7 @@ EXPORTS = (
     "slim_score_blocks_static",
     "slim_score_blocks_pooled", "slim_unit_keys", "slim_score_blocks_from_unit_keys",
     "slim_kv_swap_workspace_bytes", "slim_kv_swap", "slim_decode_attn_workspace_bytes", "slim_decode_attn", "slim_gemv", "slim_decode_layer_workspace_bytes",
-    "slim_decode_layer",
+    "slim_decode_layer", "slim_kv4_block_bytes", "slim_kv4_write", "slim_kv4_read", "slim_decode_attn_kv4", "slim_decode_layer_kv4",
     "slim_rope_table", "slim_window_query", "slim_window_query_from_rows_workspace_bytes", "slim_window_query_from_rows",
     "slim_linear_rope", "slim_score_blocks_from_token_scores",
     "slim_linear_pair", "slim_row_rstd", "slim_rmsnorm_linear", "slim_rmsnorm_swiglu_linear", "slim_fold_gain",
@@ -91,6 +91,12 @@ def load_library(path: str | None = None) -> C.CDLL:
     lib.slim_decode_layer_workspace_bytes.argtypes = [C.POINTER(LayerShape), i, i]
     lib.slim_decode_layer.argtypes = [C.POINTER(LayerShape), C.POINTER(LayerWeights), vp, i, vp, sz, sz, vp, i, i, vp, vp, i, vp, vp,
                                       vp, sz, vp]
+    lib.slim_decode_layer_kv4.argtypes = lib.slim_decode_layer.argtypes
+    lib.slim_kv4_block_bytes.restype = sz
+    lib.slim_kv4_block_bytes.argtypes = [i, i, i]
+    lib.slim_kv4_write.argtypes = [vp, vp, i, i, i, i, i, i, i, i, vp, i, vp, i, sz, sz, vp]
+    lib.slim_kv4_read.argtypes = [vp, i, sz, sz, vp, vp, i, i, i, i, i, i, vp, vp, i, i, i, vp]
+    lib.slim_decode_attn_kv4.argtypes = lib.slim_decode_attn.argtypes
     lib.slim_rope_table.argtypes = [vp, i, i, f, vp, vp]
     lib.slim_window_query.argtypes = [vp, i, i, i, i, i, vp, vp]
     lib.slim_window_query_from_rows_workspace_bytes.restype = sz
@@ -248,12 +254,8 @@ def slim_score_blocks_from_unit_keys(q_win: torch.Tensor, k_rep: torch.Tensor, n
     return scores
 
 
-def slim_decode_attn(q: torch.Tensor, gpu_pool: torch.Tensor, block_of_slot: torch.Tensor, block: int, n_prompt_tokens: int,
-                     n_kv_heads: int, k_response: torch.Tensor | None = None, v_response: torch.Tensor | None = None,
-                     layer_offset: int = 0, softmax_scale: float = 0.0, out: torch.Tensor | None = None,
-                     workspace: torch.Tensor | None = None) -> torch.Tensor:
-    """q[Hq,d] attends to the prompt tokens of the blocks in the slot pool and to the response tokens.
-    gpu_pool[n_slots, ...]: per slot K[block,Hkv,d] then V[block,Hkv,d] at byte layer_offset."""
+def _decode_attn(name: str, q, gpu_pool, block_of_slot, block, n_prompt_tokens, n_kv_heads, k_response, v_response, layer_offset, softmax_scale,
+                 out, workspace) -> torch.Tensor:
     lib = load_library()
     Hq, d = q.shape
     ns = block_of_slot.numel()
@@ -264,12 +266,30 @@ def slim_decode_attn(q: torch.Tensor, gpu_pool: torch.Tensor, block_of_slot: tor
     need = lib.slim_decode_attn_workspace_bytes(ns, n_resp, Hq)
     if workspace is None:
         workspace = torch.empty(max(need, 256), dtype=torch.uint8, device=q.device)
-    _check(lib.slim_decode_attn(_dev(q, "q"), _dev(gpu_pool, "gpu_pool"), slot_bytes, layer_offset,
-                                _dev(block_of_slot, "block_of_slot"), ns, block, n_prompt_tokens, _dev(k_response, "k_response"),
-                                _dev(v_response, "v_response"), n_resp, Hq, n_kv_heads, d, softmax_scale, _dtype_code(q),
-                                _dev(out, "out"), _dev(workspace, "workspace"), workspace.numel(), _stream()),
-           "slim_decode_attn")
+    _check(getattr(lib, name)(_dev(q, "q"), _dev(gpu_pool, "gpu_pool"), slot_bytes, layer_offset,
+                              _dev(block_of_slot, "block_of_slot"), ns, block, n_prompt_tokens, _dev(k_response, "k_response"),
+                              _dev(v_response, "v_response"), n_resp, Hq, n_kv_heads, d, softmax_scale, _dtype_code(q),
+                              _dev(out, "out"), _dev(workspace, "workspace"), workspace.numel(), _stream()), name)
     return out
+
+
+def slim_decode_attn(q: torch.Tensor, gpu_pool: torch.Tensor, block_of_slot: torch.Tensor, block: int, n_prompt_tokens: int,
+                     n_kv_heads: int, k_response: torch.Tensor | None = None, v_response: torch.Tensor | None = None,
+                     layer_offset: int = 0, softmax_scale: float = 0.0, out: torch.Tensor | None = None,
+                     workspace: torch.Tensor | None = None) -> torch.Tensor:
+    """q[Hq,d] attends to the prompt tokens of the blocks in the slot pool and to the response tokens.
+    gpu_pool[n_slots, ...]: per slot K[block,Hkv,d] then V[block,Hkv,d] at byte layer_offset."""
+    return _decode_attn("slim_decode_attn", q, gpu_pool, block_of_slot, block, n_prompt_tokens, n_kv_heads, k_response, v_response, layer_offset,
+                        softmax_scale, out, workspace)
+
+
+def slim_decode_attn_kv4(q: torch.Tensor, gpu_pool: torch.Tensor, block_of_slot: torch.Tensor, block: int, n_prompt_tokens: int,
+                         n_kv_heads: int, k_response: torch.Tensor | None = None, v_response: torch.Tensor | None = None,
+                         layer_offset: int = 0, softmax_scale: float = 0.0, out: torch.Tensor | None = None,
+                         workspace: torch.Tensor | None = None) -> torch.Tensor:
+    """slim_decode_attn on a pool of blocks in 4 bits (slim_kv4_write)."""
+    return _decode_attn("slim_decode_attn_kv4", q, gpu_pool, block_of_slot, block, n_prompt_tokens, n_kv_heads, k_response, v_response, layer_offset,
+                        softmax_scale, out, workspace)
 
 
 def slim_gemv(w: torch.Tensor, x: torch.Tensor, w_up: torch.Tensor | None = None, scale: torch.Tensor | None = None,
@@ -284,11 +304,9 @@ def slim_gemv(w: torch.Tensor, x: torch.Tensor, w_up: torch.Tensor | None = None
     return out
 
 
-def slim_decode_layer(shape: LayerShape, weights: dict, x_new: torch.Tensor, position: int, gpu_pool: torch.Tensor,
-                      block_of_slot: torch.Tensor, n_prompt_tokens: int, k_response: torch.Tensor, v_response: torch.Tensor,
-                      n_response: int, layer_offset: int = 0, workspace: torch.Tensor | None = None):
-    """One layer for one decoded token.  k_response/v_response[>= n_response+1, Hkv, d]: row n_response is written.
-    Returns (x_out[hidden], q[Hq, d])."""
+def _decode_layer(name: str, shape: LayerShape, weights: dict, x_new: torch.Tensor, position: int, gpu_pool: torch.Tensor,
+                  block_of_slot: torch.Tensor, n_prompt_tokens: int, k_response: torch.Tensor, v_response: torch.Tensor, n_response: int,
+                  layer_offset: int, workspace: torch.Tensor | None):
     lib = load_library()
     ns = block_of_slot.numel()
     slot_bytes = gpu_pool[0].numel() * gpu_pool.element_size() if ns else 0
@@ -298,12 +316,97 @@ def slim_decode_layer(shape: LayerShape, weights: dict, x_new: torch.Tensor, pos
     if workspace is None:
         workspace = torch.empty(max(need, 256), dtype=torch.uint8, device=x_new.device)
     wstruct = make_weights(weights)
-    _check(lib.slim_decode_layer(C.byref(shape), C.byref(wstruct), _dev(x_new, "x_new"), position, _dev(gpu_pool, "gpu_pool"),
-                                 slot_bytes, layer_offset, _dev(block_of_slot, "block_of_slot"), ns, n_prompt_tokens,
-                                 _dev(k_response, "k_response"), _dev(v_response, "v_response"), n_response,
-                                 _dev(x_out, "x_out"), _dev(q, "q"), _dev(workspace, "workspace"), workspace.numel(),
-                                 _stream()), "slim_decode_layer")
+    _check(getattr(lib, name)(C.byref(shape), C.byref(wstruct), _dev(x_new, "x_new"), position, _dev(gpu_pool, "gpu_pool"),
+                              slot_bytes, layer_offset, _dev(block_of_slot, "block_of_slot"), ns, n_prompt_tokens,
+                              _dev(k_response, "k_response"), _dev(v_response, "v_response"), n_response,
+                              _dev(x_out, "x_out"), _dev(q, "q"), _dev(workspace, "workspace"), workspace.numel(),
+                              _stream()), name)
     return x_out, q
+
+
+def slim_decode_layer(shape: LayerShape, weights: dict, x_new: torch.Tensor, position: int, gpu_pool: torch.Tensor,
+                      block_of_slot: torch.Tensor, n_prompt_tokens: int, k_response: torch.Tensor, v_response: torch.Tensor,
+                      n_response: int, layer_offset: int = 0, workspace: torch.Tensor | None = None):
+    """One layer for one decoded token.  k_response/v_response[>= n_response+1, Hkv, d]: row n_response is written.
+    Returns (x_out[hidden], q[Hq, d])."""
+    return _decode_layer("slim_decode_layer", shape, weights, x_new, position, gpu_pool, block_of_slot, n_prompt_tokens, k_response, v_response,
+                         n_response, layer_offset, workspace)
+
+
+def slim_decode_layer_kv4(shape: LayerShape, weights: dict, x_new: torch.Tensor, position: int, gpu_pool: torch.Tensor,
+                          block_of_slot: torch.Tensor, n_prompt_tokens: int, k_response: torch.Tensor, v_response: torch.Tensor,
+                          n_response: int, layer_offset: int = 0, workspace: torch.Tensor | None = None):
+    """slim_decode_layer on a pool of blocks in 4 bits (slim_kv4_write)."""
+    return _decode_layer("slim_decode_layer_kv4", shape, weights, x_new, position, gpu_pool, block_of_slot, n_prompt_tokens, k_response, v_response,
+                         n_response, layer_offset, workspace)
+
+
+def kv4_block_bytes(block: int, n_kv_heads: int, head_dim: int) -> int:
+    """Bytes of a block's Keys and Values in 4 bits (0: sizes that are not covered)."""
+    return load_library().slim_kv4_block_bytes(block, n_kv_heads, head_dim)
+
+
+def _rows(t: torch.Tensor, name: str):
+    """(address, row stride in elements) of rows [n, H, d] on the GPU; only the distance of the rows is free."""
+    if not t.is_cuda:
+        raise ValueError(f"{name} must be a GPU tensor")
+    n, H, d = t.shape
+    if (d > 1 and t.stride(2) != 1) or (H > 1 and t.stride(1) != d):
+        raise ValueError(f"{name} must have dense rows")
+    return t.data_ptr(), t.stride(0) if n > 1 else H * d
+
+
+def _slots(pool: torch.Tensor, host: bool = False):
+    """(address, slots, bytes of a slot) of pool[slots, ...]."""
+    at = _pinned(pool, "pool") if host and not pool.is_cuda else _dev(pool, "pool")
+    ns = pool.shape[0]
+    return at, ns, (pool.numel() // ns) * pool.element_size() if ns else 0
+
+
+def _index(t: torch.Tensor | None, name: str):
+    if t is not None and t.dtype != torch.int32:
+        raise TypeError(f"{name} must be int32")
+    return _dev(t, name)
+
+
+def slim_kv4_write(k: torch.Tensor, v: torch.Tensor, pool: torch.Tensor, block: int, slot_of_block: torch.Tensor | None = None,
+                   first_token: int = 0, layer_offset: int = 0) -> torch.Tensor:
+    """k, v[n, Hkv, d] (rows may be apart) = tokens first_token .. of the prompt -> their blocks' slots of pool[slots, ...] in 4 bits.
+    slot_of_block[n_blocks] int32, None: block b in slot b.  pool: on the GPU or pinned host memory.  Returns pool."""
+    lib = load_library()
+    n, Hkv, d = k.shape
+    if v.shape != k.shape or v.dtype != k.dtype:
+        raise ValueError("k and v must be alike")
+    (kp, ldk), (vp, ldv), (at, ns, size) = _rows(k, "k"), _rows(v, "v"), _slots(pool, host=True)
+    _check(lib.slim_kv4_write(kp, vp, ldk, ldv, first_token, n, Hkv, d, block, _dtype_code(k), _index(slot_of_block, "slot_of_block"),
+                              ns if slot_of_block is None else slot_of_block.numel(), at, ns, size, layer_offset, _stream()), "slim_kv4_write")
+    return pool
+
+
+def slim_kv4_read(pool: torch.Tensor, block: int, n_tokens: int, slot_of_block: torch.Tensor | None = None, blocks: torch.Tensor | None = None,
+                  k_out: torch.Tensor | None = None, v_out: torch.Tensor | None = None, n_kv_heads: int = 0, head_dim: int = 0,
+                  dtype: torch.dtype = torch.bfloat16, layer_offset: int = 0):
+    """Rows of the blocks listed in `blocks` (int32, ascending; None: all) of a prompt of n_tokens -> (k, v)[n', Hkv, d]; n' assumes the prompt's
+    last block among them, as slim_compact_tokens does.  Give k_out and v_out, whose first n' rows are filled, or n_kv_heads, head_dim and dtype."""
+    lib = load_library()
+    nb = n_blocks(n_tokens, block)
+    if slot_of_block is not None and slot_of_block.numel() < nb:
+        raise ValueError("slot_of_block is shorter than the prompt's blocks")
+    if (k_out is None) != (v_out is None):
+        raise ValueError("k_out and v_out go together")
+    if k_out is None:
+        rows = n_tokens if blocks is None else lib.slim_kept_tokens(n_tokens, block, blocks.numel())
+        k_out = torch.empty(rows, n_kv_heads, head_dim, dtype=dtype, device=pool.device)
+        v_out = torch.empty_like(k_out)
+    need = n_tokens if blocks is None else lib.slim_kept_tokens(n_tokens, block, blocks.numel())
+    if k_out.shape != v_out.shape or k_out.dtype != v_out.dtype or k_out.shape[0] < need:
+        raise ValueError("k_out and v_out must be alike and hold the rows")
+    _, Hkv, d = k_out.shape
+    (kp, ldk), (vp, ldv), (at, ns, size) = _rows(k_out, "k_out"), _rows(v_out, "v_out"), _slots(pool, host=True)
+    _check(lib.slim_kv4_read(at, ns, size, layer_offset, _index(slot_of_block, "slot_of_block"), _index(blocks, "blocks"),
+                             0 if blocks is None else blocks.numel(), block, n_tokens, Hkv, d, _dtype_code(k_out), kp, vp, k_out.shape[0], ldk, ldv, _stream()),
+           "slim_kv4_read")
+    return k_out, v_out
 
 
 def slim_rope_table(pos: torch.Tensor | None, n: int, head_dim: int, theta: float,

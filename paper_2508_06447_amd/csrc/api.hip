@@ -2,6 +2,7 @@
 // the pruned prefill layer.  No kernel lives here.
 #include "rows.h"
 #include "routes.h"
+#include "row_tile.h"
 #include <math.h>
 #include <algorithm>
 #include <mutex>
@@ -275,6 +276,76 @@ int slim_gemv(const void* w, const void* w_up, const void* x, const float* scale
     return launch_gemv(w, w_up, x, scale, -1.f, bias, residual, n_out, k_in, dtype, out, (hipStream_t)stream);
 }
 
+// ---- a cache in 4 bits (kv4.hip)
+static bool kv4_heads_ok(int n_kv_heads, int head_dim) { return (head_dim == 32 || head_dim == 64 || head_dim == 128) && n_kv_heads <= 65535; }
+// Whether bytes fit behind layer_offset of a slot.
+static bool slot_holds(size_t bytes, size_t layer_offset, size_t slot_bytes) { return layer_offset <= slot_bytes && bytes <= slot_bytes - layer_offset; }
+// Units of 32 keys and the bytes of a slot's rows are counted in 32 bits.
+constexpr int kKv4BlockMost = 1 << 24;
+static bool kv4_slots_ok(int n_slots, int block) { return block <= kKv4BlockMost && (long long)n_slots * ((block + kTileKeys - 1) / kTileKeys) < (1ll << 30); }
+
+size_t slim_kv4_block_bytes(int block, int n_kv_heads, int head_dim) {
+    if (block < 1 || block > kKv4BlockMost || n_kv_heads < 1 || head_dim < 1 || !kv4_heads_ok(n_kv_heads, head_dim)) return 0;
+    return align_up((size_t)block * n_kv_heads * (head_dim + head_dim / 16), 16);
+}
+
+// What the two calls below have in common.
+static int kv4_pool_checks(const void* pool, int n_slots, size_t slot_bytes, size_t layer_offset, int n_blocks, int block, int n_kv_heads, int head_dim, int dtype,
+                           const void* k, const void* v, int ldk, int ldv) {
+    if (!pool || !k || !v || n_slots < 1 || n_blocks < 1 || block < 1 || n_kv_heads < 1 || head_dim < 1 ||
+        (long long)n_kv_heads * head_dim > std::min(ldk, ldv))
+        return SLIM_INVALID_ARG;
+    if (!dtype_ok(dtype) || !kv4_heads_ok(n_kv_heads, head_dim) || block > kKv4BlockMost) return SLIM_UNSUPPORTED;
+    if (!slot_holds(slim_kv4_block_bytes(block, n_kv_heads, head_dim), layer_offset, slot_bytes)) return SLIM_INVALID_ARG;
+    const int vec = dtype == SLIM_BF16 ? 8 : 4;
+    if (slot_bytes % 16 != 0 || layer_offset % 16 != 0 || !aligned16(pool) || !aligned16(k) || !aligned16(v) || ldk % vec != 0 || ldv % vec != 0)
+        return SLIM_UNSUPPORTED;
+    return SLIM_OK;
+}
+
+int slim_kv4_write(const void* k, const void* v, int ldk, int ldv, int first_token, int n_tokens, int n_kv_heads, int head_dim, int block, int dtype,
+                   const int* slot_of_block, int n_blocks, void* pool, int n_slots, size_t slot_bytes, size_t layer_offset, void* stream) {
+    if (first_token < 0 || n_tokens < 1) return SLIM_INVALID_ARG;
+    const int rc = kv4_pool_checks(pool, n_slots, slot_bytes, layer_offset, n_blocks, block, n_kv_heads, head_dim, dtype, k, v, ldk, ldv);
+    if (rc) return rc;
+    const long long end = (long long)first_token + n_tokens;
+    if (end > (long long)n_blocks * block) return SLIM_INVALID_ARG;
+    if (end > (1ll << 31) - 65536) return SLIM_UNSUPPORTED;
+    return launch_kv4_write(k, v, ldk, ldv, first_token, n_tokens, n_kv_heads, head_dim, block, dtype, slot_of_block, n_blocks, pool, n_slots, slot_bytes, layer_offset,
+                            (hipStream_t)stream);
+}
+
+int slim_kv4_read(const void* pool, int n_slots, size_t slot_bytes, size_t layer_offset, const int* slot_of_block, const int* blocks, int n_list, int block, int n_tokens,
+                  int n_kv_heads, int head_dim, int dtype, void* k_out, void* v_out, int n_rows, int ldk, int ldv, void* stream) {
+    if (n_tokens < 1 || n_rows < 1 || (blocks && n_list < 1) || block < 1) return SLIM_INVALID_ARG;
+    const int nb = (int)(((long long)n_tokens + block - 1) / block);
+    const int rc = kv4_pool_checks(pool, n_slots, slot_bytes, layer_offset, nb, block, n_kv_heads, head_dim, dtype, k_out, v_out, ldk, ldv);
+    if (rc) return rc;
+    if (blocks && n_list > nb) return SLIM_INVALID_ARG;
+    if (n_tokens > (1ll << 31) - 65536) return SLIM_UNSUPPORTED;
+    return launch_kv4_read(pool, n_slots, slot_bytes, layer_offset, slot_of_block, blocks, blocks ? n_list : nb, nb, block, n_tokens, n_kv_heads, head_dim, dtype, k_out, v_out,
+                           n_rows, ldk, ldv, (hipStream_t)stream);
+}
+
+int slim_decode_attn_kv4(const void* q, const void* gpu_pool, size_t slot_bytes, size_t layer_offset, const int* block_of_slot, int n_slots, int block,
+                         int n_prompt_tokens, const void* k_response, const void* v_response, int n_response, int n_q_heads, int n_kv_heads, int head_dim,
+                         float softmax_scale, int dtype, void* out, void* workspace, size_t workspace_bytes, void* stream) {
+    if (!q || !out || !workspace || n_slots < 0 || n_response < 0 || n_slots + (long long)n_response < 1 || n_q_heads < 1 || n_kv_heads < 1 ||
+        n_q_heads % n_kv_heads != 0 || head_dim < 1 || !(softmax_scale >= 0.f) || (n_slots > 0 && (!gpu_pool || !block_of_slot || block < 1 || n_prompt_tokens < 1)) ||
+        (n_response > 0 && (!k_response || !v_response)))
+        return SLIM_INVALID_ARG;
+    if (!dtype_ok(dtype) || head_dim != 128 || n_q_heads / n_kv_heads > kTileRows || !kv4_heads_ok(n_kv_heads, head_dim)) return SLIM_UNSUPPORTED;
+    if (n_slots > 0 && (!kv4_slots_ok(n_slots, block) || (long long)n_prompt_tokens + block >= 1ll << 31)) return SLIM_UNSUPPORTED;
+    if (n_slots > 0 && !slot_holds(slim_kv4_block_bytes(block, n_kv_heads, head_dim), layer_offset, slot_bytes)) return SLIM_INVALID_ARG;
+    if (slot_bytes % 16 != 0 || layer_offset % 16 != 0 || !aligned16(q) || (n_slots > 0 && !aligned16(gpu_pool)) || ((uintptr_t)workspace & 255u) ||
+        (n_response > 0 && (!aligned16(k_response) || !aligned16(v_response))))
+        return SLIM_UNSUPPORTED;
+    if (workspace_bytes < slim_decode_attn_workspace_bytes(n_slots, n_response, n_q_heads)) return SLIM_WORKSPACE_TOO_SMALL;
+    if (softmax_scale == 0.f) softmax_scale = 1.0f / sqrtf((float)head_dim);
+    return launch_decode_attn_kv4(q, gpu_pool, slot_bytes, layer_offset, block_of_slot, n_slots, block, n_prompt_tokens, k_response, v_response, n_response, n_q_heads,
+                                  n_kv_heads, softmax_scale, dtype, out, (float*)workspace, (hipStream_t)stream);
+}
+
 // Workspace of slim_decode_layer: h | rstd | q | o | act | attention partials
 struct DecodePlan { size_t h, rstd, q, o, act, attn, total; };
 static DecodePlan plan_decode(const slim_layer_shape* s, int n_slots, int n_response) {
@@ -297,10 +368,11 @@ size_t slim_decode_layer_workspace_bytes(const slim_layer_shape* s, int n_slots,
     return plan_decode(s, n_slots, n_response).total;
 }
 
-int slim_decode_layer(const slim_layer_shape* s, const slim_layer_weights* w, const void* x_new, int position,
-                      const void* gpu_pool, size_t slot_bytes, size_t layer_offset, const int* block_of_slot, int n_slots,
-                      int n_prompt_tokens, void* k_response, void* v_response, int n_response, void* x_out, void* q_out,
-                      void* workspace, size_t workspace_bytes, void* stream) {
+// One decoded token's layer on a pool of blocks as the activations are (kv4 false) or in 4 bits.
+static int decode_layer(bool kv4, const slim_layer_shape* s, const slim_layer_weights* w, const void* x_new, int position,
+                        const void* gpu_pool, size_t slot_bytes, size_t layer_offset, const int* block_of_slot, int n_slots,
+                        int n_prompt_tokens, void* k_response, void* v_response, int n_response, void* x_out, void* q_out,
+                        void* workspace, size_t workspace_bytes, void* stream) {
     int rc = check_shape(s);
     if (rc) return rc;
     if (!w || !w->wq || !w->wk || !w->wv || !w->wo || !w->w_gate || !w->w_up || !w->w_down || !x_new || !x_out ||
@@ -310,12 +382,13 @@ int slim_decode_layer(const slim_layer_shape* s, const slim_layer_weights* w, co
     const int dt = s->dtype, Hd = s->hidden, Hq = s->n_q_heads, Hkv = s->n_kv_heads, d = s->head_dim;
     const int qd = Hq * d, kvd = Hkv * d, vec = dt == SLIM_BF16 ? 8 : 4;
     const size_t es = elem_size(dt);
-    if (d != 128 || Hq / Hkv > 8 || Hd % vec != 0 || s->ffn % vec != 0 || Hd > 16376 || s->ffn > 16376 || qd > 16376 ||
+    if (d != 128 || Hq / Hkv > (kv4 ? kTileRows : 8) || Hd % vec != 0 || s->ffn % vec != 0 || Hd > 16376 || s->ffn > 16376 || qd > 16376 ||
         !aligned16(x_new) || !aligned16(x_out) || !aligned16(k_response) || !aligned16(v_response) ||
         ((uintptr_t)workspace & 255u) || slot_bytes % 16 != 0 || layer_offset % 16 != 0 || (n_slots > 0 && !aligned16(gpu_pool)) ||
         (q_out && !aligned16(q_out)))
         return SLIM_UNSUPPORTED;
-    if (n_slots > 0 && layer_offset + 2 * (size_t)s->block * kvd * es > slot_bytes) return SLIM_INVALID_ARG;
+    if (n_slots > 0 && kv4 && (!kv4_slots_ok(n_slots, s->block) || (long long)n_prompt_tokens + s->block >= 1ll << 31)) return SLIM_UNSUPPORTED;
+    if (n_slots > 0 && !slot_holds(kv4 ? slim_kv4_block_bytes(s->block, Hkv, d) : 2 * (size_t)s->block * kvd * es, layer_offset, slot_bytes)) return SLIM_INVALID_ARG;
     const DecodePlan p = plan_decode(s, n_slots, n_response);
     if (workspace_bytes < p.total) return SLIM_WORKSPACE_TOO_SMALL;
     hipStream_t st = (hipStream_t)stream;
@@ -333,9 +406,9 @@ int slim_decode_layer(const slim_layer_shape* s, const slim_layer_weights* w, co
     SLIM_TRY(launch_gemv_qkv(w->wq, w->wk, w->wv, w->bq, w->bk, w->bv, a, eps, qd, kvd, Hd, position, s->rope_theta, dt, q,
                              k_new, v_new, st));
     // attention over the active blocks, the earlier response tokens and the token itself
-    SLIM_TRY(launch_decode_attn(q, gpu_pool, slot_bytes, layer_offset, block_of_slot, n_slots, s->block, n_prompt_tokens,
-                                k_response, v_response, n_response + 1, Hq, Hkv, 1.0f / sqrtf((float)d), dt, o,
-                                (float*)(ws + p.attn), st));
+    SLIM_TRY((kv4 ? launch_decode_attn_kv4 : launch_decode_attn)(q, gpu_pool, slot_bytes, layer_offset, block_of_slot, n_slots, s->block, n_prompt_tokens,
+                                                                 k_response, v_response, n_response + 1, Hq, Hkv, 1.0f / sqrtf((float)d), dt, o,
+                                                                 (float*)(ws + p.attn), st));
     // output projection + residual, FFN + residual
     SLIM_TRY(launch_gemv(w->wo, nullptr, o, nullptr, -1.f, nullptr, x_new, Hd, qd, dt, x_out, st));
     a = x_out;
@@ -345,6 +418,22 @@ int slim_decode_layer(const slim_layer_shape* s, const slim_layer_weights* w, co
     SLIM_TRY(launch_gemv(w->w_down, nullptr, act, nullptr, -1.f, nullptr, x_out, Hd, s->ffn, dt, x_out, st));
 #undef SLIM_TRY
     return SLIM_OK;
+}
+
+int slim_decode_layer(const slim_layer_shape* s, const slim_layer_weights* w, const void* x_new, int position,
+                      const void* gpu_pool, size_t slot_bytes, size_t layer_offset, const int* block_of_slot, int n_slots,
+                      int n_prompt_tokens, void* k_response, void* v_response, int n_response, void* x_out, void* q_out,
+                      void* workspace, size_t workspace_bytes, void* stream) {
+    return decode_layer(false, s, w, x_new, position, gpu_pool, slot_bytes, layer_offset, block_of_slot, n_slots, n_prompt_tokens, k_response, v_response, n_response,
+                        x_out, q_out, workspace, workspace_bytes, stream);
+}
+
+int slim_decode_layer_kv4(const slim_layer_shape* s, const slim_layer_weights* w, const void* x_new, int position,
+                          const void* gpu_pool, size_t slot_bytes, size_t layer_offset, const int* block_of_slot, int n_slots,
+                          int n_prompt_tokens, void* k_response, void* v_response, int n_response, void* x_out, void* q_out,
+                          void* workspace, size_t workspace_bytes, void* stream) {
+    return decode_layer(true, s, w, x_new, position, gpu_pool, slot_bytes, layer_offset, block_of_slot, n_slots, n_prompt_tokens, k_response, v_response, n_response,
+                        x_out, q_out, workspace, workspace_bytes, stream);
 }
 
 int slim_rope_table(const int* pos, int n, int head_dim, float theta, float* table, void* stream) {

@@ -7,7 +7,7 @@
 // kDecWgs / Hkv workgroups per kv head, each of which leaves a partial (max, sum, weighted values) for the query
 // heads of that kv head; a second kernel merges the partials.  Softmax is order-independent, so the slot order does
 // not matter.
-#include "slim_common.h"
+#include "row_tile.h"
 #include <algorithm>
 #include <type_traits>
 
@@ -21,15 +21,6 @@ constexpr int DPART = DD + 2;    // floats of a partial: values, max (base-2 dom
 // Value of lane H of the caller's row of 16 lanes.
 template <int H> __device__ __forceinline__ float row_lane(float v) {
     return __builtin_bit_cast(float, __builtin_amdgcn_update_dpp(0, __builtin_bit_cast(int, v), 0x150 + H, 0xf, 0xf, true));
-}
-// Maximum over the four lanes with the same lane % 16.
-__device__ __forceinline__ float max_over_rows(float v) {
-    const unsigned x = __builtin_bit_cast(unsigned, v);
-    const auto a = __builtin_amdgcn_permlane16_swap(x, x, false, false);
-    const float m = fmaxf(__builtin_bit_cast(float, a[0]), __builtin_bit_cast(float, a[1]));
-    const unsigned y = __builtin_bit_cast(unsigned, m);
-    const auto b = __builtin_amdgcn_permlane32_swap(y, y, false, false);
-    return fmaxf(__builtin_bit_cast(float, b[0]), __builtin_bit_cast(float, b[1]));
 }
 template <int G, int H = 0, typename F> __device__ __forceinline__ void for_heads(F f) {
     if constexpr (H < G) {

@@ -1,0 +1,405 @@
+// A Key-Value cache in 4 bits: blocks written into their slots and read back, and a decoded token's attention over the slots as they lie (Section 4.3's pools, with
+// 17/64 of the bytes to hold and to swap).
+//
+// A row is cut into groups of 32 channels.  A group has one power of two 2^e, e the smallest for which its largest magnitude stays below 7 * 2^e (so that rounding to
+// 6 * 2^e, the largest value, is off by no more than half the step that the format would have there), and a code per channel: sign and the nearest of 0, 0.5, 1, 1.5, 2, 3, 4, 6
+// times 2^e, ties to the even code.  The values are bfloat16 and float32 numbers exactly, and both directions are single instructions for two channels
+// (v_cvt_scalef32_pk_*), so what is read costs half an instruction per channel and no correction for a zero point.
+// e is kept in [-125, 125]: every value but zero is a normal number.  A group with an infinity or a NaN is stored as byte 255, which the instruction that reads makes NaN.
+//
+// Layout of a slot (block B, H kv heads, heads of d): Keys' codes [H, B, d / 2], Values' codes, Keys' e + 127 [H, B, d / 32], Values' -- a kv head's rows lie together, as the
+// attention reads them.
+#include "row_tile.h"
+#include <algorithm>
+
+namespace slim {
+
+typedef __bf16 bf16x2_t __attribute__((ext_vector_type(2)));
+
+// What lies where in a slot, for one kv head.
+struct Kv4Head {
+    size_t k, v, ks, vs;
+    __device__ __forceinline__ Kv4Head(int g, int block, int Hkv, int d) {
+        const size_t rows = (size_t)Hkv * block, at = (size_t)g * block;
+        k = at * (d / 2);
+        v = (rows + at) * (d / 2);
+        ks = rows * d + at * (d / 32);
+        vs = rows * d + (rows + at) * (d / 32);
+    }
+};
+
+// Eight channels (four bytes of codes) as bfloat16; scale: 2^e.
+__device__ __forceinline__ bf16x8 kv4_to_bf16(uint32_t c, float scale) {
+    const bf16x2_t a = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(c, scale, 0), b = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(c, scale, 1);
+    const bf16x2_t d = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(c, scale, 2), e = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(c, scale, 3);
+    return bf16x8{a[0], a[1], b[0], b[1], d[0], d[1], e[0], e[1]};
+}
+__device__ __forceinline__ float kv4_scale(uint32_t byte) { return __builtin_bit_cast(float, byte << 23); }
+
+// ---- written and read back
+// A wave takes 64 / (D / 8) rows of one kv head, Keys or Values, at a time, 8 channels a lane (four lanes a group), kSteps times in a row: what it reads is whole rows, what it writes
+// lies together.
+constexpr int kSteps = 4;
+struct Kv4Rows {
+    const unsigned char* pool;
+    size_t slot_bytes, layer_offset;
+    const int* slot_of_block;                            // null: block b lies in slot b
+    const int* blocks;                                   // read: list of blocks, null: 0, 1, ..
+    int n_slots, n_blocks, block, Hkv, first, n;         // first, n: written: tokens first .. first + n - 1; read: n = prompt tokens
+    int list, n_rows;                                    // read: entries of the list, rows that the output has room for
+    int ldk, ldv;
+};
+
+template <typename T, int D>
+__global__ void __launch_bounds__(256) kv4_write_kernel(const T* __restrict__ K, const T* __restrict__ V, Kv4Rows a) {
+    constexpr int PC = D / 8, RPW = 64 / PC;             // lanes a row, rows a step
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, piece = lane % PC;
+    const bool value = blockIdx.z;
+    const int g = blockIdx.y;
+    const int i0 = (blockIdx.x * 4 + wave) * (RPW * kSteps) + lane / PC;
+    const T* src = value ? V + (size_t)g * D : K + (size_t)g * D;
+    const size_t ld = value ? a.ldv : a.ldk;
+    const Kv4Head at(g, a.block, a.Hkv, D);
+    float f[kSteps][8];
+#pragma unroll
+    for (int s = 0; s < kSteps; ++s) {
+        const T* p = src + (size_t)min(i0 + s * RPW, a.n - 1) * ld + piece * 8;
+        Elem<T>::unpack(*reinterpret_cast<const uint4*>(p), f[s]);
+        if constexpr (sizeof(T) == 4) Elem<T>::unpack(*reinterpret_cast<const uint4*>(p + 4), f[s] + 4);
+    }
+    int b = (a.first + i0) / a.block, r = a.first + i0 - b * a.block;
+#pragma unroll
+    for (int s = 0; s < kSteps; ++s) {
+        uint32_t mx = 0;                                 // magnitudes compare as whole numbers, NaN above infinity
+#pragma unroll
+        for (int i = 0; i < 8; ++i) mx = max(mx, __builtin_bit_cast(uint32_t, f[s][i]) & 0x7fffffffu);
+        mx = max(mx, (uint32_t)__shfl_xor((int)mx, 1, 64));
+        mx = max(mx, (uint32_t)__shfl_xor((int)mx, 2, 64));
+        // + a quarter of a mantissa: from 1.75 times a power of two on the next power counts
+        const int byte = mx >= 0x7f800000u ? 255 : min(max((int)((mx + (1u << 21)) >> 23) - 2, 2), 252);
+        const float scale = kv4_scale(byte);
+        uint32_t code = 0;
+        code = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(code, f[s][0], f[s][1], scale, 0);
+        code = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(code, f[s][2], f[s][3], scale, 1);
+        code = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(code, f[s][4], f[s][5], scale, 2);
+        code = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(code, f[s][6], f[s][7], scale, 3);
+        if (byte == 255) code = 0;
+        if (i0 + s * RPW < a.n) {
+            const int slot = a.slot_of_block ? a.slot_of_block[b] : b;
+            if (slot >= 0 && slot < a.n_slots) {
+                unsigned char* dst = const_cast<unsigned char*>(a.pool) + (size_t)slot * a.slot_bytes + a.layer_offset;
+                *reinterpret_cast<uint32_t*>(dst + (value ? at.v : at.k) + (size_t)r * (D / 2) + piece * 4) = code;
+                if (piece % 4 == 0) dst[(value ? at.vs : at.ks) + (size_t)r * (D / 32) + piece / 4] = (unsigned char)byte;
+            }
+        }
+        r += RPW;
+        while (r >= a.block) { r -= a.block; ++b; }
+    }
+}
+
+template <typename T, int D>
+__global__ void __launch_bounds__(256) kv4_read_kernel(T* __restrict__ K, T* __restrict__ V, Kv4Rows a) {
+    constexpr int PC = D / 8, RPW = 64 / PC;
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, piece = lane % PC;
+    const bool value = blockIdx.z;
+    const int g = blockIdx.y;
+    const long long o0 = ((long long)blockIdx.x * 4 + wave) * (RPW * kSteps) + lane / PC;   // row of the output
+    T* out = value ? V + (size_t)g * D : K + (size_t)g * D;
+    const size_t ld = value ? a.ldv : a.ldk;
+    const Kv4Head at(g, a.block, a.Hkv, D);
+    int i = (int)(o0 / a.block), r = (int)(o0 - (long long)i * a.block);
+    uint32_t code[kSteps], byte[kSteps];
+    bool have[kSteps];
+#pragma unroll
+    for (int s = 0; s < kSteps; ++s) {
+        have[s] = false;
+        if (i < a.list && o0 + s * RPW < a.n_rows) {
+            const int b = a.blocks ? a.blocks[i] : i;
+            if (b >= 0 && b < a.n_blocks && (long long)b * a.block + r < a.n) {
+                const int slot = a.slot_of_block ? a.slot_of_block[b] : b;
+                if (slot >= 0 && slot < a.n_slots) {
+                    const unsigned char* src = a.pool + (size_t)slot * a.slot_bytes + a.layer_offset;
+                    code[s] = *reinterpret_cast<const uint32_t*>(src + (value ? at.v : at.k) + (size_t)r * (D / 2) + piece * 4);
+                    byte[s] = src[(value ? at.vs : at.ks) + (size_t)r * (D / 32) + piece / 4];
+                    have[s] = true;
+                }
+            }
+        }
+        r += RPW;
+        while (r >= a.block) { r -= a.block; ++i; }
+    }
+#pragma unroll
+    for (int s = 0; s < kSteps; ++s) {
+        if (!have[s]) continue;
+        const uint4 v = __builtin_bit_cast(uint4, kv4_to_bf16(code[s], kv4_scale(byte[s])));
+        T* dst = out + (size_t)(o0 + s * RPW) * ld + piece * 8;
+        if constexpr (sizeof(T) == 2) {
+            *reinterpret_cast<uint4*>(dst) = v;
+        } else {
+            float f[8];
+            Elem<bf16_t>::unpack(v, f);
+            *reinterpret_cast<uint4*>(dst) = Elem<float>::pack(f);
+            *reinterpret_cast<uint4*>(dst + 4) = Elem<float>::pack(f + 4);
+        }
+    }
+}
+
+int launch_kv4_write(const void* k, const void* v, int ldk, int ldv, int first, int n, int Hkv, int d, int block, int dtype, const int* slot_of_block, int n_blocks,
+                     void* pool, int n_slots, size_t slot_bytes, size_t layer_offset, hipStream_t st) {
+    const Kv4Rows a{(const unsigned char*)pool, slot_bytes, layer_offset, slot_of_block, nullptr, n_slots, n_blocks, block, Hkv, first, n, 0, 0, ldk, ldv};
+    const int per_wg = 4 * kSteps * 512 / d;
+    const dim3 grid((n + per_wg - 1) / per_wg, Hkv, 2);
+#define SLIM_KV4(T, D) hipLaunchKernelGGL((kv4_write_kernel<T, D>), grid, dim3(256), 0, st, (const T*)k, (const T*)v, a)
+#define SLIM_KV4_D(T) do { if (d == 32) SLIM_KV4(T, 32); else if (d == 64) SLIM_KV4(T, 64); else SLIM_KV4(T, 128); } while (0)
+    if (dtype == SLIM_BF16) SLIM_KV4_D(bf16_t); else SLIM_KV4_D(float);
+#undef SLIM_KV4
+    return check_launch();
+}
+
+int launch_kv4_read(const void* pool, int n_slots, size_t slot_bytes, size_t layer_offset, const int* slot_of_block, const int* blocks, int list, int n_blocks, int block,
+                    int n_tokens, int Hkv, int d, int dtype, void* k, void* v, int n_rows, int ldk, int ldv, hipStream_t st) {
+    const Kv4Rows a{(const unsigned char*)pool, slot_bytes, layer_offset, slot_of_block, blocks, n_slots, n_blocks, block, Hkv, 0, n_tokens, list, n_rows, ldk, ldv};
+    const int per_wg = 4 * kSteps * 512 / d;
+    const long long rows = std::min<long long>(n_rows, blocks ? (long long)list * block : n_tokens);
+    const dim3 grid((unsigned)((rows + per_wg - 1) / per_wg), Hkv, 2);
+#define SLIM_KV4(T, D) hipLaunchKernelGGL((kv4_read_kernel<T, D>), grid, dim3(256), 0, st, (T*)k, (T*)v, a)
+    if (dtype == SLIM_BF16) SLIM_KV4_D(bf16_t); else SLIM_KV4_D(float);
+#undef SLIM_KV4
+#undef SLIM_KV4_D
+    return check_launch();
+}
+
+// ---- attention of one decoded token
+// The units of 32 keys of the slots and of the response are dealt to the waves of gridDim.x workgroups per kv head; each workgroup leaves a partial result of the kv head's query
+// heads, or, alone, the output.  The registers of a unit's codes are requested anew as soon as they are used; the slot of the unit after that is looked up meanwhile.
+constexpr int kQ4D = 128;
+constexpr int kQ4Waves = 4;
+template <typename T>
+__global__ void __launch_bounds__(64 * kQ4Waves) decode_attn_kv4_kernel(
+    const T* __restrict__ q, const unsigned char* __restrict__ pool, size_t slot_bytes, size_t layer_offset, const int* __restrict__ block_of_slot, int n_slots, int block,
+    int n_prompt, const T* __restrict__ k_resp, const T* __restrict__ v_resp, int n_resp, int Hq, int Hkv, float scale_log2e, float* __restrict__ part, T* __restrict__ out) {
+    constexpr int D = kQ4D;
+    typedef RowTile<T, D> Tile;
+    constexpr int NT = Tile::NT, NP = Tile::NP;
+    extern __shared__ __align__(16) unsigned char lds[];
+    __shared__ float ws_m[kQ4Waves][kTileRows], ws_l[kQ4Waves][kTileRows];
+    const int g = blockIdx.y, lane = threadIdx.x & 63, l16 = lane & 15, qr = lane >> 4, G = Hq / Hkv;
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const unsigned tile = (unsigned)(uintptr_t)lds + wave * Tile::kLdsBytes;
+    const int nb = (n_prompt + block - 1) / block, per_slot = (block + kTileKeys - 1) / kTileKeys;
+    const int n_in_slots = n_slots * per_slot, n_units = n_in_slots + (n_resp + kTileKeys - 1) / kTileKeys, step = gridDim.x * kQ4Waves;
+    const Kv4Head head(g, block, Hkv, D);
+
+    int ui = (int)blockIdx.x * kQ4Waves + wave, rows = 0, c0 = 0;
+    const unsigned char* base = nullptr;                 // of the unit's slot
+    auto find = [&]() {                                  // the next unit in a slot that holds keys; false: none is left
+        for (; ui < n_in_slots; ui += step) {
+            const int slot = ui / per_slot, c = (ui - slot * per_slot) * kTileKeys, b = block_of_slot[slot];
+            if (b < 0 || b >= nb) continue;
+            const int r = min(kTileKeys, min(block, n_prompt - b * block) - c);
+            if (r <= 0) continue;
+            rows = r;
+            c0 = c;
+            base = pool + (size_t)slot * slot_bytes + layer_offset;
+            return true;
+        }
+        return false;
+    };
+    uint4 kx[2], vx[2];
+    uint32_t ks[2], vs[2];
+    // rows behind the last key repeat it: their weight is 0
+    auto load_k = [&]() {
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+            const unsigned r = c0 + min(l16 + 16 * h, rows - 1);
+            kx[h] = load_stream16(base + head.k + r * (D / 2) + qr * 16);
+            ks[h] = base[head.ks + r * (D / 32) + qr];
+        }
+    };
+    auto load_v = [&]() {
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+            const unsigned r = c0 + min(l16 + 16 * h, rows - 1);
+            vx[h] = load_stream16(base + head.v + r * (D / 2) + qr * 16);
+            vs[h] = base[head.vs + r * (D / 32) + qr];
+        }
+    };
+    bool more = find();
+    if (more) { load_k(); load_v(); }
+    Tile t;
+    t.begin(q + (size_t)(g * G + min(l16, G - 1)) * D);
+    float w[8];
+    bf16x8 p[NP];
+    auto masked = [&](f32x4* s, int have) {
+#pragma unroll
+        for (int h = 0; h < 2; ++h)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) s[h][e] = h * 16 + qr * 4 + e < have ? s[h][e] * scale_log2e : -INFINITY;
+    };
+    while (more) {
+        const int have = rows;
+        ui += step;
+        more = find();                                   // none left: the last unit is requested once more, and not used
+        f32x4 s[2] = {{0.f, 0.f, 0.f, 0.f}, {0.f, 0.f, 0.f, 0.f}};
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+            const uint32_t c[4] = {kx[h].x, kx[h].y, kx[h].z, kx[h].w};
+            const float sc = kv4_scale(ks[h]);
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                const bf16x8 k = kv4_to_bf16(c[j], sc);
+                t.template add_scores<1>(&k, j, s[h]);
+            }
+        }
+        load_k();
+        masked(s, have);
+        t.weigh(s, w);
+        bf16_terms<NP>(w, p);
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+            const uint32_t c[4] = {vx[h].x, vx[h].y, vx[h].z, vx[h].w};
+            const float sc = kv4_scale(vs[h]);
+#pragma unroll
+            for (int j = 0; j < 4; ++j) *(LdsB128)(tile + Tile::v_piece(l16 + 16 * h, qr * 4 + j)) = kv4_to_bf16(c[j], sc);
+        }
+        load_v();
+        t.template add_values<1>(p, 0, tile);
+    }
+    // response tokens: dense rows of T
+    const size_t row_stride = (size_t)Hkv * D;
+    for (; ui < n_units; ui += step) {
+        const int first = (ui - n_in_slots) * kTileKeys, have = min(kTileKeys, n_resp - first);
+        f32x4 s[2] = {{0.f, 0.f, 0.f, 0.f}, {0.f, 0.f, 0.f, 0.f}};
+        size_t at[2];
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+            at[h] = (size_t)(first + min(l16 + 16 * h, have - 1)) * row_stride + (size_t)g * D + qr * 32;
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                bf16x8 k[NT];
+                row_terms<T, NT>(k_resp + at[h] + j * 8, k);
+                t.template add_scores<NT>(k, j, s[h]);
+            }
+        }
+        masked(s, have);
+        t.weigh(s, w);
+        bf16_terms<NP>(w, p);
+        bf16x8 v[2][4][NT];
+#pragma unroll
+        for (int h = 0; h < 2; ++h)
+#pragma unroll
+            for (int j = 0; j < 4; ++j) row_terms<T, NT>(v_resp + at[h] + j * 8, v[h][j]);
+#pragma unroll
+        for (int a = 0; a < NT; ++a) {
+#pragma unroll
+            for (int h = 0; h < 2; ++h)
+#pragma unroll
+                for (int j = 0; j < 4; ++j) *(LdsB128)(tile + Tile::v_piece(l16 + 16 * h, qr * 4 + j)) = v[h][j][a];
+            t.template add_values<NT>(p, a, tile);
+        }
+    }
+    // ---- the waves' results are merged
+    t.finish_sum();
+    if (lane < kTileRows) { ws_m[wave][lane] = t.m; ws_l[wave][lane] = t.l; }
+    // O in place of the wave's V tile: row l16 of 128 floats, its 16-byte pieces turned by the row
+    float* mine = reinterpret_cast<float*>(lds + wave * Tile::kLdsBytes);
+#pragma unroll
+    for (int dt = 0; dt < Tile::DT; ++dt)
+        *reinterpret_cast<f32x4*>(mine + l16 * D + (((dt * 4 + qr) ^ l16) << 2)) = t.o[dt];
+    __syncthreads();
+    for (int i = threadIdx.x; i < G * D; i += 64 * kQ4Waves) {
+        const int h = i / D, dd = i - h * D;
+        float M = -INFINITY, acc = 0.f, l = 0.f;
+#pragma unroll
+        for (int x = 0; x < kQ4Waves; ++x) M = fmaxf(M, ws_m[x][h]);
+#pragma unroll
+        for (int x = 0; x < kQ4Waves; ++x) {
+            const float lx = ws_l[x][h], sc = lx == 0.f ? 0.f : __builtin_amdgcn_exp2f(ws_m[x][h] - M);
+            acc += sc * reinterpret_cast<const float*>(lds + x * Tile::kLdsBytes)[h * D + (((dd >> 2) ^ h) << 2) + (dd & 3)];
+            l += sc * lx;
+        }
+        const int row = g * G + h;
+        if (gridDim.x == 1) {
+            Elem<T>::st(out + (size_t)row * D + dd, l == 0.f ? 0.f : acc / l);
+        } else {
+            float* dst = part + ((size_t)blockIdx.x * Hq + row) * (D + 2);
+            dst[dd] = acc;
+            if (dd == 0) { dst[D] = M; dst[D + 1] = l; }
+        }
+    }
+}
+
+// 1024 threads a row: 1024 / D groups of D channels, group j the partials j, j + groups, ..; everything is requested at once.
+template <typename T, int D>
+__global__ void __launch_bounds__(1024) merge_rows_kernel(const float* __restrict__ part, int n_parts, int rows, T* __restrict__ out) {
+    constexpr int NG = 1024 / D, PER = kMergeParts / NG;
+    __shared__ float wts[kMergeParts], wred[2][kMergeParts / 64], accs[NG][D];
+    const int row = blockIdx.x, tid = threadIdx.x, grp = tid / D, dd = tid % D;
+    auto item = [&](int i) { return part + ((size_t)min(i, n_parts - 1) * rows + row) * (D + 2); };
+    float val[PER];
+#pragma unroll
+    for (int i = 0; i < PER; ++i) val[i] = grp + i * NG < n_parts ? item(grp + i * NG)[dd] : 0.f;
+    float m = -INFINITY, l = 0.f;
+    if (tid < kMergeParts) {
+        if (tid < n_parts) { m = item(tid)[D]; l = item(tid)[D + 1]; }
+        const float wm = wave_max(m);
+        if ((tid & 63) == 0) wred[0][tid >> 6] = wm;
+    }
+    __syncthreads();
+    const float M = fmaxf(wred[0][0], wred[0][1]);
+    if (tid < kMergeParts) {
+        const float w = l == 0.f ? 0.f : __builtin_amdgcn_exp2f(m - M);      // a partial without keys has no weight
+        wts[tid] = w;
+        const float ws = wave_sum(w * l);
+        if ((tid & 63) == 0) wred[1][tid >> 6] = ws;
+    }
+    __syncthreads();
+    float acc = 0.f;
+#pragma unroll
+    for (int i = 0; i < PER; ++i) acc += grp + i * NG < n_parts ? wts[grp + i * NG] * val[i] : 0.f;
+    accs[grp][dd] = acc;
+    __syncthreads();
+    if (grp == 0) {
+        float a = 0.f;
+#pragma unroll
+        for (int i = 0; i < NG; ++i) a += accs[i][dd];
+        const float sum = wred[1][0] + wred[1][1];
+        Elem<T>::st(out + (size_t)row * D + dd, sum == 0.f ? 0.f : a / sum);
+    }
+}
+
+int launch_merge_rows(const float* part, int n_parts, int rows, int d, int dtype, void* out, hipStream_t st) {
+#define SLIM_MERGE(T, D) hipLaunchKernelGGL((merge_rows_kernel<T, D>), dim3(rows), dim3(1024), 0, st, part, n_parts, rows, (T*)out)
+    if (dtype == SLIM_BF16) SLIM_MERGE(bf16_t, 128);
+    else if (d == 32) SLIM_MERGE(float, 32);
+    else if (d == 64) SLIM_MERGE(float, 64);
+    else SLIM_MERGE(float, 128);
+#undef SLIM_MERGE
+    return check_launch();
+}
+
+// Workgroups per kv head: about kQ4Wgs in all, every wave the same number of units where that can be, no more than the caller's workspace has room for (one partial per
+// slot and per 64 response tokens).
+constexpr int kQ4Wgs = 512;
+static int kv4_parts(int n_slots, int block, int n_resp, int Hkv) {
+    const long long units = (long long)n_slots * ((block + kTileKeys - 1) / kTileKeys) + (n_resp + kTileKeys - 1) / kTileKeys;
+    const long long most = std::min<long long>(std::max(16, std::min(kMergeParts, kQ4Wgs / Hkv)), (long long)n_slots + (n_resp + 63) / 64);
+    const long long rounds = std::max<long long>(1, (units + kQ4Waves * most - 1) / (kQ4Waves * most));
+    return (int)std::max<long long>(1, std::min(most, (units + kQ4Waves * rounds - 1) / (kQ4Waves * rounds)));
+}
+
+int launch_decode_attn_kv4(const void* q, const void* pool, size_t slot_bytes, size_t layer_offset, const int* block_of_slot, int n_slots, int block, int n_prompt,
+                           const void* k_resp, const void* v_resp, int n_resp, int Hq, int Hkv, float scale, int dtype, void* out, float* part, hipStream_t st) {
+    const float sl = scale * 1.4426950408889634f;
+    const int parts = kv4_parts(n_slots, n_slots ? block : 1, n_resp, Hkv);
+    const size_t smem = (size_t)kQ4Waves * RowTile<bf16_t, kQ4D>::kLdsBytes;
+#define SLIM_Q4(T) hipLaunchKernelGGL(decode_attn_kv4_kernel<T>, dim3(parts, Hkv), dim3(64 * kQ4Waves), smem, st, (const T*)q, (const unsigned char*)pool, slot_bytes, layer_offset, \
+                                      block_of_slot, n_slots, n_slots ? block : 1, n_prompt, (const T*)k_resp, (const T*)v_resp, n_resp, Hq, Hkv, sl, part, (T*)out)
+    if (dtype == SLIM_BF16) SLIM_Q4(bf16_t); else SLIM_Q4(float);
+#undef SLIM_Q4
+    if (parts == 1) return check_launch();
+    const int rc = check_launch();
+    return rc ? rc : launch_merge_rows(part, parts, Hq, kQ4D, dtype, out, st);
+}
+
+}  // namespace slim

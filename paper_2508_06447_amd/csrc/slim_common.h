@@ -158,6 +158,13 @@ int launch_compact_multi(int n_arrays, const void* const* src, void* const* dst,
 int launch_decode_attn(const void* q, const void* pool, size_t slot_bytes, size_t layer_offset, const int* block_of_slot,
                        int n_slots, int block, int n_prompt, const void* k_resp, const void* v_resp, int n_resp, int Hq,
                        int Hkv, float scale, int dtype, void* out, float* part, hipStream_t st);
+int launch_kv4_write(const void* k, const void* v, int ldk, int ldv, int first, int n, int Hkv, int d, int block, int dtype, const int* slot_of_block, int n_blocks,
+                     void* pool, int n_slots, size_t slot_bytes, size_t layer_offset, hipStream_t st);
+int launch_kv4_read(const void* pool, int n_slots, size_t slot_bytes, size_t layer_offset, const int* slot_of_block, const int* blocks, int list, int n_blocks, int block,
+                    int n_tokens, int Hkv, int d, int dtype, void* k, void* v, int n_rows, int ldk, int ldv, hipStream_t st);
+int launch_decode_attn_kv4(const void* q, const void* pool, size_t slot_bytes, size_t layer_offset, const int* block_of_slot,
+                           int n_slots, int block, int n_prompt, const void* k_resp, const void* v_resp, int n_resp, int Hq,
+                           int Hkv, float scale, int dtype, void* out, float* part, hipStream_t st);
 int launch_gemv(const void* w0, const void* w1, const void* x, const float* scale, float norm_eps, const void* bias,
                 const void* residual, int n_out, int k_in, int dtype, void* out, hipStream_t st);
 int launch_gemv_qkv(const void* wq, const void* wk, const void* wv, const void* bq, const void* bk, const void* bv,
