@@ -21,14 +21,16 @@ typedef __attribute__((address_space(3))) bf16x8* LdsB128;
 
 constexpr int kTileRows = 16, kTileKeys = 32;
 
-// Maximum over the four lanes with the same lane % 16.
+// Maximum over the four lanes with the same lane % 16.  (The elements leave the swap's result as whole numbers first: __builtin_bit_cast of a vector's element reads the vector's
+// first one.)
 __device__ __forceinline__ float max_over_rows(float v) {
     const unsigned x = __builtin_bit_cast(unsigned, v);
     const auto a = __builtin_amdgcn_permlane16_swap(x, x, false, false);
-    const float m = fmaxf(__builtin_bit_cast(float, a[0]), __builtin_bit_cast(float, a[1]));
-    const unsigned y = __builtin_bit_cast(unsigned, m);
+    const unsigned a0 = a[0], a1 = a[1];
+    const unsigned y = __builtin_bit_cast(unsigned, fmaxf(__builtin_bit_cast(float, a0), __builtin_bit_cast(float, a1)));
     const auto b = __builtin_amdgcn_permlane32_swap(y, y, false, false);
-    return fmaxf(__builtin_bit_cast(float, b[0]), __builtin_bit_cast(float, b[1]));
+    const unsigned b0 = b[0], b1 = b[1];
+    return fmaxf(__builtin_bit_cast(float, b0), __builtin_bit_cast(float, b1));
 }
 
 // Eight floats as bfloat16 terms: one, rounded to nearest; it and what is left, rounded to nearest (2^-18 of the float may be missing); or three that add up to the float.
@@ -150,6 +152,34 @@ template <typename T, int D> struct RowTile {
         l += __shfl_xor(l, 32, 64);
     }
 };
+
+// The results of a workgroup's NW waves for the same rows, merged: store(row, channel, values, sum, maximum) is called for the first `rows` of them.  lds: the waves' V tiles, which
+// hold 16 rows of D floats each as well (16-byte pieces turned by the row).
+template <typename T, int D, int NW, typename F> __device__ __forceinline__ void merge_waves(RowTile<T, D>& t, unsigned char* lds, int rows, F store) {
+    typedef RowTile<T, D> Tile;
+    static_assert(Tile::kLdsBytes == kTileRows * D * 4, "O fits the V tile");
+    __shared__ float ws_m[NW][kTileRows], ws_l[NW][kTileRows];
+    const int lane = threadIdx.x & 63, l16 = lane & 15, qr = lane >> 4, wave = threadIdx.x >> 6;
+    t.finish_sum();
+    if (lane < kTileRows) { ws_m[wave][lane] = t.m; ws_l[wave][lane] = t.l; }
+    float* mine = reinterpret_cast<float*>(lds + wave * Tile::kLdsBytes);
+#pragma unroll
+    for (int dt = 0; dt < Tile::DT; ++dt) *reinterpret_cast<f32x4*>(mine + l16 * D + (((dt * 4 + qr) ^ (l16 & (D / 4 - 1))) << 2)) = t.o[dt];
+    __syncthreads();
+    for (int i = threadIdx.x; i < rows * D; i += 64 * NW) {
+        const int r = i / D, dd = i % D;
+        float M = -INFINITY, acc = 0.f, l = 0.f;
+#pragma unroll
+        for (int x = 0; x < NW; ++x) M = fmaxf(M, ws_m[x][r]);
+#pragma unroll
+        for (int x = 0; x < NW; ++x) {
+            const float lx = ws_l[x][r], w = lx == 0.f ? 0.f : __builtin_amdgcn_exp2f(ws_m[x][r] - M);
+            acc += w * reinterpret_cast<const float*>(lds + x * Tile::kLdsBytes)[r * D + (((dd >> 2) ^ (r & (D / 4 - 1))) << 2) + (dd & 3)];
+            l += w * lx;
+        }
+        store(r, dd, acc, l, M);
+    }
+}
 
 // Rows of partial results (D weighted values, maximum, sum) of up to kMergeParts splits -> rows of T: sum_i 2^(m_i - M) o_i / sum_i 2^(m_i - M) l_i.  part[split][row][D + 2].
 constexpr int kMergeParts = 128;
