@@ -156,6 +156,22 @@ int slim_prefill_attn(const void* q, const void* k, const void* v, int n, int n_
                       void* stream);
 
 /* ------------------------------------------------------------------------------------------------
+ * Causal grouped-query attention with a sliding window and a few first tokens that stay visible ("sinks"), for the last n_q of n_k tokens: a prompt
+ * (n_q = n_k), a follow-up prompt behind the rows of a cache (slim_kv4_read), a decoded token (n_q = 1).  Query i is the token at p = n_k - n_q + i and sees
+ *   A(i) = { j : j <= p and (j > p - window or j < n_sinks) }       (window >= n_k: every earlier token)
+ *   out[i,h,:] = sum_{j in A(i)} softmax_j(scale * q[i,h,:].k[j,g,:]) v[j,g,:],  g = h/(Hq/Hkv)
+ *   q, out [n_q, Hq, d]   k, v [n_k, Hkv, d]   all dtype;  softmax_scale 0 => 1/sqrt(d)
+ * Keys and values that a query does not see do not reach its output, whatever they hold (infinities and NaN too); one that sees a key, value or query
+ * that is not finite is not specified.
+ *   workspace   >= slim_sliding_attn_workspace_bytes(...) bytes, 256-byte aligned: partial results of few queries; NULL where that is 0.
+ * Errors: INVALID_ARG (null, n_q < 1, n_k < n_q, Hq % Hkv, window < 1, n_sinks < 0, scale < 0 or NaN), UNSUPPORTED (bf16: d != 128; f32: d other than 32,
+ * 64, 128; alignment of 16 bytes; n_k or n_q * Hq above 2^30), WORKSPACE_TOO_SMALL.
+ */
+size_t slim_sliding_attn_workspace_bytes(int n_q, int n_k, int n_q_heads, int n_kv_heads, int head_dim, int window, int n_sinks, int dtype);
+int slim_sliding_attn(const void* q, const void* k, const void* v, int n_q, int n_k, int n_q_heads, int n_kv_heads, int head_dim, int window,
+                      int n_sinks, float softmax_scale, int dtype, void* out, void* workspace, size_t workspace_bytes, void* stream);
+
+/* ------------------------------------------------------------------------------------------------
  * Per-token building blocks of the layer ("QKV Generation" and "FFN" of Fig. 2).  Exposed so that
  * each kernel can be checked and timed on its own.
  */

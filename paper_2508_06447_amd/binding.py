@@ -27,6 +27,7 @@ EXPORTS = (
     "slim_score_blocks_pooled", "slim_unit_keys", "slim_score_blocks_from_unit_keys",
     "slim_kv_swap_workspace_bytes", "slim_kv_swap", "slim_decode_attn_workspace_bytes", "slim_decode_attn", "slim_gemv", "slim_decode_layer_workspace_bytes",
     "slim_decode_layer", "slim_kv4_block_bytes", "slim_kv4_write", "slim_kv4_read", "slim_decode_attn_kv4", "slim_decode_layer_kv4",
+    "slim_sliding_attn_workspace_bytes", "slim_sliding_attn",
     "slim_rope_table", "slim_window_query", "slim_window_query_from_rows_workspace_bytes", "slim_window_query_from_rows",
     "slim_linear_rope", "slim_score_blocks_from_token_scores",
     "slim_linear_pair", "slim_row_rstd", "slim_rmsnorm_linear", "slim_rmsnorm_swiglu_linear", "slim_fold_gain",
@@ -97,6 +98,9 @@ def load_library(path: str | None = None) -> C.CDLL:
     lib.slim_kv4_write.argtypes = [vp, vp, i, i, i, i, i, i, i, i, vp, i, vp, i, sz, sz, vp]
     lib.slim_kv4_read.argtypes = [vp, i, sz, sz, vp, vp, i, i, i, i, i, i, vp, vp, i, i, i, vp]
     lib.slim_decode_attn_kv4.argtypes = lib.slim_decode_attn.argtypes
+    lib.slim_sliding_attn_workspace_bytes.restype = sz
+    lib.slim_sliding_attn_workspace_bytes.argtypes = [i] * 8
+    lib.slim_sliding_attn.argtypes = [vp, vp, vp, i, i, i, i, i, i, i, f, i, vp, vp, sz, vp]
     lib.slim_rope_table.argtypes = [vp, i, i, f, vp, vp]
     lib.slim_window_query.argtypes = [vp, i, i, i, i, i, vp, vp]
     lib.slim_window_query_from_rows_workspace_bytes.restype = sz
@@ -605,6 +609,34 @@ def slim_prefill_attn(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, softmax
         out = torch.empty_like(q)
     _check(lib.slim_prefill_attn(_dev(q, "q"), _dev(k, "k"), _dev(v, "v"), n, Hq, Hkv, d, softmax_scale,
                                  _dtype_code(q), _dev(out, "out"), _stream()), "slim_prefill_attn")
+    return out
+
+
+def sliding_attn_workspace_bytes(n_q: int, n_k: int, n_q_heads: int, n_kv_heads: int, head_dim: int, window: int, n_sinks: int,
+                                 dtype: torch.dtype) -> int:
+    return load_library().slim_sliding_attn_workspace_bytes(n_q, n_k, n_q_heads, n_kv_heads, head_dim, window, n_sinks, BF16 if dtype == torch.bfloat16 else F32)
+
+
+def slim_sliding_attn(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, window: int, n_sinks: int = 0, softmax_scale: float = 0.0,
+                      out: torch.Tensor | None = None, workspace: torch.Tensor | None = None) -> torch.Tensor:
+    """q[n_q,Hq,d] = the last n_q of the n_k tokens of k/v[n_k,Hkv,d] -> out[n_q,Hq,d]: causal attention over the last `window` tokens and the
+    first n_sinks."""
+    lib = load_library()
+    n_q, Hq, d = q.shape
+    n_k, Hkv, _ = k.shape
+    if v.shape != k.shape or k.shape[2] != d or not q.dtype == k.dtype == v.dtype:
+        raise ValueError("q, k and v do not match")
+    if out is None:
+        out = torch.empty_like(q)
+    elif out.shape != q.shape or out.dtype != q.dtype:
+        raise ValueError("out must be like q")
+    code = _dtype_code(q)
+    if workspace is None:
+        need = lib.slim_sliding_attn_workspace_bytes(n_q, n_k, Hq, Hkv, d, window, n_sinks, code)
+        workspace = torch.empty(need, dtype=torch.uint8, device=q.device) if need else None
+    _check(lib.slim_sliding_attn(_dev(q, "q"), _dev(k, "k"), _dev(v, "v"), n_q, n_k, Hq, Hkv, d, window, n_sinks, softmax_scale, code,
+                                 _dev(out, "out"), _dev(workspace, "workspace"), 0 if workspace is None else workspace.numel(), _stream()),
+           "slim_sliding_attn")
     return out
 
 

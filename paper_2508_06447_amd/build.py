@@ -11,7 +11,7 @@ ROOT = os.path.dirname(HERE)
 CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libslim.so")
 PROBE_LIB = os.path.join(HERE, "libslim_probe.so")
-SOURCES = ("api.hip", "prune.hip", "norm_rope.hip", "gemm.hip", "split.hip", "attn.hip", "f32.hip", "kvswap.hip", "decode.hip", "kv4.hip", "gemv.hip", "window.hip", "probe.hip")
+SOURCES = ("api.hip", "prune.hip", "norm_rope.hip", "gemm.hip", "split.hip", "attn.hip", "f32.hip", "kvswap.hip", "decode.hip", "kv4.hip", "sliding.hip", "gemv.hip", "window.hip", "probe.hip")
 # Kernel arguments in registers when a wave starts (up to 16 dwords): without it a kernel's first instructions wait for their way from host memory.
 # Per launch 0.1 to 0.25 us: the five launches of scoring, selection and compaction 54.0 -> 52.8 us, the small float32 layer's nine 49.6 -> 49.1, a decoded token's
 # layer 88.9 -> 88.6.

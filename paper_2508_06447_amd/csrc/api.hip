@@ -584,6 +584,31 @@ int slim_prefill_attn(const void* q, const void* k, const void* v, int n, int n_
     return launch_attn(q, k, v, n, n_q_heads, n_kv_heads, head_dim, softmax_scale, dtype, out, (hipStream_t)stream);
 }
 
+static int sliding_checks(int n_q, int n_k, int n_q_heads, int n_kv_heads, int head_dim, int window, int n_sinks, int dtype) {
+    if (n_q < 1 || n_k < n_q || n_q_heads < 1 || n_kv_heads < 1 || head_dim < 1 || n_q_heads % n_kv_heads != 0 || window < 1 || n_sinks < 0) return SLIM_INVALID_ARG;
+    if (!dtype_ok(dtype) || (head_dim != 128 && (dtype == SLIM_BF16 || (head_dim != 32 && head_dim != 64))) || n_kv_heads > 65535) return SLIM_UNSUPPORTED;
+    // positions, rows of a kv head and heads of all rows are counted in 32 bits
+    if (n_k > (1 << 30) || (long long)n_q * n_q_heads > (1ll << 30)) return SLIM_UNSUPPORTED;
+    return SLIM_OK;
+}
+
+size_t slim_sliding_attn_workspace_bytes(int n_q, int n_k, int n_q_heads, int n_kv_heads, int head_dim, int window, int n_sinks, int dtype) {
+    if (sliding_checks(n_q, n_k, n_q_heads, n_kv_heads, head_dim, window, n_sinks, dtype) != SLIM_OK) return 0;
+    return align_up(sliding_workspace_floats(n_q, n_k, n_q_heads, n_kv_heads, head_dim, window, n_sinks, dtype) * sizeof(float), 256);
+}
+
+int slim_sliding_attn(const void* q, const void* k, const void* v, int n_q, int n_k, int n_q_heads, int n_kv_heads, int head_dim, int window, int n_sinks,
+                      float softmax_scale, int dtype, void* out, void* workspace, size_t workspace_bytes, void* stream) {
+    if (!q || !k || !v || !out || !(softmax_scale >= 0.f)) return SLIM_INVALID_ARG;
+    const int rc = sliding_checks(n_q, n_k, n_q_heads, n_kv_heads, head_dim, window, n_sinks, dtype);
+    if (rc) return rc;
+    if (!aligned16(q) || !aligned16(k) || !aligned16(v) || !aligned16(out) || ((uintptr_t)workspace & 255u)) return SLIM_UNSUPPORTED;
+    const size_t need = slim_sliding_attn_workspace_bytes(n_q, n_k, n_q_heads, n_kv_heads, head_dim, window, n_sinks, dtype);
+    if (need > 0 && (!workspace || workspace_bytes < need)) return workspace ? SLIM_WORKSPACE_TOO_SMALL : SLIM_INVALID_ARG;
+    if (softmax_scale == 0.f) softmax_scale = 1.0f / sqrtf((float)head_dim);
+    return launch_sliding_attn(q, k, v, n_q, n_k, n_q_heads, n_kv_heads, head_dim, window, n_sinks, softmax_scale, dtype, out, (float*)workspace, (hipStream_t)stream);
+}
+
 int slim_rmsnorm(const void* x, const void* gain, int n, int hidden, float eps, int dtype, void* out, void* stream) {
     if (!x || !gain || !out || n < 1 || hidden < 1 || !(eps >= 0.f)) return SLIM_INVALID_ARG;
     if (!dtype_ok(dtype)) return SLIM_UNSUPPORTED;

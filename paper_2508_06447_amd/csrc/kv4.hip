@@ -182,7 +182,6 @@ __global__ void __launch_bounds__(64 * kQ4Waves) decode_attn_kv4_kernel(
     typedef RowTile<T, D> Tile;
     constexpr int NT = Tile::NT, NP = Tile::NP;
     extern __shared__ __align__(16) unsigned char lds[];
-    __shared__ float ws_m[kQ4Waves][kTileRows], ws_l[kQ4Waves][kTileRows];
     const int g = blockIdx.y, lane = threadIdx.x & 63, l16 = lane & 15, qr = lane >> 4, G = Hq / Hkv;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const unsigned tile = (unsigned)(uintptr_t)lds + wave * Tile::kLdsBytes;
@@ -298,26 +297,7 @@ __global__ void __launch_bounds__(64 * kQ4Waves) decode_attn_kv4_kernel(
             t.template add_values<NT>(p, a, tile);
         }
     }
-    // ---- the waves' results are merged
-    t.finish_sum();
-    if (lane < kTileRows) { ws_m[wave][lane] = t.m; ws_l[wave][lane] = t.l; }
-    // O in place of the wave's V tile: row l16 of 128 floats, its 16-byte pieces turned by the row
-    float* mine = reinterpret_cast<float*>(lds + wave * Tile::kLdsBytes);
-#pragma unroll
-    for (int dt = 0; dt < Tile::DT; ++dt)
-        *reinterpret_cast<f32x4*>(mine + l16 * D + (((dt * 4 + qr) ^ l16) << 2)) = t.o[dt];
-    __syncthreads();
-    for (int i = threadIdx.x; i < G * D; i += 64 * kQ4Waves) {
-        const int h = i / D, dd = i - h * D;
-        float M = -INFINITY, acc = 0.f, l = 0.f;
-#pragma unroll
-        for (int x = 0; x < kQ4Waves; ++x) M = fmaxf(M, ws_m[x][h]);
-#pragma unroll
-        for (int x = 0; x < kQ4Waves; ++x) {
-            const float lx = ws_l[x][h], sc = lx == 0.f ? 0.f : __builtin_amdgcn_exp2f(ws_m[x][h] - M);
-            acc += sc * reinterpret_cast<const float*>(lds + x * Tile::kLdsBytes)[h * D + (((dd >> 2) ^ h) << 2) + (dd & 3)];
-            l += sc * lx;
-        }
+    merge_waves<T, D, kQ4Waves>(t, lds, G, [&](int h, int dd, float acc, float l, float M) {
         const int row = g * G + h;
         if (gridDim.x == 1) {
             Elem<T>::st(out + (size_t)row * D + dd, l == 0.f ? 0.f : acc / l);
@@ -326,7 +306,7 @@ __global__ void __launch_bounds__(64 * kQ4Waves) decode_attn_kv4_kernel(
             dst[dd] = acc;
             if (dd == 0) { dst[D] = M; dst[D + 1] = l; }
         }
-    }
+    });
 }
 
 // 1024 threads a row: 1024 / D groups of D channels, group j the partials j, j + groups, ..; everything is requested at once.

@@ -165,6 +165,9 @@ int launch_kv4_read(const void* pool, int n_slots, size_t slot_bytes, size_t lay
 int launch_decode_attn_kv4(const void* q, const void* pool, size_t slot_bytes, size_t layer_offset, const int* block_of_slot,
                            int n_slots, int block, int n_prompt, const void* k_resp, const void* v_resp, int n_resp, int Hq,
                            int Hkv, float scale, int dtype, void* out, float* part, hipStream_t st);
+size_t sliding_workspace_floats(int n_q, int n_k, int Hq, int Hkv, int d, int window, int sinks, int dtype);
+int launch_sliding_attn(const void* q, const void* k, const void* v, int n_q, int n_k, int Hq, int Hkv, int d, int window, int sinks, float scale, int dtype, void* out,
+                        float* part, hipStream_t st);
 int launch_gemv(const void* w0, const void* w1, const void* x, const float* scale, float norm_eps, const void* bias,
                 const void* residual, int n_out, int k_in, int dtype, void* out, hipStream_t st);
 int launch_gemv_qkv(const void* wq, const void* wk, const void* wv, const void* bq, const void* bk, const void* bv,
