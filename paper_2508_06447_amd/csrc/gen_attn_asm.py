@@ -2,8 +2,10 @@
 """Writes the body of the bf16 prefill-attention kernel ("Attention" stage of Fig. 2) as one block of gfx950
 assembly: attn_bf16_body.inc (the instructions, as C string literals) and attn_bf16_clobbers.inc (the registers
 the block uses).  csrc/attn.hip includes both inside an asm statement; its C++ part computes the per-lane and
-per-workgroup constants that the block takes as operands.  Run `python gen_attn_asm.py` after changing this file;
-the two .inc files are committed, so building the library needs no Python step.
+per-workgroup constants that the block takes as operands.  A second pair, sliding_bf16_body.inc and
+sliding_bf16_clobbers.inc, is the same kernel for a sliding window with visible first tokens (csrc/sliding.hip; WINDOWED
+below).  Run `python gen_attn_asm.py` after changing this file; the .inc files are committed, so building the library needs
+no Python step.
 
 Why assembly: a wave owns 64 queries (two 32-query sub-tiles), so every K and V^T fragment read from LDS feeds two
 MFMAs.  That takes 128 accumulator registers for O, 64 for the Query fragments and 64 for two S tiles per lane: more
@@ -29,6 +31,14 @@ memory straight into LDS, two stages each; per tile the workgroup meets at two b
 phase: one after which the K stage of the tile just finished is refilled, one for the V stage.  The last three
 tiles of a workgroup (where keys can lie above queries) run a second copy of the loop that masks S where needed.
 Every wave of a workgroup runs the same number of units (masked keys give P = 0), so the barriers line up.
+
+WINDOWED.  The tiles of a workgroup are those of the first tokens, if any, then those from its first query's window on: the
+tile pointers and the key index jump between them.  The masked loop runs twice, over the tiles in front (first tokens, the
+rows' window edges) and over the last ones; per unit it masks where a key lies above some query of the wave, or behind some
+window and is no first token.  The first unit may be masked for a whole row, so the reference starts at the larger of that
+unit's maximum and the query's product with its own token, which comes as an operand.  Query fragments stay as they are and
+S is scaled in float on its way into the exponential (a scaled Query rounded to bf16 again is off by 2^-9 per channel: the
+largest error of the whole); the reference is in units of unscaled products.  The epilogue reports a result that is not finite.
 
 Wait states between dependent instructions (matrix result -> vector ALU 12, vector ALU -> matrix operand 2,
 transcendental -> use 1, compare -> select 2, ...) are checked on the finished instruction list and padded with
@@ -62,6 +72,9 @@ S_RAGK, S_RAGV = 60, 62
 S_RET, S_TLK, S_TLV, S_MASKC = 64, 65, 66, 67
 S_SAVE = 68
 FIRST_S, LAST_S = 40, 69
+S_BOUND, S_T1, S_T2 = 70, 71, 72     # WINDOWED: end of the masked loop's present run, scratch
+LAST_S_WINDOWED = 73
+WINDOWED = False                     # which of the two kernels is being written
 SUM_LIMIT, NINF, ONES_BF16 = "0x43800000", "0xff800000", "0x3f803f80"      # 2^8
 AHEAD = 3
 
@@ -126,8 +139,14 @@ def exp_item(buf, qt, pair, slot, first):
     p = PB[qt] + pair
     t = EXPT[2 * slot]
     lu = LUNIT[qt]
-    out = [valu(f"v_exp_f32 {V(t)}, {V(s)}", r=vr(s), w=vr(t), kind="trans"),
-           valu(f"v_exp_f32 {V(t + 1)}, {V(s + 1)}", r=vr(s + 1), w=vr(t + 1), kind="trans")]
+    if WINDOWED:                         # S is not scaled yet
+        out = [valu(f"v_mul_f32 {V(t)}, %[scale], {V(s)}", r=vr(s), w=vr(t)),
+               valu(f"v_mul_f32 {V(t + 1)}, %[scale], {V(s + 1)}", r=vr(s + 1), w=vr(t + 1)),
+               valu(f"v_exp_f32 {V(t)}, {V(t)}", r=vr(t), w=vr(t), kind="trans"),
+               valu(f"v_exp_f32 {V(t + 1)}, {V(t + 1)}", r=vr(t + 1), w=vr(t + 1), kind="trans")]
+    else:
+        out = [valu(f"v_exp_f32 {V(t)}, {V(s)}", r=vr(s), w=vr(t), kind="trans"),
+               valu(f"v_exp_f32 {V(t + 1)}, {V(s + 1)}", r=vr(s + 1), w=vr(t + 1), kind="trans")]
     if first:
         out.append(valu(f"v_add_f32 {V(lu)}, {V(t)}, {V(t + 1)}", r=vr(t, 2), w=vr(lu)))
     else:
@@ -141,16 +160,17 @@ def exp_stream(buf, pairs, fresh):
     """The items of `pairs` for both query sub-tiles, the exponentials of an item issued ahead of the previous
     item's sum and conversion.  fresh: the first item of each sub-tile starts the unit's sum."""
     out, prev, started, n = [], None, set(), 0
+    head = 4 if WINDOWED else 2
     for p in pairs:
         for qt in (0, 1):
             sq = exp_item(buf, qt, p, n & 1, fresh and qt not in started)
             started.add(qt)
             n += 1
-            out += sq[:2]
+            out += sq[:head]
             if prev:
-                out += prev[2:]
+                out += prev[head:]
             prev = sq
-    return out + prev[2:]
+    return out + prev[head:]
 
 
 def sum_check():
@@ -190,7 +210,50 @@ def max_exchange():
     return out
 
 
+def mask_block_windowed(buf):
+    """Key ko of the unit (in the lane's order) is hidden from a query at p if ko > p - k0n, or if it is none of the first tokens, ko >= sinks - k0n, and ko <= p - k0n - window:
+    the second is one unsigned comparison of ko - (sinks - k0n) with the number of such keys."""
+    out = []
+    nsu, cnt, tmp = TMP + 4, [TMP + 5, TMP + 6], TMP + 16
+    for qt in (0, 1):
+        out.append(valu(f"v_subrev_u32 {V(LIMU[qt])}, {S(S_K0N)}, %[limabs{qt}]", r=sr(S_K0N), w=vr(LIMU[qt])))
+    out.append(valu(f"v_mov_b32 {V(TMP + 3)}, {NINF}", w=vr(TMP + 3)))
+    out.append(salu(f"s_sub_u32 {S(S_T1)}, {S(S_K0N)}, %[sinks]", r=sr(S_K0N), w=sr(S_T1) + ["scc"]))
+    out.append(valu(f"v_add_u32 {V(nsu)}, {S(S_T1)}, %[hh4]", r=sr(S_T1), w=vr(nsu)))
+    for qt in (0, 1):
+        out.append(valu(f"v_subrev_u32 {V(cnt[qt])}, %[window], {V(LIMU[qt])}", r=vr(LIMU[qt]), w=vr(cnt[qt])))
+        out.append(valu(f"v_add3_u32 {V(cnt[qt])}, {V(cnt[qt])}, {V(nsu)}, 1", r=vr(cnt[qt]) + vr(nsu), w=vr(cnt[qt])))
+        out.append(valu(f"v_max_i32 {V(cnt[qt])}, 0, {V(cnt[qt])}", r=vr(cnt[qt]), w=vr(cnt[qt])))
+    for qt in (0, 1):
+        for v0 in range(0, 16, 2):
+            for j in range(2):
+                ko = 8 * ((v0 + j) >> 2) + ((v0 + j) & 3)
+                out.append(valu(f"v_add_u32 {V(tmp + j)}, {ko}, {V(nsu)}", r=vr(nsu), w=vr(tmp + j)))
+            for j in range(2):
+                ko, sg = 8 * ((v0 + j) >> 2) + ((v0 + j) & 3), S_TMP + 4 * j
+                out.append(valu(f"v_cmp_lt_i32 {S(sg, 2)}, {V(LIMU[qt])}, {ko}", r=vr(LIMU[qt]), w=sr(sg, 2), kind="vcmp"))
+                out.append(valu(f"v_cmp_lt_u32 {S(sg + 2, 2)}, {V(tmp + j)}, {V(cnt[qt])}", r=vr(tmp + j) + vr(cnt[qt]), w=sr(sg + 2, 2), kind="vcmp"))
+            for j in range(2):
+                sj, sg = S_BUF[buf][qt] + v0 + j, S_TMP + 4 * j
+                for half in (0, 2):
+                    out.append(valu(f"v_cndmask_b32 {V(sj)}, {V(sj)}, {V(TMP + 3)}, {S(sg + half, 2)}", r=vr(sj) + vr(TMP + 3) + sr(sg + half, 2), w=vr(sj)))
+    return out
+
+
+def mask_wanted():
+    """WINDOWED: S_MASKC = some key of the unit at S_K0N lies above the wave's first query, or behind the last one's window and beyond the first tokens."""
+    return [salu(f"s_add_u32 {S(S_TMP)}, {S(S_K0N)}, 31", r=sr(S_K0N), w=sr(S_TMP) + ["scc"]),
+            salu(f"s_cmp_le_i32 {S(S_K0N)}, %[lowq]", r=sr(S_K0N), w=["scc"]),
+            salu(f"s_cselect_b32 {S(S_MASKC)}, 1, 0", r=["scc"], w=sr(S_MASKC)),
+            salu(f"s_cmp_ge_i32 {S(S_TMP)}, %[sinks]", r=sr(S_TMP), w=["scc"]),
+            salu(f"s_cselect_b32 {S(S_MASKC)}, {S(S_MASKC)}, 0", r=["scc"] + sr(S_MASKC), w=sr(S_MASKC)),
+            salu(f"s_cmp_gt_i32 {S(S_TMP)}, %[qw0]", r=sr(S_TMP), w=["scc"]),
+            salu(f"s_cselect_b32 {S(S_MASKC)}, 1, {S(S_MASKC)}", r=["scc"] + sr(S_MASKC), w=sr(S_MASKC))]
+
+
 def mask_block(buf):
+    if WINDOWED:
+        return mask_block_windowed(buf)
     out = []
     for qt in (0, 1):
         out.append(valu(f"v_subrev_u32 {V(LIMU[qt])}, {S(S_K0N)}, %[limabs{qt}]", r=sr(S_K0N), w=vr(LIMU[qt])))
@@ -241,6 +304,19 @@ def tile_advance(which):
     """After a tile's loads: next tile index; pointer moves on unless the last tile was reached; stage flips."""
     tl, st, ptr = (S_TLK, S_KST, S_KPTR) if which == 0 else (S_TLV, S_VST, S_VPTR)
     t0 = S_TMP + 8
+    if WINDOWED:                         # one piece: what lies between a comparison and its use must not compare
+        return [[salu(f"s_add_u32 {S(tl)}, {S(tl)}, 1", r=sr(tl), w=sr(tl) + ["scc"]),
+                 salu(f"s_cmp_le_u32 {S(tl)}, %[last_tile]", r=sr(tl), w=["scc"]),
+                 salu(f"s_cselect_b32 {S(t0)}, %[tile_bytes], 0", r=["scc"], w=sr(t0)),
+                 salu(f"s_add_u32 {S(ptr)}, {S(ptr)}, {S(t0)}", r=sr(ptr) + sr(t0), w=sr(ptr) + ["scc"]),
+                 salu(f"s_addc_u32 {S(ptr + 1)}, {S(ptr + 1)}, 0", r=sr(ptr + 1) + ["scc"], w=sr(ptr + 1) + ["scc"]),
+                 salu(f"s_cmp_eq_u32 {S(tl)}, %[nst]", r=sr(tl), w=["scc"]),
+                 salu(f"s_cselect_b32 {S(t0)}, %[jump_lo], 0", r=["scc"], w=sr(t0)),
+                 salu(f"s_cselect_b32 {S(t0 + 1)}, %[jump_hi], 0", r=["scc"], w=sr(t0 + 1)),
+                 salu(f"s_add_u32 {S(ptr)}, {S(ptr)}, {S(t0)}", r=sr(ptr) + sr(t0), w=sr(ptr) + ["scc"]),
+                 salu(f"s_addc_u32 {S(ptr + 1)}, {S(ptr + 1)}, {S(t0 + 1)}", r=sr(ptr + 1) + sr(t0 + 1) + ["scc"], w=sr(ptr + 1) + ["scc"]),
+                 salu(f"s_xor_b32 {S(st)}, {S(st)}, 0x10000", r=sr(st), w=sr(st) + ["scc"])],
+                ragged_switch(which)]
     return [salu(f"s_add_u32 {S(tl)}, {S(tl)}, 1", r=sr(tl), w=sr(tl) + ["scc"]),
             salu(f"s_cmp_le_u32 {S(tl)}, %[last_tile]", r=sr(tl), w=["scc"]),
             salu(f"s_cselect_b32 {S(t0)}, %[tile_bytes], 0", r=["scc"], w=sr(t0)),
@@ -353,7 +429,16 @@ def build_groups(masked, tag):
             kslot += 1
         deal(ag, exp_stream(cur, range(EARLY, 8), fresh=False) + sum_check())
         ag[7]["post"] += [branch(f"s_cbranch_vccnz RARE_{tag}{j}"), label(f"BACK_{tag}{j}")] + sum_commit()
-        if masked:
+        if masked and WINDOWED:
+            if j == 3:                   # the unit that is formed now is the next tile's first
+                ag[0]["pre"] += [salu(f"s_add_u32 {S(S_T1)}, {S(S_T)}, 1", r=sr(S_T), w=sr(S_T1) + ["scc"]),
+                                 salu(f"s_add_u32 {S(S_T2)}, {S(S_K0N)}, 32", r=sr(S_K0N), w=sr(S_T2) + ["scc"]),
+                                 salu(f"s_cmp_eq_u32 {S(S_T1)}, %[nst]", r=sr(S_T1), w=["scc"]),
+                                 salu(f"s_cselect_b32 {S(S_K0N)}, %[start], {S(S_T2)}", r=["scc"] + sr(S_T2), w=sr(S_K0N))]
+            else:
+                ag[0]["pre"] += [salu(f"s_add_u32 {S(S_K0N)}, {S(S_K0N)}, 32", r=sr(S_K0N), w=sr(S_K0N) + ["scc"])]
+            ag[0]["pre"] += mask_wanted()
+        elif masked:
             ag[0]["pre"] += [salu(f"s_add_u32 {S(S_K0N)}, {S(S_K0N)}, 32", r=sr(S_K0N), w=sr(S_K0N) + ["scc"]),
                              salu(f"s_add_u32 {S(S_TMP)}, {S(S_K0N)}, 31", r=sr(S_K0N), w=sr(S_TMP) + ["scc"]),
                              salu(f"s_cmp_gt_i32 {S(S_TMP)}, %[qw0]", r=sr(S_TMP), w=["scc"]),
@@ -451,6 +536,8 @@ def rare_block(tag, j, ret):
         out.append(valu(f"v_xor_b32 {V(TMP + 3)}, 0x80000000, {V(REF[qt])}", r=vr(REF[qt]), w=vr(TMP + 3)))
         for v in range(16):
             out.append(valu(f"v_mov_b32 {V(NEGR[qt] + v)}, {V(TMP + 3)}", r=vr(TMP + 3), w=vr(NEGR[qt] + v)))
+        if WINDOWED:
+            out.append(valu(f"v_mul_f32 {V(d)}, %[scale], {V(d)}", r=vr(d), w=vr(d)))
         out.append(valu(f"v_exp_f32_e64 {V(TMP + 4 + qt)}, -{V(d)}", r=vr(d), w=vr(TMP + 4 + qt), kind="trans"))
     out.append(nop(2))
     for qt in (0, 1):
@@ -520,9 +607,16 @@ def prologue():
     for qt in (0, 1):
         e(valu(f"v_mov_b32 {V(LRUN[qt])}, 0", w=vr(LRUN[qt])))
     e(salu(f"s_mov_b32 {S(S_T)}, 0", w=sr(S_T)))
-    e(salu(f"s_mov_b32 {S(S_K0N)}, 0", w=sr(S_K0N)))
+    if WINDOWED:
+        e(salu("s_cmp_eq_u32 %[nst], 0", w=["scc"]))
+        e(salu(f"s_cselect_b32 {S(S_K0N)}, %[start], 0", r=["scc"], w=sr(S_K0N)))
+    else:
+        e(salu(f"s_mov_b32 {S(S_K0N)}, 0", w=sr(S_K0N)))
     e(raw("s_waitcnt vmcnt(24)", "wait"))       # the Query rows are there; the 24 tile loads may still be in flight
     for i in range(64):
+        if WINDOWED:
+            e(valu(f"v_accvgpr_write_b32 {A(Q_ACC + i)}, {V(i)}", r=vr(i), w=ar(Q_ACC + i)))
+            continue
         lo, hi = TMP + 2 * (i & 3), TMP + 2 * (i & 3) + 1
         e(valu(f"v_lshlrev_b32 {V(lo)}, 16, {V(i)}", r=vr(i), w=vr(lo)))
         e(valu(f"v_and_b32 {V(hi)}, 0xffff0000, {V(i)}", r=vr(i), w=vr(hi)))
@@ -544,11 +638,18 @@ def prologue():
         out += G[g]["frag"]
     e(nop(8)); e(nop(8))
     # first tail: mask (unit 0 needs it only for the wave that owns query 0), maxima, reference = maximum
-    e(salu(f"s_cmp_gt_i32 %[qw0], 30", w=["scc"]))
+    if WINDOWED:
+        out += mask_wanted()
+        e(salu(f"s_cmp_eq_u32 {S(S_MASKC)}, 0", r=sr(S_MASKC), w=["scc"]))
+    else:
+        e(salu(f"s_cmp_gt_i32 %[qw0], 30", w=["scc"]))
     e(branch("s_cbranch_scc1 SKIPM_P"))
     out += mask_block(0)
     e(label("SKIPM_P"))
     out += max_local(0) + max_exchange()
+    if WINDOWED:
+        for qt in (0, 1):
+            e(valu(f"v_max_f32 {V(TMAX[qt])}, {V(TMAX[qt])}, %[own{qt}]", r=vr(TMAX[qt]), w=vr(TMAX[qt])))
     for qt in (0, 1):
         e(valu(f"v_mov_b32 {V(REF[qt])}, {V(TMAX[qt])}", r=vr(TMAX[qt]), w=vr(REF[qt])))
         for v in range(16):
@@ -585,6 +686,9 @@ def epilogue():
                     e(valu(f"v_accvgpr_read_b32 {V(t + k)}, {A(o + vg * 4 + k)}", r=ar(o + vg * 4 + k), w=vr(t + k)))
                 for k in range(4):
                     e(valu(f"v_mul_f32 {V(t + k)}, {V(t + k)}, {V(inv)}", r=vr(t + k) + vr(inv), w=vr(t + k)))
+                if WINDOWED:             # stays 0 while everything is finite
+                    for k in range(4):
+                        e(valu(f"v_fma_f32 %[odd], {V(t + k)}, 0, %[odd]", r=vr(t + k)))
                 e(valu(f"v_cvt_pk_bf16_f32 {V(t)}, {V(t)}, {V(t + 1)}", r=vr(t, 2), w=vr(t)))
                 e(valu(f"v_cvt_pk_bf16_f32 {V(t + 1)}, {V(t + 2)}, {V(t + 3)}", r=vr(t + 2, 2), w=vr(t + 1)))
                 e(Ins(f"global_store_dwordx2 %[orow{qt}], {V(t, 2)}, off offset:{(dt * 32 + 8 * vg) * 2}", "vmem", r=vr(t, 2)))
@@ -603,18 +707,31 @@ def stats(name, body):
           ", ".join(f"{k} {v}" for k, v in sorted(c.items())), file=sys.stderr)
 
 
-def main():
+def write(here, name, last_s):
     main_body = loop_body(False, "m")
     diag_body = loop_body(True, "d")
-    stats("main loop", main_body)
-    stats("diagonal loop", diag_body)
+    stats(f"{name}: main loop", main_body)
+    stats(f"{name}: diagonal loop", diag_body)
     pro = fix_hazards(prologue())
-    # main loop over the tiles before the last three, then the masked loop over the rest
     seq = list(pro)
-    seq += [salu(f"s_cmp_lt_u32 {S(S_T)}, %[nmain]", r=sr(S_T), w=["scc"]), branch("s_cbranch_scc0 MAIN_DONE"),
-            label("LOOP_M")] + main_body + loop_tail("LOOP_M", "%[nmain]") + [label("MAIN_DONE")]
-    seq += [salu(f"s_lshl_b32 {S(S_K0N)}, {S(S_T)}, 7", r=sr(S_T), w=sr(S_K0N) + ["scc"]),
-            label("LOOP_D")] + diag_body + loop_tail("LOOP_D", "%[nkt]")
+    if WINDOWED:
+        # the masked loop over the tiles in front, the main loop, the masked loop over the rest
+        seq += [salu(f"s_mov_b32 {S(S_BOUND)}, %[nhead]", w=sr(S_BOUND)),
+                salu(f"s_cmp_lt_u32 {S(S_T)}, %[nhead]", r=sr(S_T), w=["scc"]), branch("s_cbranch_scc1 LOOP_D"),
+                label("FRONT_DONE"), salu(f"s_cmp_lt_u32 {S(S_T)}, %[nmain]", r=sr(S_T), w=["scc"]), branch("s_cbranch_scc0 MAIN_DONE"),
+                label("LOOP_M")] + main_body + loop_tail("LOOP_M", "%[nmain]") + [label("MAIN_DONE")]
+        seq += [salu(f"s_mov_b32 {S(S_BOUND)}, %[nkt]", w=sr(S_BOUND)),
+                salu(f"s_sub_u32 {S(S_K0N)}, {S(S_T)}, %[nst]", r=sr(S_T), w=sr(S_K0N) + ["scc"]),
+                salu(f"s_lshl_b32 {S(S_K0N)}, {S(S_K0N)}, 7", r=sr(S_K0N), w=sr(S_K0N) + ["scc"]),
+                salu(f"s_add_u32 {S(S_K0N)}, {S(S_K0N)}, %[start]", r=sr(S_K0N), w=sr(S_K0N) + ["scc"]),
+                label("LOOP_D")] + diag_body + loop_tail("LOOP_D", S(S_BOUND))
+        seq += [salu(f"s_cmp_lt_u32 {S(S_T)}, %[nkt]", r=sr(S_T), w=["scc"]), branch("s_cbranch_scc1 FRONT_DONE")]
+    else:
+        # main loop over the tiles before the last three, then the masked loop over the rest
+        seq += [salu(f"s_cmp_lt_u32 {S(S_T)}, %[nmain]", r=sr(S_T), w=["scc"]), branch("s_cbranch_scc0 MAIN_DONE"),
+                label("LOOP_M")] + main_body + loop_tail("LOOP_M", "%[nmain]") + [label("MAIN_DONE")]
+        seq += [salu(f"s_lshl_b32 {S(S_K0N)}, {S(S_T)}, 7", r=sr(S_T), w=sr(S_K0N) + ["scc"]),
+                label("LOOP_D")] + diag_body + loop_tail("LOOP_D", "%[nkt]")
     seq += fix_hazards(epilogue()) + [branch("s_branch DONE")]
     returns = []
     for tag in ("m", "d"):
@@ -626,8 +743,7 @@ def main():
     used_v = max(int(r[1:]) for x in seq for r in (x.r | x.w) if r[0] == "v" and r[1:].isdigit())
     used_a = max(int(r[1:]) for x in seq for r in (x.r | x.w) if r[0] == "a" and r[1:].isdigit())
     assert used_v <= LAST_V and used_a <= LAST_A, (used_v, used_a)
-    here = sys.argv[1] if len(sys.argv) > 1 else os.path.dirname(os.path.abspath(__file__))   # output directory
-    with open(os.path.join(here, "attn_bf16_body.inc"), "w") as f:
+    with open(os.path.join(here, f"{name}_body.inc"), "w") as f:
         f.write("// generated by gen_attn_asm.py -- do not edit\n")
         # labels get the asm statement's unique number, so that the block can be instantiated more than once
         names = sorted((x.text[:-1] for x in seq if x.kind == "label"), key=len, reverse=True)
@@ -635,10 +751,19 @@ def main():
         for x in seq:
             f.write('    "' + pattern.sub(lambda m: m.group(1) + "_%=", x.text) + '\\n"\n')
     clob = ([f'"v{i}"' for i in range(LAST_V + 1)] + [f'"a{i}"' for i in range(LAST_A + 1)] +
-            [f'"s{i}"' for i in range(FIRST_S, LAST_S + 1)] + ['"vcc"', '"scc"', '"memory"'])
-    with open(os.path.join(here, "attn_bf16_clobbers.inc"), "w") as f:
+            [f'"s{i}"' for i in range(FIRST_S, last_s + 1)] + ['"vcc"', '"scc"', '"memory"'])
+    with open(os.path.join(here, f"{name}_clobbers.inc"), "w") as f:
         f.write(", ".join(clob) + "\n")
-    print(f"{len(seq)} lines, vgprs to v{used_v}, agprs to a{used_a}", file=sys.stderr)
+    print(f"{name}: {len(seq)} lines, vgprs to v{used_v}, agprs to a{used_a}", file=sys.stderr)
+
+
+def main():
+    global WINDOWED
+    here = sys.argv[1] if len(sys.argv) > 1 else os.path.dirname(os.path.abspath(__file__))   # output directory
+    for WINDOWED, name, last_s in ((False, "attn_bf16", LAST_S), (True, "sliding_bf16", LAST_S_WINDOWED)):
+        _uid[0] = 0
+        write(here, name, last_s)
+    WINDOWED = False
 
 
 if __name__ == "__main__":

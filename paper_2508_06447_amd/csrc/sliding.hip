@@ -5,27 +5,11 @@
 // fills the tiles.  What a tile of rows reads: the keys from the first one in its first query's window to its last query's position, and in front of them the first tokens that
 // this stretch leaves behind.
 #include "row_tile.h"
-#include "routes.h"
+#include "sliding_plan.h"
 #include <algorithm>
+#include <mutex>
 
 namespace slim {
-
-struct SlidingRows {
-    int n_q, n_k, G, Hkv, window, sinks;
-    float scale_log2e;
-};
-// The keys that rows r0 .. r0 + count - 1 of a kv head see: [0, first) and [start, end); rows' first and last position.
-struct SlidingSpan {
-    int p0, p1, first, start, end;
-    __device__ __forceinline__ SlidingSpan(const SlidingRows& a, int r0, int count) {
-        const int off = a.n_k - a.n_q;
-        p0 = off + min(r0 / a.G, a.n_q - 1);
-        p1 = off + min((r0 + count - 1) / a.G, a.n_q - 1);
-        start = max(0, p0 - a.window + 1);
-        first = min(a.sinks, start);
-        end = p1 + 1;
-    }
-};
 
 // ---- few rows: 16 of them per workgroup, the units of 32 keys dealt to its waves and to gridDim.z workgroups
 constexpr int kSlideWaves = 4;
@@ -176,6 +160,124 @@ __global__ void __launch_bounds__(64 * kSlideWaves) sliding_rows_kernel(const T*
     });
 }
 
+// ---- many rows: bfloat16, 256 rows per workgroup, 64 per wave
+// The loop of the prompt attention (gen_attn_asm.py, which says how it runs), over the tiles of 128 keys that the workgroup's rows see: those of the first tokens, if the stretch
+// leaves any behind, then the stretch.  Where the two would meet inside a tile the stretch begins at key 0 instead.
+constexpr int LD = 128, LW = 4, LKV = kSlideTile, LTILE_BYTES = LKV * LD * 2, LSTAGE_BYTES = 2 * LTILE_BYTES, LSTAGES = 2, LROWS = 64 * LW;
+
+__global__ void __launch_bounds__(64 * LW) __attribute__((amdgpu_waves_per_eu(1, 1)))
+sliding_many_kernel(const bf16_t* __restrict__ Q, const bf16_t* __restrict__ Kg, const bf16_t* __restrict__ Vg, bf16_t* __restrict__ O, SlidingRows a, int n_rt) {
+    extern __shared__ __align__(16) unsigned char lds[];
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), l32 = lane & 31, hh = lane >> 5;
+    // Workgroup -> (kv head, row tile): each XCD its own kv heads, whose keys then meet in one L2, the tiles with the most keys first.
+    int g, rt;
+    if (a.Hkv % 8 == 0) {
+        const int j = blockIdx.x >> 3, per = a.Hkv >> 3;
+        g = (blockIdx.x & 7) * per + j % per;
+        rt = n_rt - 1 - j / per;
+    } else {
+        g = blockIdx.x % a.Hkv;
+        rt = n_rt - 1 - blockIdx.x / a.Hkv;
+    }
+    const int Hq = a.G * a.Hkv, rows = a.n_q * a.G, off = a.n_k - a.n_q, r0 = rt * LROWS, rw = r0 + wave * 64;
+    const unsigned rowbytes = (unsigned)a.Hkv * LD * 2, tile_bytes = rowbytes * LKV;
+    const SlidingSpan all(a, r0, LROWS), mine(a, min(rw, rows - 1), 64);
+    const SlidingTiles tl(all, a.window);
+    const int start = tl.start;
+    const unsigned nst = tl.apart, nkt = tl.all, nhead = tl.clean, nmain = tl.masked, last_tile = nkt - 1;
+    const unsigned last_ragged = tl.left != LKV ? last_tile : 0xffffffffu, nl1 = tl.left - 1;   // rows of the last tile behind its keys repeat the last one
+    const uint64_t jump = (uint64_t)(start - (int)nst * LKV) * rowbytes;
+    const unsigned jump_lo = nst ? (unsigned)jump : 0, jump_hi = nst ? (unsigned)(jump >> 32) : 0;
+    const uint64_t kb = (uint64_t)(uintptr_t)(Kg + (size_t)g * LD) + (nst ? 0 : (uint64_t)start * rowbytes);
+    const uint64_t vb = (uint64_t)(uintptr_t)(Vg + (size_t)g * LD) + (nst ? 0 : (uint64_t)start * rowbytes);
+    const unsigned kbase_lo = (unsigned)kb, kbase_hi = (unsigned)(kb >> 32), vbase_lo = (unsigned)vb, vbase_hi = (unsigned)(vb >> 32);
+    const int qw0 = mine.p0, lowq = mine.p1 - a.window, window = a.window, sinks = a.sinks;
+
+    // the lane's two rows
+    const int ra = min(rw + l32, rows - 1), rb = min(rw + 32 + l32, rows - 1), ia = ra / a.G, ib = rb / a.G;
+    const size_t qa = ((size_t)ia * Hq + g * a.G + (ra - ia * a.G)) * LD, qb = ((size_t)ib * Hq + g * a.G + (rb - ib * a.G)) * LD;
+    const bf16_t *qrow0 = Q + qa + hh * 8, *qrow1 = Q + qb + hh * 8;
+    bf16_t *orow0 = O + qa + 4 * hh, *orow1 = O + qb + 4 * hh;
+    const int hh4 = 4 * hh, limabs0 = off + ia - hh4, limabs1 = off + ib - hh4;
+    const unsigned valid0 = rw + l32 < rows, valid1 = rw + 32 + l32 < rows;
+    // Each row's product with its own token: a reference that is never minus infinity, whatever the first unit's mask leaves of the row.
+    auto own_product = [&](const bf16_t* qr, int i) {
+        const bf16_t* kr = Kg + ((size_t)(off + i) * a.Hkv + g) * LD + hh * 8;
+        float sum = 0.f;
+#pragma unroll
+        for (int st = 0; st < 8; ++st) {
+            float x[8], y[8];
+            Elem<bf16_t>::unpack(*reinterpret_cast<const uint4*>(qr + st * 16), x);
+            Elem<bf16_t>::unpack(*reinterpret_cast<const uint4*>(kr + st * 16), y);
+#pragma unroll
+            for (int e = 0; e < 8; ++e) sum += x[e] * y[e];
+        }
+        return sum + __shfl_xor(sum, 32, 64);
+    };
+    const float own0 = own_product(qrow0, ia), own1 = own_product(qrow1, ib);
+
+    // LDS byte addresses of the lane's fragment reads and the operands of its tile loads, as the prompt attention's.
+    auto k_at = [](int r, int c) { return (r * 16 + (c ^ (r & 15))) * 16; };
+    auto v_at = [](int r, int c) { return (r * 16 + (c ^ ((r & 3) << 2))) * 16; };
+    const unsigned lds_base = (unsigned)(uintptr_t)lds;
+    const unsigned koff0 = lds_base + k_at(l32, hh);
+    const int q4 = lane >> 4, sl = lane & 15, key_lane = 4 * (q4 >> 1) + (sl >> 2);
+    const unsigned voff0 = lds_base + LTILE_BYTES + v_at(key_lane, 2 * (q4 & 1) + ((sl & 3) >> 1)) + (sl & 1) * 8;
+    const unsigned row0 = wave * 4 + (lane >> 4), slot = lane & 15;
+    const unsigned kchunk = (slot ^ (row0 & 15)) * 16, vchunk = (slot ^ ((row0 & 3) << 2)) * 16;
+    const unsigned ldsw = lds_base + wave * 1024;
+    float odd = 0.f;                                     // not 0: some result is not finite
+
+    asm volatile(
+#include "sliding_bf16_body.inc"
+        : [odd] "+v"(odd)
+        : [koff0] "v"(koff0), [voff0] "v"(voff0), [r0] "v"(row0), [kchunk] "v"(kchunk), [vchunk] "v"(vchunk),
+          [qrow0] "v"(qrow0), [qrow1] "v"(qrow1), [orow0] "v"(orow0), [orow1] "v"(orow1),
+          [limabs0] "v"(limabs0), [limabs1] "v"(limabs1), [valid0] "v"(valid0), [valid1] "v"(valid1), [own0] "v"(own0), [own1] "v"(own1), [hh4] "v"(hh4),
+          [kbase_lo] "s"(kbase_lo), [kbase_hi] "s"(kbase_hi), [vbase_lo] "s"(vbase_lo), [vbase_hi] "s"(vbase_hi),
+          [nkt] "s"(nkt), [nhead] "s"(nhead), [nmain] "s"(nmain), [nst] "s"(nst), [start] "s"(start), [last_tile] "s"(last_tile), [last_ragged] "s"(last_ragged),
+          [rowbytes] "s"(rowbytes), [tile_bytes] "s"(tile_bytes), [jump_lo] "s"(jump_lo), [jump_hi] "s"(jump_hi), [scale] "s"(a.scale_log2e), [nl1] "s"(nl1),
+          [ldsw] "s"(ldsw), [qw0] "s"(qw0), [lowq] "s"(lowq), [window] "s"(window), [sinks] "s"(sinks)
+        :
+#include "sliding_bf16_clobbers.inc"
+    );
+    // Keys or values that are not finite: perhaps behind a mask, where a weight of 0 does not undo them.  The wave's rows are computed again, 16 at a time.
+    __syncthreads();
+    if (!__any(!(odd == 0.f))) return;
+    const int l16 = lane & 15, qr = lane >> 4;
+#pragma unroll 1
+    for (int t = 0; t < 4; ++t) {
+        const int first = rw + t * kTileRows;
+        if (first >= rows) break;
+        const SlidingSpan sp(a, first, kTileRows);
+        const int r = min(first + l16, rows - 1), i = r / a.G;
+        const size_t at = ((size_t)i * Hq + g * a.G + (r - i * a.G)) * LD;
+        RowTile<bf16_t, LD> tile;
+        tile.begin(Q + at);
+        sliding_units<bf16_t, LD>(tile, Kg + (size_t)g * LD, Vg + (size_t)g * LD, a, sp, off + i, 0, 1, lds_base + wave * RowTile<bf16_t, LD>::kLdsBytes);
+        tile.finish_sum();
+        if (first + l16 < rows)
+#pragma unroll
+            for (int dt = 0; dt < 8; ++dt)
+                *reinterpret_cast<uint2*>(O + at + dt * 16 + qr * 4) = make_uint2(pack_bf16x2(tile.o[dt][0] / tile.l, tile.o[dt][1] / tile.l),
+                                                                                  pack_bf16x2(tile.o[dt][2] / tile.l, tile.o[dt][3] / tile.l));
+    }
+}
+
+static int launch_sliding_many(const void* q, const void* k, const void* v, const SlidingRows& a, void* out, hipStream_t st) {
+    const int smem = LSTAGES * LSTAGE_BYTES;
+    static std::once_flag once;
+    static hipError_t err = hipSuccess;
+    std::call_once(once, [&] { err = hipFuncSetAttribute((const void*)sliding_many_kernel, hipFuncAttributeMaxDynamicSharedMemorySize, smem); });
+    if (err != hipSuccess) return set_hip_error(err);
+    const int n_rt = (int)(((long long)a.n_q * a.G + LROWS - 1) / LROWS);
+    hipLaunchKernelGGL(sliding_many_kernel, dim3((unsigned)((long long)n_rt * a.Hkv)), dim3(64 * LW), smem, st, (const bf16_t*)q, (const bf16_t*)k, (const bf16_t*)v, (bf16_t*)out, a, n_rt);
+    return check_launch();
+}
+
+// Whether a call runs in tiles of 256 rows.  (rowbytes and the 24-bit multiplies of the tile loads' offsets bound the number of kv heads.)
+static bool sliding_many(int n_q, int G, int Hkv, int dtype) { return dtype == SLIM_BF16 && Hkv <= 4096 && (long long)n_q * G >= LROWS; }
+
 // Workgroups per row tile: about kSlideWgs in all, every wave the same number of units where that can be.
 constexpr int kSlideWgs = 512;
 static int sliding_splits(int n_q, int n_k, int G, int Hkv, int window, int sinks) {
@@ -188,13 +290,16 @@ static int sliding_splits(int n_q, int n_k, int G, int Hkv, int window, int sink
 }
 
 size_t sliding_workspace_floats(int n_q, int n_k, int Hq, int Hkv, int d, int window, int sinks, int dtype) {
+    if (sliding_many(n_q, Hq / Hkv, Hkv, dtype)) return 0;
     const int splits = sliding_splits(n_q, n_k, Hq / Hkv, Hkv, window, sinks);
     return splits > 1 ? (size_t)splits * n_q * Hq * (d + 2) : 0;
 }
 
 int launch_sliding_attn(const void* q, const void* k, const void* v, int n_q, int n_k, int Hq, int Hkv, int d, int window, int sinks, float scale, int dtype, void* out,
                         float* part, hipStream_t st) {
-    const SlidingRows a{n_q, n_k, Hq / Hkv, Hkv, window, sinks, scale * 1.4426950408889634f};
+    // a window or a number of first tokens beyond the keys is all of them
+    const SlidingRows a{n_q, n_k, Hq / Hkv, Hkv, std::min(window, n_k), std::min(sinks, n_k), scale * 1.4426950408889634f};
+    if (sliding_many(n_q, a.G, Hkv, dtype)) return launch_sliding_many(q, k, v, a, out, st);
     const int splits = sliding_splits(n_q, n_k, a.G, Hkv, window, sinks);
     const long long tiles = ((long long)n_q * a.G + kTileRows - 1) / kTileRows;
     const dim3 grid((unsigned)tiles, Hkv, splits);

@@ -80,21 +80,21 @@ def test_keys_and_values_that_a_query_does_not_see_do_not_reach_it(slim, n_q, n_
     """Infinities and NaN in keys and values: the rows that do not see them are what they are without them."""
     q, k, v = inputs_of(n_q, n_k, Hq, Hkv, d, dtype, 11)
     places = sorted({0, sinks, n_k - n_q, n_k - 1, n_k // 2, max(0, n_k - n_q - window), max(0, n_k - window), n_k - n_q + n_q // 3} & set(range(n_k)))
-    clean = slim.slim_sliding_attn(q.cuda(), k.cuda(), v.cuda(), window, sinks)
     seen = visible(n_q, n_k, window, sinks)
+    want, size, reach = ref.attention(ref.to64(q), ref.to64(k), ref.to64(v), seen, 1 / math.sqrt(d))
+    bound = ref.attention_bound(want, size, reach, int(seen.sum(1).max()), d, dtype, ref.to64(v))
     for which in ("v", "k"):
         for value in (math.inf, math.nan):
             for bad in (places, places[::2], places[1::2], [places[-1]]):
                 kk, vv = k.clone(), v.clone()
                 (vv if which == "v" else kk)[bad] = value
                 got = slim.slim_sliding_attn(q.cuda(), kk.cuda(), vv.cuda(), window, sinks)
-                blind = torch.from_numpy(~seen[:, bad].any(1)).cuda()
-                a, b = got[blind].double(), clean[blind].double()
-                assert torch.isfinite(a).all(), (which, value, bad)
-                # the same sums, perhaps in another order: a unit roundoff of the type beside what the bound allows is not needed, rows without such keys are summed alike
-                assert ((a - b).abs() <= 2 * torch.finfo(dtype).eps * b.abs() + 1e-5).all(), (which, value, bad)
+                blind = ~seen[:, bad].any(1)
+                print(which, value, bad, int(blind.sum()), end="", flush=True)
+                if blind.any():
+                    ref.within(got[torch.from_numpy(blind).cuda()], want[blind], bound[blind])
                 if which == "v":
-                    assert not torch.isfinite(got[~blind].float()).all(-1).any()
+                    assert not torch.isfinite(got[torch.from_numpy(~blind).cuda()].float()).all(-1).any()
 
 
 def test_window_that_covers_everything_is_plain_causal_attention(slim):

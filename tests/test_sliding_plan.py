@@ -1,0 +1,78 @@
+"""The tiles of sliding-window attention with many rows (csrc/sliding_plan.h), compiled for the CPU: every key that a row sees is in a tile, once; tiles without masks are seen whole by
+every row; nothing is read outside the keys.  No GPU."""
+import os
+import shutil
+import subprocess
+
+import pytest
+
+ROOT = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
+SOURCE = r"""
+#include "sliding_plan.h"
+#include <cstdio>
+#include <cstdlib>
+using namespace slim;
+static int fail(const SlidingRows& a, int r0, const char* what) {
+    printf("n_q %d n_k %d G %d window %d sinks %d row %d: %s\n", a.n_q, a.n_k, a.G, a.window, a.sinks, r0, what);
+    return 1;
+}
+static int check(const SlidingRows& a) {
+    const int rows = a.n_q * a.G, off = a.n_k - a.n_q;
+    for (int r0 = 0; r0 < rows; r0 += 256) {
+        const SlidingSpan s(a, r0, 256);
+        const SlidingTiles t(s, a.window);
+        if (t.all < 1 || t.left < 1 || t.left > 128 || t.clean < t.apart || t.clean > t.all || t.masked < t.clean || t.masked >= t.all + (t.clean == t.all)) return fail(a, r0, "counts");
+        const int last_row = r0 + 255 < rows ? r0 + 255 : rows - 1, p0 = off + r0 / a.G, p1 = off + last_row / a.G;
+        if (s.p0 != p0 || s.p1 != p1) return fail(a, r0, "positions");
+        int* times = (int*)calloc(a.n_k, sizeof(int));
+        for (int i = 0; i < t.all; ++i) {
+            const int k0 = i < t.apart ? i * 128 : t.start + (i - t.apart) * 128, n = i == t.all - 1 ? t.left : 128;
+            if (k0 < 0 || k0 + n > a.n_k) { free(times); return fail(a, r0, "outside"); }
+            for (int j = k0; j < k0 + n; ++j) ++times[j];
+            for (int u = 0; u < 4; ++u) {                // units whose logits the loop without masks forms
+                const int idx = 4 * i + u;
+                if (idx < 4 * t.clean + 1 || idx > 4 * t.masked) continue;
+                for (int j = k0 + 32 * u; j < k0 + 32 * u + 32; ++j)
+                    for (int p = p0; p <= p1; p += p1 > p0 ? p1 - p0 : 1)
+                        if (t.masked > t.clean && !(j <= p && (j > p - a.window || j < a.sinks))) { free(times); return fail(a, r0, "mask"); }
+            }
+        }
+        for (int p = p0; p <= p1; ++p)
+            for (int j = 0; j <= p; ++j)
+                if ((j > p - a.window || j < a.sinks) && times[j] != 1) { free(times); return fail(a, r0, "coverage"); }
+        free(times);
+    }
+    return 0;
+}
+int main() {
+    unsigned x = 12345;
+    auto rnd = [&](int n) { x = x * 1664525u + 1013904223u; return (int)((x >> 8) % (unsigned)n); };
+    int cases = 0;
+    for (int c = 0; c < 4000; ++c) {
+        SlidingRows a{};
+        a.n_k = 1 + rnd(c % 4 ? 700 : 2500);
+        a.n_q = c % 3 ? 1 + rnd(a.n_k) : a.n_k;
+        const int heads[6] = {1, 2, 3, 4, 7, 20};
+        a.G = heads[rnd(6)];
+        a.window = 1 + rnd(c % 5 ? a.n_k : 1 + a.n_k / 8);
+        const int few[6] = {0, 1, 4, 64, 128, 130};
+        a.sinks = c % 7 ? few[rnd(6)] : rnd(a.n_k + 1);
+        if (a.sinks > a.n_k) a.sinks = a.n_k;
+        if (check(a)) return 1;
+        ++cases;
+    }
+    printf("%d cases\n", cases);
+    return 0;
+}
+"""
+
+
+def test_tiles(tmp_path):
+    gxx = shutil.which("g++")
+    if not gxx:
+        pytest.skip("no host compiler")
+    src, exe = tmp_path / "plan.cpp", tmp_path / "plan"
+    src.write_text(SOURCE)
+    subprocess.run([gxx, "-O2", "-std=c++17", "-I", os.path.join(ROOT, "paper_2508_06447_amd", "csrc"), str(src), "-o", str(exe)], check=True)
+    r = subprocess.run([str(exe)], capture_output=True, text=True)
+    assert r.returncode == 0 and r.stdout.strip() == "4000 cases", r.stdout
