@@ -214,7 +214,9 @@ sliding_many_kernel(const bf16_t* __restrict__ Q, const bf16_t* __restrict__ Kg,
         }
         return sum + __shfl_xor(sum, 32, 64);
     };
-    const float own0 = own_product(qrow0, ia), own1 = own_product(qrow1, ib);
+    // (with a first token in sight the first unit holds a key that every row sees; 4.7 us of a workgroup's 110 where that is not so)
+    float own0 = -INFINITY, own1 = -INFINITY;
+    if (a.sinks == 0) { own0 = own_product(qrow0, ia); own1 = own_product(qrow1, ib); }
 
     // LDS byte addresses of the lane's fragment reads and the operands of its tile loads, as the prompt attention's.
     auto k_at = [](int r, int c) { return (r * 16 + (c ^ (r & 15))) * 16; };
