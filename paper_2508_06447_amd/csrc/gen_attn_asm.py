@@ -38,7 +38,10 @@ rows' window edges) and over the last ones; per unit it masks where a key lies a
 window and is no first token.  The first unit may be masked for a whole row, so the reference starts at the larger of that
 unit's maximum and the query's product with its own token, which comes as an operand.  Query fragments stay as they are and
 S is scaled in float on its way into the exponential (a scaled Query rounded to bf16 again is off by 2^-9 per channel: the
-largest error of the whole); the reference is in units of unscaled products.  The epilogue reports a result that is not finite.
+largest error of the whole); the reference is in units of unscaled products, and moves only for a sum above 2^60: weights, their
+sums and O are floats, whose relative error does not depend on where the reference lies (with queries that each meet one key 12
+bits above the others, half of the units moved it at 2^8).  With %[split] the workgroup has seen a part of the keys: the epilogue
+leaves O as it is, in float, with the reference (scaled) and the sum behind it.  It reports a result that is not finite.
 
 Wait states between dependent instructions (matrix result -> vector ALU 12, vector ALU -> matrix operand 2,
 transcendental -> use 1, compare -> select 2, ...) are checked on the finished instruction list and padded with
@@ -76,6 +79,7 @@ S_BOUND, S_T1, S_T2 = 70, 71, 72     # WINDOWED: end of the masked loop's presen
 LAST_S_WINDOWED = 73
 WINDOWED = False                     # which of the two kernels is being written
 SUM_LIMIT, NINF, ONES_BF16 = "0x43800000", "0xff800000", "0x3f803f80"      # 2^8
+SUM_LIMIT_WINDOWED = "0x5d800000"    # 2^60
 AHEAD = 3
 
 
@@ -177,7 +181,7 @@ def sum_check():
     """vcc = some lane's part-of-unit sum exceeds 2^8: some logit may lie more than 8 above the reference (or the
     exponential overflowed), and nothing computed from these P has been used yet."""
     return [valu(f"v_max_f32 {V(TMP + 2)}, {V(LUNIT[0])}, {V(LUNIT[1])}", r=vr(LUNIT[0]) + vr(LUNIT[1]), w=vr(TMP + 2)),
-            valu(f"v_cmp_lt_f32 vcc, {SUM_LIMIT}, {V(TMP + 2)}", r=vr(TMP + 2), w=["vcc"], kind="vcmp")]
+            valu(f"v_cmp_lt_f32 vcc, {SUM_LIMIT_WINDOWED if WINDOWED else SUM_LIMIT}, {V(TMP + 2)}", r=vr(TMP + 2), w=["vcc"], kind="vcmp")]
 
 
 def sum_commit():
@@ -608,8 +612,7 @@ def prologue():
         e(valu(f"v_mov_b32 {V(LRUN[qt])}, 0", w=vr(LRUN[qt])))
     e(salu(f"s_mov_b32 {S(S_T)}, 0", w=sr(S_T)))
     if WINDOWED:
-        e(salu("s_cmp_eq_u32 %[nst], 0", w=["scc"]))
-        e(salu(f"s_cselect_b32 {S(S_K0N)}, %[start], 0", r=["scc"], w=sr(S_K0N)))
+        e(salu(f"s_mov_b32 {S(S_K0N)}, %[k00]", w=sr(S_K0N)))
     else:
         e(salu(f"s_mov_b32 {S(S_K0N)}, 0", w=sr(S_K0N)))
     e(raw("s_waitcnt vmcnt(24)", "wait"))       # the Query rows are there; the 24 tile loads may still be in flight
@@ -674,24 +677,58 @@ def epilogue():
         e(valu(f"v_add_f32 {V(l)}, {V(l)}, {V(t)}", r=vr(l) + vr(t), w=vr(l)))
         e(valu(f"v_rcp_f32 {V(inv)}, {V(l)}", r=vr(l), w=vr(inv), kind="trans"))
     e(nop(2))
+    if WINDOWED:
+        e(salu("s_cmp_lg_u32 %[split], 0", w=["scc"]))
+        e(branch("s_cbranch_scc1 PARTIAL"))
+
+    def row(qt, vg, dt, store):
+        """Four channels of the lane's row of sub-tile qt, in t .. t + 3."""
+        t = TMP + 8 + 4 * (vg & 1)
+        for k in range(4):
+            e(valu(f"v_accvgpr_read_b32 {V(t + k)}, {A(O_ACC + (dt * 2 + qt) * 16 + vg * 4 + k)}", r=ar(O_ACC + (dt * 2 + qt) * 16 + vg * 4 + k), w=vr(t + k)))
+        store(t, vg, dt)
+
+    def not_finite(t):
+        if WINDOWED:                     # stays 0 while everything is finite
+            for k in range(4):
+                e(valu(f"v_fma_f32 %[odd], {V(t + k)}, 0, %[odd]", r=vr(t + k)))
+
     for qt in (0, 1):
         inv = TMP + 4 + qt
+
+        def finished(t, vg, dt):
+            for k in range(4):
+                e(valu(f"v_mul_f32 {V(t + k)}, {V(t + k)}, {V(inv)}", r=vr(t + k) + vr(inv), w=vr(t + k)))
+            not_finite(t)
+            e(valu(f"v_cvt_pk_bf16_f32 {V(t)}, {V(t)}, {V(t + 1)}", r=vr(t, 2), w=vr(t)))
+            e(valu(f"v_cvt_pk_bf16_f32 {V(t + 1)}, {V(t + 2)}, {V(t + 3)}", r=vr(t + 2, 2), w=vr(t + 1)))
+            e(Ins(f"global_store_dwordx2 %[orow{qt}], {V(t, 2)}, off offset:{(dt * 32 + 8 * vg) * 2}", "vmem", r=vr(t, 2)))
         e(valu(f"v_cmp_ne_u32 vcc, 0, %[valid{qt}]", w=["vcc"], kind="vcmp"))
         e(raw(f"s_and_saveexec_b64 {S(S_SAVE, 2)}, vcc", "salu", r=["vcc"], w=sr(S_SAVE, 2) + ["exec"]))
         for dt in range(4):
-            o = O_ACC + (dt * 2 + qt) * 16
             for vg in range(4):
-                t = TMP + 8 + 4 * (vg & 1)
-                for k in range(4):
-                    e(valu(f"v_accvgpr_read_b32 {V(t + k)}, {A(o + vg * 4 + k)}", r=ar(o + vg * 4 + k), w=vr(t + k)))
-                for k in range(4):
-                    e(valu(f"v_mul_f32 {V(t + k)}, {V(t + k)}, {V(inv)}", r=vr(t + k) + vr(inv), w=vr(t + k)))
-                if WINDOWED:             # stays 0 while everything is finite
-                    for k in range(4):
-                        e(valu(f"v_fma_f32 %[odd], {V(t + k)}, 0, %[odd]", r=vr(t + k)))
-                e(valu(f"v_cvt_pk_bf16_f32 {V(t)}, {V(t)}, {V(t + 1)}", r=vr(t, 2), w=vr(t)))
-                e(valu(f"v_cvt_pk_bf16_f32 {V(t + 1)}, {V(t + 2)}, {V(t + 3)}", r=vr(t + 2, 2), w=vr(t + 1)))
-                e(Ins(f"global_store_dwordx2 %[orow{qt}], {V(t, 2)}, off offset:{(dt * 32 + 8 * vg) * 2}", "vmem", r=vr(t, 2)))
+                row(qt, vg, dt, finished)
+        e(raw(f"s_mov_b64 exec, {S(S_SAVE, 2)}", "salu", r=sr(S_SAVE, 2), w=["exec"]))
+    if not WINDOWED:
+        return out
+    e(branch("s_branch DONE"))
+    e(label("PARTIAL"))
+    for qt in (0, 1):
+        def partial(t, vg, dt):
+            not_finite(t)
+            e(Ins(f"global_store_dwordx4 %[orow{qt}], {V(t, 4)}, off offset:{(dt * 32 + 8 * vg) * 4}", "vmem", r=vr(t, 4)))
+        e(valu(f"v_mul_f32 {V(TMP + 6)}, %[scale], {V(REF[qt])}", r=vr(REF[qt]), w=vr(TMP + 6)))
+        e(valu(f"v_mov_b32 {V(TMP + 7)}, {V(LRUN[qt])}", r=vr(LRUN[qt]), w=vr(TMP + 7)))
+        e(valu(f"v_fma_f32 %[odd], {V(TMP + 7)}, 0, %[odd]", r=vr(TMP + 7)))
+        e(valu(f"v_cmp_ne_u32 vcc, 0, %[valid{qt}]", w=["vcc"], kind="vcmp"))
+        e(raw(f"s_and_saveexec_b64 {S(S_SAVE, 2)}, vcc", "salu", r=["vcc"], w=sr(S_SAVE, 2) + ["exec"]))
+        for dt in range(4):
+            for vg in range(4):
+                row(qt, vg, dt, partial)
+        e(valu("v_cmp_eq_u32 vcc, 0, %[hh4]", w=["vcc"], kind="vcmp"))          # the first of the row's two lanes: its address is the row's
+        e(nop(4))
+        e(raw("s_and_b64 exec, exec, vcc", "salu", r=["vcc"], w=["exec"]))
+        e(Ins(f"global_store_dwordx2 %[orow{qt}], {V(TMP + 6, 2)}, off offset:512", "vmem", r=vr(TMP + 6, 2)))
         e(raw(f"s_mov_b64 exec, {S(S_SAVE, 2)}", "salu", r=sr(S_SAVE, 2), w=["exec"]))
     return out
 

@@ -50,17 +50,17 @@ __device__ __forceinline__ bool odd_bits(const uint4& c, bf16_t) {
     return odd;
 }
 
-// Units u0, u0 + step, .. of the rows' keys.  p: position of row l16.
+// Units u0, u0 + step, .. of the keys [f0, f1) and [s0, s1), which hold what the rows see of some stretch.  p: position of row l16.
 template <typename T, int D>
-__device__ __forceinline__ void sliding_units(RowTile<T, D>& t, const T* __restrict__ k, const T* __restrict__ v, const SlidingRows& a, const SlidingSpan& sp, int p, int u0, int step,
-                                              unsigned tile) {
+__device__ __forceinline__ void sliding_units(RowTile<T, D>& t, const T* __restrict__ k, const T* __restrict__ v, const SlidingRows& a, const SlidingSpan& sp, int f0, int f1, int s0, int s1, int p,
+                                              int u0, int step, unsigned tile) {
     typedef RowTile<T, D> Tile;
     constexpr int NT = Tile::NT, NP = Tile::NP, KS = Tile::KS, V = Elem<T>::kVec, PC = 8 / V;      // 16-byte pieces of eight channels
     const int lane = threadIdx.x & 63, l16 = lane & 15, qr = lane >> 4;
     const size_t stride = (size_t)a.Hkv * D;
-    const int u_first = (sp.first + kTileKeys - 1) / kTileKeys, n_units = u_first + (sp.end - sp.start + kTileKeys - 1) / kTileKeys;
+    const int u_first = max(0, f1 - f0 + kTileKeys - 1) / kTileKeys, n_units = u_first + max(0, s1 - s0 + kTileKeys - 1) / kTileKeys;
     for (int u = u0; u < n_units; u += step) {
-        const int j0 = u < u_first ? u * kTileKeys : sp.start + (u - u_first) * kTileKeys, have = min(kTileKeys, (u < u_first ? sp.first : sp.end) - j0);
+        const int j0 = u < u_first ? f0 + u * kTileKeys : s0 + (u - u_first) * kTileKeys, have = min(kTileKeys, (u < u_first ? f1 : s1) - j0);
         uint4 kx[2][KS][PC], vx[2][KS][PC];
         size_t at[2];
 #pragma unroll
@@ -145,7 +145,7 @@ __global__ void __launch_bounds__(64 * kSlideWaves) sliding_rows_kernel(const T*
     const int r = min(r0 + l16, rows - 1), i = r / a.G;
     Tile t;
     t.begin(q + ((size_t)i * Hq + g * a.G + (r - i * a.G)) * D);
-    sliding_units<T, D>(t, k + (size_t)g * D, v + (size_t)g * D, a, sp, a.n_k - a.n_q + i, blockIdx.z * kSlideWaves + wave, gridDim.z * kSlideWaves,
+    sliding_units<T, D>(t, k + (size_t)g * D, v + (size_t)g * D, a, sp, 0, sp.first, sp.start, sp.end, a.n_k - a.n_q + i, blockIdx.z * kSlideWaves + wave, gridDim.z * kSlideWaves,
                         (unsigned)(uintptr_t)lds + wave * Tile::kLdsBytes);
     merge_waves<T, D, kSlideWaves>(t, lds, count, [&](int x, int dd, float acc, float l, float M) {
         const int i = (r0 + x) / a.G;
@@ -164,32 +164,48 @@ __global__ void __launch_bounds__(64 * kSlideWaves) sliding_rows_kernel(const T*
 // The loop of the prompt attention (gen_attn_asm.py, which says how it runs), over the tiles of 128 keys that the workgroup's rows see: those of the first tokens, if the stretch
 // leaves any behind, then the stretch.  Where the two would meet inside a tile the stretch begins at key 0 instead.
 constexpr int LD = 128, LW = 4, LKV = kSlideTile, LTILE_BYTES = LKV * LD * 2, LSTAGE_BYTES = 2 * LTILE_BYTES, LSTAGES = 2, LROWS = 64 * LW;
+constexpr int kPartRow = LD + 4;         // floats of a row's partial result (16-byte aligned)
 
 __global__ void __launch_bounds__(64 * LW) __attribute__((amdgpu_waves_per_eu(1, 1)))
-sliding_many_kernel(const bf16_t* __restrict__ Q, const bf16_t* __restrict__ Kg, const bf16_t* __restrict__ Vg, bf16_t* __restrict__ O, SlidingRows a, int n_rt) {
+sliding_many_kernel(const bf16_t* __restrict__ Q, const bf16_t* __restrict__ Kg, const bf16_t* __restrict__ Vg, bf16_t* __restrict__ O, SlidingRows a, int n_rt, int splits,
+                    float* __restrict__ part) {
     extern __shared__ __align__(16) unsigned char lds[];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), l32 = lane & 31, hh = lane >> 5;
-    // Workgroup -> (kv head, row tile): each XCD its own kv heads, whose keys then meet in one L2, the tiles with the most keys first.
+    // Workgroup -> (kv head, row tile, part of its keys): each XCD its own kv heads, whose keys then meet in one L2, the tiles with the most keys first.
     int g, rt;
     if (a.Hkv % 8 == 0) {
         const int j = blockIdx.x >> 3, per = a.Hkv >> 3;
         g = (blockIdx.x & 7) * per + j % per;
-        rt = n_rt - 1 - j / per;
+        rt = j / per;
     } else {
         g = blockIdx.x % a.Hkv;
-        rt = n_rt - 1 - blockIdx.x / a.Hkv;
+        rt = blockIdx.x / a.Hkv;
     }
+    const int split = rt % splits;
+    rt = n_rt - 1 - rt / splits;
     const int Hq = a.G * a.Hkv, rows = a.n_q * a.G, off = a.n_k - a.n_q, r0 = rt * LROWS, rw = r0 + wave * 64;
     const unsigned rowbytes = (unsigned)a.Hkv * LD * 2, tile_bytes = rowbytes * LKV;
     const SlidingSpan all(a, r0, LROWS), mine(a, min(rw, rows - 1), 64);
-    const SlidingTiles tl(all, a.window);
-    const int start = tl.start;
+    const SlidingTiles whole(all, a.window);
+    const int from = (int)((long long)split * whole.all / splits), to = (int)((long long)(split + 1) * whole.all / splits);
+    // a partial result: rows of kPartRow floats, the values, the reference and the sum
+    float* part_rows = part + ((size_t)split * a.Hkv + g) * rows * kPartRow;
+    if (from == to) {                                    // more parts than tiles: no keys
+        const int r = r0 + threadIdx.x;
+        if (r < rows) {
+            part_rows[(size_t)r * kPartRow + LD] = -INFINITY;
+            part_rows[(size_t)r * kPartRow + LD + 1] = 0.f;
+        }
+        return;
+    }
+    const SlidingTiles tl = whole.part(from, to);
+    const int start = tl.start, k00 = tl.k00;
     const unsigned nst = tl.apart, nkt = tl.all, nhead = tl.clean, nmain = tl.masked, last_tile = nkt - 1;
     const unsigned last_ragged = tl.left != LKV ? last_tile : 0xffffffffu, nl1 = tl.left - 1;   // rows of the last tile behind its keys repeat the last one
-    const uint64_t jump = (uint64_t)(start - (int)nst * LKV) * rowbytes;
+    const uint64_t jump = (uint64_t)(start - k00 - (int)nst * LKV) * rowbytes;
     const unsigned jump_lo = nst ? (unsigned)jump : 0, jump_hi = nst ? (unsigned)(jump >> 32) : 0;
-    const uint64_t kb = (uint64_t)(uintptr_t)(Kg + (size_t)g * LD) + (nst ? 0 : (uint64_t)start * rowbytes);
-    const uint64_t vb = (uint64_t)(uintptr_t)(Vg + (size_t)g * LD) + (nst ? 0 : (uint64_t)start * rowbytes);
+    const uint64_t kb = (uint64_t)(uintptr_t)(Kg + (size_t)g * LD) + (uint64_t)k00 * rowbytes;
+    const uint64_t vb = (uint64_t)(uintptr_t)(Vg + (size_t)g * LD) + (uint64_t)k00 * rowbytes;
     const unsigned kbase_lo = (unsigned)kb, kbase_hi = (unsigned)(kb >> 32), vbase_lo = (unsigned)vb, vbase_hi = (unsigned)(vb >> 32);
     const int qw0 = mine.p0, lowq = mine.p1 - a.window, window = a.window, sinks = a.sinks;
 
@@ -197,7 +213,8 @@ sliding_many_kernel(const bf16_t* __restrict__ Q, const bf16_t* __restrict__ Kg,
     const int ra = min(rw + l32, rows - 1), rb = min(rw + 32 + l32, rows - 1), ia = ra / a.G, ib = rb / a.G;
     const size_t qa = ((size_t)ia * Hq + g * a.G + (ra - ia * a.G)) * LD, qb = ((size_t)ib * Hq + g * a.G + (rb - ib * a.G)) * LD;
     const bf16_t *qrow0 = Q + qa + hh * 8, *qrow1 = Q + qb + hh * 8;
-    bf16_t *orow0 = O + qa + 4 * hh, *orow1 = O + qb + 4 * hh;
+    void *orow0 = splits > 1 ? (void*)(part_rows + (size_t)ra * kPartRow + 4 * hh) : O + qa + 4 * hh;
+    void *orow1 = splits > 1 ? (void*)(part_rows + (size_t)rb * kPartRow + 4 * hh) : O + qb + 4 * hh;
     const int hh4 = 4 * hh, limabs0 = off + ia - hh4, limabs1 = off + ib - hh4;
     const unsigned valid0 = rw + l32 < rows, valid1 = rw + 32 + l32 < rows;
     // Each row's product with its own token: a reference that is never minus infinity, whatever the first unit's mask leaves of the row.
@@ -216,7 +233,7 @@ sliding_many_kernel(const bf16_t* __restrict__ Q, const bf16_t* __restrict__ Kg,
     };
     // (with a first token in sight the first unit holds a key that every row sees; 4.7 us of a workgroup's 110 where that is not so)
     float own0 = -INFINITY, own1 = -INFINITY;
-    if (a.sinks == 0) { own0 = own_product(qrow0, ia); own1 = own_product(qrow1, ib); }
+    if (a.sinks == 0 || splits > 1) { own0 = own_product(qrow0, ia); own1 = own_product(qrow1, ib); }
 
     // LDS byte addresses of the lane's fragment reads and the operands of its tile loads, as the prompt attention's.
     auto k_at = [](int r, int c) { return (r * 16 + (c ^ (r & 15))) * 16; };
@@ -239,7 +256,8 @@ sliding_many_kernel(const bf16_t* __restrict__ Q, const bf16_t* __restrict__ Kg,
           [kbase_lo] "s"(kbase_lo), [kbase_hi] "s"(kbase_hi), [vbase_lo] "s"(vbase_lo), [vbase_hi] "s"(vbase_hi),
           [nkt] "s"(nkt), [nhead] "s"(nhead), [nmain] "s"(nmain), [nst] "s"(nst), [start] "s"(start), [last_tile] "s"(last_tile), [last_ragged] "s"(last_ragged),
           [rowbytes] "s"(rowbytes), [tile_bytes] "s"(tile_bytes), [jump_lo] "s"(jump_lo), [jump_hi] "s"(jump_hi), [scale] "s"(a.scale_log2e), [nl1] "s"(nl1),
-          [ldsw] "s"(ldsw), [qw0] "s"(qw0), [lowq] "s"(lowq), [window] "s"(window), [sinks] "s"(sinks)
+          [ldsw] "s"(ldsw), [qw0] "s"(qw0), [lowq] "s"(lowq), [window] "s"(window), [sinks] "s"(sinks), [k00] "s"(k00),
+          [split] "s"(splits - 1)
         :
 #include "sliding_bf16_clobbers.inc"
     );
@@ -256,29 +274,69 @@ sliding_many_kernel(const bf16_t* __restrict__ Q, const bf16_t* __restrict__ Kg,
         const size_t at = ((size_t)i * Hq + g * a.G + (r - i * a.G)) * LD;
         RowTile<bf16_t, LD> tile;
         tile.begin(Q + at);
-        sliding_units<bf16_t, LD>(tile, Kg + (size_t)g * LD, Vg + (size_t)g * LD, a, sp, off + i, 0, 1, lds_base + wave * RowTile<bf16_t, LD>::kLdsBytes);
+        // the keys of the workgroup's tiles, up to the row tile's last position
+        const int f0 = nst ? k00 : 0, f1 = nst ? min(sp.first, k00 + (int)nst * LKV) : 0;
+        const int s1 = min(sp.end, start + (int)(nkt - nst - 1) * LKV + tl.left);
+        sliding_units<bf16_t, LD>(tile, Kg + (size_t)g * LD, Vg + (size_t)g * LD, a, sp, f0, f1, start, s1, off + i, 0, 1, lds_base + wave * RowTile<bf16_t, LD>::kLdsBytes);
         tile.finish_sum();
-        if (first + l16 < rows)
+        if (first + l16 >= rows) continue;
+        if (splits > 1) {
+            float* dst = part_rows + (size_t)r * kPartRow;
+#pragma unroll
+            for (int dt = 0; dt < 8; ++dt) *reinterpret_cast<f32x4*>(dst + dt * 16 + qr * 4) = tile.o[dt];
+            if (qr == 0) { dst[LD] = tile.m; dst[LD + 1] = tile.l; }
+        } else {
 #pragma unroll
             for (int dt = 0; dt < 8; ++dt)
                 *reinterpret_cast<uint2*>(O + at + dt * 16 + qr * 4) = make_uint2(pack_bf16x2(tile.o[dt][0] / tile.l, tile.o[dt][1] / tile.l),
                                                                                   pack_bf16x2(tile.o[dt][2] / tile.l, tile.o[dt][3] / tile.l));
+        }
     }
 }
 
-static int launch_sliding_many(const void* q, const void* k, const void* v, const SlidingRows& a, void* out, hipStream_t st) {
+// part[split][kv head][row][kPartRow] -> out: 32 lanes a row, four channels each.
+__global__ void __launch_bounds__(256) sliding_merge_kernel(const float* __restrict__ part, int splits, SlidingRows a, bf16_t* __restrict__ out) {
+    const int rows = a.n_q * a.G, total = rows * a.Hkv, row = blockIdx.x * 8 + (threadIdx.x >> 5), c = (threadIdx.x & 31) * 4;
+    if (row >= total) return;
+    const float* p = part + (size_t)row * kPartRow;
+    const size_t step = (size_t)total * kPartRow;
+    float M = -INFINITY;
+    for (int s = 0; s < splits; ++s) M = fmaxf(M, p[s * step + LD]);
+    float l = 0.f;
+    f32x4 o = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll 4
+    for (int s = 0; s < splits; ++s) {
+        const float m = p[s * step + LD], sum = p[s * step + LD + 1];
+        const f32x4 v = *reinterpret_cast<const f32x4*>(p + s * step + c);
+        const float w = sum == 0.f ? 0.f : __builtin_amdgcn_exp2f(m - M);
+        l += w * sum;
+        if (sum != 0.f) o += w * v;                      // (what a part without keys left is not looked at)
+    }
+    const int g = row / rows, r = row - g * rows, i = r / a.G;
+    *reinterpret_cast<uint2*>(out + ((size_t)i * a.G * a.Hkv + g * a.G + (r - i * a.G)) * LD + c) = make_uint2(pack_bf16x2(o[0] / l, o[1] / l), pack_bf16x2(o[2] / l, o[3] / l));
+}
+
+static int launch_sliding_many(const void* q, const void* k, const void* v, const SlidingRows& a, int splits, void* out, float* part, hipStream_t st) {
     const int smem = LSTAGES * LSTAGE_BYTES;
     static std::once_flag once;
     static hipError_t err = hipSuccess;
     std::call_once(once, [&] { err = hipFuncSetAttribute((const void*)sliding_many_kernel, hipFuncAttributeMaxDynamicSharedMemorySize, smem); });
     if (err != hipSuccess) return set_hip_error(err);
     const int n_rt = (int)(((long long)a.n_q * a.G + LROWS - 1) / LROWS);
-    hipLaunchKernelGGL(sliding_many_kernel, dim3((unsigned)((long long)n_rt * a.Hkv)), dim3(64 * LW), smem, st, (const bf16_t*)q, (const bf16_t*)k, (const bf16_t*)v, (bf16_t*)out, a, n_rt);
+    hipLaunchKernelGGL(sliding_many_kernel, dim3((unsigned)((long long)n_rt * a.Hkv * splits)), dim3(64 * LW), smem, st, (const bf16_t*)q, (const bf16_t*)k, (const bf16_t*)v,
+                       (bf16_t*)out, a, n_rt, splits, part);
+    const int rc = check_launch();
+    if (rc || splits == 1) return rc;
+    hipLaunchKernelGGL(sliding_merge_kernel, dim3((unsigned)(((long long)a.n_q * a.G * a.Hkv + 7) / 8)), dim3(256), 0, st, part, splits, a, (bf16_t*)out);
     return check_launch();
 }
 
-// Whether a call runs in tiles of 256 rows.  (rowbytes and the 24-bit multiplies of the tile loads' offsets bound the number of kv heads.)
-static bool sliding_many(int n_q, int G, int Hkv, int dtype) { return dtype == SLIM_BF16 && Hkv <= 4096 && (long long)n_q * G >= LROWS; }
+// How a call runs in tiles of 256 rows: in how many parts a row tile's keys are dealt to workgroups.  0: in tiles of 16.  (rowbytes and the 24-bit multiplies of the tile loads'
+// offsets bound the number of kv heads.)
+static int sliding_many(int n_q, int n_k, int G, int Hkv, int window, int sinks, int dtype) {
+    if (dtype != SLIM_BF16 || Hkv > 4096) return 0;
+    return (long long)n_q * G >= LROWS ? sliding_parts(n_q, n_k, G, Hkv, std::min(window, n_k), std::min(sinks, n_k)) : 0;
+}
 
 // Workgroups per row tile: about kSlideWgs in all, every wave the same number of units where that can be.
 constexpr int kSlideWgs = 512;
@@ -292,7 +350,7 @@ static int sliding_splits(int n_q, int n_k, int G, int Hkv, int window, int sink
 }
 
 size_t sliding_workspace_floats(int n_q, int n_k, int Hq, int Hkv, int d, int window, int sinks, int dtype) {
-    if (sliding_many(n_q, Hq / Hkv, Hkv, dtype)) return 0;
+    if (const int parts = sliding_many(n_q, n_k, Hq / Hkv, Hkv, window, sinks, dtype)) return parts > 1 ? (size_t)parts * n_q * Hq * kPartRow : 0;
     const int splits = sliding_splits(n_q, n_k, Hq / Hkv, Hkv, window, sinks);
     return splits > 1 ? (size_t)splits * n_q * Hq * (d + 2) : 0;
 }
@@ -301,7 +359,7 @@ int launch_sliding_attn(const void* q, const void* k, const void* v, int n_q, in
                         float* part, hipStream_t st) {
     // a window or a number of first tokens beyond the keys is all of them
     const SlidingRows a{n_q, n_k, Hq / Hkv, Hkv, std::min(window, n_k), std::min(sinks, n_k), scale * 1.4426950408889634f};
-    if (sliding_many(n_q, a.G, Hkv, dtype)) return launch_sliding_many(q, k, v, a, out, st);
+    if (const int parts = sliding_many(n_q, n_k, a.G, Hkv, window, sinks, dtype)) return launch_sliding_many(q, k, v, a, parts, out, part, st);
     const int splits = sliding_splits(n_q, n_k, a.G, Hkv, window, sinks);
     const long long tiles = ((long long)n_q * a.G + kTileRows - 1) / kTileRows;
     const dim3 grid((unsigned)tiles, Hkv, splits);
