@@ -233,26 +233,31 @@ __global__ void __launch_bounds__(64 * kQ4Waves) decode_attn_kv4_kernel(
 #pragma unroll
         for (int h = 0; h < 2; ++h)
 #pragma unroll
-            for (int e = 0; e < 4; ++e) s[h][e] = h * 16 + qr * 4 + e < have ? s[h][e] * scale_log2e : -INFINITY;
+            for (int e = 0; e < 4; ++e) {
+                const float x = s[h][e];
+                s[h][e] = h * 16 + qr * 4 + e < have ? x : -INFINITY;
+            }
     };
     while (more) {
         const int have = rows;
         ui += step;
         more = find();                                   // none left: the last unit is requested once more, and not used
-        f32x4 s[2] = {{0.f, 0.f, 0.f, 0.f}, {0.f, 0.f, 0.f, 0.f}};
+        f32x4 s[2];
 #pragma unroll
         for (int h = 0; h < 2; ++h) {
+            typename Tile::Scores sum;
             const uint32_t c[4] = {kx[h].x, kx[h].y, kx[h].z, kx[h].w};
             const float sc = kv4_scale(ks[h]);
 #pragma unroll
             for (int j = 0; j < 4; ++j) {
                 const bf16x8 k = kv4_to_bf16(c[j], sc);
-                t.template add_scores<1>(&k, j, s[h]);
+                t.template add_scores<1>(&k, j, sum);
             }
+            s[h] = sum.sum();
         }
         load_k();
         masked(s, have);
-        t.weigh(s, w);
+        t.weigh(s, scale_log2e, w);
         bf16_terms<NP>(w, p);
 #pragma unroll
         for (int h = 0; h < 2; ++h) {
@@ -268,20 +273,22 @@ __global__ void __launch_bounds__(64 * kQ4Waves) decode_attn_kv4_kernel(
     const size_t row_stride = (size_t)Hkv * D;
     for (; ui < n_units; ui += step) {
         const int first = (ui - n_in_slots) * kTileKeys, have = min(kTileKeys, n_resp - first);
-        f32x4 s[2] = {{0.f, 0.f, 0.f, 0.f}, {0.f, 0.f, 0.f, 0.f}};
+        f32x4 s[2];
         size_t at[2];
 #pragma unroll
         for (int h = 0; h < 2; ++h) {
+            typename Tile::Scores sum;
             at[h] = (size_t)(first + min(l16 + 16 * h, have - 1)) * row_stride + (size_t)g * D + qr * 32;
 #pragma unroll
             for (int j = 0; j < 4; ++j) {
                 bf16x8 k[NT];
                 row_terms<T, NT>(k_resp + at[h] + j * 8, k);
-                t.template add_scores<NT>(k, j, s[h]);
+                t.template add_scores<NT>(k, j, sum);
             }
+            s[h] = sum.sum();
         }
         masked(s, have);
-        t.weigh(s, w);
+        t.weigh(s, scale_log2e, w);
         bf16_terms<NP>(w, p);
         bf16x8 v[2][4][NT];
 #pragma unroll
@@ -309,51 +316,78 @@ __global__ void __launch_bounds__(64 * kQ4Waves) decode_attn_kv4_kernel(
     });
 }
 
-// 1024 threads a row: 1024 / D groups of D channels, group j the partials j, j + groups, ..; everything is requested at once.
-template <typename T, int D>
-__global__ void __launch_bounds__(1024) merge_rows_kernel(const float* __restrict__ part, int n_parts, int rows, T* __restrict__ out) {
-    constexpr int NG = 1024 / D, PER = kMergeParts / NG;
-    __shared__ float wts[kMergeParts], wred[2][kMergeParts / 64], accs[NG][D];
-    const int row = blockIdx.x, tid = threadIdx.x, grp = tid / D, dd = tid % D;
-    auto item = [&](int i) { return part + ((size_t)min(i, n_parts - 1) * rows + row) * (D + 2); };
-    float val[PER];
+// A row takes NG groups of D / 4 lanes, four channels each; group j has the partials j, j + NG, ..  Everything is requested at once: the launch is one trip to memory.
+constexpr int kMergeMost = 16;                           // partials of a group
+template <typename T, int D, int NG>
+__global__ void __launch_bounds__(256) merge_rows_kernel(const float* __restrict__ part, int n_parts, int rows, T* __restrict__ out) {
+    constexpr int LN = D / 4, PER_WG = 256 / (LN * NG);
+    static_assert(NG * kMergeMost >= (NG == 1 ? 1 : kMergeParts) && PER_WG >= 1, "all partials, within a workgroup");
+    __shared__ float ms[NG][PER_WG], ls[NG][PER_WG];
+    __shared__ __align__(16) float os[NG][PER_WG][D];
+    const int tid = threadIdx.x, lane = tid % LN, grp = tid / LN % NG, x = tid / (LN * NG), row = blockIdx.x * PER_WG + x;
+    const float* p = part + (size_t)min(row, rows - 1) * (D + 2);
+    const size_t step = (size_t)rows * (D + 2);
+    float m[kMergeMost], l[kMergeMost], M = -INFINITY;
+    float2 v[kMergeMost][2];                             // (rows of D + 2 floats are aligned to eight bytes)
 #pragma unroll
-    for (int i = 0; i < PER; ++i) val[i] = grp + i * NG < n_parts ? item(grp + i * NG)[dd] : 0.f;
-    float m = -INFINITY, l = 0.f;
-    if (tid < kMergeParts) {
-        if (tid < n_parts) { m = item(tid)[D]; l = item(tid)[D + 1]; }
-        const float wm = wave_max(m);
-        if ((tid & 63) == 0) wred[0][tid >> 6] = wm;
+    for (int i = 0; i < kMergeMost; ++i) {
+        const int at = grp + i * NG;
+        m[i] = -INFINITY;
+        l[i] = 0.f;
+        v[i][0] = v[i][1] = make_float2(0.f, 0.f);
+        if (at < n_parts) {
+            const float* r = p + at * step;
+            const float2 st = *reinterpret_cast<const float2*>(r + D);
+            v[i][0] = *reinterpret_cast<const float2*>(r + lane * 4);
+            v[i][1] = *reinterpret_cast<const float2*>(r + lane * 4 + 2);
+            m[i] = st.x;
+            l[i] = st.y;
+        }
     }
-    __syncthreads();
-    const float M = fmaxf(wred[0][0], wred[0][1]);
-    if (tid < kMergeParts) {
-        const float w = l == 0.f ? 0.f : __builtin_amdgcn_exp2f(m - M);      // a partial without keys has no weight
-        wts[tid] = w;
-        const float ws = wave_sum(w * l);
-        if ((tid & 63) == 0) wred[1][tid >> 6] = ws;
-    }
-    __syncthreads();
-    float acc = 0.f;
 #pragma unroll
-    for (int i = 0; i < PER; ++i) acc += grp + i * NG < n_parts ? wts[grp + i * NG] * val[i] : 0.f;
-    accs[grp][dd] = acc;
-    __syncthreads();
-    if (grp == 0) {
-        float a = 0.f;
+    for (int i = 0; i < kMergeMost; ++i) M = fmaxf(M, m[i]);
+    if constexpr (NG > 1) {
+        if (lane == 0) ms[grp][x] = M;
+        __syncthreads();
 #pragma unroll
-        for (int i = 0; i < NG; ++i) a += accs[i][dd];
-        const float sum = wred[1][0] + wred[1][1];
-        Elem<T>::st(out + (size_t)row * D + dd, sum == 0.f ? 0.f : a / sum);
+        for (int i = 0; i < NG; ++i) M = fmaxf(M, ms[i][x]);
     }
+    float sum = 0.f, o[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+    for (int i = 0; i < kMergeMost; ++i) {
+        const float w = l[i] == 0.f ? 0.f : __builtin_amdgcn_exp2f(m[i] - M);      // a partial without keys has no weight
+        sum += w * l[i];
+        o[0] += w * v[i][0].x;
+        o[1] += w * v[i][0].y;
+        o[2] += w * v[i][1].x;
+        o[3] += w * v[i][1].y;
+    }
+    if constexpr (NG > 1) {
+        if (lane == 0) ls[grp][x] = sum;
+        *reinterpret_cast<f32x4*>(&os[grp][x][lane * 4]) = f32x4{o[0], o[1], o[2], o[3]};
+        __syncthreads();
+        if (grp != 0) return;
+#pragma unroll
+        for (int g = 1; g < NG; ++g) {
+            sum += ls[g][x];
+#pragma unroll
+            for (int e = 0; e < 4; ++e) o[e] += os[g][x][lane * 4 + e];
+        }
+    }
+    if (row >= rows) return;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) Elem<T>::st(out + (size_t)row * D + lane * 4 + e, sum == 0.f ? 0.f : o[e] / sum);
 }
 
 int launch_merge_rows(const float* part, int n_parts, int rows, int d, int dtype, void* out, hipStream_t st) {
-#define SLIM_MERGE(T, D) hipLaunchKernelGGL((merge_rows_kernel<T, D>), dim3(rows), dim3(1024), 0, st, part, n_parts, rows, (T*)out)
-    if (dtype == SLIM_BF16) SLIM_MERGE(bf16_t, 128);
-    else if (d == 32) SLIM_MERGE(float, 32);
-    else if (d == 64) SLIM_MERGE(float, 64);
-    else SLIM_MERGE(float, 128);
+#define SLIM_MERGE(T, D, NG) do { constexpr int per = 256 / (D / 4 * NG); \
+        hipLaunchKernelGGL((merge_rows_kernel<T, D, NG>), dim3((rows + per - 1) / per), dim3(256), 0, st, part, n_parts, rows, (T*)out); } while (0)
+#define SLIM_MERGE_D(T, D) do { if (n_parts <= kMergeMost) SLIM_MERGE(T, D, 1); else SLIM_MERGE(T, D, 8); } while (0)
+    if (dtype == SLIM_BF16) SLIM_MERGE_D(bf16_t, 128);
+    else if (d == 32) SLIM_MERGE_D(float, 32);
+    else if (d == 64) SLIM_MERGE_D(float, 64);
+    else SLIM_MERGE_D(float, 128);
+#undef SLIM_MERGE_D
 #undef SLIM_MERGE
     return check_launch();
 }

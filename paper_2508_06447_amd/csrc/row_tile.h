@@ -87,7 +87,7 @@ template <typename T, int D> struct RowTile {
     static constexpr int kLdsBytes = kTileKeys * D * 2;  // of a wave's V tile
     bf16x8 q[NT][KS];
     f32x4 o[DT];                                         // channel dt * 16 + 4 qr + e of row l16
-    float m, l;                                          // of row l16: maximum (base-2 domain), the lane's share of the sum
+    float m, mc, l;                                      // of row l16: largest score, that in the base-2 domain, the lane's share of the sum
 
     __device__ __forceinline__ void begin(const T* q_row) {          // of row l16
         const int qr = (threadIdx.x & 63) >> 4;
@@ -101,32 +101,44 @@ template <typename T, int D> struct RowTile {
 #pragma unroll
         for (int dt = 0; dt < DT; ++dt) o[dt] = f32x4{0.f, 0.f, 0.f, 0.f};
         m = -INFINITY;
-        l = 0.f;
+        mc = l = 0.f;
     }
-    // s += K . Q^T over the eight channels of step j; k: NK terms of them.
-    template <int NK> __device__ __forceinline__ void add_scores(const bf16x8* k, int j, f32x4& s) const {
+    // Scores of 16 keys, from zero.  The products of first terms and the others are summed apart: among the large sums these would be rounded to their last place each time.
+    struct Scores {
+        f32x4 first = {0.f, 0.f, 0.f, 0.f}, rest = {0.f, 0.f, 0.f, 0.f};
+        __device__ __forceinline__ f32x4 sum() const {
+            if constexpr (NT == 1) return first;
+            else return first + rest;
+        }
+    };
+    // += K . Q^T over the eight channels of step j; k: NK terms of them.
+    template <int NK> __device__ __forceinline__ void add_scores(const bf16x8* k, int j, Scores& s) const {
 #pragma unroll
         for (int a = NK - 1; a >= 0; --a)
 #pragma unroll
             for (int b = NT - 1; b >= 0; --b)
-                if (a + b < 3) s = __builtin_amdgcn_mfma_f32_16x16x32_bf16(k[a], q[b][j], s, 0, 0, 0);
+                if (a + b == 0) s.first = __builtin_amdgcn_mfma_f32_16x16x32_bf16(k[a], q[b][j], s.first, 0, 0, 0);
+                else if (a + b < 3) s.rest = __builtin_amdgcn_mfma_f32_16x16x32_bf16(k[a], q[b][j], s.rest, 0, 0, 0);
     }
-    // Scores in the base-2 domain, -infinity for keys that row l16 does not see -> weights, relative to the running maximum, which O and the sum follow.
-    __device__ __forceinline__ void weigh(f32x4* s, float* w) {
+    // Scores of 32 keys, -infinity for those that row l16 does not see -> weights 2^(c s - mc) relative to the running maximum, which O and the sum follow.  The maximum is rounded
+    // into the base-2 domain once and the difference from it once, where it is small: an error of the former is common to all weights of the row, and what the
+    // reference leaves behind is rescaled by the difference of the rounded ones.
+    __device__ __forceinline__ void weigh(const f32x4* s, float c, float* w) {
         float mx = fmaxf(fmaxf(fmaxf(s[0][0], s[0][1]), fmaxf(s[0][2], s[0][3])), fmaxf(fmaxf(s[1][0], s[1][1]), fmaxf(s[1][2], s[1][3])));
         mx = fmaxf(m, max_over_rows(mx));
-        const float ref = mx == -INFINITY ? 0.f : mx;    // (a row that has seen no key yet)
         if (__any(mx > m)) {
-            const float al = __builtin_amdgcn_exp2f(m - ref);
+            const float now = mx == -INFINITY ? 0.f : mx * c;        // (a row that has seen no key yet)
+            const float al = m == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(mc - now);
             l *= al;
 #pragma unroll
             for (int dt = 0; dt < DT; ++dt) o[dt] *= al;
             m = mx;
+            mc = now;
         }
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
-            w[e] = __builtin_amdgcn_exp2f(s[0][e] - ref);
-            w[4 + e] = __builtin_amdgcn_exp2f(s[1][e] - ref);
+            w[e] = __builtin_amdgcn_exp2f(fmaf(s[0][e], c, -mc));
+            w[4 + e] = __builtin_amdgcn_exp2f(fmaf(s[1][e], c, -mc));
         }
         l += ((w[0] + w[1]) + (w[2] + w[3])) + ((w[4] + w[5]) + (w[6] + w[7]));
     }
@@ -141,11 +153,20 @@ template <typename T, int D> struct RowTile {
             const bf16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4bf16((LdsB64)at);
             const bf16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4bf16((LdsB64)(at + 16 * D * 2));
             const bf16x8 v = __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
+            if constexpr (NT == 1) {
 #pragma unroll
-            for (int b = NP - 1; b >= 0; --b)
-                if (a + b < 3) o[dt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(v, p[b], o[dt], 0, 0, 0);
+                for (int b = NP - 1; b >= 0; --b) o[dt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(v, p[b], o[dt], 0, 0, 0);
+            } else {                                     // float32: the terms' sum is rounded into the running values once
+                f32x4 x = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+                for (int b = NP - 1; b >= 0; --b)
+                    if (a + b < 3) x = __builtin_amdgcn_mfma_f32_16x16x32_bf16(v, p[b], x, 0, 0, 0);
+                o[dt] += x;
+            }
         }
     }
+    // What the weights of row l16 are relative to, in the base-2 domain.
+    __device__ __forceinline__ float reference() const { return m == -INFINITY ? m : mc; }
     // The row's sum in each of its four lanes, at the end.
     __device__ __forceinline__ void finish_sum() {
         l += __shfl_xor(l, 16, 64);
@@ -161,7 +182,7 @@ template <typename T, int D, int NW, typename F> __device__ __forceinline__ void
     __shared__ float ws_m[NW][kTileRows], ws_l[NW][kTileRows];
     const int lane = threadIdx.x & 63, l16 = lane & 15, qr = lane >> 4, wave = threadIdx.x >> 6;
     t.finish_sum();
-    if (lane < kTileRows) { ws_m[wave][lane] = t.m; ws_l[wave][lane] = t.l; }
+    if (lane < kTileRows) { ws_m[wave][lane] = t.reference(); ws_l[wave][lane] = t.l; }
     float* mine = reinterpret_cast<float*>(lds + wave * Tile::kLdsBytes);
 #pragma unroll
     for (int dt = 0; dt < Tile::DT; ++dt) *reinterpret_cast<f32x4*>(mine + l16 * D + (((dt * 4 + qr) ^ (l16 & (D / 4 - 1))) << 2)) = t.o[dt];

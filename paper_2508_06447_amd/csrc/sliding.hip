@@ -11,7 +11,18 @@
 
 namespace slim {
 
-// ---- few rows: 16 of them per workgroup, the units of 32 keys dealt to its waves and to gridDim.z workgroups
+// Workgroup -> (kv head, number within it): each XCD its own kv heads where they divide over the XCDs, so that a head's keys meet in one L2.
+__device__ __forceinline__ int own_kv_head(int Hkv, int& number) {
+    if (Hkv % 8 == 0) {
+        const int j = blockIdx.x >> 3, per = Hkv >> 3;
+        number = j / per;
+        return (blockIdx.x & 7) * per + j % per;
+    }
+    number = blockIdx.x / Hkv;
+    return blockIdx.x % Hkv;
+}
+
+// ---- few rows: 16 of them per workgroup, the units of 32 keys dealt to its waves and to `splits` workgroups
 constexpr int kSlideWaves = 4;
 
 // Values of keys of the unit that some row does not see may be infinite or undefined: their weight is 0, which a product would turn into an undefined sum.  The unit's values
@@ -87,23 +98,32 @@ __device__ __forceinline__ void sliding_units(RowTile<T, D>& t, const T* __restr
                 bf16_terms<NT>(f, x);
             }
         };
-        f32x4 s[2] = {{0.f, 0.f, 0.f, 0.f}, {0.f, 0.f, 0.f, 0.f}};
+        f32x4 s[2];
 #pragma unroll
-        for (int h = 0; h < 2; ++h)
+        for (int h = 0; h < 2; ++h) {
+            typename Tile::Scores sum;
 #pragma unroll
             for (int j = 0; j < KS; ++j) {
                 bf16x8 x[NT];
                 terms(kx[h][j], x);
-                t.template add_scores<NT>(x, j, s[h]);
+                t.template add_scores<NT>(x, j, sum);
             }
+            s[h] = sum.sum();
+        }
         const bool whole = have == kTileKeys && j0 + kTileKeys - 1 <= sp.p0 && (j0 > sp.p1 - a.window || j0 + kTileKeys <= a.sinks);      // every row sees every key
-        auto sees = [&](int key) { const int j = j0 + key; return key < have && j <= p && (j > p - a.window || j < a.sinks); };
+        // (without branches: nothing but comparisons and selections)
+        auto sees = [&](int key) { const int j = j0 + key; return (key < have) & (j <= p) & ((j > p - a.window) | (j < a.sinks)); };
+        if (!whole) {
 #pragma unroll
-        for (int h = 0; h < 2; ++h)
+            for (int h = 0; h < 2; ++h)
 #pragma unroll
-            for (int e = 0; e < 4; ++e) s[h][e] = whole || sees(h * 16 + qr * 4 + e) ? s[h][e] * a.scale_log2e : -INFINITY;
+                for (int e = 0; e < 4; ++e) {
+                    const float x = s[h][e];
+                    s[h][e] = sees(h * 16 + qr * 4 + e) ? x : -INFINITY;
+                }
+        }
         float w[8];
-        t.weigh(s, w);
+        t.weigh(s, a.scale_log2e, w);
         if (!whole) {
             bool odd = false;
 #pragma unroll
@@ -135,25 +155,28 @@ __device__ __forceinline__ void sliding_units(RowTile<T, D>& t, const T* __restr
 }
 
 template <typename T, int D>
-__global__ void __launch_bounds__(64 * kSlideWaves) sliding_rows_kernel(const T* __restrict__ q, const T* __restrict__ k, const T* __restrict__ v, SlidingRows a, T* __restrict__ out,
-                                                                        float* __restrict__ part) {
+__global__ void __launch_bounds__(64 * kSlideWaves) sliding_rows_kernel(const T* __restrict__ q, const T* __restrict__ k, const T* __restrict__ v, SlidingRows a, int n_rt, int splits,
+                                                                        T* __restrict__ out, float* __restrict__ part) {
     typedef RowTile<T, D> Tile;
     __shared__ __align__(16) unsigned char lds[kSlideWaves * Tile::kLdsBytes];
-    const int g = blockIdx.y, lane = threadIdx.x & 63, l16 = lane & 15, Hq = a.G * a.Hkv, rows = a.n_q * a.G;
-    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), r0 = blockIdx.x * kTileRows, count = min(kTileRows, rows - r0);
+    int rt;
+    const int g = own_kv_head(a.Hkv, rt), split = rt / n_rt;         // (row tiles that read the same keys side by side)
+    rt -= split * n_rt;
+    const int lane = threadIdx.x & 63, l16 = lane & 15, Hq = a.G * a.Hkv, rows = a.n_q * a.G;
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), r0 = rt * kTileRows, count = min(kTileRows, rows - r0);
     const SlidingSpan sp(a, r0, count);
     const int r = min(r0 + l16, rows - 1), i = r / a.G;
     Tile t;
     t.begin(q + ((size_t)i * Hq + g * a.G + (r - i * a.G)) * D);
-    sliding_units<T, D>(t, k + (size_t)g * D, v + (size_t)g * D, a, sp, 0, sp.first, sp.start, sp.end, a.n_k - a.n_q + i, blockIdx.z * kSlideWaves + wave, gridDim.z * kSlideWaves,
+    sliding_units<T, D>(t, k + (size_t)g * D, v + (size_t)g * D, a, sp, 0, sp.first, sp.start, sp.end, a.n_k - a.n_q + i, split * kSlideWaves + wave, splits * kSlideWaves,
                         (unsigned)(uintptr_t)lds + wave * Tile::kLdsBytes);
     merge_waves<T, D, kSlideWaves>(t, lds, count, [&](int x, int dd, float acc, float l, float M) {
         const int i = (r0 + x) / a.G;
         const size_t row = (size_t)i * Hq + g * a.G + (r0 + x - i * a.G);
-        if (gridDim.z == 1) {
+        if (splits == 1) {
             Elem<T>::st(out + row * D + dd, acc / l);
         } else {
-            float* dst = part + ((size_t)blockIdx.z * a.n_q * Hq + row) * (D + 2);
+            float* dst = part + ((size_t)split * a.n_q * Hq + row) * (D + 2);
             dst[dd] = acc;
             if (dd == 0) { dst[D] = M; dst[D + 1] = l; }
         }
@@ -172,15 +195,8 @@ sliding_many_kernel(const bf16_t* __restrict__ Q, const bf16_t* __restrict__ Kg,
     extern __shared__ __align__(16) unsigned char lds[];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), l32 = lane & 31, hh = lane >> 5;
     // Workgroup -> (kv head, row tile, part of its keys): each XCD its own kv heads, whose keys then meet in one L2, the tiles with the most keys first.
-    int g, rt;
-    if (a.Hkv % 8 == 0) {
-        const int j = blockIdx.x >> 3, per = a.Hkv >> 3;
-        g = (blockIdx.x & 7) * per + j % per;
-        rt = j / per;
-    } else {
-        g = blockIdx.x % a.Hkv;
-        rt = blockIdx.x / a.Hkv;
-    }
+    int rt;
+    const int g = own_kv_head(a.Hkv, rt);
     const int split = rt % splits;
     rt = n_rt - 1 - rt / splits;
     const int Hq = a.G * a.Hkv, rows = a.n_q * a.G, off = a.n_k - a.n_q, r0 = rt * LROWS, rw = r0 + wave * 64;
@@ -284,7 +300,7 @@ sliding_many_kernel(const bf16_t* __restrict__ Q, const bf16_t* __restrict__ Kg,
             float* dst = part_rows + (size_t)r * kPartRow;
 #pragma unroll
             for (int dt = 0; dt < 8; ++dt) *reinterpret_cast<f32x4*>(dst + dt * 16 + qr * 4) = tile.o[dt];
-            if (qr == 0) { dst[LD] = tile.m; dst[LD + 1] = tile.l; }
+            if (qr == 0) { dst[LD] = tile.reference(); dst[LD + 1] = tile.l; }
         } else {
 #pragma unroll
             for (int dt = 0; dt < 8; ++dt)
@@ -331,39 +347,30 @@ static int launch_sliding_many(const void* q, const void* k, const void* v, cons
     return check_launch();
 }
 
-// How a call runs in tiles of 256 rows: in how many parts a row tile's keys are dealt to workgroups.  0: in tiles of 16.  (rowbytes and the 24-bit multiplies of the tile loads'
-// offsets bound the number of kv heads.)
-static int sliding_many(int n_q, int n_k, int G, int Hkv, int window, int sinks, int dtype) {
-    if (dtype != SLIM_BF16 || Hkv > 4096) return 0;
-    return (long long)n_q * G >= LROWS ? sliding_parts(n_q, n_k, G, Hkv, std::min(window, n_k), std::min(sinks, n_k)) : 0;
+// In how many parts a call's tiles of 256 rows run, 0: in tiles of 16.  (rowbytes and the 24-bit multiplies of the tile loads' offsets bound the number of kv heads.)
+static int sliding_many(const SlidingRows& a, int dtype) {
+    return dtype == SLIM_BF16 && a.Hkv <= 4096 ? sliding_parts(a.n_q, a.n_k, a.G, a.Hkv, a.window, a.sinks) : 0;
 }
-
-// Workgroups per row tile: about kSlideWgs in all, every wave the same number of units where that can be.
-constexpr int kSlideWgs = 512;
-static int sliding_splits(int n_q, int n_k, int G, int Hkv, int window, int sinks) {
-    const long long tiles = ((long long)n_q * G + kTileRows - 1) / kTileRows * Hkv;
-    const long long near = std::min<long long>(n_k, (long long)window + std::min<long long>(n_q, (kTileRows + G - 1) / G + 1));
-    const long long units = (near + kTileKeys - 1) / kTileKeys + (std::min<long long>(sinks, n_k) + kTileKeys - 1) / kTileKeys;
-    const long long most = std::max<long long>(1, std::min<long long>(kMergeParts, kSlideWgs / tiles));
-    const long long rounds = std::max<long long>(1, (units + kSlideWaves * most - 1) / (kSlideWaves * most));
-    return (int)std::max<long long>(1, std::min(most, (units + kSlideWaves * rounds - 1) / (kSlideWaves * rounds)));
+// (a window or a number of first tokens beyond the keys is all of them)
+static SlidingRows sliding_rows(int n_q, int n_k, int Hq, int Hkv, int window, int sinks, float scale) {
+    return SlidingRows{n_q, n_k, Hq / Hkv, Hkv, std::min(window, n_k), std::min(sinks, n_k), scale * 1.4426950408889634f};
 }
 
 size_t sliding_workspace_floats(int n_q, int n_k, int Hq, int Hkv, int d, int window, int sinks, int dtype) {
-    if (const int parts = sliding_many(n_q, n_k, Hq / Hkv, Hkv, window, sinks, dtype)) return parts > 1 ? (size_t)parts * n_q * Hq * kPartRow : 0;
-    const int splits = sliding_splits(n_q, n_k, Hq / Hkv, Hkv, window, sinks);
+    const SlidingRows a = sliding_rows(n_q, n_k, Hq, Hkv, window, sinks, 0.f);
+    if (const int parts = sliding_many(a, dtype)) return parts > 1 ? (size_t)parts * n_q * Hq * kPartRow : 0;
+    const int splits = sliding_splits(n_q, n_k, a.G, Hkv, a.window, a.sinks, kMergeParts);
     return splits > 1 ? (size_t)splits * n_q * Hq * (d + 2) : 0;
 }
 
 int launch_sliding_attn(const void* q, const void* k, const void* v, int n_q, int n_k, int Hq, int Hkv, int d, int window, int sinks, float scale, int dtype, void* out,
                         float* part, hipStream_t st) {
-    // a window or a number of first tokens beyond the keys is all of them
-    const SlidingRows a{n_q, n_k, Hq / Hkv, Hkv, std::min(window, n_k), std::min(sinks, n_k), scale * 1.4426950408889634f};
-    if (const int parts = sliding_many(n_q, n_k, a.G, Hkv, window, sinks, dtype)) return launch_sliding_many(q, k, v, a, parts, out, part, st);
-    const int splits = sliding_splits(n_q, n_k, a.G, Hkv, window, sinks);
+    const SlidingRows a = sliding_rows(n_q, n_k, Hq, Hkv, window, sinks, scale);
+    if (const int parts = sliding_many(a, dtype)) return launch_sliding_many(q, k, v, a, parts, out, part, st);
+    const int splits = sliding_splits(n_q, n_k, a.G, Hkv, a.window, a.sinks, kMergeParts);
     const long long tiles = ((long long)n_q * a.G + kTileRows - 1) / kTileRows;
-    const dim3 grid((unsigned)tiles, Hkv, splits);
-#define SLIM_SLIDE(T, D) hipLaunchKernelGGL((sliding_rows_kernel<T, D>), grid, dim3(64 * kSlideWaves), 0, st, (const T*)q, (const T*)k, (const T*)v, a, (T*)out, part)
+    const dim3 grid((unsigned)(tiles * Hkv * splits));
+#define SLIM_SLIDE(T, D) hipLaunchKernelGGL((sliding_rows_kernel<T, D>), grid, dim3(64 * kSlideWaves), 0, st, (const T*)q, (const T*)k, (const T*)v, a, (int)tiles, splits, (T*)out, part)
     if (dtype == SLIM_BF16) SLIM_SLIDE(bf16_t, 128);
     else if (d == 32) SLIM_SLIDE(float, 32);
     else if (d == 64) SLIM_SLIDE(float, 64);

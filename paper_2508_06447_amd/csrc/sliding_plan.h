@@ -57,21 +57,49 @@ struct SlidingTiles {
     }
 };
 
-// In how many parts the keys of a row tile of 256 rows are dealt to workgroups (host).  One CU holds one workgroup, 256 of them run at once; a workgroup takes 12 us and 2.8 us a tile;
-// parts are written and read once more, 528 bytes a row, in a launch of 5 us.
-inline double sliding_parts_us(long long row_tiles, long long tiles, long long rows, int parts) {
-    const long long rounds = (row_tiles * parts + 255) / 256;
+// ---- which kernel, and over how many workgroups a tile's keys are dealt (host).  us, bfloat16, 32 / 8 heads of 128, window 4096, 64 first tokens, behind 8192 tokens.
+// Keys that a tile of `rows` rows reads, the first tokens apart.
+inline long long sliding_keys(int n_q, int n_k, int G, int window, int rows) {
+    const long long span = rows / G + 1 < n_q ? rows / G + 1 : n_q;                    // its queries, about
+    return window + span < n_k ? window + span : n_k;
+}
+
+// Tiles of 16 rows: 32-key units of a tile.  A wave's unit is 16 KB of keys and values, and what bounds these tiles is how fast the CUs take them: 1.8 ns a unit over the whole
+// chip, whatever the number of rows in it (64 queries 38 us, 17024 units; 1024 queries with a window of 300 51 us, 22528; 16 queries over 32768 keys 65 us, 32768).
+inline long long sliding_units_of_tile(int n_q, int n_k, int G, int window, int sinks) {
+    const long long near = sliding_keys(n_q, n_k, G, window, 16);
+    return (near + 31) / 32 + (near < n_k ? (sinks + 31) / 32 : 0);
+}
+// Workgroups of four waves that share a tile: 512 of them in all for up to 64 rows of the output (a token 9.0 us, with 256 10.0; 2 tokens 10.6 / 10.7), 256 where there are more, since
+// every part of a row is written and read once more (4 tokens 12.4 / 11.9, 16 20.1 / 17.7, 32 26.9 / 24.6; float32, 1000 queries of 4 / 2 heads of 64, window 300, 12.7 / 11.1); every
+// wave the same number of units where that can be.
+inline int sliding_splits(int n_q, int n_k, int G, int Hkv, int window, int sinks, int most_parts) {
+    const long long tiles = ((long long)n_q * G + 15) / 16 * Hkv, units = sliding_units_of_tile(n_q, n_k, G, window, sinks);
+    long long most = ((long long)n_q * G * Hkv <= 64 ? 512 : 256) / tiles;
+    most = most < 1 ? 1 : most > most_parts ? most_parts : most;
+    const long long rounds = (units + 4 * most - 1) / (4 * most), want = (units + 4 * rounds - 1) / (4 * rounds);
+    return (int)(want < most ? want : most);
+}
+
+// Tiles of 256 rows: one CU holds one workgroup, 256 of them run at once; a workgroup takes 12 us and 2.8 us a tile of 128 keys; parts are written and read once more, 528 bytes a
+// row, in a launch of 5 us.  64 queries in 1 / 2 / 4 / 8 / 16 parts 94 / 57 / 40 / 35 / 39, 512 96 / 65 / 53 / 71 / 107, 2048 128 / 159; 1511 queries of 28 / 4 heads behind 9856 tokens,
+// all in sight, in 1 / 2 / 3 / 4 / 6 237 / 272 / 225 / 248 / 255.
+inline double sliding_many_us(int n_q, int n_k, int G, int Hkv, int window, int sinks, int parts) {
+    const long long rows = (long long)n_q * G * Hkv, row_tiles = ((long long)n_q * G + 255) / 256 * Hkv, near = sliding_keys(n_q, n_k, G, window, 256);
+    const long long tiles = (near + kSlideTile - 1) / kSlideTile + (near < n_k ? (sinks + kSlideTile - 1) / kSlideTile : 0), rounds = (row_tiles * parts + 255) / 256;
     return rounds * (12.0 + 2.8 * ((tiles + parts - 1) / parts)) + (parts > 1 ? 5.0 + rows * parts * 528.0 * 2 / 4.5e6 : 0.0);
 }
+// In how many parts a call's tiles of 256 rows run; 0: it runs in tiles of 16 rows (7 us and 1.8 ns a unit; 16 queries 17.7 us, in tiles of 256 29; 32 24.6 / 33; 48 37.9 / 36.4; 64
+// of 28 / 4 heads with a window of 500 13.8 / 22.4; 16 over 32768 keys 65 / 58).
 inline int sliding_parts(int n_q, int n_k, int G, int Hkv, int window, int sinks) {
-    const long long rows = (long long)n_q * G * Hkv, row_tiles = ((long long)n_q * G + 255) / 256 * Hkv;
-    const int span = 256 / G + 1 < n_q ? 256 / G + 1 : n_q;                            // queries of a row tile, about
-    const long long near = (long long)window + span < n_k ? (long long)window + span : n_k;
-    const long long tiles = (near + kSlideTile - 1) / kSlideTile + (near < n_k ? (sinks + kSlideTile - 1) / kSlideTile : 0);
     int best = 1;
-    for (int parts = 2; parts <= 64 && parts <= tiles; ++parts)
-        if (sliding_parts_us(row_tiles, tiles, rows, parts) < sliding_parts_us(row_tiles, tiles, rows, best)) best = parts;
-    return best;
+    double us = sliding_many_us(n_q, n_k, G, Hkv, window, sinks, 1);
+    for (int parts = 2; parts <= 64; ++parts) {
+        const double t = sliding_many_us(n_q, n_k, G, Hkv, window, sinks, parts);
+        if (t < us) { us = t; best = parts; }
+    }
+    const double few = 7.0 + 1.8e-3 * (double)(((long long)n_q * G + 15) / 16 * Hkv * sliding_units_of_tile(n_q, n_k, G, window, sinks));
+    return few < us ? 0 : best;
 }
 
 }  // namespace slim

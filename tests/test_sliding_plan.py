@@ -85,3 +85,24 @@ def test_tiles(tmp_path):
     subprocess.run([gxx, "-O2", "-std=c++17", "-I", os.path.join(ROOT, "paper_2508_06447_amd", "csrc"), str(src), "-o", str(exe)], check=True)
     r = subprocess.run([str(exe)], capture_output=True, text=True)
     assert r.returncode == 0 and r.stdout.strip() == "4000 cases", r.stdout
+
+
+def test_routes(tmp_path):
+    """Which tiles a call runs in and over how many workgroups a tile's keys are dealt: the calls whose sides were measured."""
+    gxx = shutil.which("g++")
+    if not gxx:
+        pytest.skip("no host compiler")
+    parts = [((16, 8208, 4, 8, 4096, 64), 0), ((32, 8224, 4, 8, 4096, 64), 0), ((64, 2000, 7, 4, 500, 4), 0), ((1, 32768, 4, 8, 32768, 0), 0), ((1, 1, 1, 1, 1, 0), 0),
+             ((512, 8704, 4, 8, 4096, 64), 4), ((2048, 10240, 4, 8, 4096, 64), 1), ((1511, 11367, 7, 4, 11367, 0), 3), ((32768, 32768, 4, 8, 4096, 64), 1),
+             ((4096, 4096, 4, 8, 512, 0), 1), ((1024, 1024, 4, 8, 300, 4), 1)]
+    splits = [((1, 8193, 4, 8, 4096, 64), 33), ((16, 8208, 4, 8, 4096, 64), 7), ((1, 1, 1, 1, 1, 0), 1), ((2048, 2048, 2, 2, 2048, 0), 1)]
+    src, exe = tmp_path / "routes.cpp", tmp_path / "routes"
+    text = '#include "sliding_plan.h"\n#include <cstdio>\nusing namespace slim;\nint main() {\n'
+    for args, _ in parts:
+        text += f'    printf("%d\\n", sliding_parts({", ".join(map(str, args))}));\n'
+    for args, _ in splits:
+        text += f'    printf("%d\\n", sliding_splits({", ".join(map(str, args))}, 128));\n'
+    src.write_text(text + "}\n")
+    subprocess.run([gxx, "-O1", "-std=c++17", "-I", os.path.join(ROOT, "paper_2508_06447_amd", "csrc"), str(src), "-o", str(exe)], check=True)
+    got = [int(x) for x in subprocess.run([str(exe)], capture_output=True, text=True, check=True).stdout.split()]
+    assert got == [w for _, w in parts + splits]
