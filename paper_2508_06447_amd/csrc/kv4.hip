@@ -11,6 +11,7 @@
 // attention reads them.
 #include "row_tile.h"
 #include <algorithm>
+#include <mutex>
 
 namespace slim {
 
@@ -170,12 +171,17 @@ int launch_kv4_read(const void* pool, int n_slots, size_t slot_bytes, size_t lay
 }
 
 // ---- attention of one decoded token
+// A loaded value whose first use is here: left alone, the compiler moves the shift that makes a scale of it behind the load, in front of the loop's end, and with it the wait.
+__device__ __forceinline__ uint32_t used_here(uint32_t v) {
+    asm volatile("" : "+v"(v));
+    return v;
+}
+
 // The units of 32 keys of the slots and of the response are dealt to the waves of gridDim.x workgroups per kv head; each workgroup leaves a partial result of the kv head's query
-// heads, or, alone, the output.  The registers of a unit's codes are requested anew as soon as they are used; the slot of the unit after that is looked up meanwhile.
+// heads, or, alone, the output.  The registers of a unit's codes are requested anew as soon as they are used.
 constexpr int kQ4D = 128;
-constexpr int kQ4Waves = 4;
-template <typename T>
-__global__ void __launch_bounds__(64 * kQ4Waves) decode_attn_kv4_kernel(
+template <typename T, int NW>
+__global__ void __launch_bounds__(64 * NW) decode_attn_kv4_kernel(
     const T* __restrict__ q, const unsigned char* __restrict__ pool, size_t slot_bytes, size_t layer_offset, const int* __restrict__ block_of_slot, int n_slots, int block,
     int n_prompt, const T* __restrict__ k_resp, const T* __restrict__ v_resp, int n_resp, int Hq, int Hkv, float scale_log2e, float* __restrict__ part, T* __restrict__ out) {
     constexpr int D = kQ4D;
@@ -186,50 +192,76 @@ __global__ void __launch_bounds__(64 * kQ4Waves) decode_attn_kv4_kernel(
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const unsigned tile = (unsigned)(uintptr_t)lds + wave * Tile::kLdsBytes;
     const int nb = (n_prompt + block - 1) / block, per_slot = (block + kTileKeys - 1) / kTileKeys;
-    const int n_in_slots = n_slots * per_slot, n_units = n_in_slots + (n_resp + kTileKeys - 1) / kTileKeys, step = gridDim.x * kQ4Waves;
+    const int n_in_slots = n_slots * per_slot, n_units = n_in_slots + (n_resp + kTileKeys - 1) / kTileKeys, step = gridDim.x * NW;
     const Kv4Head head(g, block, Hkv, D);
 
-    int ui = (int)blockIdx.x * kQ4Waves + wave, rows = 0, c0 = 0;
-    const unsigned char* base = nullptr;                 // of the unit's slot
-    auto find = [&]() {                                  // the next unit in a slot that holds keys; false: none is left
-        for (; ui < n_in_slots; ui += step) {
-            const int slot = ui / per_slot, c = (ui - slot * per_slot) * kTileKeys, b = block_of_slot[slot];
-            if (b < 0 || b >= nb) continue;
-            const int r = min(kTileKeys, min(block, n_prompt - b * block) - c);
-            if (r <= 0) continue;
-            rows = r;
-            c0 = c;
-            base = pool + (size_t)slot * slot_bytes + layer_offset;
-            return true;
+    // The wave's units are u0, u0 + step, ..; those of a free slot or behind the end of a short block hold no key and are passed over.  64 of them are looked up at once, one a lane:
+    // looked up one by one, each waited for block_of_slot.
+    const int u0 = (int)blockIdx.x * NW + wave;
+    int batch = u0, u_slot = 0, u_row = 0, u_rows = 0;   // the lane's unit: slot, first row, rows
+    unsigned long long left = 0;                         // lanes whose units hold keys and have not been taken
+    auto look_up = [&]() {
+        const long long u = batch + (long long)lane * step;
+        int b = -1;
+        if (u < n_in_slots) {
+            u_slot = (int)u / per_slot;
+            u_row = ((int)u - u_slot * per_slot) * kTileKeys;
+            b = block_of_slot[u_slot];
         }
-        return false;
+        u_rows = b >= 0 && b < nb ? min(kTileKeys, min(block, n_prompt - b * block) - u_row) : 0;
+        left = __ballot(u_rows > 0);
     };
+    int rows = 0, c0 = 0;
+    const unsigned char* base = nullptr;                 // of the unit's slot
+    auto find = [&]() {                                  // the next unit; false: none is left
+        while (!left) {
+            if ((long long)batch + 64ll * step >= n_in_slots) return false;
+            batch += 64 * step;
+            look_up();
+        }
+        const int i = __builtin_ctzll(left);
+        left &= left - 1;
+        rows = __builtin_amdgcn_readlane(u_rows, i);
+        c0 = __builtin_amdgcn_readlane(u_row, i);
+        base = pool + (size_t)__builtin_amdgcn_readlane(u_slot, i) * slot_bytes + layer_offset;
+        return true;
+    };
+    look_up();
     uint4 kx[2], vx[2];
-    uint32_t ks[2], vs[2];
-    // rows behind the last key repeat it: their weight is 0
+    uint32_t ks[2], vs[2];                               // the e + 127 of a key's four groups
+    // Addresses: a wave-uniform base and a 32-bit offset of the lane, the same for Keys and Values.  Rows behind the last key repeat it: their weight is 0.
+    unsigned off[2];
     auto load_k = [&]() {
 #pragma unroll
         for (int h = 0; h < 2; ++h) {
-            const unsigned r = c0 + min(l16 + 16 * h, rows - 1);
-            kx[h] = load_stream16(base + head.k + r * (D / 2) + qr * 16);
-            ks[h] = base[head.ks + r * (D / 32) + qr];
+            const unsigned r = min(l16 + 16 * h, rows - 1);
+            off[h] = r * 4;
+            kx[h] = load_stream16(base + head.k + (size_t)c0 * (D / 2) + (r * (D / 2) + qr * 16));
+            ks[h] = *reinterpret_cast<const uint32_t*>(base + head.ks + (size_t)c0 * (D / 32) + off[h]);
         }
     };
     auto load_v = [&]() {
 #pragma unroll
         for (int h = 0; h < 2; ++h) {
-            const unsigned r = c0 + min(l16 + 16 * h, rows - 1);
-            vx[h] = load_stream16(base + head.v + r * (D / 2) + qr * 16);
-            vs[h] = base[head.vs + r * (D / 32) + qr];
+            vx[h] = load_stream16(base + head.v + (size_t)c0 * (D / 2) + (off[h] * 16 + qr * 16));
+            vs[h] = *reinterpret_cast<const uint32_t*>(base + head.vs + (size_t)c0 * (D / 32) + off[h]);
         }
     };
+    // the lane's group of a key
+    auto scale_of = [&](uint32_t groups) { return kv4_scale(__builtin_amdgcn_ubfe(used_here(groups), qr * 8, 8)); };
     bool more = find();
     if (more) { load_k(); load_v(); }
     Tile t;
     t.begin(q + (size_t)(g * G + min(l16, G - 1)) * D);
+    // the Query fragments are waited for here: waited for in the loop, they take the wait for the codes requested meanwhile with them in every turn
+#pragma unroll
+    for (int b = 0; b < NT; ++b)
+#pragma unroll
+        for (int j = 0; j < 4; ++j) asm volatile("" : "+v"(t.q[b][j]));
     float w[8];
     bf16x8 p[NP];
     auto masked = [&](f32x4* s, int have) {
+        if (have == kTileKeys) return;
 #pragma unroll
         for (int h = 0; h < 2; ++h)
 #pragma unroll
@@ -240,14 +272,13 @@ __global__ void __launch_bounds__(64 * kQ4Waves) decode_attn_kv4_kernel(
     };
     while (more) {
         const int have = rows;
-        ui += step;
         more = find();                                   // none left: the last unit is requested once more, and not used
         f32x4 s[2];
 #pragma unroll
         for (int h = 0; h < 2; ++h) {
             typename Tile::Scores sum;
             const uint32_t c[4] = {kx[h].x, kx[h].y, kx[h].z, kx[h].w};
-            const float sc = kv4_scale(ks[h]);
+            const float sc = scale_of(ks[h]);
 #pragma unroll
             for (int j = 0; j < 4; ++j) {
                 const bf16x8 k = kv4_to_bf16(c[j], sc);
@@ -255,23 +286,27 @@ __global__ void __launch_bounds__(64 * kQ4Waves) decode_attn_kv4_kernel(
             }
             s[h] = sum.sum();
         }
-        load_k();
+        __builtin_amdgcn_sched_barrier(0);
+        load_k();                                        // the next unit's Keys fly under this one's Values
+        __builtin_amdgcn_sched_barrier(0);
         masked(s, have);
         t.weigh(s, scale_log2e, w);
         bf16_terms<NP>(w, p);
 #pragma unroll
         for (int h = 0; h < 2; ++h) {
             const uint32_t c[4] = {vx[h].x, vx[h].y, vx[h].z, vx[h].w};
-            const float sc = kv4_scale(vs[h]);
+            const float sc = scale_of(vs[h]);
 #pragma unroll
             for (int j = 0; j < 4; ++j) *(LdsB128)(tile + Tile::v_piece(l16 + 16 * h, qr * 4 + j)) = kv4_to_bf16(c[j], sc);
         }
+        __builtin_amdgcn_sched_barrier(0);
         load_v();
+        __builtin_amdgcn_sched_barrier(0);
         t.template add_values<1>(p, 0, tile);
     }
     // response tokens: dense rows of T
     const size_t row_stride = (size_t)Hkv * D;
-    for (; ui < n_units; ui += step) {
+    for (int ui = n_in_slots + ((u0 - n_in_slots) % step + step) % step; ui < n_units; ui += step) {
         const int first = (ui - n_in_slots) * kTileKeys, have = min(kTileKeys, n_resp - first);
         f32x4 s[2];
         size_t at[2];
@@ -304,7 +339,7 @@ __global__ void __launch_bounds__(64 * kQ4Waves) decode_attn_kv4_kernel(
             t.template add_values<NT>(p, a, tile);
         }
     }
-    merge_waves<T, D, kQ4Waves>(t, lds, G, [&](int h, int dd, float acc, float l, float M) {
+    merge_waves<T, D, NW>(t, lds, G, [&](int h, int dd, float acc, float l, float M) {
         const int row = g * G + h;
         if (gridDim.x == 1) {
             Elem<T>::st(out + (size_t)row * D + dd, l == 0.f ? 0.f : acc / l);
@@ -392,28 +427,42 @@ int launch_merge_rows(const float* part, int n_parts, int rows, int d, int dtype
     return check_launch();
 }
 
-// Workgroups per kv head: about kQ4Wgs in all, every wave the same number of units where that can be, no more than the caller's workspace has room for (one partial per
-// slot and per 64 response tokens).
-constexpr int kQ4Wgs = 512;
-static int kv4_parts(int n_slots, int block, int n_resp, int Hkv) {
+// Workgroups per kv head and waves of a workgroup: every wave the same number of units where that can be, no more workgroups than the caller's workspace has room for (one partial per
+// slot and per 64 response tokens).  256 workgroups of eight waves where that gives every wave a unit, else up to 512 of four; us, 32 / 8 heads, blocks of 64 tokens: 64 slots 8.5 / 8.2,
+// 128 9.6 / 10.0, 512 13.5 / 14.9, 2048 30.3 / 32.2, 4096 51.6 / 53.7 (its loads alone 45); 512 of eight waves, which the registers keep from running together, 2048 slots 34.8.
+struct Q4Plan { int waves, parts; };
+static Q4Plan kv4_plan(int n_slots, int block, int n_resp, int Hkv) {
     const long long units = (long long)n_slots * ((block + kTileKeys - 1) / kTileKeys) + (n_resp + kTileKeys - 1) / kTileKeys;
-    const long long most = std::min<long long>(std::max(16, std::min(kMergeParts, kQ4Wgs / Hkv)), (long long)n_slots + (n_resp + 63) / 64);
-    const long long rounds = std::max<long long>(1, (units + kQ4Waves * most - 1) / (kQ4Waves * most));
-    return (int)std::max<long long>(1, std::min(most, (units + kQ4Waves * rounds - 1) / (kQ4Waves * rounds)));
+    const int waves = units * Hkv >= 8 * 256 ? 8 : 4;
+    const long long most = std::min<long long>(std::max(16, std::min(kMergeParts, (waves == 8 ? 256 : 512) / Hkv)), (long long)n_slots + (n_resp + 63) / 64);
+    const long long rounds = std::max<long long>(1, (units + waves * most - 1) / (waves * most));
+    return {waves, (int)std::max<long long>(1, std::min(most, (units + waves * rounds - 1) / (waves * rounds)))};
+}
+
+template <typename T, int NW>
+static int launch_q4(const void* q, const void* pool, size_t slot_bytes, size_t layer_offset, const int* block_of_slot, int n_slots, int block, int n_prompt, const void* k_resp,
+                     const void* v_resp, int n_resp, int Hq, int Hkv, float sl, void* out, float* part, int parts, hipStream_t st) {
+    constexpr int smem = NW * RowTile<T, kQ4D>::kLdsBytes;
+    if (smem >= 1 << 16) {
+        static std::once_flag once;
+        static hipError_t err = hipSuccess;
+        std::call_once(once, [&] { err = hipFuncSetAttribute((const void*)decode_attn_kv4_kernel<T, NW>, hipFuncAttributeMaxDynamicSharedMemorySize, smem); });
+        if (err != hipSuccess) return set_hip_error(err);
+    }
+    hipLaunchKernelGGL((decode_attn_kv4_kernel<T, NW>), dim3(parts, Hkv), dim3(64 * NW), smem, st, (const T*)q, (const unsigned char*)pool, slot_bytes, layer_offset, block_of_slot,
+                       n_slots, block, n_prompt, (const T*)k_resp, (const T*)v_resp, n_resp, Hq, Hkv, sl, part, (T*)out);
+    return check_launch();
 }
 
 int launch_decode_attn_kv4(const void* q, const void* pool, size_t slot_bytes, size_t layer_offset, const int* block_of_slot, int n_slots, int block, int n_prompt,
                            const void* k_resp, const void* v_resp, int n_resp, int Hq, int Hkv, float scale, int dtype, void* out, float* part, hipStream_t st) {
     const float sl = scale * 1.4426950408889634f;
-    const int parts = kv4_parts(n_slots, n_slots ? block : 1, n_resp, Hkv);
-    const size_t smem = (size_t)kQ4Waves * RowTile<bf16_t, kQ4D>::kLdsBytes;
-#define SLIM_Q4(T) hipLaunchKernelGGL(decode_attn_kv4_kernel<T>, dim3(parts, Hkv), dim3(64 * kQ4Waves), smem, st, (const T*)q, (const unsigned char*)pool, slot_bytes, layer_offset, \
-                                      block_of_slot, n_slots, n_slots ? block : 1, n_prompt, (const T*)k_resp, (const T*)v_resp, n_resp, Hq, Hkv, sl, part, (T*)out)
-    if (dtype == SLIM_BF16) SLIM_Q4(bf16_t); else SLIM_Q4(float);
+    if (n_slots == 0) block = 1;
+    const Q4Plan plan = kv4_plan(n_slots, block, n_resp, Hkv);
+#define SLIM_Q4(T, NW) launch_q4<T, NW>(q, pool, slot_bytes, layer_offset, block_of_slot, n_slots, block, n_prompt, k_resp, v_resp, n_resp, Hq, Hkv, sl, out, part, plan.parts, st)
+    const int rc = dtype == SLIM_BF16 ? (plan.waves == 8 ? SLIM_Q4(bf16_t, 8) : SLIM_Q4(bf16_t, 4)) : plan.waves == 8 ? SLIM_Q4(float, 8) : SLIM_Q4(float, 4);
 #undef SLIM_Q4
-    if (parts == 1) return check_launch();
-    const int rc = check_launch();
-    return rc ? rc : launch_merge_rows(part, parts, Hq, kQ4D, dtype, out, st);
+    return rc || plan.parts == 1 ? rc : launch_merge_rows(part, plan.parts, Hq, kQ4D, dtype, out, st);
 }
 
 }  // namespace slim
