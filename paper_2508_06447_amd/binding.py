@@ -263,13 +263,12 @@ def _decode_attn(name: str, q, gpu_pool, block_of_slot, block, n_prompt_tokens, 
     lib = load_library()
     Hq, d = q.shape
     ns = block_of_slot.numel()
-    slot_bytes = gpu_pool[0].numel() * gpu_pool.element_size() if ns else 0
+    slot_bytes = gpu_pool.numel() // gpu_pool.shape[0] * gpu_pool.element_size() if ns else 0
     n_resp = 0 if k_response is None else k_response.shape[0]
     if out is None:
         out = torch.empty_like(q)
-    need = lib.slim_decode_attn_workspace_bytes(ns, n_resp, Hq)
     if workspace is None:
-        workspace = torch.empty(max(need, 256), dtype=torch.uint8, device=q.device)
+        workspace = torch.empty(max(lib.slim_decode_attn_workspace_bytes(ns, n_resp, Hq), 256), dtype=torch.uint8, device=q.device)
     _check(getattr(lib, name)(_dev(q, "q"), _dev(gpu_pool, "gpu_pool"), slot_bytes, layer_offset,
                               _dev(block_of_slot, "block_of_slot"), ns, block, n_prompt_tokens, _dev(k_response, "k_response"),
                               _dev(v_response, "v_response"), n_resp, Hq, n_kv_heads, d, softmax_scale, _dtype_code(q),
@@ -355,20 +354,24 @@ def _rows(t: torch.Tensor, name: str):
     if not t.is_cuda:
         raise ValueError(f"{name} must be a GPU tensor")
     n, H, d = t.shape
-    if (d > 1 and t.stride(2) != 1) or (H > 1 and t.stride(1) != d):
+    if t.is_contiguous():
+        return t.data_ptr(), H * d
+    s0, s1, s2 = t.stride()
+    if (d > 1 and s2 != 1) or (H > 1 and s1 != d):
         raise ValueError(f"{name} must have dense rows")
-    return t.data_ptr(), t.stride(0) if n > 1 else H * d
+    return t.data_ptr(), s0 if n > 1 else H * d
 
 
-def _slots(pool: torch.Tensor, host: bool = False):
-    """(address, slots, bytes of a slot) of pool[slots, ...]."""
-    at = _pinned(pool, "pool") if host and not pool.is_cuda else _dev(pool, "pool")
+def _slots(pool: torch.Tensor):
+    """(address, slots, bytes of a slot) of pool[slots, ...], on the GPU or in pinned host memory."""
     ns = pool.shape[0]
-    return at, ns, (pool.numel() // ns) * pool.element_size() if ns else 0
+    return _dev(pool, "pool") if pool.is_cuda else _pinned(pool, "pool"), ns, pool.numel() // ns * pool.element_size() if ns else 0
 
 
 def _index(t: torch.Tensor | None, name: str):
-    if t is not None and t.dtype != torch.int32:
+    if t is None:
+        return None
+    if t.dtype != torch.int32:
         raise TypeError(f"{name} must be int32")
     return _dev(t, name)
 
@@ -381,7 +384,9 @@ def slim_kv4_write(k: torch.Tensor, v: torch.Tensor, pool: torch.Tensor, block: 
     n, Hkv, d = k.shape
     if v.shape != k.shape or v.dtype != k.dtype:
         raise ValueError("k and v must be alike")
-    (kp, ldk), (vp, ldv), (at, ns, size) = _rows(k, "k"), _rows(v, "v"), _slots(pool, host=True)
+    kp, ldk = _rows(k, "k")
+    vp, ldv = _rows(v, "v")
+    at, ns, size = _slots(pool)
     _check(lib.slim_kv4_write(kp, vp, ldk, ldv, first_token, n, Hkv, d, block, _dtype_code(k), _index(slot_of_block, "slot_of_block"),
                               ns if slot_of_block is None else slot_of_block.numel(), at, ns, size, layer_offset, _stream()), "slim_kv4_write")
     return pool
@@ -398,18 +403,19 @@ def slim_kv4_read(pool: torch.Tensor, block: int, n_tokens: int, slot_of_block: 
         raise ValueError("slot_of_block is shorter than the prompt's blocks")
     if (k_out is None) != (v_out is None):
         raise ValueError("k_out and v_out go together")
+    n_list = 0 if blocks is None else blocks.numel()
+    rows = n_tokens if blocks is None else n_tokens - (nb - n_list) * block
     if k_out is None:
-        rows = n_tokens if blocks is None else lib.slim_kept_tokens(n_tokens, block, blocks.numel())
-        k_out = torch.empty(rows, n_kv_heads, head_dim, dtype=dtype, device=pool.device)
+        k_out = torch.empty(max(rows, 0), n_kv_heads, head_dim, dtype=dtype, device=pool.device)
         v_out = torch.empty_like(k_out)
-    need = n_tokens if blocks is None else lib.slim_kept_tokens(n_tokens, block, blocks.numel())
-    if k_out.shape != v_out.shape or k_out.dtype != v_out.dtype or k_out.shape[0] < need:
+    n_rows, Hkv, d = k_out.shape
+    if k_out.shape != v_out.shape or k_out.dtype != v_out.dtype or n_rows < rows:
         raise ValueError("k_out and v_out must be alike and hold the rows")
-    _, Hkv, d = k_out.shape
-    (kp, ldk), (vp, ldv), (at, ns, size) = _rows(k_out, "k_out"), _rows(v_out, "v_out"), _slots(pool, host=True)
-    _check(lib.slim_kv4_read(at, ns, size, layer_offset, _index(slot_of_block, "slot_of_block"), _index(blocks, "blocks"),
-                             0 if blocks is None else blocks.numel(), block, n_tokens, Hkv, d, _dtype_code(k_out), kp, vp, k_out.shape[0], ldk, ldv, _stream()),
-           "slim_kv4_read")
+    kp, ldk = _rows(k_out, "k_out")
+    vp, ldv = _rows(v_out, "v_out")
+    at, ns, size = _slots(pool)
+    _check(lib.slim_kv4_read(at, ns, size, layer_offset, _index(slot_of_block, "slot_of_block"), _index(blocks, "blocks"), n_list, block, n_tokens, Hkv, d,
+                             _dtype_code(k_out), kp, vp, n_rows, ldk, ldv, _stream()), "slim_kv4_read")
     return k_out, v_out
 
 
