@@ -39,8 +39,10 @@ __device__ __forceinline__ float kv4_scale(uint32_t byte) { return __builtin_bit
 
 // ---- written and read back
 // A wave takes 64 / (D / 8) rows of one kv head, Keys or Values, at a time, 8 channels a lane (four lanes a group), kSteps times in a row: what it reads is whole rows, what it writes
-// lies together.
-constexpr int kSteps = 4;
+// lies together.  Bound by memory: 32768 tokens of 8 heads of 128 in bf16, in buffers that no cache holds, written 33.9 us (170 MB, 5.0 TB/s; a copy of that size on this card 5.2), read back
+// 24.8 (6.9).  Past the caches go the rows that are read (without 38.0 us) and those that are written (without 51.8: the lines push out the codes), but not the codes that are
+// written, four bytes a lane (with the read behind it 82 us for both instead of 59); four steps in a row instead of two 33.8 and 26.2.
+constexpr int kSteps = 2;
 struct Kv4Rows {
     const unsigned char* pool;
     size_t slot_bytes, layer_offset;
@@ -65,8 +67,8 @@ __global__ void __launch_bounds__(256) kv4_write_kernel(const T* __restrict__ K,
 #pragma unroll
     for (int s = 0; s < kSteps; ++s) {
         const T* p = src + (size_t)min(i0 + s * RPW, a.n - 1) * ld + piece * 8;
-        Elem<T>::unpack(*reinterpret_cast<const uint4*>(p), f[s]);
-        if constexpr (sizeof(T) == 4) Elem<T>::unpack(*reinterpret_cast<const uint4*>(p + 4), f[s] + 4);
+        Elem<T>::unpack(load_stream16(p), f[s]);
+        if constexpr (sizeof(T) == 4) Elem<T>::unpack(load_stream16(p + 4), f[s] + 4);
     }
     int b = (a.first + i0) / a.block, r = a.first + i0 - b * a.block;
 #pragma unroll
@@ -135,12 +137,12 @@ __global__ void __launch_bounds__(256) kv4_read_kernel(T* __restrict__ K, T* __r
         const uint4 v = __builtin_bit_cast(uint4, kv4_to_bf16(code[s], kv4_scale(byte[s])));
         T* dst = out + (size_t)(o0 + s * RPW) * ld + piece * 8;
         if constexpr (sizeof(T) == 2) {
-            *reinterpret_cast<uint4*>(dst) = v;
+            store_stream16(dst, v);
         } else {
             float f[8];
             Elem<bf16_t>::unpack(v, f);
-            *reinterpret_cast<uint4*>(dst) = Elem<float>::pack(f);
-            *reinterpret_cast<uint4*>(dst + 4) = Elem<float>::pack(f + 4);
+            store_stream16(dst, Elem<float>::pack(f));
+            store_stream16(dst + 4, Elem<float>::pack(f + 4));
         }
     }
 }
