@@ -165,7 +165,7 @@ int slim_prefill_attn(const void* q, const void* k, const void* v, int n, int n_
  * that is not finite is not specified.
  *   workspace   >= slim_sliding_attn_workspace_bytes(...) bytes, 256-byte aligned: partial results of few queries; NULL where that is 0.
  * Errors: INVALID_ARG (null, n_q < 1, n_k < n_q, Hq % Hkv, window < 1, n_sinks < 0, scale < 0 or NaN), UNSUPPORTED (bf16: d != 128; f32: d other than 32,
- * 64, 128; alignment of 16 bytes; n_k or n_q * Hq above 2^30), WORKSPACE_TOO_SMALL.
+ * 64, 128; alignment of 16 bytes; n_k above 2^30, n_q * Hq above 2^27), WORKSPACE_TOO_SMALL.
  */
 size_t slim_sliding_attn_workspace_bytes(int n_q, int n_k, int n_q_heads, int n_kv_heads, int head_dim, int window, int n_sinks, int dtype);
 int slim_sliding_attn(const void* q, const void* k, const void* v, int n_q, int n_k, int n_q_heads, int n_kv_heads, int head_dim, int window,
@@ -447,11 +447,12 @@ int slim_decode_layer(const slim_layer_shape* s, const slim_layer_weights* w, co
  *                    pool: device memory, or pinned device-mapped host memory (the CPU pool of slim_kv_swap, with NULL).
  *   slim_kv4_read:   rows of the blocks listed in blocks[n_list] (int32, device, ascending; NULL: every block of the n_tokens prompt tokens) -> k_out, v_out: row
  *                    i * block + r is token blocks[i] * block + r, so that the kept rows lie densely, as slim_compact_tokens leaves them (only the prompt's
- *                    last block can be short).  k_out and v_out have room for n_rows rows; those behind are not written.  Rows of a block outside the prompt, or whose slot is outside [0, n_slots), stay as they were.
+ *                    last block can be short).  k_out and v_out have room for n_rows rows; those behind
+ *                    are not written.  Rows of a block outside the prompt, or whose slot is outside [0, n_slots), stay as they were.
  *   slim_decode_attn_kv4, slim_decode_layer_kv4:  slim_decode_attn and slim_decode_layer on such slots; arguments, response rows (of dtype) and workspaces are
  *                    theirs, up to 16 query heads per kv head, softmax_scale not negative.  A token that sees no key gets zeros.
  * head_dim 32, 64 or 128 (attention: 128); pools, layer_offset and slot_bytes multiples of 16, rows 16-byte aligned (ld a multiple of 8 bf16 or 4 f32 elements),
- * block <= 2^24.  Errors: INVALID_ARG (null, sizes, ld < Hkv * head_dim, tokens behind n_blocks blocks, a slot too small), UNSUPPORTED, WORKSPACE_TOO_SMALL.
+ * block <= 2^24, fewer than 2^29 tokens in a call that writes or reads.  Errors: INVALID_ARG (null, sizes, ld < Hkv * head_dim, tokens behind n_blocks blocks, a slot too small), UNSUPPORTED, WORKSPACE_TOO_SMALL.
  */
 size_t slim_kv4_block_bytes(int block, int n_kv_heads, int head_dim);
 int slim_kv4_write(const void* k, const void* v, int ldk, int ldv, int first_token, int n_tokens, int n_kv_heads, int head_dim, int block,

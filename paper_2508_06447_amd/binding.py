@@ -286,11 +286,22 @@ def slim_decode_attn(q: torch.Tensor, gpu_pool: torch.Tensor, block_of_slot: tor
                         softmax_scale, out, workspace)
 
 
+def _response(q, k, v, n_kv_heads):
+    if v is None or k.shape != v.shape or not k.dtype == v.dtype == q.dtype or k.shape[1] != n_kv_heads or k.shape[2] != q.shape[1]:
+        raise ValueError("k_response and v_response must be alike, [n, Hkv, d] of q's type")
+
+
 def slim_decode_attn_kv4(q: torch.Tensor, gpu_pool: torch.Tensor, block_of_slot: torch.Tensor, block: int, n_prompt_tokens: int,
                          n_kv_heads: int, k_response: torch.Tensor | None = None, v_response: torch.Tensor | None = None,
                          layer_offset: int = 0, softmax_scale: float = 0.0, out: torch.Tensor | None = None,
                          workspace: torch.Tensor | None = None) -> torch.Tensor:
     """slim_decode_attn on a pool of blocks in 4 bits (slim_kv4_write)."""
+    if block_of_slot.dtype != torch.int32:
+        raise TypeError("block_of_slot must be int32")
+    if out is not None and (out.shape != q.shape or out.dtype != q.dtype):
+        raise ValueError("out must be like q")
+    if k_response is not None:
+        _response(q, k_response, v_response, n_kv_heads)
     return _decode_attn("slim_decode_attn_kv4", q, gpu_pool, block_of_slot, block, n_prompt_tokens, n_kv_heads, k_response, v_response, layer_offset,
                         softmax_scale, out, workspace)
 
@@ -340,6 +351,10 @@ def slim_decode_layer_kv4(shape: LayerShape, weights: dict, x_new: torch.Tensor,
                           block_of_slot: torch.Tensor, n_prompt_tokens: int, k_response: torch.Tensor, v_response: torch.Tensor,
                           n_response: int, layer_offset: int = 0, workspace: torch.Tensor | None = None):
     """slim_decode_layer on a pool of blocks in 4 bits (slim_kv4_write)."""
+    if block_of_slot.dtype != torch.int32:
+        raise TypeError("block_of_slot must be int32")
+    if k_response.shape != v_response.shape or not k_response.dtype == v_response.dtype == x_new.dtype or k_response.shape[0] <= n_response:
+        raise ValueError("k_response and v_response must be alike, of x_new's type, and hold the token's row")
     return _decode_layer("slim_decode_layer_kv4", shape, weights, x_new, position, gpu_pool, block_of_slot, n_prompt_tokens, k_response, v_response,
                          n_response, layer_offset, workspace)
 
@@ -406,7 +421,7 @@ def slim_kv4_read(pool: torch.Tensor, block: int, n_tokens: int, slot_of_block: 
     n_list = 0 if blocks is None else blocks.numel()
     rows = n_tokens if blocks is None else n_tokens - (nb - n_list) * block
     if k_out is None:
-        k_out = torch.empty(max(rows, 0), n_kv_heads, head_dim, dtype=dtype, device=pool.device)
+        k_out = torch.empty(max(rows, 0), n_kv_heads, head_dim, dtype=dtype, device=pool.device if pool.is_cuda else torch.cuda.current_device())
         v_out = torch.empty_like(k_out)
     n_rows, Hkv, d = k_out.shape
     if k_out.shape != v_out.shape or k_out.dtype != v_out.dtype or n_rows < rows:

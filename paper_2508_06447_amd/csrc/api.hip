@@ -282,6 +282,7 @@ static bool kv4_heads_ok(int n_kv_heads, int head_dim) { return (head_dim == 32 
 static bool slot_holds(size_t bytes, size_t layer_offset, size_t slot_bytes) { return layer_offset <= slot_bytes && bytes <= slot_bytes - layer_offset; }
 // Units of 32 keys and the bytes of a slot's rows are counted in 32 bits.
 constexpr int kKv4BlockMost = 1 << 24;
+constexpr int kKv4RowsMost = 1 << 29;                    // of a call: eight threads of a launch per row, of which there are 2^32 - 1
 static bool kv4_slots_ok(int n_slots, int block) { return block <= kKv4BlockMost && (long long)n_slots * ((block + kTileKeys - 1) / kTileKeys) < (1ll << 30); }
 
 size_t slim_kv4_block_bytes(int block, int n_kv_heads, int head_dim) {
@@ -310,7 +311,7 @@ int slim_kv4_write(const void* k, const void* v, int ldk, int ldv, int first_tok
     if (rc) return rc;
     const long long end = (long long)first_token + n_tokens;
     if (end > (long long)n_blocks * block) return SLIM_INVALID_ARG;
-    if (end > (1ll << 31) - 65536) return SLIM_UNSUPPORTED;
+    if (end > (1ll << 31) - 65536 || n_tokens >= kKv4RowsMost) return SLIM_UNSUPPORTED;
     return launch_kv4_write(k, v, ldk, ldv, first_token, n_tokens, n_kv_heads, head_dim, block, dtype, slot_of_block, n_blocks, pool, n_slots, slot_bytes, layer_offset,
                             (hipStream_t)stream);
 }
@@ -322,7 +323,7 @@ int slim_kv4_read(const void* pool, int n_slots, size_t slot_bytes, size_t layer
     const int rc = kv4_pool_checks(pool, n_slots, slot_bytes, layer_offset, nb, block, n_kv_heads, head_dim, dtype, k_out, v_out, ldk, ldv);
     if (rc) return rc;
     if (blocks && n_list > nb) return SLIM_INVALID_ARG;
-    if (n_tokens > (1ll << 31) - 65536) return SLIM_UNSUPPORTED;
+    if (n_tokens >= kKv4RowsMost) return SLIM_UNSUPPORTED;
     return launch_kv4_read(pool, n_slots, slot_bytes, layer_offset, slot_of_block, blocks, blocks ? n_list : nb, nb, block, n_tokens, n_kv_heads, head_dim, dtype, k_out, v_out,
                            n_rows, ldk, ldv, (hipStream_t)stream);
 }
@@ -588,7 +589,7 @@ static int sliding_checks(int n_q, int n_k, int n_q_heads, int n_kv_heads, int h
     if (n_q < 1 || n_k < n_q || n_q_heads < 1 || n_kv_heads < 1 || head_dim < 1 || n_q_heads % n_kv_heads != 0 || window < 1 || n_sinks < 0) return SLIM_INVALID_ARG;
     if (!dtype_ok(dtype) || (head_dim != 128 && (dtype == SLIM_BF16 || (head_dim != 32 && head_dim != 64))) || n_kv_heads > 65535) return SLIM_UNSUPPORTED;
     // positions, rows of a kv head and heads of all rows are counted in 32 bits
-    if (n_k > (1 << 30) || (long long)n_q * n_q_heads > (1ll << 30)) return SLIM_UNSUPPORTED;
+    if (n_k > (1 << 30) || (long long)n_q * n_q_heads > (1ll << 27)) return SLIM_UNSUPPORTED;      // (16 threads of a launch per row)
     return SLIM_OK;
 }
 

@@ -178,6 +178,9 @@ def test_pinned_host_pool(slim):
     slim.slim_kv4_write(k.cuda(), v.cuda(), host, block)
     torch.cuda.synchronize()
     np.testing.assert_array_equal(host.numpy(), ref.pack(ref.to64(k), ref.to64(v), block))
+    kr, vr = slim.slim_kv4_read(host, block, n, n_kv_heads=H, head_dim=d)
+    same(kr, ref.cached(ref.to64(k)))
+    same(vr, ref.cached(ref.to64(v)))
 
 
 def test_binding_refusals(slim):
@@ -201,6 +204,20 @@ def test_binding_refusals(slim):
         slim.slim_kv4_read(pool, 16, 16, k_out=k[:8], v_out=k[:8])
     with pytest.raises(ValueError):
         slim.slim_kv4_read(pool, 16, 16, k_out=k)
+    q, r = (torch.zeros(n, 2, 128, dtype=BF16, device="cuda") for n in (1, 5))
+    pool = torch.zeros(1, slim.kv4_block_bytes(16, 2, 128), dtype=torch.uint8, device="cuda")
+    slots = torch.zeros(1, dtype=torch.int32, device="cuda")
+    with pytest.raises(TypeError):
+        slim.slim_decode_attn_kv4(q[0], pool, slots.long(), 16, 16, 2)
+    with pytest.raises(ValueError):
+        slim.slim_decode_attn_kv4(q[0], pool, slots, 16, 16, 2, out=q[0, :1])
+    for k_resp, v_resp in ((r, None), (r, r[:4]), (r.float(), r.float()), (r.view(10, 1, 128), r.view(10, 1, 128))):
+        with pytest.raises(ValueError):
+            slim.slim_decode_attn_kv4(q[0], pool, slots, 16, 16, 2, k_resp, v_resp)
+    shape, x = slim.make_shape(256, 2, 2, 128, 512, 16, 8, 16, BF16), torch.zeros(256, dtype=BF16, device="cuda")
+    for k_resp, v_resp, n_resp in ((r, r[:4], 2), (r.float(), r.float(), 2), (r, r, 5)):
+        with pytest.raises(ValueError):
+            slim.slim_decode_layer_kv4(shape, {}, x, 20, pool, slots, 16, k_resp, v_resp, n_resp)
 
 
 # ---------------------------------------------------------------------------------------------------- attention

@@ -44,7 +44,8 @@ def test_write_refusals(lib):
                 dict(slots=0), dict(n=513), dict(first=413), dict(size=64 * 8 * 136 - 16), dict(at=16), dict(at=1 << 40), dict(first=2**31 - 1, n=2**31 - 1)):
         assert write(lib, **bad) == -1, bad
     for bad in (dict(dtype=2), dict(d=96, ldk=4096, ldv=4096), dict(heads=1, d=256), dict(size=64 * 8 * 136 + 8), dict(size=64 * 8 * 136 + 64, at=8), dict(k=ctypes.c_void_p(264)),
-                dict(pool=ctypes.c_void_p(264)), dict(ldk=1028), dict(ldv=1028), dict(dtype=0, ldk=1026), dict(block=(1 << 24) + 1, size=1 << 60)):
+                dict(pool=ctypes.c_void_p(264)), dict(ldk=1028), dict(ldv=1028), dict(dtype=0, ldk=1026), dict(block=(1 << 24) + 1, size=1 << 60), dict(n=1 << 29, nb=1 << 24),
+                dict(first=(1 << 31) - 70000, n=10000, nb=1 << 26)):
         assert write(lib, **bad) == -2, bad
 
 
@@ -52,7 +53,7 @@ def test_read_refusals(lib):
     for bad in (dict(k=NULL), dict(v=NULL), dict(pool=NULL), dict(ldk=1016), dict(n=0), dict(n_list=0), dict(n_list=9), dict(rows=0), dict(heads=0), dict(block=0), dict(slots=0),
                 dict(size=64 * 8 * 136 - 16), dict(at=16)):
         assert read(lib, **bad) == -1, bad
-    for bad in (dict(dtype=7), dict(d=48, ldk=4096, ldv=4096), dict(size=64 * 8 * 136 + 8), dict(v=ctypes.c_void_p(257)), dict(ldv=1028)):
+    for bad in (dict(dtype=7), dict(d=48, ldk=4096, ldv=4096), dict(size=64 * 8 * 136 + 8), dict(v=ctypes.c_void_p(257)), dict(ldv=1028), dict(n=1 << 29)):
         assert read(lib, **bad) == -2, bad
 
 

@@ -26,7 +26,8 @@ def test_refusals(lib):
                 dict(window=-5), dict(sinks=-1), dict(scale=-0.5), dict(scale=float("nan")), dict(ws=NULL)):
         assert call(lib, **bad) == -1, bad
     for bad in (dict(dtype=2), dict(d=64), dict(d=96, dtype=0), dict(q=ctypes.c_void_p(264)), dict(out=ctypes.c_void_p(258)), dict(ws=ctypes.c_void_p(272)), dict(n_k=(1 << 30) + 1),
-                dict(Hkv=70000, Hq=70000), dict(n_q=1 << 26, n_k=1 << 26)):
+                dict(Hkv=70000, Hq=70000), dict(n_q=1 << 26, n_k=1 << 26),
+                dict(n_q=(1 << 22) + 1, n_k=1 << 23), dict(n_q=(1 << 27) + 1, n_k=1 << 28, Hq=1, Hkv=1, d=32, dtype=0)):
         assert call(lib, **bad) == -2, bad
     assert call(lib, wb=16) == -3
 
