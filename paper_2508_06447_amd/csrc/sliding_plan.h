@@ -89,8 +89,10 @@ inline double sliding_many_us(int n_q, int n_k, int G, int Hkv, int window, int 
     const long long tiles = (near + kSlideTile - 1) / kSlideTile + (near < n_k ? (sinks + kSlideTile - 1) / kSlideTile : 0), rounds = (row_tiles * parts + 255) / 256;
     return rounds * (12.0 + 2.8 * ((tiles + parts - 1) / parts)) + (parts > 1 ? 5.0 + rows * parts * 528.0 * 2 / 4.5e6 : 0.0);
 }
-// In how many parts a call's tiles of 256 rows run; 0: it runs in tiles of 16 rows (7 us and 1.8 ns a unit; 16 queries 17.7 us, in tiles of 256 29; 32 24.6 / 33; 48 37.9 / 36.4; 64
-// of 28 / 4 heads with a window of 500 13.8 / 22.4; 16 over 32768 keys 65 / 58).
+// In how many parts a call's tiles of 256 rows run; 0: it runs in tiles of 16 rows (6 us, and over the whole chip 6 ns a tile and 1.8 ns a unit; 16 queries 17.7 us, in tiles of 256
+// 29; 32 24.6 / 33; 48 37.9 / 36.4; 64 of 28 / 4 heads with a window of 500 13.8 / 22.4; 16 over 32768 keys 65 / 58; windows of 16, where a tile is one unit and its other waves have
+// nothing: 1024 25.5 / 18.2, 4096 93 / 41, 32768 740 / 290).  Over 121 calls of 16 to 32768 queries, five head layouts and windows of 1 to 1024 the faster one was chosen but where
+// the two are within 1 %.
 inline int sliding_parts(int n_q, int n_k, int G, int Hkv, int window, int sinks) {
     int best = 1;
     double us = sliding_many_us(n_q, n_k, G, Hkv, window, sinks, 1);
@@ -98,7 +100,7 @@ inline int sliding_parts(int n_q, int n_k, int G, int Hkv, int window, int sinks
         const double t = sliding_many_us(n_q, n_k, G, Hkv, window, sinks, parts);
         if (t < us) { us = t; best = parts; }
     }
-    const double few = 7.0 + 1.8e-3 * (double)(((long long)n_q * G + 15) / 16 * Hkv * sliding_units_of_tile(n_q, n_k, G, window, sinks));
+    const double few = 6.0 + (double)(((long long)n_q * G + 15) / 16 * Hkv) * (6.0 + 1.8 * (double)sliding_units_of_tile(n_q, n_k, G, window, sinks)) * 1e-3;
     return few < us ? 0 : best;
 }
 

@@ -106,6 +106,14 @@ def test_window_that_covers_everything_is_plain_causal_attention(slim):
     check(out, q, k, v, n, 0, rows=np.arange(0, n, 37))
 
 
+@pytest.mark.parametrize("window,sinks", [(1, 0), (1, 3), (2, 0), (16, 4), (17, 0)])
+def test_short_windows_of_many_queries(slim, window, sinks):
+    """Most units of a tile of 256 rows hold nothing for most of its rows."""
+    q, k, v = inputs_of(1100, 1133, 32, 8, 128, BF16, 12)
+    out = slim.slim_sliding_attn(q.cuda(), k.cuda(), v.cuda(), window, sinks)
+    check(out, q, k, v, window, sinks, rows=np.unique(np.concatenate((np.arange(0, 1100, 41), np.arange(1080, 1100)))))
+
+
 def test_chunks_and_single_tokens_give_the_rows_of_the_whole(slim):
     n, Hq, Hkv, d, window, sinks = 300, 8, 2, 128, 77, 5
     q, k, v = (x.cuda() for x in inputs_of(n, n, Hq, Hkv, d, BF16, 6))
