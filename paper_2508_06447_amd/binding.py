@@ -149,11 +149,12 @@ def _check(code: int, where: str):
 
 
 def _dtype_code(t: torch.Tensor) -> int:
-    if t.dtype == torch.float32:
+    dtype = t.dtype
+    if dtype == torch.float32:
         return F32
-    if t.dtype == torch.bfloat16:
+    if dtype == torch.bfloat16:
         return BF16
-    raise TypeError(f"unsupported dtype {t.dtype}")
+    raise TypeError(f"unsupported dtype {dtype}")
 
 
 def _dev(t: torch.Tensor | None, name: str):
@@ -286,22 +287,20 @@ def slim_decode_attn(q: torch.Tensor, gpu_pool: torch.Tensor, block_of_slot: tor
                         softmax_scale, out, workspace)
 
 
-def _response(q, k, v, n_kv_heads):
-    if v is None or k.shape != v.shape or not k.dtype == v.dtype == q.dtype or k.shape[1] != n_kv_heads or k.shape[2] != q.shape[1]:
-        raise ValueError("k_response and v_response must be alike, [n, Hkv, d] of q's type")
-
-
 def slim_decode_attn_kv4(q: torch.Tensor, gpu_pool: torch.Tensor, block_of_slot: torch.Tensor, block: int, n_prompt_tokens: int,
                          n_kv_heads: int, k_response: torch.Tensor | None = None, v_response: torch.Tensor | None = None,
                          layer_offset: int = 0, softmax_scale: float = 0.0, out: torch.Tensor | None = None,
                          workspace: torch.Tensor | None = None) -> torch.Tensor:
     """slim_decode_attn on a pool of blocks in 4 bits (slim_kv4_write)."""
+    dtype = q.dtype
     if block_of_slot.dtype != torch.int32:
         raise TypeError("block_of_slot must be int32")
-    if out is not None and (out.shape != q.shape or out.dtype != q.dtype):
+    if out is not None and (out.numel() != q.numel() or out.dtype != dtype):
         raise ValueError("out must be like q")
     if k_response is not None:
-        _response(q, k_response, v_response, n_kv_heads)
+        n, h, d = k_response.shape
+        if v_response is None or h != n_kv_heads or not k_response.dtype == v_response.dtype == dtype or v_response.numel() != n * h * d or d != q.shape[-1]:
+            raise ValueError("k_response and v_response must be alike, [n, Hkv, d] of q's type")
     return _decode_attn("slim_decode_attn_kv4", q, gpu_pool, block_of_slot, block, n_prompt_tokens, n_kv_heads, k_response, v_response, layer_offset,
                         softmax_scale, out, workspace)
 
