@@ -35,7 +35,7 @@ Every wave of a workgroup runs the same number of units (masked keys give P = 0)
 WINDOWED.  The tiles of a workgroup are those of the first tokens, if any, then those from its first query's window on: the
 tile pointers and the key index jump between them.  The masked loop runs twice, over the tiles in front (first tokens, the
 rows' window edges) and over the last ones; per unit it masks where a key lies above some query of the wave, or behind some
-window and is no first token.  The first unit may be masked for a whole row, so the reference starts at the larger of that
+window and is no first token, and it ends behind the last unit with keys (2 % of a window of 4096 with four heads a kv head).  The first unit may be masked for a whole row, so the reference starts at the larger of that
 unit's maximum and the query's product with its own token, which comes as an operand.  Query fragments stay as they are and
 S is scaled in float on its way into the exponential (a scaled Query rounded to bf16 again is off by 2^-9 per channel: the
 largest error of the whole); the reference is in units of unscaled products, and moves only for a sum above 2^60: weights, their
@@ -434,6 +434,10 @@ def build_groups(masked, tag):
         deal(ag, exp_stream(cur, range(EARLY, 8), fresh=False) + sum_check())
         ag[7]["post"] += [branch(f"s_cbranch_vccnz RARE_{tag}{j}"), label(f"BACK_{tag}{j}")] + sum_commit()
         if masked and WINDOWED:
+            if j:                        # the last tile's keys may end with unit j - 1: nothing is left to add
+                ag[0]["pre"] += [salu(f"s_lshl_b32 {S(S_T1)}, {S(S_T)}, 2", r=sr(S_T), w=sr(S_T1) + ["scc"]),
+                                 salu(f"s_or_b32 {S(S_T1)}, {S(S_T1)}, {j}", r=sr(S_T1), w=sr(S_T1) + ["scc"]),
+                                 salu(f"s_cmp_eq_u32 {S(S_T1)}, %[n_units]", r=sr(S_T1), w=["scc"]), branch("s_cbranch_scc1 FINISH")]
             if j == 3:                   # the unit that is formed now is the next tile's first
                 ag[0]["pre"] += [salu(f"s_add_u32 {S(S_T1)}, {S(S_T)}, 1", r=sr(S_T), w=sr(S_T1) + ["scc"]),
                                  salu(f"s_add_u32 {S(S_T2)}, {S(S_K0N)}, 32", r=sr(S_K0N), w=sr(S_T2) + ["scc"]),
@@ -762,7 +766,7 @@ def write(here, name, last_s):
                 salu(f"s_lshl_b32 {S(S_K0N)}, {S(S_K0N)}, 7", r=sr(S_K0N), w=sr(S_K0N) + ["scc"]),
                 salu(f"s_add_u32 {S(S_K0N)}, {S(S_K0N)}, %[start]", r=sr(S_K0N), w=sr(S_K0N) + ["scc"]),
                 label("LOOP_D")] + diag_body + loop_tail("LOOP_D", S(S_BOUND))
-        seq += [salu(f"s_cmp_lt_u32 {S(S_T)}, %[nkt]", r=sr(S_T), w=["scc"]), branch("s_cbranch_scc1 FRONT_DONE")]
+        seq += [salu(f"s_cmp_lt_u32 {S(S_T)}, %[nkt]", r=sr(S_T), w=["scc"]), branch("s_cbranch_scc1 FRONT_DONE"), label("FINISH")]
     else:
         # main loop over the tiles before the last three, then the masked loop over the rest
         seq += [salu(f"s_cmp_lt_u32 {S(S_T)}, %[nmain]", r=sr(S_T), w=["scc"]), branch("s_cbranch_scc0 MAIN_DONE"),

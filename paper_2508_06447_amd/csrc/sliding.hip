@@ -218,6 +218,7 @@ sliding_many_kernel(const bf16_t* __restrict__ Q, const bf16_t* __restrict__ Kg,
     const int start = tl.start, k00 = tl.k00;
     const unsigned nst = tl.apart, nkt = tl.all, nhead = tl.clean, nmain = tl.masked, last_tile = nkt - 1;
     const unsigned last_ragged = tl.left != LKV ? last_tile : 0xffffffffu, nl1 = tl.left - 1;   // rows of the last tile behind its keys repeat the last one
+    const unsigned n_units = 4 * last_tile + (tl.left + 31) / 32;
     const uint64_t jump = (uint64_t)(start - k00 - (int)nst * LKV) * rowbytes;
     const unsigned jump_lo = nst ? (unsigned)jump : 0, jump_hi = nst ? (unsigned)(jump >> 32) : 0;
     const uint64_t kb = (uint64_t)(uintptr_t)(Kg + (size_t)g * LD) + (uint64_t)k00 * rowbytes;
@@ -273,7 +274,7 @@ sliding_many_kernel(const bf16_t* __restrict__ Q, const bf16_t* __restrict__ Kg,
           [nkt] "s"(nkt), [nhead] "s"(nhead), [nmain] "s"(nmain), [nst] "s"(nst), [start] "s"(start), [last_tile] "s"(last_tile), [last_ragged] "s"(last_ragged),
           [rowbytes] "s"(rowbytes), [tile_bytes] "s"(tile_bytes), [jump_lo] "s"(jump_lo), [jump_hi] "s"(jump_hi), [scale] "s"(a.scale_log2e), [nl1] "s"(nl1),
           [ldsw] "s"(ldsw), [qw0] "s"(qw0), [lowq] "s"(lowq), [window] "s"(window), [sinks] "s"(sinks), [k00] "s"(k00),
-          [split] "s"(splits - 1)
+          [n_units] "s"(n_units), [split] "s"(splits - 1)
         :
 #include "sliding_bf16_clobbers.inc"
     );
