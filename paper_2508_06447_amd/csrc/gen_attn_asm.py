@@ -33,7 +33,7 @@ tiles of a workgroup (where keys can lie above queries) run a second copy of the
 Every wave of a workgroup runs the same number of units (masked keys give P = 0), so the barriers line up.
 
 WINDOWED.  The tiles of a workgroup are those of the first tokens, if any, then those from its first query's window on: the
-tile pointers and the key index jump between them.  The masked loop runs twice, over the tiles in front (first tokens, the
+tile pointers and the key index jump between them, or within the first tile.  The masked loop runs twice, over the tiles in front (first tokens, the
 rows' window edges) and over the last ones; per unit it masks where a key lies above some query of the wave, or behind some
 window and is no first token, and it ends behind the last unit with keys (2 % of a window of 4096 with four heads a kv head).  The first unit may be masked for a whole row, so the reference starts at the larger of that
 unit's maximum and the query's product with its own token, which comes as an operand.  Query fragments stay as they are and
@@ -285,6 +285,26 @@ def tile_load_instrs(which):
     return out
 
 
+def first_tile_load(which):
+    """WINDOWED: the first tile may begin with one to three units of first tokens; the others' rows lie `jump` further."""
+    out = tile_load_instrs(which)
+    if not WINDOWED:
+        return out
+    ptr, t = S_KPTR if which == 0 else S_VPTR, S_TMP + 2
+    # S_TMP: the unit's pointer, S_TMP + 2: that behind the jump
+    seq = [salu(f"s_add_u32 {S(t)}, {S(ptr)}, %[jump_lo]", r=sr(ptr), w=sr(t) + ["scc"]),
+           salu(f"s_addc_u32 {S(t + 1)}, {S(ptr + 1)}, %[jump_hi]", r=sr(ptr + 1) + ["scc"], w=sr(t + 1) + ["scc"])]
+    for i, x in enumerate(out):
+        if i % 4 == 0:                   # two loads a unit, each with its m0
+            seq += [salu(f"s_cmp_gt_u32 %[first_units], {i // 4}", w=["scc"]),
+                    salu(f"s_cselect_b32 {S(S_TMP)}, {S(ptr)}, {S(t)}", r=["scc"] + sr(ptr) + sr(t), w=sr(S_TMP)),
+                    salu(f"s_cselect_b32 {S(S_TMP + 1)}, {S(ptr + 1)}, {S(t + 1)}", r=["scc"] + sr(ptr + 1) + sr(t + 1), w=sr(S_TMP + 1))]
+        if x.kind == "vmem":
+            x = Ins(x.text.replace(S(ptr, 2), S(S_TMP, 2)), "vmem", r=(x.r - set(sr(ptr, 2))) | set(sr(S_TMP, 2)))
+        seq.append(x)
+    return seq
+
+
 _uid = [0]
 
 
@@ -434,17 +454,15 @@ def build_groups(masked, tag):
         deal(ag, exp_stream(cur, range(EARLY, 8), fresh=False) + sum_check())
         ag[7]["post"] += [branch(f"s_cbranch_vccnz RARE_{tag}{j}"), label(f"BACK_{tag}{j}")] + sum_commit()
         if masked and WINDOWED:
+            ag[0]["pre"] += [salu(f"s_lshl_b32 {S(S_T1)}, {S(S_T)}, 2", r=sr(S_T), w=sr(S_T1) + ["scc"])]
             if j:                        # the last tile's keys may end with unit j - 1: nothing is left to add
-                ag[0]["pre"] += [salu(f"s_lshl_b32 {S(S_T1)}, {S(S_T)}, 2", r=sr(S_T), w=sr(S_T1) + ["scc"]),
-                                 salu(f"s_or_b32 {S(S_T1)}, {S(S_T1)}, {j}", r=sr(S_T1), w=sr(S_T1) + ["scc"]),
+                ag[0]["pre"] += [salu(f"s_or_b32 {S(S_T1)}, {S(S_T1)}, {j}", r=sr(S_T1), w=sr(S_T1) + ["scc"]),
                                  salu(f"s_cmp_eq_u32 {S(S_T1)}, %[n_units]", r=sr(S_T1), w=["scc"]), branch("s_cbranch_scc1 FINISH")]
-            if j == 3:                   # the unit that is formed now is the next tile's first
-                ag[0]["pre"] += [salu(f"s_add_u32 {S(S_T1)}, {S(S_T)}, 1", r=sr(S_T), w=sr(S_T1) + ["scc"]),
-                                 salu(f"s_add_u32 {S(S_T2)}, {S(S_K0N)}, 32", r=sr(S_K0N), w=sr(S_T2) + ["scc"]),
-                                 salu(f"s_cmp_eq_u32 {S(S_T1)}, %[nst]", r=sr(S_T1), w=["scc"]),
-                                 salu(f"s_cselect_b32 {S(S_K0N)}, %[start], {S(S_T2)}", r=["scc"] + sr(S_T2), w=sr(S_K0N))]
-            else:
-                ag[0]["pre"] += [salu(f"s_add_u32 {S(S_K0N)}, {S(S_K0N)}, 32", r=sr(S_K0N), w=sr(S_K0N) + ["scc"])]
+            # the unit that is formed now is the next one: the stretch's first, behind those of the first tokens?
+            ag[0]["pre"] += [salu(f"s_add_u32 {S(S_T1)}, {S(S_T1)}, 1", r=sr(S_T1), w=sr(S_T1) + ["scc"]),
+                             salu(f"s_add_u32 {S(S_T2)}, {S(S_K0N)}, 32", r=sr(S_K0N), w=sr(S_T2) + ["scc"]),
+                             salu(f"s_cmp_eq_u32 {S(S_T1)}, %[first_units]", r=sr(S_T1), w=["scc"]),
+                             salu(f"s_cselect_b32 {S(S_K0N)}, %[start], {S(S_T2)}", r=["scc"] + sr(S_T2), w=sr(S_K0N))]
             ag[0]["pre"] += mask_wanted()
         elif masked:
             ag[0]["pre"] += [salu(f"s_add_u32 {S(S_K0N)}, {S(S_K0N)}, 32", r=sr(S_K0N), w=sr(S_K0N) + ["scc"]),
@@ -609,7 +627,7 @@ def prologue():
     e(salu(f"s_mov_b32 {S(S_VPTR)}, %[vbase_lo]", w=sr(S_VPTR)))
     e(salu(f"s_mov_b32 {S(S_VPTR + 1)}, %[vbase_hi]", w=sr(S_VPTR + 1)))
     out += flat([ragged_switch(0), ragged_switch(1)])
-    out += flat(tile_load_instrs(0) + tile_advance(0) + tile_load_instrs(1) + tile_advance(1) + tile_load_instrs(0) + tile_advance(0))
+    out += flat(first_tile_load(0) + tile_advance(0) + first_tile_load(1) + tile_advance(1) + tile_load_instrs(0) + tile_advance(0))
     for i in range(128):
         e(valu(f"v_accvgpr_write_b32 {A(O_ACC + i)}, 0", w=ar(O_ACC + i)))
     for qt in (0, 1):
@@ -762,9 +780,8 @@ def write(here, name, last_s):
                 label("FRONT_DONE"), salu(f"s_cmp_lt_u32 {S(S_T)}, %[nmain]", r=sr(S_T), w=["scc"]), branch("s_cbranch_scc0 MAIN_DONE"),
                 label("LOOP_M")] + main_body + loop_tail("LOOP_M", "%[nmain]") + [label("MAIN_DONE")]
         seq += [salu(f"s_mov_b32 {S(S_BOUND)}, %[nkt]", w=sr(S_BOUND)),
-                salu(f"s_sub_u32 {S(S_K0N)}, {S(S_T)}, %[nst]", r=sr(S_T), w=sr(S_K0N) + ["scc"]),
-                salu(f"s_lshl_b32 {S(S_K0N)}, {S(S_K0N)}, 7", r=sr(S_K0N), w=sr(S_K0N) + ["scc"]),
-                salu(f"s_add_u32 {S(S_K0N)}, {S(S_K0N)}, %[start]", r=sr(S_K0N), w=sr(S_K0N) + ["scc"]),
+                salu(f"s_lshl_b32 {S(S_K0N)}, {S(S_T)}, 7", r=sr(S_T), w=sr(S_K0N) + ["scc"]),
+                salu(f"s_add_u32 {S(S_K0N)}, {S(S_K0N)}, %[origin]", r=sr(S_K0N), w=sr(S_K0N) + ["scc"]),
                 label("LOOP_D")] + diag_body + loop_tail("LOOP_D", S(S_BOUND))
         seq += [salu(f"s_cmp_lt_u32 {S(S_T)}, %[nkt]", r=sr(S_T), w=["scc"]), branch("s_cbranch_scc1 FRONT_DONE"), label("FINISH")]
     else:

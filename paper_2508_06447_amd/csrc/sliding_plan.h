@@ -21,35 +21,44 @@ struct SlidingSpan {
     }
 };
 
-// The tiles of 128 keys of a workgroup with many rows: `apart` tiles from key k00 on, which hold the first tokens, then tiles from key `start` on, `all` in all.  Where the two would
-// meet inside a tile the stretch begins at key 0 and there is nothing apart.  Tiles `clean` .. `masked` - 1 need no mask, but for the first unit of 32 keys of tile `clean`; neither
-// does the first unit of tile `masked`.  The last tile is never among them.  left: keys of the last tile.
+// The tiles of 128 keys of a workgroup with many rows: `units` times 32 keys from key k00 on, which hold the first tokens, then keys from key `start` on; `apart` tiles have some of the
+// former, `all` there are.  Fewer than four such units share the first tile with the beginning of the stretch; four or more fill whole tiles.  Where the two would meet inside a unit
+// (inside a tile) the stretch begins at key 0 and there is nothing apart.  Tiles `clean` .. `masked` - 1 need no mask, but for the first unit of 32 keys of tile `clean`; neither does the
+// first unit of tile `masked`.  The last tile is never among them.  left: keys of the last tile.
 constexpr int kSlideTile = 128;
 struct SlidingTiles {
-    int k00, start, apart, all, clean, masked, left;
-    constexpr SlidingTiles(const SlidingSpan& s, int window) : k00(0), start(s.start), apart(0), all(0), clean(0), masked(0), left(0) {
-        const int tiles = (s.first + kSlideTile - 1) / kSlideTile;
-        if (s.first > 0 && tiles * kSlideTile <= s.start) apart = tiles;
-        else if (s.first > 0) start = 0;
-        if (apart == 0) k00 = start;
-        all = apart + (s.end - start + kSlideTile - 1) / kSlideTile;
+    int k00, start, units, apart, all, clean, masked, left;
+    constexpr SlidingTiles(const SlidingSpan& s, int window) : k00(0), start(s.start), units(0), apart(0), all(0), clean(0), masked(0), left(0) {
+        units = (s.first + 31) / 32;
+        if (units > 3) units = (units + 3) / 4 * 4;
+        if (units * 32 > s.start) {
+            start = 0;
+            units = 0;
+        }
+        apart = (units + 3) / 4;
+        if (units == 0) k00 = start;
+        const int before = units * 32;
+        all = (before + s.end - start + kSlideTile - 1) / kSlideTile;
         const int edge = s.p1 - window + 1 - start;      // keys of the stretch that some row's window does not reach
-        clean = apart + ((edge > 0 ? edge : 0) + kSlideTile - 1) / kSlideTile;
+        clean = (before + (edge > 0 ? edge : 0) + kSlideTile - 1) / kSlideTile;
         if (clean > all) clean = all;
         const int whole = s.p0 - 31 - start;
-        masked = apart + (whole > 0 ? whole : 0) / kSlideTile;
+        masked = (before + (whole > 0 ? whole : 0)) / kSlideTile;
         if (masked < clean) masked = clean;
-        left = s.end - start - (all - 1 - apart) * kSlideTile;
+        left = before + s.end - start - (all - 1) * kSlideTile;
     }
+    // Key of the stretch's tiles: that of tile i is origin() + 128 i.
+    constexpr int origin() const { return start - units * 32; }
     // Tiles from .. to - 1 of them (from < to), as a plan of its own.
     constexpr SlidingTiles part(int from, int to) const {
         SlidingTiles r = *this;
-        r.k00 = from < apart ? from * kSlideTile : start + (from - apart) * kSlideTile;
-        r.apart = to <= apart || from >= apart ? 0 : apart - from;
-        r.start = r.apart ? start : r.k00;
+        r.k00 = (from < apart ? k00 : origin()) + from * kSlideTile;
+        r.units = from >= apart || 4 * to <= units ? 0 : units - 4 * from;
+        r.apart = (r.units + 3) / 4;
+        r.start = r.units ? start : r.k00;
         r.all = to - from;
         r.clean = clean - from < r.apart ? r.apart : clean - from;
-        if (to <= apart || r.clean > r.all) r.clean = r.all;
+        if (4 * to <= units || r.clean > r.all) r.clean = r.all;
         r.masked = masked - from < r.all - 1 ? masked - from : r.all - 1;
         if (r.masked < r.clean) r.masked = r.clean;
         r.left = to == all ? left : kSlideTile;
@@ -86,7 +95,7 @@ inline int sliding_splits(int n_q, int n_k, int G, int Hkv, int window, int sink
 // all in sight, in 1 / 2 / 3 / 4 / 6 237 / 272 / 225 / 248 / 255.
 inline double sliding_many_us(int n_q, int n_k, int G, int Hkv, int window, int sinks, int parts) {
     const long long rows = (long long)n_q * G * Hkv, row_tiles = ((long long)n_q * G + 255) / 256 * Hkv, near = sliding_keys(n_q, n_k, G, window, 256);
-    const long long tiles = (near + kSlideTile - 1) / kSlideTile + (near < n_k ? (sinks + kSlideTile - 1) / kSlideTile : 0), rounds = (row_tiles * parts + 255) / 256;
+    const long long tiles = (near + (near < n_k ? (sinks + 31ll) / 32 * 32 : 0) + kSlideTile - 1) / kSlideTile, rounds = (row_tiles * parts + 255) / 256;
     return rounds * (12.0 + 2.8 * ((tiles + parts - 1) / parts)) + (parts > 1 ? 5.0 + rows * parts * 528.0 * 2 / 4.5e6 : 0.0);
 }
 // In how many parts a call's tiles of 256 rows run; 0: it runs in tiles of 16 rows (6 us, and over the whole chip 6 ns a tile and 1.8 ns a unit; 16 queries 17.7 us, in tiles of 256

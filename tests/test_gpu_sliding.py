@@ -114,6 +114,16 @@ def test_short_windows_of_many_queries(slim, window, sinks):
     check(out, q, k, v, window, sinks, rows=np.unique(np.concatenate((np.arange(0, 1100, 41), np.arange(1080, 1100)))))
 
 
+@pytest.mark.parametrize("n_q,n_k,window,sinks", [(1100, 1100, 300, 1), (1100, 1100, 300, 32), (1100, 1100, 257, 33), (1100, 1133, 300, 96), (1100, 1133, 290, 97), (1100, 1133, 290, 200),
+                                                  (512, 3000, 2000, 64), (512, 3001, 2001, 90), (512, 3000, 2000, 129), (480, 2100, 2000, 70)])
+def test_first_tokens_of_many_queries(slim, n_q, n_k, window, sinks):
+    """First tokens that share a tile with the window's beginning, that fill tiles, that meet it; the keys in one part and in several."""
+    q, k, v = inputs_of(n_q, n_k, 32, 8, 128, BF16, 13)
+    k[:sinks] *= 2                                        # what the first tokens hold counts
+    out = slim.slim_sliding_attn(q.cuda(), k.cuda(), v.cuda(), window, sinks)
+    check(out, q, k, v, window, sinks, rows=np.unique(np.concatenate((np.arange(0, n_q, 41), np.arange(n_q - 20, n_q)))))
+
+
 def test_chunks_and_single_tokens_give_the_rows_of_the_whole(slim):
     n, Hq, Hkv, d, window, sinks = 300, 8, 2, 128, 77, 5
     q, k, v = (x.cuda() for x in inputs_of(n, n, Hq, Hkv, d, BF16, 6))

@@ -119,3 +119,30 @@ def test_a_unit_that_some_query_does_not_see_whole_is_masked(ga):
                             assert wanted(k0n, first, first + span - window, sinks) == 1
                         elif k0n + 31 < sinks or k0n > first + span - window:
                             assert wanted(k0n, first, first + span - window, sinks) == 0
+
+
+def test_the_first_tile_jumps_behind_the_first_tokens(ga):
+    """Which pointer each of the tile's eight loads (16 rows each) takes."""
+    for which, ptr in ((0, ga.S_KPTR), (1, ga.S_VPTR)):
+        for units in range(5):
+            reg = {f"s{ptr}": 0xffffff00, f"s{ptr + 1}": 7, "%[jump_lo]": 0x300, "%[jump_hi]": 2, "%[first_units]": units, "%[ldsw]": 0,
+                   f"s{ga.S_KST}": 0, f"s{ga.S_VST}": 0}
+            val = lambda t: reg[t] if t in reg else int(t, 0)
+            scc, taken = 0, []
+            for x in ga.first_tile_load(which):
+                op, rest = x.text.split(" ", 1)
+                a = [t.strip() for t in rest.split(", ")]
+                if op in ("s_add_u32", "s_addc_u32"):
+                    total = val(a[1]) + val(a[2]) + (scc if op == "s_addc_u32" else 0)
+                    reg[a[0]], scc = total % 2**32, total >> 32
+                elif op == "s_cmp_gt_u32":
+                    scc = int(val(a[0]) > val(a[1]))
+                elif op == "s_cselect_b32":
+                    reg[a[0]] = val(a[1]) if scc else val(a[2])
+                else:
+                    assert op == "global_load_lds_dwordx4", x.text
+                    lo, hi = map(int, re.match(r"s\[(\d+):(\d+)\]", a[1]).groups())
+                    assert hi == lo + 1
+                    taken.append((reg[f"s{lo}"] | reg[f"s{hi}"] << 32, reg["m0"]))
+            here, jumped = 0x7ffffff00, 0xa00000200
+            assert taken == [(here if i < 2 * units else jumped, 4096 * i) for i in range(8)]

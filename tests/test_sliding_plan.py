@@ -29,18 +29,23 @@ static int check(const SlidingRows& a, int parts) {
             const int from = (int)((long long)split * whole.all / parts), to = (int)((long long)(split + 1) * whole.all / parts);
             if (from == to) continue;
             const SlidingTiles t = whole.part(from, to);
-            if (t.all != to - from || t.left < 1 || t.left > 128 || t.apart < 0 || t.clean < t.apart || t.clean > t.all || t.masked < t.clean ||
+            if (t.all != to - from || t.left < 1 || t.left > 128 || t.units < 0 || t.apart != (t.units + 3) / 4 ||
+                (t.units > 3 && t.units % 4) || (t.units && t.k00 + t.units * 32 > t.start) || t.clean < t.apart || t.clean > t.all || t.masked < t.clean ||
                 t.masked > (t.clean == t.all ? t.all : t.all - 1))
                 return fail(a, r0, "counts");
             for (int i = 0; i < t.all; ++i) {
-                const int k0 = i < t.apart ? t.k00 + i * 128 : t.start + (i - t.apart) * 128, n = i == t.all - 1 ? t.left : 128;
-                if (i == 0 && k0 != t.k00) return fail(a, r0, "first key");
-                if (k0 < 0 || k0 + n > a.n_k) return fail(a, r0, "outside");
-                for (int j = k0; j < k0 + n; ++j) ++times[j];
-                for (int u = 0; u < 4; ++u) {            // units whose logits the loop without masks forms
-                    const int idx = 4 * i + u;
+                const int n = i == t.all - 1 ? t.left : 128;
+                for (int u = 0; u < 4; ++u) {
+                    const int idx = 4 * i + u, k0 = idx < t.units ? t.k00 + idx * 32 : t.start + (idx - t.units) * 32, here = n - 32 * u < 32 ? n - 32 * u : 32;
+                    if (idx == 0 && k0 != t.k00) return fail(a, r0, "first key");
+                    if (idx >= t.units && k0 != t.origin() + 32 * idx) return fail(a, r0, "origin");
+                    if (here < 1) break;
+                    if (k0 < 0 || k0 + here > a.n_k) return fail(a, r0, "outside");
+                    for (int j = k0; j < k0 + here; ++j) ++times[j];
+                    // units whose logits the loop without masks forms
                     if (t.masked == t.clean || idx < 4 * t.clean + 1 || idx > 4 * t.masked) continue;
-                    for (int j = k0 + 32 * u; j < k0 + 32 * u + 32; ++j)
+                    if (here < 32) return fail(a, r0, "a short unit without a mask");
+                    for (int j = k0; j < k0 + 32; ++j)
                         for (int p = p0; p <= p1; p += p1 > p0 ? p1 - p0 : 1)
                             if (!(j <= p && (j > p - a.window || j < a.sinks))) return fail(a, r0, "mask");
                 }
@@ -63,8 +68,8 @@ int main() {
         const int heads[6] = {1, 2, 3, 4, 7, 20};
         a.G = heads[rnd(6)];
         a.window = 1 + rnd(c % 5 ? a.n_k : 1 + a.n_k / 8);
-        const int few[6] = {0, 1, 4, 64, 128, 130};
-        a.sinks = c % 7 ? few[rnd(6)] : rnd(a.n_k + 1);
+        const int few[10] = {0, 1, 4, 32, 33, 64, 90, 97, 128, 130};
+        a.sinks = c % 7 ? few[rnd(10)] : rnd(a.n_k + 1);
         if (a.sinks > a.n_k) a.sinks = a.n_k;
         const int most[8] = {1, 1, 2, 3, 5, 8, 17, 64};
         if (check(a, most[rnd(8)])) return 1;
