@@ -703,9 +703,9 @@ def epilogue():
         e(salu("s_cmp_lg_u32 %[split], 0", w=["scc"]))
         e(branch("s_cbranch_scc1 PARTIAL"))
 
-    def row(qt, vg, dt, store):
+    def row(qt, vg, dt, store, t=None):
         """Four channels of the lane's row of sub-tile qt, in t .. t + 3."""
-        t = TMP + 8 + 4 * (vg & 1)
+        t = t or TMP + 8 + 4 * (vg & 1)
         for k in range(4):
             e(valu(f"v_accvgpr_read_b32 {V(t + k)}, {A(O_ACC + (dt * 2 + qt) * 16 + vg * 4 + k)}", r=ar(O_ACC + (dt * 2 + qt) * 16 + vg * 4 + k), w=vr(t + k)))
         store(t, vg, dt)
@@ -715,15 +715,28 @@ def epilogue():
             for k in range(4):
                 e(valu(f"v_fma_f32 %[odd], {V(t + k)}, 0, %[odd]", r=vr(t + k)))
 
-    for qt in (0, 1):
-        inv = TMP + 4 + qt
+    def bf16_pairs(t, inv):
+        for k in range(4):
+            e(valu(f"v_mul_f32 {V(t + k)}, {V(t + k)}, {V(inv)}", r=vr(t + k) + vr(inv), w=vr(t + k)))
+        not_finite(t)
+        e(valu(f"v_cvt_pk_bf16_f32 {V(t)}, {V(t)}, {V(t + 1)}", r=vr(t, 2), w=vr(t)))
+        e(valu(f"v_cvt_pk_bf16_f32 {V(t + 1)}, {V(t + 2)}, {V(t + 3)}", r=vr(t + 2, 2), w=vr(t + 1)))
 
+    if WINDOWED:
+        # the rows go to LDS, 16-byte piece c of row r at c ^ r % 16: from there they are written whole (in eight-byte pieces 32 rows apart they took 5 us of a workgroup)
+        e(raw("s_barrier", "barrier"))           # nobody reads tiles any more, and no load is on its way
+        for dt in range(4):
+            for vg in range(4):
+                at = TMP + 16 + (vg & 1)
+                e(valu(f"v_xor_b32 {V(at)}, {(dt * 4 + vg) << 4}, %[oaddr]", w=vr(at)))
+                for qt in (0, 1):
+                    def to_lds(t, vg, dt):
+                        bf16_pairs(t, TMP + 4 + qt)
+                        e(Ins(f"ds_write_b64 {V(at)}, {V(t, 2)} offset:{qt * 8192}", "lds", r=vr(at) + vr(t, 2)))
+                    row(qt, vg, dt, to_lds, TMP + 8 + 4 * qt)
+    for qt in () if WINDOWED else (0, 1):
         def finished(t, vg, dt):
-            for k in range(4):
-                e(valu(f"v_mul_f32 {V(t + k)}, {V(t + k)}, {V(inv)}", r=vr(t + k) + vr(inv), w=vr(t + k)))
-            not_finite(t)
-            e(valu(f"v_cvt_pk_bf16_f32 {V(t)}, {V(t)}, {V(t + 1)}", r=vr(t, 2), w=vr(t)))
-            e(valu(f"v_cvt_pk_bf16_f32 {V(t + 1)}, {V(t + 2)}, {V(t + 3)}", r=vr(t + 2, 2), w=vr(t + 1)))
+            bf16_pairs(t, TMP + 4 + qt)
             e(Ins(f"global_store_dwordx2 %[orow{qt}], {V(t, 2)}, off offset:{(dt * 32 + 8 * vg) * 2}", "vmem", r=vr(t, 2)))
         e(valu(f"v_cmp_ne_u32 vcc, 0, %[valid{qt}]", w=["vcc"], kind="vcmp"))
         e(raw(f"s_and_saveexec_b64 {S(S_SAVE, 2)}, vcc", "salu", r=["vcc"], w=sr(S_SAVE, 2) + ["exec"]))

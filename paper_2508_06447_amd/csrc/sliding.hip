@@ -235,8 +235,7 @@ sliding_many_kernel(const bf16_t* __restrict__ Q, const bf16_t* __restrict__ Kg,
     const int ra = min(rw + l32, rows - 1), rb = min(rw + 32 + l32, rows - 1), ia = ra / a.G, ib = rb / a.G;
     const size_t qa = ((size_t)ia * Hq + g * a.G + (ra - ia * a.G)) * LD, qb = ((size_t)ib * Hq + g * a.G + (rb - ib * a.G)) * LD;
     const bf16_t *qrow0 = Q + qa + hh * 8, *qrow1 = Q + qb + hh * 8;
-    void *orow0 = splits > 1 ? (void*)(part_rows + (size_t)ra * kPartRow + 4 * hh) : O + qa + 4 * hh;
-    void *orow1 = splits > 1 ? (void*)(part_rows + (size_t)rb * kPartRow + 4 * hh) : O + qb + 4 * hh;
+    float *orow0 = part_rows + (size_t)ra * kPartRow + 4 * hh, *orow1 = part_rows + (size_t)rb * kPartRow + 4 * hh;      // used where there are parts
     const int hh4 = 4 * hh, limabs0 = off + ia - hh4, limabs1 = off + ib - hh4;
     const unsigned valid0 = rw + l32 < rows, valid1 = rw + 32 + l32 < rows;
     // Each row's product with its own token: a reference that is never minus infinity, whatever the first unit's mask leaves of the row.
@@ -267,12 +266,13 @@ sliding_many_kernel(const bf16_t* __restrict__ Q, const bf16_t* __restrict__ Kg,
     const unsigned row0 = wave * 4 + (lane >> 4), slot = lane & 15;
     const unsigned kchunk = (slot ^ (row0 & 15)) * 16, vchunk = (slot ^ ((row0 & 3) << 2)) * 16;
     const unsigned ldsw = lds_base + wave * 1024;
+    const unsigned oaddr = lds_base + wave * (64 * LD * 2) + l32 * (LD * 2) + ((l32 & 15) << 4) + 8 * hh;              // of the lane's first row of the result
     float odd = 0.f;                                     // not 0: some result is not finite
 
     asm volatile(
 #include "sliding_bf16_body.inc"
         : [odd] "+v"(odd)
-        : [koff0] "v"(koff0), [voff0] "v"(voff0), [r0] "v"(row0), [kchunk] "v"(kchunk), [vchunk] "v"(vchunk),
+        : [oaddr] "v"(oaddr), [koff0] "v"(koff0), [voff0] "v"(voff0), [r0] "v"(row0), [kchunk] "v"(kchunk), [vchunk] "v"(vchunk),
           [qrow0] "v"(qrow0), [qrow1] "v"(qrow1), [orow0] "v"(orow0), [orow1] "v"(orow1),
           [limabs0] "v"(limabs0), [limabs1] "v"(limabs1), [valid0] "v"(valid0), [valid1] "v"(valid1), [own0] "v"(own0), [own1] "v"(own1), [hh4] "v"(hh4),
           [kbase_lo] "s"(kbase_lo), [kbase_hi] "s"(kbase_hi), [vbase_lo] "s"(vbase_lo), [vbase_hi] "s"(vbase_hi),
@@ -283,6 +283,21 @@ sliding_many_kernel(const bf16_t* __restrict__ Q, const bf16_t* __restrict__ Kg,
         :
 #include "sliding_bf16_clobbers.inc"
     );
+    if (splits == 1) {                                   // the wave's 64 rows lie in LDS as bfloat16: four of them at a time
+        const int c = lane & 15, step_i = 4 / a.G, step_h = 4 - step_i * a.G;
+        int r = rw + (lane >> 4), i = r / a.G, h = r - i * a.G;
+        const unsigned char* src = lds + wave * (64 * LD * 2);
+#pragma unroll
+        for (int t = 0; t < 16; ++t) {
+            const int x = t * 4 + (lane >> 4);
+            const uint4 v = *reinterpret_cast<const uint4*>(src + x * (LD * 2) + ((c ^ (x & 15)) << 4));
+            if (r < rows) *reinterpret_cast<uint4*>(O + ((size_t)i * Hq + g * a.G + h) * LD + c * 8) = v;
+            r += 4;
+            i += step_i;
+            h += step_h;
+            if (h >= a.G) { h -= a.G; ++i; }
+        }
+    }
     // Keys or values that are not finite: perhaps behind a mask, where a weight of 0 does not undo them.  The wave's rows are computed again, 16 at a time.
     __syncthreads();
     if (!__any(!(odd == 0.f))) return;
