@@ -40,8 +40,9 @@ unit's maximum and the query's product with its own token, which comes as an ope
 S is scaled in float on its way into the exponential (a scaled Query rounded to bf16 again is off by 2^-9 per channel: the
 largest error of the whole); the reference is in units of unscaled products, and moves only for a sum above 2^60: weights, their
 sums and O are floats, whose relative error does not depend on where the reference lies (with queries that each meet one key 12
-bits above the others, half of the units moved it at 2^8).  With %[split] the workgroup has seen a part of the keys: the epilogue
-leaves O as it is, in float, with the reference (scaled) and the sum behind it.  It reports a result that is not finite.
+bits above the others, half of the units moved it at 2^8).  The epilogue leaves the rows in LDS, in
+bfloat16, or, with %[split], where the workgroup has seen a part of the keys, as they are, in float, and stores each row's
+reference (scaled) and sum.  It reports a result that is not finite.
 
 Wait states between dependent instructions (matrix result -> vector ALU 12, vector ALU -> matrix operand 2,
 transcendental -> use 1, compare -> select 2, ...) are checked on the finished instruction list and padded with
@@ -747,23 +748,24 @@ def epilogue():
     if not WINDOWED:
         return out
     e(branch("s_branch DONE"))
-    e(label("PARTIAL"))
-    for qt in (0, 1):
-        def partial(t, vg, dt):
-            not_finite(t)
-            e(Ins(f"global_store_dwordx4 %[orow{qt}], {V(t, 4)}, off offset:{(dt * 32 + 8 * vg) * 4}", "vmem", r=vr(t, 4)))
+    e(label("PARTIAL"))                          # the same with floats: 16-byte piece c of row r at c ^ r % 32
+    e(raw("s_barrier", "barrier"))
+    for dt in range(4):
+        for vg in range(4):
+            at = TMP + 16 + (vg & 1)
+            e(valu(f"v_xor_b32 {V(at)}, {(dt * 8 + vg * 2) << 4}, %[oaddr]", w=vr(at)))
+            for qt in (0, 1):
+                def floats_to_lds(t, vg, dt):
+                    not_finite(t)
+                    e(Ins(f"ds_write_b128 {V(at)}, {V(t, 4)} offset:{qt * 16384}", "lds", r=vr(at) + vr(t, 4)))
+                row(qt, vg, dt, floats_to_lds, TMP + 8 + 4 * qt)
+    for qt in (0, 1):                            # the reference and the sum, by the first of the row's two lanes
         e(valu(f"v_mul_f32 {V(TMP + 6)}, %[scale], {V(REF[qt])}", r=vr(REF[qt]), w=vr(TMP + 6)))
         e(valu(f"v_mov_b32 {V(TMP + 7)}, {V(LRUN[qt])}", r=vr(LRUN[qt]), w=vr(TMP + 7)))
         e(valu(f"v_fma_f32 %[odd], {V(TMP + 7)}, 0, %[odd]", r=vr(TMP + 7)))
         e(valu(f"v_cmp_ne_u32 vcc, 0, %[valid{qt}]", w=["vcc"], kind="vcmp"))
         e(raw(f"s_and_saveexec_b64 {S(S_SAVE, 2)}, vcc", "salu", r=["vcc"], w=sr(S_SAVE, 2) + ["exec"]))
-        for dt in range(4):
-            for vg in range(4):
-                row(qt, vg, dt, partial)
-        e(valu("v_cmp_eq_u32 vcc, 0, %[hh4]", w=["vcc"], kind="vcmp"))          # the first of the row's two lanes: its address is the row's
-        e(nop(4))
-        e(raw("s_and_b64 exec, exec, vcc", "salu", r=["vcc"], w=["exec"]))
-        e(Ins(f"global_store_dwordx2 %[orow{qt}], {V(TMP + 6, 2)}, off offset:512", "vmem", r=vr(TMP + 6, 2)))
+        e(Ins(f"global_store_dwordx2 %[stat{qt}], {V(TMP + 6, 2)}, off", "vmem", r=vr(TMP + 6, 2)))
         e(raw(f"s_mov_b64 exec, {S(S_SAVE, 2)}", "salu", r=sr(S_SAVE, 2), w=["exec"]))
     return out
 

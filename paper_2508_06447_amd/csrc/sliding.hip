@@ -186,8 +186,10 @@ __global__ void __launch_bounds__(64 * kSlideWaves) sliding_rows_kernel(const T*
 // ---- many rows: bfloat16, 256 rows per workgroup, 64 per wave
 // The loop of the prompt attention (gen_attn_asm.py, which says how it runs), over the tiles of 128 keys that the workgroup's rows see: those of the first tokens, if the stretch
 // leaves any behind, then the stretch; up to 96 first tokens share a tile with its beginning (with a tile of their own 32768 tokens, window 1024 637 us instead of 596,
-// window 4096 1775 instead of 1748).
-// Where the two would meet the stretch begins at key 0 instead.
+// window 4096 1775 instead of 1748).  Where the two would meet the stretch begins at key 0 instead.
+// Bound by the matrix instructions and what stands between them in the loop, 2.8 us for a tile of 128 keys on every CU (1.5 PFLOP/s), and by what a workgroup does beside its tiles,
+// about 10 us with its CU to itself (first loads 5, softmax reference and edges 2, results 3): 32768 tokens of 32 / 8 heads, window 4096, 1.70 ms (1.21 PFLOP/s), window 1024 0.59 ms
+// (0.92), window 256 0.30 ms (0.46).
 constexpr int LD = 128, LW = 4, LKV = kSlideTile, LTILE_BYTES = LKV * LD * 2, LSTAGE_BYTES = 2 * LTILE_BYTES, LSTAGES = 2, LROWS = 64 * LW;
 constexpr int kPartRow = LD + 4;         // floats of a row's partial result (16-byte aligned)
 
@@ -235,9 +237,9 @@ sliding_many_kernel(const bf16_t* __restrict__ Q, const bf16_t* __restrict__ Kg,
     const int ra = min(rw + l32, rows - 1), rb = min(rw + 32 + l32, rows - 1), ia = ra / a.G, ib = rb / a.G;
     const size_t qa = ((size_t)ia * Hq + g * a.G + (ra - ia * a.G)) * LD, qb = ((size_t)ib * Hq + g * a.G + (rb - ib * a.G)) * LD;
     const bf16_t *qrow0 = Q + qa + hh * 8, *qrow1 = Q + qb + hh * 8;
-    float *orow0 = part_rows + (size_t)ra * kPartRow + 4 * hh, *orow1 = part_rows + (size_t)rb * kPartRow + 4 * hh;      // used where there are parts
+    float *stat0 = part_rows + (size_t)ra * kPartRow + LD, *stat1 = part_rows + (size_t)rb * kPartRow + LD;              // used where there are parts
     const int hh4 = 4 * hh, limabs0 = off + ia - hh4, limabs1 = off + ib - hh4;
-    const unsigned valid0 = rw + l32 < rows, valid1 = rw + 32 + l32 < rows;
+    const unsigned valid0 = hh == 0 && rw + l32 < rows, valid1 = hh == 0 && rw + 32 + l32 < rows;
     // Each row's product with its own token: a reference that is never minus infinity, whatever the first unit's mask leaves of the row.
     auto own_product = [&](const bf16_t* qr, int i) {
         const bf16_t* kr = Kg + ((size_t)(off + i) * a.Hkv + g) * LD + hh * 8;
@@ -266,14 +268,15 @@ sliding_many_kernel(const bf16_t* __restrict__ Q, const bf16_t* __restrict__ Kg,
     const unsigned row0 = wave * 4 + (lane >> 4), slot = lane & 15;
     const unsigned kchunk = (slot ^ (row0 & 15)) * 16, vchunk = (slot ^ ((row0 & 3) << 2)) * 16;
     const unsigned ldsw = lds_base + wave * 1024;
-    const unsigned oaddr = lds_base + wave * (64 * LD * 2) + l32 * (LD * 2) + ((l32 & 15) << 4) + 8 * hh;              // of the lane's first row of the result
+    // of the lane's first row of the result, which is there in bfloat16, or in float where there are parts
+    const unsigned oaddr = splits == 1 ? lds_base + wave * (64 * LD * 2) + l32 * (LD * 2) + ((l32 & 15) << 4) + 8 * hh : lds_base + wave * (64 * LD * 4) + l32 * (LD * 4) + ((l32 ^ hh) << 4);
     float odd = 0.f;                                     // not 0: some result is not finite
 
     asm volatile(
 #include "sliding_bf16_body.inc"
         : [odd] "+v"(odd)
         : [oaddr] "v"(oaddr), [koff0] "v"(koff0), [voff0] "v"(voff0), [r0] "v"(row0), [kchunk] "v"(kchunk), [vchunk] "v"(vchunk),
-          [qrow0] "v"(qrow0), [qrow1] "v"(qrow1), [orow0] "v"(orow0), [orow1] "v"(orow1),
+          [qrow0] "v"(qrow0), [qrow1] "v"(qrow1), [stat0] "v"(stat0), [stat1] "v"(stat1),
           [limabs0] "v"(limabs0), [limabs1] "v"(limabs1), [valid0] "v"(valid0), [valid1] "v"(valid1), [own0] "v"(own0), [own1] "v"(own1), [hh4] "v"(hh4),
           [kbase_lo] "s"(kbase_lo), [kbase_hi] "s"(kbase_hi), [vbase_lo] "s"(vbase_lo), [vbase_hi] "s"(vbase_hi),
           [nkt] "s"(nkt), [nhead] "s"(nhead), [nmain] "s"(nmain), [nst] "s"(nst), [first_units] "s"(first_units), [origin] "s"(tl.origin()), [start] "s"(start), [last_tile] "s"(last_tile), [last_ragged] "s"(last_ragged),
@@ -283,7 +286,8 @@ sliding_many_kernel(const bf16_t* __restrict__ Q, const bf16_t* __restrict__ Kg,
         :
 #include "sliding_bf16_clobbers.inc"
     );
-    if (splits == 1) {                                   // the wave's 64 rows lie in LDS as bfloat16: four of them at a time
+    // The wave's 64 rows lie in LDS: whole rows are written, past the caches, which hold keys (8192 tokens, window 256 76.7 us without, 71.0; 32768, window 4096 1720 / 1699).
+    if (splits == 1) {
         const int c = lane & 15, step_i = 4 / a.G, step_h = 4 - step_i * a.G;
         int r = rw + (lane >> 4), i = r / a.G, h = r - i * a.G;
         const unsigned char* src = lds + wave * (64 * LD * 2);
@@ -291,11 +295,20 @@ sliding_many_kernel(const bf16_t* __restrict__ Q, const bf16_t* __restrict__ Kg,
         for (int t = 0; t < 16; ++t) {
             const int x = t * 4 + (lane >> 4);
             const uint4 v = *reinterpret_cast<const uint4*>(src + x * (LD * 2) + ((c ^ (x & 15)) << 4));
-            if (r < rows) *reinterpret_cast<uint4*>(O + ((size_t)i * Hq + g * a.G + h) * LD + c * 8) = v;
+            if (r < rows) store_stream16(O + ((size_t)i * Hq + g * a.G + h) * LD + c * 8, v);
             r += 4;
             i += step_i;
             h += step_h;
             if (h >= a.G) { h -= a.G; ++i; }
+        }
+    } else {
+        const int c = lane & 31;
+        const unsigned char* src = lds + wave * (64 * LD * 4);
+#pragma unroll
+        for (int t = 0; t < 32; ++t) {
+            const int x = t * 2 + (lane >> 5);
+            const uint4 v = *reinterpret_cast<const uint4*>(src + x * (LD * 4) + ((c ^ (x & 31)) << 4));
+            if (rw + x < rows) *reinterpret_cast<uint4*>(part_rows + (size_t)(rw + x) * kPartRow + c * 4) = v;
         }
     }
     // Keys or values that are not finite: perhaps behind a mask, where a weight of 0 does not undo them.  The wave's rows are computed again, 16 at a time.
