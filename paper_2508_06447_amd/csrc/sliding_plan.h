@@ -81,13 +81,15 @@ inline long long sliding_units_of_tile(int n_q, int n_k, int G, int window, int 
 }
 // Workgroups of four waves that share a tile: 512 of them in all for up to 64 rows of the output (a token 9.0 us, with 256 10.0; 2 tokens 10.6 / 10.7), 256 where there are more, since
 // every part of a row is written and read once more (4 tokens 12.4 / 11.9, 16 20.1 / 17.7, 32 26.9 / 24.6; float32, 1000 queries of 4 / 2 heads of 64, window 300, 12.7 / 11.1); every
-// wave the same number of units where that can be.
+// wave the same number of units where that can be.  A part that saves a wave one unit costs its launch (a token with a window of 100 7.2 / 6.9 us alone, 64 with 256 12.0 / 10.8; two
+// units, a token with a window of 256 7.0 / 8.2).
 inline int sliding_splits(int n_q, int n_k, int G, int Hkv, int window, int sinks, int most_parts) {
     const long long tiles = ((long long)n_q * G + 15) / 16 * Hkv, units = sliding_units_of_tile(n_q, n_k, G, window, sinks);
     long long most = ((long long)n_q * G * Hkv <= 64 ? 512 : 256) / tiles;
     most = most < 1 ? 1 : most > most_parts ? most_parts : most;
     const long long rounds = (units + 4 * most - 1) / (4 * most), want = (units + 4 * rounds - 1) / (4 * rounds);
-    return (int)(want < most ? want : most);
+    const long long parts = want < most ? want : most;
+    return (units + 3) / 4 - (units + 4 * parts - 1) / (4 * parts) < 2 ? 1 : (int)parts;
 }
 
 // Tiles of 256 rows: one CU holds one workgroup, 256 of them run at once; a workgroup takes 12 us and 2.8 us a tile of 128 keys; parts are written and read once more, 528 bytes a

@@ -100,7 +100,8 @@ def test_routes(tmp_path):
     parts = [((16, 8208, 4, 8, 4096, 64), 0), ((32, 8224, 4, 8, 4096, 64), 0), ((64, 2000, 7, 4, 500, 4), 0), ((1, 32768, 4, 8, 32768, 0), 0), ((1, 1, 1, 1, 1, 0), 0),
              ((512, 8704, 4, 8, 4096, 64), 4), ((2048, 10240, 4, 8, 4096, 64), 1), ((1511, 11367, 7, 4, 11367, 0), 3), ((32768, 32768, 4, 8, 4096, 64), 1),
              ((4096, 4096, 4, 8, 512, 0), 1), ((1024, 1024, 4, 8, 300, 4), 1)]
-    splits = [((1, 8193, 4, 8, 4096, 64), 33), ((16, 8208, 4, 8, 4096, 64), 7), ((1, 1, 1, 1, 1, 0), 1), ((2048, 2048, 2, 2, 2048, 0), 1)]
+    splits = [((1, 8193, 4, 8, 4096, 64), 33), ((16, 8208, 4, 8, 4096, 64), 7), ((1, 1, 1, 1, 1, 0), 1), ((2048, 2048, 2, 2, 2048, 0), 1),
+              ((1, 32768, 4, 8, 100, 4), 1), ((64, 8000, 4, 8, 256, 4), 1), ((1, 32768, 4, 8, 256, 64), 3)]
     src, exe = tmp_path / "routes.cpp", tmp_path / "routes"
     text = '#include "sliding_plan.h"\n#include <cstdio>\nusing namespace slim;\nint main() {\n'
     for args, _ in parts:
