@@ -23,6 +23,8 @@ __device__ __forceinline__ int own_kv_head(int Hkv, int& number) {
 }
 
 // ---- few rows: 16 of them per workgroup, the units of 32 keys dealt to its waves and to `splits` workgroups
+// Bound by latency (a token over 4160 keys of 32 / 8 heads 7 us and 2.2 for the merge: Query and keys in one trip to memory, the waves' merge, the workgroups'), and from some hundred
+// tiles on by how fast the CUs take keys, 1.8 ns a unit of 16 KB over the whole chip (sliding_plan.h).  Keys one unit ahead in registers: slower, fewer waves share a CU then.
 constexpr int kSlideWaves = 4;
 
 // Values of keys of the unit that some row does not see may be infinite or undefined: their weight is 0, which a product would turn into an undefined sum.  The unit's values
