@@ -363,17 +363,24 @@ def kv4_block_bytes(block: int, n_kv_heads: int, head_dim: int) -> int:
     return load_library().slim_kv4_block_bytes(block, n_kv_heads, head_dim)
 
 
-def _rows(t: torch.Tensor, name: str):
-    """(address, row stride in elements) of rows [n, H, d] on the GPU; only the distance of the rows is free."""
-    if not t.is_cuda:
-        raise ValueError(f"{name} must be a GPU tensor")
+def _row_stride(t: torch.Tensor, name: str) -> int:
+    """In elements, of rows [n, H, d]; only the distance of the rows is free."""
     n, H, d = t.shape
-    if t.is_contiguous():
-        return t.data_ptr(), H * d
     s0, s1, s2 = t.stride()
     if (d > 1 and s2 != 1) or (H > 1 and s1 != d):
         raise ValueError(f"{name} must have dense rows")
-    return t.data_ptr(), s0 if n > 1 else H * d
+    return s0 if n > 1 else H * d
+
+
+def _rows(k: torch.Tensor, v: torch.Tensor, names: str):
+    """(rows, heads, head size, addresses, row strides) of two like tensors [n, H, d] on the GPU."""
+    shape = k.shape
+    if v.shape != shape or v.dtype != k.dtype:
+        raise ValueError(f"{names} must be alike")
+    if not (k.is_cuda and v.is_cuda):
+        raise ValueError(f"{names} must be GPU tensors")
+    n, H, d = shape
+    return (n, H, d, k.data_ptr(), v.data_ptr(), H * d if k.is_contiguous() else _row_stride(k, names), H * d if v.is_contiguous() else _row_stride(v, names))
 
 
 def _slots(pool: torch.Tensor):
@@ -395,11 +402,7 @@ def slim_kv4_write(k: torch.Tensor, v: torch.Tensor, pool: torch.Tensor, block: 
     """k, v[n, Hkv, d] (rows may be apart) = tokens first_token .. of the prompt -> their blocks' slots of pool[slots, ...] in 4 bits.
     slot_of_block[n_blocks] int32, None: block b in slot b.  pool: on the GPU or pinned host memory.  Returns pool."""
     lib = load_library()
-    n, Hkv, d = k.shape
-    if v.shape != k.shape or v.dtype != k.dtype:
-        raise ValueError("k and v must be alike")
-    kp, ldk = _rows(k, "k")
-    vp, ldv = _rows(v, "v")
+    n, Hkv, d, kp, vp, ldk, ldv = _rows(k, v, "k and v")
     at, ns, size = _slots(pool)
     _check(lib.slim_kv4_write(kp, vp, ldk, ldv, first_token, n, Hkv, d, block, _dtype_code(k), _index(slot_of_block, "slot_of_block"),
                               ns if slot_of_block is None else slot_of_block.numel(), at, ns, size, layer_offset, _stream()), "slim_kv4_write")
@@ -422,11 +425,9 @@ def slim_kv4_read(pool: torch.Tensor, block: int, n_tokens: int, slot_of_block: 
     if k_out is None:
         k_out = torch.empty(max(rows, 0), n_kv_heads, head_dim, dtype=dtype, device=pool.device if pool.is_cuda else torch.cuda.current_device())
         v_out = torch.empty_like(k_out)
-    n_rows, Hkv, d = k_out.shape
-    if k_out.shape != v_out.shape or k_out.dtype != v_out.dtype or n_rows < rows:
-        raise ValueError("k_out and v_out must be alike and hold the rows")
-    kp, ldk = _rows(k_out, "k_out")
-    vp, ldv = _rows(v_out, "v_out")
+    n_rows, Hkv, d, kp, vp, ldk, ldv = _rows(k_out, v_out, "k_out and v_out")
+    if n_rows < rows:
+        raise ValueError("k_out and v_out must hold the rows")
     at, ns, size = _slots(pool)
     _check(lib.slim_kv4_read(at, ns, size, layer_offset, _index(slot_of_block, "slot_of_block"), _index(blocks, "blocks"), n_list, block, n_tokens, Hkv, d,
                              _dtype_code(k_out), kp, vp, n_rows, ldk, ldv, _stream()), "slim_kv4_read")
