@@ -148,13 +148,14 @@ def _check(code: int, where: str):
         raise SlimError(code, where, detail)
 
 
+_DTYPES = {torch.float32: F32, torch.bfloat16: BF16}
+
+
 def _dtype_code(t: torch.Tensor) -> int:
-    dtype = t.dtype
-    if dtype == torch.float32:
-        return F32
-    if dtype == torch.bfloat16:
-        return BF16
-    raise TypeError(f"unsupported dtype {dtype}")
+    code = _DTYPES.get(t.dtype)
+    if code is None:
+        raise TypeError(f"unsupported dtype {t.dtype}")
+    return code
 
 
 def _dev(t: torch.Tensor | None, name: str):
@@ -167,12 +168,18 @@ def _dev(t: torch.Tensor | None, name: str):
     return t.data_ptr()
 
 
+_device = _raw_stream = None           # the runtime's functions, once torch has initialised the GPU
+
+
 def _stream() -> int:
     """The current device's current stream.  Asked of torch's runtime directly: torch.cuda.current_stream() resolves the device through
     os.environ and builds a Stream object, 7 of the 9 us that a call of this binding took on the host."""
-    if not torch.cuda.is_initialized():
-        return torch.cuda.current_stream().cuda_stream
-    return torch._C._cuda_getCurrentRawStream(torch._C._cuda_getDevice())
+    global _device, _raw_stream
+    if _raw_stream is None:
+        if not torch.cuda.is_initialized():
+            return torch.cuda.current_stream().cuda_stream
+        _device, _raw_stream = torch._C._cuda_getDevice, torch._C._cuda_getCurrentRawStream
+    return _raw_stream(_device())
 
 
 def n_blocks(n_tokens: int, block: int) -> int:
@@ -270,10 +277,12 @@ def _decode_attn(name: str, q, gpu_pool, block_of_slot, block, n_prompt_tokens, 
         out = torch.empty_like(q)
     if workspace is None:
         workspace = torch.empty(max(lib.slim_decode_attn_workspace_bytes(ns, n_resp, Hq), 256), dtype=torch.uint8, device=q.device)
-    _check(getattr(lib, name)(_dev(q, "q"), _dev(gpu_pool, "gpu_pool"), slot_bytes, layer_offset,
+    code = getattr(lib, name)(_dev(q, "q"), _dev(gpu_pool, "gpu_pool"), slot_bytes, layer_offset,
                               _dev(block_of_slot, "block_of_slot"), ns, block, n_prompt_tokens, _dev(k_response, "k_response"),
                               _dev(v_response, "v_response"), n_resp, Hq, n_kv_heads, d, softmax_scale, _dtype_code(q),
-                              _dev(out, "out"), _dev(workspace, "workspace"), workspace.numel(), _stream()), name)
+                              _dev(out, "out"), _dev(workspace, "workspace"), workspace.numel(), _stream())
+    if code:
+        _check(code, name)
     return out
 
 
@@ -299,7 +308,7 @@ def slim_decode_attn_kv4(q: torch.Tensor, gpu_pool: torch.Tensor, block_of_slot:
         raise ValueError("out must be like q")
     if k_response is not None:
         n, h, d = k_response.shape
-        if v_response is None or h != n_kv_heads or not k_response.dtype == v_response.dtype == dtype or v_response.numel() != n * h * d or d != q.shape[-1]:
+        if v_response is None or h != n_kv_heads or k_response.dtype != dtype or v_response.dtype != dtype or v_response.numel() != n * h * d or d != q.shape[-1]:
             raise ValueError("k_response and v_response must be alike, [n, Hkv, d] of q's type")
     return _decode_attn("slim_decode_attn_kv4", q, gpu_pool, block_of_slot, block, n_prompt_tokens, n_kv_heads, k_response, v_response, layer_offset,
                         softmax_scale, out, workspace)
@@ -643,13 +652,14 @@ def slim_sliding_attn(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, window:
     """q[n_q,Hq,d] = the last n_q of the n_k tokens of k/v[n_k,Hkv,d] -> out[n_q,Hq,d]: causal attention over the last `window` tokens and the
     first n_sinks."""
     lib = load_library()
-    n_q, Hq, d = q.shape
-    n_k, Hkv, _ = k.shape
-    if v.shape != k.shape or k.shape[2] != d or not q.dtype == k.dtype == v.dtype:
+    q_shape, k_shape, dtype = q.shape, k.shape, q.dtype
+    n_q, Hq, d = q_shape
+    n_k, Hkv, k_d = k_shape
+    if v.shape != k_shape or k_d != d or k.dtype != dtype or v.dtype != dtype:
         raise ValueError("q, k and v do not match")
     if out is None:
         out = torch.empty_like(q)
-    elif out.shape != q.shape or out.dtype != q.dtype:
+    elif out.shape != q_shape or out.dtype != dtype:
         raise ValueError("out must be like q")
     code = _dtype_code(q)
     if workspace is None:
