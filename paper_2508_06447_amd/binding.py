@@ -266,15 +266,25 @@ def slim_score_blocks_from_unit_keys(q_win: torch.Tensor, k_rep: torch.Tensor, n
     return scores
 
 
-def _decode_attn(name: str, q, gpu_pool, block_of_slot, block, n_prompt_tokens, n_kv_heads, k_response, v_response, layer_offset, softmax_scale,
+def _decode_attn(name: str, checked: bool, q, gpu_pool, block_of_slot, block, n_prompt_tokens, n_kv_heads, k_response, v_response, layer_offset, softmax_scale,
                  out, workspace) -> torch.Tensor:
     lib = load_library()
     Hq, d = q.shape
+    dtype = q.dtype
     ns = block_of_slot.numel()
     slot_bytes = gpu_pool.numel() // gpu_pool.shape[0] * gpu_pool.element_size() if ns else 0
-    n_resp = 0 if k_response is None else k_response.shape[0]
+    n_resp = 0
+    if k_response is not None:
+        shape = k_response.shape
+        n_resp = shape[0]
+        if checked and (shape[1:] != (n_kv_heads, d) or k_response.dtype != dtype or v_response is None or v_response.dtype != dtype or v_response.shape != shape):
+            raise ValueError("k_response and v_response must be alike, [n, Hkv, d] of q's type")
+    if checked and block_of_slot.dtype != torch.int32:
+        raise TypeError("block_of_slot must be int32")
     if out is None:
         out = torch.empty_like(q)
+    elif checked and (out.numel() != Hq * d or out.dtype != dtype):
+        raise ValueError("out must be like q")
     if workspace is None:
         workspace = torch.empty(max(lib.slim_decode_attn_workspace_bytes(ns, n_resp, Hq), 256), dtype=torch.uint8, device=q.device)
     code = getattr(lib, name)(_dev(q, "q"), _dev(gpu_pool, "gpu_pool"), slot_bytes, layer_offset,
@@ -292,7 +302,7 @@ def slim_decode_attn(q: torch.Tensor, gpu_pool: torch.Tensor, block_of_slot: tor
                      workspace: torch.Tensor | None = None) -> torch.Tensor:
     """q[Hq,d] attends to the prompt tokens of the blocks in the slot pool and to the response tokens.
     gpu_pool[n_slots, ...]: per slot K[block,Hkv,d] then V[block,Hkv,d] at byte layer_offset."""
-    return _decode_attn("slim_decode_attn", q, gpu_pool, block_of_slot, block, n_prompt_tokens, n_kv_heads, k_response, v_response, layer_offset,
+    return _decode_attn("slim_decode_attn", False, q, gpu_pool, block_of_slot, block, n_prompt_tokens, n_kv_heads, k_response, v_response, layer_offset,
                         softmax_scale, out, workspace)
 
 
@@ -301,16 +311,7 @@ def slim_decode_attn_kv4(q: torch.Tensor, gpu_pool: torch.Tensor, block_of_slot:
                          layer_offset: int = 0, softmax_scale: float = 0.0, out: torch.Tensor | None = None,
                          workspace: torch.Tensor | None = None) -> torch.Tensor:
     """slim_decode_attn on a pool of blocks in 4 bits (slim_kv4_write)."""
-    dtype = q.dtype
-    if block_of_slot.dtype != torch.int32:
-        raise TypeError("block_of_slot must be int32")
-    if out is not None and (out.numel() != q.numel() or out.dtype != dtype):
-        raise ValueError("out must be like q")
-    if k_response is not None:
-        n, h, d = k_response.shape
-        if v_response is None or h != n_kv_heads or k_response.dtype != dtype or v_response.dtype != dtype or v_response.numel() != n * h * d or d != q.shape[-1]:
-            raise ValueError("k_response and v_response must be alike, [n, Hkv, d] of q's type")
-    return _decode_attn("slim_decode_attn_kv4", q, gpu_pool, block_of_slot, block, n_prompt_tokens, n_kv_heads, k_response, v_response, layer_offset,
+    return _decode_attn("slim_decode_attn_kv4", True, q, gpu_pool, block_of_slot, block, n_prompt_tokens, n_kv_heads, k_response, v_response, layer_offset,
                         softmax_scale, out, workspace)
 
 
