@@ -272,6 +272,8 @@ def _decode_attn(name: str, checked: bool, q, gpu_pool, block_of_slot, block, n_
     Hq, d = q.shape
     dtype = q.dtype
     ns = block_of_slot.numel()
+    if checked and ns > gpu_pool.shape[0]:
+        raise ValueError("block_of_slot names more slots than gpu_pool has")
     slot_bytes = gpu_pool.numel() // gpu_pool.shape[0] * gpu_pool.element_size() if ns else 0
     n_resp = 0
     if k_response is not None:
@@ -310,7 +312,7 @@ def slim_decode_attn_kv4(q: torch.Tensor, gpu_pool: torch.Tensor, block_of_slot:
                          n_kv_heads: int, k_response: torch.Tensor | None = None, v_response: torch.Tensor | None = None,
                          layer_offset: int = 0, softmax_scale: float = 0.0, out: torch.Tensor | None = None,
                          workspace: torch.Tensor | None = None) -> torch.Tensor:
-    """slim_decode_attn on a pool of blocks in 4 bits (slim_kv4_write)."""
+    """slim_decode_attn on a pool of blocks in 4 bits (slim_kv4_write).  block_of_slot has no more entries than gpu_pool slots."""
     return _decode_attn("slim_decode_attn_kv4", True, q, gpu_pool, block_of_slot, block, n_prompt_tokens, n_kv_heads, k_response, v_response, layer_offset,
                         softmax_scale, out, workspace)
 
@@ -359,9 +361,11 @@ def slim_decode_layer(shape: LayerShape, weights: dict, x_new: torch.Tensor, pos
 def slim_decode_layer_kv4(shape: LayerShape, weights: dict, x_new: torch.Tensor, position: int, gpu_pool: torch.Tensor,
                           block_of_slot: torch.Tensor, n_prompt_tokens: int, k_response: torch.Tensor, v_response: torch.Tensor,
                           n_response: int, layer_offset: int = 0, workspace: torch.Tensor | None = None):
-    """slim_decode_layer on a pool of blocks in 4 bits (slim_kv4_write)."""
+    """slim_decode_layer on a pool of blocks in 4 bits (slim_kv4_write).  block_of_slot has no more entries than gpu_pool slots."""
     if block_of_slot.dtype != torch.int32:
         raise TypeError("block_of_slot must be int32")
+    if block_of_slot.numel() > gpu_pool.shape[0]:
+        raise ValueError("block_of_slot names more slots than gpu_pool has")
     if k_response.shape != v_response.shape or not k_response.dtype == v_response.dtype == x_new.dtype or k_response.shape[0] <= n_response:
         raise ValueError("k_response and v_response must be alike, of x_new's type, and hold the token's row")
     return _decode_layer("slim_decode_layer_kv4", shape, weights, x_new, position, gpu_pool, block_of_slot, n_prompt_tokens, k_response, v_response,

@@ -1,0 +1,42 @@
+"""What the binding of the calls on a cache in 4 bits refuses before it looks for a GPU (no GPU: the tensors lie on the host, and every refusal is named)."""
+import pytest
+import torch
+
+BF16, F32 = torch.bfloat16, torch.float32
+
+
+@pytest.fixture(scope="module")
+def slim():
+    import os
+
+    import paper_2508_06447_amd as slim
+    if not os.path.exists(slim.LIB_PATH):
+        from paper_2508_06447_amd.build import build_lib
+        build_lib(verbose=False)
+    return slim
+
+
+def layer(slim, slots=3, in_pool=3, Hq=4, Hkv=2, hidden=256, rows=9, n_response=3, x=None, kr=None, dtype=BF16):
+    """The arguments of slim_decode_layer_kv4 (the weights are looked at last)."""
+    shape = slim.make_shape(hidden, Hq, Hkv, 128, 512, 16, 4, 8, dtype)
+    pool = torch.zeros(in_pool, slim.kv4_block_bytes(16, Hkv, 128), dtype=torch.uint8)
+    kr = torch.zeros(rows, Hkv, 128, dtype=dtype) if kr is None else kr
+    return shape, {}, torch.zeros(hidden, dtype=dtype) if x is None else x, 60, pool, torch.full((slots,), -1, dtype=torch.int32), 48, kr, torch.zeros_like(kr), n_response
+
+
+def test_a_map_of_more_slots_than_the_pool_has_is_refused(slim):
+    """Every entry of the map that is not negative is an address in the pool."""
+    q = torch.zeros(4, 128, dtype=BF16)
+    for in_pool, slots in ((3, 4), (1, 2), (0, 1), (2, 1000)):
+        pool = torch.zeros(in_pool, slim.kv4_block_bytes(16, 2, 128), dtype=torch.uint8)
+        with pytest.raises(ValueError, match="slots"):
+            slim.slim_decode_attn_kv4(q, pool, torch.zeros(slots, dtype=torch.int32), 16, 16 * slots, 2)
+        with pytest.raises(ValueError, match="slots"):
+            slim.slim_decode_layer_kv4(*layer(slim, slots=slots, in_pool=in_pool))
+    # as many, and fewer: refused only for where they lie
+    for slots in (3, 2):
+        pool = torch.zeros(3, slim.kv4_block_bytes(16, 2, 128), dtype=torch.uint8)
+        with pytest.raises(ValueError, match="GPU"):
+            slim.slim_decode_attn_kv4(q, pool, torch.zeros(slots, dtype=torch.int32), 16, 16 * slots, 2)
+        with pytest.raises(ValueError, match="GPU"):
+            slim.slim_decode_layer_kv4(*layer(slim, slots=slots))
