@@ -366,8 +366,11 @@ def slim_decode_layer_kv4(shape: LayerShape, weights: dict, x_new: torch.Tensor,
         raise TypeError("block_of_slot must be int32")
     if block_of_slot.numel() > gpu_pool.shape[0]:
         raise ValueError("block_of_slot names more slots than gpu_pool has")
-    if k_response.shape != v_response.shape or not k_response.dtype == v_response.dtype == x_new.dtype or k_response.shape[0] <= n_response:
-        raise ValueError("k_response and v_response must be alike, of x_new's type, and hold the token's row")
+    if x_new.numel() != shape.hidden or _dtype_code(x_new) != shape.dtype:
+        raise ValueError("x_new must be [hidden] of the layer's type")
+    if k_response.shape != v_response.shape or not k_response.dtype == v_response.dtype == x_new.dtype or \
+            k_response.shape[1:] != (shape.n_kv_heads, shape.head_dim) or k_response.shape[0] <= n_response:
+        raise ValueError("k_response and v_response must be alike, [n, n_kv_heads, head_dim] of x_new's type, and hold the token's row")
     return _decode_layer("slim_decode_layer_kv4", shape, weights, x_new, position, gpu_pool, block_of_slot, n_prompt_tokens, k_response, v_response,
                          n_response, layer_offset, workspace)
 

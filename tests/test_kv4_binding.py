@@ -40,3 +40,20 @@ def test_a_map_of_more_slots_than_the_pool_has_is_refused(slim):
             slim.slim_decode_attn_kv4(q, pool, torch.zeros(slots, dtype=torch.int32), 16, 16 * slots, 2)
         with pytest.raises(ValueError, match="GPU"):
             slim.slim_decode_layer_kv4(*layer(slim, slots=slots))
+
+
+def test_response_rows_and_a_token_that_are_not_the_layers_are_refused(slim):
+    """The layer writes row n_response and reads the others as [n_kv_heads, head_dim], and x_new as `hidden` channels of its own type."""
+    for kr in (torch.zeros(9, 1, 128, dtype=BF16), torch.zeros(9, 2, 64, dtype=BF16), torch.zeros(9, 256, dtype=BF16), torch.zeros(9, 4, 128, dtype=BF16)):
+        with pytest.raises(ValueError, match="response"):
+            slim.slim_decode_layer_kv4(*layer(slim, kr=kr))
+    with pytest.raises(ValueError, match="response"):
+        slim.slim_decode_layer_kv4(*layer(slim, rows=3))                       # no row left for the token
+    for x in (torch.zeros(255, dtype=BF16), torch.zeros(0, dtype=BF16), torch.zeros(2, 256, dtype=BF16)):
+        with pytest.raises(ValueError, match="x_new"):
+            slim.slim_decode_layer_kv4(*layer(slim, x=x))
+    with pytest.raises(ValueError, match="x_new"):                              # tensors of one type, a layer of another
+        slim.slim_decode_layer_kv4(*layer(slim, x=torch.zeros(256, dtype=BF16), kr=torch.zeros(9, 2, 128, dtype=BF16), dtype=F32))
+    for x in (torch.zeros(256, dtype=BF16), torch.zeros(1, 256, dtype=BF16)):
+        with pytest.raises(ValueError, match="GPU"):
+            slim.slim_decode_layer_kv4(*layer(slim, x=x, rows=4))
