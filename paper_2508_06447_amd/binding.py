@@ -426,11 +426,25 @@ def slim_kv4_write(k: torch.Tensor, v: torch.Tensor, pool: torch.Tensor, block: 
     return pool
 
 
+def _kv4_rows(n_tokens: int, block: int, blocks: torch.Tensor | None) -> int:
+    """Rows of the listed blocks.  Where a list leaves blocks of a prompt with a short last one out, its last entry says whether that one is among them: the GPU is
+    waited for."""
+    n_list, nb = n_blocks(n_tokens, block) if blocks is None else blocks.numel(), n_blocks(n_tokens, block)
+    short = nb * block - n_tokens
+    if short and 0 < n_list < nb:
+        if blocks.is_cuda and torch.cuda.is_current_stream_capturing():
+            raise ValueError("n_out must be given while a graph is captured: the list's last block is not known")
+        if int(blocks[-1]) != nb - 1:
+            short = 0
+    return n_list * block - short
+
+
 def slim_kv4_read(pool: torch.Tensor, block: int, n_tokens: int, slot_of_block: torch.Tensor | None = None, blocks: torch.Tensor | None = None,
                   k_out: torch.Tensor | None = None, v_out: torch.Tensor | None = None, n_kv_heads: int = 0, head_dim: int = 0,
-                  dtype: torch.dtype = torch.bfloat16, layer_offset: int = 0):
-    """Rows of the blocks listed in `blocks` (int32, ascending; None: all) of a prompt of n_tokens -> (k, v)[n', Hkv, d]; n' assumes the prompt's
-    last block among them, as slim_compact_tokens does.  Give k_out and v_out, whose first n' rows are filled, or n_kv_heads, head_dim and dtype."""
+                  dtype: torch.dtype = torch.bfloat16, layer_offset: int = 0, n_out: int | None = None):
+    """Rows of the blocks listed in `blocks` (int32, ascending; None: all) of a prompt of n_tokens -> (k, v)[n', Hkv, d].  Give n_kv_heads, head_dim and dtype,
+    and n_out = n' where it is known (None: _kv4_rows counts, which may wait for the GPU), or k_out and v_out: they hold at least the rows of as many blocks
+    with the prompt's last one among them, and rows that they have no room for are dropped."""
     lib = load_library()
     nb = n_blocks(n_tokens, block)
     if slot_of_block is not None and slot_of_block.numel() < nb:
@@ -438,7 +452,12 @@ def slim_kv4_read(pool: torch.Tensor, block: int, n_tokens: int, slot_of_block: 
     if (k_out is None) != (v_out is None):
         raise ValueError("k_out and v_out go together")
     n_list = 0 if blocks is None else blocks.numel()
-    rows = n_tokens if blocks is None else n_tokens - (nb - n_list) * block
+    if n_out is not None:
+        rows = n_out
+    elif k_out is None:
+        rows = _kv4_rows(n_tokens, block, blocks)
+    else:
+        rows = n_tokens if blocks is None else n_tokens - (nb - n_list) * block
     if k_out is None:
         k_out = torch.empty(max(rows, 0), n_kv_heads, head_dim, dtype=dtype, device=pool.device if pool.is_cuda else torch.cuda.current_device())
         v_out = torch.empty_like(k_out)

@@ -57,3 +57,15 @@ def test_response_rows_and_a_token_that_are_not_the_layers_are_refused(slim):
     for x in (torch.zeros(256, dtype=BF16), torch.zeros(1, 256, dtype=BF16)):
         with pytest.raises(ValueError, match="GPU"):
             slim.slim_decode_layer_kv4(*layer(slim, x=x, rows=4))
+
+
+def test_rows_of_a_list_of_blocks(slim):
+    """Only the prompt's last block can be short, and only a list that ends with it has its rows."""
+    from paper_2508_06447_amd.binding import _kv4_rows
+    for n, block in ((74, 64), (65, 64), (64, 64), (128, 64), (1, 16), (205, 32)):
+        nb = -(-n // block)
+        assert _kv4_rows(n, block, None) == n
+        for some in ([0], [nb - 1], list(range(nb)), list(range(nb - 1)), list(range(1, nb))):
+            if some:
+                want = sum(min(block, n - b * block) for b in some)
+                assert _kv4_rows(n, block, torch.tensor(some, dtype=torch.int32)) == want, (n, block, some)
