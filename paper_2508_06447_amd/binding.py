@@ -452,6 +452,8 @@ def slim_kv4_read(pool: torch.Tensor, block: int, n_tokens: int, slot_of_block: 
     if (k_out is None) != (v_out is None):
         raise ValueError("k_out and v_out go together")
     n_list = 0 if blocks is None else blocks.numel()
+    if blocks is not None and n_list == 0:
+        raise ValueError("blocks is empty")              # (an empty tensor has no address, which would stand for every block)
     if n_out is not None:
         rows = n_out
     elif k_out is None:

@@ -69,3 +69,12 @@ def test_rows_of_a_list_of_blocks(slim):
             if some:
                 want = sum(min(block, n - b * block) for b in some)
                 assert _kv4_rows(n, block, torch.tensor(some, dtype=torch.int32)) == want, (n, block, some)
+
+
+def test_an_empty_list_of_blocks_is_refused(slim):
+    """An empty tensor has no address, and without a list every block is read."""
+    pool, rows = torch.zeros(3, slim.kv4_block_bytes(16, 2, 128), dtype=torch.uint8), torch.zeros(48, 2, 128, dtype=BF16)
+    none = torch.zeros(0, dtype=torch.int32)
+    for more in (dict(k_out=rows, v_out=rows), dict(n_kv_heads=2, head_dim=128), dict(n_kv_heads=2, head_dim=128, n_out=48)):
+        with pytest.raises(ValueError, match="blocks"):
+            slim.slim_kv4_read(pool, 16, 48, blocks=none, **more)
