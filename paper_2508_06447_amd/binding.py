@@ -444,7 +444,7 @@ def slim_kv4_read(pool: torch.Tensor, block: int, n_tokens: int, slot_of_block: 
                   dtype: torch.dtype = torch.bfloat16, layer_offset: int = 0, n_out: int | None = None):
     """Rows of the blocks listed in `blocks` (int32, ascending; None: all) of a prompt of n_tokens -> (k, v)[n', Hkv, d].  Give n_kv_heads, head_dim and dtype,
     and n_out = n' where it is known (None: _kv4_rows counts, which may wait for the GPU), or k_out and v_out: they hold at least the rows of as many blocks
-    with the prompt's last one among them, and rows that they have no room for are dropped."""
+    with the prompt's last one among them, and rows that they have no room for are dropped.  Rows of a block that no slot has: zero, or as k_out and v_out had them."""
     lib = load_library()
     nb = n_blocks(n_tokens, block)
     if slot_of_block is not None and slot_of_block.numel() < nb:
@@ -461,8 +461,10 @@ def slim_kv4_read(pool: torch.Tensor, block: int, n_tokens: int, slot_of_block: 
     else:
         rows = n_tokens if blocks is None else n_tokens - (nb - n_list) * block
     if k_out is None:
-        k_out = torch.empty(max(rows, 0), n_kv_heads, head_dim, dtype=dtype, device=pool.device if pool.is_cuda else torch.cuda.current_device())
-        v_out = torch.empty_like(k_out)
+        # rows that no slot has are zero; there are none where every block of the prompt lies in the slot of its number
+        whole = blocks is None and slot_of_block is None and pool.shape[0] >= nb and rows <= n_tokens
+        k_out, v_out = ((torch.empty if whole else torch.zeros)(max(rows, 0), n_kv_heads, head_dim, dtype=dtype,
+                                                                device=pool.device if pool.is_cuda else torch.cuda.current_device()) for _ in range(2))
     n_rows, Hkv, d, kp, vp, ldk, ldv = _rows(k_out, v_out, "k_out and v_out")
     if n_rows < rows:
         raise ValueError("k_out and v_out must hold the rows")

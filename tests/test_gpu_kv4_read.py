@@ -54,3 +54,29 @@ def test_captured_with_the_rows_given(slim):
         rows = np.concatenate([np.arange(b * block, (b + 1) * block) for b in (lo, hi)])
         same(kr, k[rows])
         same(vr, v[rows])
+
+
+@pytest.mark.parametrize("dtype", [BF16, F32])
+def test_rows_that_no_slot_has_are_zero(slim, dtype):
+    """Blocks without a slot, blocks that the prompt does not have, and rows behind the listed blocks: in outputs that the call allocates."""
+    n, H, d, block = 200, 2, 128, 16
+    sob = torch.arange(13, dtype=torch.int32).roll(5)
+    sob[[1, 4, 12]] = torch.tensor([-1, 99, -5], dtype=torch.int32)
+    pool, k, v = written(slim, n, H, d, block, dtype, sob.cuda(), 13)
+    for x in (k, v):
+        for b in (1, 4, 12):
+            x[b * block:(b + 1) * block] = 0
+    some = torch.tensor([0, 1, 3, 7, 40], dtype=torch.int32)
+    lists = ((None, None, np.arange(n)), (some, 5 * block, np.r_[0:32, 48:64, 112:128]), (some[:3], 60, np.r_[0:32, 48:64]))
+    for blocks, n_out, rows in lists:
+        for _ in range(3):
+            old = [torch.full((n_out or n, H, d), 7.0, dtype=dtype, device="cuda") for _ in range(4)]         # what the allocator hands out next
+            del old
+            kr, vr = slim.slim_kv4_read(pool, block, n, sob.cuda(), blocks if blocks is None else blocks.cuda(), n_kv_heads=H, head_dim=d, dtype=dtype, n_out=n_out)
+            for got, x in ((kr, k), (vr, v)):
+                want = np.zeros((n_out or n, H, d))
+                want[:len(rows)] = x[rows]
+                same(got, want)
+    # a pool that holds the first blocks only, without a map
+    kr, vr = slim.slim_kv4_read(pool[:5], block, n, n_kv_heads=H, head_dim=d, dtype=dtype)
+    assert kr[:5 * block].any() and not kr[5 * block:].any() and not vr[5 * block:].any()
