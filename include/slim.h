@@ -163,6 +163,9 @@ int slim_prefill_attn(const void* q, const void* k, const void* v, int n, int n_
  *   q, out [n_q, Hq, d]   k, v [n_k, Hkv, d]   all dtype;  softmax_scale 0 => 1/sqrt(d)
  * Keys and values that a query does not see do not reach its output, whatever they hold (infinities and NaN too); one that sees a key, value or query
  * that is not finite is not specified.
+ * Scores, sums and results are float32 until the output is rounded.  bfloat16: the weights enter the product with the values as two bfloat16 terms, or, where
+ * a call has rows enough for tiles of 256 (a rule on its sizes), as one, as in slim_prefill_attn: 1.7 or 2.3 10^-3 of the results' size from 64 bits, of which the
+ * output's rounding is 1.65.  A token's result can differ by that between a whole prompt and a chunk of it.
  *   workspace   >= slim_sliding_attn_workspace_bytes(...) bytes, 256-byte aligned: partial results of few queries; NULL where that is 0.
  * Errors: INVALID_ARG (null, n_q < 1, n_k < n_q, Hq % Hkv, window < 1, n_sinks < 0, scale < 0 or NaN), UNSUPPORTED (bf16: d != 128; f32: d other than 32,
  * 64, 128; alignment of 16 bytes; n_k above 2^30, n_q * Hq above 2^27), WORKSPACE_TOO_SMALL.

@@ -37,7 +37,7 @@ tile pointers and the key index jump between them, or within the first tile.  Th
 rows' window edges) and over the last ones; per unit it masks where a key lies above some query of the wave, or behind some
 window and is no first token, and it ends behind the last unit with keys (2 % of a window of 4096 with four heads a kv head).  The first unit may be masked for a whole row, so the reference starts at the larger of that
 unit's maximum and the query's product with its own token, which comes as an operand.  Query fragments stay as they are and
-S is scaled in float on its way into the exponential (a scaled Query rounded to bf16 again is off by 2^-9 per channel: the
+S is scaled in float on its way into the exponential (a scaled Query rounded to bf16 again is off by up to 2^-8 per channel: the
 largest error of the whole); the reference is in units of unscaled products, and moves only for a sum above 2^60: weights, their
 sums and O are floats, whose relative error does not depend on where the reference lies (with queries that each meet one key 12
 bits above the others, half of the units moved it at 2^8).  The epilogue leaves the rows in LDS, in

@@ -8,8 +8,9 @@
 // The wave's V tile is its own: rows of D bfloat16, 16-byte piece c of key r at c ^ (r % (D / 8)), which spreads both the writes (16 keys, one piece) and the
 // transposing reads (16 keys, two pieces) over all banks.  LDS serves a wave's accesses in order, so no barrier is needed.
 //
-// float32 rows run in the same instructions: a float is the sum of three bfloat16 (its 24 bits, cut into three times eight), products of the terms are exact, and of the nine
-// those below 2^-24 of the largest are left out (terms a and b with a + b > 2).  What comes from 4 bits is a single bfloat16, exactly.
+// float32 rows run in the same instructions: a float is the sum of three bfloat16 (its 24 bits, cut into three times eight: the second is below 2^-7 of the float, the third below 2^-15),
+// products of the terms are exact, and of the nine the three with a + b > 2 are left out: 2^-22 of the floats' product twice and 2^-30, in the worst case 2^-21 together, all with the
+// product's own sign (random floats: 2^-21.3 at most; results 2 to 4 10^-7 from 64 bits).  What comes from 4 bits is a single bfloat16, exactly.
 #pragma once
 #include "slim_common.h"
 
@@ -33,7 +34,7 @@ __device__ __forceinline__ float max_over_rows(float v) {
     return fmaxf(__builtin_bit_cast(float, b0), __builtin_bit_cast(float, b1));
 }
 
-// Eight floats as bfloat16 terms: one, rounded to nearest; it and what is left, rounded to nearest (2^-18 of the float may be missing); or three that add up to the float.
+// Eight floats as bfloat16 terms: one, rounded to nearest; it and what is left, rounded to nearest (2^-17 of the float may be missing); or three that add up to the float.
 template <int NT> __device__ __forceinline__ void bf16_terms(const float* f, bf16x8* t) {
     if constexpr (NT <= 2) {
         const uint4 w = Elem<bf16_t>::pack(f);
@@ -82,7 +83,7 @@ template <typename T, int NT> __device__ __forceinline__ void row_terms(const T*
 
 template <typename T, int D> struct RowTile {
     static constexpr int NT = sizeof(T) == 2 ? 1 : 3;    // terms of an operand that is a T
-    static constexpr int NP = sizeof(T) == 2 ? 2 : 3;    // and of the weights: one term alone, rounded by 2^-9, would be off as much as the bfloat16 output's own rounding
+    static constexpr int NP = sizeof(T) == 2 ? 2 : 3;    // and of the weights: one term alone, rounded by up to 2^-8, would be off as much as the bfloat16 output's own rounding
     static constexpr int KS = D / 32, DT = D / 16, CH = D / 8;
     static constexpr int kLdsBytes = kTileKeys * D * 2;  // of a wave's V tile
     bf16x8 q[NT][KS];
