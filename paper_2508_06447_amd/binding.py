@@ -272,7 +272,7 @@ def _decode_attn(name: str, checked: bool, q, gpu_pool, block_of_slot, block, n_
     Hq, d = q.shape
     dtype = q.dtype
     ns = block_of_slot.numel()
-    if checked and ns > gpu_pool.shape[0]:
+    if checked and ns and ns > gpu_pool.shape[0]:
         raise ValueError("block_of_slot names more slots than gpu_pool has")
     slot_bytes = gpu_pool.numel() // gpu_pool.shape[0] * gpu_pool.element_size() if ns else 0
     n_resp = 0
@@ -364,7 +364,8 @@ def slim_decode_layer_kv4(shape: LayerShape, weights: dict, x_new: torch.Tensor,
     """slim_decode_layer on a pool of blocks in 4 bits (slim_kv4_write).  block_of_slot has no more entries than gpu_pool slots."""
     if block_of_slot.dtype != torch.int32:
         raise TypeError("block_of_slot must be int32")
-    if block_of_slot.numel() > gpu_pool.shape[0]:
+    ns = block_of_slot.numel()
+    if ns and ns > gpu_pool.shape[0]:
         raise ValueError("block_of_slot names more slots than gpu_pool has")
     if x_new.numel() != shape.hidden or _dtype_code(x_new) != shape.dtype:
         raise ValueError("x_new must be [hidden] of the layer's type")

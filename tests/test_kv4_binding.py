@@ -78,3 +78,14 @@ def test_an_empty_list_of_blocks_is_refused(slim):
     for more in (dict(k_out=rows, v_out=rows), dict(n_kv_heads=2, head_dim=128), dict(n_kv_heads=2, head_dim=128, n_out=48)):
         with pytest.raises(ValueError, match="blocks"):
             slim.slim_kv4_read(pool, 16, 48, blocks=none, **more)
+
+
+def test_without_slots_there_need_be_no_pool(slim):
+    """A token that attends to response rows alone."""
+    none, q, r = torch.zeros(0, dtype=torch.int32), torch.zeros(4, 128, dtype=BF16), torch.zeros(5, 2, 128, dtype=BF16)
+    with pytest.raises(ValueError, match="q must be a GPU tensor"):
+        slim.slim_decode_attn_kv4(q, None, none, 16, 16, 2, r, r)
+    args = list(layer(slim))
+    args[4], args[5] = None, none
+    with pytest.raises(ValueError, match="x_new must be a GPU tensor"):
+        slim.slim_decode_layer_kv4(*args)
