@@ -89,3 +89,13 @@ def test_without_slots_there_need_be_no_pool(slim):
     args[4], args[5] = None, none
     with pytest.raises(ValueError, match="x_new must be a GPU tensor"):
         slim.slim_decode_layer_kv4(*args)
+
+
+def test_rows_too_far_apart_for_the_entry_points_are_refused():
+    """The distance of the rows is an int there: one of 2^32 elements and a row would be taken for a row."""
+    from paper_2508_06447_amd.binding import _row_stride
+    rows = lambda apart: torch.empty_strided((2, 8, 128), (apart, 128, 1), dtype=BF16, device="meta")
+    assert _row_stride(rows(2**31 - 8), "k") == 2**31 - 8
+    for apart in (2**31, 2**32 + 1024, 2**33 + 2048):
+        with pytest.raises(ValueError, match="apart"):
+            _row_stride(rows(apart), "k")
