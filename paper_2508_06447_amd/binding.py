@@ -387,7 +387,7 @@ def _row_stride(t: torch.Tensor, name: str) -> int:
     s0, s1, s2 = t.stride()
     if (d > 1 and s2 != 1) or (H > 1 and s1 != d):
         raise ValueError(f"{name} must have dense rows")
-    if s0 >= 1 << 31:
+    if n > 1 and s0 >= 1 << 31:
         raise ValueError(f"{name} must have rows less than 2^31 elements apart")
     return s0 if n > 1 else H * d
 

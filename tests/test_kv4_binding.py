@@ -99,3 +99,4 @@ def test_rows_too_far_apart_for_the_entry_points_are_refused():
     for apart in (2**31, 2**32 + 1024, 2**33 + 2048):
         with pytest.raises(ValueError, match="apart"):
             _row_stride(rows(apart), "k")
+    assert _row_stride(rows(2**33)[:1], "k") == 1024                            # (one row is nowhere apart)
