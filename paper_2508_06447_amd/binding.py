@@ -676,8 +676,14 @@ def slim_prefill_attn(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, softmax
     return out
 
 
+def _within_keys(n: int, n_k: int) -> int:
+    """A window or a number of first tokens as the entry points take it, in 32 bits: what is beyond the keys is all of them, what is negative stays so."""
+    return -1 if n < 0 else n if n < n_k else n_k
+
+
 def sliding_attn_workspace_bytes(n_q: int, n_k: int, n_q_heads: int, n_kv_heads: int, head_dim: int, window: int, n_sinks: int,
                                  dtype: torch.dtype) -> int:
+    window, n_sinks = _within_keys(window, n_k), _within_keys(n_sinks, n_k)
     return load_library().slim_sliding_attn_workspace_bytes(n_q, n_k, n_q_heads, n_kv_heads, head_dim, window, n_sinks, BF16 if dtype == torch.bfloat16 else F32)
 
 
@@ -691,6 +697,8 @@ def slim_sliding_attn(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, window:
     n_k, Hkv, k_d = k_shape
     if v.shape != k_shape or k_d != d or k.dtype != dtype or v.dtype != dtype:
         raise ValueError("q, k and v do not match")
+    if not (0 <= window <= n_k and 0 <= n_sinks <= n_k):
+        window, n_sinks = _within_keys(window, n_k), _within_keys(n_sinks, n_k)
     if out is None:
         out = torch.empty_like(q)
     elif out.shape != q_shape or out.dtype != dtype:

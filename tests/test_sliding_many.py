@@ -220,3 +220,20 @@ def test_two_calls_at_once(slim):
                 call(slim, st)
         torch.cuda.synchronize()
         assert all(torch.equal(st[3], x) for st, x in zip(state, alone))
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("n_q,n_k,Hq,Hkv,dtype", [(1, 3000, 32, 8, BF16), (900, 900, 8, 2, BF16), (40, 300, 4, 2, F32)])
+def test_windows_and_first_tokens_beyond_32_bits(slim, n_q, n_k, Hq, Hkv, dtype):
+    """Beyond the keys, all of them are meant: however far beyond."""
+    import sys
+    q, k, v = (x.cuda() for x in inputs_of(n_q, n_k, Hq, Hkv, 128, dtype, 4))
+    whole = slim.slim_sliding_attn(q, k, v, n_k)
+    size = slim.sliding_attn_workspace_bytes(n_q, n_k, Hq, Hkv, 128, n_k, 0, dtype)
+    for far in (2**31, 2**32 + 3, 2**32, 2**40 + 1, sys.maxsize):
+        assert torch.equal(slim.slim_sliding_attn(q, k, v, far), whole)
+        assert slim.sliding_attn_workspace_bytes(n_q, n_k, Hq, Hkv, 128, far, 0, dtype) == size
+        assert torch.equal(slim.slim_sliding_attn(q, k, v, 5, far), slim.slim_sliding_attn(q, k, v, 5, n_k))
+    for none in (0, -1, -2**32 + 3, -sys.maxsize):
+        with pytest.raises(slim.SlimError):
+            slim.slim_sliding_attn(q, k, v, none)
