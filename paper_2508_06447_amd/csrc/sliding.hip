@@ -193,8 +193,8 @@ __global__ void __launch_bounds__(64 * kSlideWaves) sliding_rows_kernel(const T*
 // leaves any behind, then the stretch; up to 96 first tokens share a tile with its beginning (with a tile of their own 32768 tokens, window 1024 637 us instead of 596,
 // window 4096 1775 instead of 1748).  Where the two would meet the stretch begins at key 0 instead.
 // Bound by the matrix instructions and what stands between them in the loop, 2.8 us for a tile of 128 keys on every CU (1.5 PFLOP/s), and by what a workgroup does beside its tiles,
-// about 10 us with its CU to itself (first loads 5, softmax reference and edges 2, results 3): 32768 tokens of 32 / 8 heads, window 4096, 1.70 ms (1.21 PFLOP/s), window 1024 0.59 ms
-// (0.92), window 256 0.30 ms (0.46).
+// about 10 us with its CU to itself (first loads 5, softmax reference and edges 2, results 3): 32768 tokens of 32 / 8 heads, window 4096, 1.65 to 1.77 ms (1.18 to 1.26 PFLOP/s, by inputs and cards), window 1024
+// 0.59 ms (0.92), window 256 0.30 ms (0.46).
 constexpr int LD = 128, LW = 4, LKV = kSlideTile, LTILE_BYTES = LKV * LD * 2, LSTAGE_BYTES = 2 * LTILE_BYTES, LSTAGES = 2, LROWS = 64 * LW;
 constexpr int kPartRow = LD + 4;         // floats of a row's partial result (16-byte aligned)
 
@@ -204,8 +204,10 @@ sliding_many_kernel(const bf16_t* __restrict__ Q, const bf16_t* __restrict__ Kg,
     extern __shared__ __align__(16) unsigned char lds[];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), l32 = lane & 31, hh = lane >> 5;
     // Workgroup -> (kv head, row tile, part of its keys): each XCD its own kv heads, whose keys then meet in one L2.  Long tiles of a prompt start with the last row, which has the most
-    // keys, so that short ones fill the end (32768 tokens, window 4096 1843 us against 1870 from the first row on; the whole prompt 6992 / 7660); tiles of fewer than 2048 keys with the
-    // first, so that the workgroups do not start and end together (window 1024 691 / 674; 8192 tokens, window 512 121 / 111, 1024 171 / 159, 2048 264 / 251, with 64 heads 487 / 492).
+    // keys, so that short ones fill the end; tiles of fewer than 2048 keys with the first, so that the workgroups do not start and end together.  us from the last row on / from the first,
+    // 32 / 8 heads: 32768 tokens, window 4096 1654 / 1682, 2048 962 / 975, 1024 586 / 598, 256 307 / 300; 8192 tokens, all in sight 434 / 489, window 4096 341 / 365, 2048 232 / 226,
+    // 1024 143 / 139, 512 97 / 94; with 64 heads, 2048 430 / 441 and 1024 277 / 271; 28 / 4, 2048 199 / 204.  (Around the line it goes by the rounds of workgroups too: 1 to 3 % of the
+    // slower side are taken where those are few or the windows long.)
     int rt;
     const int g = own_kv_head(a.Hkv, rt);
     const int split = rt % splits;

@@ -74,7 +74,7 @@ inline long long sliding_keys(int n_q, int n_k, int G, int window, int rows) {
 }
 
 // Tiles of 16 rows: 32-key units of a tile.  A wave's unit is 16 KB of keys and values, and what bounds these tiles is how fast the CUs take them: 1.8 ns a unit over the whole
-// chip, whatever the number of rows in it (64 queries 38 us, 17024 units; 1024 queries with a window of 300 51 us, 22528; 16 queries over 32768 keys 65 us, 32768).
+// chip, whatever the number of rows in it (64 queries 38 us, 17024 units; 512 232 us, 136192; 16 queries over 32768 keys 65 to 73 us, 32768).
 inline long long sliding_units_of_tile(int n_q, int n_k, int G, int window, int sinks) {
     const long long near = sliding_keys(n_q, n_k, G, window, 16);
     return (near + 31) / 32 + (near < n_k ? (sinks + 31) / 32 : 0);
@@ -93,17 +93,18 @@ inline int sliding_splits(int n_q, int n_k, int G, int Hkv, int window, int sink
 }
 
 // Tiles of 256 rows: one CU holds one workgroup, 256 of them run at once; a workgroup takes 12 us and 2.8 us a tile of 128 keys; parts are written and read once more, 528 bytes a
-// row, in a launch of 5 us.  64 queries in 1 / 2 / 4 / 8 / 16 parts 94 / 57 / 40 / 35 / 39, 512 96 / 65 / 53 / 71 / 107, 2048 128 / 159; 1511 queries of 28 / 4 heads behind 9856 tokens,
-// all in sight, in 1 / 2 / 3 / 4 / 6 237 / 272 / 225 / 248 / 255.
+// row, in a launch of 5 us.  64 queries in 1 / 2 / 4 / 8 / 16 parts 91 / 58 / 40 / 35 / 39, 512 92 / 64 / 50 / 70 / 107, 2048 119 / 145; 1511 queries of 28 / 4 heads behind 9856 tokens,
+// all in sight, in 1 / 2 / 3 / 4 / 6 237 / 256 / 209 / 230 / 241.  (The 12 us are those of an earlier state of the kernel, now about 10.)
 inline double sliding_many_us(int n_q, int n_k, int G, int Hkv, int window, int sinks, int parts) {
     const long long rows = (long long)n_q * G * Hkv, row_tiles = ((long long)n_q * G + 255) / 256 * Hkv, near = sliding_keys(n_q, n_k, G, window, 256);
     const long long tiles = (near + (near < n_k ? (sinks + 31ll) / 32 * 32 : 0) + kSlideTile - 1) / kSlideTile, rounds = (row_tiles * parts + 255) / 256;
     return rounds * (12.0 + 2.8 * ((tiles + parts - 1) / parts)) + (parts > 1 ? 5.0 + rows * parts * 528.0 * 2 / 4.5e6 : 0.0);
 }
-// In how many parts a call's tiles of 256 rows run; 0: it runs in tiles of 16 rows (6 us, and over the whole chip 6 ns a tile and 1.8 ns a unit; 16 queries 17.7 us, in tiles of 256
-// 29; 32 24.6 / 33; 48 37.9 / 36.4; 64 of 28 / 4 heads with a window of 500 13.8 / 22.4; 16 over 32768 keys 65 / 58; windows of 16, where a tile is one unit and its other waves have
-// nothing: 1024 25.5 / 18.2, 4096 93 / 41, 32768 740 / 290).  Over 121 calls of 16 to 32768 queries, five head layouts and windows of 1 to 1024 the faster one was chosen but where
-// the two are within 1 %.
+// In how many parts a call's tiles of 256 rows run; 0: it runs in tiles of 16 rows (6 us, and over the whole chip 6 ns a tile and 1.8 ns a unit; 16 queries 17.8 us, in tiles of 256
+// 30; 32 24.5 / 31.5; 48 38 / 34; 64 of 28 / 4 heads with a window of 500 13.4 / 21; 16 over 32768 keys 73 / 65; windows of 16, where a tile is one unit and its other waves have
+// nothing: 1024 26 / 13, 4096 92 / 30, 32768 742 / 237).  Of 26 calls of 1 to 32768 queries, six head layouts and windows of 16 to 32768, each measured both ways and
+// in several numbers of parts, the faster tiles are chosen in all; a number of parts that is more than 2 % slower than another in three (48 queries 37 us in 17 parts, 34 in eight; 200 behind
+// 2000 tokens, window 1024, 64 / 8 heads 35 in three, 32 in one; 28 / 4 29.5 in five, 28 in four).
 inline int sliding_parts(int n_q, int n_k, int G, int Hkv, int window, int sinks) {
     int best = 1;
     double us = sliding_many_us(n_q, n_k, G, Hkv, window, sinks, 1);
