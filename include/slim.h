@@ -473,6 +473,60 @@ int slim_decode_layer_kv4(const slim_layer_shape* s, const slim_layer_weights* w
                           void* k_response, void* v_response, int n_response, void* x_out, void* q_out, void* workspace,
                           size_t workspace_bytes, void* stream);
 
+/* ------------------------------------------------------------------------------------------------
+ * A batch of requests over one pool of Key-Value blocks in 8 bits: the tables of a step from the requests' lengths, its rows written into the pool, attention of each
+ * request's last tokens over its blocks where they lie, and a request's rows read back.  Lengths and tables stay on the GPU: no call waits for the host, and all
+ * of them may be captured into a graph.
+ *   A step: request r holds lens[r] tokens and adds n_new[r] (0: it rests).  The added tokens of all requests, request by request, are the rows of the step, [n_rows, ...]; rows
+ *   behind the last request's are padding.  Block b of a request's tokens (b = position / block) lies in slot block_table[r, b] (int32 [n_requests, max_blocks]); an entry outside
+ *   [0, n_slots) is a block that is nowhere in the pool (dropped, or swapped out by slim_kv_swap): not written, and not attended to.
+ *
+ *   slim_batch_map:  the tables of a step.  All arrays int32 on the device; no array that is written may overlap another one (INVALID_ARG).
+ *     lens, n_new [R]            block_table [R, max_blocks] in/out: entries of the new blocks, ceil(lens / block) .. ceil((lens + n_new) / block) - 1, are set, others stay
+ *     free_slots [n_free], used  the new blocks take free_slots[*used], free_slots[*used + 1], .. request by request (used: one number on the device; NULL: 0)
+ *     lens_out [R]               lens + n_new
+ *     row_start [R + 1]          first row of each request; row_start[R]: rows in all
+ *     row_pos [n_rows]           position of each row's token, e.g. for slim_rope; padding: 0
+ *     row_slot [n_rows]          its place in the pool, slot * block + row of the block; -1: padding, or a block that is not in the pool
+ *     info [4]                   {rows in all, slots taken, error bits, *used + slots taken: the next step's used}
+ *   Error bits: 1 = a length or a number of tokens below 0, or more tokens than a table row has room for; 2 = more rows than n_rows; 4 = too few free slots.  With a non-zero error
+ *   the step is one without rows: row_start 0, lens_out = lens, row_slot -1, row_pos 0, info {0, 0, bits, *used}, and the table stays as it was.
+ *   Errors: INVALID_ARG, UNSUPPORTED (R > 4096, max_blocks * block > 2^30, n_slots * block >= 2^31, block > 2^24, n_rows >= 2^29).
+ *
+ *   A slot at byte slot * slot_bytes of its pool, at layer_offset, for blocks of `block` tokens (B) and Hkv heads of d: the Keys' codes [Hkv, B, d], a byte a channel, the Values',
+ *   and for each head the bytes e + 127 of its Keys and of its Values [Hkv, 2].  A code is an e4m3 number: sign, four bits of exponent (bias 7), three of mantissa, largest 448,
+ *   127 not a number; it stands for that number times 2^e, exact in bfloat16 and float32.  e is the smallest in [-117, 119] for which no finite magnitude of the block's
+ *   rows in that head is above 448 * 2^e; codes are rounded to nearest, ties to even, 448 for what is above; an infinity or a NaN reads back as NaN, and only itself.
+ *   slim_kv8_block_bytes gives a slot's size, a multiple of 16 (0: sizes that are not covered).
+ *   slim_kv8_write:  rows k + t * ldk, v + t * ldv ([Hkv, d] of dtype, ld in elements) go to the places row_slot[t] (int32 [n_rows], device; one outside the pool: the row is left out).
+ *     The rows of a block must follow each other, in its order, without a gap, and no other rows of the call may be in it.  Rows that begin a block begin its exponents anew.  Rows
+ *     that join one keep the larger of its exponent and their own; where it grows, the codes in front of them are rounded again.  What the block holds behind the last row written
+ *     is of no token any longer.
+ *     pool: device memory, or pinned device-mapped host memory.
+ *   slim_kv8_read:  the n_tokens tokens of the blocks in slots[ceil(n_tokens / block)] (int32, device, e.g. a row of block_table; NULL: block b in slot b) -> rows k_out, v_out
+ *     [n_tokens, Hkv, d] of dtype with strides ldk, ldv.  Rows of a block that is not in the pool stay as they were.
+ *   slim_batch_attn_kv8:  lens counts the step's rows in (lens_out).  Query i of request r is the token at p = lens[r] - n + i (n rows of the step) and sees the request's tokens j <= p whose
+ *     block is in the pool:  out[t, h, :] = sum_j softmax_j(scale * q[t, h, :] . k[j, g, :]) v[j, g, :],  g = h / (Hq/Hkv);  softmax_scale 0 => 1/sqrt(d).
+ *     q, out rows [n_rows, Hq, d] of dtype with strides ldq, ldo; padding rows of out stay as they were.  A query that sees no key gets zeros.  What a query does not see does not
+ *     reach its output, whatever it holds.  Any number of queries per request, requests of one token among ones of many, any number of query heads per kv head.
+ *     Scores, sums and results are float32 until the output is rounded; the weights enter the product with the values as two bfloat16 terms (float32: three).
+ *     workspace >= slim_batch_attn_kv8_workspace_bytes(...) bytes, 256-byte aligned: partial results; a call writes what it reads of it.
+ * head_dim 64 or 128; pools, layer_offset and slot_bytes multiples of 16, rows 16-byte aligned (ld a multiple of 8 bf16 or 4 f32 elements), n_slots * block < 2^31, block <= 2^24, rows of a
+ * call fewer than 2^29 (attention: n_rows * Hq <= 2^26, R <= 4096, R * Hkv <= 2^22, max_blocks * block <= 2^30).  row_start must ascend within [0, n_rows], as slim_batch_map leaves it.
+ * Errors: INVALID_ARG (null, sizes, Hq % Hkv, ld too small, a slot too small, scale < 0 or NaN), UNSUPPORTED, WORKSPACE_TOO_SMALL.
+ */
+int slim_batch_map(const int* lens, const int* n_new, int n_requests, int block, int* block_table, int max_blocks, const int* free_slots, int n_free, const int* used,
+                   int n_slots, int n_rows, int* lens_out, int* row_start, int* row_pos, int* row_slot, int* info, void* stream);
+size_t slim_kv8_block_bytes(int block, int n_kv_heads, int head_dim);
+int slim_kv8_write(const void* k, const void* v, int ldk, int ldv, const int* row_slot, int n_rows, int n_kv_heads, int head_dim, int block, int dtype, void* pool, int n_slots,
+                   size_t slot_bytes, size_t layer_offset, void* stream);
+int slim_kv8_read(const void* pool, int n_slots, size_t slot_bytes, size_t layer_offset, const int* slots, int n_tokens, int n_kv_heads, int head_dim, int block, int dtype,
+                  void* k_out, void* v_out, int ldk, int ldv, void* stream);
+size_t slim_batch_attn_kv8_workspace_bytes(int n_rows, int n_requests, int n_q_heads, int n_kv_heads, int head_dim);
+int slim_batch_attn_kv8(const void* q, int ldq, const int* row_start, const int* lens, const int* block_table, int n_requests, int n_rows, int max_blocks, const void* pool,
+                        int n_slots, size_t slot_bytes, size_t layer_offset, int block, int n_q_heads, int n_kv_heads, int head_dim, float softmax_scale, int dtype, void* out,
+                        int ldo, void* workspace, size_t workspace_bytes, void* stream);
+
 #ifdef __cplusplus
 }
 #endif

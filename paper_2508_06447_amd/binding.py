@@ -28,6 +28,7 @@ EXPORTS = (
     "slim_kv_swap_workspace_bytes", "slim_kv_swap", "slim_decode_attn_workspace_bytes", "slim_decode_attn", "slim_gemv", "slim_decode_layer_workspace_bytes",
     "slim_decode_layer", "slim_kv4_block_bytes", "slim_kv4_write", "slim_kv4_read", "slim_decode_attn_kv4", "slim_decode_layer_kv4",
     "slim_sliding_attn_workspace_bytes", "slim_sliding_attn",
+    "slim_batch_map", "slim_kv8_block_bytes", "slim_kv8_write", "slim_kv8_read", "slim_batch_attn_kv8_workspace_bytes", "slim_batch_attn_kv8",
     "slim_rope_table", "slim_window_query", "slim_window_query_from_rows_workspace_bytes", "slim_window_query_from_rows",
     "slim_linear_rope", "slim_score_blocks_from_token_scores",
     "slim_linear_pair", "slim_row_rstd", "slim_rmsnorm_linear", "slim_rmsnorm_swiglu_linear", "slim_fold_gain",
@@ -101,6 +102,14 @@ def load_library(path: str | None = None) -> C.CDLL:
     lib.slim_sliding_attn_workspace_bytes.restype = sz
     lib.slim_sliding_attn_workspace_bytes.argtypes = [i] * 8
     lib.slim_sliding_attn.argtypes = [vp, vp, vp, i, i, i, i, i, i, i, f, i, vp, vp, sz, vp]
+    lib.slim_batch_map.argtypes = [vp, vp, i, i, vp, i, vp, i, vp, i, i, vp, vp, vp, vp, vp, vp]
+    lib.slim_kv8_block_bytes.restype = sz
+    lib.slim_kv8_block_bytes.argtypes = [i, i, i]
+    lib.slim_kv8_write.argtypes = [vp, vp, i, i, vp, i, i, i, i, i, vp, i, sz, sz, vp]
+    lib.slim_kv8_read.argtypes = [vp, i, sz, sz, vp, i, i, i, i, i, vp, vp, i, i, vp]
+    lib.slim_batch_attn_kv8_workspace_bytes.restype = sz
+    lib.slim_batch_attn_kv8_workspace_bytes.argtypes = [i] * 5
+    lib.slim_batch_attn_kv8.argtypes = [vp, i, vp, vp, vp, i, i, i, vp, i, sz, sz, i, i, i, i, f, i, vp, i, vp, sz, vp]
     lib.slim_rope_table.argtypes = [vp, i, i, f, vp, vp]
     lib.slim_window_query.argtypes = [vp, i, i, i, i, i, vp, vp]
     lib.slim_window_query_from_rows_workspace_bytes.restype = sz
@@ -475,6 +484,116 @@ def slim_kv4_read(pool: torch.Tensor, block: int, n_tokens: int, slot_of_block: 
     _check(lib.slim_kv4_read(at, ns, size, layer_offset, _index(slot_of_block, "slot_of_block"), _index(blocks, "blocks"), n_list, block, n_tokens, Hkv, d,
                              _dtype_code(k_out), kp, vp, n_rows, ldk, ldv, _stream()), "slim_kv4_read")
     return k_out, v_out
+
+
+# ---- a batch of requests, its cache in 8 bits
+def _here(name: str, *tensors):
+    """The tensors are on the current device, whose stream the call goes to."""
+    at = torch.cuda.current_device() if _device is None else _device()
+    for t in tensors:
+        if t is not None and t.is_cuda and t.get_device() != at:
+            raise ValueError(f"{name}: the tensors must be on the current device")
+
+
+def _counts(t: torch.Tensor, size: int, name: str):
+    """Address of an int32 tensor of `size` numbers on the GPU."""
+    if t.numel() != size:
+        raise ValueError(f"{name} must have {size} entries")
+    return _index(t, name)
+
+
+def slim_batch_map(lens: torch.Tensor, n_new: torch.Tensor, block: int, block_table: torch.Tensor, free_slots: torch.Tensor, n_slots: int, n_rows: int,
+                   used: torch.Tensor | None = None, lens_out: torch.Tensor | None = None, row_start: torch.Tensor | None = None,
+                   row_pos: torch.Tensor | None = None, row_slot: torch.Tensor | None = None, info: torch.Tensor | None = None):
+    """Tables of a step of a batch: requests that hold lens[R] tokens add n_new[R] of them, which become the first of n_rows rows.  New blocks take slots of free_slots, from entry
+    used[0] on, and are set in block_table[R, max_blocks], in place; n_slots: of the pool.  All int32 on the GPU.
+    Returns (lens_out[R], row_start[R + 1], row_pos[n_rows], row_slot[n_rows], info[4]); info[3:4] is the next step's `used`."""
+    lib = load_library()
+    R, dev = lens.numel(), lens.device
+    if block_table.dim() != 2 or block_table.shape[0] != R:
+        raise ValueError("block_table must be [requests, blocks]")
+    _here("slim_batch_map", lens, n_new, block_table, free_slots, used, lens_out, row_start, row_pos, row_slot, info)
+    new = lambda t, size: torch.empty(max(size, 0), dtype=torch.int32, device=dev) if t is None else t
+    lens_out, row_start, row_pos, row_slot, info = new(lens_out, R), new(row_start, R + 1), new(row_pos, n_rows), new(row_slot, n_rows), new(info, 4)
+    _check(lib.slim_batch_map(_index(lens, "lens"), _counts(n_new, R, "n_new"), R, block, _index(block_table, "block_table"), block_table.shape[1],
+                              _index(free_slots, "free_slots"), free_slots.numel(), None if used is None else _counts(used, 1, "used"), n_slots, n_rows,
+                              _counts(lens_out, R, "lens_out"), _counts(row_start, R + 1, "row_start"), _counts(row_pos, n_rows, "row_pos"),
+                              _counts(row_slot, n_rows, "row_slot"), _counts(info, 4, "info"), _stream()), "slim_batch_map")
+    return lens_out, row_start, row_pos, row_slot, info
+
+
+def kv8_block_bytes(block: int, n_kv_heads: int, head_dim: int) -> int:
+    """Bytes of a block's Keys and Values in 8 bits (0: sizes that are not covered)."""
+    return load_library().slim_kv8_block_bytes(block, n_kv_heads, head_dim)
+
+
+def slim_kv8_write(k: torch.Tensor, v: torch.Tensor, pool: torch.Tensor, block: int, row_slot: torch.Tensor, layer_offset: int = 0) -> torch.Tensor:
+    """k, v[n, Hkv, d] (rows may be apart) -> the places row_slot[n] (int32; outside the pool: left out) of pool[slots, ...] in 8 bits.  The rows of a block follow each other.
+    pool: on the GPU or pinned host memory.  Returns pool."""
+    lib = load_library()
+    n, Hkv, d, kp, vp, ldk, ldv = _rows(k, v, "k and v")
+    at, ns, size = _slots(pool)
+    _here("slim_kv8_write", k, v, pool, row_slot)
+    _check(lib.slim_kv8_write(kp, vp, ldk, ldv, _counts(row_slot, n, "row_slot"), n, Hkv, d, block, _dtype_code(k), at, ns, size, layer_offset, _stream()), "slim_kv8_write")
+    return pool
+
+
+def slim_kv8_read(pool: torch.Tensor, block: int, n_tokens: int, slots: torch.Tensor | None = None, k_out: torch.Tensor | None = None, v_out: torch.Tensor | None = None,
+                  n_kv_heads: int = 0, head_dim: int = 0, dtype: torch.dtype = torch.bfloat16, layer_offset: int = 0):
+    """The n_tokens tokens of the blocks in slots[>= ceil(n_tokens / block)] (int32, e.g. a row of a block table; None: block b in slot b) -> (k, v)[n_tokens, Hkv, d].
+    Give n_kv_heads, head_dim and dtype, or k_out and v_out.  Rows of a block that is not in the pool: zero, or as k_out and v_out had them."""
+    lib = load_library()
+    if slots is not None and slots.numel() < n_blocks(n_tokens, block):
+        raise ValueError("slots is shorter than the tokens' blocks")
+    if (k_out is None) != (v_out is None):
+        raise ValueError("k_out and v_out go together")
+    if k_out is None:
+        whole = slots is None and pool.shape[0] >= n_blocks(n_tokens, block)
+        k_out, v_out = ((torch.empty if whole else torch.zeros)(max(n_tokens, 0), n_kv_heads, head_dim, dtype=dtype,
+                                                                device=pool.device if pool.is_cuda else torch.cuda.current_device()) for _ in range(2))
+    n, Hkv, d, kp, vp, ldk, ldv = _rows(k_out, v_out, "k_out and v_out")
+    if n < n_tokens:
+        raise ValueError("k_out and v_out must hold the tokens")
+    at, ns, size = _slots(pool)
+    _here("slim_kv8_read", pool, slots, k_out, v_out)
+    _check(lib.slim_kv8_read(at, ns, size, layer_offset, _index(slots, "slots"), n_tokens, Hkv, d, block, _dtype_code(k_out), kp, vp, ldk, ldv, _stream()), "slim_kv8_read")
+    return k_out, v_out
+
+
+def batch_attn_kv8_workspace_bytes(n_rows: int, n_requests: int, n_q_heads: int, n_kv_heads: int, head_dim: int, dtype: torch.dtype = torch.bfloat16) -> int:
+    """Of slim_batch_attn_kv8, for either type (0: sizes that are not covered)."""
+    return load_library().slim_batch_attn_kv8_workspace_bytes(n_rows, n_requests, n_q_heads, n_kv_heads, head_dim)
+
+
+def slim_batch_attn_kv8(q: torch.Tensor, row_start: torch.Tensor, lens: torch.Tensor, block_table: torch.Tensor, pool: torch.Tensor, block: int, n_kv_heads: int,
+                        softmax_scale: float = 0.0, layer_offset: int = 0, out: torch.Tensor | None = None, workspace: torch.Tensor | None = None) -> torch.Tensor:
+    """q[n_rows, Hq, d] (rows may be apart): the rows of a step, row_start[R + 1] the first of each request, lens[R] the requests' tokens with them (slim_batch_map's lens_out).  Each
+    row attends to its request's tokens up to itself whose blocks block_table[R, max_blocks] finds in pool[slots, ...] -> out[n_rows, Hq, d]; rows behind the last request: zero, or as
+    out had them."""
+    lib = load_library()
+    n, Hq, d = shape = q.shape
+    R = lens.numel()
+    if block_table.dim() != 2 or block_table.shape[0] != R:
+        raise ValueError("block_table must be [requests, blocks]")
+    if out is None:
+        out = torch.zeros(shape, dtype=q.dtype, device=q.device)
+    elif out.shape != shape or out.dtype != q.dtype or not out.is_cuda:
+        raise ValueError("out must be like q")
+    if not q.is_cuda:
+        raise ValueError("q must be a GPU tensor")
+    if workspace is None:
+        need = lib.slim_batch_attn_kv8_workspace_bytes(n, R, Hq, n_kv_heads, d)
+        workspace = torch.empty(max(need, 256), dtype=torch.uint8, device=q.device)
+    _here("slim_batch_attn_kv8", q, row_start, lens, block_table, pool, out, workspace)
+    ns = pool.shape[0]
+    code = lib.slim_batch_attn_kv8(q.data_ptr(), Hq * d if q.is_contiguous() else _row_stride(q, "q"), _counts(row_start, R + 1, "row_start"), _index(lens, "lens"),
+                                   _index(block_table, "block_table"), R, n, block_table.shape[1], _dev(pool, "pool"), ns,
+                                   pool.numel() // ns * pool.element_size() if ns else 0, layer_offset, block, Hq, n_kv_heads, d, softmax_scale, _dtype_code(q),
+                                   out.data_ptr(), Hq * d if out.is_contiguous() else _row_stride(out, "out"), _dev(workspace, "workspace"),
+                                   workspace.numel() * workspace.element_size(), _stream())
+    if code:
+        _check(code, "slim_batch_attn_kv8")
+    return out
 
 
 def slim_rope_table(pos: torch.Tensor | None, n: int, head_dim: int, theta: float,

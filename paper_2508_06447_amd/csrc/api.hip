@@ -3,6 +3,7 @@
 #include "rows.h"
 #include "routes.h"
 #include "row_tile.h"
+#include "batch.h"
 #include <math.h>
 #include <algorithm>
 #include <mutex>
@@ -345,6 +346,101 @@ int slim_decode_attn_kv4(const void* q, const void* gpu_pool, size_t slot_bytes,
     if (softmax_scale == 0.f) softmax_scale = 1.0f / sqrtf((float)head_dim);
     return launch_decode_attn_kv4(q, gpu_pool, slot_bytes, layer_offset, block_of_slot, n_slots, block, n_prompt_tokens, k_response, v_response, n_response, n_q_heads,
                                   n_kv_heads, softmax_scale, dtype, out, (float*)workspace, (hipStream_t)stream);
+}
+
+// ---- a batch of requests (batch.hip), its cache in 8 bits (kv8.hip)
+constexpr int kKv8RowsMost = 1 << 29;                    // of a call that writes or reads: at most eight threads of a launch per row
+constexpr long long kBatchTokensMost = 1ll << 30;        // of a request, as its table has room for: units of keys are counted in 32 bits
+static bool kv8_heads_ok(int n_kv_heads, int head_dim) { return (head_dim == 64 || head_dim == 128) && n_kv_heads <= 65535; }
+static bool places_ok(int n_slots, int block) { return block <= kKv4BlockMost && (long long)n_slots * block < 1ll << 31; }      // places in the pool are counted in 32 bits
+static bool apart(const void* a, size_t a_bytes, const void* b, size_t b_bytes) {
+    return !a || !b || (uintptr_t)a + a_bytes <= (uintptr_t)b || (uintptr_t)b + b_bytes <= (uintptr_t)a;
+}
+
+int slim_batch_map(const int* lens, const int* n_new, int n_requests, int block, int* block_table, int max_blocks, const int* free_slots, int n_free, const int* used,
+                   int n_slots, int n_rows, int* lens_out, int* row_start, int* row_pos, int* row_slot, int* info, void* stream) {
+    if (!lens || !n_new || !block_table || !lens_out || !row_start || !row_pos || !row_slot || !info || n_requests < 1 || block < 1 || max_blocks < 1 || n_free < 0 ||
+        n_slots < 1 || n_rows < 1 || (n_free > 0 && !free_slots))
+        return SLIM_INVALID_ARG;
+    if (n_requests > kBatchRequestsMost || !places_ok(n_slots, block) || (long long)max_blocks * block > kBatchTokensMost || n_rows >= kKv8RowsMost) return SLIM_UNSUPPORTED;
+    // what one workgroup writes another one still reads
+    const size_t R = (size_t)n_requests * 4, rows = (size_t)n_rows * 4;
+    const struct { const void* p; size_t bytes; } outs[] = {{lens_out, R}, {row_start, R + 4}, {row_pos, rows}, {row_slot, rows}, {info, 16}, {block_table, R * max_blocks}},
+                                                  ins[] = {{lens, R}, {n_new, R}, {free_slots, (size_t)n_free * 4}, {used, 4}};
+    for (int i = 0; i < 6; ++i) {
+        for (int j = 0; j < i; ++j)
+            if (!apart(outs[i].p, outs[i].bytes, outs[j].p, outs[j].bytes)) return SLIM_INVALID_ARG;
+        for (const auto& in : ins)
+            if (!apart(outs[i].p, outs[i].bytes, in.p, in.bytes)) return SLIM_INVALID_ARG;
+    }
+    return launch_batch_map(lens, n_new, n_requests, block, block_table, max_blocks, free_slots, n_free, used, n_slots, n_rows, lens_out, row_start, row_pos, row_slot, info,
+                            (hipStream_t)stream);
+}
+
+size_t slim_kv8_block_bytes(int block, int n_kv_heads, int head_dim) {
+    if (block < 1 || block > kKv4BlockMost || n_kv_heads < 1 || !kv8_heads_ok(n_kv_heads, head_dim)) return 0;
+    return align_up(2 * (size_t)block * n_kv_heads * head_dim + 2 * (size_t)n_kv_heads, 16);
+}
+
+// What the calls on the cache have in common.
+static int kv8_pool_checks(const void* pool, int n_slots, size_t slot_bytes, size_t layer_offset, int block, int n_kv_heads, int head_dim, int dtype) {
+    if (!pool || n_slots < 1 || block < 1 || n_kv_heads < 1 || head_dim < 1) return SLIM_INVALID_ARG;
+    if (!dtype_ok(dtype) || !kv8_heads_ok(n_kv_heads, head_dim) || !places_ok(n_slots, block)) return SLIM_UNSUPPORTED;
+    if (!slot_holds(slim_kv8_block_bytes(block, n_kv_heads, head_dim), layer_offset, slot_bytes)) return SLIM_INVALID_ARG;
+    return slot_bytes % 16 != 0 || layer_offset % 16 != 0 || !aligned16(pool) ? SLIM_UNSUPPORTED : SLIM_OK;
+}
+// Rows [.., heads, head_dim] of dtype with stride ld.
+static int rows_check(const void* p, int ld, int heads, int head_dim, int dtype) {
+    if (!p || (long long)heads * head_dim > ld) return SLIM_INVALID_ARG;
+    return !aligned16(p) || ld % (dtype == SLIM_BF16 ? 8 : 4) != 0 ? SLIM_UNSUPPORTED : SLIM_OK;
+}
+
+int slim_kv8_write(const void* k, const void* v, int ldk, int ldv, const int* row_slot, int n_rows, int n_kv_heads, int head_dim, int block, int dtype, void* pool, int n_slots,
+                   size_t slot_bytes, size_t layer_offset, void* stream) {
+    if (!row_slot || n_rows < 1) return SLIM_INVALID_ARG;
+    if (const int rc = kv8_pool_checks(pool, n_slots, slot_bytes, layer_offset, block, n_kv_heads, head_dim, dtype)) return rc;
+    if (const int rc = rows_check(k, ldk, n_kv_heads, head_dim, dtype)) return rc;
+    if (const int rc = rows_check(v, ldv, n_kv_heads, head_dim, dtype)) return rc;
+    if (n_rows >= kKv8RowsMost) return SLIM_UNSUPPORTED;
+    return launch_kv8_write(k, v, ldk, ldv, row_slot, n_rows, n_kv_heads, head_dim, block, dtype, pool, n_slots, slot_bytes, layer_offset, (hipStream_t)stream);
+}
+
+int slim_kv8_read(const void* pool, int n_slots, size_t slot_bytes, size_t layer_offset, const int* slots, int n_tokens, int n_kv_heads, int head_dim, int block, int dtype,
+                  void* k_out, void* v_out, int ldk, int ldv, void* stream) {
+    if (n_tokens < 1) return SLIM_INVALID_ARG;
+    if (const int rc = kv8_pool_checks(pool, n_slots, slot_bytes, layer_offset, block, n_kv_heads, head_dim, dtype)) return rc;
+    if (const int rc = rows_check(k_out, ldk, n_kv_heads, head_dim, dtype)) return rc;
+    if (const int rc = rows_check(v_out, ldv, n_kv_heads, head_dim, dtype)) return rc;
+    if (n_tokens >= kKv8RowsMost) return SLIM_UNSUPPORTED;
+    return launch_kv8_read(pool, n_slots, slot_bytes, layer_offset, slots, n_tokens, n_kv_heads, head_dim, block, dtype, k_out, v_out, ldk, ldv, (hipStream_t)stream);
+}
+
+// Sizes of a call of slim_batch_attn_kv8 that its launches can hold.
+static bool batch_attn_ok(int n_rows, int n_requests, int n_q_heads, int n_kv_heads) {
+    return n_requests <= kBatchRequestsMost && (long long)n_rows * n_q_heads <= 1ll << 26 && (long long)n_requests * n_kv_heads <= 1ll << 22;
+}
+
+size_t slim_batch_attn_kv8_workspace_bytes(int n_rows, int n_requests, int n_q_heads, int n_kv_heads, int head_dim) {
+    if (n_rows < 1 || n_requests < 1 || n_q_heads < 1 || n_kv_heads < 1 || n_q_heads % n_kv_heads != 0 || !kv8_heads_ok(n_kv_heads, head_dim) ||
+        !batch_attn_ok(n_rows, n_requests, n_q_heads, n_kv_heads))
+        return 0;
+    return batch_attn_kv8_workspace_bytes(n_rows, n_q_heads, head_dim);
+}
+
+int slim_batch_attn_kv8(const void* q, int ldq, const int* row_start, const int* lens, const int* block_table, int n_requests, int n_rows, int max_blocks, const void* pool,
+                        int n_slots, size_t slot_bytes, size_t layer_offset, int block, int n_q_heads, int n_kv_heads, int head_dim, float softmax_scale, int dtype, void* out,
+                        int ldo, void* workspace, size_t workspace_bytes, void* stream) {
+    if (!row_start || !lens || !block_table || !workspace || n_requests < 1 || n_rows < 1 || max_blocks < 1 || n_q_heads < 1 || n_kv_heads < 1 ||
+        n_q_heads % n_kv_heads != 0 || !(softmax_scale >= 0.f))
+        return SLIM_INVALID_ARG;
+    if (const int rc = kv8_pool_checks(pool, n_slots, slot_bytes, layer_offset, block, n_kv_heads, head_dim, dtype)) return rc;
+    if (const int rc = rows_check(q, ldq, n_q_heads, head_dim, dtype)) return rc;
+    if (const int rc = rows_check(out, ldo, n_q_heads, head_dim, dtype)) return rc;
+    if (!batch_attn_ok(n_rows, n_requests, n_q_heads, n_kv_heads) || (long long)max_blocks * block > kBatchTokensMost || ((uintptr_t)workspace & 255u)) return SLIM_UNSUPPORTED;
+    if (workspace_bytes < slim_batch_attn_kv8_workspace_bytes(n_rows, n_requests, n_q_heads, n_kv_heads, head_dim)) return SLIM_WORKSPACE_TOO_SMALL;
+    if (softmax_scale == 0.f) softmax_scale = 1.0f / sqrtf((float)head_dim);
+    return launch_batch_attn_kv8(q, ldq, row_start, lens, block_table, n_requests, n_rows, max_blocks, pool, n_slots, slot_bytes, layer_offset, block, n_q_heads, n_kv_heads, head_dim,
+                                 softmax_scale, dtype, out, ldo, workspace, (hipStream_t)stream);
 }
 
 // Workspace of slim_decode_layer: h | rstd | q | o | act | attention partials

@@ -1,0 +1,597 @@
+// A Key-Value cache in 8 bits for a batch of requests: rows written into the slots that a map names, read back, and attention of each request's last tokens over its blocks where they lie.
+//
+// A slot holds, for each kv head, one power of two 2^e for the Keys of the block's rows and one for the Values', and a byte per channel: sign, four bits of exponent (bias 7), three of
+// mantissa, largest 448, 127 not a number.  e is the smallest for which no magnitude is above 448 * 2^e, kept in [-117, 119], so that what a byte stands for is a bfloat16 and a
+// float32 number exactly and zero or a normal one.  Both directions are single instructions for two channels (v_cvt_scalef32_pk_*).
+//
+// Layout of a slot (block B, H kv heads, heads of d): Keys' codes [H, B, d], Values' codes, e + 127 of Keys and Values [H, 2] -- a kv head's rows lie together, as the attention
+// reads them.
+#include "row_tile.h"
+#include "batch.h"
+#include <algorithm>
+#include <mutex>
+
+namespace slim {
+
+typedef short i16x2 __attribute__((ext_vector_type(2)));
+typedef __bf16 bf16x2_t __attribute__((ext_vector_type(2)));
+
+constexpr int kKv8ByteLow = 10, kKv8ByteHigh = 246;      // e + 127 of -117 and 119
+constexpr uint32_t kKv8NaN = 0x7f;
+
+// What lies where in a slot, for one kv head.
+struct Kv8Head {
+    size_t k, v, e;
+    __device__ __forceinline__ Kv8Head(int g, int block, int Hkv, int d) {
+        const size_t rows = (size_t)Hkv * block, at = (size_t)g * block;
+        k = at * d;
+        v = (rows + at) * d;
+        e = 2 * rows * d + 2 * g;
+    }
+};
+
+__device__ __forceinline__ float kv8_power(uint32_t byte) { return __builtin_bit_cast(float, byte << 23); }
+
+// Eight channels as bfloat16; power: 2^e.
+__device__ __forceinline__ bf16x8 kv8_to_bf16(uint2 c, float power) {
+    const bf16x2_t a = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(c.x, power, false), b = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(c.x, power, true);
+    const bf16x2_t d = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(c.y, power, false), e = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(c.y, power, true);
+    return bf16x8{a[0], a[1], b[0], b[1], d[0], d[1], e[0], e[1]};
+}
+// Four finite floats as codes relative to 2^e, 448 for what is above.
+__device__ __forceinline__ uint32_t kv8_codes(const float* f, float power) {
+    float y[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) y[i] = __builtin_amdgcn_fmed3f(f[i], -448.f * power, 448.f * power);
+    i16x2 c = {0, 0};
+    c = __builtin_amdgcn_cvt_scalef32_pk_fp8_f32(c, y[0], y[1], power, false);
+    c = __builtin_amdgcn_cvt_scalef32_pk_fp8_f32(c, y[2], y[3], power, true);
+    return __builtin_bit_cast(uint32_t, c);
+}
+
+// ---- written
+// A run is a stretch of rows whose places follow each other in one block.  A workgroup takes the runs that begin within its `chunk` rows of the map, for one kv head, Keys or Values: the run's
+// largest magnitude, the exponent, the codes.  Where rows in front of the run are in the block already, the larger exponent of both holds, and where it grows they are rounded again.
+constexpr int kKv8Keep = 4;                              // passes over a run's rows that stay in registers
+struct Kv8Write {
+    const int* row_slot;
+    unsigned char* pool;
+    size_t slot_bytes, layer_offset;
+    int n_rows, n_places, block, Hkv, ldk, ldv, chunk;   // n_places: of the pool, n_slots * block
+};
+
+template <typename T, int D>
+__global__ void __launch_bounds__(256) kv8_write_kernel(const T* __restrict__ K, const T* __restrict__ V, Kv8Write a) {
+    constexpr int PC = D / 8, RPP = 256 / PC, NV = sizeof(T) / 2;      // lanes a row, rows a pass, 16-byte loads a lane
+    __shared__ uint32_t most_of[2][4];
+    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, piece = tid % PC, row = tid / PC;
+    const bool value = blockIdx.z;
+    const int g = blockIdx.y;
+    const T* src = (value ? V : K) + (size_t)g * D + piece * 8;
+    const size_t ld = value ? a.ldv : a.ldk;
+    const Kv8Head at(g, a.block, a.Hkv, D);
+    auto place_of = [&](long long t) {                   // of row t, -1: none
+        const int p = t >= 0 && t < a.n_rows ? a.row_slot[t] : -1;
+        return p >= 0 && p < a.n_places ? p : -1;
+    };
+    auto load = [&](int t, uint4* c) {
+        const T* p = src + (size_t)t * ld;
+        c[0] = load_stream16(p);
+        if constexpr (NV == 2) c[1] = load_stream16(p + 4);
+    };
+    auto unpack = [&](const uint4* c, float* f) {
+        Elem<T>::unpack(c[0], f);
+        if constexpr (NV == 2) Elem<T>::unpack(c[1], f + 4);
+    };
+    // largest finite magnitude (as whole numbers magnitudes compare alike)
+    auto most = [&](const float* f, uint32_t m) {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            const uint32_t x = __builtin_bit_cast(uint32_t, f[i]) & 0x7fffffffu;
+            m = max(m, x >= 0x7f800000u ? 0u : x);
+        }
+        return m;
+    };
+
+    const long long first = (long long)blockIdx.x * a.chunk;
+    unsigned long long starts;
+    {
+        const int p = lane < a.chunk ? place_of(first + lane) : -1;
+        starts = __ballot(p >= 0 && (p % a.block == 0 || place_of(first + lane - 1) != p - 1));
+    }
+    int turn = 0;
+    while (starts) {
+        const int t0 = (int)(first + __builtin_ctzll(starts));
+        starts &= starts - 1;
+        const int p0 = place_of(t0), slot = p0 / a.block, r0 = p0 - slot * a.block, longest = a.block - r0;
+        int n = 1;                                       // rows of the run
+        while (n < longest) {
+            const bool same = n + lane < longest && place_of((long long)t0 + n + lane) == p0 + n + lane;
+            const unsigned long long end = ~__ballot(same);
+            n += end ? __builtin_ctzll(end) : 64;
+            if (end) break;
+        }
+        unsigned char* base = a.pool + (size_t)slot * a.slot_bytes + a.layer_offset;
+        unsigned char* codes = base + (value ? at.v : at.k);
+        unsigned char* exponent = base + at.e + (value ? 1 : 0);
+        uint4 keep[kKv8Keep][NV];
+        uint32_t m = 0;
+#pragma unroll
+        for (int i = 0; i < kKv8Keep; ++i) load(t0 + min(n - 1, i * RPP + row), keep[i]);      // rows behind the run repeat its last
+        const uint32_t before = r0 > 0 ? min(max((int)*exponent, kKv8ByteLow), kKv8ByteHigh) : kKv8ByteLow;
+#pragma unroll
+        for (int i = 0; i < kKv8Keep; ++i) {
+            float f[8];
+            unpack(keep[i], f);
+            m = most(f, m);
+        }
+        for (int i = kKv8Keep * RPP + row; i < n; i += RPP) {
+            uint4 c[NV];
+            float f[8];
+            load(t0 + i, c);
+            unpack(c, f);
+            m = most(f, m);
+        }
+#pragma unroll
+        for (int o = 32; o > 0; o >>= 1) m = max(m, (uint32_t)__shfl_xor((int)m, o, 64));
+        if (lane == 0) most_of[turn & 1][wave] = m;
+        __syncthreads();
+#pragma unroll
+        for (int w = 0; w < 4; ++w) m = max(m, most_of[turn & 1][w]);
+        ++turn;
+        // a magnitude from just above 1.75 times a power of two on counts as the next power
+        const uint32_t byte = max(before, (uint32_t)min(max((int)((m + 0x1fffffu) >> 23) - 8, kKv8ByteLow), kKv8ByteHigh));
+        const float power = kv8_power(byte);
+        auto store = [&](int i, const uint4* c) {
+            float f[8];
+            unpack(c, f);
+            uint2 code;
+            bool odd = false;
+#pragma unroll
+            for (int x = 0; x < 8; ++x) odd |= !(fabsf(f[x]) < INFINITY);
+            code.x = kv8_codes(f, power);
+            code.y = kv8_codes(f + 4, power);
+            if (odd) {
+#pragma unroll
+                for (int x = 0; x < 8; ++x)
+                    if (!(fabsf(f[x]) < INFINITY)) {
+                        uint32_t& w = x < 4 ? code.x : code.y;
+                        w = (w & ~(0xffu << (x % 4 * 8))) | kKv8NaN << (x % 4 * 8);
+                    }
+            }
+            *reinterpret_cast<uint2*>(codes + (size_t)(r0 + i) * D + piece * 8) = code;
+        };
+#pragma unroll
+        for (int i = 0; i < kKv8Keep; ++i)
+            if (i * RPP + row < n) store(i * RPP + row, keep[i]);
+        for (int i = kKv8Keep * RPP + row; i < n; i += RPP) {
+            uint4 c[NV];
+            load(t0 + i, c);
+            store(i, c);
+        }
+        if (r0 > 0 && byte > before) {                   // the rows in front, relative to the larger power
+            const float up = kv8_power(127 - min(byte - before, 100u));      // (a hundred and more: nothing is left but zeros)
+            for (size_t i = (size_t)tid * 8; i < (size_t)r0 * D; i += 256 * 8) {
+                uint2 c = *reinterpret_cast<const uint2*>(codes + i);
+#pragma unroll
+                for (int x = 0; x < 2; ++x) {
+                    uint32_t& w = x ? c.y : c.x;
+                    const auto lo = __builtin_amdgcn_cvt_scalef32_pk_f32_fp8(w, up, false), hi = __builtin_amdgcn_cvt_scalef32_pk_f32_fp8(w, up, true);
+                    const float f[4] = {lo[0], lo[1], hi[0], hi[1]};
+                    uint32_t now = kv8_codes(f, 1.f);
+#pragma unroll
+                    for (int y = 0; y < 4; ++y)
+                        if ((w >> (8 * y) & 0x7fu) == kKv8NaN) now = (now & ~(0xffu << (8 * y))) | kKv8NaN << (8 * y);
+                    w = now;
+                }
+                *reinterpret_cast<uint2*>(codes + i) = c;
+            }
+        }
+        if (tid == 0) *exponent = (unsigned char)byte;
+    }
+}
+
+int launch_kv8_write(const void* k, const void* v, int ldk, int ldv, const int* row_slot, int n_rows, int Hkv, int d, int block, int dtype, void* pool, int n_slots, size_t slot_bytes,
+                     size_t layer_offset, hipStream_t st) {
+    const long long wanted = (long long)n_rows * Hkv * 2 / 4096;
+    const int chunk = (int)std::min<long long>(64, std::max<long long>(1, wanted));
+    const Kv8Write a{row_slot, (unsigned char*)pool, slot_bytes, layer_offset, n_rows, n_slots * block, block, Hkv, ldk, ldv, chunk};
+    const dim3 grid((n_rows - 1) / chunk + 1, Hkv, 2);
+#define SLIM_KV8(T, D) hipLaunchKernelGGL((kv8_write_kernel<T, D>), grid, dim3(256), 0, st, (const T*)k, (const T*)v, a)
+    if (dtype == SLIM_BF16) { if (d == 64) SLIM_KV8(bf16_t, 64); else SLIM_KV8(bf16_t, 128); }
+    else if (d == 64) SLIM_KV8(float, 64);
+    else SLIM_KV8(float, 128);
+#undef SLIM_KV8
+    return check_launch();
+}
+
+// ---- read back
+constexpr int kKv8Steps = 4;
+struct Kv8Read {
+    const unsigned char* pool;
+    size_t slot_bytes, layer_offset;
+    const int* slots;                                    // null: block b lies in slot b
+    int n_slots, n_tokens, block, Hkv, ldk, ldv;
+};
+
+template <typename T, int D>
+__global__ void __launch_bounds__(256) kv8_read_kernel(T* __restrict__ K, T* __restrict__ V, Kv8Read a) {
+    constexpr int PC = D / 8, RPW = 64 / PC;             // lanes a row, rows a step
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, piece = lane % PC;
+    const bool value = blockIdx.z;
+    const int g = blockIdx.y;
+    const int t0 = (blockIdx.x * 4 + wave) * (RPW * kKv8Steps) + lane / PC;
+    T* out = (value ? V : K) + (size_t)g * D + piece * 8;
+    const size_t ld = value ? a.ldv : a.ldk;
+    const Kv8Head at(g, a.block, a.Hkv, D);
+    int b = t0 / a.block, r = t0 - b * a.block;
+    uint2 code[kKv8Steps];
+    uint32_t byte[kKv8Steps];
+    bool have[kKv8Steps];
+#pragma unroll
+    for (int s = 0; s < kKv8Steps; ++s) {
+        have[s] = false;
+        if (t0 + s * RPW < a.n_tokens) {
+            const int slot = a.slots ? a.slots[b] : b;
+            if (slot >= 0 && slot < a.n_slots) {
+                const unsigned char* src = a.pool + (size_t)slot * a.slot_bytes + a.layer_offset;
+                code[s] = *reinterpret_cast<const uint2*>(src + (value ? at.v : at.k) + (size_t)r * D + piece * 8);
+                byte[s] = src[at.e + (value ? 1 : 0)];
+                have[s] = true;
+            }
+        }
+        r += RPW;
+        while (r >= a.block) { r -= a.block; ++b; }
+    }
+#pragma unroll
+    for (int s = 0; s < kKv8Steps; ++s) {
+        if (!have[s]) continue;
+        const uint4 v = __builtin_bit_cast(uint4, kv8_to_bf16(code[s], kv8_power(byte[s])));
+        T* dst = out + (size_t)(t0 + s * RPW) * ld;
+        if constexpr (sizeof(T) == 2) {
+            store_stream16(dst, v);
+        } else {
+            float f[8];
+            Elem<bf16_t>::unpack(v, f);
+            store_stream16(dst, Elem<float>::pack(f));
+            store_stream16(dst + 4, Elem<float>::pack(f + 4));
+        }
+    }
+}
+
+int launch_kv8_read(const void* pool, int n_slots, size_t slot_bytes, size_t layer_offset, const int* slots, int n_tokens, int Hkv, int d, int block, int dtype, void* k, void* v,
+                    int ldk, int ldv, hipStream_t st) {
+    const Kv8Read a{(const unsigned char*)pool, slot_bytes, layer_offset, slots, n_slots, n_tokens, block, Hkv, ldk, ldv};
+    const int per_wg = 4 * kKv8Steps * 512 / d;
+    const dim3 grid((n_tokens - 1) / per_wg + 1, Hkv, 2);
+#define SLIM_KV8(T, D) hipLaunchKernelGGL((kv8_read_kernel<T, D>), grid, dim3(256), 0, st, (T*)k, (T*)v, a)
+    if (dtype == SLIM_BF16) { if (d == 64) SLIM_KV8(bf16_t, 64); else SLIM_KV8(bf16_t, 128); }
+    else if (d == 64) SLIM_KV8(float, 64);
+    else SLIM_KV8(float, 128);
+#undef SLIM_KV8
+    return check_launch();
+}
+
+// ---- attention
+// A request's rows are its (query, query head of the kv head) pairs, query by query, head by head; a tile is 16 of them.  The units of 32 keys that a tile may see are cut into
+// stretches of at most `step` units, one workgroup a stretch, whose waves take a unit in turn; a tile of one stretch writes its results, one of several leaves partial results, which a
+// second kernel merges.  step follows from the batch: all units of all tiles are dealt to about kBatchTarget workgroups.  The lengths are known to the GPU alone, so that each wave
+// forms the sums over the requests for itself, 64 of them at a time.
+constexpr int kBatchTarget = 1024, kBatchLeast = 4;
+constexpr int kBatchWaves = 4;
+constexpr int kBatchParts = 2 * kBatchTarget;            // stretches of tiles that have several: units / step + 1 of each, at most twice units / step
+
+struct BatchAttnArgs {
+    const int *row_start, *lens, *table;
+    const unsigned char* pool;
+    size_t slot_bytes, layer_offset;
+    float* part;                                         // [kBatchParts][16][D + 2]
+    int2* where;                                         // of row (t, h): its first partial result, their number * 16 + its row of the tile
+    float scale_log2e;
+    int R, max_blocks, n_slots, n_rows, block, per_block, Hq, Hkv, ldq, ldo;
+};
+
+struct BatchRequest { int lo, n, len, rows, tiles, units; };      // first row of the step, rows of it, tokens, rows of a kv head
+__device__ __forceinline__ BatchRequest batch_request(const BatchAttnArgs& a, int r) {
+    BatchRequest x;
+    x.lo = min(max(a.row_start[r], 0), a.n_rows);
+    x.n = min(max(a.row_start[r + 1], x.lo), a.n_rows) - x.lo;
+    x.len = min(max(a.lens[r], 0), a.max_blocks * a.block);
+    x.rows = x.n * (a.Hq / a.Hkv);
+    x.tiles = (x.rows + kTileRows - 1) / kTileRows;
+    const int whole = x.len / a.block;
+    x.units = whole * a.per_block + (x.len - whole * a.block + kTileKeys - 1) / kTileKeys;
+    return x;
+}
+__device__ __forceinline__ int wave_prefix(int v, int lane) {      // sum of the lanes up to this one
+#pragma unroll
+    for (int o = 1; o < 64; o <<= 1) {
+        const int x = __shfl_up(v, o, 64);
+        if (lane >= o) v += x;
+    }
+    return v;
+}
+
+template <typename T, int D>
+__global__ void __launch_bounds__(64 * kBatchWaves) batch_attn_kv8_kernel(const T* __restrict__ q, T* __restrict__ out, BatchAttnArgs a) {
+    typedef RowTile<T, D> Tile;
+    constexpr int NP = Tile::NP, KS = Tile::KS, PC = D / 64, NW = kBatchWaves;      // 16-byte pieces of a lane's channels
+    __shared__ __align__(16) unsigned char lds[NW * Tile::kLdsBytes];
+    const int lane = threadIdx.x & 63, l16 = lane & 15, qr = lane >> 4, G = a.Hq / a.Hkv;
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const unsigned tile_lds = (unsigned)(uintptr_t)lds + wave * Tile::kLdsBytes;
+
+    // Which stretch of which tile of which request and kv head.  The kv head goes fastest: with eight of them each XCD has its own.
+    const int g = blockIdx.x % a.Hkv;
+    int item = blockIdx.x / a.Hkv;
+    long long total = 0;
+    for (int r0 = 0; r0 < a.R; r0 += 64)
+        if (r0 + lane < a.R) {
+            const BatchRequest x = batch_request(a, r0 + lane);
+            total += (long long)x.tiles * x.units;
+        }
+#pragma unroll
+    for (int o = 32; o > 0; o >>= 1) total += __shfl_xor(total, o, 64);
+    const int step = (int)min(1ll << 30, max((long long)kBatchLeast, (total * a.Hkv + kBatchTarget - 1) / kBatchTarget));      // (no request has more units than 2^30)
+    BatchRequest me;
+    int r = -1, stretches = 0, part_at = 0;
+    for (int r0 = 0; r0 < a.R; r0 += 64) {
+        BatchRequest x = {0, 0, 0, 0, 0, 0};
+        if (r0 + lane < a.R) x = batch_request(a, r0 + lane);
+        const int s = max(1, (x.units + step - 1) / step), mine = x.tiles * s, parts = s > 1 ? mine : 0;
+        const int end = wave_prefix(mine, lane), parts_end = wave_prefix(parts, lane);
+        const unsigned long long behind = __ballot(end > item);
+        if (behind) {
+            const int i = __builtin_ctzll(behind);
+            r = r0 + i;
+            item -= __builtin_amdgcn_readlane(end - mine, i);
+            part_at += __builtin_amdgcn_readlane(parts_end - parts, i);
+            stretches = __builtin_amdgcn_readlane(s, i);
+            me.lo = __builtin_amdgcn_readlane(x.lo, i);
+            me.n = __builtin_amdgcn_readlane(x.n, i);
+            me.len = __builtin_amdgcn_readlane(x.len, i);
+            me.rows = __builtin_amdgcn_readlane(x.rows, i);
+            me.tiles = __builtin_amdgcn_readlane(x.tiles, i);
+            break;
+        }
+        item -= __builtin_amdgcn_readlane(end, 63);
+        part_at += __builtin_amdgcn_readlane(parts_end, 63);
+    }
+    if (r < 0 || (unsigned)item >= (unsigned)(me.tiles * stretches)) return;      // (the second: row starts that fall)
+    const int stretch = item % stretches, tile = me.tiles - 1 - item / stretches;      // the last rows see most
+    const int row0 = tile * kTileRows, rows = min(kTileRows, me.rows - row0);
+    const int p0 = me.len - me.n + row0 / G, p1 = me.len - me.n + (row0 + rows - 1) / G;      // positions of the first and the last row
+    const int limit = p1 + 1;                            // (beyond the length only if there are more rows than tokens: then no unit is found)
+    const int* table = a.table + (size_t)r * a.max_blocks;
+
+    // Units are looked up 64 at a time, one a lane.  (A unit of a block that no slot has, or behind the last row, has no keys and is passed over.)
+    const int last = limit <= 0 ? 0 : (limit - 1) / a.block * a.per_block + (limit - 1) % a.block / kTileKeys + 1;
+    const int u_end = (int)min((long long)last, (long long)(stretch + 1) * step);
+    int batch = stretch * step + wave, u_slot = 0, u_row = 0, u_pos = 0, u_rows = 0;
+    unsigned long long left = 0;
+    auto look_up = [&]() {
+        const int u = batch + lane * NW;
+        u_rows = 0;
+        if (u < u_end) {
+            const int b = u / a.per_block;
+            u_slot = table[b];
+            u_row = (u - b * a.per_block) * kTileKeys;
+            u_pos = b * a.block + u_row;
+            u_rows = u_slot >= 0 && u_slot < a.n_slots ? min(kTileKeys, min(a.block - u_row, limit - u_pos)) : 0;
+        }
+        left = __ballot(u_rows > 0);
+    };
+    const Kv8Head head(g, a.block, a.Hkv, D);
+    int have = 0, c0 = 0, pos = 0;
+    const unsigned char* base = nullptr;
+    auto find = [&]() {
+        while (!left) {
+            if (batch + 64 * NW >= u_end) return false;
+            batch += 64 * NW;
+            look_up();
+        }
+        const int i = __builtin_ctzll(left);
+        left &= left - 1;
+        have = __builtin_amdgcn_readlane(u_rows, i);
+        c0 = __builtin_amdgcn_readlane(u_row, i);
+        pos = __builtin_amdgcn_readlane(u_pos, i);
+        base = a.pool + (size_t)__builtin_amdgcn_readlane(u_slot, i) * a.slot_bytes + a.layer_offset;
+        return true;
+    };
+    look_up();
+
+    // the lane's row
+    const int lrow = row0 + min(l16, rows - 1), token = lrow / G;
+    const int p = me.len - me.n + token;
+    Tile t;
+    t.begin(q + (size_t)(me.lo + token) * a.ldq + (size_t)(g * G + lrow - token * G) * D);
+    float w[8];
+    bf16x8 pw[NP];
+    while (find()) {
+        uint4 kx[2][PC], vx[2][PC];
+        const uint32_t e2 = *reinterpret_cast<const uint16_t*>(base + head.e);
+        const float kp = kv8_power(e2 & 0xffu), vp = kv8_power(e2 >> 8);
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+            const size_t at = (size_t)(c0 + min(l16 + 16 * h, have - 1)) * D + qr * (D / 4);      // rows behind the last key repeat it: not seen
+#pragma unroll
+            for (int c = 0; c < PC; ++c) {
+                kx[h][c] = load_stream16(base + head.k + at + c * 16);
+                vx[h][c] = load_stream16(base + head.v + at + c * 16);
+            }
+        }
+        f32x4 s[2];
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+            typename Tile::Scores sum;
+#pragma unroll
+            for (int j = 0; j < KS; ++j) {
+                const uint4 c = kx[h][j / 2];
+                const bf16x8 k = kv8_to_bf16(j % 2 ? make_uint2(c.z, c.w) : make_uint2(c.x, c.y), kp);
+                t.template add_scores<1>(&k, j, sum);
+            }
+            s[h] = sum.sum();
+        }
+        const bool whole = have == kTileKeys && pos + kTileKeys - 1 <= p0;      // every row sees every key
+        const int seen = min(have, p + 1 - pos);         // keys of the unit that row l16 sees
+        if (!whole) {
+#pragma unroll
+            for (int h = 0; h < 2; ++h)
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    const float x = s[h][e];
+                    s[h][e] = h * 16 + qr * 4 + e < seen ? x : -INFINITY;
+                }
+        }
+        t.weigh(s, a.scale_log2e, w);
+        if (!whole) {
+            // Values that some row does not see and that are not numbers: their weight is 0, which a product would turn into an undefined sum.  The unit's values are added key by key
+            // then, each to the rows that see it.
+            bool odd = vp == INFINITY;
+#pragma unroll
+            for (int h = 0; h < 2; ++h)
+#pragma unroll
+                for (int c = 0; c < PC; ++c)
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) {
+                        const uint32_t x = i == 0 ? vx[h][c].x : i == 1 ? vx[h][c].y : i == 2 ? vx[h][c].z : vx[h][c].w;
+                        odd |= (((x & 0x7f7f7f7fu) + 0x01010101u) & 0x80808080u) != 0;
+                    }
+            if (__any(odd)) {
+#pragma unroll 1
+                for (int x = 0; x < 4; ++x) {
+#pragma unroll
+                    for (int i = 0; i < 8; ++i) {
+                        const int key = (i >> 2) * 16 + x * 4 + (i & 3);
+                        const float wk = __shfl(w[i], x * 16 + l16, 64);
+                        if (key < seen) {
+                            const unsigned char* src = base + head.v + (size_t)(c0 + key) * D + qr * 4;
+#pragma unroll
+                            for (int dt = 0; dt < Tile::DT; ++dt) {
+                                const uint32_t c = *reinterpret_cast<const uint32_t*>(src + dt * 16);
+                                const auto lo = __builtin_amdgcn_cvt_scalef32_pk_f32_fp8(c, vp, false), hi = __builtin_amdgcn_cvt_scalef32_pk_f32_fp8(c, vp, true);
+                                t.o[dt][0] += wk * lo[0];
+                                t.o[dt][1] += wk * lo[1];
+                                t.o[dt][2] += wk * hi[0];
+                                t.o[dt][3] += wk * hi[1];
+                            }
+                        }
+                    }
+                }
+                continue;
+            }
+        }
+        bf16_terms<NP>(w, pw);
+#pragma unroll
+        for (int h = 0; h < 2; ++h)
+#pragma unroll
+            for (int j = 0; j < KS; ++j) {
+                const uint4 c = vx[h][j / 2];
+                *(LdsB128)(tile_lds + Tile::v_piece(l16 + 16 * h, qr * KS + j)) = kv8_to_bf16(j % 2 ? make_uint2(c.z, c.w) : make_uint2(c.x, c.y), vp);
+            }
+        t.template add_values<1>(pw, 0, tile_lds);
+    }
+
+    const int first = part_at * a.Hkv + (tile * a.Hkv + g) * stretches, mine = first + stretch;
+    if (stretch == 0 && threadIdx.x < rows) {
+        const int i = row0 + threadIdx.x, n = i / G;
+        a.where[(size_t)(me.lo + n) * a.Hq + g * G + i - n * G] = make_int2(first, stretches * kTileRows + threadIdx.x);
+    }
+    merge_waves<T, D, NW>(t, lds, rows, [&](int i, int dd, float acc, float l, float M) {
+        if (stretches == 1) {
+            const int x = row0 + i, n = x / G;
+            Elem<T>::st(out + (size_t)(me.lo + n) * a.ldo + (size_t)(g * G + x - n * G) * D + dd, l == 0.f ? 0.f : acc / l);
+        } else if (mine < kBatchParts) {
+            float* dst = a.part + ((size_t)mine * kTileRows + i) * (D + 2);
+            dst[dd] = acc;
+            if (dd == 0) { dst[D] = M; dst[D + 1] = l; }
+        }
+    });
+}
+
+// The partial results of a row (t, h), merged: a group of D / 4 lanes takes one in NG of them, four channels a lane.
+template <typename T, int D, int NG>
+__global__ void __launch_bounds__(256) batch_merge_kernel(T* __restrict__ out, BatchAttnArgs a) {
+    constexpr int LN = D / 4, PER = 256 / (LN * NG);     // lanes a group, rows a workgroup
+    __shared__ float ms[NG][PER], ls[NG][PER];
+    __shared__ __align__(16) float os[NG][PER][D];
+    const int tid = threadIdx.x, c = tid % LN, grp = tid / LN % NG, x = tid / (LN * NG);
+    const long long row = (long long)blockIdx.x * PER + x;
+    const int t = (int)(row / a.Hq);
+    int first = 0, n = 0, i = 0;
+    if (t >= max(a.row_start[0], 0) && t < min(a.row_start[a.R], a.n_rows)) {
+        const int2 at = a.where[row];
+        first = at.x;
+        n = at.y / kTileRows;
+        i = at.y % kTileRows;
+        if (n <= 1 || i < 0 || first < 0 || n > kBatchParts || first > kBatchParts - n) n = 0;
+    }
+    const float* p = a.part + ((size_t)first * kTileRows + i) * (D + 2);
+    constexpr size_t kApart = (size_t)kTileRows * (D + 2);
+    float M = -INFINITY, l = 0.f, o[4] = {0.f, 0.f, 0.f, 0.f};
+    for (int y = grp; y < n; y += NG) {
+        const float* s = p + y * kApart;
+        const float2 st = *reinterpret_cast<const float2*>(s + D), v0 = *reinterpret_cast<const float2*>(s + c * 4), v1 = *reinterpret_cast<const float2*>(s + c * 4 + 2);
+        if (st.y == 0.f) continue;                       // a partial result without keys
+        const float now = fmaxf(M, st.x), al = l == 0.f ? 0.f : __builtin_amdgcn_exp2f(M - now), w = __builtin_amdgcn_exp2f(st.x - now);
+        l = l * al + w * st.y;
+        o[0] = o[0] * al + w * v0.x;
+        o[1] = o[1] * al + w * v0.y;
+        o[2] = o[2] * al + w * v1.x;
+        o[3] = o[3] * al + w * v1.y;
+        M = now;
+    }
+    if constexpr (NG > 1) {
+        if (c == 0) { ms[grp][x] = M; ls[grp][x] = l; }
+        *reinterpret_cast<f32x4*>(&os[grp][x][c * 4]) = f32x4{o[0], o[1], o[2], o[3]};
+        __syncthreads();
+        if (grp != 0) return;
+        float top = M;
+#pragma unroll
+        for (int y = 1; y < NG; ++y) top = fmaxf(top, ms[y][x]);
+        float al = l == 0.f ? 0.f : __builtin_amdgcn_exp2f(M - top);
+        l *= al;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) o[e] *= al;
+#pragma unroll
+        for (int y = 1; y < NG; ++y) {
+            al = ls[y][x] == 0.f ? 0.f : __builtin_amdgcn_exp2f(ms[y][x] - top);
+            l += al * ls[y][x];
+#pragma unroll
+            for (int e = 0; e < 4; ++e) o[e] += al * os[y][x][c * 4 + e];
+        }
+    }
+    if (n == 0) return;
+    T* dst = out + (size_t)t * a.ldo + (size_t)(row - (long long)t * a.Hq) * D + c * 4;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) Elem<T>::st(dst + e, l == 0.f ? 0.f : o[e] / l);
+}
+
+static size_t batch_part_bytes(int d) { return (size_t)kBatchParts * kTileRows * (d + 2) * sizeof(float); }
+size_t batch_attn_kv8_workspace_bytes(int n_rows, int Hq, int d) { return align_up(batch_part_bytes(d), 256) + align_up((size_t)n_rows * Hq * sizeof(int2), 256); }
+
+template <typename T, int D>
+static int launch_batch_attn(const void* q, void* out, const BatchAttnArgs& a, hipStream_t st) {
+    const long long tiles = (long long)a.n_rows * (a.Hq / a.Hkv) / kTileRows + a.R;
+    const unsigned grid = (unsigned)(tiles * a.Hkv + kBatchTarget);
+    hipLaunchKernelGGL((batch_attn_kv8_kernel<T, D>), dim3(grid), dim3(64 * kBatchWaves), 0, st, (const T*)q, (T*)out, a);
+    const int rc = check_launch();
+    if (rc) return rc;
+    const long long rows = (long long)a.n_rows * a.Hq;
+    constexpr int kOne = 256 / (D / 4);                  // rows of a workgroup without groups
+    if (tiles * a.Hkv >= kBatchTarget / 2)               // few partial results of a tile
+        hipLaunchKernelGGL((batch_merge_kernel<T, D, 1>), dim3((unsigned)((rows + kOne - 1) / kOne)), dim3(256), 0, st, (T*)out, a);
+    else
+        hipLaunchKernelGGL((batch_merge_kernel<T, D, kOne>), dim3((unsigned)rows), dim3(256), 0, st, (T*)out, a);
+    return check_launch();
+}
+
+int launch_batch_attn_kv8(const void* q, int ldq, const int* row_start, const int* lens, const int* table, int R, int n_rows, int max_blocks, const void* pool, int n_slots, size_t slot_bytes,
+                          size_t layer_offset, int block, int Hq, int Hkv, int d, float scale, int dtype, void* out, int ldo, void* workspace, hipStream_t st) {
+    BatchAttnArgs a{row_start, lens, table, (const unsigned char*)pool, slot_bytes, layer_offset, (float*)workspace, (int2*)((char*)workspace + align_up(batch_part_bytes(d), 256)),
+                    scale * 1.4426950408889634f, R, max_blocks, n_slots, n_rows, block, (block + kTileKeys - 1) / kTileKeys, Hq, Hkv, ldq, ldo};
+    if (dtype == SLIM_BF16) return d == 64 ? launch_batch_attn<bf16_t, 64>(q, out, a, st) : launch_batch_attn<bf16_t, 128>(q, out, a, st);
+    return d == 64 ? launch_batch_attn<float, 64>(q, out, a, st) : launch_batch_attn<float, 128>(q, out, a, st);
+}
+
+}  // namespace slim

@@ -171,6 +171,15 @@ int launch_kv4_read(const void* pool, int n_slots, size_t slot_bytes, size_t lay
 int launch_decode_attn_kv4(const void* q, const void* pool, size_t slot_bytes, size_t layer_offset, const int* block_of_slot,
                            int n_slots, int block, int n_prompt, const void* k_resp, const void* v_resp, int n_resp, int Hq,
                            int Hkv, float scale, int dtype, void* out, float* part, hipStream_t st);
+int launch_batch_map(const int* lens, const int* n_new, int R, int block, int* table, int max_blocks, const int* free_slots, int n_free, const int* used, int n_slots, int n_rows,
+                     int* lens_out, int* row_start, int* row_pos, int* row_slot, int* info, hipStream_t st);
+int launch_kv8_write(const void* k, const void* v, int ldk, int ldv, const int* row_slot, int n_rows, int Hkv, int d, int block, int dtype, void* pool, int n_slots, size_t slot_bytes,
+                     size_t layer_offset, hipStream_t st);
+int launch_kv8_read(const void* pool, int n_slots, size_t slot_bytes, size_t layer_offset, const int* slots, int n_tokens, int Hkv, int d, int block, int dtype, void* k, void* v,
+                    int ldk, int ldv, hipStream_t st);
+size_t batch_attn_kv8_workspace_bytes(int n_rows, int Hq, int d);
+int launch_batch_attn_kv8(const void* q, int ldq, const int* row_start, const int* lens, const int* table, int R, int n_rows, int max_blocks, const void* pool, int n_slots, size_t slot_bytes,
+                          size_t layer_offset, int block, int Hq, int Hkv, int d, float scale, int dtype, void* out, int ldo, void* workspace, hipStream_t st);
 size_t sliding_workspace_floats(int n_q, int n_k, int Hq, int Hkv, int d, int window, int sinks, int dtype);
 int launch_sliding_attn(const void* q, const void* k, const void* v, int n_q, int n_k, int Hq, int Hkv, int d, int window, int sinks, float scale, int dtype, void* out,
                         float* part, hipStream_t st);
