@@ -273,240 +273,323 @@ int launch_kv8_read(const void* pool, int n_slots, size_t slot_bytes, size_t lay
 }
 
 // ---- attention
-// A request's rows are its (query, query head of the kv head) pairs, query by query, head by head; a tile is 16 of them.  The units of 32 keys that a tile may see are cut into
-// stretches of at most `step` units, one workgroup a stretch, whose waves take a unit in turn; a tile of one stretch writes its results, one of several leaves partial results, which a
-// second kernel merges.  step follows from the batch: all units of all tiles are dealt to about kBatchTarget workgroups.  The lengths are known to the GPU alone, so that each wave
-// forms the sums over the requests for itself, 64 of them at a time.
-constexpr int kBatchTarget = 1024, kBatchLeast = 4;
+// A request's rows are its (query, query head of the kv head) pairs, query by query, head by head; a tile is 16 of them.  A piece is up to 16 keys of one block.  The pieces of all tiles of
+// all requests, one behind the other, are cut into equal shares, one workgroup a share, so that requests of any lengths keep all workgroups busy to the end.  A workgroup goes through its
+// share tile by tile; its waves take two pieces in turn, from wherever they lie.  A tile that lies in one share is written at once, one that several share is left as partial results, which
+// a second kernel merges.  The lengths are known to the GPU alone, so that each wave forms the sums over the requests for itself, 64 of them at a time.
+constexpr int kPiece = 16;
 constexpr int kBatchWaves = 4;
-constexpr int kBatchParts = 2 * kBatchTarget;            // stretches of tiles that have several: units / step + 1 of each, at most twice units / step
+constexpr int kBatchGrid = 768;                          // workgroups: as many as run together
+constexpr int kBatchLeast = 4 * 2 * kBatchWaves;         // pieces of a share
+constexpr int kBatchTile = 8;                            // what beginning and ending a tile counts for, in pieces
+
+// n / d for 0 <= n < 2^31: (n M) >> (31 + s), 2^s >= d, M = floor(2^(31 + s) / d) + 1, so that 2^(31 + s) < M d <= 2^(31 + s) + 2^s.
+struct Divide {
+    uint32_t factor;
+    int shift;
+    explicit Divide(int d) {
+        shift = 31;
+        while ((1ll << (shift - 31)) < d) ++shift;
+        factor = (uint32_t)((1ull << shift) / (unsigned)d + 1);
+    }
+    __device__ __forceinline__ int operator()(int n) const { return (int)(((unsigned long long)(unsigned)n * factor) >> shift); }
+};
 
 struct BatchAttnArgs {
     const int *row_start, *lens, *table;
     const unsigned char* pool;
     size_t slot_bytes, layer_offset;
-    float* part;                                         // [kBatchParts][16][D + 2]
-    int2* where;                                         // of row (t, h): its first partial result, their number * 16 + its row of the tile
+    float* part;                                         // [kBatchGrid][2][16][D + 2]: of the tile that a share begins within, and of the one that it leaves unfinished
+    int2* where;                                         // of row (t, h): the first share of its tile, their number * 16 + its row of the tile
     float scale_log2e;
-    int R, max_blocks, n_slots, n_rows, block, per_block, Hq, Hkv, ldq, ldo;
+    int R, max_blocks, n_slots, n_rows, block, per_block, Hq, Hkv, ldq, ldo;      // per_block: pieces
+    Divide by_block, by_piece;                           // by block, by per_block
 };
 
-struct BatchRequest { int lo, n, len, rows, tiles, units; };      // first row of the step, rows of it, tokens, rows of a kv head
+struct BatchRequest {
+    int lo, n, len;                                      // first row of the step, rows of it, tokens
+    __device__ __forceinline__ int rows(const BatchAttnArgs& a) const { return n * (a.Hq / a.Hkv); }      // of a kv head
+    __device__ __forceinline__ int tiles(const BatchAttnArgs& a) const { return (rows(a) + kTileRows - 1) / kTileRows; }
+    __device__ __forceinline__ int pieces(const BatchAttnArgs& a) const {
+        const int whole = a.by_block(len);
+        return whole * a.per_block + (len - whole * a.block + kPiece - 1) / kPiece;
+    }
+    __device__ __forceinline__ long long cost(const BatchAttnArgs& a) const { return (long long)tiles(a) * (pieces(a) + kBatchTile); }
+};
 __device__ __forceinline__ BatchRequest batch_request(const BatchAttnArgs& a, int r) {
-    BatchRequest x;
-    x.lo = min(max(a.row_start[r], 0), a.n_rows);
-    x.n = min(max(a.row_start[r + 1], x.lo), a.n_rows) - x.lo;
-    x.len = min(max(a.lens[r], 0), a.max_blocks * a.block);
-    x.rows = x.n * (a.Hq / a.Hkv);
-    x.tiles = (x.rows + kTileRows - 1) / kTileRows;
-    const int whole = x.len / a.block;
-    x.units = whole * a.per_block + (x.len - whole * a.block + kTileKeys - 1) / kTileKeys;
+    BatchRequest x = {0, 0, 0};
+    if (r < a.R) {
+        x.lo = min(max(a.row_start[r], 0), a.n_rows);
+        x.n = min(max(a.row_start[r + 1], x.lo), a.n_rows) - x.lo;
+        x.len = min(max(a.lens[r], 0), a.max_blocks * a.block);
+    }
     return x;
 }
-__device__ __forceinline__ int wave_prefix(int v, int lane) {      // sum of the lanes up to this one
+// Of lane i, which is the same in the whole wave.
+__device__ __forceinline__ int wave_value(int v, int i) { return __builtin_amdgcn_readlane(v, i); }
+__device__ __forceinline__ long long wave_value(long long v, int i) {
+    return (long long)(((unsigned long long)(unsigned)__builtin_amdgcn_readlane((int)(v >> 32), i) << 32) | (unsigned)__builtin_amdgcn_readlane((int)v, i));
+}
+__device__ __forceinline__ long long wave_prefix(long long v, int lane) {      // sum of the lanes up to this one
 #pragma unroll
     for (int o = 1; o < 64; o <<= 1) {
-        const int x = __shfl_up(v, o, 64);
+        const long long x = __shfl_up(v, o, 64);
         if (lane >= o) v += x;
     }
     return v;
 }
+// A loaded value whose first use is here (left alone, the compiler moves what is made of it behind the load, and with it the wait).
+__device__ __forceinline__ uint32_t first_used_here(uint32_t v) {
+    asm volatile("" : "+v"(v));
+    return v;
+}
 
-template <typename T, int D>
-__global__ void __launch_bounds__(64 * kBatchWaves) batch_attn_kv8_kernel(const T* __restrict__ q, T* __restrict__ out, BatchAttnArgs a) {
+template <typename T, int D, int NW>
+__global__ void __launch_bounds__(64 * NW, sizeof(T) == 2 ? 3 : 2) batch_attn_kv8_kernel(const T* __restrict__ q, T* __restrict__ out, BatchAttnArgs a) {
     typedef RowTile<T, D> Tile;
-    constexpr int NP = Tile::NP, KS = Tile::KS, PC = D / 64, NW = kBatchWaves;      // 16-byte pieces of a lane's channels
-    __shared__ __align__(16) unsigned char lds[NW * Tile::kLdsBytes];
-    const int lane = threadIdx.x & 63, l16 = lane & 15, qr = lane >> 4, G = a.Hq / a.Hkv;
-    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    const unsigned tile_lds = (unsigned)(uintptr_t)lds + wave * Tile::kLdsBytes;
-
-    // Which stretch of which tile of which request and kv head.  The kv head goes fastest: with eight of them each XCD has its own.
-    const int g = blockIdx.x % a.Hkv;
-    int item = blockIdx.x / a.Hkv;
-    long long total = 0;
-    for (int r0 = 0; r0 < a.R; r0 += 64)
-        if (r0 + lane < a.R) {
-            const BatchRequest x = batch_request(a, r0 + lane);
-            total += (long long)x.tiles * x.units;
-        }
+    constexpr int NP = Tile::NP, NT = Tile::NT, KS = Tile::KS, PC = D / 64;      // PC: 16-byte pieces of a lane's channels
+    extern __shared__ __align__(16) unsigned char lds[];
+    const int G = a.Hq / a.Hkv;
+    // The kv head goes fastest: with eight of them each XCD has its own.
+    const int g = blockIdx.x % a.Hkv, share_of = blockIdx.x / a.Hkv, shares = gridDim.x / a.Hkv;
+    int r0 = 0;                                          // x: of request r0 + the lane
+    const int lane_in = threadIdx.x & 63;
+    BatchRequest x = batch_request(a, lane_in);
+    long long total = x.cost(a);
+    for (int r = 64; r < a.R; r += 64) total += batch_request(a, r + lane_in).cost(a);
 #pragma unroll
     for (int o = 32; o > 0; o >>= 1) total += __shfl_xor(total, o, 64);
-    const int step = (int)min(1ll << 30, max((long long)kBatchLeast, (total * a.Hkv + kBatchTarget - 1) / kBatchTarget));      // (no request has more units than 2^30)
-    BatchRequest me;
-    int r = -1, stretches = 0, part_at = 0;
-    for (int r0 = 0; r0 < a.R; r0 += 64) {
-        BatchRequest x = {0, 0, 0, 0, 0, 0};
-        if (r0 + lane < a.R) x = batch_request(a, r0 + lane);
-        const int s = max(1, (x.units + step - 1) / step), mine = x.tiles * s, parts = s > 1 ? mine : 0;
-        const int end = wave_prefix(mine, lane), parts_end = wave_prefix(parts, lane);
-        const unsigned long long behind = __ballot(end > item);
+    total = wave_value(total, 0);                        // (in scalar registers, with all that follows from it)
+    const long long share = max((long long)kBatchLeast, (total + shares - 1) / shares), begin = share * share_of;
+    long long left_over = min(total - begin, share);     // of the share
+    if (left_over <= 0) return;
+    long long at = begin;                                // of the share's beginning, counted from request r0's, then from its own request's
+    int i_req;
+    while (true) {
+        const long long mine = x.cost(a), end = wave_prefix(mine, lane_in);
+        const unsigned long long behind = __ballot(end > at);
         if (behind) {
-            const int i = __builtin_ctzll(behind);
-            r = r0 + i;
-            item -= __builtin_amdgcn_readlane(end - mine, i);
-            part_at += __builtin_amdgcn_readlane(parts_end - parts, i);
-            stretches = __builtin_amdgcn_readlane(s, i);
-            me.lo = __builtin_amdgcn_readlane(x.lo, i);
-            me.n = __builtin_amdgcn_readlane(x.n, i);
-            me.len = __builtin_amdgcn_readlane(x.len, i);
-            me.rows = __builtin_amdgcn_readlane(x.rows, i);
-            me.tiles = __builtin_amdgcn_readlane(x.tiles, i);
+            i_req = __builtin_ctzll(behind);
+            at -= wave_value(end - mine, i_req);
             break;
         }
-        item -= __builtin_amdgcn_readlane(end, 63);
-        part_at += __builtin_amdgcn_readlane(parts_end, 63);
+        at -= wave_value(end, 63);
+        r0 += 64;
+        if (r0 >= a.R) return;
+        x = batch_request(a, r0 + lane_in);
     }
-    if (r < 0 || (unsigned)item >= (unsigned)(me.tiles * stretches)) return;      // (the second: row starts that fall)
-    const int stretch = item % stretches, tile = me.tiles - 1 - item / stretches;      // the last rows see most
-    const int row0 = tile * kTileRows, rows = min(kTileRows, me.rows - row0);
+    int tile, from;
+    {
+        const int apart = wave_value(x.pieces(a), i_req) + kBatchTile;
+        tile = (int)(at / apart);
+        from = (int)(at - (long long)tile * apart);
+    }
+
+    const Kv8Head head(g, a.block, a.Hkv, D);
+    while (true) {
+    const BatchRequest me{wave_value(x.lo, i_req), wave_value(x.n, i_req), wave_value(x.len, i_req)};
+    const int pieces = me.pieces(a);
+    int tid = threadIdx.x;
+    asm volatile("" : "+v"(tid));                        // (what follows from it would be kept in registers from tile to tile)
+    const int lane = tid & 63, l16 = lane & 15, qr = lane >> 4, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const unsigned tile_lds = (unsigned)(uintptr_t)lds + wave * Tile::kLdsBytes;
+    const int r = r0 + i_req, take = (int)min((long long)(pieces + kBatchTile - from), left_over);
+    const int row0 = tile * kTileRows, rows = min(kTileRows, me.rows(a) - row0);
     const int p0 = me.len - me.n + row0 / G, p1 = me.len - me.n + (row0 + rows - 1) / G;      // positions of the first and the last row
-    const int limit = p1 + 1;                            // (beyond the length only if there are more rows than tokens: then no unit is found)
+    const int limit = p1 + 1;                            // (zero and below if there are more rows than tokens: then no piece is found)
     const int* table = a.table + (size_t)r * a.max_blocks;
 
-    // Units are looked up 64 at a time, one a lane.  (A unit of a block that no slot has, or behind the last row, has no keys and is passed over.)
-    const int last = limit <= 0 ? 0 : (limit - 1) / a.block * a.per_block + (limit - 1) % a.block / kTileKeys + 1;
-    const int u_end = (int)min((long long)last, (long long)(stretch + 1) * step);
-    int batch = stretch * step + wave, u_slot = 0, u_row = 0, u_pos = 0, u_rows = 0;
+    // The wave's pieces, in pairs: u0, u0 + 1, u0 + 2 NW, ..  64 of them are looked up at once, one a lane, and the table entries of the next 64 are on their way.  A piece of a block that no
+    // slot has, or behind the last row, has no keys and is passed over.
+    const int last = limit <= 0 ? 0 : a.by_block(limit - 1) * a.per_block + (limit - 1 - a.by_block(limit - 1) * a.block) / kPiece + 1;
+    const int u_end = min(last, from + take);
+    constexpr int kBatch = 64 * NW;
+    int u = from + 2 * wave + (lane >> 1) * 2 * NW + (lane & 1);      // the lane's
+    int batch = __builtin_amdgcn_readfirstlane(u) - kBatch;
+    int u_slot = 0, u_pos = 0, u_rows = 0, next_slot = u < u_end ? table[a.by_piece(u)] : -1;
     unsigned long long left = 0;
-    auto look_up = [&]() {
-        const int u = batch + lane * NW;
-        u_rows = 0;
-        if (u < u_end) {
-            const int b = u / a.per_block;
-            u_slot = table[b];
-            u_row = (u - b * a.per_block) * kTileKeys;
-            u_pos = b * a.block + u_row;
-            u_rows = u_slot >= 0 && u_slot < a.n_slots ? min(kTileKeys, min(a.block - u_row, limit - u_pos)) : 0;
-        }
-        left = __ballot(u_rows > 0);
-    };
-    const Kv8Head head(g, a.block, a.Hkv, D);
-    int have = 0, c0 = 0, pos = 0;
-    const unsigned char* base = nullptr;
-    auto find = [&]() {
+    int have[2], c0[2], pos[2];
+    const unsigned char* base[2];
+    auto find = [&]() {                                  // the next two pieces; false: none is left
         while (!left) {
-            if (batch + 64 * NW >= u_end) return false;
-            batch += 64 * NW;
-            look_up();
+            batch += kBatch;
+            if (batch >= u_end) return false;
+            const int b = a.by_piece(u), row = (u - b * a.per_block) * kPiece;
+            u_slot = next_slot;
+            u_pos = b * a.block + row;
+            u_rows = u_slot >= 0 && u_slot < a.n_slots ? min(kPiece, min(a.block - row, limit - u_pos)) : 0;
+            left = __ballot(u_rows > 0);
+            u += kBatch;
+            next_slot = u < u_end ? table[a.by_piece(u)] : -1;
         }
-        const int i = __builtin_ctzll(left);
-        left &= left - 1;
-        have = __builtin_amdgcn_readlane(u_rows, i);
-        c0 = __builtin_amdgcn_readlane(u_row, i);
-        pos = __builtin_amdgcn_readlane(u_pos, i);
-        base = a.pool + (size_t)__builtin_amdgcn_readlane(u_slot, i) * a.slot_bytes + a.layer_offset;
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+            if (h == 1 && !left) {                       // a single one: the other half repeats it, unseen
+                have[1] = 0;
+                c0[1] = c0[0];
+                pos[1] = pos[0];
+                base[1] = base[0];
+                break;
+            }
+            const int i = __builtin_ctzll(left);
+            left &= left - 1;
+            have[h] = __builtin_amdgcn_readlane(u_rows, i);
+            pos[h] = __builtin_amdgcn_readlane(u_pos, i);
+            c0[h] = pos[h] - a.by_block(pos[h]) * a.block;
+            base[h] = a.pool + (size_t)__builtin_amdgcn_readlane(u_slot, i) * a.slot_bytes + a.layer_offset;
+        }
         return true;
     };
-    look_up();
+
+    uint4 kx[2][PC], vx[2][PC];
+    uint32_t ke[2], ve[2];                               // e + 127
+    // Addresses: a wave-uniform base and a 32-bit offset of the lane.  Rows behind the last key repeat it: not seen.  A lane's channels are 16 in a row of each 64, so that an instruction
+    // takes 64 bytes in a row of each key.
+    auto row_offset = [&](int h) { return (unsigned)(min(l16, max(have[h], 1) - 1) * D + qr * 16); };
+    auto channel = [&](int j) { return j / 2 * 64 + qr * 16 + j % 2 * 8; };
+    auto load_k = [&]() {
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+            const unsigned char* at = base[h] + head.k + (size_t)c0[h] * D;
+            const unsigned off = row_offset(h);
+#pragma unroll
+            for (int c = 0; c < PC; ++c) kx[h][c] = *reinterpret_cast<const uint4*>(at + (off + c * 64));
+            ke[h] = base[h][head.e + (lane & 0)];
+        }
+    };
+    auto load_v = [&]() {
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+            const unsigned char* at = base[h] + head.v + (size_t)c0[h] * D;
+            const unsigned off = row_offset(h);
+#pragma unroll
+            for (int c = 0; c < PC; ++c) vx[h][c] = *reinterpret_cast<const uint4*>(at + (off + c * 64));
+            ve[h] = base[h][head.e + 1 + (lane & 0)];
+        }
+    };
+    auto half_of = [](const uint4& c, int j) { return j % 2 ? make_uint2(c.z, c.w) : make_uint2(c.x, c.y); };
+    bool more = find();
+    if (more) { load_k(); load_v(); }
 
     // the lane's row
     const int lrow = row0 + min(l16, rows - 1), token = lrow / G;
     const int p = me.len - me.n + token;
     Tile t;
-    t.begin(q + (size_t)(me.lo + token) * a.ldq + (size_t)(g * G + lrow - token * G) * D);
+    t.begin(q + (size_t)(me.lo + token) * a.ldq + (size_t)(g * G + lrow - token * G) * D, channel);
+    // waited for here: waited for in the loop, the Query fragments take the wait for the codes requested meanwhile with them in every turn
+#pragma unroll
+    for (int b = 0; b < NT; ++b)
+#pragma unroll
+        for (int j = 0; j < KS; ++j) asm volatile("" : "+v"(t.q[b][j]));
+    // Where the lane writes and reads the wave's V tile: one address each, whose bits 4 .. 7 are turned for the pieces and channels.  (Hidden from the compiler in every turn: it would keep
+    // them all in registers, and the Query fragments out of them.)
+    const int vr = 4 * qr + (l16 >> 2);
+    unsigned v_to = tile_lds + Tile::v_piece(l16, qr * 2), v_from = tile_lds + Tile::v_piece(vr, (l16 & 3) >> 1) + (l16 & 1) * 8;
     float w[8];
     bf16x8 pw[NP];
-    while (find()) {
-        uint4 kx[2][PC], vx[2][PC];
-        const uint32_t e2 = *reinterpret_cast<const uint16_t*>(base + head.e);
-        const float kp = kv8_power(e2 & 0xffu), vp = kv8_power(e2 >> 8);
-#pragma unroll
-        for (int h = 0; h < 2; ++h) {
-            const size_t at = (size_t)(c0 + min(l16 + 16 * h, have - 1)) * D + qr * (D / 4);      // rows behind the last key repeat it: not seen
-#pragma unroll
-            for (int c = 0; c < PC; ++c) {
-                kx[h][c] = load_stream16(base + head.k + at + c * 16);
-                vx[h][c] = load_stream16(base + head.v + at + c * 16);
-            }
-        }
+    while (more) {
+        asm volatile("" : "+v"(v_to), "+v"(v_from));
+        const bool whole = have[0] == kPiece && have[1] == kPiece && max(pos[0], pos[1]) + kPiece - 1 <= p0;      // every row sees every key
+        const int seen[2] = {min(have[0], p + 1 - pos[0]), min(have[1], p + 1 - pos[1])};      // keys that row l16 sees
+        more = find();                                   // none left: the last pieces are requested once more, and not used
         f32x4 s[2];
 #pragma unroll
         for (int h = 0; h < 2; ++h) {
             typename Tile::Scores sum;
+            const float kp = kv8_power(first_used_here(ke[h]));
 #pragma unroll
             for (int j = 0; j < KS; ++j) {
-                const uint4 c = kx[h][j / 2];
-                const bf16x8 k = kv8_to_bf16(j % 2 ? make_uint2(c.z, c.w) : make_uint2(c.x, c.y), kp);
+                const bf16x8 k = kv8_to_bf16(half_of(kx[h][j / 2], j), kp);
                 t.template add_scores<1>(&k, j, sum);
             }
             s[h] = sum.sum();
         }
-        const bool whole = have == kTileKeys && pos + kTileKeys - 1 <= p0;      // every row sees every key
-        const int seen = min(have, p + 1 - pos);         // keys of the unit that row l16 sees
+        __builtin_amdgcn_sched_barrier(0);
+        load_k();                                        // the next pieces' Keys fly under these Values
+        __builtin_amdgcn_sched_barrier(0);
         if (!whole) {
 #pragma unroll
             for (int h = 0; h < 2; ++h)
 #pragma unroll
                 for (int e = 0; e < 4; ++e) {
                     const float x = s[h][e];
-                    s[h][e] = h * 16 + qr * 4 + e < seen ? x : -INFINITY;
+                    s[h][e] = qr * 4 + e < seen[h] ? x : -INFINITY;
                 }
         }
         t.weigh(s, a.scale_log2e, w);
-        if (!whole) {
-            // Values that some row does not see and that are not numbers: their weight is 0, which a product would turn into an undefined sum.  The unit's values are added key by key
-            // then, each to the rows that see it.
-            bool odd = vp == INFINITY;
+        float vp[2];
 #pragma unroll
-            for (int h = 0; h < 2; ++h)
+        for (int h = 0; h < 2; ++h) vp[h] = kv8_power(first_used_here(ve[h]));
+        if (!whole) {
+            // Values that some row does not see and that are not numbers: their weight is 0, which a product would turn into an undefined sum.  They become zeros here, and what makes a row
+            // that sees one of them undefined is its sum.
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+                bool odd = false;
 #pragma unroll
                 for (int c = 0; c < PC; ++c)
 #pragma unroll
                     for (int i = 0; i < 4; ++i) {
-                        const uint32_t x = i == 0 ? vx[h][c].x : i == 1 ? vx[h][c].y : i == 2 ? vx[h][c].z : vx[h][c].w;
-                        odd |= (((x & 0x7f7f7f7fu) + 0x01010101u) & 0x80808080u) != 0;
+                        uint32_t& x = i == 0 ? vx[h][c].x : i == 1 ? vx[h][c].y : i == 2 ? vx[h][c].z : vx[h][c].w;
+                        const uint32_t bytes = (((x & 0x7f7f7f7fu) + 0x01010101u) >> 7 & 0x01010101u) * 0xffu;
+                        odd |= bytes != 0;
+                        x &= ~bytes;
                     }
-            if (__any(odd)) {
-#pragma unroll 1
-                for (int x = 0; x < 4; ++x) {
-#pragma unroll
-                    for (int i = 0; i < 8; ++i) {
-                        const int key = (i >> 2) * 16 + x * 4 + (i & 3);
-                        const float wk = __shfl(w[i], x * 16 + l16, 64);
-                        if (key < seen) {
-                            const unsigned char* src = base + head.v + (size_t)(c0 + key) * D + qr * 4;
-#pragma unroll
-                            for (int dt = 0; dt < Tile::DT; ++dt) {
-                                const uint32_t c = *reinterpret_cast<const uint32_t*>(src + dt * 16);
-                                const auto lo = __builtin_amdgcn_cvt_scalef32_pk_f32_fp8(c, vp, false), hi = __builtin_amdgcn_cvt_scalef32_pk_f32_fp8(c, vp, true);
-                                t.o[dt][0] += wk * lo[0];
-                                t.o[dt][1] += wk * lo[1];
-                                t.o[dt][2] += wk * hi[0];
-                                t.o[dt][3] += wk * hi[1];
-                            }
-                        }
-                    }
+                const unsigned long long lanes = __ballot(odd);
+                if (lanes) {
+                    const unsigned keys = (unsigned)(lanes | lanes >> 16 | lanes >> 32 | lanes >> 48) & 0xffffu;
+                    if (keys & ((1u << max(seen[h], 0)) - 1u)) t.l = NAN;
                 }
-                continue;
             }
         }
         bf16_terms<NP>(w, pw);
 #pragma unroll
         for (int h = 0; h < 2; ++h)
 #pragma unroll
-            for (int j = 0; j < KS; ++j) {
-                const uint4 c = vx[h][j / 2];
-                *(LdsB128)(tile_lds + Tile::v_piece(l16 + 16 * h, qr * KS + j)) = kv8_to_bf16(j % 2 ? make_uint2(c.z, c.w) : make_uint2(c.x, c.y), vp);
-            }
-        t.template add_values<1>(pw, 0, tile_lds);
+            for (int j = 0; j < KS; ++j) *(LdsB128)((v_to ^ ((j / 2 * 8 + j % 2) << 4)) + h * (16 * D * 2)) = kv8_to_bf16(half_of(vx[h][j / 2], j), vp[h]);
+        __builtin_amdgcn_sched_barrier(0);
+        load_v();
+        __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+        for (int dt = 0; dt < Tile::DT; ++dt) t.template add_channels<1>(pw, 0, dt, v_from ^ (dt << 5));
     }
 
-    const int first = part_at * a.Hkv + (tile * a.Hkv + g) * stretches, mine = first + stretch;
-    if (stretch == 0 && threadIdx.x < rows) {
-        const int i = row0 + threadIdx.x, n = i / G;
-        a.where[(size_t)(me.lo + n) * a.Hq + g * G + i - n * G] = make_int2(first, stretches * kTileRows + threadIdx.x);
-    }
-    merge_waves<T, D, NW>(t, lds, rows, [&](int i, int dd, float acc, float l, float M) {
-        if (stretches == 1) {
-            const int x = row0 + i, n = x / G;
-            Elem<T>::st(out + (size_t)(me.lo + n) * a.ldo + (size_t)(g * G + x - n * G) * D + dd, l == 0.f ? 0.f : acc / l);
-        } else if (mine < kBatchParts) {
-            float* dst = a.part + ((size_t)mine * kTileRows + i) * (D + 2);
-            dst[dd] = acc;
-            if (dd == 0) { dst[D] = M; dst[D + 1] = l; }
+    const bool whole_tile = from == 0 && take >= pieces;
+    if (from < pieces || whole_tile) {                // (else nothing but the tile's end is left in this share)
+        if (from == 0 && tid < rows) {
+            const int i = row0 + tid, n = i / G;
+            const long long to = begin + share - left_over + pieces - 1;      // (what the share has taken so far is share - left_over, but for the last one, which ends with its tile)
+            const int n_shares = whole_tile ? 1 : (int)(to / share) - share_of + 1;
+            a.where[(size_t)(me.lo + n) * a.Hq + g * G + i - n * G] = make_int2(blockIdx.x, n_shares * kTileRows + tid);
         }
-    });
+        float* part = a.part + (size_t)(blockIdx.x * 2 + (from == 0)) * kTileRows * (D + 2);
+        merge_waves<T, D, NW>(t, lds, rows, [&](int i, int dd, float acc, float l, float M) {
+            if (whole_tile) {
+                const int x = row0 + i, n = x / G;
+                Elem<T>::st(out + (size_t)(me.lo + n) * a.ldo + (size_t)(g * G + x - n * G) * D + dd, l == 0.f ? 0.f : acc / l);
+            } else {
+                float* dst = part + i * (D + 2);
+                dst[dd] = acc;
+                if (dd == 0) { dst[D] = M; dst[D + 1] = l; }
+            }
+        }, tid);
+        __syncthreads();                                 // the waves' tiles are read before they are written again
+    }
+    left_over -= take;
+    if (left_over <= 0) return;
+    from = 0;
+    if (++tile == me.tiles(a)) {
+        tile = 0;
+        unsigned long long more_rows = __ballot(x.n > 0) & ~((2ull << i_req) - 1);
+        while (!more_rows) {
+            r0 += 64;
+            if (r0 >= a.R) return;
+            x = batch_request(a, r0 + lane_in);
+            more_rows = __ballot(x.n > 0);
+        }
+        i_req = __builtin_ctzll(more_rows);
+    }
+    }
 }
 
 // The partial results of a row (t, h), merged: a group of D / 4 lanes takes one in NG of them, four channels a lane.
@@ -524,22 +607,42 @@ __global__ void __launch_bounds__(256) batch_merge_kernel(T* __restrict__ out, B
         first = at.x;
         n = at.y / kTileRows;
         i = at.y % kTileRows;
-        if (n <= 1 || i < 0 || first < 0 || n > kBatchParts || first > kBatchParts - n) n = 0;
+        if (n <= 1 || i < 0 || first < 0 || first + (long long)(n - 1) * a.Hkv >= kBatchGrid) n = 0;
     }
-    const float* p = a.part + ((size_t)first * kTileRows + i) * (D + 2);
-    constexpr size_t kApart = (size_t)kTileRows * (D + 2);
+    const float* p = a.part + ((size_t)first * 2 * kTileRows + i) * (D + 2);
+    constexpr size_t kPart = (size_t)kTileRows * (D + 2);
     float M = -INFINITY, l = 0.f, o[4] = {0.f, 0.f, 0.f, 0.f};
-    for (int y = grp; y < n; y += NG) {
-        const float* s = p + y * kApart;
-        const float2 st = *reinterpret_cast<const float2*>(s + D), v0 = *reinterpret_cast<const float2*>(s + c * 4), v1 = *reinterpret_cast<const float2*>(s + c * 4 + 2);
-        if (st.y == 0.f) continue;                       // a partial result without keys
-        const float now = fmaxf(M, st.x), al = l == 0.f ? 0.f : __builtin_amdgcn_exp2f(M - now), w = __builtin_amdgcn_exp2f(st.x - now);
-        l = l * al + w * st.y;
-        o[0] = o[0] * al + w * v0.x;
-        o[1] = o[1] * al + w * v0.y;
-        o[2] = o[2] * al + w * v1.x;
-        o[3] = o[3] * al + w * v1.y;
+    constexpr int kAtOnce = 8;                           // requested together
+    for (int y0 = grp; y0 < n; y0 += NG * kAtOnce) {
+        float2 st[kAtOnce], v0[kAtOnce], v1[kAtOnce];
+#pragma unroll
+        for (int b = 0; b < kAtOnce; ++b) {
+            const int y = min(y0 + b * NG, n - 1);       // the first one is what its share has left unfinished
+            const float* s = p + (y == 0 ? kPart : (size_t)y * a.Hkv * 2 * kPart);
+            st[b] = *reinterpret_cast<const float2*>(s + D);
+            v0[b] = *reinterpret_cast<const float2*>(s + c * 4);
+            v1[b] = *reinterpret_cast<const float2*>(s + c * 4 + 2);
+        }
+        float now = M;
+#pragma unroll
+        for (int b = 0; b < kAtOnce; ++b) {
+            if (y0 + b * NG >= n) st[b].y = 0.f;
+            if (st[b].y != 0.f) now = fmaxf(now, st[b].x);         // (a partial result without keys has no weight)
+        }
+        const float al = l == 0.f ? 0.f : __builtin_amdgcn_exp2f(M - now);
         M = now;
+        l *= al;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) o[e] *= al;
+#pragma unroll
+        for (int b = 0; b < kAtOnce; ++b) {
+            const float w = st[b].y == 0.f ? 0.f : __builtin_amdgcn_exp2f(st[b].x - M);
+            l += w * st[b].y;
+            o[0] += w * v0[b].x;
+            o[1] += w * v0[b].y;
+            o[2] += w * v1[b].x;
+            o[3] += w * v1[b].y;
+        }
     }
     if constexpr (NG > 1) {
         if (c == 0) { ms[grp][x] = M; ls[grp][x] = l; }
@@ -567,19 +670,26 @@ __global__ void __launch_bounds__(256) batch_merge_kernel(T* __restrict__ out, B
     for (int e = 0; e < 4; ++e) Elem<T>::st(dst + e, l == 0.f ? 0.f : o[e] / l);
 }
 
-static size_t batch_part_bytes(int d) { return (size_t)kBatchParts * kTileRows * (d + 2) * sizeof(float); }
+static size_t batch_part_bytes(int d) { return (size_t)kBatchGrid * 2 * kTileRows * (d + 2) * sizeof(float); }
 size_t batch_attn_kv8_workspace_bytes(int n_rows, int Hq, int d) { return align_up(batch_part_bytes(d), 256) + align_up((size_t)n_rows * Hq * sizeof(int2), 256); }
 
 template <typename T, int D>
 static int launch_batch_attn(const void* q, void* out, const BatchAttnArgs& a, hipStream_t st) {
-    const long long tiles = (long long)a.n_rows * (a.Hq / a.Hkv) / kTileRows + a.R;
-    const unsigned grid = (unsigned)(tiles * a.Hkv + kBatchTarget);
-    hipLaunchKernelGGL((batch_attn_kv8_kernel<T, D>), dim3(grid), dim3(64 * kBatchWaves), 0, st, (const T*)q, (T*)out, a);
+    const int shares = std::max(1, kBatchGrid / a.Hkv);
+    constexpr int NW = kBatchWaves, smem = NW * RowTile<T, D>::kLdsBytes;
+    if (smem >= 1 << 16) {
+        static std::once_flag once;
+        static hipError_t err = hipSuccess;
+        std::call_once(once, [&] { err = hipFuncSetAttribute((const void*)batch_attn_kv8_kernel<T, D, NW>, hipFuncAttributeMaxDynamicSharedMemorySize, smem); });
+        if (err != hipSuccess) return set_hip_error(err);
+    }
+    hipLaunchKernelGGL((batch_attn_kv8_kernel<T, D, NW>), dim3(shares * a.Hkv), dim3(64 * NW), smem, st, (const T*)q, (T*)out, a);
     const int rc = check_launch();
     if (rc) return rc;
+    if (shares == 1) return rc;                          // no tile is shared
     const long long rows = (long long)a.n_rows * a.Hq;
     constexpr int kOne = 256 / (D / 4);                  // rows of a workgroup without groups
-    if (tiles * a.Hkv >= kBatchTarget / 2)               // few partial results of a tile
+    if (rows >= kBatchGrid * 4)                          // few partial results of a tile
         hipLaunchKernelGGL((batch_merge_kernel<T, D, 1>), dim3((unsigned)((rows + kOne - 1) / kOne)), dim3(256), 0, st, (T*)out, a);
     else
         hipLaunchKernelGGL((batch_merge_kernel<T, D, kOne>), dim3((unsigned)rows), dim3(256), 0, st, (T*)out, a);
@@ -589,7 +699,7 @@ static int launch_batch_attn(const void* q, void* out, const BatchAttnArgs& a, h
 int launch_batch_attn_kv8(const void* q, int ldq, const int* row_start, const int* lens, const int* table, int R, int n_rows, int max_blocks, const void* pool, int n_slots, size_t slot_bytes,
                           size_t layer_offset, int block, int Hq, int Hkv, int d, float scale, int dtype, void* out, int ldo, void* workspace, hipStream_t st) {
     BatchAttnArgs a{row_start, lens, table, (const unsigned char*)pool, slot_bytes, layer_offset, (float*)workspace, (int2*)((char*)workspace + align_up(batch_part_bytes(d), 256)),
-                    scale * 1.4426950408889634f, R, max_blocks, n_slots, n_rows, block, (block + kTileKeys - 1) / kTileKeys, Hq, Hkv, ldq, ldo};
+                    scale * 1.4426950408889634f, R, max_blocks, n_slots, n_rows, block, (block + kPiece - 1) / kPiece, Hq, Hkv, ldq, ldo, Divide(block), Divide((block + kPiece - 1) / kPiece)};
     if (dtype == SLIM_BF16) return d == 64 ? launch_batch_attn<bf16_t, 64>(q, out, a, st) : launch_batch_attn<bf16_t, 128>(q, out, a, st);
     return d == 64 ? launch_batch_attn<float, 64>(q, out, a, st) : launch_batch_attn<float, 128>(q, out, a, st);
 }

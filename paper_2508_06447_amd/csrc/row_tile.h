@@ -92,10 +92,14 @@ template <typename T, int D> struct RowTile {
 
     __device__ __forceinline__ void begin(const T* q_row) {          // of row l16
         const int qr = (threadIdx.x & 63) >> 4;
+        begin(q_row, [&](int j) { return qr * (D / 4) + j * 8; });
+    }
+    // channel(j): the lane's eight channels of step j, in another order than the above.
+    template <typename F> __device__ __forceinline__ void begin(const T* q_row, F channel) {
 #pragma unroll
         for (int j = 0; j < KS; ++j) {
             bf16x8 t[NT];
-            row_terms<T, NT>(q_row + qr * (D / 4) + j * 8, t);
+            row_terms<T, NT>(q_row + channel(j), t);
 #pragma unroll
             for (int a = 0; a < NT; ++a) q[a][j] = t[a];
         }
@@ -149,21 +153,22 @@ template <typename T, int D> struct RowTile {
     template <int NV> __device__ __forceinline__ void add_values(const bf16x8* p, int a, unsigned lds_tile) {
         const int lane = threadIdx.x & 63, s16 = lane & 15, r = 4 * (lane >> 4) + (s16 >> 2);
 #pragma unroll
-        for (int dt = 0; dt < DT; ++dt) {
-            const unsigned at = lds_tile + v_piece(r, dt * 2 + ((s16 & 3) >> 1)) + (s16 & 1) * 8;
-            const bf16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4bf16((LdsB64)at);
-            const bf16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4bf16((LdsB64)(at + 16 * D * 2));
-            const bf16x8 v = __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
-            if constexpr (NT == 1) {
+        for (int dt = 0; dt < DT; ++dt) add_channels<NV>(p, a, dt, lds_tile + v_piece(r, dt * 2 + ((s16 & 3) >> 1)) + (s16 & 1) * 8);
+    }
+    // The same for channels 16 dt ..; at: where the lane reads them.
+    template <int NV> __device__ __forceinline__ void add_channels(const bf16x8* p, int a, int dt, unsigned at) {
+        const bf16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4bf16((LdsB64)at);
+        const bf16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4bf16((LdsB64)(at + 16 * D * 2));
+        const bf16x8 v = __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
+        if constexpr (NT == 1) {
 #pragma unroll
-                for (int b = NP - 1; b >= 0; --b) o[dt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(v, p[b], o[dt], 0, 0, 0);
-            } else {                                     // float32: the terms' sum is rounded into the running values once
-                f32x4 x = {0.f, 0.f, 0.f, 0.f};
+            for (int b = NP - 1; b >= 0; --b) o[dt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(v, p[b], o[dt], 0, 0, 0);
+        } else {                                         // float32: the terms' sum is rounded into the running values once
+            f32x4 x = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-                for (int b = NP - 1; b >= 0; --b)
-                    if (a + b < 3) x = __builtin_amdgcn_mfma_f32_16x16x32_bf16(v, p[b], x, 0, 0, 0);
-                o[dt] += x;
-            }
+            for (int b = NP - 1; b >= 0; --b)
+                if (a + b < 3) x = __builtin_amdgcn_mfma_f32_16x16x32_bf16(v, p[b], x, 0, 0, 0);
+            o[dt] += x;
         }
     }
     // What the weights of row l16 are relative to, in the base-2 domain.
@@ -177,18 +182,18 @@ template <typename T, int D> struct RowTile {
 
 // The results of a workgroup's NW waves for the same rows, merged: store(row, channel, values, sum, maximum) is called for the first `rows` of them.  lds: the waves' V tiles, which
 // hold 16 rows of D floats each as well (16-byte pieces turned by the row).
-template <typename T, int D, int NW, typename F> __device__ __forceinline__ void merge_waves(RowTile<T, D>& t, unsigned char* lds, int rows, F store) {
+template <typename T, int D, int NW, typename F> __device__ __forceinline__ void merge_waves(RowTile<T, D>& t, unsigned char* lds, int rows, F store, const int tid = threadIdx.x) {
     typedef RowTile<T, D> Tile;
     static_assert(Tile::kLdsBytes == kTileRows * D * 4, "O fits the V tile");
     __shared__ float ws_m[NW][kTileRows], ws_l[NW][kTileRows];
-    const int lane = threadIdx.x & 63, l16 = lane & 15, qr = lane >> 4, wave = threadIdx.x >> 6;
+    const int lane = tid & 63, l16 = lane & 15, qr = lane >> 4, wave = tid >> 6;
     t.finish_sum();
     if (lane < kTileRows) { ws_m[wave][lane] = t.reference(); ws_l[wave][lane] = t.l; }
     float* mine = reinterpret_cast<float*>(lds + wave * Tile::kLdsBytes);
 #pragma unroll
     for (int dt = 0; dt < Tile::DT; ++dt) *reinterpret_cast<f32x4*>(mine + l16 * D + (((dt * 4 + qr) ^ (l16 & (D / 4 - 1))) << 2)) = t.o[dt];
     __syncthreads();
-    for (int i = threadIdx.x; i < rows * D; i += 64 * NW) {
+    for (int i = tid; i < rows * D; i += 64 * NW) {
         const int r = i / D, dd = i % D;
         float M = -INFINITY, acc = 0.f, l = 0.f;
 #pragma unroll
