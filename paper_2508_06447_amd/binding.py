@@ -486,20 +486,42 @@ def slim_kv4_read(pool: torch.Tensor, block: int, n_tokens: int, slot_of_block: 
     return k_out, v_out
 
 
-# ---- a batch of requests, its cache in 8 bits
-def _here(name: str, *tensors):
-    """The tensors are on the current device, whose stream the call goes to."""
-    at = torch.cuda.current_device() if _device is None else _device()
-    for t in tensors:
-        if t is not None and t.is_cuda and t.get_device() != at:
-            raise ValueError(f"{name}: the tensors must be on the current device")
+# ---- a batch of requests, its cache in 8 bits.  (Every look at a tensor costs 0.06 to 0.1 us on the host, of the 3 to 6 that a call's launches take: each is asked for once.)
+def _current() -> int:
+    """The current device, whose stream a call goes to; without a GPU one that no tensor is on."""
+    if _device is not None:
+        return _device()
+    return torch.cuda.current_device() if torch.cuda.is_available() else -2
 
 
-def _counts(t: torch.Tensor, size: int, name: str):
-    """Address of an int32 tensor of `size` numbers on the GPU."""
-    if t.numel() != size:
-        raise ValueError(f"{name} must have {size} entries")
-    return _index(t, name)
+def _i32(t: torch.Tensor, size: int, at: int, name: str) -> int:
+    """Address of `size` dense int32 numbers on device `at`."""
+    if t.dtype is not torch.int32:
+        raise TypeError(f"{name} must be int32")
+    if t.get_device() != at:
+        raise ValueError(f"{name} must be a GPU tensor, on the current device")
+    if t.numel() != size or not t.is_contiguous():
+        raise ValueError(f"{name} must have {size} entries, contiguous")
+    return t.data_ptr()
+
+
+def _bytes(t: torch.Tensor, at: int, name: str):
+    """(address, slots, bytes of a slot) of pool[slots, ...] on device `at`, or in pinned host memory."""
+    if t.get_device() != at:
+        if t.is_cuda:
+            raise ValueError(f"{name} must be on the current device")
+        return _slots(t)
+    if not t.is_contiguous():
+        raise ValueError(f"{name} must be contiguous")
+    ns = t.shape[0]
+    return t.data_ptr(), ns, t.nbytes // ns if ns else 0
+
+
+def _pairs(k: torch.Tensor, v: torch.Tensor, at: int, names: str):
+    """_rows of two like tensors on device `at`."""
+    if k.get_device() != at or v.get_device() != at:
+        raise ValueError(f"{names} must be alike GPU tensors, on the current device")
+    return _rows(k, v, names)
 
 
 def slim_batch_map(lens: torch.Tensor, n_new: torch.Tensor, block: int, block_table: torch.Tensor, free_slots: torch.Tensor, n_slots: int, n_rows: int,
@@ -509,16 +531,26 @@ def slim_batch_map(lens: torch.Tensor, n_new: torch.Tensor, block: int, block_ta
     used[0] on, and are set in block_table[R, max_blocks], in place; n_slots: of the pool.  All int32 on the GPU.
     Returns (lens_out[R], row_start[R + 1], row_pos[n_rows], row_slot[n_rows], info[4]); info[3:4] is the next step's `used`."""
     lib = load_library()
-    R, dev = lens.numel(), lens.device
+    R, n_free, at = lens.numel(), free_slots.numel(), _current()
     if block_table.dim() != 2 or block_table.shape[0] != R:
         raise ValueError("block_table must be [requests, blocks]")
-    _here("slim_batch_map", lens, n_new, block_table, free_slots, used, lens_out, row_start, row_pos, row_slot, info)
-    new = lambda t, size: torch.empty(max(size, 0), dtype=torch.int32, device=dev) if t is None else t
-    lens_out, row_start, row_pos, row_slot, info = new(lens_out, R), new(row_start, R + 1), new(row_pos, n_rows), new(row_slot, n_rows), new(info, 4)
-    _check(lib.slim_batch_map(_index(lens, "lens"), _counts(n_new, R, "n_new"), R, block, _index(block_table, "block_table"), block_table.shape[1],
-                              _index(free_slots, "free_slots"), free_slots.numel(), None if used is None else _counts(used, 1, "used"), n_slots, n_rows,
-                              _counts(lens_out, R, "lens_out"), _counts(row_start, R + 1, "row_start"), _counts(row_pos, n_rows, "row_pos"),
-                              _counts(row_slot, n_rows, "row_slot"), _counts(info, 4, "info"), _stream()), "slim_batch_map")
+    wide = block_table.shape[1]
+    if lens_out is None:
+        lens_out = torch.empty(R, dtype=torch.int32, device=lens.device)
+    if row_start is None:
+        row_start = torch.empty(R + 1, dtype=torch.int32, device=lens.device)
+    if row_pos is None:
+        row_pos = torch.empty(max(n_rows, 0), dtype=torch.int32, device=lens.device)
+    if row_slot is None:
+        row_slot = torch.empty(max(n_rows, 0), dtype=torch.int32, device=lens.device)
+    if info is None:
+        info = torch.empty(4, dtype=torch.int32, device=lens.device)
+    code = lib.slim_batch_map(_i32(lens, R, at, "lens"), _i32(n_new, R, at, "n_new"), R, block, _i32(block_table, R * wide, at, "block_table"), wide,
+                              _i32(free_slots, n_free, at, "free_slots"), n_free, None if used is None else _i32(used, 1, at, "used"), n_slots, n_rows,
+                              _i32(lens_out, R, at, "lens_out"), _i32(row_start, R + 1, at, "row_start"), _i32(row_pos, max(n_rows, 0), at, "row_pos"),
+                              _i32(row_slot, max(n_rows, 0), at, "row_slot"), _i32(info, 4, at, "info"), _stream())
+    if code:
+        _check(code, "slim_batch_map")
     return lens_out, row_start, row_pos, row_slot, info
 
 
@@ -530,33 +562,39 @@ def kv8_block_bytes(block: int, n_kv_heads: int, head_dim: int) -> int:
 def slim_kv8_write(k: torch.Tensor, v: torch.Tensor, pool: torch.Tensor, block: int, row_slot: torch.Tensor, layer_offset: int = 0) -> torch.Tensor:
     """k, v[n, Hkv, d] (rows may be apart) -> the places row_slot[n] (int32; outside the pool: left out) of pool[slots, ...] in 8 bits.  The rows of a block follow each other.
     pool: on the GPU or pinned host memory.  Returns pool."""
-    lib = load_library()
-    n, Hkv, d, kp, vp, ldk, ldv = _rows(k, v, "k and v")
-    at, ns, size = _slots(pool)
-    _here("slim_kv8_write", k, v, pool, row_slot)
-    _check(lib.slim_kv8_write(kp, vp, ldk, ldv, _counts(row_slot, n, "row_slot"), n, Hkv, d, block, _dtype_code(k), at, ns, size, layer_offset, _stream()), "slim_kv8_write")
+    lib, here = load_library(), _current()
+    n, Hkv, d, kp, vp, ldk, ldv = _pairs(k, v, here, "k and v")
+    at, ns, size = _bytes(pool, here, "pool")
+    code = lib.slim_kv8_write(kp, vp, ldk, ldv, _i32(row_slot, n, here, "row_slot"), n, Hkv, d, block, _dtype_code(k), at, ns, size, layer_offset, _stream())
+    if code:
+        _check(code, "slim_kv8_write")
     return pool
 
 
 def slim_kv8_read(pool: torch.Tensor, block: int, n_tokens: int, slots: torch.Tensor | None = None, k_out: torch.Tensor | None = None, v_out: torch.Tensor | None = None,
                   n_kv_heads: int = 0, head_dim: int = 0, dtype: torch.dtype = torch.bfloat16, layer_offset: int = 0):
     """The n_tokens tokens of the blocks in slots[>= ceil(n_tokens / block)] (int32, e.g. a row of a block table; None: block b in slot b) -> (k, v)[n_tokens, Hkv, d].
-    Give n_kv_heads, head_dim and dtype, or k_out and v_out.  Rows of a block that is not in the pool: zero, or as k_out and v_out had them."""
-    lib = load_library()
-    if slots is not None and slots.numel() < n_blocks(n_tokens, block):
-        raise ValueError("slots is shorter than the tokens' blocks")
+    Give n_kv_heads, head_dim and dtype, or k_out and v_out, which may have more rows.  Rows of a block that is not in the pool: zero, or as k_out and v_out had them."""
+    lib, here = load_library(), _current()
+    nb = n_blocks(n_tokens, block)
+    where = None
+    if slots is not None:
+        n_list = slots.numel()
+        if n_list < nb:
+            raise ValueError("slots is shorter than the tokens' blocks")
+        where = _i32(slots, n_list, here, "slots")
     if (k_out is None) != (v_out is None):
         raise ValueError("k_out and v_out go together")
     if k_out is None:
-        whole = slots is None and pool.shape[0] >= n_blocks(n_tokens, block)
-        k_out, v_out = ((torch.empty if whole else torch.zeros)(max(n_tokens, 0), n_kv_heads, head_dim, dtype=dtype,
-                                                                device=pool.device if pool.is_cuda else torch.cuda.current_device()) for _ in range(2))
-    n, Hkv, d, kp, vp, ldk, ldv = _rows(k_out, v_out, "k_out and v_out")
+        whole = slots is None and pool.shape[0] >= nb
+        k_out, v_out = ((torch.empty if whole else torch.zeros)(max(n_tokens, 0), n_kv_heads, head_dim, dtype=dtype, device=here) for _ in range(2))
+    n, Hkv, d, kp, vp, ldk, ldv = _pairs(k_out, v_out, here, "k_out and v_out")
     if n < n_tokens:
         raise ValueError("k_out and v_out must hold the tokens")
-    at, ns, size = _slots(pool)
-    _here("slim_kv8_read", pool, slots, k_out, v_out)
-    _check(lib.slim_kv8_read(at, ns, size, layer_offset, _index(slots, "slots"), n_tokens, Hkv, d, block, _dtype_code(k_out), kp, vp, ldk, ldv, _stream()), "slim_kv8_read")
+    at, ns, size = _bytes(pool, here, "pool")
+    code = lib.slim_kv8_read(at, ns, size, layer_offset, where, n_tokens, Hkv, d, block, _dtype_code(k_out), kp, vp, ldk, ldv, _stream())
+    if code:
+        _check(code, "slim_kv8_read")
     return k_out, v_out
 
 
@@ -570,27 +608,29 @@ def slim_batch_attn_kv8(q: torch.Tensor, row_start: torch.Tensor, lens: torch.Te
     """q[n_rows, Hq, d] (rows may be apart): the rows of a step, row_start[R + 1] the first of each request, lens[R] the requests' tokens with them (slim_batch_map's lens_out).  Each
     row attends to its request's tokens up to itself whose blocks block_table[R, max_blocks] finds in pool[slots, ...] -> out[n_rows, Hq, d]; rows behind the last request: zero, or as
     out had them."""
-    lib = load_library()
+    lib, at = load_library(), _current()
     n, Hq, d = shape = q.shape
-    R = lens.numel()
+    R, dtype = lens.numel(), q.dtype
     if block_table.dim() != 2 or block_table.shape[0] != R:
         raise ValueError("block_table must be [requests, blocks]")
+    wide = block_table.shape[1]
     if out is None:
-        out = torch.zeros(shape, dtype=q.dtype, device=q.device)
-    elif out.shape != shape or out.dtype != q.dtype or not out.is_cuda:
-        raise ValueError("out must be like q")
-    if not q.is_cuda:
-        raise ValueError("q must be a GPU tensor")
+        out = torch.zeros(shape, dtype=dtype, device=q.device)
+    elif out.shape != shape or out.dtype != dtype or out.get_device() != at:
+        raise ValueError("out must be like q, on the current device")
+    if q.get_device() != at:
+        raise ValueError("q must be a GPU tensor, on the current device")
     if workspace is None:
         need = lib.slim_batch_attn_kv8_workspace_bytes(n, R, Hq, n_kv_heads, d)
         workspace = torch.empty(max(need, 256), dtype=torch.uint8, device=q.device)
-    _here("slim_batch_attn_kv8", q, row_start, lens, block_table, pool, out, workspace)
-    ns = pool.shape[0]
-    code = lib.slim_batch_attn_kv8(q.data_ptr(), Hq * d if q.is_contiguous() else _row_stride(q, "q"), _counts(row_start, R + 1, "row_start"), _index(lens, "lens"),
-                                   _index(block_table, "block_table"), R, n, block_table.shape[1], _dev(pool, "pool"), ns,
-                                   pool.numel() // ns * pool.element_size() if ns else 0, layer_offset, block, Hq, n_kv_heads, d, softmax_scale, _dtype_code(q),
-                                   out.data_ptr(), Hq * d if out.is_contiguous() else _row_stride(out, "out"), _dev(workspace, "workspace"),
-                                   workspace.numel() * workspace.element_size(), _stream())
+    elif workspace.get_device() != at or not workspace.is_contiguous():
+        raise ValueError("workspace must be contiguous, on the current device")
+    if pool.get_device() != at:
+        raise ValueError("pool must be a GPU tensor, on the current device")
+    slots, ns, size = _bytes(pool, at, "pool")
+    code = lib.slim_batch_attn_kv8(q.data_ptr(), Hq * d if q.is_contiguous() else _row_stride(q, "q"), _i32(row_start, R + 1, at, "row_start"), _i32(lens, R, at, "lens"),
+                                   _i32(block_table, R * wide, at, "block_table"), R, n, wide, slots, ns, size, layer_offset, block, Hq, n_kv_heads, d, softmax_scale,
+                                   _dtype_code(q), out.data_ptr(), Hq * d if out.is_contiguous() else _row_stride(out, "out"), workspace.data_ptr(), workspace.nbytes, _stream())
     if code:
         _check(code, "slim_batch_attn_kv8")
     return out

@@ -50,32 +50,80 @@ __device__ __forceinline__ uint32_t kv8_codes(const float* f, float power) {
 }
 
 // ---- written
-// A run is a stretch of rows whose places follow each other in one block.  A workgroup takes the runs that begin within its `chunk` rows of the map, for one kv head, Keys or Values: the run's
-// largest magnitude, the exponent, the codes.  Where rows in front of the run are in the block already, the larger exponent of both holds, and where it grows they are rounded again.
-constexpr int kKv8Keep = 4;                              // passes over a run's rows that stay in registers
+// A run is a stretch of rows whose places follow each other in one block; its largest magnitude gives the exponent, and with it the codes.  Where rows in front of the run are in the block
+// already, the larger exponent of both holds, and where it grows they are rounded again.
+// A workgroup takes the runs that begin within its `chunk` rows of the map, for Keys or Values of `heads` kv heads.  A run of more than kKv8Short rows is the whole workgroup's, head by head:
+// its rows stay in registers, up to kKv8Keep passes of them, and the next head's are on their way.  Shorter ones, the new tokens of a step, are a wave's, for as many heads as it has
+// rows' lanes for (64 / (D / 8)).  Rows, old exponent and the run's length are requested together: two trips to memory.
+constexpr int kKv8Keep = 4, kKv8Short = 8;
 struct Kv8Write {
     const int* row_slot;
     unsigned char* pool;
     size_t slot_bytes, layer_offset;
-    int n_rows, n_places, block, Hkv, ldk, ldv, chunk;   // n_places: of the pool, n_slots * block
+    int n_rows, n_places, block, Hkv, ldk, ldv, chunk, heads;      // n_places: of the pool, n_slots * block; heads: of a workgroup, a divisor of 64 / (D / 8)
+    Divide by_block;
 };
+
+// Largest finite magnitude (magnitudes compare alike as whole numbers).
+__device__ __forceinline__ uint32_t largest(const float* f, uint32_t m) {
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+        const uint32_t x = __builtin_bit_cast(uint32_t, f[i]) & 0x7fffffffu;
+        m = max(m, x >= 0x7f800000u ? 0u : x);
+    }
+    return m;
+}
+// e + 127 for the largest magnitude m: from just above 1.75 times a power of two on it counts as the next power.
+__device__ __forceinline__ uint32_t exponent_byte(uint32_t m) { return (uint32_t)min(max((int)((m + 0x1fffffu) >> 23) - 8, kKv8ByteLow), kKv8ByteHigh); }
+// Eight floats -> their codes.
+__device__ __forceinline__ uint2 kv8_eight(const float* f, float power) {
+    uint2 code = make_uint2(kv8_codes(f, power), kv8_codes(f + 4, power));
+    bool odd = false;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) odd |= !(fabsf(f[i]) < INFINITY);
+    if (odd) {
+#pragma unroll
+        for (int i = 0; i < 8; ++i)
+            if (!(fabsf(f[i]) < INFINITY)) {
+                uint32_t& w = i < 4 ? code.x : code.y;
+                w = (w & ~(0xffu << (i % 4 * 8))) | kKv8NaN << (i % 4 * 8);
+            }
+    }
+    return code;
+}
+// `bytes` codes, a multiple of 8, rounded again relative to a power that is 2^by times as large; by thread tid of n.
+__device__ __forceinline__ void kv8_round_again(unsigned char* codes, size_t bytes, uint32_t by, int tid, int n) {
+    const float up = kv8_power(127 - min(by, 100u));     // (a hundred and more: nothing is left but zeros)
+    for (size_t i = (size_t)tid * 8; i < bytes; i += (size_t)n * 8) {
+        uint2 c = *reinterpret_cast<const uint2*>(codes + i);
+#pragma unroll
+        for (int x = 0; x < 2; ++x) {
+            uint32_t& w = x ? c.y : c.x;
+            const auto lo = __builtin_amdgcn_cvt_scalef32_pk_f32_fp8(w, up, false), hi = __builtin_amdgcn_cvt_scalef32_pk_f32_fp8(w, up, true);
+            const float f[4] = {lo[0], lo[1], hi[0], hi[1]};
+            uint32_t now = kv8_codes(f, 1.f);
+#pragma unroll
+            for (int y = 0; y < 4; ++y)
+                if ((w >> (8 * y) & 0x7fu) == kKv8NaN) now = (now & ~(0xffu << (8 * y))) | kKv8NaN << (8 * y);
+            w = now;
+        }
+        *reinterpret_cast<uint2*>(codes + i) = c;
+    }
+}
 
 template <typename T, int D>
 __global__ void __launch_bounds__(256) kv8_write_kernel(const T* __restrict__ K, const T* __restrict__ V, Kv8Write a) {
-    constexpr int PC = D / 8, RPP = 256 / PC, NV = sizeof(T) / 2;      // lanes a row, rows a pass, 16-byte loads a lane
+    constexpr int PC = D / 8, RPP = 256 / PC, HEADS = 64 / PC, NV = sizeof(T) / 2;      // lanes a row, rows a pass, heads of a wave, 16-byte loads a lane
     __shared__ uint32_t most_of[2][4];
-    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, piece = tid % PC, row = tid / PC;
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), piece = tid % PC, row = tid / PC;
     const bool value = blockIdx.z;
-    const int g = blockIdx.y;
-    const T* src = (value ? V : K) + (size_t)g * D + piece * 8;
+    const T* src = (value ? V : K) + piece * 8;
     const size_t ld = value ? a.ldv : a.ldk;
-    const Kv8Head at(g, a.block, a.Hkv, D);
     auto place_of = [&](long long t) {                   // of row t, -1: none
         const int p = t >= 0 && t < a.n_rows ? a.row_slot[t] : -1;
         return p >= 0 && p < a.n_places ? p : -1;
     };
-    auto load = [&](int t, uint4* c) {
-        const T* p = src + (size_t)t * ld;
+    auto load = [&](const T* p, uint4* c) {
         c[0] = load_stream16(p);
         if constexpr (NV == 2) c[1] = load_stream16(p + 4);
     };
@@ -83,120 +131,157 @@ __global__ void __launch_bounds__(256) kv8_write_kernel(const T* __restrict__ K,
         Elem<T>::unpack(c[0], f);
         if constexpr (NV == 2) Elem<T>::unpack(c[1], f + 4);
     };
-    // largest finite magnitude (as whole numbers magnitudes compare alike)
-    auto most = [&](const float* f, uint32_t m) {
-#pragma unroll
-        for (int i = 0; i < 8; ++i) {
-            const uint32_t x = __builtin_bit_cast(uint32_t, f[i]) & 0x7fffffffu;
-            m = max(m, x >= 0x7f800000u ? 0u : x);
-        }
-        return m;
-    };
+    auto old_byte = [&](const unsigned char* p, int r0) { return r0 > 0 ? (uint32_t)min(max((int)*p, kKv8ByteLow), kKv8ByteHigh) : (uint32_t)kKv8ByteLow; };
 
     const long long first = (long long)blockIdx.x * a.chunk;
-    unsigned long long starts;
+    unsigned long long shorts, longs;
+    int place = -1;
     {
-        const int p = lane < a.chunk ? place_of(first + lane) : -1;
-        starts = __ballot(p >= 0 && (p % a.block == 0 || place_of(first + lane - 1) != p - 1));
+        bool start = false, is_long = false;
+        if (lane < a.chunk) {
+            place = place_of(first + lane);
+            const int before = place_of(first + lane - 1), far = place_of(first + lane + kKv8Short);
+            if (place >= 0) {
+                const int r = place - a.by_block(place) * a.block;
+                start = r == 0 || before != place - 1;
+                is_long = start && r < a.block - kKv8Short && far == place + kKv8Short;
+            }
+        }
+        shorts = __ballot(start && !is_long);
+        longs = __ballot(is_long);
     }
-    int turn = 0;
-    while (starts) {
-        const int t0 = (int)(first + __builtin_ctzll(starts));
-        starts &= starts - 1;
-        const int p0 = place_of(t0), slot = p0 / a.block, r0 = p0 - slot * a.block, longest = a.block - r0;
-        int n = 1;                                       // rows of the run
+
+    const int g0 = blockIdx.y * a.heads, g1 = min(g0 + a.heads, a.Hkv);
+    if (g0 % HEADS != 0) shorts = 0;
+    const int g_short = min(g0 + lane / PC, a.Hkv - 1);
+    const bool mine = g0 + lane / PC < a.Hkv;            // (lanes without a head do as the last one's, but write nothing)
+    const Kv8Head at(g_short, a.block, a.Hkv, D);
+    for (int number = 0; shorts; ++number) {
+        const int i0 = __builtin_ctzll(shorts);
+        shorts &= shorts - 1;
+        if (number % 4 != wave) continue;
+        const int p0 = __builtin_amdgcn_readlane(place, i0), slot = a.by_block(p0), r0 = p0 - slot * a.block;
+        const long long t0 = first + i0;
+        const int longest = (int)min((long long)min(kKv8Short, a.block - r0), a.n_rows - t0);
+        uint4 c[kKv8Short][NV];
+#pragma unroll
+        for (int i = 0; i < kKv8Short; ++i)
+            load(src + (size_t)g_short * D + (size_t)(t0 + min(i, longest - 1)) * ld, c[i]);
+        unsigned char* base = a.pool + (size_t)slot * a.slot_bytes + a.layer_offset;
+        unsigned char* codes = base + (value ? at.v : at.k);
+        unsigned char* exponent = base + at.e + (value ? 1 : 0);
+        const uint32_t before = old_byte(exponent, r0);
+        const int n = __builtin_ctzll(~__ballot(lane < longest && place_of(t0 + lane) == p0 + lane));      // rows of the run
+        uint32_t m = 0;
+#pragma unroll
+        for (int i = 0; i < kKv8Short; ++i) {
+            float f[8];
+            unpack(c[i], f);
+            const uint32_t now = largest(f, m);
+            m = i < n ? now : m;
+        }
+#pragma unroll
+        for (int o = 1; o < PC; o <<= 1) m = max(m, (uint32_t)__shfl_xor((int)m, o, 64));
+        const uint32_t byte = max(before, exponent_byte(m));
+        const float power = kv8_power(byte);
+        if (mine) {
+#pragma unroll
+            for (int i = 0; i < kKv8Short; ++i)
+                if (i < n) {
+                    float f[8];
+                    unpack(c[i], f);
+                    *reinterpret_cast<uint2*>(codes + (size_t)(r0 + i) * D + piece * 8) = kv8_eight(f, power);
+                }
+            if (piece == 0) *exponent = (unsigned char)byte;
+        }
+        unsigned long long grown = r0 > 0 ? __ballot(mine && piece == 0 && byte > before) : 0;
+        while (grown) {
+            const int x = __builtin_ctzll(grown);
+            grown &= grown - 1;
+            const Kv8Head there(g0 + x / PC, a.block, a.Hkv, D);
+            kv8_round_again(base + (value ? there.v : there.k), (size_t)r0 * D, (uint32_t)__builtin_amdgcn_readlane((int)(byte - before), x), lane, 64);
+        }
+    }
+
+    for (int turn = 0; longs;) {
+        const int i0 = __builtin_ctzll(longs);
+        longs &= longs - 1;
+        const int p0 = __builtin_amdgcn_readlane(place, i0), slot = a.by_block(p0), r0 = p0 - slot * a.block;
+        const long long t0 = first + i0;
+        const int longest = (int)min((long long)a.block - r0, a.n_rows - t0);
+        unsigned char* base = a.pool + (size_t)slot * a.slot_bytes + a.layer_offset;
+        uint4 keep[kKv8Keep][NV];
+        uint32_t before;
+        auto request = [&](int g) {                      // a head's rows (the last one again where the block has no more) and exponent
+            const T* rows = src + (size_t)g * D;
+#pragma unroll
+            for (int i = 0; i < kKv8Keep; ++i) load(rows + (size_t)(t0 + min(i * RPP + row, longest - 1)) * ld, keep[i]);
+            before = old_byte(base + Kv8Head(g, a.block, a.Hkv, D).e + (value ? 1 : 0), r0);
+        };
+        request(g0);
+        int n = 0;                                       // rows of the run
         while (n < longest) {
-            const bool same = n + lane < longest && place_of((long long)t0 + n + lane) == p0 + n + lane;
+            const bool same = n + lane < longest && place_of(t0 + n + lane) == p0 + n + lane;
             const unsigned long long end = ~__ballot(same);
             n += end ? __builtin_ctzll(end) : 64;
             if (end) break;
         }
-        unsigned char* base = a.pool + (size_t)slot * a.slot_bytes + a.layer_offset;
-        unsigned char* codes = base + (value ? at.v : at.k);
-        unsigned char* exponent = base + at.e + (value ? 1 : 0);
-        uint4 keep[kKv8Keep][NV];
-        uint32_t m = 0;
+        for (int g = g0; g < g1; ++g, ++turn) {
+            const T* rows = src + (size_t)g * D;
+            const Kv8Head at(g, a.block, a.Hkv, D);
+            unsigned char* codes = base + (value ? at.v : at.k);
+            uint32_t m = 0;
 #pragma unroll
-        for (int i = 0; i < kKv8Keep; ++i) load(t0 + min(n - 1, i * RPP + row), keep[i]);      // rows behind the run repeat its last
-        const uint32_t before = r0 > 0 ? min(max((int)*exponent, kKv8ByteLow), kKv8ByteHigh) : kKv8ByteLow;
-#pragma unroll
-        for (int i = 0; i < kKv8Keep; ++i) {
-            float f[8];
-            unpack(keep[i], f);
-            m = most(f, m);
-        }
-        for (int i = kKv8Keep * RPP + row; i < n; i += RPP) {
-            uint4 c[NV];
-            float f[8];
-            load(t0 + i, c);
-            unpack(c, f);
-            m = most(f, m);
-        }
-#pragma unroll
-        for (int o = 32; o > 0; o >>= 1) m = max(m, (uint32_t)__shfl_xor((int)m, o, 64));
-        if (lane == 0) most_of[turn & 1][wave] = m;
-        __syncthreads();
-#pragma unroll
-        for (int w = 0; w < 4; ++w) m = max(m, most_of[turn & 1][w]);
-        ++turn;
-        // a magnitude from just above 1.75 times a power of two on counts as the next power
-        const uint32_t byte = max(before, (uint32_t)min(max((int)((m + 0x1fffffu) >> 23) - 8, kKv8ByteLow), kKv8ByteHigh));
-        const float power = kv8_power(byte);
-        auto store = [&](int i, const uint4* c) {
-            float f[8];
-            unpack(c, f);
-            uint2 code;
-            bool odd = false;
-#pragma unroll
-            for (int x = 0; x < 8; ++x) odd |= !(fabsf(f[x]) < INFINITY);
-            code.x = kv8_codes(f, power);
-            code.y = kv8_codes(f + 4, power);
-            if (odd) {
-#pragma unroll
-                for (int x = 0; x < 8; ++x)
-                    if (!(fabsf(f[x]) < INFINITY)) {
-                        uint32_t& w = x < 4 ? code.x : code.y;
-                        w = (w & ~(0xffu << (x % 4 * 8))) | kKv8NaN << (x % 4 * 8);
-                    }
+            for (int i = 0; i < kKv8Keep; ++i) {
+                float f[8];
+                unpack(keep[i], f);
+                const uint32_t now = largest(f, m);
+                m = i * RPP + row < n ? now : m;
             }
-            *reinterpret_cast<uint2*>(codes + (size_t)(r0 + i) * D + piece * 8) = code;
-        };
-#pragma unroll
-        for (int i = 0; i < kKv8Keep; ++i)
-            if (i * RPP + row < n) store(i * RPP + row, keep[i]);
-        for (int i = kKv8Keep * RPP + row; i < n; i += RPP) {
-            uint4 c[NV];
-            load(t0 + i, c);
-            store(i, c);
-        }
-        if (r0 > 0 && byte > before) {                   // the rows in front, relative to the larger power
-            const float up = kv8_power(127 - min(byte - before, 100u));      // (a hundred and more: nothing is left but zeros)
-            for (size_t i = (size_t)tid * 8; i < (size_t)r0 * D; i += 256 * 8) {
-                uint2 c = *reinterpret_cast<const uint2*>(codes + i);
-#pragma unroll
-                for (int x = 0; x < 2; ++x) {
-                    uint32_t& w = x ? c.y : c.x;
-                    const auto lo = __builtin_amdgcn_cvt_scalef32_pk_f32_fp8(w, up, false), hi = __builtin_amdgcn_cvt_scalef32_pk_f32_fp8(w, up, true);
-                    const float f[4] = {lo[0], lo[1], hi[0], hi[1]};
-                    uint32_t now = kv8_codes(f, 1.f);
-#pragma unroll
-                    for (int y = 0; y < 4; ++y)
-                        if ((w >> (8 * y) & 0x7fu) == kKv8NaN) now = (now & ~(0xffu << (8 * y))) | kKv8NaN << (8 * y);
-                    w = now;
-                }
-                *reinterpret_cast<uint2*>(codes + i) = c;
+            for (int i = kKv8Keep * RPP + row; i < n; i += RPP) {
+                uint4 c[NV];
+                float f[8];
+                load(rows + (size_t)(t0 + i) * ld, c);
+                unpack(c, f);
+                m = largest(f, m);
             }
+#pragma unroll
+            for (int o = 32; o > 0; o >>= 1) m = max(m, (uint32_t)__shfl_xor((int)m, o, 64));
+            if (lane == 0) most_of[turn & 1][wave] = m;
+            __syncthreads();
+#pragma unroll
+            for (int w = 0; w < 4; ++w) m = max(m, most_of[turn & 1][w]);
+            const uint32_t was = before, byte = max(was, exponent_byte(m));
+            const float power = kv8_power(byte);
+            auto eight = [&](const uint4* c) {
+                float f[8];
+                unpack(c, f);
+                return kv8_eight(f, power);
+            };
+            uint2 code[kKv8Keep];
+#pragma unroll
+            for (int i = 0; i < kKv8Keep; ++i) code[i] = eight(keep[i]);
+            if (g + 1 < g1) request(g + 1);              // on its way while this head's codes are written
+#pragma unroll
+            for (int i = 0; i < kKv8Keep; ++i)
+                if (i * RPP + row < n) *reinterpret_cast<uint2*>(codes + (size_t)(r0 + i * RPP + row) * D + piece * 8) = code[i];
+            for (int i = kKv8Keep * RPP + row; i < n; i += RPP) {
+                uint4 c[NV];
+                load(rows + (size_t)(t0 + i) * ld, c);
+                *reinterpret_cast<uint2*>(codes + (size_t)(r0 + i) * D + piece * 8) = eight(c);
+            }
+            if (byte > was && r0 > 0) kv8_round_again(codes, (size_t)r0 * D, byte - was, tid, 256);
+            if (tid == 0) base[at.e + (value ? 1 : 0)] = (unsigned char)byte;
         }
-        if (tid == 0) *exponent = (unsigned char)byte;
     }
 }
 
 int launch_kv8_write(const void* k, const void* v, int ldk, int ldv, const int* row_slot, int n_rows, int Hkv, int d, int block, int dtype, void* pool, int n_slots, size_t slot_bytes,
                      size_t layer_offset, hipStream_t st) {
-    const long long wanted = (long long)n_rows * Hkv * 2 / 4096;
-    const int chunk = (int)std::min<long long>(64, std::max<long long>(1, wanted));
-    const Kv8Write a{row_slot, (unsigned char*)pool, slot_bytes, layer_offset, n_rows, n_slots * block, block, Hkv, ldk, ldv, chunk};
-    const dim3 grid((n_rows - 1) / chunk + 1, Hkv, 2);
+    const int chunk = (int)std::min<long long>(64, std::max<long long>(4, (long long)n_rows * Hkv * 2 / 4096));
+    const int heads = 4;
+    const Kv8Write a{row_slot, (unsigned char*)pool, slot_bytes, layer_offset, n_rows, n_slots * block, block, Hkv, ldk, ldv, chunk, heads, Divide(block)};
+    const dim3 grid((n_rows - 1) / chunk + 1, (Hkv - 1) / heads + 1, 2);
 #define SLIM_KV8(T, D) hipLaunchKernelGGL((kv8_write_kernel<T, D>), grid, dim3(256), 0, st, (const T*)k, (const T*)v, a)
     if (dtype == SLIM_BF16) { if (d == 64) SLIM_KV8(bf16_t, 64); else SLIM_KV8(bf16_t, 128); }
     else if (d == 64) SLIM_KV8(float, 64);
@@ -282,18 +367,6 @@ constexpr int kBatchWaves = 4;
 constexpr int kBatchGrid = 768;                          // workgroups: as many as run together
 constexpr int kBatchLeast = 4 * 2 * kBatchWaves;         // pieces of a share
 constexpr int kBatchTile = 8;                            // what beginning and ending a tile counts for, in pieces
-
-// n / d for 0 <= n < 2^31: (n M) >> (31 + s), 2^s >= d, M = floor(2^(31 + s) / d) + 1, so that 2^(31 + s) < M d <= 2^(31 + s) + 2^s.
-struct Divide {
-    uint32_t factor;
-    int shift;
-    explicit Divide(int d) {
-        shift = 31;
-        while ((1ll << (shift - 31)) < d) ++shift;
-        factor = (uint32_t)((1ull << shift) / (unsigned)d + 1);
-    }
-    __device__ __forceinline__ int operator()(int n) const { return (int)(((unsigned long long)(unsigned)n * factor) >> shift); }
-};
 
 struct BatchAttnArgs {
     const int *row_start, *lens, *table;
@@ -602,8 +675,8 @@ __global__ void __launch_bounds__(256) batch_merge_kernel(T* __restrict__ out, B
     const long long row = (long long)blockIdx.x * PER + x;
     const int t = (int)(row / a.Hq);
     int first = 0, n = 0, i = 0;
+    const int2 at = a.where[min(row, (long long)a.n_rows * a.Hq - 1)];
     if (t >= max(a.row_start[0], 0) && t < min(a.row_start[a.R], a.n_rows)) {
-        const int2 at = a.where[row];
         first = at.x;
         n = at.y / kTileRows;
         i = at.y % kTileRows;

@@ -216,7 +216,8 @@ def test_binding_refusals(slim):
     k = torch.zeros(16, 2, 64, dtype=BF16, device="cuda")
     pool = torch.zeros(1, slim.kv8_block_bytes(16, 2, 64), dtype=torch.uint8, device="cuda")
     places = i32(np.arange(16))
-    for bad in (lambda: slim.slim_kv8_write(k.transpose(0, 1), k.transpose(0, 1), pool, 16, places), lambda: slim.slim_kv8_write(k, k, pool, 16, places[:8]),
+    for bad in (lambda: slim.slim_kv8_write(k, k[:4], pool, 16, places), lambda: slim.slim_kv8_write(k, k.float(), pool, 16, places), lambda: slim.slim_kv8_write(k, k.cpu(), pool, 16, places),
+                lambda: slim.slim_kv8_write(k.transpose(0, 1), k.transpose(0, 1), pool, 16, places), lambda: slim.slim_kv8_write(k, k, pool, 16, places[:8]),
                 lambda: slim.slim_kv8_write(k, k, pool, 16, places.cpu()), lambda: slim.slim_kv8_write(k, k, pool.cpu(), 16, places),
                 lambda: slim.slim_kv8_read(pool, 16, 16, k_out=k[:8], v_out=k[:8]), lambda: slim.slim_kv8_read(pool, 16, 16, k_out=k),
                 lambda: slim.slim_kv8_read(pool, 16, 17, i32([0]), n_kv_heads=2, head_dim=64)):
