@@ -424,7 +424,7 @@ size_t slim_batch_attn_kv8_workspace_bytes(int n_rows, int n_requests, int n_q_h
     if (n_rows < 1 || n_requests < 1 || n_q_heads < 1 || n_kv_heads < 1 || n_q_heads % n_kv_heads != 0 || !kv8_heads_ok(n_kv_heads, head_dim) ||
         !batch_attn_ok(n_rows, n_requests, n_q_heads, n_kv_heads))
         return 0;
-    return batch_attn_kv8_workspace_bytes(n_rows, n_q_heads, head_dim);
+    return batch_attn_kv8_workspace_bytes(n_rows, n_q_heads, n_kv_heads, head_dim);
 }
 
 int slim_batch_attn_kv8(const void* q, int ldq, const int* row_start, const int* lens, const int* block_table, int n_requests, int n_rows, int max_blocks, const void* pool,

@@ -367,16 +367,19 @@ constexpr int kBatchWaves = 4;
 constexpr int kBatchGrid = 768;                          // workgroups: as many as run together
 constexpr int kBatchLeast = 4 * 2 * kBatchWaves;         // pieces of a share
 constexpr int kBatchTile = 8;                            // what beginning and ending a tile counts for, in pieces
+constexpr int kFewRows = 64, kManyRows = 256, kManyGrid = 256;      // rows of a request up to which tiles have 16 rows; rows of the tiles for more; their workgroups
+constexpr int kFewPartRows = kBatchGrid * 2 * kTileRows, kPartRows = kFewPartRows + kManyGrid * 2 * kManyRows;      // rows of partial results
 
 struct BatchAttnArgs {
     const int *row_start, *lens, *table;
     const unsigned char* pool;
     size_t slot_bytes, layer_offset;
-    float* part;                                         // [kBatchGrid][2][16][D + 2]: of the tile that a share begins within, and of the one that it leaves unfinished
-    int2* where;                                         // of row (t, h): the first share of its tile, their number * 16 + its row of the tile
+    float* part;                                         // rows of D + 4: values, maximum, sum; [shares][2][rows of a tile]: of the tile that a share begins within, and of the one that it leaves unfinished
+    int2* where;                                         // of row (t, h): its row of `part` in the share that begins its tile, and 2 * the number of shares + 1 for tiles of many rows
     float scale_log2e;
     int R, max_blocks, n_slots, n_rows, block, per_block, Hq, Hkv, ldq, ldo;      // per_block: pieces
-    Divide by_block, by_piece;                           // by block, by per_block
+    int few;                                             // requests of more rows (of a kv head) are left to the kernel for many
+    Divide by_block, by_piece, by_group;                 // by block, per_block, Hq / Hkv
 };
 
 struct BatchRequest {
@@ -388,6 +391,7 @@ struct BatchRequest {
         return whole * a.per_block + (len - whole * a.block + kPiece - 1) / kPiece;
     }
     __device__ __forceinline__ long long cost(const BatchAttnArgs& a) const { return (long long)tiles(a) * (pieces(a) + kBatchTile); }
+    __device__ __forceinline__ bool many(const BatchAttnArgs& a) const { return n > 0 && rows(a) > a.few; }
 };
 __device__ __forceinline__ BatchRequest batch_request(const BatchAttnArgs& a, int r) {
     BatchRequest x = {0, 0, 0};
@@ -427,9 +431,14 @@ __global__ void __launch_bounds__(64 * NW, sizeof(T) == 2 ? 3 : 2) batch_attn_kv
     const int g = blockIdx.x % a.Hkv, share_of = blockIdx.x / a.Hkv, shares = gridDim.x / a.Hkv;
     int r0 = 0;                                          // x: of request r0 + the lane
     const int lane_in = threadIdx.x & 63;
-    BatchRequest x = batch_request(a, lane_in);
+    auto request = [&](int r) {
+        BatchRequest x = batch_request(a, r);
+        if (x.many(a)) x.n = 0;
+        return x;
+    };
+    BatchRequest x = request(lane_in);
     long long total = x.cost(a);
-    for (int r = 64; r < a.R; r += 64) total += batch_request(a, r + lane_in).cost(a);
+    for (int r = 64; r < a.R; r += 64) total += request(r + lane_in).cost(a);
 #pragma unroll
     for (int o = 32; o > 0; o >>= 1) total += __shfl_xor(total, o, 64);
     total = wave_value(total, 0);                        // (in scalar registers, with all that follows from it)
@@ -449,7 +458,7 @@ __global__ void __launch_bounds__(64 * NW, sizeof(T) == 2 ? 3 : 2) batch_attn_kv
         at -= wave_value(end, 63);
         r0 += 64;
         if (r0 >= a.R) return;
-        x = batch_request(a, r0 + lane_in);
+        x = request(r0 + lane_in);
     }
     int tile, from;
     {
@@ -633,15 +642,15 @@ __global__ void __launch_bounds__(64 * NW, sizeof(T) == 2 ? 3 : 2) batch_attn_kv
             const int i = row0 + tid, n = i / G;
             const long long to = begin + share - left_over + pieces - 1;      // (what the share has taken so far is share - left_over, but for the last one, which ends with its tile)
             const int n_shares = whole_tile ? 1 : (int)(to / share) - share_of + 1;
-            a.where[(size_t)(me.lo + n) * a.Hq + g * G + i - n * G] = make_int2(blockIdx.x, n_shares * kTileRows + tid);
+            a.where[(size_t)(me.lo + n) * a.Hq + g * G + i - n * G] = make_int2((blockIdx.x * 2 + 1) * kTileRows + tid, 2 * n_shares);
         }
-        float* part = a.part + (size_t)(blockIdx.x * 2 + (from == 0)) * kTileRows * (D + 2);
+        float* part = a.part + (size_t)(blockIdx.x * 2 + (from == 0)) * kTileRows * (D + 4);
         merge_waves<T, D, NW>(t, lds, rows, [&](int i, int dd, float acc, float l, float M) {
             if (whole_tile) {
                 const int x = row0 + i, n = x / G;
                 Elem<T>::st(out + (size_t)(me.lo + n) * a.ldo + (size_t)(g * G + x - n * G) * D + dd, l == 0.f ? 0.f : acc / l);
             } else {
-                float* dst = part + i * (D + 2);
+                float* dst = part + i * (D + 4);
                 dst[dd] = acc;
                 if (dd == 0) { dst[D] = M; dst[D + 1] = l; }
             }
@@ -657,11 +666,389 @@ __global__ void __launch_bounds__(64 * NW, sizeof(T) == 2 ? 3 : 2) batch_attn_kv
         while (!more_rows) {
             r0 += 64;
             if (r0 >= a.R) return;
-            x = batch_request(a, r0 + lane_in);
+            x = request(r0 + lane_in);
             more_rows = __ballot(x.n > 0);
         }
         i_req = __builtin_ctzll(more_rows);
     }
+    }
+}
+
+// ---- requests of many rows (bfloat16)
+// Tiles of 256 rows, 64 a wave; the four waves turn 64 keys at a time into bfloat16 in LDS, once for all of them, and each forms, in 32x32x16 matrix instructions,
+//   S^T[key, row] = K . Q^T       32 keys of 32 rows; the lane (l32, h) = (lane % 32, lane / 32) is left scores of row l32: keys 8 i + 4 h + 0 .. 3, i < 4
+//   O^T[d, row]   = V^T . P^T     whose operand P^T is what the lane holds: V comes through the transposing read in the same order of keys
+// The two halves A and B of a wave's rows are half a turn apart, so that the exponentials of one always stand beside matrix instructions of the other:
+//   softmax A | scores of B, values of B before        softmax B | values of A, scores of A behind
+// which also use the same fragments of K and V right after each other: LDS is read once for both.
+// Three buffers of 64 keys: one is read, one is filled, one may still be read by a slower wave; a barrier each 64 keys.
+// A weight is one bfloat16 (off by 2^-9 of itself at most, as the output is in the end), and the sum is that of the unrounded ones.  The reference of a row's weights is the
+// largest score when it was set, and is set anew only when a score is more than 2^30 above it: float32 and bfloat16 have room for that on both sides, and the results need no rescaling
+// in nearly all turns.
+constexpr int kManyKeys = 64;
+template <int D> struct ManyTile {
+    static constexpr int kSide = kManyKeys * D * 2, kBuffer = 2 * kSide, kLdsBytes = 3 * kBuffer + 3 * 8;      // Keys or Values; both; three, and a bit for each key with a Value that is not a number
+    static constexpr int KS = D / 16, DT = D / 32, CH = D / 8;
+    __device__ static __forceinline__ unsigned piece(int r, int c) { return (unsigned)(r * (D * 2) + ((c ^ (r & (CH - 1))) << 4)); }
+};
+constexpr float kManyRoom = 30.f;
+
+struct ManyRows {                                        // half of a wave's rows: the lane's share of row l32
+    float mc, lim, l;                                    // reference in the base-2 domain, score above which it moves, sum
+};
+
+template <int D>
+__global__ void __launch_bounds__(256, 1) batch_attn_many_kernel(const bf16_t* __restrict__ q, bf16_t* __restrict__ out, BatchAttnArgs a) {
+    typedef ManyTile<D> Tile;
+    constexpr int KS = Tile::KS, DT = Tile::DT, PR = D / 16, KPP = 256 / PR, NPASS = kManyKeys / KPP;      // 16-byte pieces of a key's codes, keys a pass, passes
+    extern __shared__ __align__(16) unsigned char lds[];
+    const int G = a.Hq / a.Hkv, g = blockIdx.x % a.Hkv, share_of = blockIdx.x / a.Hkv, shares = gridDim.x / a.Hkv;
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), l32 = lane & 31, h = lane >> 5;
+    const unsigned lds0 = (unsigned)(uintptr_t)lds;
+
+    // What a tile costs: the tokens that its last row sees, and some for beginning and ending it, times G so that it is a whole number: each of a request's tiles kManyRows more.
+    constexpr int kManyTile = 256;
+    auto tiles_of = [&](const BatchRequest& x) { return (x.rows(a) + kManyRows - 1) / kManyRows; };
+    auto first_cost = [&](const BatchRequest& x) { return (long long)G * (max(x.len - x.n, 0) + kManyTile) + kManyRows; };
+    auto cost_to = [&](const BatchRequest& x, long long tiles) { return tiles * first_cost(x) + tiles * (tiles - 1) / 2 * kManyRows; };
+    auto request = [&](int r) {
+        BatchRequest x = batch_request(a, r);
+        if (!x.many(a)) x.n = 0;
+        return x;
+    };
+    int r0 = 0;
+    BatchRequest x = request(lane);
+    auto cost = [&](const BatchRequest& x) { return cost_to(x, tiles_of(x)); };
+    long long total = cost(x);
+    for (int r = 64; r < a.R; r += 64) total += cost(request(r + lane));
+#pragma unroll
+    for (int o = 32; o > 0; o >>= 1) total += __shfl_xor(total, o, 64);
+    total = wave_value(total, 0);
+    const long long share = max((long long)G * 1024, (total + shares - 1) / shares), begin = share * share_of;
+    long long left_over = min(total - begin, share);
+    if (left_over <= 0) return;
+    long long at = begin;
+    int i_req;
+    while (true) {
+        const long long mine = cost(x), end = wave_prefix(mine, lane);
+        const unsigned long long behind = __ballot(end > at);
+        if (behind) {
+            i_req = __builtin_ctzll(behind);
+            at -= wave_value(end - mine, i_req);
+            break;
+        }
+        at -= wave_value(end, 63);
+        r0 += 64;
+        if (r0 >= a.R) return;
+        x = request(r0 + lane);
+    }
+    BatchRequest me{wave_value(x.lo, i_req), wave_value(x.n, i_req), wave_value(x.len, i_req)};
+    int tile = 0;                                        // the one that position `at` lies in: the last one whose beginning is not behind it
+    for (int n = tiles_of(me); n > 1;) {
+        const int half = n >> 1;
+        if (cost_to(me, tile + half) <= at) tile += half;
+        n -= half;
+    }
+    long long from_cost = at - cost_to(me, tile);
+    const Kv8Head head(g, a.block, a.Hkv, D);
+
+    while (true) {
+        const long long tile_cost = first_cost(me) + (long long)tile * kManyRows, take = min(tile_cost - from_cost, left_over);
+        const int row0 = tile * kManyRows, rows = min(kManyRows, me.rows(a) - row0), before = me.len - me.n;
+        const int p0 = before + a.by_group(row0), limit = before + a.by_group(row0 + rows - 1) + 1;
+        const int* table = a.table + (size_t)(r0 + i_req) * a.max_blocks;
+        const int last = limit <= 0 ? 0 : a.by_block(limit - 1) * a.per_block + (limit - 1 - a.by_block(limit - 1) * a.block) / kPiece + 1;
+        auto piece_at = [&](long long c) { return c >= tile_cost ? last : (int)((double)last * ((double)c / (double)tile_cost)); };
+        const int u_begin = piece_at(from_cost), u_end = piece_at(from_cost + take);
+
+        // The pieces, four at a time, looked up 64 at once by every wave for itself.
+        int u = u_begin + lane, batch = u_begin - 64, u_slot = 0, u_pos = 0, u_rows = 0, next_slot = u < u_end ? table[a.by_piece(u)] : -1;
+        unsigned long long left = 0;
+        struct Keys { int have[4], pos[4], c0[4]; const unsigned char* base[4]; bool any; };
+        auto find = [&](Keys& k) {
+            while (!left) {
+                batch += 64;
+                if (batch >= u_end) {
+                    k.any = false;
+                    return;
+                }
+                const int b = a.by_piece(u), row = (u - b * a.per_block) * kPiece;
+                u_slot = next_slot;
+                u_pos = b * a.block + row;
+                u_rows = u < u_end && u_slot >= 0 && u_slot < a.n_slots ? min(kPiece, min(a.block - row, limit - u_pos)) : 0;
+                left = __ballot(u_rows > 0);
+                u += 64;
+                next_slot = u < u_end ? table[a.by_piece(u)] : -1;
+            }
+            k.any = true;
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                if (j > 0 && !left) {                    // fewer than four: the first one again, unseen
+                    k.have[j] = 0;
+                    k.pos[j] = k.pos[0];
+                    k.c0[j] = k.c0[0];
+                    k.base[j] = k.base[0];
+                    continue;
+                }
+                const int i = __builtin_ctzll(left);
+                left &= left - 1;
+                k.have[j] = __builtin_amdgcn_readlane(u_rows, i);
+                k.pos[j] = __builtin_amdgcn_readlane(u_pos, i);
+                k.c0[j] = k.pos[j] - a.by_block(k.pos[j]) * a.block;
+                k.base[j] = a.pool + (size_t)__builtin_amdgcn_readlane(u_slot, i) * a.slot_bytes + a.layer_offset;
+            }
+        };
+        auto is_whole = [&](const Keys& k) {
+            return k.have[0] == kPiece && k.have[1] == kPiece && k.have[2] == kPiece && k.have[3] == kPiece &&
+                   max(max(k.pos[0], k.pos[1]), max(k.pos[2], k.pos[3])) + kPiece - 1 <= p0;
+        };
+        // A thread's codes of the next 64 keys: 16 channels of key tid / PR, and of one 32 further on.
+        const int my_key = threadIdx.x / PR, my_piece = threadIdx.x % PR;
+        uint4 kx[NPASS], vx[NPASS];
+        uint32_t ex[NPASS];
+        auto load = [&](const Keys& k) {
+#pragma unroll
+            for (int s = 0; s < NPASS; ++s) {
+                const int j = NPASS == 1 ? wave : (wave >> 1) + 2 * s;      // the piece that the wave's keys lie in
+                const int have = j == 0 ? k.have[0] : j == 1 ? k.have[1] : j == 2 ? k.have[2] : k.have[3], c0 = j == 0 ? k.c0[0] : j == 1 ? k.c0[1] : j == 2 ? k.c0[2] : k.c0[3];
+                const unsigned char* base = j == 0 ? k.base[0] : j == 1 ? k.base[1] : j == 2 ? k.base[2] : k.base[3];
+                const unsigned off = min(my_key & 15, max(have, 1) - 1) * D + my_piece * 16;
+                kx[s] = *reinterpret_cast<const uint4*>(base + head.k + (size_t)c0 * D + off);
+                vx[s] = *reinterpret_cast<const uint4*>(base + head.v + (size_t)c0 * D + off);
+                ex[s] = *reinterpret_cast<const uint16_t*>(base + head.e);
+            }
+        };
+        auto fill = [&](int buffer, bool whole) {
+#pragma unroll
+            for (int s = 0; s < NPASS; ++s) {
+                const int key = my_key + s * KPP;
+                const float kp = kv8_power(ex[s] & 0xffu), vp = kv8_power(ex[s] >> 8);
+                const unsigned to = lds0 + buffer * Tile::kBuffer + Tile::piece(key, my_piece * 2);
+                uint4 v = vx[s];
+                if (!whole) {                            // (as for few rows)
+                    bool odd = false;
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) {
+                        uint32_t& x = i == 0 ? v.x : i == 1 ? v.y : i == 2 ? v.z : v.w;
+                        const uint32_t bytes = (((x & 0x7f7f7f7fu) + 0x01010101u) >> 7 & 0x01010101u) * 0xffu;
+                        odd |= bytes != 0;
+                        x &= ~bytes;
+                    }
+                    const unsigned long long lanes = __ballot(odd);
+                    unsigned bits = 0;                   // of the wave's 64 / PR keys
+#pragma unroll
+                    for (int i = 0; i < 64 / PR; ++i) bits |= (lanes >> (i * PR) & ((1ull << PR) - 1)) ? 1u << i : 0u;
+                    unsigned char* flags = lds + 3 * Tile::kBuffer + buffer * 8 + s * (KPP / 8);
+                    if (lane == 0) {
+                        if constexpr (PR == 8) flags[wave] = (unsigned char)bits;
+                        else *reinterpret_cast<uint16_t*>(flags + wave * 2) = (uint16_t)bits;
+                    }
+                }
+                *(LdsB128)(to) = kv8_to_bf16(make_uint2(kx[s].x, kx[s].y), kp);
+                *(LdsB128)(to ^ 16) = kv8_to_bf16(make_uint2(kx[s].z, kx[s].w), kp);
+                *(LdsB128)(to + Tile::kSide) = kv8_to_bf16(make_uint2(v.x, v.y), vp);
+                *(LdsB128)((to ^ 16) + Tile::kSide) = kv8_to_bf16(make_uint2(v.z, v.w), vp);
+            }
+        };
+
+        Keys now, next;
+        find(now);
+        if (now.any) load(now);
+        // Query fragments: the lane's row of either half, channels 16 c + 8 h ..
+        bf16x8 qf[2][KS];
+        int pos_of[2];                                   // of the lane's row
+#pragma unroll
+        for (int y = 0; y < 2; ++y) {
+            const int lrow = row0 + min(wave * 64 + y * 32 + l32, rows - 1), token = a.by_group(lrow);
+            pos_of[y] = before + token;
+            const bf16_t* src = q + (size_t)(me.lo + token) * a.ldq + (size_t)(g * G + lrow - token * G) * D + h * 8;
+#pragma unroll
+            for (int c = 0; c < KS; ++c) qf[y][c] = *reinterpret_cast<const bf16x8*>(src + c * 16);
+        }
+        f32x16 o[2][DT];
+        ManyRows st[2];
+#pragma unroll
+        for (int y = 0; y < 2; ++y) {
+            st[y] = ManyRows{0.f, -INFINITY, 0.f};
+#pragma unroll
+            for (int d = 0; d < DT; ++d)
+#pragma unroll
+                for (int i = 0; i < 16; ++i) o[y][d][i] = 0.f;
+        }
+        // Addresses of the lane in a buffer: K fragments (key l32, channels 16 c + 8 h: pieces 2 c + h), V fragments (keys 16 m + 4 h + .., channels 32 d + ..).
+        const unsigned k_from = lds0 + Tile::piece(l32, h);
+        const int s16 = lane & 15, v_row = 4 * h + (s16 >> 2);
+        const unsigned v_from = lds0 + Tile::kSide + Tile::piece(v_row, (lane >> 4 & 1) * 2 + ((s16 & 3) >> 1)) + (s16 & 1) * 8;
+        const unsigned v_from8 = lds0 + Tile::kSide + Tile::piece(v_row + 8, (lane >> 4 & 1) * 2 + ((s16 & 3) >> 1)) + (s16 & 1) * 8;
+        bf16x8 kf[KS], vf[DT][2], pf[2][2];
+        f32x16 s[2];
+        auto read_k = [&](int buffer, int sub) {
+#pragma unroll
+            for (int c = 0; c < KS; ++c) kf[c] = *(LdsB128)((k_from ^ (c << 5)) + buffer * Tile::kBuffer + sub * (32 * D * 2));
+        };
+        auto read_v = [&](int buffer, int sub) {
+#pragma unroll
+            for (int d = 0; d < DT; ++d)
+#pragma unroll
+                for (int m = 0; m < 2; ++m) {
+                    const bf16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4bf16((LdsB64)((v_from ^ (d << 6)) + buffer * Tile::kBuffer + (sub * 32 + m * 16) * (D * 2)));
+                    const bf16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4bf16((LdsB64)((v_from8 ^ (d << 6)) + buffer * Tile::kBuffer + (sub * 32 + m * 16) * (D * 2)));
+                    vf[d][m] = __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
+                }
+        };
+        auto scores = [&](int y) {
+#pragma unroll
+            for (int i = 0; i < 16; ++i) s[y][i] = 0.f;
+#pragma unroll
+            for (int c = 0; c < KS; ++c) s[y] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf[c], qf[y][c], s[y], 0, 0, 0);
+        };
+        auto values = [&](int y) {
+#pragma unroll
+            for (int m = 0; m < 2; ++m)
+#pragma unroll
+                for (int d = 0; d < DT; ++d) o[y][d] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vf[d][m], pf[y][m], o[y][d], 0, 0, 0);
+        };
+        // What rows do not see of 32 keys; where values that are not numbers became zeros, a row that sees one of them is undefined by its sum.
+        auto hide = [&](int y, const Keys& k, int buffer, int sub) {
+            const unsigned odd = *reinterpret_cast<const uint32_t*>(lds + 3 * Tile::kBuffer + buffer * 8 + sub * 4);
+            unsigned seen_keys = 0;
+#pragma unroll
+            for (int j = 0; j < 2; ++j) {
+                const int seen = min(k.have[sub * 2 + j], pos_of[y] + 1 - k.pos[sub * 2 + j]);
+                seen_keys |= ((1u << max(seen, 0)) - 1u) << (16 * j);
+#pragma unroll
+                for (int i = 0; i < 8; ++i) {
+                    const float v = s[y][8 * j + i];
+                    s[y][8 * j + i] = (i & 3) + 8 * (i >> 2) + 4 * h < seen ? v : -INFINITY;
+                }
+            }
+            if (odd & seen_keys) st[y].l = NAN;
+        };
+        // Moves the reference of rows that have a score too far above it.
+        auto settle = [&](int y) {
+            float mx = s[y][0];
+#pragma unroll
+            for (int i = 1; i < 16; ++i) mx = fmaxf(mx, s[y][i]);
+            if (!__any(mx > st[y].lim)) return;
+            mx = fmaxf(mx, __shfl_xor(mx, 32, 64));
+            if (mx > st[y].lim) {
+                const float to = mx * a.scale_log2e, al = st[y].lim == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(st[y].mc - to);
+                st[y].l *= al;
+                st[y].mc = to;
+                st[y].lim = mx + kManyRoom / a.scale_log2e;
+#pragma unroll
+                for (int d = 0; d < DT; ++d) o[y][d] *= al;
+            }
+        };
+        auto weigh = [&](int y) {
+            float w[16];
+#pragma unroll
+            for (int i = 0; i < 16; ++i) w[i] = __builtin_amdgcn_exp2f(fmaf(s[y][i], a.scale_log2e, -st[y].mc));
+#pragma unroll
+            for (int m = 0; m < 2; ++m) bf16_terms<1>(w + 8 * m, &pf[y][m]);
+            float sum[4];
+#pragma unroll
+            for (int i = 0; i < 4; ++i) sum[i] = (w[i] + w[4 + i]) + (w[8 + i] + w[12 + i]);
+            st[y].l += (sum[0] + sum[1]) + (sum[2] + sum[3]);
+        };
+
+        int buffer = 0;
+        if (now.any) {
+            bool whole = is_whole(now);
+            fill(0, whole);
+            find(next);
+            if (next.any) load(next);
+            __syncthreads();
+            read_k(0, 0);
+            read_v(0, 0);
+#pragma unroll
+            for (int m = 0; m < 2; ++m) pf[1][m] = bf16x8{};      // (the first turn's values of B: nothing, or undefined where they are undefined for all rows)
+            scores(0);
+            while (true) {
+                const int ahead = buffer == 2 ? 0 : buffer + 1;
+                const bool next_whole = next.any && is_whole(next);
+                Keys behind;
+                behind.any = false;
+#pragma unroll
+                for (int sub = 0; sub < 2; ++sub) {
+                    if (!whole) hide(0, now, buffer, sub);
+                    settle(0);
+                    weigh(0);
+                    scores(1);
+                    values(1);
+                    if (sub == 1) {
+                        if (next.any) fill(ahead, next_whole);
+                        __syncthreads();
+                        if (next.any) {
+                            find(behind);
+                            if (behind.any) load(behind);
+                        }
+                    }
+                    if (!whole) hide(1, now, buffer, sub);
+                    settle(1);
+                    weigh(1);
+                    read_v(buffer, sub);
+                    values(0);
+                    read_k(sub == 0 ? buffer : ahead, 1 - sub);      // (behind the last keys: whatever lies there, not used)
+                    scores(0);
+                }
+                if (!next.any) break;
+                now = next;
+                next = behind;
+                whole = next_whole;
+                buffer = ahead;
+            }
+            values(1);
+        }
+        __syncthreads();                                 // the buffers are read before they are written again
+
+        const bool whole_tile = from_cost == 0 && take == tile_cost;
+        if (from_cost == 0 && threadIdx.x < rows) {
+            const int i = row0 + threadIdx.x, n = a.by_group(i);
+            const long long to = begin + share - left_over + tile_cost - 1;      // (what the share has taken so far is share - left_over, but for the last one, which ends with its tile)
+            const int n_shares = whole_tile ? 1 : (int)(to / share) - share_of + 1;
+            a.where[(size_t)(me.lo + n) * a.Hq + g * G + i - n * G] = make_int2(kFewPartRows + (blockIdx.x * 2 + 1) * kManyRows + threadIdx.x, 2 * n_shares + 1);
+        }
+#pragma unroll
+        for (int y = 0; y < 2; ++y) {
+            const float l = st[y].l + __shfl_xor(st[y].l, 32, 64);
+            const int in_tile = wave * 64 + y * 32 + l32;
+            if (in_tile >= rows) continue;
+            if (whole_tile) {
+                const int lrow = row0 + in_tile, token = a.by_group(lrow);
+                bf16_t* dst = out + (size_t)(me.lo + token) * a.ldo + (size_t)(g * G + lrow - token * G) * D + 4 * h;
+                const float inv = l == 0.f ? 0.f : 1.f / l;
+#pragma unroll
+                for (int d = 0; d < DT; ++d)
+#pragma unroll
+                    for (int i = 0; i < 4; ++i)
+                        *reinterpret_cast<uint2*>(dst + d * 32 + i * 8) = make_uint2(pack_bf16x2(o[y][d][4 * i] * inv, o[y][d][4 * i + 1] * inv),
+                                                                                    pack_bf16x2(o[y][d][4 * i + 2] * inv, o[y][d][4 * i + 3] * inv));
+            } else {
+                float* dst = a.part + (size_t)(kFewPartRows + (blockIdx.x * 2 + (from_cost == 0)) * kManyRows + in_tile) * (D + 4);
+#pragma unroll
+                for (int d = 0; d < DT; ++d)
+#pragma unroll
+                    for (int i = 0; i < 4; ++i)
+                        *reinterpret_cast<f32x4*>(dst + d * 32 + i * 8 + 4 * h) = f32x4{o[y][d][4 * i], o[y][d][4 * i + 1], o[y][d][4 * i + 2], o[y][d][4 * i + 3]};
+                if (h == 0) { dst[D] = st[y].lim == -INFINITY ? -INFINITY : st[y].mc; dst[D + 1] = l; }
+            }
+        }
+        left_over -= take;
+        if (left_over <= 0) return;
+        from_cost = 0;
+        if (++tile == tiles_of(me)) {
+            tile = 0;
+            unsigned long long more_rows = __ballot(x.n > 0) & ~((2ull << i_req) - 1);
+            while (!more_rows) {
+                r0 += 64;
+                if (r0 >= a.R) return;
+                x = request(r0 + lane);
+                more_rows = __ballot(x.n > 0);
+            }
+            i_req = __builtin_ctzll(more_rows);
+            me = BatchRequest{wave_value(x.lo, i_req), wave_value(x.n, i_req), wave_value(x.len, i_req)};
+        }
     }
 }
 
@@ -674,27 +1061,28 @@ __global__ void __launch_bounds__(256) batch_merge_kernel(T* __restrict__ out, B
     const int tid = threadIdx.x, c = tid % LN, grp = tid / LN % NG, x = tid / (LN * NG);
     const long long row = (long long)blockIdx.x * PER + x;
     const int t = (int)(row / a.Hq);
-    int first = 0, n = 0, i = 0;
+    int first = 0, n = 0, apart = 0, back = 0;           // in rows of `part`: from share to share, from the first one's second tile to the others' first
     const int2 at = a.where[min(row, (long long)a.n_rows * a.Hq - 1)];
     if (t >= max(a.row_start[0], 0) && t < min(a.row_start[a.R], a.n_rows)) {
+        const bool many = at.y & 1;
         first = at.x;
-        n = at.y / kTileRows;
-        i = at.y % kTileRows;
-        if (n <= 1 || i < 0 || first < 0 || first + (long long)(n - 1) * a.Hkv >= kBatchGrid) n = 0;
+        n = at.y >> 1;
+        back = many ? kManyRows : kTileRows;
+        apart = 2 * a.Hkv * back;
+        if (n <= 1 || first < back || first - back + (long long)(n - 1) * apart >= (many ? kPartRows : kFewPartRows)) n = 0;
     }
-    const float* p = a.part + ((size_t)first * 2 * kTileRows + i) * (D + 2);
-    constexpr size_t kPart = (size_t)kTileRows * (D + 2);
+    const float* p = a.part + (size_t)first * (D + 4);
     float M = -INFINITY, l = 0.f, o[4] = {0.f, 0.f, 0.f, 0.f};
     constexpr int kAtOnce = 8;                           // requested together
     for (int y0 = grp; y0 < n; y0 += NG * kAtOnce) {
-        float2 st[kAtOnce], v0[kAtOnce], v1[kAtOnce];
+        float2 st[kAtOnce];
+        f32x4 v[kAtOnce];
 #pragma unroll
         for (int b = 0; b < kAtOnce; ++b) {
             const int y = min(y0 + b * NG, n - 1);       // the first one is what its share has left unfinished
-            const float* s = p + (y == 0 ? kPart : (size_t)y * a.Hkv * 2 * kPart);
+            const float* s = p + (y == 0 ? 0ll : (long long)y * apart - back) * (D + 4);
             st[b] = *reinterpret_cast<const float2*>(s + D);
-            v0[b] = *reinterpret_cast<const float2*>(s + c * 4);
-            v1[b] = *reinterpret_cast<const float2*>(s + c * 4 + 2);
+            v[b] = *reinterpret_cast<const f32x4*>(s + c * 4);
         }
         float now = M;
 #pragma unroll
@@ -711,10 +1099,8 @@ __global__ void __launch_bounds__(256) batch_merge_kernel(T* __restrict__ out, B
         for (int b = 0; b < kAtOnce; ++b) {
             const float w = st[b].y == 0.f ? 0.f : __builtin_amdgcn_exp2f(st[b].x - M);
             l += w * st[b].y;
-            o[0] += w * v0[b].x;
-            o[1] += w * v0[b].y;
-            o[2] += w * v1[b].x;
-            o[3] += w * v1[b].y;
+#pragma unroll
+            for (int e = 0; e < 4; ++e) o[e] += w * v[b][e];
         }
     }
     if constexpr (NG > 1) {
@@ -743,24 +1129,36 @@ __global__ void __launch_bounds__(256) batch_merge_kernel(T* __restrict__ out, B
     for (int e = 0; e < 4; ++e) Elem<T>::st(dst + e, l == 0.f ? 0.f : o[e] / l);
 }
 
-static size_t batch_part_bytes(int d) { return (size_t)kBatchGrid * 2 * kTileRows * (d + 2) * sizeof(float); }
-size_t batch_attn_kv8_workspace_bytes(int n_rows, int Hq, int d) { return align_up(batch_part_bytes(d), 256) + align_up((size_t)n_rows * Hq * sizeof(int2), 256); }
+static size_t batch_part_bytes(int n_rows, int Hq, int Hkv, int d) {
+    const bool many = (long long)n_rows * (Hq / Hkv) > kFewRows;      // (of either type, so that one workspace serves both)
+    return align_up((size_t)(many ? kPartRows : kFewPartRows) * (d + 4) * sizeof(float), 256);
+}
+size_t batch_attn_kv8_workspace_bytes(int n_rows, int Hq, int Hkv, int d) { return batch_part_bytes(n_rows, Hq, Hkv, d) + align_up((size_t)n_rows * Hq * sizeof(int2), 256); }
+
+template <typename K> static int raise_lds(K kernel, int bytes, std::once_flag& once, hipError_t& err) {
+    std::call_once(once, [&] { err = hipFuncSetAttribute((const void*)kernel, hipFuncAttributeMaxDynamicSharedMemorySize, bytes); });
+    return err == hipSuccess ? SLIM_OK : set_hip_error(err);
+}
 
 template <typename T, int D>
-static int launch_batch_attn(const void* q, void* out, const BatchAttnArgs& a, hipStream_t st) {
+static int launch_batch_attn(const void* q, void* out, BatchAttnArgs& a, hipStream_t st) {
     const int shares = std::max(1, kBatchGrid / a.Hkv);
+    const long long rows = (long long)a.n_rows * a.Hq;
     constexpr int NW = kBatchWaves, smem = NW * RowTile<T, D>::kLdsBytes;
-    if (smem >= 1 << 16) {
-        static std::once_flag once;
-        static hipError_t err = hipSuccess;
-        std::call_once(once, [&] { err = hipFuncSetAttribute((const void*)batch_attn_kv8_kernel<T, D, NW>, hipFuncAttributeMaxDynamicSharedMemorySize, smem); });
-        if (err != hipSuccess) return set_hip_error(err);
-    }
+    static_assert(smem < 1 << 16, "within the limit that needs no raising");
+    if constexpr (sizeof(T) == 2)
+        if ((long long)a.n_rows * (a.Hq / a.Hkv) > kFewRows) {
+            constexpr int many_smem = ManyTile<D>::kLdsBytes;
+            static std::once_flag once;
+            static hipError_t err = hipSuccess;
+            if (const int rc = raise_lds(batch_attn_many_kernel<D>, many_smem, once, err)) return rc;
+            a.few = kFewRows;
+            hipLaunchKernelGGL((batch_attn_many_kernel<D>), dim3(std::max(1, kManyGrid / a.Hkv) * a.Hkv), dim3(256), many_smem, st, (const bf16_t*)q, (bf16_t*)out, a);
+            if (const int rc = check_launch()) return rc;
+        }
     hipLaunchKernelGGL((batch_attn_kv8_kernel<T, D, NW>), dim3(shares * a.Hkv), dim3(64 * NW), smem, st, (const T*)q, (T*)out, a);
     const int rc = check_launch();
-    if (rc) return rc;
-    if (shares == 1) return rc;                          // no tile is shared
-    const long long rows = (long long)a.n_rows * a.Hq;
+    if (rc || shares == 1) return rc;                    // (no tile is shared)
     constexpr int kOne = 256 / (D / 4);                  // rows of a workgroup without groups
     if (rows >= kBatchGrid * 4)                          // few partial results of a tile
         hipLaunchKernelGGL((batch_merge_kernel<T, D, 1>), dim3((unsigned)((rows + kOne - 1) / kOne)), dim3(256), 0, st, (T*)out, a);
@@ -771,8 +1169,9 @@ static int launch_batch_attn(const void* q, void* out, const BatchAttnArgs& a, h
 
 int launch_batch_attn_kv8(const void* q, int ldq, const int* row_start, const int* lens, const int* table, int R, int n_rows, int max_blocks, const void* pool, int n_slots, size_t slot_bytes,
                           size_t layer_offset, int block, int Hq, int Hkv, int d, float scale, int dtype, void* out, int ldo, void* workspace, hipStream_t st) {
-    BatchAttnArgs a{row_start, lens, table, (const unsigned char*)pool, slot_bytes, layer_offset, (float*)workspace, (int2*)((char*)workspace + align_up(batch_part_bytes(d), 256)),
-                    scale * 1.4426950408889634f, R, max_blocks, n_slots, n_rows, block, (block + kPiece - 1) / kPiece, Hq, Hkv, ldq, ldo, Divide(block), Divide((block + kPiece - 1) / kPiece)};
+    const int per_block = (block + kPiece - 1) / kPiece;
+    BatchAttnArgs a{row_start, lens, table, (const unsigned char*)pool, slot_bytes, layer_offset, (float*)workspace, (int2*)((char*)workspace + batch_part_bytes(n_rows, Hq, Hkv, d)),
+                    scale * 1.4426950408889634f, R, max_blocks, n_slots, n_rows, block, per_block, Hq, Hkv, ldq, ldo, 0x7fffffff, Divide(block), Divide(per_block), Divide(Hq / Hkv)};
     if (dtype == SLIM_BF16) return d == 64 ? launch_batch_attn<bf16_t, 64>(q, out, a, st) : launch_batch_attn<bf16_t, 128>(q, out, a, st);
     return d == 64 ? launch_batch_attn<float, 64>(q, out, a, st) : launch_batch_attn<float, 128>(q, out, a, st);
 }

@@ -177,7 +177,7 @@ int launch_kv8_write(const void* k, const void* v, int ldk, int ldv, const int* 
                      size_t layer_offset, hipStream_t st);
 int launch_kv8_read(const void* pool, int n_slots, size_t slot_bytes, size_t layer_offset, const int* slots, int n_tokens, int Hkv, int d, int block, int dtype, void* k, void* v,
                     int ldk, int ldv, hipStream_t st);
-size_t batch_attn_kv8_workspace_bytes(int n_rows, int Hq, int d);
+size_t batch_attn_kv8_workspace_bytes(int n_rows, int Hq, int Hkv, int d);
 int launch_batch_attn_kv8(const void* q, int ldq, const int* row_start, const int* lens, const int* table, int R, int n_rows, int max_blocks, const void* pool, int n_slots, size_t slot_bytes,
                           size_t layer_offset, int block, int Hq, int Hkv, int d, float scale, int dtype, void* out, int ldo, void* workspace, hipStream_t st);
 size_t sliding_workspace_floats(int n_q, int n_k, int Hq, int Hkv, int d, int window, int sinks, int dtype);
