@@ -10,6 +10,7 @@
 #include "batch.h"
 #include <algorithm>
 #include <mutex>
+#include <type_traits>
 
 namespace slim {
 
@@ -762,7 +763,7 @@ __global__ void __launch_bounds__(256, 1) batch_attn_many_kernel(const bf16_t* _
         const int u_begin = piece_at(from_cost), u_end = piece_at(from_cost + take);
 
         // The pieces, four at a time, looked up 64 at once by every wave for itself.
-        int u = u_begin + lane, batch = u_begin - 64, u_slot = 0, u_pos = 0, u_rows = 0, next_slot = u < u_end ? table[a.by_piece(u)] : -1;
+        int u = u_begin + lane, batch = u_begin - 64, u_slot = 0, u_row = 0, u_pos = 0, u_rows = 0, next_slot = u < u_end ? table[a.by_piece(u)] : -1;
         unsigned long long left = 0;
         struct Keys { int have[4], pos[4], c0[4]; const unsigned char* base[4]; bool any; };
         auto find = [&](Keys& k) {
@@ -772,10 +773,11 @@ __global__ void __launch_bounds__(256, 1) batch_attn_many_kernel(const bf16_t* _
                     k.any = false;
                     return;
                 }
-                const int b = a.by_piece(u), row = (u - b * a.per_block) * kPiece;
+                const int b = a.by_piece(u);
+                u_row = (u - b * a.per_block) * kPiece;
                 u_slot = next_slot;
-                u_pos = b * a.block + row;
-                u_rows = u < u_end && u_slot >= 0 && u_slot < a.n_slots ? min(kPiece, min(a.block - row, limit - u_pos)) : 0;
+                u_pos = b * a.block + u_row;
+                u_rows = u < u_end && u_slot >= 0 && u_slot < a.n_slots ? min(kPiece, min(a.block - u_row, limit - u_pos)) : 0;
                 left = __ballot(u_rows > 0);
                 u += 64;
                 next_slot = u < u_end ? table[a.by_piece(u)] : -1;
@@ -794,7 +796,7 @@ __global__ void __launch_bounds__(256, 1) batch_attn_many_kernel(const bf16_t* _
                 left &= left - 1;
                 k.have[j] = __builtin_amdgcn_readlane(u_rows, i);
                 k.pos[j] = __builtin_amdgcn_readlane(u_pos, i);
-                k.c0[j] = k.pos[j] - a.by_block(k.pos[j]) * a.block;
+                k.c0[j] = __builtin_amdgcn_readlane(u_row, i);
                 k.base[j] = a.pool + (size_t)__builtin_amdgcn_readlane(u_slot, i) * a.slot_bytes + a.layer_offset;
             }
         };
@@ -818,36 +820,39 @@ __global__ void __launch_bounds__(256, 1) batch_attn_many_kernel(const bf16_t* _
                 ex[s] = *reinterpret_cast<const uint16_t*>(base + head.e);
             }
         };
-        auto fill = [&](int buffer, bool whole) {
+        // Values of the next keys that are not numbers become zeros, a bit each, where some row does not see all of them (as for few rows).
+        auto clear_odd = [&](int buffer) {
 #pragma unroll
             for (int s = 0; s < NPASS; ++s) {
-                const int key = my_key + s * KPP;
-                const float kp = kv8_power(ex[s] & 0xffu), vp = kv8_power(ex[s] >> 8);
-                const unsigned to = lds0 + buffer * Tile::kBuffer + Tile::piece(key, my_piece * 2);
-                uint4 v = vx[s];
-                if (!whole) {                            // (as for few rows)
-                    bool odd = false;
+                bool odd = false;
 #pragma unroll
-                    for (int i = 0; i < 4; ++i) {
-                        uint32_t& x = i == 0 ? v.x : i == 1 ? v.y : i == 2 ? v.z : v.w;
-                        const uint32_t bytes = (((x & 0x7f7f7f7fu) + 0x01010101u) >> 7 & 0x01010101u) * 0xffu;
-                        odd |= bytes != 0;
-                        x &= ~bytes;
-                    }
-                    const unsigned long long lanes = __ballot(odd);
-                    unsigned bits = 0;                   // of the wave's 64 / PR keys
-#pragma unroll
-                    for (int i = 0; i < 64 / PR; ++i) bits |= (lanes >> (i * PR) & ((1ull << PR) - 1)) ? 1u << i : 0u;
-                    unsigned char* flags = lds + 3 * Tile::kBuffer + buffer * 8 + s * (KPP / 8);
-                    if (lane == 0) {
-                        if constexpr (PR == 8) flags[wave] = (unsigned char)bits;
-                        else *reinterpret_cast<uint16_t*>(flags + wave * 2) = (uint16_t)bits;
-                    }
+                for (int i = 0; i < 4; ++i) {
+                    uint32_t& x = i == 0 ? vx[s].x : i == 1 ? vx[s].y : i == 2 ? vx[s].z : vx[s].w;
+                    const uint32_t bytes = (((x & 0x7f7f7f7fu) + 0x01010101u) >> 7 & 0x01010101u) * 0xffu;
+                    odd |= bytes != 0;
+                    x &= ~bytes;
                 }
-                *(LdsB128)(to) = kv8_to_bf16(make_uint2(kx[s].x, kx[s].y), kp);
-                *(LdsB128)(to ^ 16) = kv8_to_bf16(make_uint2(kx[s].z, kx[s].w), kp);
-                *(LdsB128)(to + Tile::kSide) = kv8_to_bf16(make_uint2(v.x, v.y), vp);
-                *(LdsB128)((to ^ 16) + Tile::kSide) = kv8_to_bf16(make_uint2(v.z, v.w), vp);
+                const unsigned long long lanes = __ballot(odd);
+                unsigned bits = 0;                       // of the wave's 64 / PR keys
+#pragma unroll
+                for (int i = 0; i < 64 / PR; ++i) bits |= (lanes >> (i * PR) & ((1ull << PR) - 1)) ? 1u << i : 0u;
+                unsigned char* flags = lds + 3 * Tile::kBuffer + buffer * 8 + s * (KPP / 8);
+                if (lane == 0) {
+                    if constexpr (PR == 8) flags[wave] = (unsigned char)bits;
+                    else *reinterpret_cast<uint16_t*>(flags + wave * 2) = (uint16_t)bits;
+                }
+            }
+        };
+        const unsigned fill_to = lds0 + Tile::piece(my_key, my_piece * 2);
+        auto fill = [&](int buffer) {
+#pragma unroll
+            for (int s = 0; s < NPASS; ++s) {
+                const float kp = kv8_power(ex[s] & 0xffu), vp = kv8_power(ex[s] >> 8);
+                const unsigned at = buffer * Tile::kBuffer + s * (KPP * D * 2);
+                *(LdsB128)(fill_to + at) = kv8_to_bf16(make_uint2(kx[s].x, kx[s].y), kp);
+                *(LdsB128)((fill_to ^ 16) + at) = kv8_to_bf16(make_uint2(kx[s].z, kx[s].w), kp);
+                *(LdsB128)(fill_to + at + Tile::kSide) = kv8_to_bf16(make_uint2(vx[s].x, vx[s].y), vp);
+                *(LdsB128)((fill_to ^ 16) + at + Tile::kSide) = kv8_to_bf16(make_uint2(vx[s].z, vx[s].w), vp);
             }
         };
 
@@ -940,6 +945,18 @@ __global__ void __launch_bounds__(256, 1) batch_attn_many_kernel(const bf16_t* _
                 for (int d = 0; d < DT; ++d) o[y][d] *= al;
             }
         };
+        // The order of a phase: a matrix instruction, and what a lane computes and reads meanwhile (0: scores and values from fragments that are there, 1: from LDS).
+        auto interleave = [](auto reads) {
+            constexpr int kMfma = 0x8, kValu = 0x2, kTrans = 0x400, kRead = 0x100;
+            if constexpr (reads.value) __builtin_amdgcn_sched_group_barrier(kRead, KS, 0);
+#pragma unroll
+            for (int i = 0; i < KS + 2 * DT; ++i) {
+                __builtin_amdgcn_sched_group_barrier(kMfma, 1, 0);
+                __builtin_amdgcn_sched_group_barrier(kTrans, 1, 0);
+                __builtin_amdgcn_sched_group_barrier(kValu, 4, 0);
+                if constexpr (reads.value) if (i < KS) __builtin_amdgcn_sched_group_barrier(kRead, 2, 0);
+            }
+        };
         auto weigh = [&](int y) {
             float w[16];
 #pragma unroll
@@ -950,12 +967,14 @@ __global__ void __launch_bounds__(256, 1) batch_attn_many_kernel(const bf16_t* _
 #pragma unroll
             for (int i = 0; i < 4; ++i) sum[i] = (w[i] + w[4 + i]) + (w[8 + i] + w[12 + i]);
             st[y].l += (sum[0] + sum[1]) + (sum[2] + sum[3]);
+            asm volatile("" : "+v"(pf[y][0]), "+v"(pf[y][1]), "+v"(st[y].l));      // (formed here, beside the matrix instructions, and not where they are used)
         };
 
         int buffer = 0;
         if (now.any) {
             bool whole = is_whole(now);
-            fill(0, whole);
+            if (!whole) clear_odd(0);
+            fill(0);
             find(next);
             if (next.any) load(next);
             __syncthreads();
@@ -970,14 +989,20 @@ __global__ void __launch_bounds__(256, 1) batch_attn_many_kernel(const bf16_t* _
                 Keys behind;
                 behind.any = false;
 #pragma unroll
+                for (int y = 0; y < 2; ++y)
+#pragma unroll
+                    for (int c = 0; c < KS; ++c) asm volatile("" : "+a"(qf[y][c]));      // (they stay among the accumulation registers, where matrix instructions read them too)
+#pragma unroll
                 for (int sub = 0; sub < 2; ++sub) {
                     if (!whole) hide(0, now, buffer, sub);
                     settle(0);
-                    weigh(0);
+                    if (sub == 1 && next.any && !next_whole) clear_odd(ahead);
                     scores(1);
                     values(1);
+                    weigh(0);
+                    if (sub == 1) fill(ahead);           // (behind the last keys: the last codes again, not used)
+                    interleave(std::integral_constant<int, 0>());
                     if (sub == 1) {
-                        if (next.any) fill(ahead, next_whole);
                         __syncthreads();
                         if (next.any) {
                             find(behind);
@@ -986,11 +1011,12 @@ __global__ void __launch_bounds__(256, 1) batch_attn_many_kernel(const bf16_t* _
                     }
                     if (!whole) hide(1, now, buffer, sub);
                     settle(1);
-                    weigh(1);
+                    read_k(sub == 0 ? buffer : ahead, 1 - sub);
+                    scores(0);
                     read_v(buffer, sub);
                     values(0);
-                    read_k(sub == 0 ? buffer : ahead, 1 - sub);      // (behind the last keys: whatever lies there, not used)
-                    scores(0);
+                    weigh(1);
+                    interleave(std::integral_constant<int, 1>());
                 }
                 if (!next.any) break;
                 now = next;
