@@ -690,7 +690,11 @@ constexpr int kManyKeys = 64;
 template <int D> struct ManyTile {
     static constexpr int kSide = kManyKeys * D * 2, kBuffer = 2 * kSide, kLdsBytes = 3 * kBuffer + 3 * 8;      // Keys or Values; both; three, and a bit for each key with a Value that is not a number
     static constexpr int KS = D / 16, DT = D / 32, CH = D / 8;
-    __device__ static __forceinline__ unsigned piece(int r, int c) { return (unsigned)(r * (D * 2) + ((c ^ (r & (CH - 1))) << 4)); }
+    // Byte offset of 16-byte piece c of key r.  The turn of the pieces spreads the reads of K (16 keys, one piece), the transposing ones of V (8 keys, four pieces) over all banks.
+    __device__ static __forceinline__ unsigned piece(int r, int c) {
+        const int turn = D == 128 ? (r << 1 & 14) | (r >> 3 & 1) : r & (CH - 1);
+        return (unsigned)(r * (D * 2) + ((c ^ turn) << 4));
+    }
 };
 constexpr float kManyRoom = 30.f;
 
@@ -762,10 +766,25 @@ __global__ void __launch_bounds__(256, 1) batch_attn_many_kernel(const bf16_t* _
         auto piece_at = [&](long long c) { return c >= tile_cost ? last : (int)((double)last * ((double)c / (double)tile_cost)); };
         const int u_begin = piece_at(from_cost), u_end = piece_at(from_cost + take);
 
-        // The pieces, four at a time, looked up 64 at once by every wave for itself.
-        int u = u_begin + lane, batch = u_begin - 64, u_slot = 0, u_row = 0, u_pos = 0, u_rows = 0, next_slot = u < u_end ? table[a.by_piece(u)] : -1;
-        unsigned long long left = 0;
-        struct Keys { int have[4], pos[4], c0[4]; const unsigned char* base[4]; bool any; };
+        // The pieces, four at a time, looked up 64 at once by every wave for itself, one a lane: where the Keys begin, exponents, rows, position.  Slots are requested two lookups ahead,
+        // exponents one.
+        int u = u_begin + lane, batch = u_begin - 64, u_pos = 0, u_rows = 0;
+        unsigned u_low = 0, u_high = 0;
+        uint32_t u_e = 0;
+        auto slot_at = [&](int u) { return u < u_end ? table[a.by_piece(u)] : -1; };
+        auto exponents_at = [&](int slot) {
+            return slot >= 0 && slot < a.n_slots ? *reinterpret_cast<const uint16_t*>(a.pool + (size_t)slot * a.slot_bytes + a.layer_offset + head.e) : (uint16_t)0;
+        };
+        int slot_1 = slot_at(u), slot_2 = slot_at(u + 64);
+        uint32_t e_1 = exponents_at(slot_1);
+        unsigned long long left = 0, full = 0;           // lanes whose pieces hold keys and have not been taken; that hold 16 which all rows see
+        struct Keys {
+            bool any, whole;
+            const unsigned char* from[NPASS];            // of the piece that the wave's keys lie in, in either pass
+            int rows[NPASS];
+            uint32_t e[NPASS];
+            int have[4], pos[4];                         // unless whole
+        };
         auto find = [&](Keys& k) {
             while (!left) {
                 batch += 64;
@@ -773,51 +792,62 @@ __global__ void __launch_bounds__(256, 1) batch_attn_many_kernel(const bf16_t* _
                     k.any = false;
                     return;
                 }
-                const int b = a.by_piece(u);
-                u_row = (u - b * a.per_block) * kPiece;
-                u_slot = next_slot;
-                u_pos = b * a.block + u_row;
-                u_rows = u < u_end && u_slot >= 0 && u_slot < a.n_slots ? min(kPiece, min(a.block - u_row, limit - u_pos)) : 0;
+                const int b = a.by_piece(u), row = (u - b * a.per_block) * kPiece;
+                u_pos = b * a.block + row;
+                u_rows = slot_1 >= 0 && slot_1 < a.n_slots ? min(kPiece, min(a.block - row, limit - u_pos)) : 0;
+                const size_t from = (size_t)a.pool + (size_t)max(slot_1, 0) * a.slot_bytes + a.layer_offset + head.k + (size_t)row * D;
+                u_low = (unsigned)from;
+                u_high = (unsigned)(from >> 32);
+                u_e = e_1;
                 left = __ballot(u_rows > 0);
+                full = __ballot(u_rows == kPiece && u_pos + kPiece - 1 <= p0);
                 u += 64;
-                next_slot = u < u_end ? table[a.by_piece(u)] : -1;
+                e_1 = exponents_at(slot_2);
+                slot_1 = slot_2;
+                slot_2 = slot_at(u + 64);
             }
             k.any = true;
+            int i[4];
+            unsigned long long taken = 0;
 #pragma unroll
             for (int j = 0; j < 4; ++j) {
-                if (j > 0 && !left) {                    // fewer than four: the first one again, unseen
-                    k.have[j] = 0;
-                    k.pos[j] = k.pos[0];
-                    k.c0[j] = k.c0[0];
-                    k.base[j] = k.base[0];
-                    continue;
+                i[j] = left ? __builtin_ctzll(left) : -1;
+                const unsigned long long bit = left & (0 - left);
+                taken |= bit;
+                left ^= bit;
+            }
+            k.whole = i[3] >= 0 && (taken & ~full) == 0;
+#pragma unroll
+            for (int s = 0; s < NPASS; ++s) {
+                const int j = NPASS == 1 ? wave : (wave >> 1) + 2 * s;
+                int x = j == 0 ? i[0] : j == 1 ? i[1] : j == 2 ? i[2] : i[3];
+                if (x < 0) x = i[0];                     // fewer than four: the first one again, unseen
+                k.from[s] = (const unsigned char*)((size_t)(unsigned)__builtin_amdgcn_readlane(u_high, x) << 32 | (unsigned)__builtin_amdgcn_readlane(u_low, x));
+                k.rows[s] = __builtin_amdgcn_readlane(u_rows, x);
+                k.e[s] = __builtin_amdgcn_readlane(u_e, x);
+            }
+            if (!k.whole) {
+#pragma unroll
+                for (int j = 0; j < 4; ++j) {
+                    const int x = max(i[j], 0);
+                    k.have[j] = i[j] < 0 ? 0 : __builtin_amdgcn_readlane(u_rows, x);
+                    k.pos[j] = __builtin_amdgcn_readlane(u_pos, x);
                 }
-                const int i = __builtin_ctzll(left);
-                left &= left - 1;
-                k.have[j] = __builtin_amdgcn_readlane(u_rows, i);
-                k.pos[j] = __builtin_amdgcn_readlane(u_pos, i);
-                k.c0[j] = __builtin_amdgcn_readlane(u_row, i);
-                k.base[j] = a.pool + (size_t)__builtin_amdgcn_readlane(u_slot, i) * a.slot_bytes + a.layer_offset;
             }
         };
-        auto is_whole = [&](const Keys& k) {
-            return k.have[0] == kPiece && k.have[1] == kPiece && k.have[2] == kPiece && k.have[3] == kPiece &&
-                   max(max(k.pos[0], k.pos[1]), max(k.pos[2], k.pos[3])) + kPiece - 1 <= p0;
-        };
-        // A thread's codes of the next 64 keys: 16 channels of key tid / PR, and of one 32 further on.
+        // A thread's codes of the next 64 keys: 16 channels of key tid / PR, and of one KPP further on.
         const int my_key = threadIdx.x / PR, my_piece = threadIdx.x % PR;
+        const size_t values_apart = head.v - head.k;
         uint4 kx[NPASS], vx[NPASS];
-        uint32_t ex[NPASS];
+        float kp[NPASS], vp[NPASS];
         auto load = [&](const Keys& k) {
 #pragma unroll
             for (int s = 0; s < NPASS; ++s) {
-                const int j = NPASS == 1 ? wave : (wave >> 1) + 2 * s;      // the piece that the wave's keys lie in
-                const int have = j == 0 ? k.have[0] : j == 1 ? k.have[1] : j == 2 ? k.have[2] : k.have[3], c0 = j == 0 ? k.c0[0] : j == 1 ? k.c0[1] : j == 2 ? k.c0[2] : k.c0[3];
-                const unsigned char* base = j == 0 ? k.base[0] : j == 1 ? k.base[1] : j == 2 ? k.base[2] : k.base[3];
-                const unsigned off = min(my_key & 15, max(have, 1) - 1) * D + my_piece * 16;
-                kx[s] = *reinterpret_cast<const uint4*>(base + head.k + (size_t)c0 * D + off);
-                vx[s] = *reinterpret_cast<const uint4*>(base + head.v + (size_t)c0 * D + off);
-                ex[s] = *reinterpret_cast<const uint16_t*>(base + head.e);
+                const unsigned off = min(my_key & 15, k.rows[s] - 1) * D + my_piece * 16;
+                kx[s] = *reinterpret_cast<const uint4*>(k.from[s] + off);
+                vx[s] = *reinterpret_cast<const uint4*>(k.from[s] + values_apart + off);
+                kp[s] = kv8_power(k.e[s] & 0xffu);
+                vp[s] = kv8_power(k.e[s] >> 8);
             }
         };
         // Values of the next keys that are not numbers become zeros, a bit each, where some row does not see all of them (as for few rows).
@@ -847,12 +877,11 @@ __global__ void __launch_bounds__(256, 1) batch_attn_many_kernel(const bf16_t* _
         auto fill = [&](int buffer) {
 #pragma unroll
             for (int s = 0; s < NPASS; ++s) {
-                const float kp = kv8_power(ex[s] & 0xffu), vp = kv8_power(ex[s] >> 8);
                 const unsigned at = buffer * Tile::kBuffer + s * (KPP * D * 2);
-                *(LdsB128)(fill_to + at) = kv8_to_bf16(make_uint2(kx[s].x, kx[s].y), kp);
-                *(LdsB128)((fill_to ^ 16) + at) = kv8_to_bf16(make_uint2(kx[s].z, kx[s].w), kp);
-                *(LdsB128)(fill_to + at + Tile::kSide) = kv8_to_bf16(make_uint2(vx[s].x, vx[s].y), vp);
-                *(LdsB128)((fill_to ^ 16) + at + Tile::kSide) = kv8_to_bf16(make_uint2(vx[s].z, vx[s].w), vp);
+                *(LdsB128)(fill_to + at) = kv8_to_bf16(make_uint2(kx[s].x, kx[s].y), kp[s]);
+                *(LdsB128)((fill_to ^ 16) + at) = kv8_to_bf16(make_uint2(kx[s].z, kx[s].w), kp[s]);
+                *(LdsB128)(fill_to + at + Tile::kSide) = kv8_to_bf16(make_uint2(vx[s].x, vx[s].y), vp[s]);
+                *(LdsB128)((fill_to ^ 16) + at + Tile::kSide) = kv8_to_bf16(make_uint2(vx[s].z, vx[s].w), vp[s]);
             }
         };
 
@@ -885,33 +914,40 @@ __global__ void __launch_bounds__(256, 1) batch_attn_many_kernel(const bf16_t* _
         const int s16 = lane & 15, v_row = 4 * h + (s16 >> 2);
         const unsigned v_from = lds0 + Tile::kSide + Tile::piece(v_row, (lane >> 4 & 1) * 2 + ((s16 & 3) >> 1)) + (s16 & 1) * 8;
         const unsigned v_from8 = lds0 + Tile::kSide + Tile::piece(v_row + 8, (lane >> 4 & 1) * 2 + ((s16 & 3) >> 1)) + (s16 & 1) * 8;
-        bf16x8 kf[KS], vf[DT][2], pf[2][2];
+        bf16x8 kf[2][KS], vf[2][DT][2], pf[2][2];        // of 32 keys, and of the next
         f32x16 s[2];
-        auto read_k = [&](int buffer, int sub) {
+        float top[2];                                    // the lane's largest score
+        auto read_k = [&](bf16x8* k, int buffer, int sub) {
 #pragma unroll
-            for (int c = 0; c < KS; ++c) kf[c] = *(LdsB128)((k_from ^ (c << 5)) + buffer * Tile::kBuffer + sub * (32 * D * 2));
+            for (int c = 0; c < KS; ++c) k[c] = *(LdsB128)((k_from ^ (c << 5)) + buffer * Tile::kBuffer + sub * (32 * D * 2));
         };
-        auto read_v = [&](int buffer, int sub) {
-#pragma unroll
-            for (int d = 0; d < DT; ++d)
-#pragma unroll
-                for (int m = 0; m < 2; ++m) {
-                    const bf16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4bf16((LdsB64)((v_from ^ (d << 6)) + buffer * Tile::kBuffer + (sub * 32 + m * 16) * (D * 2)));
-                    const bf16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4bf16((LdsB64)((v_from8 ^ (d << 6)) + buffer * Tile::kBuffer + (sub * 32 + m * 16) * (D * 2)));
-                    vf[d][m] = __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
-                }
-        };
-        auto scores = [&](int y) {
-#pragma unroll
-            for (int i = 0; i < 16; ++i) s[y][i] = 0.f;
-#pragma unroll
-            for (int c = 0; c < KS; ++c) s[y] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf[c], qf[y][c], s[y], 0, 0, 0);
-        };
-        auto values = [&](int y) {
+        auto read_v = [&](bf16x8 (*v)[2], int buffer, int sub) {
 #pragma unroll
             for (int m = 0; m < 2; ++m)
 #pragma unroll
-                for (int d = 0; d < DT; ++d) o[y][d] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vf[d][m], pf[y][m], o[y][d], 0, 0, 0);
+                for (int d = 0; d < DT; ++d) {
+                    const bf16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4bf16((LdsB64)((v_from ^ (d << 6)) + buffer * Tile::kBuffer + (sub * 32 + m * 16) * (D * 2)));
+                    const bf16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4bf16((LdsB64)((v_from8 ^ (d << 6)) + buffer * Tile::kBuffer + (sub * 32 + m * 16) * (D * 2)));
+                    v[d][m] = __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
+                }
+        };
+        auto largest_of = [&](int y) {
+            float mx = s[y][0];
+#pragma unroll
+            for (int i = 1; i < 16; ++i) mx = fmaxf(mx, s[y][i]);
+            top[y] = mx;
+        };
+        auto scores = [&](int y, const bf16x8* k) {
+#pragma unroll
+            for (int i = 0; i < 16; ++i) s[y][i] = 0.f;
+#pragma unroll
+            for (int c = 0; c < KS; ++c) s[y] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(k[c], qf[y][c], s[y], 0, 0, 0);
+        };
+        auto values = [&](int y, const bf16x8 (*v)[2]) {
+#pragma unroll
+            for (int m = 0; m < 2; ++m)
+#pragma unroll
+                for (int d = 0; d < DT; ++d) o[y][d] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(v[d][m], pf[y][m], o[y][d], 0, 0, 0);
         };
         // What rows do not see of 32 keys; where values that are not numbers became zeros, a row that sees one of them is undefined by its sum.
         auto hide = [&](int y, const Keys& k, int buffer, int sub) {
@@ -928,14 +964,12 @@ __global__ void __launch_bounds__(256, 1) batch_attn_many_kernel(const bf16_t* _
                 }
             }
             if (odd & seen_keys) st[y].l = NAN;
+            largest_of(y);
         };
         // Moves the reference of rows that have a score too far above it.
         auto settle = [&](int y) {
-            float mx = s[y][0];
-#pragma unroll
-            for (int i = 1; i < 16; ++i) mx = fmaxf(mx, s[y][i]);
-            if (!__any(mx > st[y].lim)) return;
-            mx = fmaxf(mx, __shfl_xor(mx, 32, 64));
+            if (!__any(top[y] > st[y].lim)) return;
+            const float mx = fmaxf(top[y], __shfl_xor(top[y], 32, 64));
             if (mx > st[y].lim) {
                 const float to = mx * a.scale_log2e, al = st[y].lim == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(st[y].mc - to);
                 st[y].l *= al;
@@ -943,18 +977,6 @@ __global__ void __launch_bounds__(256, 1) batch_attn_many_kernel(const bf16_t* _
                 st[y].lim = mx + kManyRoom / a.scale_log2e;
 #pragma unroll
                 for (int d = 0; d < DT; ++d) o[y][d] *= al;
-            }
-        };
-        // The order of a phase: a matrix instruction, and what a lane computes and reads meanwhile (0: scores and values from fragments that are there, 1: from LDS).
-        auto interleave = [](auto reads) {
-            constexpr int kMfma = 0x8, kValu = 0x2, kTrans = 0x400, kRead = 0x100;
-            if constexpr (reads.value) __builtin_amdgcn_sched_group_barrier(kRead, KS, 0);
-#pragma unroll
-            for (int i = 0; i < KS + 2 * DT; ++i) {
-                __builtin_amdgcn_sched_group_barrier(kMfma, 1, 0);
-                __builtin_amdgcn_sched_group_barrier(kTrans, 1, 0);
-                __builtin_amdgcn_sched_group_barrier(kValu, 4, 0);
-                if constexpr (reads.value) if (i < KS) __builtin_amdgcn_sched_group_barrier(kRead, 2, 0);
             }
         };
         auto weigh = [&](int y) {
@@ -967,25 +989,37 @@ __global__ void __launch_bounds__(256, 1) batch_attn_many_kernel(const bf16_t* _
 #pragma unroll
             for (int i = 0; i < 4; ++i) sum[i] = (w[i] + w[4 + i]) + (w[8 + i] + w[12 + i]);
             st[y].l += (sum[0] + sum[1]) + (sum[2] + sum[3]);
-            asm volatile("" : "+v"(pf[y][0]), "+v"(pf[y][1]), "+v"(st[y].l));      // (formed here, beside the matrix instructions, and not where they are used)
+        };
+        // The end of a phase: what it has formed is formed here, beside the matrix instructions, and not where it is used.  Its order: a matrix instruction, and what a lane computes and reads
+        // meanwhile.
+        auto close = [&](int y) {
+            asm volatile("" : "+v"(pf[y][0]), "+v"(pf[y][1]), "+v"(st[y].l), "+v"(top[1 - y]));
+            constexpr int kMfma = 0x8, kValu = 0x2, kTrans = 0x400, kRead = 0x100;
+#pragma unroll
+            for (int i = 0; i < KS + 2 * DT; ++i) {
+                __builtin_amdgcn_sched_group_barrier(kMfma, 1, 0);
+                __builtin_amdgcn_sched_group_barrier(kTrans, 1, 0);
+                __builtin_amdgcn_sched_group_barrier(kRead, 1, 0);
+                __builtin_amdgcn_sched_group_barrier(kValu, 4, 0);
+            }
         };
 
         int buffer = 0;
         if (now.any) {
-            bool whole = is_whole(now);
-            if (!whole) clear_odd(0);
+            if (!now.whole) clear_odd(0);
             fill(0);
             find(next);
             if (next.any) load(next);
             __syncthreads();
-            read_k(0, 0);
-            read_v(0, 0);
+            read_k(kf[0], 0, 0);
+            read_v(vf[0], 0, 0);
+            read_v(vf[1], 0, 0);
 #pragma unroll
             for (int m = 0; m < 2; ++m) pf[1][m] = bf16x8{};      // (the first turn's values of B: nothing, or undefined where they are undefined for all rows)
-            scores(0);
+            scores(0, kf[0]);
+            largest_of(0);
             while (true) {
                 const int ahead = buffer == 2 ? 0 : buffer + 1;
-                const bool next_whole = next.any && is_whole(next);
                 Keys behind;
                 behind.any = false;
 #pragma unroll
@@ -994,37 +1028,40 @@ __global__ void __launch_bounds__(256, 1) batch_attn_many_kernel(const bf16_t* _
                     for (int c = 0; c < KS; ++c) asm volatile("" : "+a"(qf[y][c]));      // (they stay among the accumulation registers, where matrix instructions read them too)
 #pragma unroll
                 for (int sub = 0; sub < 2; ++sub) {
-                    if (!whole) hide(0, now, buffer, sub);
+                    // A: weights; B: scores, values of the keys before; the next keys' K
+                    if (!now.whole) hide(0, now, buffer, sub);
                     settle(0);
-                    if (sub == 1 && next.any && !next_whole) clear_odd(ahead);
-                    scores(1);
-                    values(1);
+                    scores(1, kf[sub]);
+                    values(1, vf[1 - sub]);
                     weigh(0);
-                    if (sub == 1) fill(ahead);           // (behind the last keys: the last codes again, not used)
-                    interleave(std::integral_constant<int, 0>());
-                    if (sub == 1) {
+                    largest_of(1);
+                    read_k(kf[1 - sub], sub == 0 ? buffer : ahead, 1 - sub);      // (behind the last keys: whatever lies there, not used)
+                    close(0);
+                    if (sub == 0 && next.any && !next.whole) clear_odd(ahead);
+                    // B: weights; A: values, scores of the next keys; their V
+                    if (!now.whole) hide(1, now, buffer, sub);
+                    settle(1);
+                    scores(0, kf[1 - sub]);
+                    values(0, vf[sub]);
+                    weigh(1);
+                    largest_of(0);
+                    read_v(vf[1 - sub], sub == 0 ? buffer : ahead, 1 - sub);
+                    if (sub == 0) fill(ahead);           // (behind the last keys: the last codes again, not used)
+                    close(1);
+                    if (sub == 0) {
                         __syncthreads();
                         if (next.any) {
                             find(behind);
                             if (behind.any) load(behind);
                         }
                     }
-                    if (!whole) hide(1, now, buffer, sub);
-                    settle(1);
-                    read_k(sub == 0 ? buffer : ahead, 1 - sub);
-                    scores(0);
-                    read_v(buffer, sub);
-                    values(0);
-                    weigh(1);
-                    interleave(std::integral_constant<int, 1>());
                 }
                 if (!next.any) break;
                 now = next;
                 next = behind;
-                whole = next_whole;
                 buffer = ahead;
             }
-            values(1);
+            values(1, vf[1]);
         }
         __syncthreads();                                 // the buffers are read before they are written again
 
