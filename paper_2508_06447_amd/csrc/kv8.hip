@@ -688,13 +688,10 @@ __global__ void __launch_bounds__(64 * NW, sizeof(T) == 2 ? 3 : 2) batch_attn_kv
 // in nearly all turns.
 constexpr int kManyKeys = 64;
 template <int D> struct ManyTile {
-    static constexpr int kSide = kManyKeys * D * 2, kBuffer = 2 * kSide, kLdsBytes = 3 * kBuffer + 3 * 8;      // Keys or Values; both; three, and a bit for each key with a Value that is not a number
-    static constexpr int KS = D / 16, DT = D / 32, CH = D / 8;
-    // Byte offset of 16-byte piece c of key r.  The turn of the pieces spreads the reads of K (16 keys, one piece), the transposing ones of V (8 keys, four pieces) over all banks.
-    __device__ static __forceinline__ unsigned piece(int r, int c) {
-        const int turn = D == 128 ? (r << 1 & 14) | (r >> 3 & 1) : r & (CH - 1);
-        return (unsigned)(r * (D * 2) + ((c ^ turn) << 4));
-    }
+    // Rows of D bfloat16 and 32 bytes: eight keys' same piece, or four keys' same two, lie in different banks, and every address of a lane is one base and a constant.
+    static constexpr int kRow = D * 2 + 32, kSide = kManyKeys * kRow, kBuffer = 2 * kSide;      // a key; Keys or Values; both
+    static constexpr int kLdsBytes = 3 * kBuffer + 3 * 8;      // three, and a bit for each key with a Value that is not a number
+    static constexpr int KS = D / 16, DT = D / 32;
 };
 constexpr float kManyRoom = 30.f;
 
@@ -873,16 +870,13 @@ __global__ void __launch_bounds__(256, 1) batch_attn_many_kernel(const bf16_t* _
                 }
             }
         };
-        const unsigned fill_to = lds0 + Tile::piece(my_key, my_piece * 2);
-        auto fill = [&](int buffer) {
-#pragma unroll
-            for (int s = 0; s < NPASS; ++s) {
-                const unsigned at = buffer * Tile::kBuffer + s * (KPP * D * 2);
-                *(LdsB128)(fill_to + at) = kv8_to_bf16(make_uint2(kx[s].x, kx[s].y), kp[s]);
-                *(LdsB128)((fill_to ^ 16) + at) = kv8_to_bf16(make_uint2(kx[s].z, kx[s].w), kp[s]);
-                *(LdsB128)(fill_to + at + Tile::kSide) = kv8_to_bf16(make_uint2(vx[s].x, vx[s].y), vp[s]);
-                *(LdsB128)((fill_to ^ 16) + at + Tile::kSide) = kv8_to_bf16(make_uint2(vx[s].z, vx[s].w), vp[s]);
-            }
+        const unsigned fill_to = lds0 + my_key * Tile::kRow + my_piece * 32;
+        // A part of the keys' way into a buffer: eight channels of Keys (part 0, 1) or Values (2, 3) of a pass.
+        auto fill_part = [&](int buffer, int pass, int part) {
+            const uint4 c = part < 2 ? kx[pass] : vx[pass];
+            const unsigned to = fill_to + buffer * Tile::kBuffer;
+            *(LdsB128)(to + pass * (KPP * Tile::kRow) + part / 2 * Tile::kSide + part % 2 * 16) =
+                kv8_to_bf16(part % 2 ? make_uint2(c.z, c.w) : make_uint2(c.x, c.y), part < 2 ? kp[pass] : vp[pass]);
         };
 
         Keys now, next;
@@ -910,26 +904,16 @@ __global__ void __launch_bounds__(256, 1) batch_attn_many_kernel(const bf16_t* _
                 for (int i = 0; i < 16; ++i) o[y][d][i] = 0.f;
         }
         // Addresses of the lane in a buffer: K fragments (key l32, channels 16 c + 8 h: pieces 2 c + h), V fragments (keys 16 m + 4 h + .., channels 32 d + ..).
-        const unsigned k_from = lds0 + Tile::piece(l32, h);
-        const int s16 = lane & 15, v_row = 4 * h + (s16 >> 2);
-        const unsigned v_from = lds0 + Tile::kSide + Tile::piece(v_row, (lane >> 4 & 1) * 2 + ((s16 & 3) >> 1)) + (s16 & 1) * 8;
-        const unsigned v_from8 = lds0 + Tile::kSide + Tile::piece(v_row + 8, (lane >> 4 & 1) * 2 + ((s16 & 3) >> 1)) + (s16 & 1) * 8;
+        const unsigned k_from = lds0 + l32 * Tile::kRow + h * 16;
+        const unsigned v_from = lds0 + Tile::kSide + (4 * h + (lane >> 2 & 3)) * Tile::kRow + (lane >> 4 & 1) * 32 + (lane & 3) * 8;
         bf16x8 kf[2][KS], vf[2][DT][2], pf[2][2];        // of 32 keys, and of the next
         f32x16 s[2];
         float top[2];                                    // the lane's largest score
-        auto read_k = [&](bf16x8* k, int buffer, int sub) {
-#pragma unroll
-            for (int c = 0; c < KS; ++c) k[c] = *(LdsB128)((k_from ^ (c << 5)) + buffer * Tile::kBuffer + sub * (32 * D * 2));
-        };
-        auto read_v = [&](bf16x8 (*v)[2], int buffer, int sub) {
-#pragma unroll
-            for (int m = 0; m < 2; ++m)
-#pragma unroll
-                for (int d = 0; d < DT; ++d) {
-                    const bf16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4bf16((LdsB64)((v_from ^ (d << 6)) + buffer * Tile::kBuffer + (sub * 32 + m * 16) * (D * 2)));
-                    const bf16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4bf16((LdsB64)((v_from8 ^ (d << 6)) + buffer * Tile::kBuffer + (sub * 32 + m * 16) * (D * 2)));
-                    v[d][m] = __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
-                }
+        auto read_k = [&](bf16x8* k, int buffer, int sub, int c) { k[c] = *(LdsB128)(k_from + buffer * Tile::kBuffer + sub * (32 * Tile::kRow) + c * 32); };
+        auto read_v = [&](bf16x8 (*v)[2], int buffer, int sub, int d, int m) {
+            const unsigned from = v_from + buffer * Tile::kBuffer + (sub * 32 + m * 16) * Tile::kRow + d * 64;
+            const bf16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4bf16((LdsB64)from), hi = __builtin_amdgcn_ds_read_tr16_b64_v4bf16((LdsB64)(from + 8 * Tile::kRow));
+            v[d][m] = __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
         };
         auto largest_of = [&](int y) {
             float mx = s[y][0];
@@ -937,18 +921,13 @@ __global__ void __launch_bounds__(256, 1) batch_attn_many_kernel(const bf16_t* _
             for (int i = 1; i < 16; ++i) mx = fmaxf(mx, s[y][i]);
             top[y] = mx;
         };
-        auto scores = [&](int y, const bf16x8* k) {
+        auto score = [&](int y, const bf16x8* k, int c) {
+            if (c == 0)
 #pragma unroll
-            for (int i = 0; i < 16; ++i) s[y][i] = 0.f;
-#pragma unroll
-            for (int c = 0; c < KS; ++c) s[y] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(k[c], qf[y][c], s[y], 0, 0, 0);
+                for (int i = 0; i < 16; ++i) s[y][i] = 0.f;
+            s[y] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(k[c], qf[y][c], s[y], 0, 0, 0);
         };
-        auto values = [&](int y, const bf16x8 (*v)[2]) {
-#pragma unroll
-            for (int m = 0; m < 2; ++m)
-#pragma unroll
-                for (int d = 0; d < DT; ++d) o[y][d] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(v[d][m], pf[y][m], o[y][d], 0, 0, 0);
-        };
+        auto value = [&](int y, const bf16x8 (*v)[2], int m, int d) { o[y][d] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(v[d][m], pf[y][m], o[y][d], 0, 0, 0); };
         // What rows do not see of 32 keys; where values that are not numbers became zeros, a row that sees one of them is undefined by its sum.
         auto hide = [&](int y, const Keys& k, int buffer, int sub) {
             const unsigned odd = *reinterpret_cast<const uint32_t*>(lds + 3 * Tile::kBuffer + buffer * 8 + sub * 4);
@@ -979,44 +958,59 @@ __global__ void __launch_bounds__(256, 1) batch_attn_many_kernel(const bf16_t* _
                 for (int d = 0; d < DT; ++d) o[y][d] *= al;
             }
         };
-        auto weigh = [&](int y) {
-            float w[16];
+        // A phase: the weights of half y beside the other half's scores (k) and values (v), a matrix instruction (32 cycles) and what a lane computes meanwhile, in this order: a weight or two,
+        // the rounding and sum of those before, the largest of the new scores, and more(i): reads, conversions.
+        auto phase = [&](int y, const bf16x8* k, const bf16x8 (*v)[2], auto more) {
+            constexpr int NM = KS + 2 * DT, EP = 16 / NM;
+            const int z = 1 - y;
+            float w[16], sum[2] = {0.f, 0.f}, mx = 0.f;
+            uint32_t words[2][4];
+            auto round_pair = [&](int i) {
+                words[i / 4][i % 4] = pack_bf16x2(w[2 * i], w[2 * i + 1]);
+                sum[i % 2] += w[2 * i] + w[2 * i + 1];
+            };
 #pragma unroll
-            for (int i = 0; i < 16; ++i) w[i] = __builtin_amdgcn_exp2f(fmaf(s[y][i], a.scale_log2e, -st[y].mc));
+            for (int i = 0; i < NM; ++i) {
+                if (i < KS) score(z, k, i);
+                else value(z, v, (i - KS) / DT, (i - KS) % DT);
 #pragma unroll
-            for (int m = 0; m < 2; ++m) bf16_terms<1>(w + 8 * m, &pf[y][m]);
-            float sum[4];
+                for (int e = 0; e < EP; ++e) w[i * EP + e] = __builtin_amdgcn_exp2f(fmaf(s[y][i * EP + e], a.scale_log2e, -st[y].mc));
+                if (EP == 1 ? i >= 2 && i % 2 == 0 : i >= 1) round_pair(EP == 1 ? i / 2 - 1 : i - 1);
+                // from three instructions behind the last scores' on: 16 of them over the instructions that are left
+                constexpr int kFrom = KS + 2, kEach = (16 + NM - kFrom - 1) / (NM - kFrom);
+                if (i >= kFrom)
 #pragma unroll
-            for (int i = 0; i < 4; ++i) sum[i] = (w[i] + w[4 + i]) + (w[8 + i] + w[12 + i]);
-            st[y].l += (sum[0] + sum[1]) + (sum[2] + sum[3]);
-        };
-        // The end of a phase: what it has formed is formed here, beside the matrix instructions, and not where it is used.  Its order: a matrix instruction, and what a lane computes and reads
-        // meanwhile.
-        auto close = [&](int y) {
-            asm volatile("" : "+v"(pf[y][0]), "+v"(pf[y][1]), "+v"(st[y].l), "+v"(top[1 - y]));
-            constexpr int kMfma = 0x8, kValu = 0x2, kTrans = 0x400, kRead = 0x100;
-#pragma unroll
-            for (int i = 0; i < KS + 2 * DT; ++i) {
-                __builtin_amdgcn_sched_group_barrier(kMfma, 1, 0);
-                __builtin_amdgcn_sched_group_barrier(kTrans, 1, 0);
-                __builtin_amdgcn_sched_group_barrier(kRead, 1, 0);
-                __builtin_amdgcn_sched_group_barrier(kValu, 4, 0);
+                    for (int e = (i - kFrom) * kEach; e < (i - kFrom + 1) * kEach && e < 16; ++e) mx = e == 0 ? s[z][0] : fmaxf(mx, s[z][e]);
+                more(i);
+                __builtin_amdgcn_sched_barrier(0);
             }
+            round_pair(7);
+            top[z] = mx;
+            st[y].l += sum[0] + sum[1];
+#pragma unroll
+            for (int m = 0; m < 2; ++m) pf[y][m] = __builtin_bit_cast(bf16x8, make_uint4(words[m][0], words[m][1], words[m][2], words[m][3]));
+            asm volatile("" : "+v"(pf[y][0]), "+v"(pf[y][1]), "+v"(st[y].l), "+v"(top[z]));      // (formed here and not where it is used)
         };
 
         int buffer = 0;
         if (now.any) {
             if (!now.whole) clear_odd(0);
-            fill(0);
+#pragma unroll
+            for (int i = 0; i < 4 * NPASS; ++i) fill_part(0, i / 4, i % 4);
             find(next);
             if (next.any) load(next);
             __syncthreads();
-            read_k(kf[0], 0, 0);
-            read_v(vf[0], 0, 0);
-            read_v(vf[1], 0, 0);
+#pragma unroll
+            for (int c = 0; c < KS; ++c) read_k(kf[0], 0, 0, c);
+#pragma unroll
+            for (int i = 0; i < 2 * DT; ++i) {
+                read_v(vf[0], 0, 0, i % DT, i / DT);
+                vf[1][i % DT][i / DT] = vf[0][i % DT][i / DT];
+            }
 #pragma unroll
             for (int m = 0; m < 2; ++m) pf[1][m] = bf16x8{};      // (the first turn's values of B: nothing, or undefined where they are undefined for all rows)
-            scores(0, kf[0]);
+#pragma unroll
+            for (int c = 0; c < KS; ++c) score(0, kf[0], c);
             largest_of(0);
             while (true) {
                 const int ahead = buffer == 2 ? 0 : buffer + 1;
@@ -1031,23 +1025,17 @@ __global__ void __launch_bounds__(256, 1) batch_attn_many_kernel(const bf16_t* _
                     // A: weights; B: scores, values of the keys before; the next keys' K
                     if (!now.whole) hide(0, now, buffer, sub);
                     settle(0);
-                    scores(1, kf[sub]);
-                    values(1, vf[1 - sub]);
-                    weigh(0);
-                    largest_of(1);
-                    read_k(kf[1 - sub], sub == 0 ? buffer : ahead, 1 - sub);      // (behind the last keys: whatever lies there, not used)
-                    close(0);
+                    phase(0, kf[sub], vf[1 - sub], [&](int i) {
+                        if (i < KS) read_k(kf[1 - sub], sub == 0 ? buffer : ahead, 1 - sub, i);      // (behind the last keys: whatever lies there, not used)
+                    });
                     if (sub == 0 && next.any && !next.whole) clear_odd(ahead);
                     // B: weights; A: values, scores of the next keys; their V
                     if (!now.whole) hide(1, now, buffer, sub);
                     settle(1);
-                    scores(0, kf[1 - sub]);
-                    values(0, vf[sub]);
-                    weigh(1);
-                    largest_of(0);
-                    read_v(vf[1 - sub], sub == 0 ? buffer : ahead, 1 - sub);
-                    if (sub == 0) fill(ahead);           // (behind the last keys: the last codes again, not used)
-                    close(1);
+                    phase(1, kf[1 - sub], vf[sub], [&](int i) {
+                        if (i < 2 * DT) read_v(vf[1 - sub], sub == 0 ? buffer : ahead, 1 - sub, i % DT, i / DT);
+                        else if (sub == 0 && i - 2 * DT < 4 * NPASS) fill_part(ahead, (i - 2 * DT) / 4, (i - 2 * DT) % 4);      // (behind the last keys: the last codes again, not used)
+                    });
                     if (sub == 0) {
                         __syncthreads();
                         if (next.any) {
@@ -1061,7 +1049,8 @@ __global__ void __launch_bounds__(256, 1) batch_attn_many_kernel(const bf16_t* _
                 next = behind;
                 buffer = ahead;
             }
-            values(1, vf[1]);
+#pragma unroll
+            for (int i = 0; i < 2 * DT; ++i) value(1, vf[1], i / DT, i % DT);
         }
         __syncthreads();                                 // the buffers are read before they are written again
 
