@@ -968,19 +968,25 @@ __global__ void __launch_bounds__(256, 1) batch_attn_many_kernel(const bf16_t* _
             auto round_pair = [&](int i) {
                 words[i / 4][i % 4] = pack_bf16x2(w[2 * i], w[2 * i + 1]);
                 sum[i % 2] += w[2 * i] + w[2 * i + 1];
+                asm volatile("" : "+v"(words[i / 4][i % 4]), "+v"(sum[i % 2]));
             };
 #pragma unroll
             for (int i = 0; i < NM; ++i) {
                 if (i < KS) score(z, k, i);
                 else value(z, v, (i - KS) / DT, (i - KS) % DT);
 #pragma unroll
-                for (int e = 0; e < EP; ++e) w[i * EP + e] = __builtin_amdgcn_exp2f(fmaf(s[y][i * EP + e], a.scale_log2e, -st[y].mc));
+                for (int e = 0; e < EP; ++e) {
+                    w[i * EP + e] = __builtin_amdgcn_exp2f(fmaf(s[y][i * EP + e], a.scale_log2e, -st[y].mc));
+                    asm volatile("" : "+v"(w[i * EP + e]));      // (formed in this place)
+                }
                 if (EP == 1 ? i >= 2 && i % 2 == 0 : i >= 1) round_pair(EP == 1 ? i / 2 - 1 : i - 1);
                 // from three instructions behind the last scores' on: 16 of them over the instructions that are left
                 constexpr int kFrom = KS + 2, kEach = (16 + NM - kFrom - 1) / (NM - kFrom);
-                if (i >= kFrom)
+                if (i >= kFrom) {
 #pragma unroll
                     for (int e = (i - kFrom) * kEach; e < (i - kFrom + 1) * kEach && e < 16; ++e) mx = e == 0 ? s[z][0] : fmaxf(mx, s[z][e]);
+                    asm volatile("" : "+v"(mx));
+                }
                 more(i);
                 __builtin_amdgcn_sched_barrier(0);
             }
