@@ -690,7 +690,7 @@ constexpr int kManyKeys = 64;
 template <int D> struct ManyTile {
     // Rows of D bfloat16 and 32 bytes: eight keys' same piece, or four keys' same two, lie in different banks, and every address of a lane is one base and a constant.
     static constexpr int kRow = D * 2 + 32, kSide = kManyKeys * kRow, kBuffer = 2 * kSide;      // a key; Keys or Values; both
-    static constexpr int kLdsBytes = 3 * kBuffer + 3 * 8;      // three, and a bit for each key with a Value that is not a number
+    static constexpr int kFlags = 3 * kBuffer, kLists = kFlags + 32, kLdsBytes = kLists + 4 * 64 * 16;      // three; a bit for each of their keys with a Value that is not a number; a wave's pieces
     static constexpr int KS = D / 16, DT = D / 32;
 };
 constexpr float kManyRoom = 30.f;
@@ -763,90 +763,68 @@ __global__ void __launch_bounds__(256, 1) batch_attn_many_kernel(const bf16_t* _
         auto piece_at = [&](long long c) { return c >= tile_cost ? last : (int)((double)last * ((double)c / (double)tile_cost)); };
         const int u_begin = piece_at(from_cost), u_end = piece_at(from_cost + take);
 
-        // The pieces, four at a time, looked up 64 at once by every wave for itself, one a lane: where the Keys begin, exponents, rows, position.  Slots are requested two lookups ahead,
-        // exponents one.
-        int u = u_begin + lane, batch = u_begin - 64, u_pos = 0, u_rows = 0;
-        unsigned u_low = 0, u_high = 0;
-        uint32_t u_e = 0;
+        // The pieces, looked up 64 at once by every wave for itself, one a lane; those with keys are listed in LDS: where the Keys begin, exponents | rows << 16 | 1 << 24 if there are 16 which all
+        // rows of the tile see, position.  Four make 64 keys; the list is filled up with pieces without rows.  Slots are requested two lookups ahead, exponents one.
+        int u = u_begin + lane, batch = u_begin - 64;
         auto slot_at = [&](int u) { return u < u_end ? table[a.by_piece(u)] : -1; };
         auto exponents_at = [&](int slot) {
             return slot >= 0 && slot < a.n_slots ? *reinterpret_cast<const uint16_t*>(a.pool + (size_t)slot * a.slot_bytes + a.layer_offset + head.e) : (uint16_t)0;
         };
         int slot_1 = slot_at(u), slot_2 = slot_at(u + 64);
         uint32_t e_1 = exponents_at(slot_1);
-        unsigned long long left = 0, full = 0;           // lanes whose pieces hold keys and have not been taken; that hold 16 which all rows see
-        struct Keys {
-            bool any, whole;
-            const unsigned char* from[NPASS];            // of the piece that the wave's keys lie in, in either pass
-            int rows[NPASS];
-            uint32_t e[NPASS];
-            int have[4], pos[4];                         // unless whole
-        };
-        auto find = [&](Keys& k) {
-            while (!left) {
+        uint4* list = reinterpret_cast<uint4*>(lds + Tile::kLists) + wave * 64;
+        int at_list = 0, n_list = 0;                     // in fours
+        auto advance = [&]() {                           // to the next four; false: there are none, and the last ones stay
+            if (at_list + 1 < n_list) {
+                ++at_list;
+                return true;
+            }
+            while (true) {
                 batch += 64;
-                if (batch >= u_end) {
-                    k.any = false;
-                    return;
-                }
-                const int b = a.by_piece(u), row = (u - b * a.per_block) * kPiece;
-                u_pos = b * a.block + row;
-                u_rows = slot_1 >= 0 && slot_1 < a.n_slots ? min(kPiece, min(a.block - row, limit - u_pos)) : 0;
+                if (batch >= u_end) return false;
+                const int b = a.by_piece(u), row = (u - b * a.per_block) * kPiece, pos = b * a.block + row;
+                const int rows = slot_1 >= 0 && slot_1 < a.n_slots ? min(kPiece, min(a.block - row, limit - pos)) : 0;
                 const size_t from = (size_t)a.pool + (size_t)max(slot_1, 0) * a.slot_bytes + a.layer_offset + head.k + (size_t)row * D;
-                u_low = (unsigned)from;
-                u_high = (unsigned)(from >> 32);
-                u_e = e_1;
-                left = __ballot(u_rows > 0);
-                full = __ballot(u_rows == kPiece && u_pos + kPiece - 1 <= p0);
+                const uint4 entry = make_uint4((unsigned)from, (unsigned)(from >> 32), e_1 | (unsigned)max(rows, 0) << 16 | (rows == kPiece && pos + kPiece - 1 <= p0 ? 1u << 24 : 0u), (unsigned)pos);
                 u += 64;
                 e_1 = exponents_at(slot_2);
                 slot_1 = slot_2;
                 slot_2 = slot_at(u + 64);
-            }
-            k.any = true;
-            int i[4];
-            unsigned long long taken = 0;
-#pragma unroll
-            for (int j = 0; j < 4; ++j) {
-                i[j] = left ? __builtin_ctzll(left) : -1;
-                const unsigned long long bit = left & (0 - left);
-                taken |= bit;
-                left ^= bit;
-            }
-            k.whole = i[3] >= 0 && (taken & ~full) == 0;
-#pragma unroll
-            for (int s = 0; s < NPASS; ++s) {
-                const int j = NPASS == 1 ? wave : (wave >> 1) + 2 * s;
-                int x = j == 0 ? i[0] : j == 1 ? i[1] : j == 2 ? i[2] : i[3];
-                if (x < 0) x = i[0];                     // fewer than four: the first one again, unseen
-                k.from[s] = (const unsigned char*)((size_t)(unsigned)__builtin_amdgcn_readlane(u_high, x) << 32 | (unsigned)__builtin_amdgcn_readlane(u_low, x));
-                k.rows[s] = __builtin_amdgcn_readlane(u_rows, x);
-                k.e[s] = __builtin_amdgcn_readlane(u_e, x);
-            }
-            if (!k.whole) {
-#pragma unroll
-                for (int j = 0; j < 4; ++j) {
-                    const int x = max(i[j], 0);
-                    k.have[j] = i[j] < 0 ? 0 : __builtin_amdgcn_readlane(u_rows, x);
-                    k.pos[j] = __builtin_amdgcn_readlane(u_pos, x);
-                }
+                const unsigned long long have = __ballot(rows > 0);
+                if (!have) continue;
+                const int count = __builtin_popcountll(have), number = __builtin_amdgcn_mbcnt_hi((unsigned)(have >> 32), __builtin_amdgcn_mbcnt_lo((unsigned)have, 0));
+                if (rows > 0) list[number] = entry;
+                n_list = (count + 3) / 4;
+                at_list = 0;
+                if (rows > 0 && number == 0)
+                    for (int i = count; i < n_list * 4; ++i) list[i] = make_uint4(entry.x, entry.y, entry.z & 0xffffu, entry.w);
+                return true;
             }
         };
         // A thread's codes of the next 64 keys: 16 channels of key tid / PR, and of one KPP further on.
         const int my_key = threadIdx.x / PR, my_piece = threadIdx.x % PR;
         const size_t values_apart = head.v - head.k;
-        uint4 kx[NPASS], vx[NPASS];
+        uint4 kx[NPASS], vx[NPASS], entry[NPASS];
         float kp[NPASS], vp[NPASS];
-        auto load = [&](const Keys& k) {
+        uint2 info_behind;                               // of lanes 0 .. 3: exponents, rows, position
+        auto read_list = [&]() {
+#pragma unroll
+            for (int s = 0; s < NPASS; ++s) entry[s] = list[at_list * 4 + (NPASS == 1 ? wave : (wave >> 1) + 2 * s)];
+            const uint4 e = list[at_list * 4 + (lane & 3)];
+            info_behind = make_uint2(e.z, e.w);
+        };
+        auto load = [&]() {
 #pragma unroll
             for (int s = 0; s < NPASS; ++s) {
-                const unsigned off = min(my_key & 15, k.rows[s] - 1) * D + my_piece * 16;
-                kx[s] = *reinterpret_cast<const uint4*>(k.from[s] + off);
-                vx[s] = *reinterpret_cast<const uint4*>(k.from[s] + values_apart + off);
-                kp[s] = kv8_power(k.e[s] & 0xffu);
-                vp[s] = kv8_power(k.e[s] >> 8);
+                const unsigned char* from = (const unsigned char*)((size_t)entry[s].y << 32 | entry[s].x);
+                const unsigned off = min(my_key & 15, max((int)(entry[s].z >> 16 & 31u), 1) - 1) * D + my_piece * 16;
+                kx[s] = *reinterpret_cast<const uint4*>(from + off);
+                vx[s] = *reinterpret_cast<const uint4*>(from + values_apart + off);
+                kp[s] = kv8_power(entry[s].z & 0xffu);
+                vp[s] = kv8_power(entry[s].z >> 8 & 0xffu);
             }
         };
+        auto all_full = [](const uint2& info) { return (__ballot(info.x >> 24 & 1u) & 15u) == 15u; };
         // Values of the next keys that are not numbers become zeros, a bit each, where some row does not see all of them (as for few rows).
         auto clear_odd = [&](int buffer) {
 #pragma unroll
@@ -863,7 +841,7 @@ __global__ void __launch_bounds__(256, 1) batch_attn_many_kernel(const bf16_t* _
                 unsigned bits = 0;                       // of the wave's 64 / PR keys
 #pragma unroll
                 for (int i = 0; i < 64 / PR; ++i) bits |= (lanes >> (i * PR) & ((1ull << PR) - 1)) ? 1u << i : 0u;
-                unsigned char* flags = lds + 3 * Tile::kBuffer + buffer * 8 + s * (KPP / 8);
+                unsigned char* flags = lds + Tile::kFlags + buffer * 8 + s * (KPP / 8);
                 if (lane == 0) {
                     if constexpr (PR == 8) flags[wave] = (unsigned char)bits;
                     else *reinterpret_cast<uint16_t*>(flags + wave * 2) = (uint16_t)bits;
@@ -879,9 +857,11 @@ __global__ void __launch_bounds__(256, 1) batch_attn_many_kernel(const bf16_t* _
                 kv8_to_bf16(part % 2 ? make_uint2(c.z, c.w) : make_uint2(c.x, c.y), part < 2 ? kp[pass] : vp[pass]);
         };
 
-        Keys now, next;
-        find(now);
-        if (now.any) load(now);
+        const bool any = advance();
+        if (any) {
+            read_list();
+            load();
+        }
         // Query fragments: the lane's row of either half, channels 16 c + 8 h ..
         bf16x8 qf[2][KS];
         int pos_of[2];                                   // of the lane's row
@@ -929,12 +909,12 @@ __global__ void __launch_bounds__(256, 1) batch_attn_many_kernel(const bf16_t* _
         };
         auto value = [&](int y, const bf16x8 (*v)[2], int m, int d) { o[y][d] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(v[d][m], pf[y][m], o[y][d], 0, 0, 0); };
         // What rows do not see of 32 keys; where values that are not numbers became zeros, a row that sees one of them is undefined by its sum.
-        auto hide = [&](int y, const Keys& k, int buffer, int sub) {
-            const unsigned odd = *reinterpret_cast<const uint32_t*>(lds + 3 * Tile::kBuffer + buffer * 8 + sub * 4);
+        auto hide = [&](int y, const uint2& info, int buffer, int sub) {
+            const unsigned odd = *reinterpret_cast<const uint32_t*>(lds + Tile::kFlags + buffer * 8 + sub * 4);
             unsigned seen_keys = 0;
 #pragma unroll
             for (int j = 0; j < 2; ++j) {
-                const int seen = min(k.have[sub * 2 + j], pos_of[y] + 1 - k.pos[sub * 2 + j]);
+                const int seen = min((int)((unsigned)__builtin_amdgcn_readlane(info.x, sub * 2 + j) >> 16 & 31u), pos_of[y] + 1 - __builtin_amdgcn_readlane(info.y, sub * 2 + j));
                 seen_keys |= ((1u << max(seen, 0)) - 1u) << (16 * j);
 #pragma unroll
                 for (int i = 0; i < 8; ++i) {
@@ -999,12 +979,17 @@ __global__ void __launch_bounds__(256, 1) batch_attn_many_kernel(const bf16_t* _
         };
 
         int buffer = 0;
-        if (now.any) {
-            if (!now.whole) clear_odd(0);
+        if (any) {
+            uint2 info = info_behind, info_next;
+            bool whole = all_full(info);
+            if (!whole) clear_odd(0);
 #pragma unroll
             for (int i = 0; i < 4 * NPASS; ++i) fill_part(0, i / 4, i % 4);
-            find(next);
-            if (next.any) load(next);
+            bool next = advance();
+            read_list();
+            load();
+            info_next = info_behind;
+            bool next_whole = all_full(info_next);
             __syncthreads();
 #pragma unroll
             for (int c = 0; c < KS; ++c) read_k(kf[0], 0, 0, c);
@@ -1020,8 +1005,7 @@ __global__ void __launch_bounds__(256, 1) batch_attn_many_kernel(const bf16_t* _
             largest_of(0);
             while (true) {
                 const int ahead = buffer == 2 ? 0 : buffer + 1;
-                Keys behind;
-                behind.any = false;
+                bool behind = false;
 #pragma unroll
                 for (int y = 0; y < 2; ++y)
 #pragma unroll
@@ -1029,29 +1013,31 @@ __global__ void __launch_bounds__(256, 1) batch_attn_many_kernel(const bf16_t* _
 #pragma unroll
                 for (int sub = 0; sub < 2; ++sub) {
                     // A: weights; B: scores, values of the keys before; the next keys' K
-                    if (!now.whole) hide(0, now, buffer, sub);
+                    if (!whole) hide(0, info, buffer, sub);
                     settle(0);
                     phase(0, kf[sub], vf[1 - sub], [&](int i) {
                         if (i < KS) read_k(kf[1 - sub], sub == 0 ? buffer : ahead, 1 - sub, i);      // (behind the last keys: whatever lies there, not used)
+                        if (sub == 1 && i == KS) load();      // (behind the last keys: the last codes again, not used)
                     });
-                    if (sub == 0 && next.any && !next.whole) clear_odd(ahead);
+                    if (sub == 0 && !next_whole) clear_odd(ahead);
                     // B: weights; A: values, scores of the next keys; their V
-                    if (!now.whole) hide(1, now, buffer, sub);
+                    if (!whole) hide(1, info, buffer, sub);
                     settle(1);
                     phase(1, kf[1 - sub], vf[sub], [&](int i) {
                         if (i < 2 * DT) read_v(vf[1 - sub], sub == 0 ? buffer : ahead, 1 - sub, i % DT, i / DT);
-                        else if (sub == 0 && i - 2 * DT < 4 * NPASS) fill_part(ahead, (i - 2 * DT) / 4, (i - 2 * DT) % 4);      // (behind the last keys: the last codes again, not used)
+                        else if (sub == 0 && i - 2 * DT < 4 * NPASS) fill_part(ahead, (i - 2 * DT) / 4, (i - 2 * DT) % 4);
                     });
                     if (sub == 0) {
                         __syncthreads();
-                        if (next.any) {
-                            find(behind);
-                            if (behind.any) load(behind);
-                        }
+                        behind = next && advance();
+                        read_list();
                     }
                 }
-                if (!next.any) break;
-                now = next;
+                if (!next) break;
+                info = info_next;
+                info_next = info_behind;
+                whole = next_whole;
+                next_whole = all_full(info_next);
                 next = behind;
                 buffer = ahead;
             }
