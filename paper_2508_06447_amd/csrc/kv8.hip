@@ -676,33 +676,27 @@ __global__ void __launch_bounds__(64 * NW, sizeof(T) == 2 ? 3 : 2) batch_attn_kv
 }
 
 // ---- requests of many rows (bfloat16)
-// Tiles of 256 rows, 64 a wave; the four waves turn 64 keys at a time into bfloat16 in LDS, once for all of them, and each forms, in 32x32x16 matrix instructions,
-//   S^T[key, row] = K . Q^T       32 keys of 32 rows; the lane (l32, h) = (lane % 32, lane / 32) is left scores of row l32: keys 8 i + 4 h + 0 .. 3, i < 4
+// Tiles of 256 rows, 32 a wave; the eight waves turn 64 keys at a time into bfloat16 in LDS, once for all of them, and each forms, in 32x32x16 matrix instructions,
+//   S^T[key, row] = K . Q^T       32 keys; the lane (l32, h) = (lane % 32, lane / 32) is left scores of row l32: keys 8 i + 4 h + 0 .. 3, i < 4
 //   O^T[d, row]   = V^T . P^T     whose operand P^T is what the lane holds: V comes through the transposing read in the same order of keys
-// The two halves A and B of a wave's rows are half a turn apart, so that the exponentials of one always stand beside matrix instructions of the other:
-//   softmax A | scores of B, values of B before        softmax B | values of A, scores of A behind
-// which also use the same fragments of K and V right after each other: LDS is read once for both.
-// Three buffers of 64 keys: one is read, one is filled, one may still be read by a slower wave; a barrier each 64 keys.
-// A weight is one bfloat16 (off by 2^-9 of itself at most, as the output is in the end), and the sum is that of the unrounded ones.  The reference of a row's weights is the
-// largest score when it was set, and is set anew only when a score is more than 2^30 above it: float32 and bfloat16 have room for that on both sides, and the results need no rescaling
-// in nearly all turns.
+// A phase stands for 32 keys: their weights, beside the scores of the 32 behind and the values of the 32 before, a matrix instruction and a lane's arithmetic in turn.  It reads the Values in its
+// first half, the Keys of the next phase in its second.  Four buffers of 64 keys: Values of the keys before, the present and the next keys, and the ones being filled; a barrier each 64 keys.
+// A weight is one bfloat16 (off by 2^-9 of itself at most, as the output is in the end), and the sum is that of the unrounded ones.  The reference of a row's weights is a power of
+// two at the largest score when it was set, and is set anew only when a score is more than 2^30 above it: float32 and bfloat16 have room for that on both sides, and nothing is
+// rescaled in nearly all phases.
 constexpr int kManyKeys = 64;
 template <int D> struct ManyTile {
     // Rows of D bfloat16 and 32 bytes: eight keys' same piece, or four keys' same two, lie in different banks, and every address of a lane is one base and a constant.
     static constexpr int kRow = D * 2 + 32, kSide = kManyKeys * kRow, kBuffer = 2 * kSide;      // a key; Keys or Values; both
-    static constexpr int kFlags = 3 * kBuffer, kLists = kFlags + 32, kLdsBytes = kLists + 4 * 64 * 16;      // three; a bit for each of their keys with a Value that is not a number; a wave's pieces
+    static constexpr int kFlags = 4 * kBuffer, kLists = kFlags + 32, kLdsBytes = kLists + 8 * 64 * 16;      // four; a bit for each of their keys with a Value that is not a number; a wave's pieces
     static constexpr int KS = D / 16, DT = D / 32;
 };
 constexpr float kManyRoom = 30.f;
 
-struct ManyRows {                                        // half of a wave's rows: the lane's share of row l32
-    float mc, lim, l;                                    // reference in the base-2 domain, score above which it moves, sum
-};
-
 template <int D>
-__global__ void __launch_bounds__(256, 1) batch_attn_many_kernel(const bf16_t* __restrict__ q, bf16_t* __restrict__ out, BatchAttnArgs a) {
+__global__ void __launch_bounds__(512, 2) batch_attn_many_kernel(const bf16_t* __restrict__ q, bf16_t* __restrict__ out, BatchAttnArgs a) {
     typedef ManyTile<D> Tile;
-    constexpr int KS = Tile::KS, DT = Tile::DT, PR = D / 16, KPP = 256 / PR, NPASS = kManyKeys / KPP;      // 16-byte pieces of a key's codes, keys a pass, passes
+    constexpr int KS = Tile::KS, DT = Tile::DT, PR = D / 16;      // PR: 16-byte pieces of a key's codes
     extern __shared__ __align__(16) unsigned char lds[];
     const int G = a.Hq / a.Hkv, g = blockIdx.x % a.Hkv, share_of = blockIdx.x / a.Hkv, shares = gridDim.x / a.Hkv;
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), l32 = lane & 31, h = lane >> 5;
@@ -801,60 +795,53 @@ __global__ void __launch_bounds__(256, 1) batch_attn_many_kernel(const bf16_t* _
                 return true;
             }
         };
-        // A thread's codes of the next 64 keys: 16 channels of key tid / PR, and of one KPP further on.
+        // A thread's codes of 64 keys: 16 channels of key tid / PR (of heads of 64 the first half of the threads).
         const int my_key = threadIdx.x / PR, my_piece = threadIdx.x % PR;
+        const bool mine = D == 128 || my_key < kManyKeys;
         const size_t values_apart = head.v - head.k;
-        uint4 kx[NPASS], vx[NPASS], entry[NPASS];
-        float kp[NPASS], vp[NPASS];
-        uint2 info_behind;                               // of lanes 0 .. 3: exponents, rows, position
+        uint4 kx, vx, entry;
+        float kp, vp;
+        uint2 info_new;                                  // of lanes 0 .. 3: exponents, rows, position
         auto read_list = [&]() {
-#pragma unroll
-            for (int s = 0; s < NPASS; ++s) entry[s] = list[at_list * 4 + (NPASS == 1 ? wave : (wave >> 1) + 2 * s)];
+            entry = list[at_list * 4 + (D == 128 ? wave >> 1 : wave & 3)];
             const uint4 e = list[at_list * 4 + (lane & 3)];
-            info_behind = make_uint2(e.z, e.w);
+            info_new = make_uint2(e.z, e.w);
         };
         auto load = [&]() {
-#pragma unroll
-            for (int s = 0; s < NPASS; ++s) {
-                const unsigned char* from = (const unsigned char*)((size_t)entry[s].y << 32 | entry[s].x);
-                const unsigned off = min(my_key & 15, max((int)(entry[s].z >> 16 & 31u), 1) - 1) * D + my_piece * 16;
-                kx[s] = *reinterpret_cast<const uint4*>(from + off);
-                vx[s] = *reinterpret_cast<const uint4*>(from + values_apart + off);
-                kp[s] = kv8_power(entry[s].z & 0xffu);
-                vp[s] = kv8_power(entry[s].z >> 8 & 0xffu);
-            }
+            const unsigned char* from = (const unsigned char*)((size_t)entry.y << 32 | entry.x);
+            const unsigned off = min(my_key & 15, max((int)(entry.z >> 16 & 31u), 1) - 1) * D + my_piece * 16;
+            kx = *reinterpret_cast<const uint4*>(from + off);
+            vx = *reinterpret_cast<const uint4*>(from + values_apart + off);
+            kp = kv8_power(entry.z & 0xffu);
+            vp = kv8_power(entry.z >> 8 & 0xffu);
         };
         auto all_full = [](const uint2& info) { return (__ballot(info.x >> 24 & 1u) & 15u) == 15u; };
         // Values of the next keys that are not numbers become zeros, a bit each, where some row does not see all of them (as for few rows).
         auto clear_odd = [&](int buffer) {
+            bool odd = false;
 #pragma unroll
-            for (int s = 0; s < NPASS; ++s) {
-                bool odd = false;
+            for (int i = 0; i < 4; ++i) {
+                uint32_t& x = i == 0 ? vx.x : i == 1 ? vx.y : i == 2 ? vx.z : vx.w;
+                const uint32_t bytes = (((x & 0x7f7f7f7fu) + 0x01010101u) >> 7 & 0x01010101u) * 0xffu;
+                odd |= bytes != 0;
+                x &= ~bytes;
+            }
+            const unsigned long long lanes = __ballot(odd);
+            unsigned bits = 0;                           // of the wave's 64 / PR keys
 #pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    uint32_t& x = i == 0 ? vx[s].x : i == 1 ? vx[s].y : i == 2 ? vx[s].z : vx[s].w;
-                    const uint32_t bytes = (((x & 0x7f7f7f7fu) + 0x01010101u) >> 7 & 0x01010101u) * 0xffu;
-                    odd |= bytes != 0;
-                    x &= ~bytes;
-                }
-                const unsigned long long lanes = __ballot(odd);
-                unsigned bits = 0;                       // of the wave's 64 / PR keys
-#pragma unroll
-                for (int i = 0; i < 64 / PR; ++i) bits |= (lanes >> (i * PR) & ((1ull << PR) - 1)) ? 1u << i : 0u;
-                unsigned char* flags = lds + Tile::kFlags + buffer * 8 + s * (KPP / 8);
-                if (lane == 0) {
-                    if constexpr (PR == 8) flags[wave] = (unsigned char)bits;
-                    else *reinterpret_cast<uint16_t*>(flags + wave * 2) = (uint16_t)bits;
-                }
+            for (int i = 0; i < 64 / PR; ++i) bits |= (lanes >> (i * PR) & ((1ull << PR) - 1)) ? 1u << i : 0u;
+            unsigned char* flags = lds + Tile::kFlags + buffer * 8;
+            if (lane == 0 && mine) {
+                if constexpr (D == 128) flags[wave] = (unsigned char)bits;
+                else *reinterpret_cast<uint16_t*>(flags + wave * 2) = (uint16_t)bits;
             }
         };
         const unsigned fill_to = lds0 + my_key * Tile::kRow + my_piece * 32;
-        // A part of the keys' way into a buffer: eight channels of Keys (part 0, 1) or Values (2, 3) of a pass.
-        auto fill_part = [&](int buffer, int pass, int part) {
-            const uint4 c = part < 2 ? kx[pass] : vx[pass];
-            const unsigned to = fill_to + buffer * Tile::kBuffer;
-            *(LdsB128)(to + pass * (KPP * Tile::kRow) + part / 2 * Tile::kSide + part % 2 * 16) =
-                kv8_to_bf16(part % 2 ? make_uint2(c.z, c.w) : make_uint2(c.x, c.y), part < 2 ? kp[pass] : vp[pass]);
+        // A part of the keys' way into a buffer: eight channels of Keys (part 0, 1) or Values (2, 3).
+        auto fill_part = [&](int buffer, int part) {
+            const uint4 c = part < 2 ? kx : vx;
+            const bf16x8 x = kv8_to_bf16(part % 2 ? make_uint2(c.z, c.w) : make_uint2(c.x, c.y), part < 2 ? kp : vp);
+            if (mine) *(LdsB128)(fill_to + buffer * Tile::kBuffer + part / 2 * Tile::kSide + part % 2 * 16) = x;
         };
 
         const bool any = advance();
@@ -862,38 +849,29 @@ __global__ void __launch_bounds__(256, 1) batch_attn_many_kernel(const bf16_t* _
             read_list();
             load();
         }
-        // Query fragments: the lane's row of either half, channels 16 c + 8 h ..
-        bf16x8 qf[2][KS];
-        int pos_of[2];                                   // of the lane's row
+        // Query fragments: the lane's row, channels 16 c + 8 h ..
+        const int lrow = row0 + min(wave * 32 + l32, rows - 1), token = a.by_group(lrow), my_pos = before + token;
+        const bf16_t* q_row = q + (size_t)(me.lo + token) * a.ldq + (size_t)(g * G + lrow - token * G) * D + h * 8;
+        bf16x8 qf[KS];
 #pragma unroll
-        for (int y = 0; y < 2; ++y) {
-            const int lrow = row0 + min(wave * 64 + y * 32 + l32, rows - 1), token = a.by_group(lrow);
-            pos_of[y] = before + token;
-            const bf16_t* src = q + (size_t)(me.lo + token) * a.ldq + (size_t)(g * G + lrow - token * G) * D + h * 8;
+        for (int c = 0; c < KS; ++c) qf[c] = *reinterpret_cast<const bf16x8*>(q_row + c * 16);
+        f32x16 o[DT];
 #pragma unroll
-            for (int c = 0; c < KS; ++c) qf[y][c] = *reinterpret_cast<const bf16x8*>(src + c * 16);
-        }
-        f32x16 o[2][DT];
-        ManyRows st[2];
+        for (int d = 0; d < DT; ++d)
 #pragma unroll
-        for (int y = 0; y < 2; ++y) {
-            st[y] = ManyRows{0.f, -INFINITY, 0.f};
-#pragma unroll
-            for (int d = 0; d < DT; ++d)
-#pragma unroll
-                for (int i = 0; i < 16; ++i) o[y][d][i] = 0.f;
-        }
+            for (int i = 0; i < 16; ++i) o[d][i] = 0.f;
+        float mc = 0.f, lim = -INFINITY, l = 0.f;        // of row l32: reference in the base-2 domain, score above which it moves, the lane's share of the sum
         // Addresses of the lane in a buffer: K fragments (key l32, channels 16 c + 8 h: pieces 2 c + h), V fragments (keys 16 m + 4 h + .., channels 32 d + ..).
         const unsigned k_from = lds0 + l32 * Tile::kRow + h * 16;
         const unsigned v_from = lds0 + Tile::kSide + (4 * h + (lane >> 2 & 3)) * Tile::kRow + (lane >> 4 & 1) * 32 + (lane & 3) * 8;
-        bf16x8 kf[2][KS], vf[2][DT][2], pf[2][2];        // of 32 keys, and of the next
-        f32x16 s[2];
+        bf16x8 kf[KS], vf[DT][2], pf[2][2];
+        f32x16 s[2];                                     // of 32 keys, and of the next
         float top[2];                                    // the lane's largest score
-        auto read_k = [&](bf16x8* k, int buffer, int sub, int c) { k[c] = *(LdsB128)(k_from + buffer * Tile::kBuffer + sub * (32 * Tile::kRow) + c * 32); };
-        auto read_v = [&](bf16x8 (*v)[2], int buffer, int sub, int d, int m) {
+        auto read_k = [&](int buffer, int sub, int c) { kf[c] = *(LdsB128)(k_from + buffer * Tile::kBuffer + sub * (32 * Tile::kRow) + c * 32); };
+        auto read_v = [&](int buffer, int sub, int d, int m) {
             const unsigned from = v_from + buffer * Tile::kBuffer + (sub * 32 + m * 16) * Tile::kRow + d * 64;
             const bf16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4bf16((LdsB64)from), hi = __builtin_amdgcn_ds_read_tr16_b64_v4bf16((LdsB64)(from + 8 * Tile::kRow));
-            v[d][m] = __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
+            vf[d][m] = __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
         };
         auto largest_of = [&](int y) {
             float mx = s[y][0];
@@ -901,20 +879,20 @@ __global__ void __launch_bounds__(256, 1) batch_attn_many_kernel(const bf16_t* _
             for (int i = 1; i < 16; ++i) mx = fmaxf(mx, s[y][i]);
             top[y] = mx;
         };
-        auto score = [&](int y, const bf16x8* k, int c) {
+        auto score = [&](int y, int c) {
             if (c == 0)
 #pragma unroll
                 for (int i = 0; i < 16; ++i) s[y][i] = 0.f;
-            s[y] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(k[c], qf[y][c], s[y], 0, 0, 0);
+            s[y] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf[c], qf[c], s[y], 0, 0, 0);
         };
-        auto value = [&](int y, const bf16x8 (*v)[2], int m, int d) { o[y][d] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(v[d][m], pf[y][m], o[y][d], 0, 0, 0); };
-        // What rows do not see of 32 keys; where values that are not numbers became zeros, a row that sees one of them is undefined by its sum.
-        auto hide = [&](int y, const uint2& info, int buffer, int sub) {
-            const unsigned odd = *reinterpret_cast<const uint32_t*>(lds + Tile::kFlags + buffer * 8 + sub * 4);
+        auto value = [&](int y, int m, int d) { o[d] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vf[d][m], pf[y][m], o[d], 0, 0, 0); };
+        // What the row does not see of 32 keys; where values that are not numbers became zeros, a row that sees one of them is undefined by its sum.
+        auto hide = [&](int y, const uint2& info, int buffer) {
+            const unsigned odd = *reinterpret_cast<const uint32_t*>(lds + Tile::kFlags + buffer * 8 + y * 4);
             unsigned seen_keys = 0;
 #pragma unroll
             for (int j = 0; j < 2; ++j) {
-                const int seen = min((int)((unsigned)__builtin_amdgcn_readlane(info.x, sub * 2 + j) >> 16 & 31u), pos_of[y] + 1 - __builtin_amdgcn_readlane(info.y, sub * 2 + j));
+                const int seen = min((int)((unsigned)__builtin_amdgcn_readlane(info.x, y * 2 + j) >> 16 & 31u), my_pos + 1 - __builtin_amdgcn_readlane(info.y, y * 2 + j));
                 seen_keys |= ((1u << max(seen, 0)) - 1u) << (16 * j);
 #pragma unroll
                 for (int i = 0; i < 8; ++i) {
@@ -922,25 +900,33 @@ __global__ void __launch_bounds__(256, 1) batch_attn_many_kernel(const bf16_t* _
                     s[y][8 * j + i] = (i & 3) + 8 * (i >> 2) + 4 * h < seen ? v : -INFINITY;
                 }
             }
-            if (odd & seen_keys) st[y].l = NAN;
+            if (odd & seen_keys) l = NAN;
             largest_of(y);
         };
-        // Moves the reference of rows that have a score too far above it.
+        // Moves the reference of rows that have a score too far above it, and with it what the weights so far have left: results, sum, and the weights before, whose values are still to come.
         auto settle = [&](int y) {
-            if (!__any(top[y] > st[y].lim)) return;
+            if (!__any(top[y] > lim)) return;
             const float mx = fmaxf(top[y], __shfl_xor(top[y], 32, 64));
-            if (mx > st[y].lim) {
-                const float to = mx * a.scale_log2e, al = st[y].lim == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(st[y].mc - to);
-                st[y].l *= al;
-                st[y].mc = to;
-                st[y].lim = mx + kManyRoom / a.scale_log2e;
+            if (mx > lim) {
+                const float to = ceilf(mx * a.scale_log2e), al = lim == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(mc - to);
+                l *= al;
+                mc = to;
+                lim = mx + kManyRoom / a.scale_log2e;
 #pragma unroll
-                for (int d = 0; d < DT; ++d) o[y][d] *= al;
+                for (int d = 0; d < DT; ++d) o[d] *= al;
+#pragma unroll
+                for (int m = 0; m < 2; ++m) {
+                    float f[8];
+                    Elem<bf16_t>::unpack(__builtin_bit_cast(uint4, pf[1 - y][m]), f);
+#pragma unroll
+                    for (int i = 0; i < 8; ++i) f[i] *= al;
+                    pf[1 - y][m] = __builtin_bit_cast(bf16x8, Elem<bf16_t>::pack(f));
+                }
             }
         };
-        // A phase: the weights of half y beside the other half's scores (k) and values (v), a matrix instruction (32 cycles) and what a lane computes meanwhile, in this order: a weight or two,
-        // the rounding and sum of those before, the largest of the new scores, and more(i): reads, conversions.
-        auto phase = [&](int y, const bf16x8* k, const bf16x8 (*v)[2], auto more) {
+        // A phase: the weights of keys y beside the scores of the next (kf) and the values of those before (vf), a matrix instruction (32 cycles) and what a lane computes meanwhile, in this order: a
+        // weight or two, the rounding and sum of those before, the largest of the new scores, and more(i): reads, conversions.
+        auto phase = [&](int y, auto more) {
             constexpr int NM = KS + 2 * DT, EP = 16 / NM;
             const int z = 1 - y;
             float w[16], sum[2] = {0.f, 0.f}, mx = 0.f;
@@ -952,11 +938,11 @@ __global__ void __launch_bounds__(256, 1) batch_attn_many_kernel(const bf16_t* _
             };
 #pragma unroll
             for (int i = 0; i < NM; ++i) {
-                if (i < KS) score(z, k, i);
-                else value(z, v, (i - KS) / DT, (i - KS) % DT);
+                if (i < KS) score(z, i);
+                else value(z, (i - KS) / DT, (i - KS) % DT);
 #pragma unroll
                 for (int e = 0; e < EP; ++e) {
-                    w[i * EP + e] = __builtin_amdgcn_exp2f(fmaf(s[y][i * EP + e], a.scale_log2e, -st[y].mc));
+                    w[i * EP + e] = __builtin_amdgcn_exp2f(fmaf(s[y][i * EP + e], a.scale_log2e, -mc));
                     asm volatile("" : "+v"(w[i * EP + e]));      // (formed in this place)
                 }
                 if (EP == 1 ? i >= 2 && i % 2 == 0 : i >= 1) round_pair(EP == 1 ? i / 2 - 1 : i - 1);
@@ -972,77 +958,78 @@ __global__ void __launch_bounds__(256, 1) batch_attn_many_kernel(const bf16_t* _
             }
             round_pair(7);
             top[z] = mx;
-            st[y].l += sum[0] + sum[1];
+            l += sum[0] + sum[1];
 #pragma unroll
             for (int m = 0; m < 2; ++m) pf[y][m] = __builtin_bit_cast(bf16x8, make_uint4(words[m][0], words[m][1], words[m][2], words[m][3]));
-            asm volatile("" : "+v"(pf[y][0]), "+v"(pf[y][1]), "+v"(st[y].l), "+v"(top[z]));      // (formed here and not where it is used)
+            asm volatile("" : "+v"(pf[y][0]), "+v"(pf[y][1]), "+v"(l), "+v"(top[z]));
         };
 
-        int buffer = 0;
         if (any) {
-            uint2 info = info_behind, info_next;
+            // two tiles of keys in LDS, a third in registers
+            uint2 info = info_new, info_1, info_2;
             bool whole = all_full(info);
             if (!whole) clear_odd(0);
 #pragma unroll
-            for (int i = 0; i < 4 * NPASS; ++i) fill_part(0, i / 4, i % 4);
+            for (int i = 0; i < 4; ++i) fill_part(0, i);
             bool next = advance();
             read_list();
             load();
-            info_next = info_behind;
-            bool next_whole = all_full(info_next);
+            info_1 = info_new;
+            bool whole_1 = all_full(info_1);
+            if (!whole_1) clear_odd(1);
+#pragma unroll
+            for (int i = 0; i < 4; ++i) fill_part(1, i);
+            bool after = next && advance();
+            read_list();
+            load();
+            info_2 = info_new;
+            bool whole_2 = all_full(info_2);
             __syncthreads();
 #pragma unroll
-            for (int c = 0; c < KS; ++c) read_k(kf[0], 0, 0, c);
+            for (int c = 0; c < KS; ++c) read_k(0, 0, c);
 #pragma unroll
-            for (int i = 0; i < 2 * DT; ++i) {
-                read_v(vf[0], 0, 0, i % DT, i / DT);
-                vf[1][i % DT][i / DT] = vf[0][i % DT][i / DT];
-            }
+            for (int m = 0; m < 2; ++m) pf[1][m] = bf16x8{};      // (the first phase's values: nothing, or undefined where they are undefined for all rows)
 #pragma unroll
-            for (int m = 0; m < 2; ++m) pf[1][m] = bf16x8{};      // (the first turn's values of B: nothing, or undefined where they are undefined for all rows)
-#pragma unroll
-            for (int c = 0; c < KS; ++c) score(0, kf[0], c);
+            for (int c = 0; c < KS; ++c) score(0, c);
             largest_of(0);
+#pragma unroll
+            for (int c = 0; c < KS; ++c) read_k(0, 1, c);
+            int buffer = 0, behind = 0;                  // of the present keys, of those before
             while (true) {
-                const int ahead = buffer == 2 ? 0 : buffer + 1;
-                bool behind = false;
-#pragma unroll
-                for (int y = 0; y < 2; ++y)
-#pragma unroll
-                    for (int c = 0; c < KS; ++c) asm volatile("" : "+a"(qf[y][c]));      // (they stay among the accumulation registers, where matrix instructions read them too)
-#pragma unroll
-                for (int sub = 0; sub < 2; ++sub) {
-                    // A: weights; B: scores, values of the keys before; the next keys' K
-                    if (!whole) hide(0, info, buffer, sub);
-                    settle(0);
-                    phase(0, kf[sub], vf[1 - sub], [&](int i) {
-                        if (i < KS) read_k(kf[1 - sub], sub == 0 ? buffer : ahead, 1 - sub, i);      // (behind the last keys: whatever lies there, not used)
-                        if (sub == 1 && i == KS) load();      // (behind the last keys: the last codes again, not used)
-                    });
-                    if (sub == 0 && !next_whole) clear_odd(ahead);
-                    // B: weights; A: values, scores of the next keys; their V
-                    if (!whole) hide(1, info, buffer, sub);
-                    settle(1);
-                    phase(1, kf[1 - sub], vf[sub], [&](int i) {
-                        if (i < 2 * DT) read_v(vf[1 - sub], sub == 0 ? buffer : ahead, 1 - sub, i % DT, i / DT);
-                        else if (sub == 0 && i - 2 * DT < 4 * NPASS) fill_part(ahead, (i - 2 * DT) / 4, (i - 2 * DT) % 4);
-                    });
-                    if (sub == 0) {
-                        __syncthreads();
-                        behind = next && advance();
-                        read_list();
-                    }
-                }
+                const int ahead = (buffer + 1) & 3, filled = (buffer + 2) & 3;
+                if (!whole) hide(0, info, buffer);
+                settle(0);
+                phase(0, [&](int i) {
+                    if (i < 2 * DT) read_v(behind, behind == buffer ? 0 : 1, i % DT, i / DT);
+                    if (i >= 2 * DT && i - 2 * DT < KS) read_k(ahead, 0, i - 2 * DT);      // (behind the last keys: whatever lies there, not used)
+                });
+                if (!whole) hide(1, info, buffer);
+                settle(1);
+                if (!whole_2) clear_odd(filled);
+                phase(1, [&](int i) {
+                    if (i < 2 * DT) read_v(buffer, 0, i % DT, i / DT);
+                    if (i >= 2 * DT && i - 2 * DT < KS) read_k(ahead, 1, i - 2 * DT);
+                    if (i >= KS && (i - KS) % (2 * DT / 4) == 0) fill_part(filled, (i - KS) / (2 * DT / 4));      // (behind the last keys: the last codes again, not used)
+                });
+                __syncthreads();
                 if (!next) break;
-                info = info_next;
-                info_next = info_behind;
-                whole = next_whole;
-                next_whole = all_full(info_next);
-                next = behind;
+                info = info_1;
+                info_1 = info_2;
+                whole = whole_1;
+                whole_1 = whole_2;
+                next = after;
+                after = after && advance();
+                read_list();
+                load();
+                info_2 = info_new;
+                whole_2 = all_full(info_2);
+                behind = buffer;
                 buffer = ahead;
             }
 #pragma unroll
-            for (int i = 0; i < 2 * DT; ++i) value(1, vf[1], i / DT, i % DT);
+            for (int i = 0; i < 2 * DT; ++i) read_v(buffer, 1, i % DT, i / DT);
+#pragma unroll
+            for (int i = 0; i < 2 * DT; ++i) value(1, i / DT, i % DT);
         }
         __syncthreads();                                 // the buffers are read before they are written again
 
@@ -1053,29 +1040,25 @@ __global__ void __launch_bounds__(256, 1) batch_attn_many_kernel(const bf16_t* _
             const int n_shares = whole_tile ? 1 : (int)(to / share) - share_of + 1;
             a.where[(size_t)(me.lo + n) * a.Hq + g * G + i - n * G] = make_int2(kFewPartRows + (blockIdx.x * 2 + 1) * kManyRows + threadIdx.x, 2 * n_shares + 1);
         }
-#pragma unroll
-        for (int y = 0; y < 2; ++y) {
-            const float l = st[y].l + __shfl_xor(st[y].l, 32, 64);
-            const int in_tile = wave * 64 + y * 32 + l32;
-            if (in_tile >= rows) continue;
+        l += __shfl_xor(l, 32, 64);
+        const int in_tile = wave * 32 + l32;
+        if (in_tile < rows) {
             if (whole_tile) {
-                const int lrow = row0 + in_tile, token = a.by_group(lrow);
                 bf16_t* dst = out + (size_t)(me.lo + token) * a.ldo + (size_t)(g * G + lrow - token * G) * D + 4 * h;
                 const float inv = l == 0.f ? 0.f : 1.f / l;
 #pragma unroll
                 for (int d = 0; d < DT; ++d)
 #pragma unroll
                     for (int i = 0; i < 4; ++i)
-                        *reinterpret_cast<uint2*>(dst + d * 32 + i * 8) = make_uint2(pack_bf16x2(o[y][d][4 * i] * inv, o[y][d][4 * i + 1] * inv),
-                                                                                    pack_bf16x2(o[y][d][4 * i + 2] * inv, o[y][d][4 * i + 3] * inv));
+                        *reinterpret_cast<uint2*>(dst + d * 32 + i * 8) =
+                            make_uint2(pack_bf16x2(o[d][4 * i] * inv, o[d][4 * i + 1] * inv), pack_bf16x2(o[d][4 * i + 2] * inv, o[d][4 * i + 3] * inv));
             } else {
                 float* dst = a.part + (size_t)(kFewPartRows + (blockIdx.x * 2 + (from_cost == 0)) * kManyRows + in_tile) * (D + 4);
 #pragma unroll
                 for (int d = 0; d < DT; ++d)
 #pragma unroll
-                    for (int i = 0; i < 4; ++i)
-                        *reinterpret_cast<f32x4*>(dst + d * 32 + i * 8 + 4 * h) = f32x4{o[y][d][4 * i], o[y][d][4 * i + 1], o[y][d][4 * i + 2], o[y][d][4 * i + 3]};
-                if (h == 0) { dst[D] = st[y].lim == -INFINITY ? -INFINITY : st[y].mc; dst[D + 1] = l; }
+                    for (int i = 0; i < 4; ++i) *reinterpret_cast<f32x4*>(dst + d * 32 + i * 8 + 4 * h) = f32x4{o[d][4 * i], o[d][4 * i + 1], o[d][4 * i + 2], o[d][4 * i + 3]};
+                if (h == 0) { dst[D] = lim == -INFINITY ? -INFINITY : mc; dst[D + 1] = l; }
             }
         }
         left_over -= take;
@@ -1197,7 +1180,7 @@ static int launch_batch_attn(const void* q, void* out, BatchAttnArgs& a, hipStre
             static hipError_t err = hipSuccess;
             if (const int rc = raise_lds(batch_attn_many_kernel<D>, many_smem, once, err)) return rc;
             a.few = kFewRows;
-            hipLaunchKernelGGL((batch_attn_many_kernel<D>), dim3(std::max(1, kManyGrid / a.Hkv) * a.Hkv), dim3(256), many_smem, st, (const bf16_t*)q, (bf16_t*)out, a);
+            hipLaunchKernelGGL((batch_attn_many_kernel<D>), dim3(std::max(1, kManyGrid / a.Hkv) * a.Hkv), dim3(512), many_smem, st, (const bf16_t*)q, (bf16_t*)out, a);
             if (const int rc = check_launch()) return rc;
         }
     hipLaunchKernelGGL((batch_attn_kv8_kernel<T, D, NW>), dim3(shares * a.Hkv), dim3(64 * NW), smem, st, (const T*)q, (T*)out, a);
