@@ -876,7 +876,7 @@ __global__ void __launch_bounds__(512, 2) batch_attn_many_kernel(const bf16_t* _
         auto largest_of = [&](int y) {
             float mx = s[y][0];
 #pragma unroll
-            for (int i = 1; i < 16; ++i) mx = fmaxf(mx, s[y][i]);
+            for (int i = 1; i < 16; ++i) mx = __builtin_elementwise_maximum(mx, s[y][i]);
             top[y] = mx;
         };
         auto score = [&](int y, int c) {
@@ -894,10 +894,11 @@ __global__ void __launch_bounds__(512, 2) batch_attn_many_kernel(const bf16_t* _
             for (int j = 0; j < 2; ++j) {
                 const int seen = min((int)((unsigned)__builtin_amdgcn_readlane(info.x, y * 2 + j) >> 16 & 31u), my_pos + 1 - __builtin_amdgcn_readlane(info.y, y * 2 + j));
                 seen_keys |= ((1u << max(seen, 0)) - 1u) << (16 * j);
+                const int mine = seen - 4 * h;
 #pragma unroll
                 for (int i = 0; i < 8; ++i) {
                     const float v = s[y][8 * j + i];
-                    s[y][8 * j + i] = (i & 3) + 8 * (i >> 2) + 4 * h < seen ? v : -INFINITY;
+                    s[y][8 * j + i] = (i & 3) + 8 * (i >> 2) < mine ? v : -INFINITY;
                 }
             }
             if (odd & seen_keys) l = NAN;
@@ -950,7 +951,7 @@ __global__ void __launch_bounds__(512, 2) batch_attn_many_kernel(const bf16_t* _
                 constexpr int kFrom = KS + 2, kEach = (16 + NM - kFrom - 1) / (NM - kFrom);
                 if (i >= kFrom) {
 #pragma unroll
-                    for (int e = (i - kFrom) * kEach; e < (i - kFrom + 1) * kEach && e < 16; ++e) mx = e == 0 ? s[z][0] : fmaxf(mx, s[z][e]);
+                    for (int e = (i - kFrom) * kEach; e < (i - kFrom + 1) * kEach && e < 16; ++e) mx = e == 0 ? s[z][0] : __builtin_elementwise_maximum(mx, s[z][e]);      // (fmaxf costs a second instruction for each score)
                     asm volatile("" : "+v"(mx));
                 }
                 more(i);
