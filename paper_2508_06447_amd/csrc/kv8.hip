@@ -686,8 +686,8 @@ __global__ void __launch_bounds__(64 * NW, sizeof(T) == 2 ? 3 : 2) batch_attn_kv
 // rescaled in nearly all phases.
 constexpr int kManyKeys = 64;
 template <int D> struct ManyTile {
-    // Rows of D bfloat16 and 32 bytes: eight keys' same piece, or four keys' same two, lie in different banks, and every address of a lane is one base and a constant.
-    static constexpr int kRow = D * 2 + 32, kSide = kManyKeys * kRow, kBuffer = 2 * kSide;      // a key; Keys or Values; both
+    // Rows of D bfloat16 and 16 bytes (Keys: 16 keys' same piece of 16 bytes) or 64 (Values: four keys' same 64 bytes) cover all banks once, and every address of a lane is one base and a constant.
+    static constexpr int kRowK = D * 2 + 16, kRowV = D * 2 + 64, kSide = kManyKeys * kRowK, kBuffer = kSide + kManyKeys * kRowV;      // a key; the Keys; both
     static constexpr int kFlags = 4 * kBuffer, kLists = kFlags + 32, kLdsBytes = kLists + 8 * 64 * 16;      // four; a bit for each of their keys with a Value that is not a number; a wave's pieces
     static constexpr int KS = D / 16, DT = D / 32;
 };
@@ -836,12 +836,12 @@ __global__ void __launch_bounds__(512, 2) batch_attn_many_kernel(const bf16_t* _
                 else *reinterpret_cast<uint16_t*>(flags + wave * 2) = (uint16_t)bits;
             }
         };
-        const unsigned fill_to = lds0 + my_key * Tile::kRow + my_piece * 32;
+        const unsigned fill_k = lds0 + my_key * Tile::kRowK + my_piece * 32, fill_v = lds0 + Tile::kSide + my_key * Tile::kRowV + my_piece * 32;
         // A part of the keys' way into a buffer: eight channels of Keys (part 0, 1) or Values (2, 3).
         auto fill_part = [&](int buffer, int part) {
             const uint4 c = part < 2 ? kx : vx;
             const bf16x8 x = kv8_to_bf16(part % 2 ? make_uint2(c.z, c.w) : make_uint2(c.x, c.y), part < 2 ? kp : vp);
-            if (mine) *(LdsB128)(fill_to + buffer * Tile::kBuffer + part / 2 * Tile::kSide + part % 2 * 16) = x;
+            if (mine) *(LdsB128)((part < 2 ? fill_k : fill_v) + buffer * Tile::kBuffer + part % 2 * 16) = x;
         };
 
         const bool any = advance();
@@ -862,15 +862,15 @@ __global__ void __launch_bounds__(512, 2) batch_attn_many_kernel(const bf16_t* _
             for (int i = 0; i < 16; ++i) o[d][i] = 0.f;
         float mc = 0.f, lim = -INFINITY, l = 0.f;        // of row l32: reference in the base-2 domain, score above which it moves, the lane's share of the sum
         // Addresses of the lane in a buffer: K fragments (key l32, channels 16 c + 8 h: pieces 2 c + h), V fragments (keys 16 m + 4 h + .., channels 32 d + ..).
-        const unsigned k_from = lds0 + l32 * Tile::kRow + h * 16;
-        const unsigned v_from = lds0 + Tile::kSide + (4 * h + (lane >> 2 & 3)) * Tile::kRow + (lane >> 4 & 1) * 32 + (lane & 3) * 8;
+        const unsigned k_from = lds0 + l32 * Tile::kRowK + h * 16;
+        const unsigned v_from = lds0 + Tile::kSide + (4 * h + (lane >> 2 & 3)) * Tile::kRowV + (lane >> 4 & 1) * 32 + (lane & 3) * 8;
         bf16x8 kf[KS], vf[DT][2], pf[2][2];
         f32x16 s[2];                                     // of 32 keys, and of the next
         float top[2];                                    // the lane's largest score
-        auto read_k = [&](int buffer, int sub, int c) { kf[c] = *(LdsB128)(k_from + buffer * Tile::kBuffer + sub * (32 * Tile::kRow) + c * 32); };
+        auto read_k = [&](int buffer, int sub, int c) { kf[c] = *(LdsB128)(k_from + buffer * Tile::kBuffer + sub * (32 * Tile::kRowK) + c * 32); };
         auto read_v = [&](int buffer, int sub, int d, int m) {
-            const unsigned from = v_from + buffer * Tile::kBuffer + (sub * 32 + m * 16) * Tile::kRow + d * 64;
-            const bf16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4bf16((LdsB64)from), hi = __builtin_amdgcn_ds_read_tr16_b64_v4bf16((LdsB64)(from + 8 * Tile::kRow));
+            const unsigned from = v_from + buffer * Tile::kBuffer + (sub * 32 + m * 16) * Tile::kRowV + d * 64;
+            const bf16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4bf16((LdsB64)from), hi = __builtin_amdgcn_ds_read_tr16_b64_v4bf16((LdsB64)(from + 8 * Tile::kRowV));
             vf[d][m] = __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
         };
         auto largest_of = [&](int y) {
