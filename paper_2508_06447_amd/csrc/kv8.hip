@@ -720,7 +720,7 @@ __global__ void __launch_bounds__(512, 2) batch_attn_many_kernel(const bf16_t* _
 #pragma unroll
     for (int o = 32; o > 0; o >>= 1) total += __shfl_xor(total, o, 64);
     total = wave_value(total, 0);
-    const long long share = max((long long)G * 1024, (total + shares - 1) / shares), begin = share * share_of;
+    const long long share = max((long long)G * 256, (total + shares - 1) / shares), begin = share * share_of;
     long long left_over = min(total - begin, share);
     if (left_over <= 0) return;
     long long at = begin;
@@ -1175,7 +1175,9 @@ static int launch_batch_attn(const void* q, void* out, BatchAttnArgs& a, hipStre
     constexpr int NW = kBatchWaves, smem = NW * RowTile<T, D>::kLdsBytes;
     static_assert(smem < 1 << 16, "within the limit that needs no raising");
     if constexpr (sizeof(T) == 2)
-        if ((long long)a.n_rows * (a.Hq / a.Hkv) > kFewRows) {
+        // A request of many rows can only be there with more rows than that; with 16 and fewer on average the batch is taken for one of new tokens and drafts, which the other kernel
+        // alone serves (empty, the launch costs 5 us; a request of 256 rows among 255 new tokens costs some reads of its keys more).
+        if ((long long)a.n_rows * (a.Hq / a.Hkv) > std::max(kFewRows, kTileRows * a.R)) {
             constexpr int many_smem = ManyTile<D>::kLdsBytes;
             static std::once_flag once;
             static hipError_t err = hipSuccess;
