@@ -366,7 +366,7 @@ int launch_kv8_read(const void* pool, int n_slots, size_t slot_bytes, size_t lay
 constexpr int kPiece = 16;
 constexpr int kBatchWaves = 4;
 constexpr int kBatchGrid = 768;                          // workgroups: as many as run together
-constexpr int kBatchLeast = 4 * 2 * kBatchWaves;         // pieces of a share
+constexpr int kBatchLeast = 2 * 2 * kBatchWaves;         // pieces of a share: two turns of its waves (one request of 500 to 4000 tokens 13 us; with one turn 13, with four 14 to 16, with eight 14 to 20)
 constexpr int kBatchTile = 8;                            // what beginning and ending a tile counts for, in pieces
 constexpr int kFewRows = 64, kManyRows = 256, kManyGrid = 256;      // rows of a request up to which tiles have 16 rows; rows of the tiles for more; their workgroups
 constexpr int kFewPartRows = kBatchGrid * 2 * kTileRows, kPartRows = kFewPartRows + kManyGrid * 2 * kManyRows;      // rows of partial results
@@ -380,7 +380,7 @@ struct BatchAttnArgs {
     float scale_log2e;
     int R, max_blocks, n_slots, n_rows, block, per_block, Hq, Hkv, ldq, ldo;      // per_block: pieces
     int few;                                             // requests of more rows (of a kv head) are left to the kernel for many
-    Divide by_block, by_piece, by_group;                 // by block, per_block, Hq / Hkv
+    Divide by_block, by_piece, by_group, by_shares;      // by block, per_block, Hq / Hkv, the shares of a kv head (few rows)
 };
 
 struct BatchRequest {
@@ -438,18 +438,15 @@ __global__ void __launch_bounds__(64 * NW, sizeof(T) == 2 ? 3 : 2) batch_attn_kv
         return x;
     };
     BatchRequest x = request(lane_in);
-    long long total = x.cost(a);
-    for (int r = 64; r < a.R; r += 64) total += request(r + lane_in).cost(a);
-#pragma unroll
-    for (int o = 32; o > 0; o >>= 1) total += __shfl_xor(total, o, 64);
-    total = wave_value(total, 0);                        // (in scalar registers, with all that follows from it)
-    const long long share = max((long long)kBatchLeast, (total + shares - 1) / shares), begin = share * share_of;
+    long long mine = x.cost(a), end = a.R == 1 ? mine : wave_prefix(mine, lane_in);
+    long long total = wave_value(end, a.R == 1 ? 0 : 63);      // (in scalar registers, with all that follows from it)
+    for (int r = 64; r < a.R; r += 64) total += wave_value(wave_prefix(request(r + lane_in).cost(a), lane_in), 63);
+    const long long share = max((long long)kBatchLeast, total < 1ll << 30 ? (long long)a.by_shares((int)total + shares - 1) : (total + shares - 1) / shares), begin = share * share_of;
     long long left_over = min(total - begin, share);     // of the share
     if (left_over <= 0) return;
     long long at = begin;                                // of the share's beginning, counted from request r0's, then from its own request's
     int i_req;
     while (true) {
-        const long long mine = x.cost(a), end = wave_prefix(mine, lane_in);
         const unsigned long long behind = __ballot(end > at);
         if (behind) {
             i_req = __builtin_ctzll(behind);
@@ -460,10 +457,12 @@ __global__ void __launch_bounds__(64 * NW, sizeof(T) == 2 ? 3 : 2) batch_attn_kv
         r0 += 64;
         if (r0 >= a.R) return;
         x = request(r0 + lane_in);
+        mine = x.cost(a);
+        end = wave_prefix(mine, lane_in);
     }
-    int tile, from;
-    {
-        const int apart = wave_value(x.pieces(a), i_req) + kBatchTile;
+    int tile = 0, from = (int)at;
+    const int apart = wave_value(x.pieces(a), i_req) + kBatchTile;
+    if (at >= apart) {
         tile = (int)(at / apart);
         from = (int)(at - (long long)tile * apart);
     }
@@ -1201,7 +1200,7 @@ int launch_batch_attn_kv8(const void* q, int ldq, const int* row_start, const in
                           size_t layer_offset, int block, int Hq, int Hkv, int d, float scale, int dtype, void* out, int ldo, void* workspace, hipStream_t st) {
     const int per_block = (block + kPiece - 1) / kPiece;
     BatchAttnArgs a{row_start, lens, table, (const unsigned char*)pool, slot_bytes, layer_offset, (float*)workspace, (int2*)((char*)workspace + batch_part_bytes(n_rows, Hq, Hkv, d)),
-                    scale * 1.4426950408889634f, R, max_blocks, n_slots, n_rows, block, per_block, Hq, Hkv, ldq, ldo, 0x7fffffff, Divide(block), Divide(per_block), Divide(Hq / Hkv)};
+                    scale * 1.4426950408889634f, R, max_blocks, n_slots, n_rows, block, per_block, Hq, Hkv, ldq, ldo, 0x7fffffff, Divide(block), Divide(per_block), Divide(Hq / Hkv), Divide(std::max(1, kBatchGrid / Hkv))};
     if (dtype == SLIM_BF16) return d == 64 ? launch_batch_attn<bf16_t, 64>(q, out, a, st) : launch_batch_attn<bf16_t, 128>(q, out, a, st);
     return d == 64 ? launch_batch_attn<float, 64>(q, out, a, st) : launch_batch_attn<float, 128>(q, out, a, st);
 }
