@@ -349,7 +349,7 @@ int slim_decode_attn_kv4(const void* q, const void* gpu_pool, size_t slot_bytes,
 }
 
 // ---- a batch of requests (batch.hip), its cache in 8 bits (kv8.hip)
-constexpr int kKv8RowsMost = 1 << 29;                    // of a call that writes or reads: at most eight threads of a launch per row
+constexpr int kKv8RowsMost = 1 << 29;                    // rows times kv heads of a call that writes or reads: at most eight threads of a launch for each
 constexpr long long kBatchTokensMost = 1ll << 30;        // of a request, as its table has room for: units of keys are counted in 32 bits
 static bool kv8_heads_ok(int n_kv_heads, int head_dim) { return (head_dim == 64 || head_dim == 128) && n_kv_heads <= 65535; }
 static bool places_ok(int n_slots, int block) { return block <= kKv4BlockMost && (long long)n_slots * block < 1ll << 31; }      // places in the pool are counted in 32 bits
@@ -401,7 +401,7 @@ int slim_kv8_write(const void* k, const void* v, int ldk, int ldv, const int* ro
     if (const int rc = kv8_pool_checks(pool, n_slots, slot_bytes, layer_offset, block, n_kv_heads, head_dim, dtype)) return rc;
     if (const int rc = rows_check(k, ldk, n_kv_heads, head_dim, dtype)) return rc;
     if (const int rc = rows_check(v, ldv, n_kv_heads, head_dim, dtype)) return rc;
-    if (n_rows >= kKv8RowsMost) return SLIM_UNSUPPORTED;
+    if ((long long)n_rows * n_kv_heads >= kKv8RowsMost) return SLIM_UNSUPPORTED;
     return launch_kv8_write(k, v, ldk, ldv, row_slot, n_rows, n_kv_heads, head_dim, block, dtype, pool, n_slots, slot_bytes, layer_offset, (hipStream_t)stream);
 }
 
@@ -411,7 +411,7 @@ int slim_kv8_read(const void* pool, int n_slots, size_t slot_bytes, size_t layer
     if (const int rc = kv8_pool_checks(pool, n_slots, slot_bytes, layer_offset, block, n_kv_heads, head_dim, dtype)) return rc;
     if (const int rc = rows_check(k_out, ldk, n_kv_heads, head_dim, dtype)) return rc;
     if (const int rc = rows_check(v_out, ldv, n_kv_heads, head_dim, dtype)) return rc;
-    if (n_tokens >= kKv8RowsMost) return SLIM_UNSUPPORTED;
+    if ((long long)n_tokens * n_kv_heads >= kKv8RowsMost) return SLIM_UNSUPPORTED;
     return launch_kv8_read(pool, n_slots, slot_bytes, layer_offset, slots, n_tokens, n_kv_heads, head_dim, block, dtype, k_out, v_out, ldk, ldv, (hipStream_t)stream);
 }
 

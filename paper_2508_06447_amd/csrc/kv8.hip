@@ -1162,9 +1162,16 @@ static size_t batch_part_bytes(int n_rows, int Hq, int Hkv, int d) {
 }
 size_t batch_attn_kv8_workspace_bytes(int n_rows, int Hq, int Hkv, int d) { return batch_part_bytes(n_rows, Hq, Hkv, d) + align_up((size_t)n_rows * Hq * sizeof(int2), 256); }
 
-template <typename K> static int raise_lds(K kernel, int bytes, std::once_flag& once, hipError_t& err) {
-    std::call_once(once, [&] { err = hipFuncSetAttribute((const void*)kernel, hipFuncAttributeMaxDynamicSharedMemorySize, bytes); });
-    return err == hipSuccess ? SLIM_OK : set_hip_error(err);
+// Raises a kernel's LDS limit, once on each device.
+constexpr int kDevices = 64;
+struct Raised { std::once_flag once[kDevices]; hipError_t err[kDevices] = {}; };
+template <typename K> static int raise_lds(K kernel, int bytes, Raised& raised) {
+    int dev = -1;
+    const hipError_t e = hipGetDevice(&dev);
+    if (e != hipSuccess) return set_hip_error(e);
+    if (dev < 0 || dev >= kDevices) return SLIM_UNSUPPORTED;
+    std::call_once(raised.once[dev], [&] { raised.err[dev] = hipFuncSetAttribute((const void*)kernel, hipFuncAttributeMaxDynamicSharedMemorySize, bytes); });
+    return raised.err[dev] == hipSuccess ? SLIM_OK : set_hip_error(raised.err[dev]);
 }
 
 template <typename T, int D>
@@ -1178,9 +1185,8 @@ static int launch_batch_attn(const void* q, void* out, BatchAttnArgs& a, hipStre
         // alone serves (empty, the launch costs 5 us; a request of 256 rows among 255 new tokens costs some reads of its keys more).
         if ((long long)a.n_rows * (a.Hq / a.Hkv) > std::max(kFewRows, kTileRows * a.R)) {
             constexpr int many_smem = ManyTile<D>::kLdsBytes;
-            static std::once_flag once;
-            static hipError_t err = hipSuccess;
-            if (const int rc = raise_lds(batch_attn_many_kernel<D>, many_smem, once, err)) return rc;
+            static Raised raised;
+            if (const int rc = raise_lds(batch_attn_many_kernel<D>, many_smem, raised)) return rc;
             a.few = kFewRows;
             hipLaunchKernelGGL((batch_attn_many_kernel<D>), dim3(std::max(1, kManyGrid / a.Hkv) * a.Hkv), dim3(512), many_smem, st, (const bf16_t*)q, (bf16_t*)out, a);
             if (const int rc = check_launch()) return rc;

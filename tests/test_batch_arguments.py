@@ -75,7 +75,7 @@ POOL_INVALID = (dict(pool=NULL), dict(slots=0), dict(block=0), dict(heads=0), di
                 dict(ldv=1016), dict(n=0))
 POOL_UNSUPPORTED = (dict(dtype=2), dict(d=96), dict(d=32), dict(heads=1, d=256), dict(heads=70000, ldk=1 << 24, ldv=1 << 24, size=1 << 60), dict(size=SIZE + 8), dict(size=SIZE + 16, off=8),
                     dict(pool=ODD), dict(k=ODD), dict(v=ODD), dict(ldk=1028), dict(ldv=1028), dict(dtype=0, ldk=1026), dict(block=(1 << 24) + 1, size=1 << 60),
-                    dict(slots=1 << 25), dict(n=1 << 29))
+                    dict(slots=1 << 25), dict(n=1 << 26), dict(n=1 << 29))
 
 
 def test_write_and_read_refusals(lib):
