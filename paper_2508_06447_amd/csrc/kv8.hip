@@ -365,7 +365,9 @@ int launch_kv8_read(const void* pool, int n_slots, size_t slot_bytes, size_t lay
 // a second kernel merges.  The lengths are known to the GPU alone, so that each wave forms the sums over the requests for itself, 64 of them at a time.
 constexpr int kPiece = 16;
 constexpr int kBatchWaves = 4;
-constexpr int kBatchGrid = 768;                          // workgroups: as many as run together
+constexpr int kBatchGrid = 768;                          // workgroups: as many as run together, three a CU (bfloat16 heads of 128: 256 requests 150 us, with 512 157, drafts 73 and 84)
+// Heads of 64, and float32 ones of 128, of which only two fit: 512 (64 requests of 4000 tokens 55 instead of 60 us, and 101 instead of 132).
+template <typename T, int D> constexpr int batch_grid() { return sizeof(T) == 2 && D == 128 ? kBatchGrid : 512; }
 constexpr int kBatchLeast = 2 * 2 * kBatchWaves;         // pieces of a share: two turns of its waves (one request of 500 to 4000 tokens 13 us; with one turn 13, with four 14 to 16, with eight 14 to 20)
 constexpr int kBatchTile = 8;                            // what beginning and ending a tile counts for, in pieces
 constexpr int kFewRows = 64, kManyRows = 256, kManyGrid = 256;      // rows of a request up to which tiles have 16 rows; rows of the tiles for more; their workgroups
@@ -1176,7 +1178,8 @@ template <typename K> static int raise_lds(K kernel, int bytes, Raised& raised) 
 
 template <typename T, int D>
 static int launch_batch_attn(const void* q, void* out, BatchAttnArgs& a, hipStream_t st) {
-    const int shares = std::max(1, kBatchGrid / a.Hkv);
+    const int shares = std::max(1, batch_grid<T, D>() / a.Hkv);
+    a.by_shares = Divide(shares);
     const long long rows = (long long)a.n_rows * a.Hq;
     constexpr int NW = kBatchWaves, smem = NW * RowTile<T, D>::kLdsBytes;
     static_assert(smem < 1 << 16, "within the limit that needs no raising");
@@ -1206,7 +1209,7 @@ int launch_batch_attn_kv8(const void* q, int ldq, const int* row_start, const in
                           size_t layer_offset, int block, int Hq, int Hkv, int d, float scale, int dtype, void* out, int ldo, void* workspace, hipStream_t st) {
     const int per_block = (block + kPiece - 1) / kPiece;
     BatchAttnArgs a{row_start, lens, table, (const unsigned char*)pool, slot_bytes, layer_offset, (float*)workspace, (int2*)((char*)workspace + batch_part_bytes(n_rows, Hq, Hkv, d)),
-                    scale * 1.4426950408889634f, R, max_blocks, n_slots, n_rows, block, per_block, Hq, Hkv, ldq, ldo, 0x7fffffff, Divide(block), Divide(per_block), Divide(Hq / Hkv), Divide(std::max(1, kBatchGrid / Hkv))};
+                    scale * 1.4426950408889634f, R, max_blocks, n_slots, n_rows, block, per_block, Hq, Hkv, ldq, ldo, 0x7fffffff, Divide(block), Divide(per_block), Divide(Hq / Hkv), Divide(1)};
     if (dtype == SLIM_BF16) return d == 64 ? launch_batch_attn<bf16_t, 64>(q, out, a, st) : launch_batch_attn<bf16_t, 128>(q, out, a, st);
     return d == 64 ? launch_batch_attn<float, 64>(q, out, a, st) : launch_batch_attn<float, 128>(q, out, a, st);
 }
