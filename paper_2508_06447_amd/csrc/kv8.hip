@@ -359,7 +359,7 @@ int launch_kv8_read(const void* pool, int n_slots, size_t slot_bytes, size_t lay
 }
 
 // ---- attention
-// A request's rows are its (query, query head of the kv head) pairs, query by query, head by head; a tile is 16 of them.  A piece is up to 16 keys of one block.  The pieces of all tiles of
+// A request's rows are its (query, query head of the kv head) pairs, query by query, head by head; a tile is 16 of them, or, in batches of drafts, 32.  A piece is up to 16 keys of one block.  The pieces of all tiles of
 // all requests, one behind the other, are cut into equal shares, one workgroup a share, so that requests of any lengths keep all workgroups busy to the end.  A workgroup goes through its
 // share tile by tile; its waves take two pieces in turn, from wherever they lie.  A tile that lies in one share is written at once, one that several share is left as partial results, which
 // a second kernel merges.  The lengths are known to the GPU alone, so that each wave forms the sums over the requests for itself, 64 of them at a time.
@@ -367,11 +367,12 @@ constexpr int kPiece = 16;
 constexpr int kBatchWaves = 4;
 constexpr int kBatchGrid = 768;                          // workgroups: as many as run together, three a CU (bfloat16 heads of 128: 256 requests 150 us, with 512 157, drafts 73 and 84)
 // Heads of 64, and float32 ones of 128, of which only two fit: 512 (64 requests of 4000 tokens 55 instead of 60 us, and 101 instead of 132).
-template <typename T, int D> constexpr int batch_grid() { return sizeof(T) == 2 && D == 128 ? kBatchGrid : 512; }
-constexpr int kBatchLeast = 2 * 2 * kBatchWaves;         // pieces of a share: two turns of its waves (one request of 500 to 4000 tokens 13 us; with one turn 13, with four 14 to 16, with eight 14 to 20)
+template <typename T, int D, int NR> constexpr int batch_grid() { return sizeof(T) == 2 && D == 128 && NR == 1 ? kBatchGrid : 512; }
+constexpr int kBatchLeast = 2 * 2 * kBatchWaves;         // pieces of a share: two turns of its waves (one request of 500 to 4000 tokens 13 us; with one turn 13, with four 14 to 16, with eight
+                                                         // 14 to 20); of tiles of 32 rows, whose turns are longer, one (16 queries of a request of 512 or 2048 tokens 17 and 21 us, with two 23 and 25)
 constexpr int kBatchTile = 8;                            // what beginning and ending a tile counts for, in pieces
-constexpr int kFewRows = 64, kManyRows = 256, kManyGrid = 256;      // rows of a request up to which tiles have 16 rows; rows of the tiles for more; their workgroups
-constexpr int kFewPartRows = kBatchGrid * 2 * kTileRows, kPartRows = kFewPartRows + kManyGrid * 2 * kManyRows;      // rows of partial results
+constexpr int kFewRows = 64, kManyRows = 256, kManyGrid = 256;      // rows of a request up to which tiles have 16 or 32 rows; rows of the tiles for more; their workgroups
+constexpr int kFewPartRows = 512 * 2 * 2 * kTileRows, kPartRows = kFewPartRows + kManyGrid * 2 * kManyRows;      // rows of partial results
 
 struct BatchAttnArgs {
     const int *row_start, *lens, *table;
@@ -381,19 +382,19 @@ struct BatchAttnArgs {
     int2* where;                                         // of row (t, h): its row of `part` in the share that begins its tile, and 2 * the number of shares + 1 for tiles of many rows
     float scale_log2e;
     int R, max_blocks, n_slots, n_rows, block, per_block, Hq, Hkv, ldq, ldo;      // per_block: pieces
-    int few;                                             // requests of more rows (of a kv head) are left to the kernel for many
+    int few, tile_rows;                                  // requests of more rows (of a kv head) are left to the kernel for many; rows of the tiles of the others
     Divide by_block, by_piece, by_group, by_shares;      // by block, per_block, Hq / Hkv, the shares of a kv head (few rows)
 };
 
 struct BatchRequest {
     int lo, n, len;                                      // first row of the step, rows of it, tokens
     __device__ __forceinline__ int rows(const BatchAttnArgs& a) const { return n * (a.Hq / a.Hkv); }      // of a kv head
-    __device__ __forceinline__ int tiles(const BatchAttnArgs& a) const { return (rows(a) + kTileRows - 1) / kTileRows; }
+    template <int TR> __device__ __forceinline__ int tiles(const BatchAttnArgs& a) const { return (rows(a) + TR - 1) / TR; }
     __device__ __forceinline__ int pieces(const BatchAttnArgs& a) const {
         const int whole = a.by_block(len);
         return whole * a.per_block + (len - whole * a.block + kPiece - 1) / kPiece;
     }
-    __device__ __forceinline__ long long cost(const BatchAttnArgs& a) const { return (long long)tiles(a) * (pieces(a) + kBatchTile); }
+    template <int TR> __device__ __forceinline__ long long cost(const BatchAttnArgs& a) const { return (long long)tiles<TR>(a) * (pieces(a) + kBatchTile); }
     __device__ __forceinline__ bool many(const BatchAttnArgs& a) const { return n > 0 && rows(a) > a.few; }
 };
 __device__ __forceinline__ BatchRequest batch_request(const BatchAttnArgs& a, int r) {
@@ -424,11 +425,11 @@ __device__ __forceinline__ uint32_t first_used_here(uint32_t v) {
     return v;
 }
 
-template <typename T, int D, int NW>
-__global__ void __launch_bounds__(64 * NW, sizeof(T) == 2 ? 3 : 2) batch_attn_kv8_kernel(const T* __restrict__ q, T* __restrict__ out, BatchAttnArgs a) {
+template <typename T, int D, int NW, int NR>
+__global__ void __launch_bounds__(64 * NW, sizeof(T) == 2 && NR == 1 ? 3 : 2) batch_attn_kv8_kernel(const T* __restrict__ q, T* __restrict__ out, BatchAttnArgs a) {
     typedef RowTile<T, D> Tile;
-    constexpr int NP = Tile::NP, NT = Tile::NT, KS = Tile::KS, PC = D / 64;      // PC: 16-byte pieces of a lane's channels
-    extern __shared__ __align__(16) unsigned char lds[];
+    constexpr int NP = Tile::NP, NT = Tile::NT, KS = Tile::KS, PC = D / 64, TR = NR * kTileRows;      // PC: 16-byte pieces of a lane's channels
+    extern __shared__ __align__(256) unsigned char lds[];
     const int G = a.Hq / a.Hkv;
     // The kv head goes fastest: with eight of them each XCD has its own.
     const int g = blockIdx.x % a.Hkv, share_of = blockIdx.x / a.Hkv, shares = gridDim.x / a.Hkv;
@@ -440,10 +441,10 @@ __global__ void __launch_bounds__(64 * NW, sizeof(T) == 2 ? 3 : 2) batch_attn_kv
         return x;
     };
     BatchRequest x = request(lane_in);
-    long long mine = x.cost(a), end = a.R == 1 ? mine : wave_prefix(mine, lane_in);
+    long long mine = x.template cost<TR>(a), end = a.R == 1 ? mine : wave_prefix(mine, lane_in);
     long long total = wave_value(end, a.R == 1 ? 0 : 63);      // (in scalar registers, with all that follows from it)
-    for (int r = 64; r < a.R; r += 64) total += wave_value(wave_prefix(request(r + lane_in).cost(a), lane_in), 63);
-    const long long share = max((long long)kBatchLeast, total < 1ll << 30 ? (long long)a.by_shares((int)total + shares - 1) : (total + shares - 1) / shares), begin = share * share_of;
+    for (int r = 64; r < a.R; r += 64) total += wave_value(wave_prefix(request(r + lane_in).template cost<TR>(a), lane_in), 63);
+    const long long share = max((long long)kBatchLeast / NR, total < 1ll << 30 ? (long long)a.by_shares((int)total + shares - 1) : (total + shares - 1) / shares), begin = share * share_of;
     long long left_over = min(total - begin, share);     // of the share
     if (left_over <= 0) return;
     long long at = begin;                                // of the share's beginning, counted from request r0's, then from its own request's
@@ -459,7 +460,7 @@ __global__ void __launch_bounds__(64 * NW, sizeof(T) == 2 ? 3 : 2) batch_attn_kv
         r0 += 64;
         if (r0 >= a.R) return;
         x = request(r0 + lane_in);
-        mine = x.cost(a);
+        mine = x.template cost<TR>(a);
         end = wave_prefix(mine, lane_in);
     }
     int tile = 0, from = (int)at;
@@ -471,208 +472,235 @@ __global__ void __launch_bounds__(64 * NW, sizeof(T) == 2 ? 3 : 2) batch_attn_kv
 
     const Kv8Head head(g, a.block, a.Hkv, D);
     while (true) {
-    const BatchRequest me{wave_value(x.lo, i_req), wave_value(x.n, i_req), wave_value(x.len, i_req)};
-    const int pieces = me.pieces(a);
-    int tid = threadIdx.x;
-    asm volatile("" : "+v"(tid));                        // (what follows from it would be kept in registers from tile to tile)
-    const int lane = tid & 63, l16 = lane & 15, qr = lane >> 4, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-    const unsigned tile_lds = (unsigned)(uintptr_t)lds + wave * Tile::kLdsBytes;
-    const int r = r0 + i_req, take = (int)min((long long)(pieces + kBatchTile - from), left_over);
-    const int row0 = tile * kTileRows, rows = min(kTileRows, me.rows(a) - row0);
-    const int p0 = me.len - me.n + row0 / G, p1 = me.len - me.n + (row0 + rows - 1) / G;      // positions of the first and the last row
-    const int limit = p1 + 1;                            // (zero and below if there are more rows than tokens: then no piece is found)
-    const int* table = a.table + (size_t)r * a.max_blocks;
+        const BatchRequest me{wave_value(x.lo, i_req), wave_value(x.n, i_req), wave_value(x.len, i_req)};
+        const int pieces = me.pieces(a);
+        int tid = threadIdx.x;
+        asm volatile("" : "+v"(tid));                        // (what follows from it would be kept in registers from tile to tile)
+        const int lane = tid & 63, l16 = lane & 15, qr = lane >> 4, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+        const unsigned tile_lds = (unsigned)(uintptr_t)lds + wave * Tile::kLdsBytes;
+        const int r = r0 + i_req, take = (int)min((long long)(pieces + kBatchTile - from), left_over);
+        const int row0 = tile * TR, rows = min(TR, me.rows(a) - row0);
+        const int p0 = me.len - me.n + row0 / G, p1 = me.len - me.n + (row0 + rows - 1) / G;      // positions of the first and the last row
+        const int limit = p1 + 1;                            // (zero and below if there are more rows than tokens: then no piece is found)
+        const int* table = a.table + (size_t)r * a.max_blocks;
 
-    // The wave's pieces, in pairs: u0, u0 + 1, u0 + 2 NW, ..  64 of them are looked up at once, one a lane, and the table entries of the next 64 are on their way.  A piece of a block that no
-    // slot has, or behind the last row, has no keys and is passed over.
-    const int last = limit <= 0 ? 0 : a.by_block(limit - 1) * a.per_block + (limit - 1 - a.by_block(limit - 1) * a.block) / kPiece + 1;
-    const int u_end = min(last, from + take);
-    constexpr int kBatch = 64 * NW;
-    int u = from + 2 * wave + (lane >> 1) * 2 * NW + (lane & 1);      // the lane's
-    int batch = __builtin_amdgcn_readfirstlane(u) - kBatch;
-    int u_slot = 0, u_pos = 0, u_rows = 0, next_slot = u < u_end ? table[a.by_piece(u)] : -1;
-    unsigned long long left = 0;
-    int have[2], c0[2], pos[2];
-    const unsigned char* base[2];
-    auto find = [&]() {                                  // the next two pieces; false: none is left
-        while (!left) {
-            batch += kBatch;
-            if (batch >= u_end) return false;
-            const int b = a.by_piece(u), row = (u - b * a.per_block) * kPiece;
-            u_slot = next_slot;
-            u_pos = b * a.block + row;
-            u_rows = u_slot >= 0 && u_slot < a.n_slots ? min(kPiece, min(a.block - row, limit - u_pos)) : 0;
-            left = __ballot(u_rows > 0);
-            u += kBatch;
-            next_slot = u < u_end ? table[a.by_piece(u)] : -1;
-        }
-#pragma unroll
-        for (int h = 0; h < 2; ++h) {
-            if (h == 1 && !left) {                       // a single one: the other half repeats it, unseen
-                have[1] = 0;
-                c0[1] = c0[0];
-                pos[1] = pos[0];
-                base[1] = base[0];
-                break;
+        // The wave's pieces, in pairs: u0, u0 + 1, u0 + 2 NW, ..  64 of them are looked up at once, one a lane, and the table entries of the next 64 are on their way.  A piece of a block that no
+        // slot has, or behind the last row, has no keys and is passed over.
+        const int last = limit <= 0 ? 0 : a.by_block(limit - 1) * a.per_block + (limit - 1 - a.by_block(limit - 1) * a.block) / kPiece + 1;
+        const int u_end = min(last, from + take);
+        constexpr int kBatch = 64 * NW;
+        int u = from + 2 * wave + (lane >> 1) * 2 * NW + (lane & 1);      // the lane's
+        int batch = __builtin_amdgcn_readfirstlane(u) - kBatch;
+        int u_slot = 0, u_pos = 0, u_rows = 0, next_slot = u < u_end ? table[a.by_piece(u)] : -1;
+        unsigned long long left = 0;
+        int have[2], c0[2], pos[2];
+        const unsigned char* base[2];
+        auto find = [&]() {                                  // the next two pieces; false: none is left
+            while (!left) {
+                batch += kBatch;
+                if (batch >= u_end) return false;
+                const int b = a.by_piece(u), row = (u - b * a.per_block) * kPiece;
+                u_slot = next_slot;
+                u_pos = b * a.block + row;
+                u_rows = u_slot >= 0 && u_slot < a.n_slots ? min(kPiece, min(a.block - row, limit - u_pos)) : 0;
+                left = __ballot(u_rows > 0);
+                u += kBatch;
+                next_slot = u < u_end ? table[a.by_piece(u)] : -1;
             }
-            const int i = __builtin_ctzll(left);
-            left &= left - 1;
-            have[h] = __builtin_amdgcn_readlane(u_rows, i);
-            pos[h] = __builtin_amdgcn_readlane(u_pos, i);
-            c0[h] = pos[h] - a.by_block(pos[h]) * a.block;
-            base[h] = a.pool + (size_t)__builtin_amdgcn_readlane(u_slot, i) * a.slot_bytes + a.layer_offset;
-        }
-        return true;
-    };
-
-    uint4 kx[2][PC], vx[2][PC];
-    uint32_t ke[2], ve[2];                               // e + 127
-    // Addresses: a wave-uniform base and a 32-bit offset of the lane.  Rows behind the last key repeat it: not seen.  A lane's channels are 16 in a row of each 64, so that an instruction
-    // takes 64 bytes in a row of each key.
-    auto row_offset = [&](int h) { return (unsigned)(min(l16, max(have[h], 1) - 1) * D + qr * 16); };
-    auto channel = [&](int j) { return j / 2 * 64 + qr * 16 + j % 2 * 8; };
-    auto load_k = [&]() {
 #pragma unroll
-        for (int h = 0; h < 2; ++h) {
-            const unsigned char* at = base[h] + head.k + (size_t)c0[h] * D;
-            const unsigned off = row_offset(h);
-#pragma unroll
-            for (int c = 0; c < PC; ++c) kx[h][c] = *reinterpret_cast<const uint4*>(at + (off + c * 64));
-            ke[h] = base[h][head.e + (lane & 0)];
-        }
-    };
-    auto load_v = [&]() {
-#pragma unroll
-        for (int h = 0; h < 2; ++h) {
-            const unsigned char* at = base[h] + head.v + (size_t)c0[h] * D;
-            const unsigned off = row_offset(h);
-#pragma unroll
-            for (int c = 0; c < PC; ++c) vx[h][c] = *reinterpret_cast<const uint4*>(at + (off + c * 64));
-            ve[h] = base[h][head.e + 1 + (lane & 0)];
-        }
-    };
-    auto half_of = [](const uint4& c, int j) { return j % 2 ? make_uint2(c.z, c.w) : make_uint2(c.x, c.y); };
-    bool more = find();
-    if (more) { load_k(); load_v(); }
-
-    // the lane's row
-    const int lrow = row0 + min(l16, rows - 1), token = lrow / G;
-    const int p = me.len - me.n + token;
-    Tile t;
-    t.begin(q + (size_t)(me.lo + token) * a.ldq + (size_t)(g * G + lrow - token * G) * D, channel);
-    // waited for here: waited for in the loop, the Query fragments take the wait for the codes requested meanwhile with them in every turn
-#pragma unroll
-    for (int b = 0; b < NT; ++b)
-#pragma unroll
-        for (int j = 0; j < KS; ++j) asm volatile("" : "+v"(t.q[b][j]));
-    // Where the lane writes and reads the wave's V tile: one address each, whose bits 4 .. 7 are turned for the pieces and channels.  (Hidden from the compiler in every turn: it would keep
-    // them all in registers, and the Query fragments out of them.)
-    const int vr = 4 * qr + (l16 >> 2);
-    unsigned v_to = tile_lds + Tile::v_piece(l16, qr * 2), v_from = tile_lds + Tile::v_piece(vr, (l16 & 3) >> 1) + (l16 & 1) * 8;
-    float w[8];
-    bf16x8 pw[NP];
-    while (more) {
-        asm volatile("" : "+v"(v_to), "+v"(v_from));
-        const bool whole = have[0] == kPiece && have[1] == kPiece && max(pos[0], pos[1]) + kPiece - 1 <= p0;      // every row sees every key
-        const int seen[2] = {min(have[0], p + 1 - pos[0]), min(have[1], p + 1 - pos[1])};      // keys that row l16 sees
-        more = find();                                   // none left: the last pieces are requested once more, and not used
-        f32x4 s[2];
-#pragma unroll
-        for (int h = 0; h < 2; ++h) {
-            typename Tile::Scores sum;
-            const float kp = kv8_power(first_used_here(ke[h]));
-#pragma unroll
-            for (int j = 0; j < KS; ++j) {
-                const bf16x8 k = kv8_to_bf16(half_of(kx[h][j / 2], j), kp);
-                t.template add_scores<1>(&k, j, sum);
+            for (int h = 0; h < 2; ++h) {
+                if (h == 1 && !left) {                       // a single one: the other half repeats it, unseen
+                    have[1] = 0;
+                    c0[1] = c0[0];
+                    pos[1] = pos[0];
+                    base[1] = base[0];
+                    break;
+                }
+                const int i = __builtin_ctzll(left);
+                left &= left - 1;
+                have[h] = __builtin_amdgcn_readlane(u_rows, i);
+                pos[h] = __builtin_amdgcn_readlane(u_pos, i);
+                c0[h] = pos[h] - a.by_block(pos[h]) * a.block;
+                base[h] = a.pool + (size_t)__builtin_amdgcn_readlane(u_slot, i) * a.slot_bytes + a.layer_offset;
             }
-            s[h] = sum.sum();
+            return true;
+        };
+
+        uint4 kx[2][PC], vx[2][PC];
+        uint32_t ke[2], ve[2];                               // e + 127
+        // Addresses: a wave-uniform base and a 32-bit offset of the lane.  Rows behind the last key repeat it: not seen.  A lane's channels are 16 in a row of each 64, so that an instruction
+        // takes 64 bytes in a row of each key.
+        auto row_offset = [&](int h) { return (unsigned)(min(l16, max(have[h], 1) - 1) * D + qr * 16); };
+        auto channel = [&](int j) { return j / 2 * 64 + qr * 16 + j % 2 * 8; };
+        auto load_k = [&]() {
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+                const unsigned char* at = base[h] + head.k + (size_t)c0[h] * D;
+                const unsigned off = row_offset(h);
+#pragma unroll
+                for (int c = 0; c < PC; ++c) kx[h][c] = *reinterpret_cast<const uint4*>(at + (off + c * 64));
+                ke[h] = base[h][head.e + (lane & 0)];
+            }
+        };
+        auto load_v = [&]() {
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+                const unsigned char* at = base[h] + head.v + (size_t)c0[h] * D;
+                const unsigned off = row_offset(h);
+#pragma unroll
+                for (int c = 0; c < PC; ++c) vx[h][c] = *reinterpret_cast<const uint4*>(at + (off + c * 64));
+                ve[h] = base[h][head.e + 1 + (lane & 0)];
+            }
+        };
+        auto half_of = [](const uint4& c, int j) { return j % 2 ? make_uint2(c.z, c.w) : make_uint2(c.x, c.y); };
+        bool more = find();
+        if (more) { load_k(); load_v(); }
+
+        // the lane's rows, one in each 16
+        int p[NR];
+        Tile t[NR];
+#pragma unroll
+        for (int y = 0; y < NR; ++y) {
+            const int lrow = row0 + min(y * kTileRows + l16, rows - 1), token = a.by_group(lrow);
+            p[y] = me.len - me.n + token;
+            t[y].begin(q + (size_t)(me.lo + token) * a.ldq + (size_t)(g * G + lrow - token * G) * D, channel);
+            // waited for here: waited for in the loop, the Query fragments take the wait for the codes requested meanwhile with them in every turn
+#pragma unroll
+            for (int b = 0; b < NT; ++b)
+#pragma unroll
+                for (int j = 0; j < KS; ++j) asm volatile("" : "+v"(t[y].q[b][j]));
         }
-        __builtin_amdgcn_sched_barrier(0);
-        load_k();                                        // the next pieces' Keys fly under these Values
-        __builtin_amdgcn_sched_barrier(0);
-        if (!whole) {
+        // Where the lane writes and reads the wave's V tile: one address each, whose bits 4 .. 7 are turned for the pieces and channels.  (Hidden from the compiler in every turn: it would keep
+        // them all in registers, and the Query fragments out of them.)
+        const int vr = 4 * qr + (l16 >> 2);
+        unsigned v_to = tile_lds + Tile::v_piece(l16, qr * 2), v_from = tile_lds + Tile::v_piece(vr, (l16 & 3) >> 1) + (l16 & 1) * 8;
+        while (more) {
+            asm volatile("" : "+v"(v_to), "+v"(v_from));
+            const bool whole = have[0] == kPiece && have[1] == kPiece && max(pos[0], pos[1]) + kPiece - 1 <= p0;      // every row sees every key
+            int seen[NR][2];                                 // keys that the lane's rows see
+#pragma unroll
+            for (int y = 0; y < NR; ++y)
+#pragma unroll
+                for (int h = 0; h < 2; ++h) seen[y][h] = min(have[h], p[y] + 1 - pos[h]);
+            more = find();                                   // none left: the last pieces are requested once more, and not used
+            f32x4 s[NR][2];
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+                typename Tile::Scores sum[NR];
+                const float kp = kv8_power(first_used_here(ke[h]));
+#pragma unroll
+                for (int j = 0; j < KS; ++j) {
+                    const bf16x8 k = kv8_to_bf16(half_of(kx[h][j / 2], j), kp);
+#pragma unroll
+                    for (int y = 0; y < NR; ++y) t[y].template add_scores<1>(&k, j, sum[y]);
+                }
+#pragma unroll
+                for (int y = 0; y < NR; ++y) s[y][h] = sum[y].sum();
+            }
+            __builtin_amdgcn_sched_barrier(0);
+            load_k();                                        // the next pieces' Keys fly under these Values
+            __builtin_amdgcn_sched_barrier(0);
+            if (!whole) {
+#pragma unroll
+                for (int y = 0; y < NR; ++y)
+#pragma unroll
+                    for (int h = 0; h < 2; ++h)
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) {
+                            const float x = s[y][h][e];
+                            s[y][h][e] = qr * 4 + e < seen[y][h] ? x : -INFINITY;
+                        }
+            }
+            bf16x8 pw[NR][NP];
+#pragma unroll
+            for (int y = 0; y < NR; ++y) {
+                float w[8];
+                t[y].weigh(s[y], a.scale_log2e, w);
+                bf16_terms<NP>(w, pw[y]);
+            }
+            float vp[2];
+#pragma unroll
+            for (int h = 0; h < 2; ++h) vp[h] = kv8_power(first_used_here(ve[h]));
+            if (!whole) {
+                // Values that some row does not see and that are not numbers: their weight is 0, which a product would turn into an undefined sum.  They become zeros here, and what makes a row
+                // that sees one of them undefined is its sum.
+#pragma unroll
+                for (int h = 0; h < 2; ++h) {
+                    bool odd = false;
+#pragma unroll
+                    for (int c = 0; c < PC; ++c)
+#pragma unroll
+                        for (int i = 0; i < 4; ++i) {
+                            uint32_t& x = i == 0 ? vx[h][c].x : i == 1 ? vx[h][c].y : i == 2 ? vx[h][c].z : vx[h][c].w;
+                            const uint32_t bytes = (((x & 0x7f7f7f7fu) + 0x01010101u) >> 7 & 0x01010101u) * 0xffu;
+                            odd |= bytes != 0;
+                            x &= ~bytes;
+                        }
+                    const unsigned long long lanes = __ballot(odd);
+                    if (lanes) {
+                        const unsigned keys = (unsigned)(lanes | lanes >> 16 | lanes >> 32 | lanes >> 48) & 0xffffu;
+#pragma unroll
+                        for (int y = 0; y < NR; ++y)
+                            if (keys & ((1u << max(seen[y][h], 0)) - 1u)) t[y].l = NAN;
+                    }
+                }
+            }
 #pragma unroll
             for (int h = 0; h < 2; ++h)
 #pragma unroll
-                for (int e = 0; e < 4; ++e) {
-                    const float x = s[h][e];
-                    s[h][e] = qr * 4 + e < seen[h] ? x : -INFINITY;
-                }
-        }
-        t.weigh(s, a.scale_log2e, w);
-        float vp[2];
+                for (int j = 0; j < KS; ++j) *(LdsB128)((v_to ^ ((j / 2 * 8 + j % 2) << 4)) + h * (16 * D * 2)) = kv8_to_bf16(half_of(vx[h][j / 2], j), vp[h]);
+            __builtin_amdgcn_sched_barrier(0);
+            load_v();
+            __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
-        for (int h = 0; h < 2; ++h) vp[h] = kv8_power(first_used_here(ve[h]));
-        if (!whole) {
-            // Values that some row does not see and that are not numbers: their weight is 0, which a product would turn into an undefined sum.  They become zeros here, and what makes a row
-            // that sees one of them undefined is its sum.
+            for (int dt = 0; dt < Tile::DT; ++dt) {
+                const bf16x8 v = Tile::read_channels(v_from ^ (dt << 5));
 #pragma unroll
-            for (int h = 0; h < 2; ++h) {
-                bool odd = false;
-#pragma unroll
-                for (int c = 0; c < PC; ++c)
-#pragma unroll
-                    for (int i = 0; i < 4; ++i) {
-                        uint32_t& x = i == 0 ? vx[h][c].x : i == 1 ? vx[h][c].y : i == 2 ? vx[h][c].z : vx[h][c].w;
-                        const uint32_t bytes = (((x & 0x7f7f7f7fu) + 0x01010101u) >> 7 & 0x01010101u) * 0xffu;
-                        odd |= bytes != 0;
-                        x &= ~bytes;
-                    }
-                const unsigned long long lanes = __ballot(odd);
-                if (lanes) {
-                    const unsigned keys = (unsigned)(lanes | lanes >> 16 | lanes >> 32 | lanes >> 48) & 0xffffu;
-                    if (keys & ((1u << max(seen[h], 0)) - 1u)) t.l = NAN;
-                }
+                for (int y = 0; y < NR; ++y) t[y].template add_read<1>(pw[y], 0, dt, v);
             }
         }
-        bf16_terms<NP>(w, pw);
-#pragma unroll
-        for (int h = 0; h < 2; ++h)
-#pragma unroll
-            for (int j = 0; j < KS; ++j) *(LdsB128)((v_to ^ ((j / 2 * 8 + j % 2) << 4)) + h * (16 * D * 2)) = kv8_to_bf16(half_of(vx[h][j / 2], j), vp[h]);
-        __builtin_amdgcn_sched_barrier(0);
-        load_v();
-        __builtin_amdgcn_sched_barrier(0);
-#pragma unroll
-        for (int dt = 0; dt < Tile::DT; ++dt) t.template add_channels<1>(pw, 0, dt, v_from ^ (dt << 5));
-    }
 
-    const bool whole_tile = from == 0 && take >= pieces;
-    if (from < pieces || whole_tile) {                // (else nothing but the tile's end is left in this share)
-        if (from == 0 && tid < rows) {
-            const int i = row0 + tid, n = i / G;
-            const long long to = begin + share - left_over + pieces - 1;      // (what the share has taken so far is share - left_over, but for the last one, which ends with its tile)
-            const int n_shares = whole_tile ? 1 : (int)(to / share) - share_of + 1;
-            a.where[(size_t)(me.lo + n) * a.Hq + g * G + i - n * G] = make_int2((blockIdx.x * 2 + 1) * kTileRows + tid, 2 * n_shares);
-        }
-        float* part = a.part + (size_t)(blockIdx.x * 2 + (from == 0)) * kTileRows * (D + 4);
-        merge_waves<T, D, NW>(t, lds, rows, [&](int i, int dd, float acc, float l, float M) {
-            if (whole_tile) {
-                const int x = row0 + i, n = x / G;
-                Elem<T>::st(out + (size_t)(me.lo + n) * a.ldo + (size_t)(g * G + x - n * G) * D + dd, l == 0.f ? 0.f : acc / l);
-            } else {
-                float* dst = part + i * (D + 4);
-                dst[dd] = acc;
-                if (dd == 0) { dst[D] = M; dst[D + 1] = l; }
+        const bool whole_tile = from == 0 && take >= pieces;
+        if (from < pieces || whole_tile) {                // (else nothing but the tile's end is left in this share)
+            if (from == 0 && tid < rows) {
+                const int i = row0 + tid, n = i / G;
+                const long long to = begin + share - left_over + pieces - 1;      // (what the share has taken so far is share - left_over, but for the last one, which ends with its tile)
+                const int n_shares = whole_tile ? 1 : (int)(to / share) - share_of + 1;
+                a.where[(size_t)(me.lo + n) * a.Hq + g * G + i - n * G] = make_int2((blockIdx.x * 2 + 1) * TR + tid, 2 * n_shares);
             }
-        }, tid);
-        __syncthreads();                                 // the waves' tiles are read before they are written again
-    }
-    left_over -= take;
-    if (left_over <= 0) return;
-    from = 0;
-    if (++tile == me.tiles(a)) {
-        tile = 0;
-        unsigned long long more_rows = __ballot(x.n > 0) & ~((2ull << i_req) - 1);
-        while (!more_rows) {
-            r0 += 64;
-            if (r0 >= a.R) return;
-            x = request(r0 + lane_in);
-            more_rows = __ballot(x.n > 0);
+            float* part = a.part + (size_t)(blockIdx.x * 2 + (from == 0)) * TR * (D + 4);
+#pragma unroll
+            for (int y = 0; y < NR; ++y) {
+                const int in_half = rows - y * kTileRows;
+                if (y > 0 && in_half <= 0) break;
+                merge_waves<T, D, NW>(t[y], lds, min(kTileRows, in_half), [&](int i, int dd, float acc, float l, float M) {
+                    i += y * kTileRows;
+                    if (whole_tile) {
+                        const int x = row0 + i, n = x / G;
+                        Elem<T>::st(out + (size_t)(me.lo + n) * a.ldo + (size_t)(g * G + x - n * G) * D + dd, l == 0.f ? 0.f : acc / l);
+                    } else {
+                        float* dst = part + i * (D + 4);
+                        dst[dd] = acc;
+                        if (dd == 0) { dst[D] = M; dst[D + 1] = l; }
+                    }
+                }, tid);
+                __syncthreads();                             // the waves' tiles are read before they are written again
+            }
         }
-        i_req = __builtin_ctzll(more_rows);
-    }
+        left_over -= take;
+        if (left_over <= 0) return;
+        from = 0;
+        if (++tile == me.template tiles<TR>(a)) {
+            tile = 0;
+            unsigned long long more_rows = __ballot(x.n > 0) & ~((2ull << i_req) - 1);
+            while (!more_rows) {
+                r0 += 64;
+                if (r0 >= a.R) return;
+                x = request(r0 + lane_in);
+                more_rows = __ballot(x.n > 0);
+            }
+            i_req = __builtin_ctzll(more_rows);
+        }
     }
 }
 
@@ -1096,7 +1124,7 @@ __global__ void __launch_bounds__(256) batch_merge_kernel(T* __restrict__ out, B
         const bool many = at.y & 1;
         first = at.x;
         n = at.y >> 1;
-        back = many ? kManyRows : kTileRows;
+        back = many ? kManyRows : a.tile_rows;
         apart = 2 * a.Hkv * back;
         if (n <= 1 || first < back || first - back + (long long)(n - 1) * apart >= (many ? kPartRows : kFewPartRows)) n = 0;
     }
@@ -1176,25 +1204,15 @@ template <typename K> static int raise_lds(K kernel, int bytes, Raised& raised) 
     return raised.err[dev] == hipSuccess ? SLIM_OK : set_hip_error(raised.err[dev]);
 }
 
-template <typename T, int D>
-static int launch_batch_attn(const void* q, void* out, BatchAttnArgs& a, hipStream_t st) {
-    const int shares = std::max(1, batch_grid<T, D>() / a.Hkv);
-    a.by_shares = Divide(shares);
+template <typename T, int D, int NR>
+static int launch_few(const void* q, void* out, BatchAttnArgs& a, hipStream_t st) {
+    const int shares = std::max(1, batch_grid<T, D, NR>() / a.Hkv);
     const long long rows = (long long)a.n_rows * a.Hq;
+    a.by_shares = Divide(shares);
+    a.tile_rows = NR * kTileRows;
     constexpr int NW = kBatchWaves, smem = NW * RowTile<T, D>::kLdsBytes;
-    static_assert(smem < 1 << 16, "within the limit that needs no raising");
-    if constexpr (sizeof(T) == 2)
-        // A request of many rows can only be there with more rows than that; with 16 and fewer on average the batch is taken for one of new tokens and drafts, which the other kernel
-        // alone serves (empty, the launch costs 5 us; a request of 256 rows among 255 new tokens costs some reads of its keys more).
-        if ((long long)a.n_rows * (a.Hq / a.Hkv) > std::max(kFewRows, kTileRows * a.R)) {
-            constexpr int many_smem = ManyTile<D>::kLdsBytes;
-            static Raised raised;
-            if (const int rc = raise_lds(batch_attn_many_kernel<D>, many_smem, raised)) return rc;
-            a.few = kFewRows;
-            hipLaunchKernelGGL((batch_attn_many_kernel<D>), dim3(std::max(1, kManyGrid / a.Hkv) * a.Hkv), dim3(512), many_smem, st, (const bf16_t*)q, (bf16_t*)out, a);
-            if (const int rc = check_launch()) return rc;
-        }
-    hipLaunchKernelGGL((batch_attn_kv8_kernel<T, D, NW>), dim3(shares * a.Hkv), dim3(64 * NW), smem, st, (const T*)q, (T*)out, a);
+    static_assert(smem < 1 << 16 && batch_grid<T, D, NR>() * 2 * NR * kTileRows <= kFewPartRows, "within the limit that needs no raising, and the workspace");
+    hipLaunchKernelGGL((batch_attn_kv8_kernel<T, D, NW, NR>), dim3(shares * a.Hkv), dim3(64 * NW), smem, st, (const T*)q, (T*)out, a);
     const int rc = check_launch();
     if (rc || shares == 1) return rc;                    // (no tile is shared)
     constexpr int kOne = 256 / (D / 4);                  // rows of a workgroup without groups
@@ -1205,11 +1223,32 @@ static int launch_batch_attn(const void* q, void* out, BatchAttnArgs& a, hipStre
     return check_launch();
 }
 
+template <typename T, int D>
+static int launch_batch_attn(const void* q, void* out, BatchAttnArgs& a, hipStream_t st) {
+    if constexpr (sizeof(T) == 2)
+        // With 16 rows a request and fewer on average the batch is taken for one of new tokens and short drafts, which tiles of 16 rows alone serve (a request of 256 rows among 255 new tokens
+        // costs some reads of its keys more).  With more, tiles of 32 rows read the keys half as often: 64 requests of 4096 tokens and 20 rows 110 us, with tiles of 16 rows 195; of 2048 tokens
+        // and 64 rows 121 and 193; a single request of 2048 tokens and 64 rows, which leaves workgroups free, 21 and 18.  (Longer tiles still, of 48 rows, do not fit the registers; float32
+        // tiles of 32 do not either.)  A request of many rows can only be there with more than kFewRows altogether: empty, the launch for many costs 5 us.
+        if (const long long rows = (long long)a.n_rows * (a.Hq / a.Hkv); rows > (long long)kTileRows * a.R) {
+            if (rows > kFewRows) {
+                constexpr int many_smem = ManyTile<D>::kLdsBytes;
+                static Raised raised;
+                if (const int rc = raise_lds(batch_attn_many_kernel<D>, many_smem, raised)) return rc;
+                a.few = kFewRows;
+                hipLaunchKernelGGL((batch_attn_many_kernel<D>), dim3(std::max(1, kManyGrid / a.Hkv) * a.Hkv), dim3(512), many_smem, st, (const bf16_t*)q, (bf16_t*)out, a);
+                if (const int rc = check_launch()) return rc;
+            }
+            return launch_few<T, D, 2>(q, out, a, st);
+        }
+    return launch_few<T, D, 1>(q, out, a, st);
+}
+
 int launch_batch_attn_kv8(const void* q, int ldq, const int* row_start, const int* lens, const int* table, int R, int n_rows, int max_blocks, const void* pool, int n_slots, size_t slot_bytes,
                           size_t layer_offset, int block, int Hq, int Hkv, int d, float scale, int dtype, void* out, int ldo, void* workspace, hipStream_t st) {
     const int per_block = (block + kPiece - 1) / kPiece;
     BatchAttnArgs a{row_start, lens, table, (const unsigned char*)pool, slot_bytes, layer_offset, (float*)workspace, (int2*)((char*)workspace + batch_part_bytes(n_rows, Hq, Hkv, d)),
-                    scale * 1.4426950408889634f, R, max_blocks, n_slots, n_rows, block, per_block, Hq, Hkv, ldq, ldo, 0x7fffffff, Divide(block), Divide(per_block), Divide(Hq / Hkv), Divide(1)};
+                    scale * 1.4426950408889634f, R, max_blocks, n_slots, n_rows, block, per_block, Hq, Hkv, ldq, ldo, 0x7fffffff, kTileRows, Divide(block), Divide(per_block), Divide(Hq / Hkv), Divide(1)};
     if (dtype == SLIM_BF16) return d == 64 ? launch_batch_attn<bf16_t, 64>(q, out, a, st) : launch_batch_attn<bf16_t, 128>(q, out, a, st);
     return d == 64 ? launch_batch_attn<float, 64>(q, out, a, st) : launch_batch_attn<float, 128>(q, out, a, st);
 }

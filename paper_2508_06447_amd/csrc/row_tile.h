@@ -156,10 +156,13 @@ template <typename T, int D> struct RowTile {
         for (int dt = 0; dt < DT; ++dt) add_channels<NV>(p, a, dt, lds_tile + v_piece(r, dt * 2 + ((s16 & 3) >> 1)) + (s16 & 1) * 8);
     }
     // The same for channels 16 dt ..; at: where the lane reads them.
-    template <int NV> __device__ __forceinline__ void add_channels(const bf16x8* p, int a, int dt, unsigned at) {
+    template <int NV> __device__ __forceinline__ void add_channels(const bf16x8* p, int a, int dt, unsigned at) { add_read<NV>(p, a, dt, read_channels(at)); }
+    __device__ static __forceinline__ bf16x8 read_channels(unsigned at) {
         const bf16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4bf16((LdsB64)at);
         const bf16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4bf16((LdsB64)(at + 16 * D * 2));
-        const bf16x8 v = __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
+        return __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
+    }
+    template <int NV> __device__ __forceinline__ void add_read(const bf16x8* p, int a, int dt, bf16x8 v) {
         if constexpr (NT == 1) {
 #pragma unroll
             for (int b = NP - 1; b >= 0; --b) o[dt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(v, p[b], o[dt], 0, 0, 0);
