@@ -18,10 +18,6 @@ SOURCES = ("api.hip", "prune.hip", "norm_rope.hip", "gemm.hip", "split.hip", "at
 FLAGS = ["-O3", "-mllvm", "-amdgpu-kernarg-preload-count=16", "--offload-arch=gfx950", "-std=c++17", "-fPIC", "-Xclang", "-target-feature", "-Xclang",
          "-packed-fp32-ops", "-Wno-unused-command-line-argument", "-I" + os.path.join(ROOT, "include"), "-I" + CSRC]
 
-# Matrix instructions whose results stay among the registers that vector instructions read: otherwise the kernel for requests of many rows (392 registers a lane) moves 370 registers from
-# one kind to the other for 64 keys, 20 with it.
-SOURCE_FLAGS = {"kv8.hip": ["-mllvm", "-amdgpu-mfma-vgpr-form=1"]}
-
 
 def build_lib(verbose: bool = True, extra_flags=()) -> str:
     """Compile every HIP source and link libslim.so; returns its path."""
@@ -30,7 +26,7 @@ def build_lib(verbose: bool = True, extra_flags=()) -> str:
     procs = []
     for src in SOURCES:
         obj = os.path.join(CSRC, src.replace(".hip", ".o"))
-        cmd = [hipcc, *FLAGS, *SOURCE_FLAGS.get(src, ()), *extra_flags, "-c", os.path.join(CSRC, src), "-o", obj]
+        cmd = [hipcc, *FLAGS, *extra_flags, "-c", os.path.join(CSRC, src), "-o", obj]
         if verbose:
             print(" ".join(cmd), flush=True)
         procs.append((src, subprocess.Popen(cmd, stdout=subprocess.PIPE, stderr=subprocess.STDOUT, text=True)))

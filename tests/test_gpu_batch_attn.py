@@ -93,6 +93,12 @@ CASES = [
     ([100], [70], 48, 17, 1, 128, F32),
     ([2000, 5, 64, 900], [1, 130, 1, 2], 64, 8, 2, 128, BF16),
     ([12000], [40], 64, 4, 1, 128, BF16),
+    # more than 16 rows a request, and up to 64: tiles of 32 rows, some of them half empty
+    ([5000], [13], 64, 8, 2, 128, BF16),
+    ([600, 0, 31, 2000, 64, 1], [17, 16, 33, 32, 1, 15], 32, 4, 2, 64, BF16),
+    ([90 * i % 1300 for i in range(90)], [1 + 7 * i % 12 for i in range(90)], 48, 10, 2, 128, BF16),
+    ([40, 700, 0], [30, 100, 2], 16, 4, 2, 64, BF16),
+    ([4000, 200], [3, 2], 64, 64, 8, 64, BF16),
 ]
 
 
@@ -123,7 +129,7 @@ def test_rows_that_see_nothing_are_zero_and_padding_stays(slim, dtype):
     assert (out == 0).all()
 
 
-@pytest.mark.parametrize("n,dtype", [(3, BF16), (40, BF16), (200, BF16), (40, F32)])
+@pytest.mark.parametrize("n,dtype", [(3, BF16), (14, BF16), (40, BF16), (200, BF16), (40, F32)])
 def test_what_a_row_does_not_see_does_not_reach_it(slim, n, dtype):
     """Keys and values of later tokens that are not numbers, and exponents of blocks behind them."""
     lens, block, Hq, Hkv, d = 50, 16, 4, 2, 128
@@ -163,11 +169,13 @@ def test_large_and_flat_scores(slim):
         within(out, want[0], ref.attention_bound(want, dtype))
 
 
-def test_results_do_not_depend_on_the_workspace_the_slots_or_the_call(slim):
+@pytest.mark.parametrize("new", [[1, 5, 70], [10, 5, 1]])
+def test_results_do_not_depend_on_the_workspace_the_slots_or_the_call(slim, new):
     """The same bits again, from a workspace of other bytes and from slots in another order."""
-    lens, new, block, Hq, Hkv, d = [900, 40, 3000], [1, 5, 70], 64, 8, 2, 128
+    lens, block, Hq, Hkv, d = [900, 40, 3000], 64, 8, 2, 128
     pool, table, start, total = make(lens, new, block, Hkv, d, 1)
-    q = rand((76, Hq, d), BF16, 3).cuda()
+    n = sum(new)
+    q = rand((n, Hq, d), BF16, 3).cuda()
     outs = []
     for seed in (0, 1, 2):
         g = np.random.default_rng(seed)
@@ -175,7 +183,7 @@ def test_results_do_not_depend_on_the_workspace_the_slots_or_the_call(slim):
         moved = np.empty_like(pool)
         moved[order] = pool
         t = np.where((table >= 0) & (table < len(order)), order[np.clip(table, 0, len(order) - 1)], -1)
-        ws = torch.full((slim.batch_attn_kv8_workspace_bytes(76, 3, Hq, Hkv, d),), 127 * seed, dtype=torch.uint8, device="cuda")
+        ws = torch.full((slim.batch_attn_kv8_workspace_bytes(n, 3, Hq, Hkv, d),), 127 * seed, dtype=torch.uint8, device="cuda")
         outs.append(slim.slim_batch_attn_kv8(q, i32(start), i32(total), i32(t), torch.from_numpy(moved).cuda(), block, Hkv, workspace=ws))
     assert torch.equal(outs[0], outs[1]) and torch.equal(outs[0], outs[2]) and torch.isfinite(outs[0]).all()
 
