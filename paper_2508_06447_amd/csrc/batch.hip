@@ -5,7 +5,8 @@
 //
 // One launch: every workgroup forms both sums for itself in LDS, since a row needs all of them in front of it, and takes a share of the rows and of the new blocks (there are no
 // more new blocks than rows).  A row finds its request by bisection of row_start; its block's slot comes from the table where the block was there and from the list where it is new, so
-// that no workgroup reads what another one writes.  What is read and written is small (32768 rows: 0.2 MB); bound by the trips to memory one behind the other.
+// that no workgroup reads what another one writes.  What is read and written is small (32768 rows: 0.26 MB); bound by the trips to memory one behind the other: 4.4 us for 256 requests of a
+// token, 4.3 for 37 prompts of 26028, of which 2.5 are a launch's.
 #include "slim_common.h"
 #include "batch.h"
 #include <algorithm>

@@ -56,6 +56,8 @@ __device__ __forceinline__ uint32_t kv8_codes(const float* f, float power) {
 // A workgroup takes the runs that begin within its `chunk` rows of the map, for Keys or Values of `heads` kv heads.  A run of more than kKv8Short rows is the whole workgroup's, head by head:
 // its rows stay in registers, up to kKv8Keep passes of them, and the next head's are on their way.  Shorter ones, the new tokens of a step, are a wave's, for as many heads as it has
 // rows' lanes for (64 / (D / 8)).  Rows, old exponent and the run's length are requested together: two trips to memory.
+// Bound by memory where there are many rows: 26381 of 24 prompts, 8 heads of 128, 161 MB, 41 us, 3.9 TB/s (a copy of as much takes 32); by the trips where there are few: 256 new tokens
+// 6.3 us, 3 us of which a launch costs.
 constexpr int kKv8Keep = 4, kKv8Short = 8;
 struct Kv8Write {
     const int* row_slot;
@@ -279,6 +281,8 @@ __global__ void __launch_bounds__(256) kv8_write_kernel(const T* __restrict__ K,
 
 int launch_kv8_write(const void* k, const void* v, int ldk, int ldv, const int* row_slot, int n_rows, int Hkv, int d, int block, int dtype, void* pool, int n_slots, size_t slot_bytes,
                      size_t layer_offset, hipStream_t st) {
+    // Few rows in small chunks, so that there are workgroups for all CUs, many in the largest, which look at the map least: 256 tokens of 8 heads 6.2 us in chunks of 4, 37 of 64 (whose waves
+    // take run after run); 26381 rows 78 and 42.  Four heads a workgroup: with 4, 2, 1 those take 41.9, 42.3 and 44.6.
     const int chunk = (int)std::min<long long>(64, std::max<long long>(4, (long long)n_rows * Hkv * 2 / 4096));
     const int heads = 4;
     const Kv8Write a{row_slot, (unsigned char*)pool, slot_bytes, layer_offset, n_rows, n_slots * block, block, Hkv, ldk, ldv, chunk, heads, Divide(block)};
@@ -292,7 +296,9 @@ int launch_kv8_write(const void* k, const void* v, int ldk, int ldv, const int* 
 }
 
 // ---- read back
-constexpr int kKv8Steps = 4;
+// Codes once, rows once: a lane takes eight channels of kKv8Steps rows, a wave the rows of its head that lie side by side.  Bound by memory: 9856 tokens of 8 heads of 128 (60 MB) 11.4 us,
+// 32768 (201 MB) 24.3, what its launch and the lookup of a slot cost beside it: 64 tokens 3.0.  One, two, four rows: 9856 tokens 10.8, 11.4, 12.3 us, 32768 26.6, 24.3, 26.0.
+constexpr int kKv8Steps = 2;
 struct Kv8Read {
     const unsigned char* pool;
     size_t slot_bytes, layer_offset;
@@ -359,10 +365,14 @@ int launch_kv8_read(const void* pool, int n_slots, size_t slot_bytes, size_t lay
 }
 
 // ---- attention
-// A request's rows are its (query, query head of the kv head) pairs, query by query, head by head; a tile is 16 of them, or, in batches of drafts, 32.  A piece is up to 16 keys of one block.  The pieces of all tiles of
-// all requests, one behind the other, are cut into equal shares, one workgroup a share, so that requests of any lengths keep all workgroups busy to the end.  A workgroup goes through its
-// share tile by tile; its waves take two pieces in turn, from wherever they lie.  A tile that lies in one share is written at once, one that several share is left as partial results, which
-// a second kernel merges.  The lengths are known to the GPU alone, so that each wave forms the sums over the requests for itself, 64 of them at a time.
+// A request's rows are its (query, query head of the kv head) pairs, query by query, head by head; a tile is 16 of them, or 32 in batches of longer drafts.  A piece is up to 16 keys of one
+// block.  The pieces of all tiles of all requests, one behind the other, are cut into equal shares, one workgroup a share, so that requests of any lengths keep all workgroups busy to the
+// end.  A workgroup goes through its share tile by tile; its waves take two pieces in turn, from wherever they lie.  A tile that lies in one share is written at once, one that several
+// share is left as partial results, which a second kernel merges.  The lengths are known to the GPU alone, so that each wave forms the sums over the requests for itself, 64 of them at a time.
+// The Keys' codes become bfloat16 in the lanes that read them, in the order of the matrix instruction; the Values' go through LDS, whose transposing read gives the other operand.  The
+// next pieces' codes are requested as soon as the registers of the present ones are free.
+// Bound by the codes' way from memory: 256 requests of one token, 32 heads over 8 of 128, of 751 MB altogether, 150 us and 5 to merge, 4.9 TB/s (a kernel that only reads them 145); one of
+// 131072 tokens, 268 MB, 54 and 5 (52); 48 requests with up to 4 drafts, 279 MB, 73 and 5 (65).
 constexpr int kPiece = 16;
 constexpr int kBatchWaves = 4;
 constexpr int kBatchGrid = 768;                          // workgroups: as many as run together, three a CU (bfloat16 heads of 128: 256 requests 150 us, with 512 157, drafts 73 and 84)
@@ -370,7 +380,7 @@ constexpr int kBatchGrid = 768;                          // workgroups: as many 
 template <typename T, int D, int NR> constexpr int batch_grid() { return sizeof(T) == 2 && D == 128 && NR == 1 ? kBatchGrid : 512; }
 constexpr int kBatchLeast = 2 * 2 * kBatchWaves;         // pieces of a share: two turns of its waves (one request of 500 to 4000 tokens 13 us; with one turn 13, with four 14 to 16, with eight
                                                          // 14 to 20); of tiles of 32 rows, whose turns are longer, one (16 queries of a request of 512 or 2048 tokens 17 and 21 us, with two 23 and 25)
-constexpr int kBatchTile = 8;                            // what beginning and ending a tile counts for, in pieces
+constexpr int kBatchTile = 8;                            // what beginning and ending a tile counts for, in pieces (256 requests 156 us, with 2 165, with 24 156)
 constexpr int kFewRows = 64, kManyRows = 256, kManyGrid = 256;      // rows of a request up to which tiles have 16 or 32 rows; rows of the tiles for more; their workgroups
 constexpr int kFewPartRows = 512 * 2 * 2 * kTileRows, kPartRows = kFewPartRows + kManyGrid * 2 * kManyRows;      // rows of partial results
 
@@ -713,6 +723,9 @@ __global__ void __launch_bounds__(64 * NW, sizeof(T) == 2 && NR == 1 ? 3 : 2) ba
 // A weight is one bfloat16 (off by 2^-9 of itself at most, as the output is in the end), and the sum is that of the unrounded ones.  The reference of a row's weights is a power of
 // two at the largest score when it was set, and is set anew only when a score is more than 2^30 above it: float32 and bfloat16 have room for that on both sides, and nothing is
 // rescaled in nearly all phases.
+// Bound by the matrix units at the clock that the chip's power leaves them, and by the arithmetic beside them: 1511 queries behind 9856 tokens, 28 heads over 4 of 128, 230 GFLOP in
+// 245 to 275 us, 0.84 to 0.94 PFLOP/s, where a library product of 8192^3 reaches 1.37 and matrix instructions alone 1.75.  Without exponentials it takes 57 us less, without LDS 39: no one
+// of them bounds it alone.  16 rows a wave 484 us; 64 rows a wave, with all 512 registers, 271 to 279.
 constexpr int kManyKeys = 64;
 template <int D> struct ManyTile {
     // Rows of D bfloat16 and 16 bytes (Keys: 16 keys' same piece of 16 bytes) or 64 (Values: four keys' same 64 bytes) cover all banks once, and every address of a lane is one base and a constant.
@@ -731,7 +744,8 @@ __global__ void __launch_bounds__(512, 2) batch_attn_many_kernel(const bf16_t* _
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), l32 = lane & 31, h = lane >> 5;
     const unsigned lds0 = (unsigned)(uintptr_t)lds;
 
-    // What a tile costs: the tokens that its last row sees, and some for beginning and ending it, times G so that it is a whole number: each of a request's tiles kManyRows more.
+    // What a tile costs: the tokens that its last row sees, and some for beginning and ending it, times G so that it is a whole number: each of a request's tiles kManyRows more.  (64, 256 or
+    // 1024 tokens for it make no difference to long requests.)
     constexpr int kManyTile = 256;
     auto tiles_of = [&](const BatchRequest& x) { return (x.rows(a) + kManyRows - 1) / kManyRows; };
     auto first_cost = [&](const BatchRequest& x) { return (long long)G * (max(x.len - x.n, 0) + kManyTile) + kManyRows; };
@@ -749,6 +763,7 @@ __global__ void __launch_bounds__(512, 2) batch_attn_many_kernel(const bf16_t* _
 #pragma unroll
     for (int o = 32; o > 0; o >>= 1) total += __shfl_xor(total, o, 64);
     total = wave_value(total, 0);
+    // (A new prompt of 512 tokens 40 us in shares of 256 tokens' cost at least, 55 without.)
     const long long share = max((long long)G * 256, (total + shares - 1) / shares), begin = share * share_of;
     long long left_over = min(total - begin, share);
     if (left_over <= 0) return;
@@ -1130,7 +1145,7 @@ __global__ void __launch_bounds__(256) batch_merge_kernel(T* __restrict__ out, B
     }
     const float* p = a.part + (size_t)first * (D + 4);
     float M = -INFINITY, l = 0.f, o[4] = {0.f, 0.f, 0.f, 0.f};
-    constexpr int kAtOnce = 8;                           // requested together
+    constexpr int kAtOnce = NG == 1 ? 3 : 8;             // requested together (NG 1, two or three partial results a row in most cases: 1511 queries of 28 heads 13.5, 12.8, 13.9 and 19.0 us with 2, 3, 4 and 8)
     for (int y0 = grp; y0 < n; y0 += NG * kAtOnce) {
         float2 st[kAtOnce];
         f32x4 v[kAtOnce];
@@ -1216,7 +1231,8 @@ static int launch_few(const void* q, void* out, BatchAttnArgs& a, hipStream_t st
     const int rc = check_launch();
     if (rc || shares == 1) return rc;                    // (no tile is shared)
     constexpr int kOne = 256 / (D / 4);                  // rows of a workgroup without groups
-    if (rows >= kBatchGrid * 4)                          // few partial results of a tile
+    // Many rows have few partial results each, and a group of lanes for each is enough (256 new tokens of 32 heads 5.1 us, with kOne groups 11.5); few have many (131072 tokens 5.2, with one 15.9).
+    if (rows >= kBatchGrid * 4)
         hipLaunchKernelGGL((batch_merge_kernel<T, D, 1>), dim3((unsigned)((rows + kOne - 1) / kOne)), dim3(256), 0, st, (T*)out, a);
     else
         hipLaunchKernelGGL((batch_merge_kernel<T, D, kOne>), dim3((unsigned)rows), dim3(256), 0, st, (T*)out, a);
@@ -1228,8 +1244,8 @@ static int launch_batch_attn(const void* q, void* out, BatchAttnArgs& a, hipStre
     if constexpr (sizeof(T) == 2)
         // With 16 rows a request and fewer on average the batch is taken for one of new tokens and short drafts, which tiles of 16 rows alone serve (a request of 256 rows among 255 new tokens
         // costs some reads of its keys more).  With more, tiles of 32 rows read the keys half as often: 64 requests of 4096 tokens and 20 rows 110 us, with tiles of 16 rows 195; of 2048 tokens
-        // and 64 rows 121 and 193; a single request of 2048 tokens and 64 rows, which leaves workgroups free, 21 and 18.  (Longer tiles still, of 48 rows, do not fit the registers; float32
-        // tiles of 32 do not either.)  A request of many rows can only be there with more than kFewRows altogether: empty, the launch for many costs 5 us.
+        // and 64 rows 121 and 193; a single request of 2048 tokens and 64 rows, which leaves workgroups free, 21 and 18.  A request of many rows can only be there with more than kFewRows altogether: empty, the launch for many costs 5 us.
+        // kFewRows: 8 requests of 8192 tokens with 64 rows each take 70 us in tiles of 32 rows, 81 in those for many, with 96 rows 89 and 84, with 128 96 and 86.
         if (const long long rows = (long long)a.n_rows * (a.Hq / a.Hkv); rows > (long long)kTileRows * a.R) {
             if (rows > kFewRows) {
                 constexpr int many_smem = ManyTile<D>::kLdsBytes;
