@@ -1241,22 +1241,26 @@ static int launch_few(const void* q, void* out, BatchAttnArgs& a, hipStream_t st
 
 template <typename T, int D>
 static int launch_batch_attn(const void* q, void* out, BatchAttnArgs& a, hipStream_t st) {
-    if constexpr (sizeof(T) == 2)
-        // With 16 rows a request and fewer on average the batch is taken for one of new tokens and short drafts, which tiles of 16 rows alone serve (a request of 256 rows among 255 new tokens
-        // costs some reads of its keys more).  With more, tiles of 32 rows read the keys half as often: 64 requests of 4096 tokens and 20 rows 110 us, with tiles of 16 rows 195; of 2048 tokens
-        // and 64 rows 121 and 193; a single request of 2048 tokens and 64 rows, which leaves workgroups free, 21 and 18.  A request of many rows can only be there with more than kFewRows altogether: empty, the launch for many costs 5 us.
+    if constexpr (sizeof(T) == 2) {
+        // The host knows only how many rows there are altogether, and from them what the batch can hold.
+        // A request of more than kFewRows takes the kernel for many, if it is launched: empty, that costs 3 to 5 us.  It is where rows and requests leave room for two of its tiles beside a token
+        // for each request, or for more than 16 rows a request: 255 new tokens behind 1400 with 64, 256, 512 queries behind 8192 take 203, 229, 263 us with it, 178, 265, 376 without.
         // kFewRows: 8 requests of 8192 tokens with 64 rows each take 70 us in tiles of 32 rows, 81 in those for many, with 96 rows 89 and 84, with 128 96 and 86.
-        if (const long long rows = (long long)a.n_rows * (a.Hq / a.Hkv); rows > (long long)kTileRows * a.R) {
-            if (rows > kFewRows) {
-                constexpr int many_smem = ManyTile<D>::kLdsBytes;
-                static Raised raised;
-                if (const int rc = raise_lds(batch_attn_many_kernel<D>, many_smem, raised)) return rc;
-                a.few = kFewRows;
-                hipLaunchKernelGGL((batch_attn_many_kernel<D>), dim3(std::max(1, kManyGrid / a.Hkv) * a.Hkv), dim3(512), many_smem, st, (const bf16_t*)q, (bf16_t*)out, a);
-                if (const int rc = check_launch()) return rc;
-            }
-            return launch_few<T, D, 2>(q, out, a, st);
+        const int G = a.Hq / a.Hkv;
+        const long long rows = (long long)a.n_rows * G;
+        const bool longer = rows > (long long)kTileRows * a.R;
+        if (rows > kFewRows && (longer || (long long)(a.n_rows - a.R) * G > 2 * kManyRows)) {
+            constexpr int many_smem = ManyTile<D>::kLdsBytes;
+            static Raised raised;
+            if (const int rc = raise_lds(batch_attn_many_kernel<D>, many_smem, raised)) return rc;
+            a.few = kFewRows;
+            hipLaunchKernelGGL((batch_attn_many_kernel<D>), dim3(std::max(1, kManyGrid / a.Hkv) * a.Hkv), dim3(512), many_smem, st, (const bf16_t*)q, (bf16_t*)out, a);
+            if (const int rc = check_launch()) return rc;
         }
+        // Tiles of 32 rows read the keys half as often: 64 requests of 4096 tokens and 20 rows 110 us, with tiles of 16 rows 195; of 2048 tokens and 64 rows 121 and 193; a single request of
+        // 2048 tokens and 64 rows, which leaves workgroups free, 21 and 18.
+        if (longer) return launch_few<T, D, 2>(q, out, a, st);
+    }
     return launch_few<T, D, 1>(q, out, a, st);
 }
 
