@@ -16,6 +16,9 @@ namespace slim {
 
 typedef short i16x2 __attribute__((ext_vector_type(2)));
 typedef __bf16 bf16x2_t __attribute__((ext_vector_type(2)));
+typedef _Float16 f16x2 __attribute__((ext_vector_type(2)));
+typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
+typedef float f32x2 __attribute__((ext_vector_type(2)));
 
 constexpr int kKv8ByteLow = 10, kKv8ByteHigh = 246;      // e + 127 of -117 and 119
 constexpr uint32_t kKv8NaN = 0x7f;
@@ -38,6 +41,12 @@ __device__ __forceinline__ bf16x8 kv8_to_bf16(uint2 c, float power) {
     const bf16x2_t a = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(c.x, power, false), b = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(c.x, power, true);
     const bf16x2_t d = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(c.y, power, false), e = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(c.y, power, true);
     return bf16x8{a[0], a[1], b[0], b[1], d[0], d[1], e[0], e[1]};
+}
+// The same as float16.
+__device__ __forceinline__ f16x8 kv8_to_f16(uint2 c, float power) {
+    const f16x2 a = __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(c.x, power, false), b = __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(c.x, power, true);
+    const f16x2 d = __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(c.y, power, false), e = __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(c.y, power, true);
+    return f16x8{a[0], a[1], b[0], b[1], d[0], d[1], e[0], e[1]};
 }
 // Four finite floats as codes relative to 2^e, 448 for what is above.
 __device__ __forceinline__ uint32_t kv8_codes(const float* f, float power) {
@@ -720,9 +729,11 @@ __global__ void __launch_bounds__(64 * NW, sizeof(T) == 2 && NR == 1 ? 3 : 2) ba
 //   O^T[d, row]   = V^T . P^T     whose operand P^T is what the lane holds: V comes through the transposing read in the same order of keys
 // A phase stands for 32 keys: their weights, beside the scores of the 32 behind and the values of the 32 before, a matrix instruction and a lane's arithmetic in turn.  It reads the Values in its
 // first half, the Keys of the next phase in its second.  Four buffers of 64 keys: Values of the keys before, the present and the next keys, and the ones being filled; a barrier each 64 keys.
-// A weight is one bfloat16 (off by 2^-9 of itself at most, as the output is in the end), and the sum is that of the unrounded ones.  The reference of a row's weights is a power of
-// two at the largest score when it was set, and is set anew only when a score is more than 2^30 above it: float32 and bfloat16 have room for that on both sides, and nothing is
-// rescaled in nearly all phases.
+// A weight is one float16, and the Values are theirs as codes, exact in it, so that nothing but a weight's rounding (2^-12 of itself at most) is lost; the power of two 2^e of a key's block
+// goes into the weight: w = 2^(score + e - reference), O = sum of w * code, and the sum of the softmax is that of w * 2^-e, unrounded.  The reference of a row is a whole number, 4 below the
+// largest score + e when it was set, and is set anew only when one is more than 15 above it: nothing is rescaled in nearly all phases, and weights down to 2^-18 of the row's largest keep
+// all places, down to 2^-28 some.  So that the sum stays within float32, e counts as -76 at least, and the codes of blocks with a smaller one are multiplied by the rest, which leaves
+// Values below 2^-67 fewer places.
 // Bound by the matrix units at the clock that the chip's power leaves them, and by the arithmetic beside them: 1511 queries behind 9856 tokens, 28 heads over 4 of 128, 230 GFLOP in
 // 245 to 275 us, 0.84 to 0.94 PFLOP/s, where a library product of 8192^3 reaches 1.37 and matrix instructions alone 1.75.  Without exponentials it takes 57 us less, without LDS 39: no one
 // of them bounds it alone.  16 rows a wave 484 us; 64 rows a wave, with all 512 registers, 271 to 279.
@@ -733,7 +744,8 @@ template <int D> struct ManyTile {
     static constexpr int kFlags = 4 * kBuffer, kLists = kFlags + 32, kLdsBytes = kLists + 8 * 64 * 16;      // four; a bit for each of their keys with a Value that is not a number; a wave's pieces
     static constexpr int KS = D / 16, DT = D / 32;
 };
-constexpr float kManyRoom = 30.f;
+constexpr float kManyAbove = 4.f, kManyRoom = 15.f;      // where the largest weight begins, and how far it may grow: 2^4, 2^15
+constexpr int kManyByteLow = 51, kManySum = 14;          // e + 127 of -76; the sum is kept times 2^14
 
 template <int D>
 __global__ void __launch_bounds__(512, 2) batch_attn_many_kernel(const bf16_t* __restrict__ q, bf16_t* __restrict__ out, BatchAttnArgs a) {
@@ -846,10 +858,12 @@ __global__ void __launch_bounds__(512, 2) batch_attn_many_kernel(const bf16_t* _
         uint4 kx, vx, entry;
         float kp, vp;
         uint2 info_new;                                  // of lanes 0 .. 3: exponents, rows, position
+        int e_new;                                       // and the Values' e
         auto read_list = [&]() {
             entry = list[at_list * 4 + (D == 128 ? wave >> 1 : wave & 3)];
             const uint4 e = list[at_list * 4 + (lane & 3)];
             info_new = make_uint2(e.z, e.w);
+            e_new = min(max((int)(e.z >> 8 & 0xffu), kManyByteLow), kKv8ByteHigh) - 127;
         };
         auto load = [&]() {
             const unsigned char* from = (const unsigned char*)((size_t)entry.y << 32 | entry.x);
@@ -857,7 +871,7 @@ __global__ void __launch_bounds__(512, 2) batch_attn_many_kernel(const bf16_t* _
             kx = *reinterpret_cast<const uint4*>(from + off);
             vx = *reinterpret_cast<const uint4*>(from + values_apart + off);
             kp = kv8_power(entry.z & 0xffu);
-            vp = kv8_power(entry.z >> 8 & 0xffu);
+            vp = kv8_power(127 + min((int)(entry.z >> 8 & 0xffu) - kManyByteLow, 0));
         };
         auto all_full = [](const uint2& info) { return (__ballot(info.x >> 24 & 1u) & 15u) == 15u; };
         // Values of the next keys that are not numbers become zeros, a bit each, where some row does not see all of them (as for few rows).
@@ -884,7 +898,8 @@ __global__ void __launch_bounds__(512, 2) batch_attn_many_kernel(const bf16_t* _
         // A part of the keys' way into a buffer: eight channels of Keys (part 0, 1) or Values (2, 3).
         auto fill_part = [&](int buffer, int part) {
             const uint4 c = part < 2 ? kx : vx;
-            const bf16x8 x = kv8_to_bf16(part % 2 ? make_uint2(c.z, c.w) : make_uint2(c.x, c.y), part < 2 ? kp : vp);
+            const uint2 half = part % 2 ? make_uint2(c.z, c.w) : make_uint2(c.x, c.y);
+            const bf16x8 x = part < 2 ? kv8_to_bf16(half, kp) : __builtin_bit_cast(bf16x8, kv8_to_f16(half, vp));
             if (mine) *(LdsB128)((part < 2 ? fill_k : fill_v) + buffer * Tile::kBuffer + part % 2 * 16) = x;
         };
 
@@ -904,24 +919,37 @@ __global__ void __launch_bounds__(512, 2) batch_attn_many_kernel(const bf16_t* _
         for (int d = 0; d < DT; ++d)
 #pragma unroll
             for (int i = 0; i < 16; ++i) o[d][i] = 0.f;
-        float mc = 0.f, lim = -INFINITY, l = 0.f;        // of row l32: reference in the base-2 domain, score above which it moves, the lane's share of the sum
+        float mc = 0.f, lim = -INFINITY, l = 0.f;        // of row l32: reference in the base-2 domain, what it moves above, the lane's share of the sum
         // Addresses of the lane in a buffer: K fragments (key l32, channels 16 c + 8 h: pieces 2 c + h), V fragments (keys 16 m + 4 h + .., channels 32 d + ..).
         const unsigned k_from = lds0 + l32 * Tile::kRowK + h * 16;
         const unsigned v_from = lds0 + Tile::kSide + (4 * h + (lane >> 2 & 3)) * Tile::kRowV + (lane >> 4 & 1) * 32 + (lane & 3) * 8;
-        bf16x8 kf[KS], vf[DT][2], pf[2][2];
+        bf16x8 kf[KS];
+        f16x8 vf[DT][2], pf[2][2];
         f32x16 s[2];                                     // of 32 keys, and of the next
-        float top[2];                                    // the lane's largest score
+        float top[2];                                    // the lane's largest score + e
+        int e_of[2][2];                                  // of their 16 keys each, in scalar registers
         auto read_k = [&](int buffer, int sub, int c) { kf[c] = *(LdsB128)(k_from + buffer * Tile::kBuffer + sub * (32 * Tile::kRowK) + c * 32); };
         auto read_v = [&](int buffer, int sub, int d, int m) {
             const unsigned from = v_from + buffer * Tile::kBuffer + (sub * 32 + m * 16) * Tile::kRowV + d * 64;
             const bf16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4bf16((LdsB64)from), hi = __builtin_amdgcn_ds_read_tr16_b64_v4bf16((LdsB64)(from + 8 * Tile::kRowV));
-            vf[d][m] = __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
+            vf[d][m] = __builtin_bit_cast(f16x8, __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
+        };
+        auto exponents = [&](int y, int of_lanes) {
+#pragma unroll
+            for (int j = 0; j < 2; ++j) e_of[y][j] = wave_value(of_lanes, y * 2 + j);
+        };
+        auto top_of = [&](int y, float a0, float a1) {
+            return __builtin_elementwise_maximum(fmaf(a0, a.scale_log2e, (float)e_of[y][0]), fmaf(a1, a.scale_log2e, (float)e_of[y][1]));
         };
         auto largest_of = [&](int y) {
-            float mx = s[y][0];
+            float mx[2];
 #pragma unroll
-            for (int i = 1; i < 16; ++i) mx = __builtin_elementwise_maximum(mx, s[y][i]);
-            top[y] = mx;
+            for (int j = 0; j < 2; ++j) {
+                mx[j] = s[y][8 * j];
+#pragma unroll
+                for (int i = 1; i < 8; ++i) mx[j] = __builtin_elementwise_maximum(mx[j], s[y][8 * j + i]);
+            }
+            top[y] = top_of(y, mx[0], mx[1]);
         };
         auto score = [&](int y, int c) {
             if (c == 0)
@@ -929,7 +957,7 @@ __global__ void __launch_bounds__(512, 2) batch_attn_many_kernel(const bf16_t* _
                 for (int i = 0; i < 16; ++i) s[y][i] = 0.f;
             s[y] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf[c], qf[c], s[y], 0, 0, 0);
         };
-        auto value = [&](int y, int m, int d) { o[d] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vf[d][m], pf[y][m], o[d], 0, 0, 0); };
+        auto value = [&](int y, int m, int d) { o[d] = __builtin_amdgcn_mfma_f32_32x32x16_f16(vf[d][m], pf[y][m], o[d], 0, 0, 0); };
         // What the row does not see of 32 keys; where values that are not numbers became zeros, a row that sees one of them is undefined by its sum.
         auto hide = [&](int y, const uint2& info, int buffer) {
             const unsigned odd = *reinterpret_cast<const uint32_t*>(lds + Tile::kFlags + buffer * 8 + y * 4);
@@ -953,20 +981,16 @@ __global__ void __launch_bounds__(512, 2) batch_attn_many_kernel(const bf16_t* _
             if (!__any(top[y] > lim)) return;
             const float mx = fmaxf(top[y], __shfl_xor(top[y], 32, 64));
             if (mx > lim) {
-                const float to = ceilf(mx * a.scale_log2e), al = lim == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(mc - to);
-                l *= al;
+                const float to = ceilf(mx) - kManyAbove, half = lim == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(0.5f * (mc - to)), al = half * half;
+                l = l * half * half;                     // (in two: sums of blocks with small Values are large)
                 mc = to;
-                lim = mx + kManyRoom / a.scale_log2e;
+                lim = to + kManyRoom;
 #pragma unroll
                 for (int d = 0; d < DT; ++d) o[d] *= al;
 #pragma unroll
-                for (int m = 0; m < 2; ++m) {
-                    float f[8];
-                    Elem<bf16_t>::unpack(__builtin_bit_cast(uint4, pf[1 - y][m]), f);
+                for (int m = 0; m < 2; ++m)
 #pragma unroll
-                    for (int i = 0; i < 8; ++i) f[i] *= al;
-                    pf[1 - y][m] = __builtin_bit_cast(bf16x8, Elem<bf16_t>::pack(f));
-                }
+                    for (int i = 0; i < 8; ++i) pf[1 - y][m][i] = (_Float16)((float)pf[1 - y][m][i] * al);
             }
         };
         // A phase: the weights of keys y beside the scores of the next (kf) and the values of those before (vf), a matrix instruction (32 cycles) and what a lane computes meanwhile, in this order: a
@@ -974,12 +998,13 @@ __global__ void __launch_bounds__(512, 2) batch_attn_many_kernel(const bf16_t* _
         auto phase = [&](int y, auto more) {
             constexpr int NM = KS + 2 * DT, EP = 16 / NM;
             const int z = 1 - y;
-            float w[16], sum[2] = {0.f, 0.f}, mx = 0.f;
+            float w[16], sum[2] = {0.f, 0.f}, mx[2] = {0.f, 0.f};
+            const float from[2] = {(float)e_of[y][0] - mc, (float)e_of[y][1] - mc};
             uint32_t words[2][4];
             auto round_pair = [&](int i) {
-                words[i / 4][i % 4] = pack_bf16x2(w[2 * i], w[2 * i + 1]);
-                sum[i % 2] += w[2 * i] + w[2 * i + 1];
-                asm volatile("" : "+v"(words[i / 4][i % 4]), "+v"(sum[i % 2]));
+                words[i / 4][i % 4] = __builtin_bit_cast(uint32_t, __builtin_convertvector(f32x2{w[2 * i], w[2 * i + 1]}, f16x2));
+                sum[i / 4] += w[2 * i] + w[2 * i + 1];
+                asm volatile("" : "+v"(words[i / 4][i % 4]), "+v"(sum[i / 4]));
             };
 #pragma unroll
             for (int i = 0; i < NM; ++i) {
@@ -987,7 +1012,7 @@ __global__ void __launch_bounds__(512, 2) batch_attn_many_kernel(const bf16_t* _
                 else value(z, (i - KS) / DT, (i - KS) % DT);
 #pragma unroll
                 for (int e = 0; e < EP; ++e) {
-                    w[i * EP + e] = __builtin_amdgcn_exp2f(fmaf(s[y][i * EP + e], a.scale_log2e, -mc));
+                    w[i * EP + e] = __builtin_amdgcn_exp2f(fmaf(s[y][i * EP + e], a.scale_log2e, from[(i * EP + e) / 8]));
                     asm volatile("" : "+v"(w[i * EP + e]));      // (formed in this place)
                 }
                 if (EP == 1 ? i >= 2 && i % 2 == 0 : i >= 1) round_pair(EP == 1 ? i / 2 - 1 : i - 1);
@@ -995,23 +1020,26 @@ __global__ void __launch_bounds__(512, 2) batch_attn_many_kernel(const bf16_t* _
                 constexpr int kFrom = KS + 2, kEach = (16 + NM - kFrom - 1) / (NM - kFrom);
                 if (i >= kFrom) {
 #pragma unroll
-                    for (int e = (i - kFrom) * kEach; e < (i - kFrom + 1) * kEach && e < 16; ++e) mx = e == 0 ? s[z][0] : __builtin_elementwise_maximum(mx, s[z][e]);      // (fmaxf costs a second instruction for each score)
-                    asm volatile("" : "+v"(mx));
+                    for (int e = (i - kFrom) * kEach; e < (i - kFrom + 1) * kEach && e < 16; ++e)
+                        mx[e / 8] = e % 8 == 0 ? s[z][e] : __builtin_elementwise_maximum(mx[e / 8], s[z][e]);      // (fmaxf costs a second instruction for each score)
+                    asm volatile("" : "+v"(mx[0]), "+v"(mx[1]));
                 }
                 more(i);
                 __builtin_amdgcn_sched_barrier(0);
             }
             round_pair(7);
-            top[z] = mx;
-            l += sum[0] + sum[1];
+            top[z] = top_of(z, mx[0], mx[1]);
 #pragma unroll
-            for (int m = 0; m < 2; ++m) pf[y][m] = __builtin_bit_cast(bf16x8, make_uint4(words[m][0], words[m][1], words[m][2], words[m][3]));
+            for (int j = 0; j < 2; ++j) l = fmaf(sum[j], kv8_power(127 + kManySum - e_of[y][j]), l);
+#pragma unroll
+            for (int m = 0; m < 2; ++m) pf[y][m] = __builtin_bit_cast(f16x8, make_uint4(words[m][0], words[m][1], words[m][2], words[m][3]));
             asm volatile("" : "+v"(pf[y][0]), "+v"(pf[y][1]), "+v"(l), "+v"(top[z]));
         };
 
         if (any) {
             // two tiles of keys in LDS, a third in registers
             uint2 info = info_new, info_1, info_2;
+            int e_now = e_new, e_next, e_after;
             bool whole = all_full(info);
             if (!whole) clear_odd(0);
 #pragma unroll
@@ -1020,6 +1048,7 @@ __global__ void __launch_bounds__(512, 2) batch_attn_many_kernel(const bf16_t* _
             read_list();
             load();
             info_1 = info_new;
+            e_next = e_new;
             bool whole_1 = all_full(info_1);
             if (!whole_1) clear_odd(1);
 #pragma unroll
@@ -1028,14 +1057,16 @@ __global__ void __launch_bounds__(512, 2) batch_attn_many_kernel(const bf16_t* _
             read_list();
             load();
             info_2 = info_new;
+            e_after = e_new;
             bool whole_2 = all_full(info_2);
             __syncthreads();
 #pragma unroll
             for (int c = 0; c < KS; ++c) read_k(0, 0, c);
 #pragma unroll
-            for (int m = 0; m < 2; ++m) pf[1][m] = bf16x8{};      // (the first phase's values: nothing, or undefined where they are undefined for all rows)
+            for (int m = 0; m < 2; ++m) pf[1][m] = f16x8{};      // (the first phase's values: nothing, or undefined where they are undefined for all rows)
 #pragma unroll
             for (int c = 0; c < KS; ++c) score(0, c);
+            exponents(0, e_now);
             largest_of(0);
 #pragma unroll
             for (int c = 0; c < KS; ++c) read_k(0, 1, c);
@@ -1044,12 +1075,14 @@ __global__ void __launch_bounds__(512, 2) batch_attn_many_kernel(const bf16_t* _
                 const int ahead = (buffer + 1) & 3, filled = (buffer + 2) & 3;
                 if (!whole) hide(0, info, buffer);
                 settle(0);
+                exponents(1, e_now);
                 phase(0, [&](int i) {
                     if (i < 2 * DT) read_v(behind, behind == buffer ? 0 : 1, i % DT, i / DT);
                     if (i >= 2 * DT && i - 2 * DT < KS) read_k(ahead, 0, i - 2 * DT);      // (behind the last keys: whatever lies there, not used)
                 });
                 if (!whole) hide(1, info, buffer);
                 settle(1);
+                exponents(0, e_next);
                 if (!whole_2) clear_odd(filled);
                 phase(1, [&](int i) {
                     if (i < 2 * DT) read_v(buffer, 0, i % DT, i / DT);
@@ -1060,6 +1093,8 @@ __global__ void __launch_bounds__(512, 2) batch_attn_many_kernel(const bf16_t* _
                 if (!next) break;
                 info = info_1;
                 info_1 = info_2;
+                e_now = e_next;
+                e_next = e_after;
                 whole = whole_1;
                 whole_1 = whole_2;
                 next = after;
@@ -1067,6 +1102,7 @@ __global__ void __launch_bounds__(512, 2) batch_attn_many_kernel(const bf16_t* _
                 read_list();
                 load();
                 info_2 = info_new;
+                e_after = e_new;
                 whole_2 = all_full(info_2);
                 behind = buffer;
                 buffer = ahead;
@@ -1085,7 +1121,7 @@ __global__ void __launch_bounds__(512, 2) batch_attn_many_kernel(const bf16_t* _
             const int n_shares = whole_tile ? 1 : (int)(to / share) - share_of + 1;
             a.where[(size_t)(me.lo + n) * a.Hq + g * G + i - n * G] = make_int2(kFewPartRows + (blockIdx.x * 2 + 1) * kManyRows + threadIdx.x, 2 * n_shares + 1);
         }
-        l += __shfl_xor(l, 32, 64);
+        l = (l + __shfl_xor(l, 32, 64)) * (1.f / (1 << kManySum));
         const int in_tile = wave * 32 + l32;
         if (in_tile < rows) {
             if (whole_tile) {
@@ -1162,15 +1198,23 @@ __global__ void __launch_bounds__(256) batch_merge_kernel(T* __restrict__ out, B
             if (y0 + b * NG >= n) st[b].y = 0.f;
             if (st[b].y != 0.f) now = fmaxf(now, st[b].x);         // (a partial result without keys has no weight)
         }
-        const float al = l == 0.f ? 0.f : __builtin_amdgcn_exp2f(M - now);
+        float al = l == 0.f ? 0.f : __builtin_amdgcn_exp2f(sizeof(T) == 2 ? 0.5f * (M - now) : M - now);
         M = now;
         l *= al;
+        if constexpr (sizeof(T) == 2) { l *= al; al *= al; }
 #pragma unroll
         for (int e = 0; e < 4; ++e) o[e] *= al;
 #pragma unroll
         for (int b = 0; b < kAtOnce; ++b) {
-            const float w = st[b].y == 0.f ? 0.f : __builtin_amdgcn_exp2f(st[b].x - M);
-            l += w * st[b].y;
+            float w = 0.f;
+            if constexpr (sizeof(T) == 2) {              // in two steps: sums of tiles of many rows are relative to more than their largest score, and large or small by that
+                const float half = st[b].y == 0.f ? 0.f : __builtin_amdgcn_exp2f(0.5f * (st[b].x - M));
+                w = half * half;
+                l += st[b].y * half * half;
+            } else {
+                w = st[b].y == 0.f ? 0.f : __builtin_amdgcn_exp2f(st[b].x - M);
+                l += w * st[b].y;
+            }
 #pragma unroll
             for (int e = 0; e < 4; ++e) o[e] += w * v[b][e];
         }
@@ -1183,14 +1227,17 @@ __global__ void __launch_bounds__(256) batch_merge_kernel(T* __restrict__ out, B
         float top = M;
 #pragma unroll
         for (int y = 1; y < NG; ++y) top = fmaxf(top, ms[y][x]);
-        float al = l == 0.f ? 0.f : __builtin_amdgcn_exp2f(M - top);
+        float al = l == 0.f ? 0.f : __builtin_amdgcn_exp2f(sizeof(T) == 2 ? 0.5f * (M - top) : M - top);
         l *= al;
+        if constexpr (sizeof(T) == 2) { l *= al; al *= al; }
 #pragma unroll
         for (int e = 0; e < 4; ++e) o[e] *= al;
 #pragma unroll
         for (int y = 1; y < NG; ++y) {
-            al = ls[y][x] == 0.f ? 0.f : __builtin_amdgcn_exp2f(ms[y][x] - top);
-            l += al * ls[y][x];
+            al = ls[y][x] == 0.f ? 0.f : __builtin_amdgcn_exp2f(sizeof(T) == 2 ? 0.5f * (ms[y][x] - top) : ms[y][x] - top);
+            float part = ls[y][x] * al;
+            if constexpr (sizeof(T) == 2) { part *= al; al *= al; }
+            l += part;
 #pragma unroll
             for (int e = 0; e < 4; ++e) o[e] += al * os[y][x][c * 4 + e];
         }
