@@ -172,6 +172,51 @@ def test_large_and_flat_scores(slim):
         within(out, want[0], ref.attention_bound(want, dtype))
 
 
+@pytest.mark.parametrize("n,dtype", [(1, BF16), (9, BF16), (40, BF16), (1, F32)])
+def test_many_small_weights_beside_a_large_one(slim, n, dtype):
+    """One key 12 to 21 binary places above 20000 others, whose values all have one sign: half of the sum to a hundredth of it, each weight beyond the places of a half-precision one."""
+    block, Hq, Hkv, d, tokens = 64, 8, 2, 128, 20000
+    v = rand((tokens, Hkv, d), F32, 2).abs() + 0.25
+    k = torch.zeros(tokens, Hkv, d)
+    k[77, :, 0] = 1.0
+    q = torch.zeros(n, Hq, d)
+    q[:, :, 0] = torch.linspace(12, 21, n * Hq).reshape(n, Hq) * math.log(2) * math.sqrt(d)
+    nb = -(-tokens // block)
+    pool = torch.zeros(nb, slim.kv8_block_bytes(block, Hkv, d), dtype=torch.uint8, device="cuda")
+    slim.slim_kv8_write(k.cuda(), v.cuda(), pool, block, i32(np.arange(tokens)))
+    q = q.to(dtype)
+    out = slim.slim_batch_attn_kv8(q.cuda(), i32([0, n]), i32([tokens]), i32([np.arange(nb)]), pool, block, Hkv)
+    want = ref.attention(to64(q), [0, n], [tokens], np.arange(nb)[None], pool.cpu().numpy(), block, Hkv)
+    within(out, want[0], ref.attention_bound(want, dtype))
+
+
+@pytest.mark.parametrize("n,dtype", [(1, BF16), (9, BF16), (40, BF16), (40, F32)])
+def test_blocks_of_very_different_values(slim, n, dtype):
+    """Blocks with Values of 0, 10^-12 to 10^12, in turn; queries that look at one kind of block, a token later at another."""
+    block, Hq, Hkv, d, tokens = 16, 8, 2, 64, 900
+    sizes = [0.0, 1.0, 1e-12, 1e12, 1e-6, 1e6]
+    kind = np.arange(tokens) // block % len(sizes)
+    v = rand((tokens, Hkv, d), F32, 2) * torch.tensor(sizes)[kind][:, None, None]
+    k = rand((tokens, Hkv, d), F32, 3) * 0.1
+    k[torch.arange(tokens), :, kind] += 8.0
+    q = rand((n, Hq, d), F32, 4) * 0.1
+    for i in range(n):
+        for h in range(Hq):
+            q[i, h, :len(sizes)] = 0.0
+            q[i, h, (i + h) % len(sizes)] = 60.0         # 86 binary places above the others
+    nb = -(-tokens // block)
+    pool = torch.zeros(nb, slim.kv8_block_bytes(block, Hkv, d), dtype=torch.uint8, device="cuda")
+    slim.slim_kv8_write(k.cuda(), v.cuda(), pool, block, i32(np.arange(tokens)))
+    q = q.to(dtype)
+    out = slim.slim_batch_attn_kv8(q.cuda(), i32([0, n]), i32([tokens]), i32([np.arange(nb)]), pool, block, Hkv)
+    want = ref.attention(to64(q), [0, n], [tokens], np.arange(nb)[None], pool.cpu().numpy(), block, Hkv)
+    for i in range(n):                                   # each row and head by the size of what it looks at
+        for h in range(Hq):
+            top = max(sizes[(i + h) % len(sizes)], 1e12 * 2.0 ** -80)
+            part = (want[0][i:i + 1, h:h + 1], want[1][i:i + 1, h:h + 1], want[2], want[3], np.array([4.0 * top]))
+            within(out[i:i + 1, h:h + 1], part[0], ref.attention_bound(part, dtype))
+
+
 @pytest.mark.parametrize("new", [[1, 5, 70], [10, 5, 1]])
 def test_results_do_not_depend_on_the_workspace_the_slots_or_the_call(slim, new):
     """The same bits again, from a workspace of other bytes and from slots in another order."""
