@@ -919,15 +919,15 @@ __global__ void __launch_bounds__(512, 2) batch_attn_many_kernel(const bf16_t* _
         for (int d = 0; d < DT; ++d)
 #pragma unroll
             for (int i = 0; i < 16; ++i) o[d][i] = 0.f;
-        float mc = 0.f, lim = -INFINITY, l = 0.f;        // of row l32: reference in the base-2 domain, what it moves above, the lane's share of the sum
+        float mc = 0.f, lim = -INFINITY, l = 0.f;        // of row l32: reference in the base-2 domain, weights' exponent that it moves above (-inf: not set yet), the lane's share of the sum
         // Addresses of the lane in a buffer: K fragments (key l32, channels 16 c + 8 h: pieces 2 c + h), V fragments (keys 16 m + 4 h + .., channels 32 d + ..).
         const unsigned k_from = lds0 + l32 * Tile::kRowK + h * 16;
         const unsigned v_from = lds0 + Tile::kSide + (4 * h + (lane >> 2 & 3)) * Tile::kRowV + (lane >> 4 & 1) * 32 + (lane & 3) * 8;
         bf16x8 kf[KS];
         f16x8 vf[DT][2], pf[2][2];
         f32x16 s[2];                                     // of 32 keys, and of the next
-        float top[2];                                    // the lane's largest score + e
-        int e_of[2][2];                                  // of their 16 keys each, in scalar registers
+        float top[2], from[2][2];                        // the lane's largest exponent of a weight; of 16 keys each, e - reference
+        int e_of[2][2];                                  // in scalar registers
         auto read_k = [&](int buffer, int sub, int c) { kf[c] = *(LdsB128)(k_from + buffer * Tile::kBuffer + sub * (32 * Tile::kRowK) + c * 32); };
         auto read_v = [&](int buffer, int sub, int d, int m) {
             const unsigned from = v_from + buffer * Tile::kBuffer + (sub * 32 + m * 16) * Tile::kRowV + d * 64;
@@ -938,9 +938,11 @@ __global__ void __launch_bounds__(512, 2) batch_attn_many_kernel(const bf16_t* _
 #pragma unroll
             for (int j = 0; j < 2; ++j) e_of[y][j] = wave_value(of_lanes, y * 2 + j);
         };
-        auto top_of = [&](int y, float a0, float a1) {
-            return __builtin_elementwise_maximum(fmaf(a0, a.scale_log2e, (float)e_of[y][0]), fmaf(a1, a.scale_log2e, (float)e_of[y][1]));
+        auto set_from = [&](int y) {
+#pragma unroll
+            for (int j = 0; j < 2; ++j) from[y][j] = (float)e_of[y][j] - mc;
         };
+        auto top_of = [&](int y, float a0, float a1) { return __builtin_elementwise_maximum(fmaf(a0, a.scale_log2e, from[y][0]), fmaf(a1, a.scale_log2e, from[y][1])); };
         auto largest_of = [&](int y) {
             float mx[2];
 #pragma unroll
@@ -981,10 +983,11 @@ __global__ void __launch_bounds__(512, 2) batch_attn_many_kernel(const bf16_t* _
             if (!__any(top[y] > lim)) return;
             const float mx = fmaxf(top[y], __shfl_xor(top[y], 32, 64));
             if (mx > lim) {
-                const float to = ceilf(mx) - kManyAbove, half = lim == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(0.5f * (mc - to)), al = half * half;
+                const float to = ceilf(mx + mc) - kManyAbove, half = lim == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(0.5f * (mc - to)), al = half * half;
                 l = l * half * half;                     // (in two: sums of blocks with small Values are large)
                 mc = to;
-                lim = to + kManyRoom;
+                lim = kManyRoom;
+                set_from(y);
 #pragma unroll
                 for (int d = 0; d < DT; ++d) o[d] *= al;
 #pragma unroll
@@ -996,10 +999,9 @@ __global__ void __launch_bounds__(512, 2) batch_attn_many_kernel(const bf16_t* _
         // A phase: the weights of keys y beside the scores of the next (kf) and the values of those before (vf), a matrix instruction (32 cycles) and what a lane computes meanwhile, in this order: a
         // weight or two, the rounding and sum of those before, the largest of the new scores, and more(i): reads, conversions.
         auto phase = [&](int y, auto more) {
-            constexpr int NM = KS + 2 * DT, EP = 16 / NM;
+            constexpr int NM = KS + 2 * DT, EP = 16 / NM, kDone = D == 128 ? NM - 2 : NM;
             const int z = 1 - y;
             float w[16], sum[2] = {0.f, 0.f}, mx[2] = {0.f, 0.f};
-            const float from[2] = {(float)e_of[y][0] - mc, (float)e_of[y][1] - mc};
             uint32_t words[2][4];
             auto round_pair = [&](int i) {
                 words[i / 4][i % 4] = __builtin_bit_cast(uint32_t, __builtin_convertvector(f32x2{w[2 * i], w[2 * i + 1]}, f16x2));
@@ -1012,28 +1014,36 @@ __global__ void __launch_bounds__(512, 2) batch_attn_many_kernel(const bf16_t* _
                 else value(z, (i - KS) / DT, (i - KS) % DT);
 #pragma unroll
                 for (int e = 0; e < EP; ++e) {
-                    w[i * EP + e] = __builtin_amdgcn_exp2f(fmaf(s[y][i * EP + e], a.scale_log2e, from[(i * EP + e) / 8]));
+                    w[i * EP + e] = __builtin_amdgcn_exp2f(fmaf(s[y][i * EP + e], a.scale_log2e, from[y][(i * EP + e) / 8]));
                     asm volatile("" : "+v"(w[i * EP + e]));      // (formed in this place)
                 }
                 if (EP == 1 ? i >= 2 && i % 2 == 0 : i >= 1) round_pair(EP == 1 ? i / 2 - 1 : i - 1);
-                // from three instructions behind the last scores' on: 16 of them over the instructions that are left
-                constexpr int kFrom = KS + 2, kEach = (16 + NM - kFrom - 1) / (NM - kFrom);
+                // from three instructions behind the last scores' on, 16 of them over the instructions that are left (heads of 128: up to the last but two, as the next phase begins with their largest)
+                constexpr int kFrom = KS + 2, kEach = (16 + kDone - kFrom - 1) / (kDone - kFrom);
                 if (i >= kFrom) {
 #pragma unroll
                     for (int e = (i - kFrom) * kEach; e < (i - kFrom + 1) * kEach && e < 16; ++e)
                         mx[e / 8] = e % 8 == 0 ? s[z][e] : __builtin_elementwise_maximum(mx[e / 8], s[z][e]);      // (fmaxf costs a second instruction for each score)
                     asm volatile("" : "+v"(mx[0]), "+v"(mx[1]));
                 }
+                if (i == kFrom - 1) {
+                    set_from(z);
+                    asm volatile("" : "+v"(from[z][0]), "+v"(from[z][1]));
+                }
+                if (i == kDone) {
+                    top[z] = top_of(z, mx[0], mx[1]);
+                    asm volatile("" : "+v"(top[z]));
+                }
                 more(i);
                 __builtin_amdgcn_sched_barrier(0);
             }
             round_pair(7);
-            top[z] = top_of(z, mx[0], mx[1]);
+            if (kDone == NM) top[z] = top_of(z, mx[0], mx[1]);
 #pragma unroll
             for (int j = 0; j < 2; ++j) l = fmaf(sum[j], kv8_power(127 + kManySum - e_of[y][j]), l);
 #pragma unroll
             for (int m = 0; m < 2; ++m) pf[y][m] = __builtin_bit_cast(f16x8, make_uint4(words[m][0], words[m][1], words[m][2], words[m][3]));
-            asm volatile("" : "+v"(pf[y][0]), "+v"(pf[y][1]), "+v"(l), "+v"(top[z]));
+            asm volatile("" : "+v"(pf[y][0]), "+v"(pf[y][1]), "+v"(l));
         };
 
         if (any) {
@@ -1067,6 +1077,7 @@ __global__ void __launch_bounds__(512, 2) batch_attn_many_kernel(const bf16_t* _
 #pragma unroll
             for (int c = 0; c < KS; ++c) score(0, c);
             exponents(0, e_now);
+            set_from(0);
             largest_of(0);
 #pragma unroll
             for (int c = 0; c < KS; ++c) read_k(0, 1, c);
