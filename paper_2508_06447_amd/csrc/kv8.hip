@@ -734,9 +734,10 @@ __global__ void __launch_bounds__(64 * NW, sizeof(T) == 2 && NR == 1 ? 3 : 2) ba
 // largest score + e when it was set, and is set anew only when one is more than 15 above it: nothing is rescaled in nearly all phases, and weights down to 2^-18 of the row's largest keep
 // all places, down to 2^-28 some.  So that the sum stays within float32, e counts as -76 at least, and the codes of blocks with a smaller one are multiplied by the rest, which leaves
 // Values below 2^-67 fewer places.
-// Bound by the matrix units at the clock that the chip's power leaves them, and by the arithmetic beside them: 1511 queries behind 9856 tokens, 28 heads over 4 of 128, 230 GFLOP in
-// 245 to 275 us, 0.84 to 0.94 PFLOP/s, where a library product of 8192^3 reaches 1.37 and matrix instructions alone 1.75.  Without exponentials it takes 57 us less, without LDS 39: no one
-// of them bounds it alone.  16 rows a wave 484 us; 64 rows a wave, with all 512 registers, 271 to 279.
+// Bound by the matrix units at the clock that the chip's power leaves them, and by the arithmetic beside them: 1511 queries behind 9856 tokens, 28 heads over 4 of 128, 230 GFLOP in 247 us
+// by themselves and 280 to 290 one call behind the other, 0.93 and 0.8 PFLOP/s, where a library product of 8192^3 reaches 1.37 and matrix instructions alone 1.75; the matrix units are
+// busy half of the time.  With weights of one bfloat16 243 and 275, but an error of 2.4 10^-3 from 64 bits where rounding the output leaves 1.7.  Without the exponentials 57 us less,
+// without LDS 39: no one of them bounds it alone.  16 rows a wave 484 us; 64 rows a wave, with all 512 registers, as 32.
 constexpr int kManyKeys = 64;
 template <int D> struct ManyTile {
     // Rows of D bfloat16 and 16 bytes (Keys: 16 keys' same piece of 16 bytes) or 64 (Values: four keys' same 64 bytes) cover all banks once, and every address of a lane is one base and a constant.
@@ -775,7 +776,7 @@ __global__ void __launch_bounds__(512, 2) batch_attn_many_kernel(const bf16_t* _
 #pragma unroll
     for (int o = 32; o > 0; o >>= 1) total += __shfl_xor(total, o, 64);
     total = wave_value(total, 0);
-    // (A new prompt of 512 tokens 40 us in shares of 256 tokens' cost at least, 55 without.)
+    // (A new prompt of 512 tokens 37 us in shares of 256 tokens' cost at least, 55 without.)
     const long long share = max((long long)G * 256, (total + shares - 1) / shares), begin = share * share_of;
     long long left_over = min(total - begin, share);
     if (left_over <= 0) return;
@@ -1302,7 +1303,7 @@ static int launch_batch_attn(const void* q, void* out, BatchAttnArgs& a, hipStre
     if constexpr (sizeof(T) == 2) {
         // The host knows only how many rows there are altogether, and from them what the batch can hold.
         // A request of more than kFewRows takes the kernel for many, if it is launched: empty, that costs 3 to 5 us.  It is where rows and requests leave room for two of its tiles beside a token
-        // for each request, or for more than 16 rows a request: 255 new tokens behind 1400 with 64, 256, 512 queries behind 8192 take 203, 229, 263 us with it, 178, 265, 376 without.
+        // for each request, or for more than 16 rows a request: 255 new tokens behind 1400 with 64, 256, 512 queries behind 8192 take 203, 230, 265 us with it, 178, 265, 376 without.
         // kFewRows: 8 requests of 8192 tokens with 64 rows each take 70 us in tiles of 32 rows, 81 in those for many, with 96 rows 89 and 84, with 128 96 and 86.
         const int G = a.Hq / a.Hkv;
         const long long rows = (long long)a.n_rows * G;
