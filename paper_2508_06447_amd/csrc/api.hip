@@ -415,9 +415,9 @@ int slim_kv8_read(const void* pool, int n_slots, size_t slot_bytes, size_t layer
     return launch_kv8_read(pool, n_slots, slot_bytes, layer_offset, slots, n_tokens, n_kv_heads, head_dim, block, dtype, k_out, v_out, ldk, ldv, (hipStream_t)stream);
 }
 
-// Sizes of a call of slim_batch_attn_kv8 that its launches can hold.
+// Sizes of a call of slim_batch_attn_kv8 that its launches can hold; what its tiles cost, query heads of a kv head squared times rows times tokens, is counted in 64 bits.
 static bool batch_attn_ok(int n_rows, int n_requests, int n_q_heads, int n_kv_heads) {
-    return n_requests <= kBatchRequestsMost && (long long)n_rows * n_q_heads <= 1ll << 26 && (long long)n_requests * n_kv_heads <= 1ll << 22;
+    return n_requests <= kBatchRequestsMost && n_q_heads / n_kv_heads <= 1 << 14 && (long long)n_rows * n_q_heads <= 1ll << 26 && (long long)n_requests * n_kv_heads <= 1ll << 22;
 }
 
 size_t slim_batch_attn_kv8_workspace_bytes(int n_rows, int n_requests, int n_q_heads, int n_kv_heads, int head_dim) {

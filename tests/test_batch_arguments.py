@@ -98,11 +98,12 @@ def test_attention_refusals(lib):
                 dict(ldo=4088)):
         assert attn(lib, **bad) == -1, bad
     for bad in (dict(dtype=2), dict(d=96), dict(R=4097), dict(n=1 << 22, ldq=4096), dict(wide=1 << 25), dict(q=ODD), dict(out=ODD), dict(pool=ODD), dict(ws=at(128)), dict(ldq=4100),
-                dict(ldo=4100), dict(slots=1 << 25), dict(R=4096, Hq=2048, heads=2048, ldq=1 << 18, ldo=1 << 18, size=1 << 40)):
+                dict(ldo=4100), dict(slots=1 << 25), dict(R=4096, Hq=2048, heads=2048, ldq=1 << 18, ldo=1 << 18, size=1 << 40),
+                dict(Hq=1 << 15, heads=1, ldq=1 << 22, ldo=1 << 22)):
         assert attn(lib, **bad) == -2, bad
     need = lib.slim_batch_attn_kv8_workspace_bytes(5, 3, 32, 8, 128)
     assert need > 0 and need % 256 == 0 and attn(lib, ws_bytes=need - 1) == -3
-    for bad in ((0, 3, 32, 8, 128), (5, 0, 32, 8, 128), (5, 3, 0, 8, 128), (5, 3, 32, 0, 128), (5, 3, 33, 8, 128), (5, 3, 32, 8, 96), (5, 4097, 32, 8, 128), (1 << 22, 3, 32, 8, 128)):
+    for bad in ((0, 3, 32, 8, 128), (5, 0, 32, 8, 128), (5, 3, 0, 8, 128), (5, 3, 32, 0, 128), (5, 3, 33, 8, 128), (5, 3, 32, 8, 96), (5, 4097, 32, 8, 128), (1 << 22, 3, 32, 8, 128), (5, 3, 1 << 15, 1, 128)):
         assert lib.slim_batch_attn_kv8_workspace_bytes(*bad) == 0
     # a workspace for more rows serves fewer
     sizes = [lib.slim_batch_attn_kv8_workspace_bytes(n, 4, 32, 8, 128) for n in (1, 2, 64, 65, 1000, 100000)]

@@ -155,6 +155,22 @@ def test_what_a_row_does_not_see_does_not_reach_it(slim, n, dtype):
     assert torch.isfinite(clean).all()
 
 
+@pytest.mark.parametrize("n,dtype", [(3, BF16), (14, BF16), (80, BF16), (14, F32)])
+def test_a_query_that_is_not_a_number_is_its_own(slim, n, dtype):
+    """One head of one query: the others of its tile are as they would be."""
+    block, Hq, Hkv, d = 16, 4, 2, 128
+    pool, table, start, total = make([50], [n], block, Hkv, d, 11, odd=False)
+    q = rand((n, Hq, d), dtype, 5)
+    q[1, 2, 7] = math.nan
+    out = slim.slim_batch_attn_kv8(q.cuda(), i32(start), i32(total), i32(table), torch.from_numpy(pool).cuda(), block, Hkv)
+    assert torch.isnan(out[1, 2]).all()
+    q[1, 2] = 0.0
+    out[1, 2] = 0.0
+    want = ref.attention(to64(q), start, total, table, pool, block, Hkv)
+    want[0][1, 2] = 0.0
+    within(out, want[0], ref.attention_bound(want, dtype))
+
+
 def test_large_and_flat_scores(slim):
     """Logits of some hundreds (one key takes everything) and equal keys (the mean of the values)."""
     n, block, Hkv, d = 640, 64, 2, 128
