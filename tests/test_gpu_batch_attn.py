@@ -99,6 +99,11 @@ CASES = [
     ([90 * i % 1300 for i in range(90)], [1 + 7 * i % 12 for i in range(90)], 48, 10, 2, 128, BF16),
     ([40, 700, 0], [30, 100, 2], 16, 4, 2, 64, BF16),
     ([4000, 200], [3, 2], 64, 64, 8, 64, BF16),
+    # more kv heads than workgroups run together: a share is all of a head's
+    ([100, 3], [1, 4], 16, 160, 160, 64, BF16),
+    ([50, 0], [90, 1], 16, 300, 300, 64, BF16),
+    ([40], [12], 16, 1800, 900, 64, BF16),
+    ([30], [2], 16, 800, 800, 64, F32),
     # a chunk of a prompt among requests of one token, in tiles of 256 rows and, too short for them, of 16
     ([37 * i % 400 for i in range(60)] + [500, 0], [1] * 60 + [140, 12], 64, 8, 2, 128, BF16),
     ([37 * i % 400 for i in range(60)] + [500, 0], [1] * 60 + [100, 12], 64, 8, 2, 128, BF16),
