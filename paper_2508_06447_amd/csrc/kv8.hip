@@ -724,12 +724,12 @@ __global__ void __launch_bounds__(64 * NW, sizeof(T) == 2 && NR == 1 ? 3 : 2) ba
 }
 
 // ---- requests of many rows (bfloat16)
-// Tiles of 256 rows, 32 a wave; the eight waves turn 64 keys at a time into bfloat16 in LDS, once for all of them, and each forms, in 32x32x16 matrix instructions,
+// Tiles of 256 rows, 32 a wave; the eight waves turn 64 keys at a time into bfloat16 Keys and float16 Values in LDS, once for all of them, and each forms, in 32x32x16 matrix instructions,
 //   S^T[key, row] = K . Q^T       32 keys; the lane (l32, h) = (lane % 32, lane / 32) is left scores of row l32: keys 8 i + 4 h + 0 .. 3, i < 4
 //   O^T[d, row]   = V^T . P^T     whose operand P^T is what the lane holds: V comes through the transposing read in the same order of keys
 // A phase stands for 32 keys: their weights, beside the scores of the 32 behind and the values of the 32 before, a matrix instruction and a lane's arithmetic in turn.  It reads the Values in its
 // first half, the Keys of the next phase in its second.  Four buffers of 64 keys: Values of the keys before, the present and the next keys, and the ones being filled; a barrier each 64 keys.
-// A weight is one float16, and the Values are theirs as codes, exact in it, so that nothing but a weight's rounding (2^-12 of itself at most) is lost; the power of two 2^e of a key's block
+// A weight is one float16, and the Values are theirs as codes, exact in it, so that nothing but a weight's rounding (2^-11 of itself at most) is lost; the power of two 2^e of a key's block
 // goes into the weight: w = 2^(score + e - reference), O = sum of w * code, and the sum of the softmax is that of w * 2^-e, unrounded.  The reference of a row is a whole number, 4 below the
 // largest score + e when it was set, and is set anew only when one is more than 15 above it: nothing is rescaled in nearly all phases, and weights down to 2^-18 of the row's largest keep
 // all places, down to 2^-28 some.  So that the sum stays within float32, e counts as -76 at least, and the codes of blocks with a smaller one are multiplied by the rest, which leaves
@@ -740,7 +740,7 @@ __global__ void __launch_bounds__(64 * NW, sizeof(T) == 2 && NR == 1 ? 3 : 2) ba
 // without LDS 39: no one of them bounds it alone.  16 rows a wave 484 us; 64 rows a wave, with all 512 registers, as 32.
 constexpr int kManyKeys = 64;
 template <int D> struct ManyTile {
-    // Rows of D bfloat16 and 16 bytes (Keys: 16 keys' same piece of 16 bytes) or 64 (Values: four keys' same 64 bytes) cover all banks once, and every address of a lane is one base and a constant.
+    // Rows of D 16-bit numbers and 16 bytes (Keys: 16 keys' same piece of 16 bytes) or 64 (Values: four keys' same 64 bytes) cover all banks once, and every address of a lane is one base and a constant.
     static constexpr int kRowK = D * 2 + 16, kRowV = D * 2 + 64, kSide = kManyKeys * kRowK, kBuffer = kSide + kManyKeys * kRowV;      // a key; the Keys; both
     static constexpr int kFlags = 4 * kBuffer, kLists = kFlags + 32, kLdsBytes = kLists + 8 * 64 * 16;      // four; a bit for each of their keys with a Value that is not a number; a wave's pieces
     static constexpr int KS = D / 16, DT = D / 32;
