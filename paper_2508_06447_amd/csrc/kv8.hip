@@ -384,9 +384,11 @@ int launch_kv8_read(const void* pool, int n_slots, size_t slot_bytes, size_t lay
 // 131072 tokens, 268 MB, 54 and 5 (52); 48 requests with up to 4 drafts, 279 MB, 73 and 5 (65).
 constexpr int kPiece = 16;
 constexpr int kBatchWaves = 4;
-constexpr int kBatchGrid = 768;                          // workgroups: as many as run together, three a CU (bfloat16 heads of 128: 256 requests 150 us, with 512 157, drafts 73 and 84)
-// Heads of 64, and float32 ones of 128, of which only two fit: 512 (64 requests of 4000 tokens 55 instead of 60 us, and 101 instead of 132).
-template <typename T, int D, int NR> constexpr int batch_grid() { return sizeof(T) == 2 && D == 128 && NR == 1 ? kBatchGrid : 512; }
+// Workgroups: as many as run together, three a CU, and where the registers leave two (float32 heads of 128, tiles of 32 rows) 512.  With 768 and 512, 256 requests of 64 to 8192 tokens: bfloat16
+// heads of 128 150 and 157 us, of 64 105 and 114, float32 heads of 64 115 and 129, of 128 239 and 204; 64 drafts of 8 queries, heads of 64, 52 and 45.  (Where the requests are as many as the
+// shares of a head and alike, nothing is shared: 64 of 4000 tokens, 8 heads of 64, 61 and 55.)
+constexpr int kBatchGrid = 768;
+template <typename T, int D, int NR> constexpr int batch_grid() { return NR == 1 && (sizeof(T) == 2 || D == 64) ? kBatchGrid : 512; }
 constexpr int kBatchLeast = 2 * 2 * kBatchWaves;         // pieces of a share: two turns of its waves (one request of 500 to 4000 tokens 13 us; with one turn 13, with four 14 to 16, with eight
                                                          // 14 to 20); of tiles of 32 rows, whose turns are longer, one (16 queries of a request of 512 or 2048 tokens 17 and 21 us, with two 23 and 25)
 constexpr int kBatchTile = 8;                            // what beginning and ending a tile counts for, in pieces (256 requests 156 us, with 2 165, with 24 156)
