@@ -731,24 +731,28 @@ __global__ void __launch_bounds__(64 * NW, sizeof(T) == 2 && NR == 1 ? 3 : 2) ba
 //   O^T[d, row]   = V^T . P^T     whose operand P^T is what the lane holds: V comes through the transposing read in the same order of keys
 // A phase stands for 32 keys: their weights, beside the scores of the 32 behind and the values of the 32 before, a matrix instruction and a lane's arithmetic in turn.  It reads the Values in its
 // first half, the Keys of the next phase in its second.  Four buffers of 64 keys: Values of the keys before, the present and the next keys, and the ones being filled; a barrier each 64 keys.
-// A weight is one float16, and the Values are theirs as codes, exact in it, so that nothing but a weight's rounding (2^-11 of itself at most) is lost; the power of two 2^e of a key's block
-// goes into the weight: w = 2^(score + e - reference), O = sum of w * code, and the sum of the softmax is that of w * 2^-e, unrounded.  The reference of a row is a whole number, 4 below the
-// largest score + e when it was set, and is set anew only when one is more than 15 above it: nothing is rescaled in nearly all phases, and weights down to 2^-18 of the row's largest keep
-// all places, down to 2^-28 some.  So that the sum stays within float32, e counts as -76 at least, and the codes of blocks with a smaller one are multiplied by the rest, which leaves
-// Values below 2^-67 fewer places.
-// Bound by the matrix units at the clock that the chip's power leaves them, and by the arithmetic beside them: 1511 queries behind 9856 tokens, 28 heads over 4 of 128, 230 GFLOP in 247 us
-// by themselves and 280 to 290 one call behind the other, 0.93 and 0.8 PFLOP/s, where a library product of 8192^3 reaches 1.37 and matrix instructions alone 1.75; the matrix units are
-// busy half of the time.  With weights of one bfloat16 243 and 275, but an error of 2.4 10^-3 from 64 bits where rounding the output leaves 1.7.  Without the exponentials 57 us less,
+// A weight is 2^(score - reference), the sum of the softmax that of the weights, unrounded; what a key's block holds beside it, or behind what the row sees, touches neither.  Two loops:
+//   Where the exponents e of the Values' blocks that a workgroup's part of a tile meets lie within kManySpan of each other (nearly always): a weight is rounded to one float16, a Value is
+//   code * 2^(e - largest e + kManyShift) in float16, exact (with kManySpan 12 and kManyShift 7 from 2^-14, the smallest normal one, to 57344), and the results are multiplied by the power
+//   that is left.  The reference of a row is a whole number, 10 below its largest score when it was set, and is set anew, by a power of two, only when a score is more than 15 above it: nothing
+//   is rescaled in nearly all phases.  Weights from 2^-14 on, 2^-23 of the row's largest at least, are off by 2^-11 of themselves, smaller ones by 2^-25, 2^-34 of the largest: so a result is
+//   off by 2^-11 of sum p |v| and 2^-34 of sum |v|.
+//   Where they are further apart, that last sum may be anything beside the first, and a weight has to keep its places however small it is: two bfloat16 terms (2^-17 of itself), Values as
+//   bfloat16 with their powers, the reference the running maximum.  One buffer, filled and read in turn: 358 us for a call of 1511 queries behind 9856 tokens where the other loop takes 240.
+// Bound by the matrix units at the clock that the chip's power leaves them, and by the arithmetic beside them: 1511 queries behind 9856 tokens, 28 heads over 4 of 128, 230 GFLOP in 250 us
+// by themselves and 280 to 290 one call behind the other, 0.92 and 0.8 PFLOP/s, where a library product of 8192^3 reaches 1.37 and matrix instructions alone 1.75; the matrix units are
+// busy half of the time.  With weights of one bfloat16 4 to 10 us less, but an error of 2.4 10^-3 from 64 bits where rounding the output leaves 1.7.  Without the exponentials 57 us less,
 // without LDS 39: no one of them bounds it alone.  16 rows a wave 484 us; 64 rows a wave, with all 512 registers, as 32.
 constexpr int kManyKeys = 64;
 template <int D> struct ManyTile {
     // Rows of D 16-bit numbers and 16 bytes (Keys: 16 keys' same piece of 16 bytes) or 64 (Values: four keys' same 64 bytes) cover all banks once, and every address of a lane is one base and a constant.
     static constexpr int kRowK = D * 2 + 16, kRowV = D * 2 + 64, kSide = kManyKeys * kRowK, kBuffer = kSide + kManyKeys * kRowV;      // a key; the Keys; both
-    static constexpr int kFlags = 4 * kBuffer, kLists = kFlags + 32, kLdsBytes = kLists + 8 * 64 * 16;      // four; a bit for each of their keys with a Value that is not a number; a wave's pieces
+    static constexpr int kFlags = 4 * kBuffer, kSpans = kFlags + 32, kLists = kSpans + 32, kLdsBytes = kLists + 8 * 64 * 16;      // four; a bit for each of their keys with a Value that is not a
+                                                                                                                          // number; the exponents that the waves have met; a wave's pieces
     static constexpr int KS = D / 16, DT = D / 32;
 };
-constexpr float kManyAbove = 4.f, kManyRoom = 15.f;      // where the largest weight begins, and how far it may grow: 2^4, 2^15
-constexpr int kManyByteLow = 51, kManySum = 14;          // e + 127 of -76; the sum is kept times 2^14
+constexpr float kManyAbove = 10.f, kManyRoom = 15.f;     // where the largest weight begins, and how far it may grow: 2^10, 2^15
+constexpr int kManySpan = 12, kManyShift = 7, kManyFar = 64;      // of the Values' exponents, see above; their magnitude (partial results are not divided by their sums, and stay far from float32's ends)
 
 template <int D>
 __global__ void __launch_bounds__(512, 2) batch_attn_many_kernel(const bf16_t* __restrict__ q, bf16_t* __restrict__ out, BatchAttnArgs a) {
@@ -825,6 +829,33 @@ __global__ void __launch_bounds__(512, 2) batch_attn_many_kernel(const bf16_t* _
         };
         int slot_1 = slot_at(u), slot_2 = slot_at(u + 64);
         uint32_t e_1 = exponents_at(slot_1);
+        // The Values' exponents of all blocks in the tile's part, a block a lane, all waves together: the largest, and how far the smallest lies below it.
+        typedef unsigned short u16x2 __attribute__((ext_vector_type(2)));
+        int e_top, e_low;                                // + 127
+        {
+            u16x2 span = {0, 0};                         // largest byte, 255 - smallest
+            const int b_end = u_begin < u_end ? a.by_piece(u_end - 1) + 1 : 0;
+            for (int b = u_begin < u_end ? a.by_piece(u_begin) + (int)threadIdx.x : 0; b < b_end; b += 512) {
+                const int slot = table[b];
+                if (slot >= 0 && slot < a.n_slots) {
+                    const int byte = min(max((int)a.pool[(size_t)slot * a.slot_bytes + a.layer_offset + head.e + 1], kKv8ByteLow), kKv8ByteHigh);
+                    span = __builtin_elementwise_max(span, u16x2{(unsigned short)byte, (unsigned short)(255 - byte)});
+                }
+            }
+#pragma unroll
+            for (int o = 32; o > 0; o >>= 1) span = __builtin_elementwise_max(span, __builtin_bit_cast(u16x2, __shfl_xor(__builtin_bit_cast(int, span), o, 64)));
+            uint32_t* spans = reinterpret_cast<uint32_t*>(lds + Tile::kSpans);
+            if (lane == 0) spans[wave] = __builtin_bit_cast(uint32_t, span);
+            __syncthreads();
+#pragma unroll
+            for (int i = 0; i < 8; ++i) span = __builtin_elementwise_max(span, __builtin_bit_cast(u16x2, spans[i]));
+            const int both = __builtin_amdgcn_readfirstlane(__builtin_bit_cast(int, span));
+            e_top = both == 0 ? 127 : both & 0xffff;     // (no block: nothing is read)
+            e_low = both == 0 ? 127 : 255 - (both >> 16 & 0xffff);
+        }
+        const bool apart = e_top - e_low > kManySpan || e_top > 127 + kManyFar || e_low < 127 - kManyFar;
+        const int e_shift = apart ? 0 : 127 - e_top + kManyShift;                                      // added to a Value's exponent when it becomes a number
+        const float left_power = kv8_power((uint32_t)(127 - e_shift));                                 // and what a result is multiplied by for it
         uint4* list = reinterpret_cast<uint4*>(lds + Tile::kLists) + wave * 64;
         int at_list = 0, n_list = 0;                     // in fours
         auto advance = [&]() {                           // to the next four; false: there are none, and the last ones stay
@@ -854,19 +885,17 @@ __global__ void __launch_bounds__(512, 2) batch_attn_many_kernel(const bf16_t* _
                 return true;
             }
         };
-        // A thread's codes of 64 keys: 16 channels of key tid / PR (of heads of 64 the first half of the threads).
+        // A thread's codes of 64 keys: 16 channels of key threadIdx.x / PR (of heads of 64 the first half of the threads).
         const int my_key = threadIdx.x / PR, my_piece = threadIdx.x % PR;
         const bool mine = D == 128 || my_key < kManyKeys;
         const size_t values_apart = head.v - head.k;
         uint4 kx, vx, entry;
         float kp, vp;
         uint2 info_new;                                  // of lanes 0 .. 3: exponents, rows, position
-        int e_new;                                       // and the Values' e
         auto read_list = [&]() {
             entry = list[at_list * 4 + (D == 128 ? wave >> 1 : wave & 3)];
             const uint4 e = list[at_list * 4 + (lane & 3)];
             info_new = make_uint2(e.z, e.w);
-            e_new = min(max((int)(e.z >> 8 & 0xffu), kManyByteLow), kKv8ByteHigh) - 127;
         };
         auto load = [&]() {
             const unsigned char* from = (const unsigned char*)((size_t)entry.y << 32 | entry.x);
@@ -874,7 +903,7 @@ __global__ void __launch_bounds__(512, 2) batch_attn_many_kernel(const bf16_t* _
             kx = *reinterpret_cast<const uint4*>(from + off);
             vx = *reinterpret_cast<const uint4*>(from + values_apart + off);
             kp = kv8_power(entry.z & 0xffu);
-            vp = kv8_power(127 + min((int)(entry.z >> 8 & 0xffu) - kManyByteLow, 0));
+            vp = kv8_power((uint32_t)(min(max((int)(entry.z >> 8 & 0xffu), kKv8ByteLow), kKv8ByteHigh) + e_shift));
         };
         auto all_full = [](const uint2& info) { return (__ballot(info.x >> 24 & 1u) & 15u) == 15u; };
         // Values of the next keys that are not numbers become zeros, a bit each, where some row does not see all of them (as for few rows).
@@ -898,11 +927,11 @@ __global__ void __launch_bounds__(512, 2) batch_attn_many_kernel(const bf16_t* _
             }
         };
         const unsigned fill_k = lds0 + my_key * Tile::kRowK + my_piece * 32, fill_v = lds0 + Tile::kSide + my_key * Tile::kRowV + my_piece * 32;
-        // A part of the keys' way into a buffer: eight channels of Keys (part 0, 1) or Values (2, 3).
-        auto fill_part = [&](int buffer, int part) {
+        // A part of the keys' way into a buffer: eight channels of Keys (part 0, 1) or Values (2, 3; as float16, or as bfloat16 too).
+        auto fill_part = [&](int buffer, int part, auto bf16_values) {
             const uint4 c = part < 2 ? kx : vx;
             const uint2 half = part % 2 ? make_uint2(c.z, c.w) : make_uint2(c.x, c.y);
-            const bf16x8 x = part < 2 ? kv8_to_bf16(half, kp) : __builtin_bit_cast(bf16x8, kv8_to_f16(half, vp));
+            const bf16x8 x = part < 2 ? kv8_to_bf16(half, kp) : bf16_values.value ? kv8_to_bf16(half, vp) : __builtin_bit_cast(bf16x8, kv8_to_f16(half, vp));
             if (mine) *(LdsB128)((part < 2 ? fill_k : fill_v) + buffer * Tile::kBuffer + part % 2 * 16) = x;
         };
 
@@ -922,40 +951,28 @@ __global__ void __launch_bounds__(512, 2) batch_attn_many_kernel(const bf16_t* _
         for (int d = 0; d < DT; ++d)
 #pragma unroll
             for (int i = 0; i < 16; ++i) o[d][i] = 0.f;
-        float mc = 0.f, lim = -INFINITY, l = 0.f;        // of row l32: reference in the base-2 domain, weights' exponent that it moves above (-inf: not set yet), the lane's share of the sum
+        // of row l32: reference in the base-2 domain, weights' exponent that it moves above (-inf: not set yet; where exponents are far apart the largest score itself), the lane's share of the sum
+        float mc = 0.f, lim = -INFINITY, l = 0.f;
         // Addresses of the lane in a buffer: K fragments (key l32, channels 16 c + 8 h: pieces 2 c + h), V fragments (keys 16 m + 4 h + .., channels 32 d + ..).
         const unsigned k_from = lds0 + l32 * Tile::kRowK + h * 16;
         const unsigned v_from = lds0 + Tile::kSide + (4 * h + (lane >> 2 & 3)) * Tile::kRowV + (lane >> 4 & 1) * 32 + (lane & 3) * 8;
         bf16x8 kf[KS];
         f16x8 vf[DT][2], pf[2][2];
         f32x16 s[2];                                     // of 32 keys, and of the next
-        float top[2], from[2][2];                        // the lane's largest exponent of a weight; of 16 keys each, e - reference
-        int e_of[2][2];                                  // in scalar registers
+        float top[2];                                    // the lane's largest exponent of a weight
         auto read_k = [&](int buffer, int sub, int c) { kf[c] = *(LdsB128)(k_from + buffer * Tile::kBuffer + sub * (32 * Tile::kRowK) + c * 32); };
         auto read_v = [&](int buffer, int sub, int d, int m) {
             const unsigned from = v_from + buffer * Tile::kBuffer + (sub * 32 + m * 16) * Tile::kRowV + d * 64;
             const bf16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4bf16((LdsB64)from), hi = __builtin_amdgcn_ds_read_tr16_b64_v4bf16((LdsB64)(from + 8 * Tile::kRowV));
             vf[d][m] = __builtin_bit_cast(f16x8, __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
         };
-        auto exponents = [&](int y, int of_lanes) {
-#pragma unroll
-            for (int j = 0; j < 2; ++j) e_of[y][j] = wave_value(of_lanes, y * 2 + j);
-        };
-        auto set_from = [&](int y) {
-#pragma unroll
-            for (int j = 0; j < 2; ++j) from[y][j] = (float)e_of[y][j] - mc;
-        };
-        auto top_of = [&](int y, float a0, float a1) { return __builtin_elementwise_maximum(fmaf(a0, a.scale_log2e, from[y][0]), fmaf(a1, a.scale_log2e, from[y][1])); };
         auto largest_of = [&](int y) {
-            float mx[2];
+            float mx = s[y][0];
 #pragma unroll
-            for (int j = 0; j < 2; ++j) {
-                mx[j] = s[y][8 * j];
-#pragma unroll
-                for (int i = 1; i < 8; ++i) mx[j] = __builtin_elementwise_maximum(mx[j], s[y][8 * j + i]);
-            }
-            top[y] = top_of(y, mx[0], mx[1]);
+            for (int i = 1; i < 16; ++i) mx = __builtin_elementwise_maximum(mx, s[y][i]);
+            return mx;
         };
+        auto top_of = [&](float score) { return fmaf(score, a.scale_log2e, -mc); };
         auto score = [&](int y, int c) {
             if (c == 0)
 #pragma unroll
@@ -964,7 +981,7 @@ __global__ void __launch_bounds__(512, 2) batch_attn_many_kernel(const bf16_t* _
         };
         auto value = [&](int y, int m, int d) { o[d] = __builtin_amdgcn_mfma_f32_32x32x16_f16(vf[d][m], pf[y][m], o[d], 0, 0, 0); };
         // What the row does not see of 32 keys; where values that are not numbers became zeros, a row that sees one of them is undefined by its sum.
-        auto hide = [&](int y, const uint2& info, int buffer) {
+        auto hide = [&](f32x16& scores, int y, const uint2& info, int buffer) {
             const unsigned odd = *reinterpret_cast<const uint32_t*>(lds + Tile::kFlags + buffer * 8 + y * 4);
             unsigned seen_keys = 0;
 #pragma unroll
@@ -974,23 +991,21 @@ __global__ void __launch_bounds__(512, 2) batch_attn_many_kernel(const bf16_t* _
                 const int mine = seen - 4 * h;
 #pragma unroll
                 for (int i = 0; i < 8; ++i) {
-                    const float v = s[y][8 * j + i];
-                    s[y][8 * j + i] = (i & 3) + 8 * (i >> 2) < mine ? v : -INFINITY;
+                    const float v = scores[8 * j + i];
+                    scores[8 * j + i] = (i & 3) + 8 * (i >> 2) < mine ? v : -INFINITY;
                 }
             }
             if (odd & seen_keys) l = NAN;
-            largest_of(y);
         };
         // Moves the reference of rows that have a score too far above it, and with it what the weights so far have left: results, sum, and the weights before, whose values are still to come.
         auto settle = [&](int y) {
             if (!__any(top[y] > lim)) return;
             const float mx = fmaxf(top[y], __shfl_xor(top[y], 32, 64));
             if (mx > lim) {
-                const float to = ceilf(mx + mc) - kManyAbove, half = lim == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(0.5f * (mc - to)), al = half * half;
-                l = l * half * half;                     // (in two: sums of blocks with small Values are large)
+                const float to = ceilf(mx + mc) - kManyAbove, al = lim == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(mc - to);
+                l *= al;
                 mc = to;
                 lim = kManyRoom;
-                set_from(y);
 #pragma unroll
                 for (int d = 0; d < DT; ++d) o[d] *= al;
 #pragma unroll
@@ -1004,12 +1019,12 @@ __global__ void __launch_bounds__(512, 2) batch_attn_many_kernel(const bf16_t* _
         auto phase = [&](int y, auto more) {
             constexpr int NM = KS + 2 * DT, EP = 16 / NM, kDone = D == 128 ? NM - 2 : NM;
             const int z = 1 - y;
-            float w[16], sum[2] = {0.f, 0.f}, mx[2] = {0.f, 0.f};
+            float w[16], sum = 0.f, mx = 0.f;
             uint32_t words[2][4];
             auto round_pair = [&](int i) {
                 words[i / 4][i % 4] = __builtin_bit_cast(uint32_t, __builtin_convertvector(f32x2{w[2 * i], w[2 * i + 1]}, f16x2));
-                sum[i / 4] += w[2 * i] + w[2 * i + 1];
-                asm volatile("" : "+v"(words[i / 4][i % 4]), "+v"(sum[i / 4]));
+                sum += w[2 * i] + w[2 * i + 1];
+                asm volatile("" : "+v"(words[i / 4][i % 4]), "+v"(sum));
             };
 #pragma unroll
             for (int i = 0; i < NM; ++i) {
@@ -1017,7 +1032,7 @@ __global__ void __launch_bounds__(512, 2) batch_attn_many_kernel(const bf16_t* _
                 else value(z, (i - KS) / DT, (i - KS) % DT);
 #pragma unroll
                 for (int e = 0; e < EP; ++e) {
-                    w[i * EP + e] = __builtin_amdgcn_exp2f(fmaf(s[y][i * EP + e], a.scale_log2e, from[y][(i * EP + e) / 8]));
+                    w[i * EP + e] = __builtin_amdgcn_exp2f(top_of(s[y][i * EP + e]));
                     asm volatile("" : "+v"(w[i * EP + e]));      // (formed in this place)
                 }
                 if (EP == 1 ? i >= 2 && i % 2 == 0 : i >= 1) round_pair(EP == 1 ? i / 2 - 1 : i - 1);
@@ -1026,51 +1041,94 @@ __global__ void __launch_bounds__(512, 2) batch_attn_many_kernel(const bf16_t* _
                 if (i >= kFrom) {
 #pragma unroll
                     for (int e = (i - kFrom) * kEach; e < (i - kFrom + 1) * kEach && e < 16; ++e)
-                        mx[e / 8] = e % 8 == 0 ? s[z][e] : __builtin_elementwise_maximum(mx[e / 8], s[z][e]);      // (fmaxf costs a second instruction for each score)
-                    asm volatile("" : "+v"(mx[0]), "+v"(mx[1]));
-                }
-                if (i == kFrom - 1) {
-                    set_from(z);
-                    asm volatile("" : "+v"(from[z][0]), "+v"(from[z][1]));
+                        mx = e == 0 ? s[z][e] : __builtin_elementwise_maximum(mx, s[z][e]);      // (fmaxf costs a second instruction for each score)
+                    asm volatile("" : "+v"(mx));
                 }
                 if (i == kDone) {
-                    top[z] = top_of(z, mx[0], mx[1]);
+                    top[z] = top_of(mx);
                     asm volatile("" : "+v"(top[z]));
                 }
                 more(i);
                 __builtin_amdgcn_sched_barrier(0);
             }
             round_pair(7);
-            if (kDone == NM) top[z] = top_of(z, mx[0], mx[1]);
-#pragma unroll
-            for (int j = 0; j < 2; ++j) l = fmaf(sum[j], kv8_power(127 + kManySum - e_of[y][j]), l);
+            if (kDone == NM) top[z] = top_of(mx);
+            l += sum;
 #pragma unroll
             for (int m = 0; m < 2; ++m) pf[y][m] = __builtin_bit_cast(f16x8, make_uint4(words[m][0], words[m][1], words[m][2], words[m][3]));
             asm volatile("" : "+v"(pf[y][0]), "+v"(pf[y][1]), "+v"(l));
         };
 
-        if (any) {
-            // two tiles of keys in LDS, a third in registers
+        constexpr std::false_type as_f16;
+        constexpr std::true_type as_bf16;
+        const int loop = __builtin_amdgcn_readfirstlane(!any ? 0 : apart ? 2 : 1);
+        if (loop == 2) {
+            for (bool next = true; next;) {
+                const uint2 info = info_new;
+                const bool whole = all_full(info);
+                if (!whole) clear_odd(0);
+#pragma unroll
+                for (int i = 0; i < 4; ++i) fill_part(0, i, as_bf16);
+                next = advance();
+                read_list();
+                load();
+                __syncthreads();
+#pragma unroll 1
+                for (int y = 0; y < 2; ++y) {
+#pragma unroll
+                    for (int c = 0; c < KS; ++c) read_k(0, y, c);
+#pragma unroll
+                    for (int c = 0; c < KS; ++c) score(0, c);
+                    if (!whole) hide(s[0], y, info, 0);
+                    float mx = largest_of(0);
+                    mx = fmaxf(mx, __shfl_xor(mx, 32, 64));
+                    if (__any(mx > lim)) {
+                        const float now = fmaxf(mx, lim), to = now == -INFINITY ? 0.f : now * a.scale_log2e, al = lim == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(mc - to);
+                        lim = now;
+                        mc = to;
+                        l *= al;
+#pragma unroll
+                        for (int d = 0; d < DT; ++d) o[d] *= al;
+                    }
+#pragma unroll
+                    for (int m = 0; m < 2; ++m) {
+                        float w[8];
+#pragma unroll
+                        for (int i = 0; i < 8; ++i) w[i] = __builtin_amdgcn_exp2f(top_of(s[0][8 * m + i]));
+                        l += ((w[0] + w[1]) + (w[2] + w[3])) + ((w[4] + w[5]) + (w[6] + w[7]));
+                        bf16x8 terms[2];
+                        bf16_terms<2>(w, terms);
+#pragma unroll
+                        for (int d = 0; d < DT; ++d) {
+                            read_v(0, y, d, m);
+#pragma unroll
+                            for (int t = 1; t >= 0; --t) o[d] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, vf[d][m]), terms[t], o[d], 0, 0, 0);
+                        }
+                    }
+                }
+                __syncthreads();
+            }
+        }
+        if (loop == 1) {
+            // Two tiles of 64 keys in LDS, a third in registers, on its way.  Turn i reads the Values of tiles i - 1 and i and the Keys of i + 1, and fills the buffer of i + 2, which is that of
+            // i - 2: turn i - 1 was the last to read it, turn i + 1 is the first to read what it gets.  So one barrier, at a turn's end, keeps both apart.
             uint2 info = info_new, info_1, info_2;
-            int e_now = e_new, e_next, e_after;
             bool whole = all_full(info);
             if (!whole) clear_odd(0);
 #pragma unroll
-            for (int i = 0; i < 4; ++i) fill_part(0, i);
+            for (int i = 0; i < 4; ++i) fill_part(0, i, as_f16);
             bool next = advance();
             read_list();
             load();
             info_1 = info_new;
-            e_next = e_new;
             bool whole_1 = all_full(info_1);
             if (!whole_1) clear_odd(1);
 #pragma unroll
-            for (int i = 0; i < 4; ++i) fill_part(1, i);
+            for (int i = 0; i < 4; ++i) fill_part(1, i, as_f16);
             bool after = next && advance();
             read_list();
             load();
             info_2 = info_new;
-            e_after = e_new;
             bool whole_2 = all_full(info_2);
             __syncthreads();
 #pragma unroll
@@ -1079,36 +1137,36 @@ __global__ void __launch_bounds__(512, 2) batch_attn_many_kernel(const bf16_t* _
             for (int m = 0; m < 2; ++m) pf[1][m] = f16x8{};      // (the first phase's values: nothing, or undefined where they are undefined for all rows)
 #pragma unroll
             for (int c = 0; c < KS; ++c) score(0, c);
-            exponents(0, e_now);
-            set_from(0);
-            largest_of(0);
+            top[0] = top_of(largest_of(0));
 #pragma unroll
             for (int c = 0; c < KS; ++c) read_k(0, 1, c);
             int buffer = 0, behind = 0;                  // of the present keys, of those before
             while (true) {
                 const int ahead = (buffer + 1) & 3, filled = (buffer + 2) & 3;
-                if (!whole) hide(0, info, buffer);
+                if (!whole) {
+                    hide(s[0], 0, info, buffer);
+                    top[0] = top_of(largest_of(0));
+                }
                 settle(0);
-                exponents(1, e_now);
                 phase(0, [&](int i) {
                     if (i < 2 * DT) read_v(behind, behind == buffer ? 0 : 1, i % DT, i / DT);
                     if (i >= 2 * DT && i - 2 * DT < KS) read_k(ahead, 0, i - 2 * DT);      // (behind the last keys: whatever lies there, not used)
                 });
-                if (!whole) hide(1, info, buffer);
+                if (!whole) {
+                    hide(s[1], 1, info, buffer);
+                    top[1] = top_of(largest_of(1));
+                }
                 settle(1);
-                exponents(0, e_next);
                 if (!whole_2) clear_odd(filled);
                 phase(1, [&](int i) {
                     if (i < 2 * DT) read_v(buffer, 0, i % DT, i / DT);
                     if (i >= 2 * DT && i - 2 * DT < KS) read_k(ahead, 1, i - 2 * DT);
-                    if (i >= KS && (i - KS) % (2 * DT / 4) == 0) fill_part(filled, (i - KS) / (2 * DT / 4));      // (behind the last keys: the last codes again, not used)
+                    if (i >= KS && (i - KS) % (2 * DT / 4) == 0) fill_part(filled, (i - KS) / (2 * DT / 4), as_f16);      // (behind the last keys: the last codes again, not used)
                 });
                 __syncthreads();
                 if (!next) break;
                 info = info_1;
                 info_1 = info_2;
-                e_now = e_next;
-                e_next = e_after;
                 whole = whole_1;
                 whole_1 = whole_2;
                 next = after;
@@ -1116,7 +1174,6 @@ __global__ void __launch_bounds__(512, 2) batch_attn_many_kernel(const bf16_t* _
                 read_list();
                 load();
                 info_2 = info_new;
-                e_after = e_new;
                 whole_2 = all_full(info_2);
                 behind = buffer;
                 buffer = ahead;
@@ -1135,12 +1192,12 @@ __global__ void __launch_bounds__(512, 2) batch_attn_many_kernel(const bf16_t* _
             const int n_shares = whole_tile ? 1 : (int)(to / share) - share_of + 1;
             a.where[(size_t)(me.lo + n) * a.Hq + g * G + i - n * G] = make_int2(kFewPartRows + (blockIdx.x * 2 + 1) * kManyRows + threadIdx.x, 2 * n_shares + 1);
         }
-        l = (l + __shfl_xor(l, 32, 64)) * (1.f / (1 << kManySum));
+        l += __shfl_xor(l, 32, 64);
         const int in_tile = wave * 32 + l32;
         if (in_tile < rows) {
             if (whole_tile) {
                 bf16_t* dst = out + (size_t)(me.lo + token) * a.ldo + (size_t)(g * G + lrow - token * G) * D + 4 * h;
-                const float inv = l == 0.f ? 0.f : 1.f / l;
+                const float inv = l == 0.f ? 0.f : left_power / l;
 #pragma unroll
                 for (int d = 0; d < DT; ++d)
 #pragma unroll
@@ -1152,8 +1209,8 @@ __global__ void __launch_bounds__(512, 2) batch_attn_many_kernel(const bf16_t* _
 #pragma unroll
                 for (int d = 0; d < DT; ++d)
 #pragma unroll
-                    for (int i = 0; i < 4; ++i) *reinterpret_cast<f32x4*>(dst + d * 32 + i * 8 + 4 * h) = f32x4{o[d][4 * i], o[d][4 * i + 1], o[d][4 * i + 2], o[d][4 * i + 3]};
-                if (h == 0) { dst[D] = lim == -INFINITY ? -INFINITY : mc; dst[D + 1] = l; }
+                    for (int i = 0; i < 4; ++i) *reinterpret_cast<f32x4*>(dst + d * 32 + i * 8 + 4 * h) = f32x4{o[d][4 * i], o[d][4 * i + 1], o[d][4 * i + 2], o[d][4 * i + 3]} * left_power;
+                if (h == 0) { dst[D] = mc; dst[D + 1] = l; }
             }
         }
         left_over -= take;
@@ -1212,23 +1269,15 @@ __global__ void __launch_bounds__(256) batch_merge_kernel(T* __restrict__ out, B
             if (y0 + b * NG >= n) st[b].y = 0.f;
             if (st[b].y != 0.f) now = fmaxf(now, st[b].x);         // (a partial result without keys has no weight)
         }
-        float al = l == 0.f ? 0.f : __builtin_amdgcn_exp2f(sizeof(T) == 2 ? 0.5f * (M - now) : M - now);
+        const float al = l == 0.f ? 0.f : __builtin_amdgcn_exp2f(M - now);
         M = now;
         l *= al;
-        if constexpr (sizeof(T) == 2) { l *= al; al *= al; }
 #pragma unroll
         for (int e = 0; e < 4; ++e) o[e] *= al;
 #pragma unroll
         for (int b = 0; b < kAtOnce; ++b) {
-            float w = 0.f;
-            if constexpr (sizeof(T) == 2) {              // in two steps: sums of tiles of many rows are relative to more than their largest score, and large or small by that
-                const float half = st[b].y == 0.f ? 0.f : __builtin_amdgcn_exp2f(0.5f * (st[b].x - M));
-                w = half * half;
-                l += st[b].y * half * half;
-            } else {
-                w = st[b].y == 0.f ? 0.f : __builtin_amdgcn_exp2f(st[b].x - M);
-                l += w * st[b].y;
-            }
+            const float w = st[b].y == 0.f ? 0.f : __builtin_amdgcn_exp2f(st[b].x - M);
+            l += w * st[b].y;
 #pragma unroll
             for (int e = 0; e < 4; ++e) o[e] += w * v[b][e];
         }
@@ -1241,17 +1290,14 @@ __global__ void __launch_bounds__(256) batch_merge_kernel(T* __restrict__ out, B
         float top = M;
 #pragma unroll
         for (int y = 1; y < NG; ++y) top = fmaxf(top, ms[y][x]);
-        float al = l == 0.f ? 0.f : __builtin_amdgcn_exp2f(sizeof(T) == 2 ? 0.5f * (M - top) : M - top);
+        float al = l == 0.f ? 0.f : __builtin_amdgcn_exp2f(M - top);
         l *= al;
-        if constexpr (sizeof(T) == 2) { l *= al; al *= al; }
 #pragma unroll
         for (int e = 0; e < 4; ++e) o[e] *= al;
 #pragma unroll
         for (int y = 1; y < NG; ++y) {
-            al = ls[y][x] == 0.f ? 0.f : __builtin_amdgcn_exp2f(sizeof(T) == 2 ? 0.5f * (ms[y][x] - top) : ms[y][x] - top);
-            float part = ls[y][x] * al;
-            if constexpr (sizeof(T) == 2) { part *= al; al *= al; }
-            l += part;
+            al = ls[y][x] == 0.f ? 0.f : __builtin_amdgcn_exp2f(ms[y][x] - top);
+            l += ls[y][x] * al;
 #pragma unroll
             for (int e = 0; e < 4; ++e) o[e] += al * os[y][x][c * 4 + e];
         }
