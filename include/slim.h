@@ -509,12 +509,13 @@ int slim_decode_layer_kv4(const slim_layer_shape* s, const slim_layer_weights* w
  *     block is in the pool:  out[t, h, :] = sum_j softmax_j(scale * q[t, h, :] . k[j, g, :]) v[j, g, :],  g = h / (Hq/Hkv);  softmax_scale 0 => 1/sqrt(d).
  *     q, out rows [n_rows, Hq, d] of dtype with strides ldq, ldo; padding rows of out stay as they were.  A query that sees no key gets zeros.  What a query does not see does not
  *     reach its output, whatever it holds; one that sees a number that is not finite is not specified.  Any number of queries per request, requests of one token among ones of many, up to 2^14 query heads per kv head.
- *     Scores, sums and results are float32 until the output is rounded, the Values' sum relative to the largest weight among them.  bfloat16: the weights enter the product with the values as two
-     bfloat16 terms (2^-17 of a weight), or, for requests of many rows (n * Hq/Hkv above 64, in a batch whose rows leave room for them: n_rows * Hq/Hkv above 16 * R, or (n_rows - R) * Hq/Hkv above
-     512), as one float16, where the exponents e of the Values that are taken together lie in [-64, 64] and within 12 of each other (elsewhere as two terms, in half as long again): off by 2^-11 of
-     itself, or where that is less by 2^-34 of the row's largest weight.  Either way 1.7 10^-3 of the results' size from 64 bits, nearly all of it the output's rounding.  float32: three terms, 2 to
-     5 10^-7.  (A token of a seen block that a query does not see can decide, by the block's e, which of the two its weights are.)
-     The order of the sums follows from the batch's lengths, and so a token's result can differ in its last places with the requests beside it; the same call gives the same bits.
+ *     Scores, sums and results are float32 until the output is rounded (the sum of the Values with a weight of 1 for the largest: above 3 10^38 it is infinite).  bfloat16: the weights enter the
+ *     product with the Values as two bfloat16 terms, off by 2^-17 of a weight, or, for requests of many rows (n * Hq/Hkv above 64, in a batch whose rows leave room for them: n_rows * Hq/Hkv
+ *     above 16 * R, or (n_rows - R) * Hq/Hkv above 512), as one float16 where the exponents e of the Values that are taken together lie in [-64, 64] and within 12 of each other (elsewhere as two
+ *     terms, which takes half as long again): off by 2^-11 of a weight, or by 2^-34 of the row's largest where that is more.  Either way 1.7 10^-3 of the results' size from 64 bits, nearly all of
+ *     it the output's rounding.  float32: three terms, 2 to 5 10^-7.  (A token that a query does not see, in a block that it does, can decide by the block's e in which of the two ways its
+ *     weights are rounded.)
+ *     The order of the sums follows from the batch's lengths, and so a token's result can differ in its last places with the requests beside it; the same call gives the same bits.
  *     workspace >= slim_batch_attn_kv8_workspace_bytes(...) bytes, 256-byte aligned: partial results; a call writes what it reads of it.
  * head_dim 64 or 128; pools, layer_offset and slot_bytes multiples of 16, rows 16-byte aligned (ld a multiple of 8 bf16 or 4 f32 elements), n_slots * block < 2^31, block <= 2^24, rows of a
  * call that writes or reads times Hkv fewer than 2^29 (attention: n_rows * Hq <= 2^26, Hq / Hkv <= 2^14, R <= 4096, R * Hkv <= 2^22, max_blocks * block <= 2^30).  row_start must ascend within [0, n_rows], as slim_batch_map leaves it.
