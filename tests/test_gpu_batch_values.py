@@ -103,3 +103,79 @@ def test_rows_that_look_at_one_kind_of_block(slim, n, d, dtype, tokens):
     rest = want[3] * 2.0 ** -126 * want[4].max()         # what weights below the smallest normal number leave out is of the largest Values' size
     assert rest < 1e-3
     within(out, want[0], bound)
+
+
+@pytest.mark.parametrize("n,d,dtype", MANY)
+@pytest.mark.parametrize("apart", [False, True])
+def test_values_that_are_not_numbers_are_seen_by_their_rows_alone(slim, n, d, dtype, apart):
+    """A token with a Value that is not a number, at places all over a tile of keys and in channels of every lane: rows in front of it are as they would be, later ones are not numbers.
+    Blocks alike, or too far apart for float16."""
+    held, block, Hq, Hkv = 150, 16, 8, 2
+    tokens = held + n
+    nb = -(-tokens // block)
+    v = rand((tokens, Hkv, d), F32, 2) * torch.tensor([1.0, 2.0 ** -20 if apart else 1.0])[torch.arange(tokens) // block % 2][:, None, None]
+    k = rand((tokens, Hkv, d), F32, 3)
+    q = rand((n, Hq, d), F32, 4).to(dtype)
+    pool = torch.zeros(nb, slim.kv8_block_bytes(block, Hkv, d), dtype=torch.uint8, device="cuda")
+    slim.slim_kv8_write(k.cuda(), v.cuda(), pool, block, i32(np.arange(tokens)))
+    clean = pool.cpu().numpy()
+    want = ref.attention(to64(q), [0, n], [tokens], np.arange(nb)[None], clean, block, Hkv)
+    bound = ref.attention_bound(want, dtype)
+    for j in list(range(held, tokens - 1, 7)) + [tokens - 1]:
+        bad = clean.copy()
+        ref.parts(bad[j // block], block, Hkv, d)[1][:, j % block, (5 * j) % d] = 127 if j % 2 else 255
+        out = slim.slim_batch_attn_kv8(q.cuda(), i32([0, n]), i32([tokens]), i32([np.arange(nb)]), torch.from_numpy(bad).cuda(), block, Hkv)
+        first = j - held                                 # row i is token held + i
+        within(out[:first], want[0][:first], bound[:first]) if first else None
+        assert torch.isnan(out[first:]).any(-1).all()
+        assert torch.isfinite(out[:first]).all()
+
+
+def test_calls_that_overlap_on_two_streams(slim):
+    """Both streams' queues are filled behind a kernel that runs longer than that takes; every call's bits are those of the same calls one behind the other."""
+    block, Hq, Hkv, d, steps = 32, 8, 2, 128, 6
+    work = []
+    for seed in (1, 2):
+        lens, new = [600 * seed, 40, 2000], [180, 1, 30 * seed]
+        total = [l + m for l, m in zip(lens, new)]
+        nbs = [-(-t // block) for t in total]
+        table = np.full((3, max(nbs)), -1)
+        order, at = np.random.default_rng(seed).permutation(sum(nbs)), 0
+        for r, nb in enumerate(nbs):
+            table[r, :nb], at = order[at:at + nb], at + nb
+        slots = np.concatenate([table[r][np.arange(l, t) // block] * block + np.arange(l, t) % block for r, (l, t) in enumerate(zip(lens, total))])
+        pool = torch.zeros(sum(nbs), slim.kv8_block_bytes(block, Hkv, d), dtype=torch.uint8, device="cuda")
+        slim.slim_kv8_write(rand((sum(nbs) * block, Hkv, d), BF16, seed).cuda(), rand((sum(nbs) * block, Hkv, d), BF16, seed + 5).cuda(), pool, block, i32(np.arange(sum(nbs) * block)))
+        n = sum(new)
+        kvs = [(rand((n, Hkv, d), BF16, 10 * seed + s).cuda(), rand((n, Hkv, d), BF16, 20 * seed + s).cuda()) for s in range(steps)]
+        qs = [rand((n, Hq, d), BF16, 30 * seed + s).cuda() for s in range(steps)]
+        ws = torch.empty(slim.batch_attn_kv8_workspace_bytes(n, 3, Hq, Hkv, d), dtype=torch.uint8, device="cuda")
+        args = (i32(np.concatenate([[0], np.cumsum(new)])), i32(total), i32(table))
+        work.append((pool, i32(slots), kvs, qs, ws, args))
+
+    def step(w, s, out):
+        pool, slots, kvs, qs, ws, args = w
+        slim.slim_kv8_write(*kvs[s], pool, block, slots)
+        slim.slim_batch_attn_kv8(qs[s], *args, pool, block, Hkv, out=out, workspace=ws)
+
+    start = [w[0].clone() for w in work]
+    want = [[torch.zeros_like(w[3][s]) for s in range(steps)] for w in work]
+    for w, outs in zip(work, want):
+        for s in range(steps):
+            step(w, s, outs[s])
+    for w, pool in zip(work, start):
+        w[0].copy_(pool)
+    got = [[torch.zeros_like(w[3][s]) for s in range(steps)] for w in work]
+    torch.cuda.synchronize()
+    streams = [torch.cuda.Stream() for _ in work]
+    for stream in streams:
+        with torch.cuda.stream(stream):
+            torch.cuda._sleep(20_000_000)                # 10 ms at least
+    for s in range(steps):
+        for w, outs, stream in zip(work, got, streams):
+            with torch.cuda.stream(stream):
+                step(w, s, outs[s])
+    torch.cuda.synchronize()
+    for a, b in zip(want, got):
+        for s in range(steps):
+            assert torch.equal(a[s], b[s]) and torch.isfinite(a[s]).all()
