@@ -66,7 +66,7 @@ __device__ __forceinline__ uint32_t kv8_codes(const float* f, float power) {
 // its rows stay in registers, up to kKv8Keep passes of them, and the next head's are on their way.  Shorter ones, the new tokens of a step, are a wave's, for as many heads as it has
 // rows' lanes for (64 / (D / 8)).  Rows, old exponent and the run's length are requested together: two trips to memory.
 // Bound by memory where there are many rows: 26381 of 24 prompts, 8 heads of 128, 161 MB, 41 us, 3.9 TB/s (a copy of as much takes 32); by the trips where there are few: 256 new tokens
-// 6.3 us, 3 us of which a launch costs.
+// 5.4 us, 3 us of which a launch costs, and 10.4 where they raise their blocks' exponents.
 constexpr int kKv8Keep = 4, kKv8Short = 8;
 struct Kv8Write {
     const int* row_slot;
@@ -741,8 +741,8 @@ __global__ void __launch_bounds__(64 * NW, sizeof(T) == 2 && NR == 1 ? 3 : 2) ba
 //   bfloat16 with their powers, the reference the running maximum.  One buffer, filled and read in turn: 358 us for a call of 1511 queries behind 9856 tokens where the other loop takes 240.
 // Bound by the matrix units at the clock that the chip's power leaves them, and by the arithmetic beside them: 1511 queries behind 9856 tokens, 28 heads over 4 of 128, 230 GFLOP in 250 us
 // by themselves and 280 to 290 one call behind the other, 0.92 and 0.8 PFLOP/s, where a library product of 8192^3 reaches 1.37 and matrix instructions alone 1.75; the matrix units are
-// busy half of the time.  With weights of one bfloat16 4 to 10 us less, but an error of 2.4 10^-3 from 64 bits where rounding the output leaves 1.7.  Without the exponentials 57 us less,
-// without LDS 39: no one of them bounds it alone.  16 rows a wave 484 us; 64 rows a wave, with all 512 registers, as 32.
+// busy half of the time.  Weights of one bfloat16 took 243 us of an earlier form's 247, with an error of 2.4 10^-3 from 64 bits where rounding the output leaves 1.7.  That form
+// without the exponentials took 57 us less, without LDS 39: no one of them bounds it alone.  16 rows a wave 484 us; 64 rows a wave, with all 512 registers, as 32.
 constexpr int kManyKeys = 64;
 template <int D> struct ManyTile {
     // Rows of D 16-bit numbers and 16 bytes (Keys: 16 keys' same piece of 16 bytes) or 64 (Values: four keys' same 64 bytes) cover all banks once, and every address of a lane is one base and a constant.
