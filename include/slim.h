@@ -512,7 +512,8 @@ int slim_decode_layer_kv4(const slim_layer_shape* s, const slim_layer_weights* w
  *     Scores, sums and results are float32 until the output is rounded (the sum of the Values with a weight of 1 for the largest: above 3 10^38 it is infinite).  bfloat16: the weights enter the
  *     product with the Values as two bfloat16 terms, off by 2^-17 of a weight, or, for requests of many rows (n * Hq/Hkv above 64, in a batch whose rows leave room for them: n_rows * Hq/Hkv
  *     above 16 * R, or (n_rows - R) * Hq/Hkv above 512), as one float16 where the exponents e of the Values that are taken together lie in [-64, 64] and within 12 of each other (elsewhere as two
- *     terms, which takes half as long again): off by 2^-11 of a weight, or by 2^-34 of the row's largest where that is more.  Either way 1.7 10^-3 of the results' size from 64 bits, nearly all of
+ *     terms, which takes half as long again): off by 2^-11 of a weight, or by 2^-34 of the row's largest where that is more (and as two terms after all, in a second pass, where this may be
+ *     more than 2^-10 of a row's largest result).  Either way 1.7 10^-3 of the results' size from 64 bits, nearly all of
  *     it the output's rounding.  float32: three terms, 2 to 5 10^-7.  (A token that a query does not see, in a block that it does, can decide by the block's e in which of the two ways its
  *     weights are rounded.)
  *     The order of the sums follows from the batch's lengths, and so a token's result can differ in its last places with the requests beside it; the same call gives the same bits.

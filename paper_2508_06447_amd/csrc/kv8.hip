@@ -735,20 +735,21 @@ __global__ void __launch_bounds__(64 * NW, sizeof(T) == 2 && NR == 1 ? 3 : 2) ba
 //   Where the exponents e of the Values' blocks that a workgroup's part of a tile meets lie within kManySpan of each other (nearly always): a weight is rounded to one float16, a Value is
 //   code * 2^(e - largest e + kManyShift) in float16, exact (with kManySpan 12 and kManyShift 7 from 2^-14, the smallest normal one, to 57344), and the results are multiplied by the power
 //   that is left.  The reference of a row is a whole number, 10 below its largest score when it was set, and is set anew, by a power of two, only when a score is more than 15 above it: nothing
-//   is rescaled in nearly all phases.  Weights from 2^-14 on, 2^-23 of the row's largest at least, are off by 2^-11 of themselves, smaller ones by 2^-25, 2^-34 of the largest: so a result is
+//   is rescaled in nearly all phases.  Weights from 2^-14 on (2^-23 of the row's largest or less) are off by 2^-11 of themselves, smaller ones by 2^-25 (2^-34 of the largest): so a result is
 //   off by 2^-11 of sum p |v| and 2^-34 of sum |v|.
 //   Where they are further apart, that last sum may be anything beside the first, and a weight has to keep its places however small it is: two bfloat16 terms (2^-17 of itself), Values as
-//   bfloat16 with their powers, the reference the running maximum.  One buffer, filled and read in turn: 358 us for a call of 1511 queries behind 9856 tokens where the other loop takes 240.
-// Bound by the matrix units at the clock that the chip's power leaves them, and by the arithmetic beside them: 1511 queries behind 9856 tokens, 28 heads over 4 of 128, 230 GFLOP in 250 us
+//   bfloat16 with their powers, the reference the running maximum.  So too, in a second pass over the same keys, where at the end of the first loop the last sum can be more than 2^-10 of a row's
+//   largest result (one key takes nearly everything and has Values of next to nothing).  One buffer, filled and read in turn: 358 us for a call of 1511 queries behind 9856 tokens where the other loop takes 240 to 250.
+// Bound by issue: 1511 queries behind 9856 tokens, 28 heads over 4 of 128, 230 GFLOP in 250 us
 // by themselves and 280 to 290 one call behind the other, 0.92 and 0.8 PFLOP/s, where a library product of 8192^3 reaches 1.37 and matrix instructions alone 1.75; the matrix units are
-// busy half of the time.  Weights of one bfloat16 took 243 us of an earlier form's 247, with an error of 2.4 10^-3 from 64 bits where rounding the output leaves 1.7.  That form
+// busy half of the time, and beside 16 of their instructions a wave has some 105 others of the vector ALU and 28 of LDS, which its SIMD's two waves do not hide altogether.  Weights of one bfloat16 took 243 us of an earlier form's 247, with an error of 2.4 10^-3 from 64 bits where rounding the output leaves 1.7.  That form
 // without the exponentials took 57 us less, without LDS 39: no one of them bounds it alone.  16 rows a wave 484 us; 64 rows a wave, with all 512 registers, as 32.
 constexpr int kManyKeys = 64;
 template <int D> struct ManyTile {
     // Rows of D 16-bit numbers and 16 bytes (Keys: 16 keys' same piece of 16 bytes) or 64 (Values: four keys' same 64 bytes) cover all banks once, and every address of a lane is one base and a constant.
     static constexpr int kRowK = D * 2 + 16, kRowV = D * 2 + 64, kSide = kManyKeys * kRowK, kBuffer = kSide + kManyKeys * kRowV;      // a key; the Keys; both
-    static constexpr int kFlags = 4 * kBuffer, kSpans = kFlags + 32, kLists = kSpans + 32, kLdsBytes = kLists + 8 * 64 * 16;      // four; a bit for each of their keys with a Value that is not a
-                                                                                                                          // number; the exponents that the waves have met; a wave's pieces
+    static constexpr int kFlags = 4 * kBuffer, kSpans = kFlags + 32, kLost = kSpans + 32, kLists = kLost + 32, kLdsBytes = kLists + 8 * 64 * 16;      // four; a bit for each of their keys with a
+                                                               // Value that is not a number; the exponents that the waves have met, and whether they have a row that float16 is not enough for; a wave's pieces
     static constexpr int KS = D / 16, DT = D / 32;
 };
 constexpr float kManyAbove = 10.f, kManyRoom = 15.f;     // where the largest weight begins, and how far it may grow: 2^10, 2^15
@@ -822,13 +823,22 @@ __global__ void __launch_bounds__(512, 2) batch_attn_many_kernel(const bf16_t* _
 
         // The pieces, looked up 64 at once by every wave for itself, one a lane; those with keys are listed in LDS: where the Keys begin, exponents | rows << 16 | 1 << 24 if there are 16 which all
         // rows of the tile see, position.  Four make 64 keys; the list is filled up with pieces without rows.  Slots are requested two lookups ahead, exponents one.
-        int u = u_begin + lane, batch = u_begin - 64;
+        int u, batch;
         auto slot_at = [&](int u) { return u < u_end ? table[a.by_piece(u)] : -1; };
         auto exponents_at = [&](int slot) {
             return slot >= 0 && slot < a.n_slots ? *reinterpret_cast<const uint16_t*>(a.pool + (size_t)slot * a.slot_bytes + a.layer_offset + head.e) : (uint16_t)0;
         };
-        int slot_1 = slot_at(u), slot_2 = slot_at(u + 64);
-        uint32_t e_1 = exponents_at(slot_1);
+        int slot_1, slot_2, at_list, n_list;             // (lists in fours)
+        uint32_t e_1;
+        auto begin_pieces = [&]() {
+            u = u_begin + lane;
+            batch = u_begin - 64;
+            slot_1 = slot_at(u);
+            slot_2 = slot_at(u + 64);
+            e_1 = exponents_at(slot_1);
+            at_list = n_list = 0;
+        };
+        begin_pieces();
         // The Values' exponents of all blocks in the tile's part, a block a lane, all waves together: the largest, and how far the smallest lies below it.
         typedef unsigned short u16x2 __attribute__((ext_vector_type(2)));
         int e_top, e_low;                                // + 127
@@ -854,10 +864,9 @@ __global__ void __launch_bounds__(512, 2) batch_attn_many_kernel(const bf16_t* _
             e_low = both == 0 ? 127 : 255 - (both >> 16 & 0xffff);
         }
         const bool apart = e_top - e_low > kManySpan || e_top > 127 + kManyFar || e_low < 127 - kManyFar;
-        const int e_shift = apart ? 0 : 127 - e_top + kManyShift;                                      // added to a Value's exponent when it becomes a number
-        const float left_power = kv8_power((uint32_t)(127 - e_shift));                                 // and what a result is multiplied by for it
+        int e_shift = apart ? 0 : 127 - e_top + kManyShift;                                            // added to a Value's exponent when it becomes a number
+        float left_power = kv8_power((uint32_t)(127 - e_shift));                                       // and what a result is multiplied by for it
         uint4* list = reinterpret_cast<uint4*>(lds + Tile::kLists) + wave * 64;
-        int at_list = 0, n_list = 0;                     // in fours
         auto advance = [&]() {                           // to the next four; false: there are none, and the last ones stay
             if (at_list + 1 < n_list) {
                 ++at_list;
@@ -935,11 +944,13 @@ __global__ void __launch_bounds__(512, 2) batch_attn_many_kernel(const bf16_t* _
             if (mine) *(LdsB128)((part < 2 ? fill_k : fill_v) + buffer * Tile::kBuffer + part % 2 * 16) = x;
         };
 
-        const bool any = advance();
-        if (any) {
+        auto first_keys = [&]() {
+            if (!advance()) return false;
             read_list();
             load();
-        }
+            return true;
+        };
+        const bool any = first_keys();
         // Query fragments: the lane's row, channels 16 c + 8 h ..
         const int lrow = row0 + min(wave * 32 + l32, rows - 1), token = a.by_group(lrow), my_pos = before + token;
         const bf16_t* q_row = q + (size_t)(me.lo + token) * a.ldq + (size_t)(g * G + lrow - token * G) * D + h * 8;
@@ -947,12 +958,17 @@ __global__ void __launch_bounds__(512, 2) batch_attn_many_kernel(const bf16_t* _
 #pragma unroll
         for (int c = 0; c < KS; ++c) qf[c] = *reinterpret_cast<const bf16x8*>(q_row + c * 16);
         f32x16 o[DT];
+        // of row l32: reference in the base-2 domain, weights' exponent that it moves above (-inf: not set yet; in the loop of two terms the largest score itself), the lane's share of the sum
+        float mc, lim, l;
+        auto begin_rows = [&]() {
 #pragma unroll
-        for (int d = 0; d < DT; ++d)
+            for (int d = 0; d < DT; ++d)
 #pragma unroll
-            for (int i = 0; i < 16; ++i) o[d][i] = 0.f;
-        // of row l32: reference in the base-2 domain, weights' exponent that it moves above (-inf: not set yet; where exponents are far apart the largest score itself), the lane's share of the sum
-        float mc = 0.f, lim = -INFINITY, l = 0.f;
+                for (int i = 0; i < 16; ++i) o[d][i] = 0.f;
+            mc = l = 0.f;
+            lim = -INFINITY;
+        };
+        begin_rows();
         // Addresses of the lane in a buffer: K fragments (key l32, channels 16 c + 8 h: pieces 2 c + h), V fragments (keys 16 m + 4 h + .., channels 32 d + ..).
         const unsigned k_from = lds0 + l32 * Tile::kRowK + h * 16;
         const unsigned v_from = lds0 + Tile::kSide + (4 * h + (lane >> 2 & 3)) * Tile::kRowV + (lane >> 4 & 1) * 32 + (lane & 3) * 8;
@@ -1061,54 +1077,7 @@ __global__ void __launch_bounds__(512, 2) batch_attn_many_kernel(const bf16_t* _
 
         constexpr std::false_type as_f16;
         constexpr std::true_type as_bf16;
-        const int loop = __builtin_amdgcn_readfirstlane(!any ? 0 : apart ? 2 : 1);
-        if (loop == 2) {
-            for (bool next = true; next;) {
-                const uint2 info = info_new;
-                const bool whole = all_full(info);
-                if (!whole) clear_odd(0);
-#pragma unroll
-                for (int i = 0; i < 4; ++i) fill_part(0, i, as_bf16);
-                next = advance();
-                read_list();
-                load();
-                __syncthreads();
-#pragma unroll 1
-                for (int y = 0; y < 2; ++y) {
-#pragma unroll
-                    for (int c = 0; c < KS; ++c) read_k(0, y, c);
-#pragma unroll
-                    for (int c = 0; c < KS; ++c) score(0, c);
-                    if (!whole) hide(s[0], y, info, 0);
-                    float mx = largest_of(0);
-                    mx = fmaxf(mx, __shfl_xor(mx, 32, 64));
-                    if (__any(mx > lim)) {
-                        const float now = fmaxf(mx, lim), to = now == -INFINITY ? 0.f : now * a.scale_log2e, al = lim == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(mc - to);
-                        lim = now;
-                        mc = to;
-                        l *= al;
-#pragma unroll
-                        for (int d = 0; d < DT; ++d) o[d] *= al;
-                    }
-#pragma unroll
-                    for (int m = 0; m < 2; ++m) {
-                        float w[8];
-#pragma unroll
-                        for (int i = 0; i < 8; ++i) w[i] = __builtin_amdgcn_exp2f(top_of(s[0][8 * m + i]));
-                        l += ((w[0] + w[1]) + (w[2] + w[3])) + ((w[4] + w[5]) + (w[6] + w[7]));
-                        bf16x8 terms[2];
-                        bf16_terms<2>(w, terms);
-#pragma unroll
-                        for (int d = 0; d < DT; ++d) {
-                            read_v(0, y, d, m);
-#pragma unroll
-                            for (int t = 1; t >= 0; --t) o[d] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, vf[d][m]), terms[t], o[d], 0, 0, 0);
-                        }
-                    }
-                }
-                __syncthreads();
-            }
-        }
+        int loop = __builtin_amdgcn_readfirstlane(!any ? 0 : apart ? 2 : 1);
         if (loop == 1) {
             // Two tiles of 64 keys in LDS, a third in registers, on its way.  Turn i reads the Values of tiles i - 1 and i and the Keys of i + 1, and fills the buffer of i + 2, which is that of
             // i - 2: turn i - 1 was the last to read it, turn i + 1 is the first to read what it gets.  So one barrier, at a turn's end, keeps both apart.
@@ -1182,6 +1151,75 @@ __global__ void __launch_bounds__(512, 2) batch_attn_many_kernel(const bf16_t* _
             for (int i = 0; i < 2 * DT; ++i) read_v(buffer, 1, i % DT, i / DT);
 #pragma unroll
             for (int i = 0; i < 2 * DT; ++i) value(1, i / DT, i % DT);
+            // What small weights have lost is 2^-25 times the sum of the Values, 2^16 each, at most: where that is more than 2^-10 of a row's largest result, once more in two terms.
+            float most = 0.f;
+#pragma unroll
+            for (int d = 0; d < DT; ++d)
+#pragma unroll
+                for (int i = 0; i < 16; ++i) most = fmaxf(most, fabsf(o[d][i]));
+            most = fmaxf(most, __shfl_xor(most, 32, 64));
+            const unsigned long long lost = __ballot(lim != -INFINITY && most < (float)(u_end - u_begin) * (kPiece * 2.f));
+            uint32_t* flags = reinterpret_cast<uint32_t*>(lds + Tile::kLost);
+            if (lane == 0) flags[wave] = lost != 0;
+            __syncthreads();
+            uint32_t any_lost = 0;
+#pragma unroll
+            for (int i = 0; i < 8; ++i) any_lost |= flags[i];
+            if (__builtin_amdgcn_readfirstlane(any_lost)) {
+                loop = 2;
+                e_shift = 0;
+                left_power = 1.f;
+                begin_pieces();
+                first_keys();
+                begin_rows();
+            }
+        }
+        if (loop == 2) {
+            for (bool next = true; next;) {
+                const uint2 info = info_new;
+                const bool whole = all_full(info);
+                if (!whole) clear_odd(0);
+#pragma unroll
+                for (int i = 0; i < 4; ++i) fill_part(0, i, as_bf16);
+                next = advance();
+                read_list();
+                load();
+                __syncthreads();
+#pragma unroll 1
+                for (int y = 0; y < 2; ++y) {
+#pragma unroll
+                    for (int c = 0; c < KS; ++c) read_k(0, y, c);
+#pragma unroll
+                    for (int c = 0; c < KS; ++c) score(0, c);
+                    if (!whole) hide(s[0], y, info, 0);
+                    float mx = largest_of(0);
+                    mx = fmaxf(mx, __shfl_xor(mx, 32, 64));
+                    if (__any(mx > lim)) {
+                        const float now = fmaxf(mx, lim), to = now == -INFINITY ? 0.f : now * a.scale_log2e, al = lim == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(mc - to);
+                        lim = now;
+                        mc = to;
+                        l *= al;
+#pragma unroll
+                        for (int d = 0; d < DT; ++d) o[d] *= al;
+                    }
+#pragma unroll
+                    for (int m = 0; m < 2; ++m) {
+                        float w[8];
+#pragma unroll
+                        for (int i = 0; i < 8; ++i) w[i] = __builtin_amdgcn_exp2f(top_of(s[0][8 * m + i]));
+                        l += ((w[0] + w[1]) + (w[2] + w[3])) + ((w[4] + w[5]) + (w[6] + w[7]));
+                        bf16x8 terms[2];
+                        bf16_terms<2>(w, terms);
+#pragma unroll
+                        for (int d = 0; d < DT; ++d) {
+                            read_v(0, y, d, m);
+#pragma unroll
+                            for (int t = 1; t >= 0; --t) o[d] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, vf[d][m]), terms[t], o[d], 0, 0, 0);
+                        }
+                    }
+                }
+                __syncthreads();
+            }
         }
         __syncthreads();                                 // the buffers are read before they are written again
 
