@@ -183,14 +183,15 @@ def test_calls_that_overlap_on_two_streams(slim):
 
 @pytest.mark.parametrize("n,d,dtype", MANY)
 @pytest.mark.parametrize("tokens", [640, 2500])
+@pytest.mark.parametrize("at", [5, 333, 470])
 @pytest.mark.parametrize("places", [20.4, 24.4, 28.4, 32.4, 40.4, 70.4])
-def test_a_key_that_takes_nearly_everything_and_has_no_value(slim, n, d, dtype, tokens, places):
+def test_a_key_that_takes_nearly_everything_and_has_no_value(slim, n, d, dtype, tokens, places, at):
     """One key `places` binary places above the others, its Values zeros: the result is of the others alone, whose weights are far below a float16's beside it."""
     block, Hq, Hkv = 64, 8, 2
     v = rand((tokens, Hkv, d), F32, int(places)) * 0.2 + 1.0
-    v[5] = 0.0
+    v[at] = 0.0
     k = torch.zeros(tokens, Hkv, d)
-    k[5, :, 0] = 1.0
+    k[at, :, 0] = 1.0
     q = torch.zeros(n, Hq, d)
     q[:, :, 0] = places * math.log(2) * math.sqrt(d)
     q = q.to(dtype)
